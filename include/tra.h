@@ -275,6 +275,88 @@ int tra_hot_path_host(tra_plan_t* plan, const void* Q_host, const void* K_host, 
                       void* O_host, void* workspace, size_t workspace_bytes, int heads, int group,
                       int first_group, float sm_scale, void* stream);
 
+/* ---- head norm, rotary positions and token order, before the attention and back (the paper starts from the
+ * Q, K and V its models hand to the attention; this is the step that makes them) ------------ */
+
+/* One call turns the projections' Q, K and V into what the attention calls take, and one call takes the
+ * gradients back.  A row is one (token, head), d = head_dim channels x.
+ *   norm    : n = x (TRA_NORM_NONE), x r (TRA_NORM_RMS) or (x - mean) r (TRA_NORM_LAYER) with
+ *             r = (mean square [of x, or of x - mean] + eps)^-1/2 over the d channels; z = weight n + bias,
+ *             weight and bias [d], shared by all heads, of the tensors' type (NULL = 1 and 0; bias with
+ *             TRA_NORM_LAYER only).
+ *   rotary  : d / 2 channel pairs, pair p = channels (2p, 2p + 1), or (p, p + d/2) with `halves`; pair p belongs to
+ *             axis axis[p] and turns by the angle pos[axis[p]] * inv_freq[p]:
+ *             (z1, z2) -> (z1 cos - z2 sin, z1 sin + z2 cos).  inv_freq[p] = 0 leaves a pair as it is.
+ *             Angles are reduced exactly for every int32 position.
+ *   order   : see TRA_ROTARY_TILE_MAJOR.
+ * All arithmetic is fp32 and rounded once, to the tensors' type. */
+#define TRA_ROTARY_MAX_HEAD_DIM 256
+
+/* types of the tensors of the rotary and packed-attention calls */
+#define TRA_BF16 0
+#define TRA_FP16 1
+#define TRA_FP32 2
+
+#define TRA_NORM_NONE 0
+#define TRA_NORM_RMS 1
+#define TRA_NORM_LAYER 2
+
+typedef struct tra_rotary tra_rotary_t; /* opaque, host memory only: frequencies, axes, norm */
+
+typedef struct {
+  int head_dim;           /* d: a multiple of 16, 16 .. 256                               */
+  int n_axes;             /* 1 .. 4                                                       */
+  const int* axis;        /* HOST [d / 2]: 0 .. n_axes - 1                                */
+  const double* inv_freq; /* HOST [d / 2]: radians per position, finite                   */
+  int halves;             /* how channels pair: 0 = (2p, 2p + 1), 1 = (p, p + d/2)        */
+  int norm;               /* TRA_NORM_*                                                   */
+  double eps;             /* of the norm, >= 0                                            */
+} tra_rotary_config_t;
+
+#define TRA_ROTARY_ROTATE 1u     /* norm and rotate (Q, K); without it the rows are only moved (V)              */
+#define TRA_ROTARY_TILE_MAJOR 2u /* the attention side (dst of the forward call, src of the backward call) is in */
+                                 /* the plan's tile-major order; the other side is in raster order               */
+
+typedef struct {           /* one tensor of a call: [B, tokens, heads, d] behind strides, channels contiguous */
+  const void* src;         /* forward: x.  backward: the gradient of the forward's dst              */
+  void* dst;               /* forward: y.  backward: the gradient of the forward's src              */
+  const void* x;           /* backward with a norm: the forward's src (NULL otherwise)              */
+  const void* weight;      /* [d] or NULL                                                          */
+  const void* bias;        /* [d] or NULL (read by the forward call only)                          */
+  float* weight_grad;      /* backward with a norm: fp32 [d] (written) or NULL                     */
+  float* bias_grad;        /* backward with TRA_NORM_LAYER: fp32 [d] (written) or NULL             */
+  int64_t src_stride[3];   /* batch, token, head, in elements; multiples of 16 bytes               */
+  int64_t dst_stride[3];
+  int64_t x_stride[3];
+  int heads;
+  unsigned flags;          /* TRA_ROTARY_ROTATE | TRA_ROTARY_TILE_MAJOR                            */
+} tra_rotary_tensor_t;
+
+int tra_rotary_create(tra_rotary_t** out, const tra_rotary_config_t* cfg);
+int tra_rotary_destroy(tra_rotary_t* rot);
+
+/* Up to three tensors (HOST array), one launch.
+ *   plan : NULL, or the grid: tokens must then be its S (video tokens in raster order, then text).  Needed for
+ *          TRA_ROTARY_TILE_MAJOR and for positions from the grid.  Its device must be the current one.
+ *   pos  : int32 [tokens, n_axes], the position of every token in the order of the projection side, shared by the
+ *          batch entries; or NULL: video token (t*H + y)*W + x of the plan has position (t, y, x) (n_axes = 3) and
+ *          text tokens are normed and not turned.
+ * Pointers 16-byte aligned.  src and dst must not overlap, except that a tensor that is not TILE_MAJOR may be worked
+ * on in place (dst = src with the same strides).
+ * Errors: TRA_ERR_INVALID_ARG, TRA_ERR_UNSUPPORTED, TRA_ERR_CUDA. */
+int tra_rotary_forward(const tra_rotary_t* rot, const tra_plan_t* plan, const int32_t* pos,
+                       const tra_rotary_tensor_t* tensors, int n_tensors, int B, int tokens, int dtype,
+                       void* stream);
+
+/* The gradients.  weight_grad = sum over rows of u n, bias_grad = sum of u, u = the gradient turned back: summed in
+ * fp32 in a fixed order (the same bits every time) through `workspace`, device memory of at least
+ * tra_rotary_backward_workspace_bytes, 16-byte aligned, owned by the caller and free to reuse once `stream` has passed the call
+ * (NULL when no weight_grad or bias_grad is asked for; TRA_ERR_CAPACITY when it is too small). */
+size_t tra_rotary_backward_workspace_bytes(const tra_rotary_t* rot);
+int tra_rotary_backward(const tra_rotary_t* rot, const tra_plan_t* plan, const int32_t* pos,
+                        const tra_rotary_tensor_t* tensors, int n_tensors, int B, int tokens, int dtype,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

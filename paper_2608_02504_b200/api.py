@@ -25,6 +25,9 @@ TRA_RADII_EXTENDED = 0
 TRA_RADII_LITERAL = 1
 TRA_BUDGET_UNIFORM = 0
 TRA_BUDGET_LOGNORMAL = 1
+TRA_BF16, TRA_FP16, TRA_FP32 = 0, 1, 2
+TRA_NORM_NONE, TRA_NORM_RMS, TRA_NORM_LAYER = 0, 1, 2
+TRA_ROTARY_ROTATE, TRA_ROTARY_TILE_MAJOR = 1, 2
 
 EXPORTS = [
     "tra_plan_create", "tra_plan_destroy", "tra_plan_num_tokens", "tra_plan_num_video_tokens", "tra_plan_num_blocks",
@@ -33,6 +36,8 @@ EXPORTS = [
     "tra_entropy_attn", "tra_budget_radius", "tra_build_block_mask", "tra_sparse_attn",
     "tra_build_block_list_static",
     "tra_hot_path_host_workspace_bytes", "tra_hot_path_host",
+    "tra_rotary_create", "tra_rotary_destroy", "tra_rotary_forward", "tra_rotary_backward_workspace_bytes",
+    "tra_rotary_backward",
 ]
 
 
@@ -45,6 +50,23 @@ class tra_config_t(ctypes.Structure):
         ("radii", ctypes.POINTER(ctypes.c_double)), ("n_radii", ctypes.c_int),
         ("radius_policy", ctypes.c_int), ("flags", ctypes.c_uint), ("budget_map", ctypes.c_int),
         ("n_text", ctypes.c_int),
+    ]
+
+
+class tra_rotary_config_t(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int), ("n_axes", ctypes.c_int), ("axis", ctypes.POINTER(ctypes.c_int)),
+        ("inv_freq", ctypes.POINTER(ctypes.c_double)), ("halves", ctypes.c_int), ("norm", ctypes.c_int),
+        ("eps", ctypes.c_double),
+    ]
+
+
+class tra_rotary_tensor_t(ctypes.Structure):
+    _fields_ = [
+        ("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("x", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p), ("weight_grad", ctypes.c_void_p), ("bias_grad", ctypes.c_void_p),
+        ("src_stride", ctypes.c_int64 * 3), ("dst_stride", ctypes.c_int64 * 3), ("x_stride", ctypes.c_int64 * 3),
+        ("heads", ctypes.c_int), ("flags", ctypes.c_uint),
     ]
 
 
@@ -76,6 +98,12 @@ def _load():
     lib.tra_build_block_mask.argtypes = [vp, vp, vp, vp, vp, ctypes.c_int64, vp, vp, i32, i32, vp]
     lib.tra_sparse_attn.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, vp]
     lib.tra_build_block_list_static.argtypes = [vp, vp, vp, vp, ctypes.c_int64, vp, vp, i32, i32, vp]
+    lib.tra_rotary_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(tra_rotary_config_t)]
+    lib.tra_rotary_destroy.argtypes = [vp]
+    lib.tra_rotary_forward.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp]
+    lib.tra_rotary_backward_workspace_bytes.argtypes = [vp]
+    lib.tra_rotary_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.tra_rotary_backward.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, ctypes.c_size_t, vp]
     return lib
 
 
@@ -374,3 +402,189 @@ class HostPipeline:
                                       self.group, self.first_group, self.scale,
                                       _stream(torch.cuda.current_stream(self.dev))), "tra_hot_path_host")
         return self.n_groups * self.launches_per_group
+
+
+_DTYPES = {torch.bfloat16: TRA_BF16, torch.float16: TRA_FP16, torch.float32: TRA_FP32}
+
+
+class Rotary:
+    """Head norm, rotary positions with several axes, and token order: what Q, K and V go through between a
+    layer's projections and its attention, in one pass, and its gradients (``tra_rotary_forward`` / ``_backward``).
+
+    ``axis_dims``: channels of each axis, e.g. (44, 42, 42) for (time, height, width) of 128 channels; pair k of
+    an axis with c channels turns by ``scale[axis] * theta ** (-2 k / c)`` radians per position.  Any other
+    layout of frequencies: pass ``axis`` and ``inv_freq``, one entry per channel pair, instead.
+    ``halves``: channels p and p + d/2 form a pair (default: 2p and 2p + 1).
+    ``norm``: None, "rms" or "layer", over the channels of every head.
+    """
+
+    def __init__(self, head_dim, axis_dims=None, theta=10000.0, scale=None, axis=None, inv_freq=None, halves=False,
+                 norm=None, eps=1e-6):
+        if norm not in (None, "rms", "layer"):
+            raise ValueError("norm: expected None, 'rms' or 'layer'")
+        if (axis_dims is None) == (axis is None or inv_freq is None) or (axis is None) != (inv_freq is None):
+            raise ValueError("expected either axis_dims, or axis and inv_freq")
+        if axis_dims is not None:
+            if any(c < 0 or c % 2 for c in axis_dims) or sum(axis_dims) != head_dim:
+                raise ValueError("axis_dims: expected even numbers of channels that add up to head_dim")
+            scale = [1.0] * len(axis_dims) if scale is None else list(scale)
+            if len(scale) != len(axis_dims):
+                raise ValueError("scale: expected one factor per axis")
+            axis = [a for a, c in enumerate(axis_dims) for _ in range(c // 2)]
+            inv_freq = [scale[a] * theta ** (-2.0 * k / c) for a, c in enumerate(axis_dims) for k in range(c // 2)]
+            n_axes = len(axis_dims)
+        else:
+            if scale is not None:
+                raise ValueError("scale: goes with axis_dims")
+            axis, inv_freq = [int(a) for a in axis], [float(f) for f in inv_freq]
+            if len(axis) != len(inv_freq) or 2 * len(axis) != head_dim:
+                raise ValueError("axis, inv_freq: expected head_dim / 2 entries")
+            n_axes = max(axis) + 1 if axis else 0
+        cfg = tra_rotary_config_t()
+        cfg.head_dim, cfg.n_axes, cfg.halves, cfg.eps = head_dim, n_axes, int(halves), eps
+        cfg.axis = (ctypes.c_int * len(axis))(*axis)
+        cfg.inv_freq = (ctypes.c_double * len(inv_freq))(*inv_freq)
+        cfg.norm = {None: TRA_NORM_NONE, "rms": TRA_NORM_RMS, "layer": TRA_NORM_LAYER}[norm]
+        self._h = ctypes.c_void_p()
+        _check(_lib.tra_rotary_create(ctypes.byref(self._h), ctypes.byref(cfg)), "tra_rotary_create")
+        self.head_dim, self.n_axes, self.norm = head_dim, n_axes, norm
+        self.workspace_bytes = int(_lib.tra_rotary_backward_workspace_bytes(self._h))
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            _lib.tra_rotary_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # -- argument marshalling -----------------------------------------------------------------
+    @staticmethod
+    def _tile_major(plan, name):
+        """Which tensors the plan's attention calls take in tile-major order."""
+        if plan is None or plan.flags & TRA_ORDER_RASTER:
+            return False
+        return name != "q" or not plan.flags & TRA_ORDER_RASTER_QO
+
+    def _param(self, t, name, like):
+        if t is None:
+            return None
+        if t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != (self.head_dim,) or \
+                not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous [head_dim] tensor of the tensors' type and device")
+        return t.data_ptr()
+
+    def _strides(self, t, name, like, shape, heads_first):
+        """Strides (batch, token, head) of a tensor [B, tokens, heads, d] or, heads first, [B, heads, tokens, d]."""
+        if not t.is_cuda or t.device != like.device or t.dtype != like.dtype or tuple(t.shape) != shape or \
+                (t.stride(3) != 1 and t.shape[3] > 1):
+            raise ValueError(f"{name}: expected a CUDA tensor of shape {shape}, type {like.dtype}, on {like.device}, "
+                             "with contiguous channels")
+        s = t.stride()
+        return (s[0], s[2], s[1]) if heads_first else (s[0], s[1], s[2])
+
+    def _begin(self, first, plan, pos, heads_first):
+        if first.dim() != 4 or first.shape[3] != self.head_dim or first.dtype not in _DTYPES or not first.is_cuda:
+            raise ValueError("expected CUDA tensors [B, tokens, heads, head_dim] "
+                             "([B, heads, tokens, head_dim] on the attention side of a plan), bf16, fp16 or fp32")
+        if first.device.index != torch.cuda.current_device():
+            raise ValueError("the tensors' device must be the current one")
+        B, tokens = first.shape[0], first.shape[2 if heads_first else 1]
+        if plan is not None and tokens != plan.N:
+            raise ValueError(f"expected {plan.N} tokens, the plan's")
+        if plan is None and pos is None:
+            raise ValueError("expected a plan or pos")
+        pos_ptr = None
+        if pos is not None:
+            if not pos.is_cuda or pos.device != first.device or pos.dtype != torch.int32 or \
+                    tuple(pos.shape) != (tokens, self.n_axes) or not pos.is_contiguous():
+                raise ValueError("pos: expected a contiguous int32 CUDA tensor [tokens, n_axes]")
+            pos_ptr = pos.data_ptr()
+        return B, tokens, pos_ptr
+
+    def forward(self, q, k=None, v=None, *, plan=None, pos=None, q_weight=None, k_weight=None, q_bias=None, k_bias=None,
+                out=None):
+        """Projections q, k, v [B, tokens, heads, d] (any strides with contiguous channels, e.g. slices of a fused
+        projection; k and v may be None) -> (q', k', v').
+
+        With ``plan`` the tokens are its raster-order sequence, positions come from its grid (unless ``pos`` is
+        given) and the outputs are [B, heads, tokens, d] in the order its attention calls take; without it,
+        ``pos`` int32 [tokens, n_axes] names every token's position and outputs keep the inputs' layout.
+        V is only moved: without a plan it comes back as a copy.  ``out``: output tensors instead of new ones."""
+        tensors = [("q", q, q_weight, q_bias), ("k", k, k_weight, k_bias), ("v", v, None, None)]
+        if k is None and (k_weight is not None or k_bias is not None):
+            raise ValueError("k_weight, k_bias: given without k")
+        B, tokens, pos_ptr = self._begin(q, plan, pos, False)
+        on_plan = plan is not None
+        args, outs, n = (tra_rotary_tensor_t * 3)(), [], 0
+        for i, (name, x, w, b) in enumerate(tensors):
+            if x is None:
+                outs.append(None)
+                continue
+            heads = x.shape[2] if x.dim() == 4 else 0
+            src = self._strides(x, name, q, (B, tokens, heads, self.head_dim), False)
+            y = out[i] if out is not None else None
+            shape = (B, heads, tokens, self.head_dim) if on_plan else (B, tokens, heads, self.head_dim)
+            if y is None:
+                y = torch.empty(shape, dtype=x.dtype, device=x.device)
+            a = args[n]
+            a.src, a.dst = x.data_ptr(), y.data_ptr()
+            a.src_stride[:], a.dst_stride[:] = src, self._strides(y, "out " + name, q, shape, on_plan)
+            a.weight, a.bias = self._param(w, name + "_weight", q), self._param(b, name + "_bias", q)
+            a.heads = heads
+            a.flags = (TRA_ROTARY_ROTATE if name != "v" else 0) | \
+                (TRA_ROTARY_TILE_MAJOR if self._tile_major(plan, name) else 0)
+            outs.append(y)
+            n += 1
+        _check(_lib.tra_rotary_forward(self._h, plan._h if on_plan else None, pos_ptr, ctypes.byref(args), n, B, tokens,
+                                       _DTYPES[q.dtype], _stream()), "tra_rotary_forward")
+        return tuple(outs)
+
+    def backward(self, dq, dk=None, dv=None, *, q=None, k=None, plan=None, pos=None, q_weight=None, k_weight=None,
+                 want_weight_grads=True, out=None):
+        """Gradients of ``forward``'s outputs (in their layout) -> ((dq, dk, dv) in the inputs' layout, grads).
+
+        ``q``, ``k``: the forward's inputs, needed (and only taken) with a norm.  ``grads``: fp32 [d] tensors
+        "q_weight", "k_weight" (and "q_bias", "k_bias" of a layer norm), summed over all rows, whether or not a
+        weight was passed; empty without a norm or with ``want_weight_grads=False``."""
+        on_plan = plan is not None
+        if k is not None and dk is None:
+            raise ValueError("k: given without dk")
+        B, tokens, pos_ptr = self._begin(dq, plan, pos, on_plan)
+        args, outs, grads, n = (tra_rotary_tensor_t * 3)(), [], {}, 0
+        for i, (name, dy, x, w) in enumerate((("q", dq, q, q_weight), ("k", dk, k, k_weight), ("v", dv, None, None))):
+            if dy is None:
+                outs.append(None)
+                continue
+            heads = dy.shape[1 if on_plan else 2] if dy.dim() == 4 else 0
+            y_shape = (B, heads, tokens, self.head_dim) if on_plan else (B, tokens, heads, self.head_dim)
+            x_shape = (B, tokens, heads, self.head_dim)
+            a = args[n]
+            a.src, a.src_stride[:] = dy.data_ptr(), self._strides(dy, "d" + name, dq, y_shape, on_plan)
+            dx = out[i] if out is not None else None
+            if dx is None:
+                dx = torch.empty(x_shape, dtype=dy.dtype, device=dy.device)
+            a.dst, a.dst_stride[:] = dx.data_ptr(), self._strides(dx, "out d" + name, dq, x_shape, False)
+            if name != "v":
+                if (x is not None) != (self.norm is not None):
+                    raise ValueError(f"{name}: the forward's input is needed with a norm and only with one")
+                if x is not None:
+                    a.x, a.x_stride[:] = x.data_ptr(), self._strides(x, name, dq, x_shape, False)
+                    if want_weight_grads:
+                        for end in ("weight", "bias")[:2 if self.norm == "layer" else 1]:
+                            g = grads[f"{name}_{end}"] = torch.empty(self.head_dim, dtype=torch.float32, device=dq.device)
+                            setattr(a, end + "_grad", g.data_ptr())
+                a.weight = self._param(w, name + "_weight", dq)
+            a.heads = heads
+            a.flags = (TRA_ROTARY_ROTATE if name != "v" else 0) | \
+                (TRA_ROTARY_TILE_MAJOR if self._tile_major(plan, name) else 0)
+            outs.append(dx)
+            n += 1
+        ws = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dq.device) if grads else None
+        _check(_lib.tra_rotary_backward(self._h, plan._h if on_plan else None, pos_ptr, ctypes.byref(args), n, B, tokens,
+                                        _DTYPES[dq.dtype], ws.data_ptr() if grads else None,
+                                        self.workspace_bytes if grads else 0, _stream()), "tra_rotary_backward")
+        return tuple(outs), grads

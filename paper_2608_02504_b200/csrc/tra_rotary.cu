@@ -1,0 +1,609 @@
+// What a layer does to Q, K and V between its projections and its attention, in one pass: a norm over the
+// channels of every head (RMS or layer norm, optional), rotary positions with several axes, and the token
+// order the attention calls want; and the gradients of all of it.
+//
+// One row = one (token, head), d channels.  n = x, x r or (x - mean) r with r = (mean square + eps)^-1/2;
+// z = weight n + bias; the channel pair (z1, z2) of pair p turns by the angle pos[axis_p] * f_p:
+//   y = (z1 cos - z2 sin, z1 sin + z2 cos).
+// Gradients: u = the pair of dy turned back, dweight = sum u n, dbias = sum u, g = weight u,
+//   dx = r (g - n mean(g n))            RMS norm
+//   dx = r (g - mean g - n mean(g n))   layer norm.
+//
+// Angles.  F_p = f_p / 2 pi modulo one turn, as a 64-bit binary fraction (rounded once, on the host, from long
+// double).  pos * F_p modulo 2^64 is then the angle in turns with its whole turns already gone, whatever the
+// position: an integer product in place of a range reduction, off by pos * 2^-65 turns.  Its high word, as a
+// signed number of half turns, goes to sincospif.
+//
+// Bound: HBM.  Every element is read once and written once (the norm's backward pass reads x too); a row stays
+// in the registers of d / 16 neighbouring threads, 16 channels each (a 16-byte piece of either half of the row
+// for 16-bit types, so that both ways of pairing channels find their partner in the same thread and a row is
+// read in whole 128-byte lines), and its sums are shuffles among those threads.  The angles of a token are
+// computed once per thread and used for all the heads it walks.  The weights' gradients stay in
+// registers over a thread's rows, are added up per thread block in a fixed order, and a second small kernel
+// adds the blocks: no atomics, the same bits every time.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+#include <string.h>
+
+#include <new>
+
+#include "tra_common.cuh"
+
+struct tra_rotary {
+  int head_dim, n_axes, halves, norm;
+  float eps;
+  uint64_t turn[TRA_ROTARY_MAX_HEAD_DIM / 2];     // F_p
+  uint8_t axis[TRA_ROTARY_MAX_HEAD_DIM / 2];
+};
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxD = TRA_ROTARY_MAX_HEAD_DIM;
+constexpr int kReduceRows = 32;       // block partials summed side by side in the second kernel
+constexpr int kReduceCols = 8;
+
+struct RotTensor {
+  const void* src;       // forward: x; backward: dy
+  void* dst;             // forward: y; backward: dx
+  const void* x;         // backward with a norm: the forward's input
+  const void* weight;
+  const void* bias;
+  float* partial;        // backward: [2][blocks][d] of this tensor, or NULL
+  long long src_stride[3], dst_stride[3], x_stride[3];      // batch, token, head (elements)
+  int heads, rotate, tile_major, head_slots;
+};
+
+struct RotArgs {
+  RotTensor t[3];
+  uint64_t turn[kMaxD / 2];
+  uint8_t axis[kMaxD / 2];
+  const int32_t* raster_of_pos;   // plan, or NULL
+  const int32_t* pos;             // explicit positions [tokens][n_axes], or NULL
+  int n_axes, H, W, n_video;      // grid positions: token n -> (n / (H W), n / W % H, n % W)
+  int d, lanes;                   // lanes: threads per row, d / 16 rounded up to a power of two
+  float eps, inv_d;
+  long long rows;                 // batch * tokens
+  int tokens;
+};
+
+template <typename T>
+struct Piece;                     // eight consecutive channels as loaded
+template <>
+struct Piece<__nv_bfloat16> {
+  uint4 v;
+  __device__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ void get(float* f) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ void store(__nv_bfloat16* p, const float* f) {
+    __nv_bfloat162 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<uint4*>(h);
+  }
+};
+template <>
+struct Piece<__half> {
+  uint4 v;
+  __device__ void load(const __half* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ void get(float* f) const {
+    const __half2* h = reinterpret_cast<const __half2*>(&v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 t = __half22float2(h[i]);
+      f[2 * i] = t.x;
+      f[2 * i + 1] = t.y;
+    }
+  }
+  static __device__ void store(__half* p, const float* f) {
+    __half2 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<uint4*>(h);
+  }
+};
+template <>
+struct Piece<float> {
+  float4 a, b;
+  __device__ void load(const float* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ void get(float* f) const {
+    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+  }
+  static __device__ void store(float* p, const float* f) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  }
+};
+
+// Sum over the threads of a row (a power of two of neighbouring lanes).
+__device__ __forceinline__ float row_sum(float s, int lanes) {
+  for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
+}
+
+// Channel c of the thread's sixteen: 0 .. 7 in the lower half of the row, 8 .. 15 in the upper half.  Pair j (0 .. 7) of the
+// thread: (j, j + 8) when channels pair across the halves, (2 j, 2 j + 1) otherwise.
+template <bool kHalves>
+__device__ __forceinline__ void turn_pairs(float* z, const float* cs, const float* sn, float sign) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float& a = z[kHalves ? j : 2 * j];
+    float& b = z[kHalves ? j + 8 : 2 * j + 1];
+    const float s = sign * sn[j];
+    const float ta = a * cs[j] - b * s, tb = a * s + b * cs[j];
+    a = ta;
+    b = tb;
+  }
+}
+
+template <typename T, int kNorm, bool kHalves, bool kBackward>
+__global__ void __launch_bounds__(kThreads) tra_rotary_kernel(const __grid_constant__ RotArgs p) {
+  __shared__ uint64_t s_turn[kMaxD / 2];
+  __shared__ uint8_t s_axis[kMaxD / 2];
+  __shared__ float s_red[kBackward && kNorm ? kThreads / 32 : 1][kBackward && kNorm ? kMaxD : 1];
+  const RotTensor& t = p.t[blockIdx.y];
+  const int tid = threadIdx.x;
+  for (int i = tid; i < p.d / 2; i += kThreads) {
+    s_turn[i] = p.turn[i];
+    s_axis[i] = p.axis[i];
+  }
+  __syncthreads();
+  const int lane = tid % p.lanes, slot = tid / p.lanes;
+  const bool on = lane * 16 < p.d;                     // d / 16 need not be a power of two
+  const int c_lo = lane * 8, c_hi = p.d / 2 + lane * 8;
+  const int head0 = slot % t.head_slots;
+  const int tokens_per_block = kThreads / p.lanes / t.head_slots;
+  const bool rotate = t.rotate != 0;
+  const bool normed = kNorm != TRA_NORM_NONE && rotate;
+
+  Piece<T> w_lo, w_hi, b_lo, b_hi;
+  const bool has_w = normed && t.weight != nullptr && on;
+  const bool has_b = !kBackward && normed && t.bias != nullptr && on;
+  if (has_w) {
+    w_lo.load((const T*)t.weight + c_lo);
+    w_hi.load((const T*)t.weight + c_hi);
+  }
+  if (has_b) {
+    b_lo.load((const T*)t.bias + c_lo);
+    b_hi.load((const T*)t.bias + c_hi);
+  }
+  float acc_w[kBackward && kNorm ? 16 : 1], acc_b[kBackward && kNorm == TRA_NORM_LAYER ? 16 : 1];
+  if (kBackward && kNorm) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      acc_w[i] = 0.f;
+      if (kNorm == TRA_NORM_LAYER) acc_b[i] = 0.f;
+    }
+  }
+
+  // All threads of a warp walk the same number of rows (row sums are warp-wide shuffles): a thread whose token or head
+  // does not exist takes part with zeros.
+  for (long long base = (long long)blockIdx.x * tokens_per_block; base < p.rows;
+       base += (long long)gridDim.x * tokens_per_block) {
+    const long long row = base + slot / t.head_slots;
+    const bool token_on = on && row < p.rows;
+    long long batch = 0;
+    int pos_idx = 0, src_tok = 0;
+    if (token_on) {
+      batch = row / p.tokens;
+      pos_idx = (int)(row - batch * p.tokens);
+      src_tok = t.tile_major && pos_idx < p.n_video ? __ldg(p.raster_of_pos + pos_idx) : pos_idx;
+    }
+    float cs[8], sn[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      cs[j] = 1.f;
+      sn[j] = 0.f;
+    }
+    if (rotate && token_on && (p.pos != nullptr || src_tok < p.n_video)) {
+      int axis_pos[4] = {0, 0, 0, 0};
+      if (p.pos != nullptr) {
+        for (int a = 0; a < p.n_axes; ++a) {
+          const int v = __ldg(p.pos + (long long)src_tok * p.n_axes + a);
+          if (a == 0) axis_pos[0] = v;
+          if (a == 1) axis_pos[1] = v;
+          if (a == 2) axis_pos[2] = v;
+          if (a == 3) axis_pos[3] = v;
+        }
+      } else {
+        const int hw = p.H * p.W;
+        axis_pos[0] = src_tok / hw;
+        const int in_frame = src_tok - axis_pos[0] * hw;
+        axis_pos[1] = in_frame / p.W;
+        axis_pos[2] = in_frame - axis_pos[1] * p.W;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int pair = kHalves ? c_lo + j : (j < 4 ? c_lo / 2 + j : c_hi / 2 + j - 4);
+        const int a = s_axis[pair];
+        const int v = a == 0 ? axis_pos[0] : a == 1 ? axis_pos[1] : a == 2 ? axis_pos[2] : axis_pos[3];
+        const uint64_t turns = (uint64_t)(int64_t)v * s_turn[pair];
+        const float half_turns = (float)(int32_t)(turns >> 32) * 4.656612873077393e-10f;      // 2^-31
+        sincospif(half_turns, &sn[j], &cs[j]);
+      }
+    }
+    // forward reads at the source row and writes at the ordered one, backward the other way round
+    const int in_tok = kBackward ? pos_idx : src_tok, out_tok = kBackward ? src_tok : pos_idx;
+    const T* in = (const T*)t.src + batch * t.src_stride[0] + (long long)in_tok * t.src_stride[1];
+    T* out = (T*)t.dst + batch * t.dst_stride[0] + (long long)out_tok * t.dst_stride[1];
+    const T* xin = kBackward && normed ? (const T*)t.x + batch * t.x_stride[0] + (long long)out_tok * t.x_stride[1] : nullptr;
+
+    Piece<T> lo, hi, xlo, xhi;
+    auto fetch = [&](int h) {
+      if (token_on && h < t.heads) {
+        lo.load(in + h * t.src_stride[2] + c_lo);
+        hi.load(in + h * t.src_stride[2] + c_hi);
+        if (kBackward && normed) {
+          xlo.load(xin + h * t.x_stride[2] + c_lo);
+          xhi.load(xin + h * t.x_stride[2] + c_hi);
+        }
+      } else {
+        lo.zero();
+        hi.zero();
+        if (kBackward && normed) {
+          xlo.zero();
+          xhi.zero();
+        }
+      }
+    };
+    const int steps = (t.heads + t.head_slots - 1) / t.head_slots;
+    fetch(head0);
+    for (int step = 0; step < steps; ++step) {
+      const int h = head0 + step * t.head_slots;
+      const bool row_on = token_on && h < t.heads;
+      float z[16];
+      lo.get(z);
+      hi.get(z + 8);
+      if (!kBackward) {
+        if (step + 1 < steps) fetch(h + t.head_slots);       // the next head's row while this one is worked on
+        if (normed) {
+          float mean = 0.f;
+          if (kNorm == TRA_NORM_LAYER) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s += z[i];
+            mean = row_sum(s, p.lanes) * p.inv_d;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = on ? z[i] - mean : 0.f;
+          }
+          float q = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) q = fmaf(z[i], z[i], q);
+          const float r = rsqrtf(fmaf(row_sum(q, p.lanes), p.inv_d, p.eps));
+          float w[16];
+          if (has_w) {
+            w_lo.get(w);
+            w_hi.get(w + 8);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = z[i] * r * w[i];
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] *= r;
+          }
+          if (has_b) {
+            b_lo.get(w);
+            b_hi.get(w + 8);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] += w[i];
+          }
+        }
+        if (rotate) turn_pairs<kHalves>(z, cs, sn, 1.f);
+      } else {
+        float n[16];
+        if (normed) {
+          xlo.get(n);
+          xhi.get(n + 8);
+        }
+        if (step + 1 < steps) fetch(h + t.head_slots);
+        if (rotate) turn_pairs<kHalves>(z, cs, sn, -1.f);      // z = u
+        if (normed) {
+          if (kNorm == TRA_NORM_LAYER) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s += n[i];
+            const float mean = row_sum(s, p.lanes) * p.inv_d;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) n[i] = on ? n[i] - mean : 0.f;
+          }
+          float q = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) q = fmaf(n[i], n[i], q);
+          const float r = rsqrtf(fmaf(row_sum(q, p.lanes), p.inv_d, p.eps));
+          float w[16];
+          if (has_w) {
+            w_lo.get(w);
+            w_hi.get(w + 8);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = 1.f;
+          }
+          float sg = 0.f, sgn = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            n[i] *= r;
+            // a row that does not exist is left out (eps = 0 would make 0 * inf of it)
+            acc_w[i] += row_on ? z[i] * n[i] : 0.f;
+            if (kNorm == TRA_NORM_LAYER) acc_b[i] += row_on ? z[i] : 0.f;
+            z[i] *= w[i];                                       // g
+            sg += z[i];
+            sgn = fmaf(z[i], n[i], sgn);
+          }
+          const float mgn = row_sum(sgn, p.lanes) * p.inv_d;
+          const float mg = kNorm == TRA_NORM_LAYER ? row_sum(sg, p.lanes) * p.inv_d : 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) z[i] = r * (z[i] - mg - n[i] * mgn);
+        }
+      }
+      if (row_on) {
+        Piece<T>::store(out + h * t.dst_stride[2] + c_lo, z);
+        Piece<T>::store(out + h * t.dst_stride[2] + c_hi, z + 8);
+      }
+    }
+  }
+
+  if constexpr (kBackward && kNorm != TRA_NORM_NONE) {
+    if (t.partial == nullptr) return;
+    // threads of the same lane hold the same channels: add them over the warp, then over the block's warps in order
+    constexpr int kSums = kNorm == TRA_NORM_LAYER ? 2 : 1;
+    const int warp = tid >> 5;
+#pragma unroll
+    for (int which = 0; which < kSums; ++which) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float v = acc_w[i];
+        if constexpr (kNorm == TRA_NORM_LAYER)
+          if (which == 1) v = acc_b[i];
+        for (int o = p.lanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if ((tid & 31) < p.lanes && on) s_red[warp][i < 8 ? c_lo + i : c_hi + i - 8] = v;
+      }
+      __syncthreads();
+      for (int c = tid; c < p.d; c += kThreads) {
+        float v = 0.f;
+        for (int k = 0; k < kThreads / 32; ++k) v += s_red[k][c];
+        t.partial[((long long)which * gridDim.x + blockIdx.x) * p.d + c] = v;
+      }
+      __syncthreads();
+    }
+  }
+}
+
+struct ReduceArgs {
+  const float* partial[6];
+  float* out[6];
+  int blocks, d;
+};
+
+// out[c] = sum over the blocks' partials, in a fixed order: 32 strided sums side by side, then those in order.
+__global__ void __launch_bounds__(kReduceRows * kReduceCols) tra_rotary_reduce_kernel(const __grid_constant__ ReduceArgs p) {
+  __shared__ float s[kReduceRows][kReduceCols];
+  const int col = threadIdx.x % kReduceCols, r = threadIdx.x / kReduceCols;
+  const int c = blockIdx.x * kReduceCols + col;
+  float v = 0.f;
+  if (c < p.d)
+    for (int b = r; b < p.blocks; b += kReduceRows) v += p.partial[blockIdx.y][(long long)b * p.d + c];
+  s[r][col] = v;
+  __syncthreads();
+  if (r == 0 && c < p.d) {
+    for (int i = 1; i < kReduceRows; ++i) v += s[i][col];
+    p.out[blockIdx.y][c] = v;
+  }
+}
+
+int lanes_of(int d) {
+  int l = 1;
+  while (l * 16 < d) l *= 2;
+  return l;
+}
+
+// Blocks of a backward launch: up to four per SM, so that the weights' partial sums stay few.
+constexpr int kBackwardBlocksMax = 592;
+
+int elem_bytes(int dtype) { return dtype == TRA_FP32 ? 4 : 2; }
+
+bool aligned_strides(const int64_t* s, int dtype) {
+  for (int i = 0; i < 3; ++i)
+    if ((s[i] * elem_bytes(dtype)) & 15) return false;
+  return true;
+}
+
+template <typename T, int kNorm, bool kBackward>
+void launch_halves(bool halves, dim3 grid, const RotArgs& a, cudaStream_t stream) {
+  if (halves)
+    tra_rotary_kernel<T, kNorm, true, kBackward><<<grid, kThreads, 0, stream>>>(a);
+  else
+    tra_rotary_kernel<T, kNorm, false, kBackward><<<grid, kThreads, 0, stream>>>(a);
+}
+template <typename T, bool kBackward>
+void launch_norm(int norm, bool halves, dim3 grid, const RotArgs& a, cudaStream_t stream) {
+  if (norm == TRA_NORM_RMS)
+    launch_halves<T, TRA_NORM_RMS, kBackward>(halves, grid, a, stream);
+  else if (norm == TRA_NORM_LAYER)
+    launch_halves<T, TRA_NORM_LAYER, kBackward>(halves, grid, a, stream);
+  else
+    launch_halves<T, TRA_NORM_NONE, kBackward>(halves, grid, a, stream);
+}
+
+int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const tra_rotary_tensor_t* tensors,
+        int n_tensors, int B, int tokens, int dtype, bool backward, void* workspace, size_t workspace_bytes,
+        cudaStream_t stream) {
+  if (!rot || !tensors || n_tensors < 1 || n_tensors > 3 || B < 1 || tokens < 1) return TRA_ERR_INVALID_ARG;
+  if (dtype != TRA_BF16 && dtype != TRA_FP16 && dtype != TRA_FP32) return TRA_ERR_INVALID_ARG;
+  if (((uintptr_t)pos & 3)) return TRA_ERR_INVALID_ARG;
+  int device = 0;
+  if (plan) {
+    if (cudaGetDevice(&device) != cudaSuccess) return TRA_ERR_CUDA;
+    if (device != plan->device || tokens != plan->S) return TRA_ERR_INVALID_ARG;
+    if (!pos && rot->n_axes != 3) return TRA_ERR_INVALID_ARG;
+  }
+  RotArgs a;
+  memset(&a, 0, sizeof(a));
+  bool any_rotate = false, grads = false;
+  const int lanes = lanes_of(rot->head_dim);
+  const long long rows = (long long)B * tokens;
+  for (int i = 0; i < n_tensors; ++i) {
+    const tra_rotary_tensor_t& s = tensors[i];
+    RotTensor& t = a.t[i];
+    if (!s.src || !s.dst || s.heads < 1 || (s.flags & ~(TRA_ROTARY_ROTATE | TRA_ROTARY_TILE_MAJOR))) return TRA_ERR_INVALID_ARG;
+    t.rotate = (s.flags & TRA_ROTARY_ROTATE) != 0;
+    t.tile_major = (s.flags & TRA_ROTARY_TILE_MAJOR) != 0;
+    if (t.tile_major && !plan) return TRA_ERR_INVALID_ARG;
+    const bool normed = t.rotate && rot->norm != TRA_NORM_NONE;
+    if ((s.weight && !normed) || (s.bias && (!normed || rot->norm != TRA_NORM_LAYER))) return TRA_ERR_INVALID_ARG;
+    if (backward ? (normed != (s.x != nullptr)) : (s.x != nullptr)) return TRA_ERR_INVALID_ARG;
+    if ((s.weight_grad && (!backward || !normed)) || (s.bias_grad && (!backward || !normed || rot->norm != TRA_NORM_LAYER)))
+      return TRA_ERR_INVALID_ARG;
+    if (((uintptr_t)s.src | (uintptr_t)s.dst | (uintptr_t)s.x | (uintptr_t)s.weight | (uintptr_t)s.bias) & 15)
+      return TRA_ERR_INVALID_ARG;
+    if (!aligned_strides(s.src_stride, dtype) || !aligned_strides(s.dst_stride, dtype) ||
+        (s.x && !aligned_strides(s.x_stride, dtype)))
+      return TRA_ERR_INVALID_ARG;
+    any_rotate |= t.rotate != 0;
+    grads |= s.weight_grad != nullptr || s.bias_grad != nullptr;
+    t.src = s.src, t.dst = s.dst, t.x = s.x, t.weight = s.weight, t.bias = s.bias;
+    for (int k = 0; k < 3; ++k) {
+      t.src_stride[k] = s.src_stride[k];
+      t.dst_stride[k] = s.dst_stride[k];
+      t.x_stride[k] = s.x_stride[k];
+    }
+    t.heads = s.heads;
+    // Heads side by side in a block: a power of two that divides the heads (no idle threads), at most 8 so that a token's
+    // angles are reused; with few tokens all heads side by side, so that the launch still fills the GPU.
+    const int slots = kThreads / lanes;
+    int hs = 1;
+    while (hs < 8 && hs < slots && s.heads % (2 * hs) == 0) hs *= 2;
+    if (rows * hs * lanes < 148 * 1024)
+      while (hs < slots && hs < s.heads) hs *= 2;
+    t.head_slots = hs;
+  }
+  if (any_rotate && !pos && !plan) return TRA_ERR_INVALID_ARG;
+  memcpy(a.turn, rot->turn, sizeof(a.turn));
+  memcpy(a.axis, rot->axis, sizeof(a.axis));
+  a.raster_of_pos = plan ? plan->d_raster_of_pos : nullptr;
+  a.pos = pos;
+  a.n_axes = rot->n_axes;
+  a.H = plan ? plan->cfg.H : 1;
+  a.W = plan ? plan->cfg.W : 1;
+  a.n_video = plan ? plan->N : 0;
+  a.d = rot->head_dim;
+  a.lanes = lanes;
+  a.eps = rot->eps;
+  a.inv_d = 1.0f / (float)rot->head_dim;
+  a.rows = rows;
+  a.tokens = tokens;
+
+  long long blocks = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    const int tpb = kThreads / lanes / a.t[i].head_slots;
+    const long long n = (rows + tpb - 1) / tpb;
+    if (n > blocks) blocks = n;
+  }
+  if (backward && blocks > kBackwardBlocksMax) blocks = kBackwardBlocksMax;
+  if (blocks > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
+  ReduceArgs red;
+  memset(&red, 0, sizeof(red));
+  int n_red = 0;
+  if (grads) {
+    if (!workspace || ((uintptr_t)workspace & 15)) return TRA_ERR_INVALID_ARG;
+    if (workspace_bytes < tra_rotary_backward_workspace_bytes(rot)) return TRA_ERR_CAPACITY;
+    const long long per = 2ll * blocks * rot->head_dim;
+    for (int i = 0; i < n_tensors; ++i) {
+      if (!tensors[i].weight_grad && !tensors[i].bias_grad) continue;
+      a.t[i].partial = (float*)workspace + per * i;
+      if (tensors[i].weight_grad) {
+        red.partial[n_red] = a.t[i].partial;
+        red.out[n_red++] = tensors[i].weight_grad;
+      }
+      if (tensors[i].bias_grad) {
+        red.partial[n_red] = a.t[i].partial + blocks * rot->head_dim;
+        red.out[n_red++] = tensors[i].bias_grad;
+      }
+    }
+    red.blocks = (int)blocks;
+    red.d = rot->head_dim;
+  }
+  const dim3 grid((unsigned)blocks, (unsigned)n_tensors);
+  const bool halves = rot->halves != 0;
+  if (dtype == TRA_BF16) {
+    backward ? launch_norm<__nv_bfloat16, true>(rot->norm, halves, grid, a, stream)
+             : launch_norm<__nv_bfloat16, false>(rot->norm, halves, grid, a, stream);
+  } else if (dtype == TRA_FP16) {
+    backward ? launch_norm<__half, true>(rot->norm, halves, grid, a, stream)
+             : launch_norm<__half, false>(rot->norm, halves, grid, a, stream);
+  } else {
+    backward ? launch_norm<float, true>(rot->norm, halves, grid, a, stream)
+             : launch_norm<float, false>(rot->norm, halves, grid, a, stream);
+  }
+  TRA_CUDA_CHECK(cudaGetLastError());
+  if (n_red) {
+    tra_rotary_reduce_kernel<<<dim3((rot->head_dim + kReduceCols - 1) / kReduceCols, n_red), kReduceRows * kReduceCols, 0,
+                               stream>>>(red);
+    TRA_CUDA_CHECK(cudaGetLastError());
+  }
+  return TRA_OK;
+}
+
+}  // namespace
+
+extern "C" int tra_rotary_create(tra_rotary_t** out, const tra_rotary_config_t* cfg) {
+  if (!out || !cfg) return TRA_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!cfg->axis || !cfg->inv_freq || cfg->n_axes < 1 || cfg->n_axes > 4) return TRA_ERR_INVALID_ARG;
+  if (cfg->norm != TRA_NORM_NONE && cfg->norm != TRA_NORM_RMS && cfg->norm != TRA_NORM_LAYER) return TRA_ERR_INVALID_ARG;
+  if (!(cfg->eps >= 0.0 && cfg->eps < 1e30)) return TRA_ERR_INVALID_ARG;
+  if (cfg->head_dim < 16 || cfg->head_dim > kMaxD || cfg->head_dim % 16) return TRA_ERR_UNSUPPORTED;
+  for (int i = 0; i < cfg->head_dim / 2; ++i)
+    if (cfg->axis[i] < 0 || cfg->axis[i] >= cfg->n_axes || !isfinite(cfg->inv_freq[i])) return TRA_ERR_INVALID_ARG;
+  tra_rotary* r = new (std::nothrow) tra_rotary;
+  if (!r) return TRA_ERR_CAPACITY;
+  memset(r, 0, sizeof(*r));
+  r->head_dim = cfg->head_dim;
+  r->n_axes = cfg->n_axes;
+  r->halves = cfg->halves != 0;
+  r->norm = cfg->norm;
+  r->eps = (float)cfg->eps;
+  const long double two_pi = 6.283185307179586476925286766559005768L;
+  for (int i = 0; i < cfg->head_dim / 2; ++i) {
+    long double turns = (long double)cfg->inv_freq[i] / two_pi;
+    turns -= floorl(turns);                                       // in [0, 1]
+    const long double scaled = floorl(turns * 18446744073709551616.0L + 0.5L);
+    r->turn[i] = scaled >= 18446744073709551616.0L ? 0ull : (uint64_t)scaled;
+    r->axis[i] = (uint8_t)cfg->axis[i];
+  }
+  *out = r;
+  return TRA_OK;
+}
+
+extern "C" int tra_rotary_destroy(tra_rotary_t* rot) {
+  if (!rot) return TRA_ERR_INVALID_ARG;
+  delete rot;
+  return TRA_OK;
+}
+
+extern "C" size_t tra_rotary_backward_workspace_bytes(const tra_rotary_t* rot) {
+  return rot ? sizeof(float) * 3 * 2 * (size_t)kBackwardBlocksMax * rot->head_dim : 0;
+}
+
+extern "C" int tra_rotary_forward(const tra_rotary_t* rot, const tra_plan_t* plan, const int32_t* pos,
+                                  const tra_rotary_tensor_t* tensors, int n_tensors, int B, int tokens, int dtype,
+                                  void* stream) {
+  return run(rot, plan, pos, tensors, n_tensors, B, tokens, dtype, false, nullptr, 0, (cudaStream_t)stream);
+}
+
+extern "C" int tra_rotary_backward(const tra_rotary_t* rot, const tra_plan_t* plan, const int32_t* pos,
+                                   const tra_rotary_tensor_t* tensors, int n_tensors, int B, int tokens, int dtype,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+  return run(rot, plan, pos, tensors, n_tensors, B, tokens, dtype, true, workspace, workspace_bytes, (cudaStream_t)stream);
+}
