@@ -357,6 +357,57 @@ int tra_rotary_backward(const tra_rotary_t* rot, const tra_plan_t* plan, const i
                         const tra_rotary_tensor_t* tensors, int n_tensors, int B, int tokens, int dtype,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- attention over packed sequences (the paper's layer attends inside one clip; this is attention for the
+ * sequences around it: prompts and clips of different lengths in one batch, chunks behind a cache, one new token) ---- */
+
+/* Tokens of all sequences lie one after the other: Q, O [total_q, heads, d], K, V [total_k, kv_heads, d], bf16 or fp16, channels
+ * contiguous, tokens and heads behind strides.  Query heads g * group .. g * group + group - 1 share key/value head g,
+ * group = heads / kv_heads.  Sequence s has the queries cu_q[s] .. cu_q[s + 1] - 1 and the keys k_begin[s] .. k_end[s] - 1
+ * (device int32; ranges of keys may leave gaps and may be shared).  With `causal`, query i of a sequence sees its keys
+ * 0 .. i + (number of keys - number of queries): the last query sees every key.
+ *   O = softmax(sm_scale Q K^T) V,  lse = log sum exp of the scores a query sees, fp32 [total_q, heads].
+ * A query that sees no key gets O = 0 and lse = -inf.  Rows of O and lse in front of cu_q[0] and behind cu_q[n_seq] are
+ * left as they were.  What lies in K and V outside a sequence's range, or in Q outside of all, is never used and may be
+ * anything, NaN too. */
+typedef struct tra_packed tra_packed_t; /* opaque: head layout, type, order, a device status word */
+
+typedef struct {
+  int heads, kv_heads; /* heads a multiple of kv_heads, group <= 128 */
+  int head_dim;        /* 64 or 128                                  */
+  int dtype;           /* TRA_BF16 or TRA_FP16                       */
+  int causal;
+} tra_packed_config_t;
+
+typedef struct {
+  const void *q, *k, *v;  /* 16-byte aligned                                                     */
+  void* o;                /* forward: written; backward: read                                     */
+  float* lse;             /* forward: written, or NULL; backward: read                            */
+  int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2]; /* token, head: elements, multiples of 8 */
+  const int32_t *cu_q;    /* device [n_seq + 1], ascending                                        */
+  const int32_t *k_begin, *k_end; /* device [n_seq]; packed keys: cu_k and cu_k + 1               */
+  int n_seq, total_q, total_k;
+  int max_q, max_k;       /* upper bounds of the sequences' queries and keys                      */
+  float sm_scale;
+} tra_packed_args_t;
+
+/* Creates the handle on the current device (allocates its status word). */
+int tra_packed_create(tra_packed_t** out, const tra_packed_config_t* cfg);
+int tra_packed_destroy(tra_packed_t* packed);
+/* Reads and clears the handle's device status word (synchronises `stream`): TRA_OK, TRA_ERR_TIMEOUT, or
+ * TRA_ERR_INVALID_ARG: a range on the device lay outside its tensor, ran backwards or was longer than the stated maximum; it was
+ * cut to fit and the results of that call are incomplete. */
+int tra_packed_status(tra_packed_t* packed, void* stream);
+
+/* Forward.  The launch follows from the sizes alone: sequences of at most 16 rows (max_q * group) go to a kernel for few
+ * rows over many keys, others to 128-row tensor-core tiles; either splits the keys over thread blocks when there
+ * are too few rows to fill the GPU, and a second launch joins the parts, which lie in `workspace`: device memory of
+ * tra_packed_attn_workspace_bytes (0: none needed, pass NULL), 16-byte aligned, owned by the caller and free to reuse once
+ * `stream` has passed the call.  The current device must be the handle's.
+ * Errors: TRA_ERR_INVALID_ARG, TRA_ERR_UNSUPPORTED, TRA_ERR_CAPACITY (workspace too small), TRA_ERR_CUDA. */
+size_t tra_packed_attn_workspace_bytes(const tra_packed_t* packed, int n_seq, int total_q, int max_q, int max_k);
+int tra_packed_attn(const tra_packed_t* packed, const tra_packed_args_t* args, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
 #ifdef __cplusplus
 }
 #endif

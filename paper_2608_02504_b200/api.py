@@ -38,6 +38,8 @@ EXPORTS = [
     "tra_hot_path_host_workspace_bytes", "tra_hot_path_host",
     "tra_rotary_create", "tra_rotary_destroy", "tra_rotary_forward", "tra_rotary_backward_workspace_bytes",
     "tra_rotary_backward",
+    "tra_packed_create", "tra_packed_destroy", "tra_packed_status", "tra_packed_attn_workspace_bytes",
+    "tra_packed_attn",
 ]
 
 
@@ -68,6 +70,17 @@ class tra_rotary_tensor_t(ctypes.Structure):
         ("src_stride", ctypes.c_int64 * 3), ("dst_stride", ctypes.c_int64 * 3), ("x_stride", ctypes.c_int64 * 3),
         ("heads", ctypes.c_int), ("flags", ctypes.c_uint),
     ]
+
+
+class tra_packed_config_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("heads", "kv_heads", "head_dim", "dtype", "causal")]
+
+
+class tra_packed_args_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "o", "lse")] + \
+        [(n, ctypes.c_int64 * 2) for n in ("q_stride", "k_stride", "v_stride", "o_stride")] + \
+        [(n, ctypes.c_void_p) for n in ("cu_q", "k_begin", "k_end")] + \
+        [(n, ctypes.c_int) for n in ("n_seq", "total_q", "total_k", "max_q", "max_k")] + [("sm_scale", ctypes.c_float)]
 
 
 def _load():
@@ -104,6 +117,12 @@ def _load():
     lib.tra_rotary_backward_workspace_bytes.argtypes = [vp]
     lib.tra_rotary_backward_workspace_bytes.restype = ctypes.c_size_t
     lib.tra_rotary_backward.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, ctypes.c_size_t, vp]
+    lib.tra_packed_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(tra_packed_config_t)]
+    lib.tra_packed_destroy.argtypes = [vp]
+    lib.tra_packed_status.argtypes = [vp, vp]
+    lib.tra_packed_attn_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
+    lib.tra_packed_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.tra_packed_attn.argtypes = [vp, vp, vp, ctypes.c_size_t, vp]
     return lib
 
 
@@ -588,3 +607,94 @@ class Rotary:
                                         _DTYPES[dq.dtype], ws.data_ptr() if grads else None,
                                         self.workspace_bytes if grads else 0, _stream()), "tra_rotary_backward")
         return tuple(outs), grads
+
+
+class PackedAttn:
+    """Attention over packed sequences: prompts and clips of different lengths in one batch, grouped heads, causal
+    or not, chunks and single new tokens behind a cache (``tra_packed_attn``), and its gradients.
+
+    Tensors: q, o [total_q, heads, head_dim], k, v [total_k, kv_heads, head_dim], any strides (multiples of 8
+    elements) with contiguous channels.  ``cu_q`` int32 [n_seq + 1]: sequence s has the queries cu_q[s] .. cu_q[s+1] - 1.
+    """
+
+    def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, causal=True):
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("dtype: expected bf16 or fp16")
+        cfg = tra_packed_config_t(heads, kv_heads, head_dim, _DTYPES[dtype], int(causal))
+        self._h = ctypes.c_void_p()
+        _check(_lib.tra_packed_create(ctypes.byref(self._h), ctypes.byref(cfg)), "tra_packed_create")
+        self.heads, self.kv_heads, self.head_dim, self.dtype, self.causal = heads, kv_heads, head_dim, dtype, bool(causal)
+        self.device = torch.device("cuda", torch.cuda.current_device())
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            _lib.tra_packed_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def status(self, stream=None):
+        return _lib.tra_packed_status(self._h, _stream(stream))
+
+    def check_status(self, stream=None):
+        _check(self.status(stream), "tra_packed_status")
+
+    def _tensor(self, t, name, total, heads):
+        if t.device != self.device or t.dtype != self.dtype or tuple(t.shape) != (total, heads, self.head_dim) or \
+                t.stride(2) != 1:
+            raise ValueError(f"{name}: expected {self.dtype} [{total}, {heads}, {self.head_dim}] on {self.device} with "
+                             "contiguous channels")
+        return t.data_ptr(), t.stride()[:2]
+
+    def _ints(self, t, name, n):
+        if t.device != self.device or t.dtype != torch.int32 or tuple(t.shape) != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous int32 tensor of {n} entries on {self.device}")
+        return t.data_ptr()
+
+    def _args(self, q, k, v, o, lse, cu_q, cu_k, k_range, max_q, max_k, sm_scale):
+        if q.dim() != 3 or k.dim() != 3 or cu_q.dim() != 1 or cu_q.shape[0] < 2:
+            raise ValueError("expected q, k, v [tokens, heads, head_dim] and cu_q [n_seq + 1]")
+        if torch.cuda.current_device() != self.device.index:
+            raise ValueError(f"the current device must be {self.device}")
+        a = tra_packed_args_t()
+        tq, tk, n = q.shape[0], k.shape[0], cu_q.shape[0] - 1
+        a.q, a.q_stride[:] = self._tensor(q, "q", tq, self.heads)
+        a.k, a.k_stride[:] = self._tensor(k, "k", tk, self.kv_heads)
+        a.v, a.v_stride[:] = self._tensor(v, "v", tk, self.kv_heads)
+        a.o, a.o_stride[:] = self._tensor(o, "o", tq, self.heads)
+        if lse is not None:
+            if lse.device != self.device or lse.dtype != torch.float32 or tuple(lse.shape) != (tq, self.heads) or \
+                    not lse.is_contiguous():
+                raise ValueError("lse: expected a contiguous fp32 tensor [total_q, heads]")
+            a.lse = lse.data_ptr()
+        a.cu_q = self._ints(cu_q, "cu_q", n + 1)
+        if k_range is not None:
+            if cu_k is not None:
+                raise ValueError("expected cu_k or k_range, not both")
+            a.k_begin, a.k_end = self._ints(k_range[0], "k_range", n), self._ints(k_range[1], "k_range", n)
+        else:
+            a.k_begin = a.cu_q if cu_k is None else self._ints(cu_k, "cu_k", n + 1)
+            a.k_end = a.k_begin + 4
+        a.n_seq, a.total_q, a.total_k, a.max_q, a.max_k = n, tq, tk, max_q, max_k
+        a.sm_scale = self.head_dim ** -0.5 if sm_scale is None else sm_scale
+        return a
+
+    def forward(self, q, k, v, cu_q, cu_k=None, *, k_range=None, max_q, max_k, o=None, lse=None, want_lse=False,
+                sm_scale=None):
+        """-> (o, lse).  Keys: packed like the queries (``cu_k``, default ``cu_q``), or ``k_range`` = (begin, end), two
+        int32 [n_seq] tensors, e.g. the filled parts of a cache's slots.  ``max_q``, ``max_k``: upper bounds of the
+        sequences' queries and keys (a longer one is cut and reported by ``check_status``).  Rows of o and lse that
+        belong to no sequence are not written."""
+        if o is None:
+            o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None and want_lse:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        a = self._args(q, k, v, o, lse, cu_q, cu_k, k_range, max_q, max_k, sm_scale)
+        n = _lib.tra_packed_attn_workspace_bytes(self._h, a.n_seq, a.total_q, max_q, max_k)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+        _check(_lib.tra_packed_attn(self._h, ctypes.byref(a), ws.data_ptr() if n else None, n, _stream()), "tra_packed_attn")
+        return o, lse

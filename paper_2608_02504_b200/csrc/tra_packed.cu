@@ -1,0 +1,271 @@
+// Packed attention: handle, argument checks, the choice of the launch, the join of split launches.
+#include <string.h>
+
+#include <new>
+
+#include "tra_packed.h"
+#include "tra_packed_ptx.cuh"
+
+namespace {
+
+constexpr int kJoinWarps = 4;
+
+// O = sum_s w_s O_s, w_s = 2^(lse2_s - lse2), lse2 = log2 sum_s 2^lse2_s over the parts of a split launch; lse from the
+// unrounded sums in the same way.  One block per (token, head), its warps take every fourth part.
+template <typename T, int D>
+__global__ void __launch_bounds__(32 * kJoinWarps) tra_packed_join_kernel(const __grid_constant__ tra_packed_launch p) {
+  constexpr int kPer = D / 32;
+  __shared__ float s_o[kJoinWarps][D];
+  __shared__ float s_max[kJoinWarps], s_sum[kJoinWarps], s_emax[kJoinWarps], s_esum[kJoinWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long row = blockIdx.x, stride = (long long)p.total_q * p.heads;
+  const int tok = (int)(row / p.heads), head = (int)(row - (long long)tok * p.heads);
+  // rows in front of the first and behind the last sequence stay as they are
+  if (tok < p.cu_q[0] || tok >= p.cu_q[p.n_seq]) return;
+  float top = -INFINITY, sum = 0.f, etop = -INFINITY, esum = 0.f, o[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) o[i] = 0.f;
+  for (int s = warp; s < p.splits; s += kJoinWarps) {
+    const float v = p.part_lse2[s * stride + row];
+    if (v == -INFINITY) continue;                    // the part held no key this row sees
+    const float up = fmaxf(top, v), f = ex2(top - up), g = ex2(v - up);
+    const float* src = p.part_o + (s * stride + row) * D + lane * kPer;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) o[i] = o[i] * f + g * src[i];
+    sum = sum * f + g;
+    top = up;
+    if (p.part_exact) {
+      const float e = p.part_exact[s * stride + row], eup = fmaxf(etop, e);
+      esum = esum * ex2(etop - eup) + ex2(e - eup);
+      etop = eup;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) s_o[warp][lane * kPer + i] = o[i];
+  if (lane == 0) {
+    s_max[warp] = top, s_sum[warp] = sum, s_emax[warp] = etop, s_esum[warp] = esum;
+  }
+  __syncthreads();
+  float all = -INFINITY, eall = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    all = fmaxf(all, s_max[w]);
+    eall = fmaxf(eall, s_emax[w]);
+  }
+  const float ref = all > -INFINITY ? all : 0.f, eref = eall > -INFINITY ? eall : 0.f;
+  float den = 0.f, eden = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    den += s_sum[w] * ex2(s_max[w] - ref);
+    eden += s_esum[w] * ex2(s_emax[w] - eref);
+  }
+  const float inv = den != 0.f ? 1.f / den : 0.f;
+  T* dst = (T*)p.o + tok * p.o_stride[0] + head * p.o_stride[1];
+  if (threadIdx.x < D / 2) {
+    const int c = 2 * threadIdx.x;
+    float a = 0.f, b = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) {
+      const float f = ex2(s_max[w] - ref);
+      a += f * s_o[w][c];
+      b += f * s_o[w][c + 1];
+    }
+    reinterpret_cast<uint32_t*>(dst)[threadIdx.x] = pack_pair<T>(a * inv, b * inv);
+  }
+  if (threadIdx.x == 0 && p.lse) p.lse[row] = eden != 0.f ? (eref + log2f(eden)) * kLn2 : -INFINITY;
+}
+
+// How a call runs: rows = the kernel for few rows (at most 16 per sequence and key/value head), with `splits` parts
+// of `chunk` keys; else the 128-row tiles, with `splits` ranges of key blocks.
+struct Choice {
+  bool rows;
+  int splits, chunk;
+};
+
+Choice choose(const tra_packed* h, int n_seq, int total_q, int max_q, int max_k) {
+  const int group = h->cfg.heads / h->cfg.kv_heads;
+  Choice c = {(long long)max_q * group <= 16, 1, 0};
+  if (c.rows) {
+    const long long units = (long long)n_seq * h->cfg.kv_heads, target = 8ll * h->sm_count;
+    const long long want = (target + units - 1) / units;
+    long long chunk = (max_k + want - 1) / want;
+    if (chunk < 256) chunk = 256;
+    c.chunk = (int)((chunk + 63) / 64 * 64);
+    c.splits = max_k > 0 ? (max_k + c.chunk - 1) / c.chunk : 1;
+  } else {
+    const int tile = kTileM / group;
+    const long long blocks = ((max_q <= 2 * tile ? 0 : total_q / (2 * tile)) + n_seq) * (long long)h->cfg.kv_heads;
+    const long long nb = (max_k + 127) / 128;
+    long long s = h->sm_count / blocks;
+    if (s > nb / 4) s = nb / 4;
+    c.splits = s > 1 ? (int)s : 1;
+  }
+  return c;
+}
+
+size_t workspace_of(const tra_packed* h, const Choice& c, int total_q) {
+  return c.splits > 1 ? sizeof(float) * (size_t)c.splits * total_q * h->cfg.heads * (h->cfg.head_dim + 2) : 0;
+}
+
+bool bad_sizes(const tra_packed* h, int n_seq, int total_q, int max_q, int max_k) {
+  return !h || n_seq < 1 || total_q < 0 || max_q < 0 || max_k < 0 || max_q > total_q;
+}
+
+// [tokens, heads, d] behind strides, viewed with the channels innermost; box = 64 channels x box_heads x box_tokens.
+int make_packed_map(CUtensorMap* map, const tra_packed* h, const void* base, const int64_t* stride, int heads, long long tokens,
+                    int box_heads, int box_tokens) {
+  encode_tiled_fn enc = get_encode_tiled();
+  if (!enc) return TRA_ERR_CUDA;
+  cuuint64_t dims[3] = {(cuuint64_t)h->cfg.head_dim, (cuuint64_t)heads, (cuuint64_t)tokens};
+  // the stride of a dimension of one entry is never used; a legal value keeps the encoder content
+  cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)stride[1] * 2 : 128u, tokens > 1 ? (cuuint64_t)stride[0] * 2 : 128u};
+  cuuint32_t box[3] = {64u, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+  cuuint32_t estr[3] = {1u, 1u, 1u};
+  const CUresult r = enc(map, h->cfg.dtype == TRA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                         const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? TRA_OK : TRA_ERR_CUDA;
+}
+
+// The stride of a dimension of one entry is never used; the others are positive multiples of 16 bytes.
+bool bad_tensor(const void* ptr, const int64_t* stride, long long tokens, int heads) {
+  if (tokens == 0) return false;
+  if (!ptr || ((uintptr_t)ptr & 15)) return true;
+  const long long n[2] = {tokens, heads};
+  for (int i = 0; i < 2; ++i)
+    if (n[i] > 1 && (stride[i] < 8 || (stride[i] & 7) || stride[i] >= (1ll << 38))) return true;
+  return false;
+}
+
+// Checks what the forward and the backward call share and fills the launch.
+int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_launch* p) {
+  if (!h || !a || bad_sizes(h, a->n_seq, a->total_q, a->max_q, a->max_k) || a->total_k < 0 || a->max_k > a->total_k)
+    return TRA_ERR_INVALID_ARG;
+  if (!a->cu_q || !a->k_begin || !a->k_end || !(a->sm_scale > 0.f) || a->sm_scale > 1e30f) return TRA_ERR_INVALID_ARG;
+  if (((uintptr_t)a->cu_q | (uintptr_t)a->k_begin | (uintptr_t)a->k_end | (uintptr_t)a->lse) & 3) return TRA_ERR_INVALID_ARG;
+  if (a->total_q > (1 << 30) || a->total_k > (1 << 30)) return TRA_ERR_UNSUPPORTED;
+  const int heads = h->cfg.heads, kv = h->cfg.kv_heads;
+  if (bad_tensor(a->q, a->q_stride, a->total_q, heads) || bad_tensor(a->o, a->o_stride, a->total_q, heads) ||
+      bad_tensor(a->k, a->k_stride, a->total_k, kv) || bad_tensor(a->v, a->v_stride, a->total_k, kv))
+    return TRA_ERR_INVALID_ARG;
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return TRA_ERR_CUDA;
+  if (device != h->device) return TRA_ERR_INVALID_ARG;
+  memset(p, 0, sizeof(*p));
+  p->q = a->q, p->k = a->k, p->v = a->v;
+  p->lse = a->lse;
+  for (int i = 0; i < 2; ++i) {
+    p->q_stride[i] = a->q_stride[i];
+    p->k_stride[i] = a->k_stride[i];
+    p->v_stride[i] = a->v_stride[i];
+    p->o_stride[i] = a->o_stride[i];
+  }
+  p->cu_q = a->cu_q, p->k_begin = a->k_begin, p->k_end = a->k_end;
+  p->n_seq = a->n_seq, p->total_q = a->total_q, p->total_k = a->total_k, p->max_q = a->max_q, p->max_k = a->max_k;
+  p->heads = h->cfg.heads, p->kv_heads = h->cfg.kv_heads, p->group = h->cfg.heads / h->cfg.kv_heads;
+  p->tile_tokens = kTileM / p->group;
+  p->causal = h->cfg.causal, p->splits = 1;
+  p->sm_scale = a->sm_scale;
+  p->status = h->d_status;
+  return TRA_OK;
+}
+
+template <typename T>
+void launch_join(const tra_packed* h, const tra_packed_launch& p, cudaStream_t stream) {
+  const unsigned blocks = (unsigned)((long long)p.total_q * p.heads);
+  if (h->cfg.head_dim == 128)
+    tra_packed_join_kernel<T, 128><<<blocks, 32 * kJoinWarps, 0, stream>>>(p);
+  else
+    tra_packed_join_kernel<T, 64><<<blocks, 32 * kJoinWarps, 0, stream>>>(p);
+}
+
+}  // namespace
+
+extern "C" int tra_packed_create(tra_packed_t** out, const tra_packed_config_t* cfg) {
+  if (!out || !cfg) return TRA_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (cfg->heads < 1 || cfg->kv_heads < 1 || cfg->heads % cfg->kv_heads) return TRA_ERR_INVALID_ARG;
+  if (cfg->dtype != TRA_BF16 && cfg->dtype != TRA_FP16) return TRA_ERR_INVALID_ARG;
+  if (cfg->head_dim != 64 && cfg->head_dim != 128) return TRA_ERR_UNSUPPORTED;
+  if (cfg->heads > 4096 || cfg->heads / cfg->kv_heads > kTileM) return TRA_ERR_UNSUPPORTED;
+  tra_packed* h = new (std::nothrow) tra_packed;
+  if (!h) return TRA_ERR_CAPACITY;
+  memset(h, 0, sizeof(*h));
+  h->cfg = *cfg;
+  h->cfg.causal = cfg->causal != 0;
+  if (cudaGetDevice(&h->device) != cudaSuccess ||
+      cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->device) != cudaSuccess ||
+      cudaMalloc(&h->d_status, sizeof(int)) != cudaSuccess || cudaMemset(h->d_status, 0, sizeof(int)) != cudaSuccess ||
+      cudaStreamSynchronize(nullptr) != cudaSuccess) {
+    cudaFree(h->d_status);
+    delete h;
+    return TRA_ERR_CUDA;
+  }
+  *out = h;
+  return TRA_OK;
+}
+
+extern "C" int tra_packed_destroy(tra_packed_t* h) {
+  if (!h) return TRA_ERR_INVALID_ARG;
+  cudaFree(h->d_status);
+  delete h;
+  return TRA_OK;
+}
+
+extern "C" int tra_packed_status(tra_packed_t* h, void* stream_) {
+  if (!h) return TRA_ERR_INVALID_ARG;
+  cudaStream_t stream = (cudaStream_t)stream_;
+  int code = 0;
+  TRA_CUDA_CHECK(cudaMemcpyAsync(&code, h->d_status, sizeof(int), cudaMemcpyDeviceToHost, stream));
+  TRA_CUDA_CHECK(cudaMemsetAsync(h->d_status, 0, sizeof(int), stream));
+  TRA_CUDA_CHECK(cudaStreamSynchronize(stream));
+  return code;
+}
+
+extern "C" size_t tra_packed_attn_workspace_bytes(const tra_packed_t* h, int n_seq, int total_q, int max_q, int max_k) {
+  if (bad_sizes(h, n_seq, total_q, max_q, max_k)) return 0;
+  return workspace_of(h, choose(h, n_seq, total_q, max_q, max_k), total_q);
+}
+
+extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes,
+                               void* stream_) {
+  tra_packed_launch p;
+  int rc = begin_launch(h, a, &p);
+  if (rc != TRA_OK) return rc;
+  if (a->max_q == 0) return TRA_OK;                        // no query at all
+  const tra_packed_ctx ctx = {h, (cudaStream_t)stream_};
+  p.o = a->o;
+  const Choice c = choose(h, a->n_seq, a->total_q, a->max_q, a->max_k);
+  if (c.splits > 65535) return TRA_ERR_UNSUPPORTED;
+  p.splits = c.splits;
+  if (c.splits > 1) {
+    if ((long long)a->total_q * p.heads > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
+    if (!workspace || ((uintptr_t)workspace & 15)) return TRA_ERR_INVALID_ARG;
+    if (workspace_bytes < workspace_of(h, c, a->total_q)) return TRA_ERR_CAPACITY;
+    const long long rows = (long long)c.splits * a->total_q * p.heads;
+    p.part_o = (float*)workspace;
+    p.part_lse2 = p.part_o + rows * h->cfg.head_dim;
+    p.part_exact = a->lse ? p.part_lse2 + rows : nullptr;
+  }
+  const int key_box = c.rows ? 64 : 128;
+  // without keys no tile is loaded; the maps then describe the queries
+  const void *kk = a->total_k > 0 ? a->k : a->q, *vv = a->total_k > 0 ? a->v : a->q;
+  const int64_t *ks = a->total_k > 0 ? a->k_stride : a->q_stride, *vs = a->total_k > 0 ? a->v_stride : a->q_stride;
+  const long long tk = a->total_k > 0 ? a->total_k : a->total_q;
+  if ((rc = make_packed_map(&p.map_k, h, kk, ks, p.kv_heads, tk, 1, key_box)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p.map_v, h, vv, vs, p.kv_heads, tk, 1, key_box)) != TRA_OK) return rc;
+  if (c.rows) {
+    rc = tra_packed_rows(ctx, p, c.chunk);
+  } else {
+    if ((rc = make_packed_map(&p.map_q, h, a->q, a->q_stride, p.heads, a->total_q, p.group, p.tile_tokens)) != TRA_OK) return rc;
+    p.n_units = (a->max_q <= 2 * p.tile_tokens ? 0 : a->total_q / (2 * p.tile_tokens)) + a->n_seq;
+    rc = h->cfg.head_dim == 128 ? tra_packed_fwd_d128(ctx, p) : tra_packed_fwd_d64(ctx, p);
+  }
+  if (rc != TRA_OK || c.splits == 1) return rc;
+  if (h->cfg.dtype == TRA_BF16)
+    launch_join<__nv_bfloat16>(h, p, ctx.stream);
+  else
+    launch_join<__half>(h, p, ctx.stream);
+  TRA_CUDA_CHECK(cudaGetLastError());
+  return TRA_OK;
+}

@@ -1,0 +1,94 @@
+// Kernel arguments of the packed-attention launches, where a thread block finds its sequence, and the per-shape
+// launchers (one translation unit per kernel and head_dim, so that they compile in parallel).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "tra.h"
+
+struct tra_packed {
+  tra_packed_config_t cfg;
+  int device, sm_count;
+  int* d_status;
+};
+
+// One launch, as the kernels see it.  Rows of a (sequence, key/value head) are its tokens times the `group` query
+// heads that share the key/value head, token-major: row r of a tile is token r / group, head r % group.
+struct tra_packed_launch {
+  CUtensorMap map_q, map_k, map_v, map_do;   // boxes: 64 channels x (group heads x tile tokens | 1 head x 128 tokens)
+  const void *q, *k, *v, *o_in, *d_o;
+  void *o, *dq, *dk, *dv;
+  float* lse;                  // forward: written or NULL; backward: read
+  float* part_o;               // forward, split over the keys: [splits][total_q][heads][d]
+  float* part_lse2;            //   [splits][total_q][heads] base-2 log of the sum the part was divided by
+  float* part_exact;           //   [splits][total_q][heads] base-2 log of the unrounded sum (lse asked for) or NULL
+  float* delta;                // backward: [total_q][heads] sum of dO O
+  long long q_stride[2], k_stride[2], v_stride[2], o_stride[2], do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2];
+  const int32_t *cu_q, *k_begin, *k_end;
+  int n_seq, total_q, total_k, max_q, max_k;
+  int heads, kv_heads, group, tile_tokens;   // tile_tokens = 128 / group: query tokens of a 128-row tile
+  int causal, splits, n_units;               // n_units: query-tile pairs (forward) or key / query tiles (backward) launched
+  float sm_scale;
+  int* status;
+};
+
+struct tra_packed_ctx {
+  const tra_packed_t* h;
+  cudaStream_t stream;
+};
+
+int tra_packed_fwd_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_fwd_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk);
+
+#ifdef __CUDACC__
+namespace {
+
+// The token range of a sequence, brought inside the tensor and the stated maximum; what had to be cut is recorded.
+struct tra_seq_range {
+  int begin, len;
+};
+__device__ __forceinline__ tra_seq_range tra_clamp_range(int begin, int end, int total, int max_len, int* status) {
+  const int b = min(max(begin, 0), total);
+  const int e = min(max(end, b), total);
+  const int len = min(e - b, max_len);
+  if (b != begin || b + len != end) atomicCAS(status, 0, TRA_ERR_INVALID_ARG);
+  return {b, len};
+}
+
+// Which (sequence, unit) a thread block works on, units numbered sequence by sequence, ceil(length / unit_tokens)
+// each; one warp calls it.  seq = -1: past the last unit.  Lengths are read 32 sequences at a time.
+__device__ __forceinline__ void tra_find_unit(const int32_t* begin, const int32_t* end, int n_seq, int total, int max_len,
+                                              int unit_tokens, int unit, int* status, int& seq, int& index) {
+  const int lane = threadIdx.x & 31;
+  seq = -1;
+  index = 0;
+  int before = 0;
+  for (int s0 = 0; s0 < n_seq; s0 += 32) {
+    int n = 0;
+    if (s0 + lane < n_seq) {
+      const tra_seq_range r = tra_clamp_range(begin[s0 + lane], end[s0 + lane], total, max_len, status);
+      n = (r.len + unit_tokens - 1) / unit_tokens;
+    }
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    const int excl = before + incl - n;
+    const unsigned hit = __ballot_sync(0xffffffffu, unit >= excl && unit < before + incl);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      seq = s0 + l;
+      index = unit - __shfl_sync(0xffffffffu, excl, l);
+      return;
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+}
+
+}  // namespace
+#endif
