@@ -408,6 +408,21 @@ size_t tra_packed_attn_workspace_bytes(const tra_packed_t* packed, int n_seq, in
 int tra_packed_attn(const tra_packed_t* packed, const tra_packed_args_t* args, void* workspace, size_t workspace_bytes,
                     void* stream);
 
+/* Gradients of a forward call over PACKED keys (args->k_end must be args->k_begin + 1: ascending bounds, so that no key
+ * belongs to two sequences).  args as in the forward call, with its o and lse.  dq, dk, dv are written for the rows of the
+ * sequences (zeros where nothing is seen) and left alone elsewhere; sums of gradients that heads share are formed in fp32
+ * inside one thread block: no atomics, the same bits every time.  d_o outside the sequences may be anything.
+ *   workspace: device memory of tra_packed_attn_backward_workspace_bytes, as for the forward call. */
+typedef struct {
+  const void* d_o;        /* the gradient of o */
+  void *dq, *dk, *dv;     /* written           */
+  int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2];
+} tra_packed_grads_t;
+
+size_t tra_packed_attn_backward_workspace_bytes(const tra_packed_t* packed, int total_q);
+int tra_packed_attn_backward(const tra_packed_t* packed, const tra_packed_args_t* args, const tra_packed_grads_t* grads,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -39,7 +39,7 @@ EXPORTS = [
     "tra_rotary_create", "tra_rotary_destroy", "tra_rotary_forward", "tra_rotary_backward_workspace_bytes",
     "tra_rotary_backward",
     "tra_packed_create", "tra_packed_destroy", "tra_packed_status", "tra_packed_attn_workspace_bytes",
-    "tra_packed_attn",
+    "tra_packed_attn", "tra_packed_attn_backward_workspace_bytes", "tra_packed_attn_backward",
 ]
 
 
@@ -83,6 +83,11 @@ class tra_packed_args_t(ctypes.Structure):
         [(n, ctypes.c_int) for n in ("n_seq", "total_q", "total_k", "max_q", "max_k")] + [("sm_scale", ctypes.c_float)]
 
 
+class tra_packed_grads_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("d_o", "dq", "dk", "dv")] + \
+        [(n, ctypes.c_int64 * 2) for n in ("do_stride", "dq_stride", "dk_stride", "dv_stride")]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -123,6 +128,9 @@ def _load():
     lib.tra_packed_attn_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
     lib.tra_packed_attn_workspace_bytes.restype = ctypes.c_size_t
     lib.tra_packed_attn.argtypes = [vp, vp, vp, ctypes.c_size_t, vp]
+    lib.tra_packed_attn_backward_workspace_bytes.argtypes = [vp, i32]
+    lib.tra_packed_attn_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.tra_packed_attn_backward.argtypes = [vp, vp, vp, vp, ctypes.c_size_t, vp]
     return lib
 
 
@@ -698,3 +706,23 @@ class PackedAttn:
         ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
         _check(_lib.tra_packed_attn(self._h, ctypes.byref(a), ws.data_ptr() if n else None, n, _stream()), "tra_packed_attn")
         return o, lse
+
+    def backward(self, do, q, k, v, o, lse, cu_q, cu_k=None, *, max_q, max_k, dq=None, dk=None, dv=None, sm_scale=None):
+        """Gradients (dq, dk, dv) of ``forward`` over packed keys, from its o and lse.  Rows that belong to no sequence
+        are not written."""
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+        dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
+        if lse is None:
+            raise ValueError("lse: the forward call's, made with want_lse")
+        a = self._args(q, k, v, o, lse, cu_q, cu_k, None, max_q, max_k, sm_scale)
+        g = tra_packed_grads_t()
+        g.d_o, g.do_stride[:] = self._tensor(do, "do", a.total_q, self.heads)
+        g.dq, g.dq_stride[:] = self._tensor(dq, "dq", a.total_q, self.heads)
+        g.dk, g.dk_stride[:] = self._tensor(dk, "dk", a.total_k, self.kv_heads)
+        g.dv, g.dv_stride[:] = self._tensor(dv, "dv", a.total_k, self.kv_heads)
+        n = _lib.tra_packed_attn_backward_workspace_bytes(self._h, a.total_q)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+        _check(_lib.tra_packed_attn_backward(self._h, ctypes.byref(a), ctypes.byref(g), ws.data_ptr() if n else None, n,
+                                             _stream()), "tra_packed_attn_backward")
+        return dq, dk, dv

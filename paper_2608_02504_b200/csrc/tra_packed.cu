@@ -269,3 +269,50 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
   TRA_CUDA_CHECK(cudaGetLastError());
   return TRA_OK;
 }
+
+extern "C" size_t tra_packed_attn_backward_workspace_bytes(const tra_packed_t* h, int total_q) {
+  return h && total_q > 0 ? sizeof(float) * (size_t)total_q * h->cfg.heads : 0;
+}
+
+extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_args_t* a, const tra_packed_grads_t* g,
+                                        void* workspace, size_t workspace_bytes, void* stream_) {
+  tra_packed_launch p;
+  int rc = begin_launch(h, a, &p);
+  if (rc != TRA_OK) return rc;
+  // packed keys only: a key that two sequences share would have two gradients
+  if (!g || a->k_end != a->k_begin + 1 || (!a->lse && a->total_q > 0)) return TRA_ERR_INVALID_ARG;
+  if (bad_tensor(g->d_o, g->do_stride, a->total_q, p.heads) || bad_tensor(g->dq, g->dq_stride, a->total_q, p.heads) ||
+      bad_tensor(g->dk, g->dk_stride, a->total_k, p.kv_heads) || bad_tensor(g->dv, g->dv_stride, a->total_k, p.kv_heads))
+    return TRA_ERR_INVALID_ARG;
+  if ((long long)a->total_q * p.heads > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
+  if (a->total_q == 0 && a->total_k == 0) return TRA_OK;
+  if (a->total_q > 0) {
+    if (!workspace || ((uintptr_t)workspace & 15)) return TRA_ERR_INVALID_ARG;
+    if (workspace_bytes < tra_packed_attn_backward_workspace_bytes(h, a->total_q)) return TRA_ERR_CAPACITY;
+  }
+  p.delta = (float*)workspace;
+  p.o_in = a->o, p.d_o = g->d_o;
+  p.dq = g->dq, p.dk = g->dk, p.dv = g->dv;
+  for (int i = 0; i < 2; ++i) {
+    p.do_stride[i] = g->do_stride[i];
+    p.dq_stride[i] = g->dq_stride[i];
+    p.dk_stride[i] = g->dk_stride[i];
+    p.dv_stride[i] = g->dv_stride[i];
+  }
+  // a side without tokens is never loaded; its maps then describe the other side
+  const bool q = a->total_q > 0, k = a->total_k > 0;
+  if ((rc = make_packed_map(&p.map_q, h, q ? a->q : a->k, q ? a->q_stride : a->k_stride, q ? p.heads : p.kv_heads,
+                            q ? a->total_q : a->total_k, q ? p.group : 1, p.tile_tokens)) != TRA_OK)
+    return rc;
+  if ((rc = make_packed_map(&p.map_do, h, q ? g->d_o : a->k, q ? g->do_stride : a->k_stride, q ? p.heads : p.kv_heads,
+                            q ? a->total_q : a->total_k, q ? p.group : 1, p.tile_tokens)) != TRA_OK)
+    return rc;
+  if ((rc = make_packed_map(&p.map_k, h, k ? a->k : a->q, k ? a->k_stride : a->q_stride, p.kv_heads, k ? a->total_k : a->total_q, 1,
+                            kTileM)) != TRA_OK)
+    return rc;
+  if ((rc = make_packed_map(&p.map_v, h, k ? a->v : a->q, k ? a->v_stride : a->q_stride, p.kv_heads, k ? a->total_k : a->total_q, 1,
+                            kTileM)) != TRA_OK)
+    return rc;
+  const tra_packed_ctx ctx = {h, (cudaStream_t)stream_};
+  return h->cfg.head_dim == 128 ? tra_packed_bwd_d128(ctx, p) : tra_packed_bwd_d64(ctx, p);
+}

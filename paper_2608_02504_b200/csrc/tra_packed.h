@@ -41,6 +41,8 @@ struct tra_packed_ctx {
 
 int tra_packed_fwd_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_fwd_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_bwd_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_bwd_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk);
 
 #ifdef __CUDACC__

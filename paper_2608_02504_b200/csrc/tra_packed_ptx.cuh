@@ -47,6 +47,20 @@ __device__ __forceinline__ void add_pair<__half>(float& acc_lo, float& acc_hi, u
       : "r"(packed));
 }
 
+template <typename T>
+__device__ __forceinline__ void unpack_pair(uint32_t packed, float& lo, float& hi);
+template <>
+__device__ __forceinline__ void unpack_pair<__nv_bfloat16>(uint32_t packed, float& lo, float& hi) {
+  lo = __uint_as_float(packed << 16);
+  hi = __uint_as_float(packed & 0xffff0000u);
+}
+template <>
+__device__ __forceinline__ void unpack_pair<__half>(uint32_t packed, float& lo, float& hi) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&packed));
+  lo = f.x;
+  hi = f.y;
+}
+
 // Zeroes rows [row0, row1) of `atoms` 64-column pieces of a tile, rows 128 bytes apart (the 128-byte swizzle moves
 // 16-byte chunks inside a row only).
 __device__ __forceinline__ void zero_tile_rows(uint8_t* tile, int row0, int row1, int atoms, int atom_bytes, int tid,
