@@ -17,8 +17,8 @@
 // Bound: HBM.  Every element is read once and written once (the norm's backward pass reads x too); a row stays
 // in the registers of d / 16 neighbouring threads, 16 channels each (a 16-byte piece of either half of the row
 // for 16-bit types, so that both ways of pairing channels find their partner in the same thread and a row is
-// read in whole 128-byte lines), and its sums are shuffles among those threads.  The angles of a token are
-// computed once per thread and used for all the heads it walks.  The weights' gradients stay in
+// read in whole 128-byte lines), and its sums are shuffles among those threads.  The cosines and sines of a block's
+// tokens are computed once, into shared memory, and used for all heads.  The weights' gradients stay in
 // registers over a thread's rows, are added up per thread block in a fixed order, and a second small kernel
 // adds the blocks: no atomics, the same bits every time.
 #include <cuda_bf16.h>
@@ -52,7 +52,7 @@ struct RotTensor {
   const void* bias;
   float* partial;        // backward: [2][blocks][d] of this tensor, or NULL
   long long src_stride[3], dst_stride[3], x_stride[3];      // batch, token, head (elements)
-  int heads, rotate, tile_major, head_slots;
+  int heads, rotate, tile_major;
 };
 
 struct RotArgs {
@@ -63,9 +63,11 @@ struct RotArgs {
   const int32_t* pos;             // explicit positions [tokens][n_axes], or NULL
   int n_axes, H, W, n_video;      // grid positions: token n -> (n / (H W), n / W % H, n % W)
   int d, lanes;                   // lanes: threads per row, d / 16 rounded up to a power of two
+  int n_tensors, one_tensor;      // one_tensor: a block works on the tensor blockIdx.y, else on all of them
+  int by_source;                  // !one_tensor: the rotated tensors are tile-major
+  int head_slots;                 // heads of a token side by side in a block
   float eps, inv_d;
-  long long rows;                 // batch * tokens
-  int tokens;
+  int rows, tokens;               // rows = batch * tokens
 };
 
 template <typename T>
@@ -134,54 +136,80 @@ __device__ __forceinline__ float row_sum(float s, int lanes) {
   return s;
 }
 
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_float(float x) { return x; }
+// z[0 .. 7] times, or plus, eight values in shared memory
+__device__ __forceinline__ void times8(float* z, const float* s) {
+  const float4 a = reinterpret_cast<const float4*>(s)[0], b = reinterpret_cast<const float4*>(s)[1];
+  z[0] *= a.x, z[1] *= a.y, z[2] *= a.z, z[3] *= a.w, z[4] *= b.x, z[5] *= b.y, z[6] *= b.z, z[7] *= b.w;
+}
+__device__ __forceinline__ void plus8(float* z, const float* s) {
+  const float4 a = reinterpret_cast<const float4*>(s)[0], b = reinterpret_cast<const float4*>(s)[1];
+  z[0] += a.x, z[1] += a.y, z[2] += a.z, z[3] += a.w, z[4] += b.x, z[5] += b.y, z[6] += b.z, z[7] += b.w;
+}
+
 // Channel c of the thread's sixteen: 0 .. 7 in the lower half of the row, 8 .. 15 in the upper half.  Pair j (0 .. 7) of the
-// thread: (j, j + 8) when channels pair across the halves, (2 j, 2 j + 1) otherwise.
+// thread: (j, j + 8) when channels pair across the halves, (2 j, 2 j + 1) otherwise.  cs, sn: the token's cosines and sines
+// by pair, in shared memory.
 template <bool kHalves>
-__device__ __forceinline__ void turn_pairs(float* z, const float* cs, const float* sn, float sign) {
+__device__ __forceinline__ void turn_pairs(float* z, const float* cs, const float* sn, int c_lo, int c_hi, float sign) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    float& a = z[kHalves ? j : 2 * j];
-    float& b = z[kHalves ? j + 8 : 2 * j + 1];
-    const float s = sign * sn[j];
-    const float ta = a * cs[j] - b * s, tb = a * s + b * cs[j];
-    a = ta;
-    b = tb;
+  for (int q = 0; q < 2; ++q) {
+    const int pair = kHalves ? c_lo + 4 * q : (q ? c_hi : c_lo) / 2;
+    const float4 c4 = *reinterpret_cast<const float4*>(cs + pair), s4 = *reinterpret_cast<const float4*>(sn + pair);
+    const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = 4 * q + i;
+      float& x = z[kHalves ? j : 2 * j];
+      float& y = z[kHalves ? j + 8 : 2 * j + 1];
+      const float si = sign * s[i];
+      const float tx = x * c[i] - y * si, ty = x * si + y * c[i];
+      x = tx;
+      y = ty;
+    }
   }
 }
 
+// The token a thread works on: its index in the batch entry on the attention side (ordered) and on the projection side.
+struct Token {
+  int batch, ordered, source;
+  bool there;
+};
+
+// A block takes groups of tokens_per_block tokens: the same number of threads for every token, each walking every
+// head_slots-th head of the block's tensors (all of them one after the other, or the one blockIdx.y names).  Loads run one row
+// ahead of the arithmetic, across heads, tensors and groups; the angles of the next group go to the other half of s_turn
+// behind the current group's rows, so that a group costs one barrier and no exposed load.
 template <typename T, int kNorm, bool kHalves, bool kBackward>
-__global__ void __launch_bounds__(kThreads) tra_rotary_kernel(const __grid_constant__ RotArgs p) {
-  __shared__ uint64_t s_turn[kMaxD / 2];
-  __shared__ uint8_t s_axis[kMaxD / 2];
-  __shared__ float s_red[kBackward && kNorm ? kThreads / 32 : 1][kBackward && kNorm ? kMaxD : 1];
-  const RotTensor& t = p.t[blockIdx.y];
+__global__ void __launch_bounds__(kThreads, kBackward && kNorm != TRA_NORM_NONE ? 2 : 4)
+tra_rotary_kernel(const __grid_constant__ RotArgs p) {
+  constexpr bool kSums = kBackward && kNorm != TRA_NORM_NONE;
+  // [buffer][cosines, then sines][token of the group][pair]: tokens_per_block * d / 2 <= 8 * kThreads
+  __shared__ __align__(16) float s_turn[2][16 * kThreads];
+  __shared__ __align__(16) float s_weight[kNorm != TRA_NORM_NONE ? 3 * kMaxD : 4], s_bias[kNorm == TRA_NORM_LAYER ? 3 * kMaxD : 4];
   const int tid = threadIdx.x;
-  for (int i = tid; i < p.d / 2; i += kThreads) {
-    s_turn[i] = p.turn[i];
-    s_axis[i] = p.axis[i];
-  }
-  __syncthreads();
   const int lane = tid % p.lanes, slot = tid / p.lanes;
   const bool on = lane * 16 < p.d;                     // d / 16 need not be a power of two
   const int c_lo = lane * 8, c_hi = p.d / 2 + lane * 8;
-  const int head0 = slot % t.head_slots;
-  const int tokens_per_block = kThreads / p.lanes / t.head_slots;
-  const bool rotate = t.rotate != 0;
-  const bool normed = kNorm != TRA_NORM_NONE && rotate;
+  const int head0 = slot % p.head_slots, token_slot = slot / p.head_slots;
+  const int tokens_per_block = kThreads / p.lanes / p.head_slots;
+  const int pairs = p.d / 2, sines = tokens_per_block * pairs;
+  const int t_first = p.one_tensor ? (int)blockIdx.y : 0, t_end = p.one_tensor ? t_first + 1 : p.n_tensors;
+  const bool by_source = p.one_tensor ? p.t[t_first].tile_major != 0 : p.by_source != 0;
+  const bool turns_any = !p.one_tensor || p.t[t_first].rotate;
 
-  Piece<T> w_lo, w_hi, b_lo, b_hi;
-  const bool has_w = normed && t.weight != nullptr && on;
-  const bool has_b = !kBackward && normed && t.bias != nullptr && on;
-  if (has_w) {
-    w_lo.load((const T*)t.weight + c_lo);
-    w_hi.load((const T*)t.weight + c_hi);
+  if (kNorm != TRA_NORM_NONE) {
+    for (int i = tid; i < 3 * p.d; i += kThreads) {
+      const int k = i / p.d, c = i - k * p.d;
+      if (k < t_first || k >= t_end) continue;
+      if (p.t[k].weight) s_weight[k * kMaxD + c] = to_float(((const T*)p.t[k].weight)[c]);
+      if (kNorm == TRA_NORM_LAYER && !kBackward && p.t[k].bias) s_bias[k * kMaxD + c] = to_float(((const T*)p.t[k].bias)[c]);
+    }
   }
-  if (has_b) {
-    b_lo.load((const T*)t.bias + c_lo);
-    b_hi.load((const T*)t.bias + c_hi);
-  }
-  float acc_w[kBackward && kNorm ? 16 : 1], acc_b[kBackward && kNorm == TRA_NORM_LAYER ? 16 : 1];
-  if (kBackward && kNorm) {
+  float acc_w[kSums ? 16 : 1], acc_b[kSums && kNorm == TRA_NORM_LAYER ? 16 : 1];
+  if (kSums) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       acc_w[i] = 0.f;
@@ -189,190 +217,210 @@ __global__ void __launch_bounds__(kThreads) tra_rotary_kernel(const __grid_const
     }
   }
 
+  auto locate = [&](int base) -> Token {
+    Token k = {0, 0, 0, base + token_slot < p.rows};
+    if (k.there) {
+      k.ordered = base + token_slot;
+      if (p.tokens != p.rows) {
+        k.batch = k.ordered / p.tokens;
+        k.ordered -= k.batch * p.tokens;
+      }
+      // tensors that are not tile-major ignore the source index
+      k.source = p.raster_of_pos != nullptr && k.ordered < p.n_video ? __ldg(p.raster_of_pos + k.ordered) : k.ordered;
+    }
+    return k;
+  };
+  // cosines and sines of a token, shared out over its threads
+  auto angles = [&](const Token& k, float* turn) {
+    if (!k.there || !turns_any) return;
+    // positions belong to the projection side, which is the ordered index of a tensor that is not tile-major
+    const int tok = by_source ? k.source : k.ordered;
+    int frame = 0, y = 0, x = 0;
+    if (p.pos == nullptr) {
+      const int hw = p.H * p.W;
+      frame = tok / hw;
+      const int in_frame = tok - frame * hw;
+      y = in_frame / p.W;
+      x = in_frame - y * p.W;
+    }
+    const bool turned = p.pos != nullptr || tok < p.n_video;           // text keeps its channels
+    for (int pair = head0 * p.lanes + lane; pair < pairs; pair += p.head_slots * p.lanes) {
+      float c = 1.f, sine = 0.f;
+      if (turned) {
+        const int axis = p.axis[pair];
+        const int v = p.pos != nullptr ? __ldg(p.pos + (long long)tok * p.n_axes + axis) : axis == 0 ? frame : axis == 1 ? y : x;
+        const uint64_t turns = (uint64_t)(int64_t)v * p.turn[pair];
+        sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f /* 2^-31 */, &sine, &c);
+      }
+      turn[token_slot * pairs + pair] = c;
+      turn[sines + token_slot * pairs + pair] = sine;
+    }
+  };
+
+  Piece<T> lo, hi, xlo, xhi;
+  auto fetch = [&](const Token& k, int ti, int h) {
+    const RotTensor& t = p.t[ti];
+    if (k.there && on && h < t.heads) {
+      // forward reads at the source row and writes at the ordered one, backward the other way round
+      const int source = t.tile_major ? k.source : k.ordered;
+      const T* in = (const T*)t.src + k.batch * t.src_stride[0] + (kBackward ? k.ordered : source) * t.src_stride[1] + h * t.src_stride[2];
+      lo.load(in + c_lo);
+      hi.load(in + c_hi);
+      if (kSums && t.rotate) {
+        const T* x = (const T*)t.x + k.batch * t.x_stride[0] + source * t.x_stride[1] + h * t.x_stride[2];
+        xlo.load(x + c_lo);
+        xhi.load(x + c_hi);
+      }
+    } else {
+      lo.zero();
+      hi.zero();
+      if (kSums) {
+        xlo.zero();
+        xhi.zero();
+      }
+    }
+  };
+
+  const int stride = (int)gridDim.x * tokens_per_block;
+  int base = (int)blockIdx.x * tokens_per_block;
+  Token cur = locate(base);
+  fetch(cur, t_first, head0);
+  angles(cur, s_turn[0]);
+  __syncthreads();
+  int buffer = 0;
   // All threads of a warp walk the same number of rows (row sums are warp-wide shuffles): a thread whose token or head
   // does not exist takes part with zeros.
-  for (long long base = (long long)blockIdx.x * tokens_per_block; base < p.rows;
-       base += (long long)gridDim.x * tokens_per_block) {
-    const long long row = base + slot / t.head_slots;
-    const bool token_on = on && row < p.rows;
-    long long batch = 0;
-    int pos_idx = 0, src_tok = 0;
-    if (token_on) {
-      batch = row / p.tokens;
-      pos_idx = (int)(row - batch * p.tokens);
-      src_tok = t.tile_major && pos_idx < p.n_video ? __ldg(p.raster_of_pos + pos_idx) : pos_idx;
-    }
-    float cs[8], sn[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      cs[j] = 1.f;
-      sn[j] = 0.f;
-    }
-    if (rotate && token_on && (p.pos != nullptr || src_tok < p.n_video)) {
-      int axis_pos[4] = {0, 0, 0, 0};
-      if (p.pos != nullptr) {
-        for (int a = 0; a < p.n_axes; ++a) {
-          const int v = __ldg(p.pos + (long long)src_tok * p.n_axes + a);
-          if (a == 0) axis_pos[0] = v;
-          if (a == 1) axis_pos[1] = v;
-          if (a == 2) axis_pos[2] = v;
-          if (a == 3) axis_pos[3] = v;
-        }
-      } else {
-        const int hw = p.H * p.W;
-        axis_pos[0] = src_tok / hw;
-        const int in_frame = src_tok - axis_pos[0] * hw;
-        axis_pos[1] = in_frame / p.W;
-        axis_pos[2] = in_frame - axis_pos[1] * p.W;
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int pair = kHalves ? c_lo + j : (j < 4 ? c_lo / 2 + j : c_hi / 2 + j - 4);
-        const int a = s_axis[pair];
-        const int v = a == 0 ? axis_pos[0] : a == 1 ? axis_pos[1] : a == 2 ? axis_pos[2] : axis_pos[3];
-        const uint64_t turns = (uint64_t)(int64_t)v * s_turn[pair];
-        const float half_turns = (float)(int32_t)(turns >> 32) * 4.656612873077393e-10f;      // 2^-31
-        sincospif(half_turns, &sn[j], &cs[j]);
-      }
-    }
-    // forward reads at the source row and writes at the ordered one, backward the other way round
-    const int in_tok = kBackward ? pos_idx : src_tok, out_tok = kBackward ? src_tok : pos_idx;
-    const T* in = (const T*)t.src + batch * t.src_stride[0] + (long long)in_tok * t.src_stride[1];
-    T* out = (T*)t.dst + batch * t.dst_stride[0] + (long long)out_tok * t.dst_stride[1];
-    const T* xin = kBackward && normed ? (const T*)t.x + batch * t.x_stride[0] + (long long)out_tok * t.x_stride[1] : nullptr;
-
-    Piece<T> lo, hi, xlo, xhi;
-    auto fetch = [&](int h) {
-      if (token_on && h < t.heads) {
-        lo.load(in + h * t.src_stride[2] + c_lo);
-        hi.load(in + h * t.src_stride[2] + c_hi);
-        if (kBackward && normed) {
-          xlo.load(xin + h * t.x_stride[2] + c_lo);
-          xhi.load(xin + h * t.x_stride[2] + c_hi);
-        }
-      } else {
-        lo.zero();
-        hi.zero();
-        if (kBackward && normed) {
-          xlo.zero();
-          xhi.zero();
-        }
-      }
-    };
-    const int steps = (t.heads + t.head_slots - 1) / t.head_slots;
-    fetch(head0);
-    for (int step = 0; step < steps; ++step) {
-      const int h = head0 + step * t.head_slots;
-      const bool row_on = token_on && h < t.heads;
-      float z[16];
-      lo.get(z);
-      hi.get(z + 8);
-      if (!kBackward) {
-        if (step + 1 < steps) fetch(h + t.head_slots);       // the next head's row while this one is worked on
-        if (normed) {
-          float mean = 0.f;
-          if (kNorm == TRA_NORM_LAYER) {
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s += z[i];
-            mean = row_sum(s, p.lanes) * p.inv_d;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = on ? z[i] - mean : 0.f;
-          }
-          float q = 0.f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) q = fmaf(z[i], z[i], q);
-          const float r = rsqrtf(fmaf(row_sum(q, p.lanes), p.inv_d, p.eps));
-          float w[16];
-          if (has_w) {
-            w_lo.get(w);
-            w_hi.get(w + 8);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = z[i] * r * w[i];
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] *= r;
-          }
-          if (has_b) {
-            b_lo.get(w);
-            b_hi.get(w + 8);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] += w[i];
-          }
-        }
-        if (rotate) turn_pairs<kHalves>(z, cs, sn, 1.f);
-      } else {
-        float n[16];
-        if (normed) {
+  while (true) {
+    const bool more = p.rows - base > stride;          // base + stride < rows
+    const Token next = more ? locate(base + stride) : Token{0, 0, 0, false};
+    const float* const cs = s_turn[buffer] + token_slot * pairs;
+    const float* const sn = cs + sines;
+    for (int ti = t_first; ti < t_end; ++ti) {
+      const RotTensor& t = p.t[ti];
+      const bool rotate = t.rotate != 0, normed = kNorm != TRA_NORM_NONE && rotate;
+      const bool has_w = normed && t.weight != nullptr;
+      const bool has_b = !kBackward && kNorm == TRA_NORM_LAYER && normed && t.bias != nullptr;
+      const int heads = t.heads;
+      for (int h = head0; h - head0 < heads; h += p.head_slots) {
+        const bool row_on = cur.there && on && h < heads;
+        float z[16];
+        lo.get(z);
+        hi.get(z + 8);
+        float n[kSums ? 16 : 1];
+        if constexpr (kSums) {
           xlo.get(n);
           xhi.get(n + 8);
         }
-        if (step + 1 < steps) fetch(h + t.head_slots);
-        if (rotate) turn_pairs<kHalves>(z, cs, sn, -1.f);      // z = u
-        if (normed) {
-          if (kNorm == TRA_NORM_LAYER) {
-            float s = 0.f;
+        // the next row, while this one is worked on
+        if (h - head0 + p.head_slots < heads)
+          fetch(cur, ti, h + p.head_slots);
+        else if (ti + 1 < t_end)
+          fetch(cur, ti + 1, head0);
+        else
+          fetch(next, t_first, head0);
+        if (!kBackward) {
+          if (normed) {
+            if (kNorm == TRA_NORM_LAYER) {
+              float s = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s += n[i];
-            const float mean = row_sum(s, p.lanes) * p.inv_d;
+              for (int i = 0; i < 16; ++i) s += z[i];
+              const float mean = row_sum(s, p.lanes) * p.inv_d;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) n[i] = on ? n[i] - mean : 0.f;
+              for (int i = 0; i < 16; ++i) z[i] = on ? z[i] - mean : 0.f;
+            }
+            float q = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) q = fmaf(z[i], z[i], q);
+            const float r = rsqrtf(fmaf(row_sum(q, p.lanes), p.inv_d, p.eps));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] *= r;
+            if (has_w && on) {
+              times8(z, s_weight + ti * kMaxD + c_lo);
+              times8(z + 8, s_weight + ti * kMaxD + c_hi);
+            }
+            if (has_b && on) {
+              plus8(z, s_bias + ti * kMaxD + c_lo);
+              plus8(z + 8, s_bias + ti * kMaxD + c_hi);
+            }
           }
-          float q = 0.f;
+          if (rotate && on) turn_pairs<kHalves>(z, cs, sn, c_lo, c_hi, 1.f);
+        } else {
+          if (rotate && on) turn_pairs<kHalves>(z, cs, sn, c_lo, c_hi, -1.f);      // z = u
+          if constexpr (kSums) {
+            if (normed) {
+              if (kNorm == TRA_NORM_LAYER) {
+                float s = 0.f;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) q = fmaf(n[i], n[i], q);
-          const float r = rsqrtf(fmaf(row_sum(q, p.lanes), p.inv_d, p.eps));
-          float w[16];
-          if (has_w) {
-            w_lo.get(w);
-            w_hi.get(w + 8);
-          } else {
+                for (int i = 0; i < 16; ++i) s += n[i];
+                const float mean = row_sum(s, p.lanes) * p.inv_d;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = 1.f;
+                for (int i = 0; i < 16; ++i) n[i] = on ? n[i] - mean : 0.f;
+              }
+              float q = 0.f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) q = fmaf(n[i], n[i], q);
+              const float r = rsqrtf(fmaf(row_sum(q, p.lanes), p.inv_d, p.eps));
+              float sg = 0.f, sgn = 0.f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                n[i] *= r;
+                // a row that does not exist is left out (eps = 0 would make 0 * inf of it)
+                acc_w[i] += row_on ? z[i] * n[i] : 0.f;
+                if (kNorm == TRA_NORM_LAYER) acc_b[i] += row_on ? z[i] : 0.f;
+              }
+              if (has_w && on) {                                     // g
+                times8(z, s_weight + ti * kMaxD + c_lo);
+                times8(z + 8, s_weight + ti * kMaxD + c_hi);
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                sg += z[i];
+                sgn = fmaf(z[i], n[i], sgn);
+              }
+              const float mgn = row_sum(sgn, p.lanes) * p.inv_d;
+              const float mg = kNorm == TRA_NORM_LAYER ? row_sum(sg, p.lanes) * p.inv_d : 0.f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) z[i] = r * (z[i] - mg - n[i] * mgn);
+            }
           }
-          float sg = 0.f, sgn = 0.f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            n[i] *= r;
-            // a row that does not exist is left out (eps = 0 would make 0 * inf of it)
-            acc_w[i] += row_on ? z[i] * n[i] : 0.f;
-            if (kNorm == TRA_NORM_LAYER) acc_b[i] += row_on ? z[i] : 0.f;
-            z[i] *= w[i];                                       // g
-            sg += z[i];
-            sgn = fmaf(z[i], n[i], sgn);
-          }
-          const float mgn = row_sum(sgn, p.lanes) * p.inv_d;
-          const float mg = kNorm == TRA_NORM_LAYER ? row_sum(sg, p.lanes) * p.inv_d : 0.f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) z[i] = r * (z[i] - mg - n[i] * mgn);
+        }
+        if (row_on) {
+          const int source = t.tile_major ? cur.source : cur.ordered;
+          T* out = (T*)t.dst + cur.batch * t.dst_stride[0] + (kBackward ? source : cur.ordered) * t.dst_stride[1] + h * t.dst_stride[2];
+          Piece<T>::store(out + c_lo, z);
+          Piece<T>::store(out + c_hi, z + 8);
         }
       }
-      if (row_on) {
-        Piece<T>::store(out + h * t.dst_stride[2] + c_lo, z);
-        Piece<T>::store(out + h * t.dst_stride[2] + c_hi, z + 8);
-      }
     }
+    if (!more) break;
+    buffer ^= 1;
+    angles(next, s_turn[buffer]);
+    __syncthreads();
+    base += stride;
+    cur = next;
   }
 
-  if constexpr (kBackward && kNorm != TRA_NORM_NONE) {
+  if constexpr (kSums) {
+    const RotTensor& t = p.t[t_first];
     if (t.partial == nullptr) return;
     // threads of the same lane hold the same channels: add them over the warp, then over the block's warps in order
-    constexpr int kSums = kNorm == TRA_NORM_LAYER ? 2 : 1;
+    float* s_red = s_turn[0];                          // [warp][d], d <= 256
     const int warp = tid >> 5;
+    __syncthreads();
 #pragma unroll
-    for (int which = 0; which < kSums; ++which) {
+    for (int which = 0; which < (kNorm == TRA_NORM_LAYER ? 2 : 1); ++which) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         float v = acc_w[i];
         if constexpr (kNorm == TRA_NORM_LAYER)
           if (which == 1) v = acc_b[i];
         for (int o = p.lanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if ((tid & 31) < p.lanes && on) s_red[warp][i < 8 ? c_lo + i : c_hi + i - 8] = v;
+        if ((tid & 31) < p.lanes && on) s_red[warp * p.d + (i < 8 ? c_lo + i : c_hi + i - 8)] = v;
       }
       __syncthreads();
       for (int c = tid; c < p.d; c += kThreads) {
         float v = 0.f;
-        for (int k = 0; k < kThreads / 32; ++k) v += s_red[k][c];
+        for (int k = 0; k < kThreads / 32; ++k) v += s_red[k * p.d + c];
         t.partial[((long long)which * gridDim.x + blockIdx.x) * p.d + c] = v;
       }
       __syncthreads();
@@ -408,8 +456,9 @@ int lanes_of(int d) {
   return l;
 }
 
-// Blocks of a backward launch: up to four per SM, so that the weights' partial sums stay few.
-constexpr int kBackwardBlocksMax = 592;
+// Blocks of a launch, per tensor of a backward launch: what fits 148 SMs at once.
+constexpr int kForwardBlocksMax = 4 * 148;
+constexpr int kBackwardBlocksMax = 2 * 148;
 
 int elem_bytes(int dtype) { return dtype == TRA_FP32 ? 4 : 2; }
 
@@ -450,9 +499,11 @@ int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const
   }
   RotArgs a;
   memset(&a, 0, sizeof(a));
-  bool any_rotate = false, grads = false;
+  bool any_rotate = false, mixed = false, grads = false;
+  int common = 0, most_heads = 1;
   const int lanes = lanes_of(rot->head_dim);
-  const long long rows = (long long)B * tokens;
+  if ((long long)B * tokens > (1 << 30)) return TRA_ERR_UNSUPPORTED;
+  const int rows = B * tokens;
   for (int i = 0; i < n_tensors; ++i) {
     const tra_rotary_tensor_t& s = tensors[i];
     RotTensor& t = a.t[i];
@@ -470,7 +521,6 @@ int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const
     if (!aligned_strides(s.src_stride, dtype) || !aligned_strides(s.dst_stride, dtype) ||
         (s.x && !aligned_strides(s.x_stride, dtype)))
       return TRA_ERR_INVALID_ARG;
-    any_rotate |= t.rotate != 0;
     grads |= s.weight_grad != nullptr || s.bias_grad != nullptr;
     t.src = s.src, t.dst = s.dst, t.x = s.x, t.weight = s.weight, t.bias = s.bias;
     for (int k = 0; k < 3; ++k) {
@@ -479,21 +529,33 @@ int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const
       t.x_stride[k] = s.x_stride[k];
     }
     t.heads = s.heads;
-    // Heads side by side in a block: a power of two that divides the heads (no idle threads), at most 8 so that a token's
-    // angles are reused; with few tokens all heads side by side, so that the launch still fills the GPU.
-    const int slots = kThreads / lanes;
-    int hs = 1;
-    while (hs < 8 && hs < slots && s.heads % (2 * hs) == 0) hs *= 2;
-    if (rows * hs * lanes < 148 * 1024)
-      while (hs < slots && hs < s.heads) hs *= 2;
-    t.head_slots = hs;
+    common |= s.heads;
+    if (s.heads > most_heads) most_heads = s.heads;
+    if (t.rotate) {
+      mixed |= any_rotate && a.by_source != t.tile_major;
+      a.by_source = t.tile_major;
+      any_rotate = true;
+    }
   }
+  // Heads side by side in a block: a power of two that divides the heads of every tensor (no idle threads), at most 8, so
+  // that a token's angles serve many rows.  With few tokens one block per tensor and all heads side by side, so that the
+  // launch still fills the GPU (148 SMs of 1024 threads).
+  const int slots = kThreads / lanes;
+  int hs = 1;
+  while (hs < 8 && hs < slots && common % (2 * hs) == 0) hs *= 2;
+  const bool few = (long long)rows * hs * lanes < 148 * 1024;
+  if (few)
+    while (hs < slots && hs < most_heads) hs *= 2;
+  a.head_slots = hs;
+  // the weights' sums of a backward launch stay in registers: one tensor per block
+  a.one_tensor = few || mixed || (backward && rot->norm != TRA_NORM_NONE);
   if (any_rotate && !pos && !plan) return TRA_ERR_INVALID_ARG;
   memcpy(a.turn, rot->turn, sizeof(a.turn));
   memcpy(a.axis, rot->axis, sizeof(a.axis));
   a.raster_of_pos = plan ? plan->d_raster_of_pos : nullptr;
   a.pos = pos;
   a.n_axes = rot->n_axes;
+  a.n_tensors = n_tensors;
   a.H = plan ? plan->cfg.H : 1;
   a.W = plan ? plan->cfg.W : 1;
   a.n_video = plan ? plan->N : 0;
@@ -504,14 +566,11 @@ int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const
   a.rows = rows;
   a.tokens = tokens;
 
-  long long blocks = 0;
-  for (int i = 0; i < n_tensors; ++i) {
-    const int tpb = kThreads / lanes / a.t[i].head_slots;
-    const long long n = (rows + tpb - 1) / tpb;
-    if (n > blocks) blocks = n;
-  }
-  if (backward && blocks > kBackwardBlocksMax) blocks = kBackwardBlocksMax;
-  if (blocks > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
+  // blocks that stay: one wave of the four (backward with a norm: two) that fit an SM
+  const int tokens_per_block = kThreads / lanes / hs;
+  const int wave = backward && rot->norm != TRA_NORM_NONE ? kBackwardBlocksMax : kForwardBlocksMax;
+  int blocks = (rows + tokens_per_block - 1) / tokens_per_block;
+  if (blocks > wave) blocks = wave;
   ReduceArgs red;
   memset(&red, 0, sizeof(red));
   int n_red = 0;
@@ -531,10 +590,10 @@ int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const
         red.out[n_red++] = tensors[i].bias_grad;
       }
     }
-    red.blocks = (int)blocks;
+    red.blocks = blocks;
     red.d = rot->head_dim;
   }
-  const dim3 grid((unsigned)blocks, (unsigned)n_tensors);
+  const dim3 grid((unsigned)blocks, a.one_tensor ? (unsigned)n_tensors : 1u);
   const bool halves = rot->halves != 0;
   if (dtype == TRA_BF16) {
     backward ? launch_norm<__nv_bfloat16, true>(rot->norm, halves, grid, a, stream)
