@@ -29,6 +29,7 @@
 #include <new>
 
 #include "tra_common.cuh"
+#include "tra_tcgen05.cuh"
 
 struct tra_rotary {
   int head_dim, n_axes, halves, norm;
@@ -65,111 +66,184 @@ struct RotArgs {
   int d, lanes;                   // lanes: threads per row, d / 16 rounded up to a power of two
   int n_tensors, one_tensor;      // one_tensor: a block works on the tensor blockIdx.y, else on all of them
   int by_source;                  // !one_tensor: the rotated tensors are tile-major
-  int head_slots;                 // heads of a token side by side in a block
+  int head_slots, head_slots_log2, lanes_log2;   // heads of a token side by side in a block; both powers of two
   float eps, inv_d;
   int rows, tokens;               // rows = batch * tokens
 };
 
+// A thread's sixteen channels as loaded: eight of the lower half of the row, eight of the upper half.
 template <typename T>
-struct Piece;                     // eight consecutive channels as loaded
-template <>
-struct Piece<__nv_bfloat16> {
-  uint4 v;
-  __device__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint4*>(p); }
-  __device__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
-  __device__ void get(float* f) const {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+struct Raw {
+  static constexpr int kVec = sizeof(T) / 2;         // 16-byte loads per eight channels
+  uint4 v[2 * kVec];
+  __device__ __forceinline__ void load(const T* lo, const T* hi) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < kVec; ++i) {
+      v[i] = reinterpret_cast<const uint4*>(lo)[i];
+      v[kVec + i] = reinterpret_cast<const uint4*>(hi)[i];
     }
   }
-  static __device__ void store(__nv_bfloat16* p, const float* f) {
-    __nv_bfloat162 h[4];
+  __device__ __forceinline__ void store(T* lo, T* hi) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<uint4*>(h);
-  }
-};
-template <>
-struct Piece<__half> {
-  uint4 v;
-  __device__ void load(const __half* p) { v = *reinterpret_cast<const uint4*>(p); }
-  __device__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
-  __device__ void get(float* f) const {
-    const __half2* h = reinterpret_cast<const __half2*>(&v);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 t = __half22float2(h[i]);
-      f[2 * i] = t.x;
-      f[2 * i + 1] = t.y;
+    for (int i = 0; i < kVec; ++i) {
+      reinterpret_cast<uint4*>(lo)[i] = v[i];
+      reinterpret_cast<uint4*>(hi)[i] = v[kVec + i];
     }
   }
-  static __device__ void store(__half* p, const float* f) {
-    __half2 h[4];
+  __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
-    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<uint4*>(h);
+    for (int i = 0; i < 2 * kVec; ++i) v[i] = make_uint4(0u, 0u, 0u, 0u);
   }
 };
+
+// two neighbouring channels of a 16-bit type
+template <typename T>
+__device__ __forceinline__ void split(uint32_t w, float& a, float& b);
 template <>
-struct Piece<float> {
-  float4 a, b;
-  __device__ void load(const float* p) {
-    a = reinterpret_cast<const float4*>(p)[0];
-    b = reinterpret_cast<const float4*>(p)[1];
+__device__ __forceinline__ void split<__nv_bfloat16>(uint32_t w, float& a, float& b) {
+  a = __uint_as_float(w << 16);
+  b = __uint_as_float(w & 0xffff0000u);
+}
+template <>
+__device__ __forceinline__ void split<__half>(uint32_t w, float& a, float& b) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  a = f.x;
+  b = f.y;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t join(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t join<__nv_bfloat16>(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t join<__half>(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The sixteen channels as eight fp32 pairs for the packed arithmetic: z[0 .. 3] the first channels of the rotation's pairs
+// 0 .. 7 of the thread, z[4 .. 7] their second channels.
+template <typename T, bool kHalves>
+__device__ __forceinline__ void unpack(const Raw<T>& r, uint64_t* z) {
+  if constexpr (sizeof(T) == 4) {
+    const float* f = reinterpret_cast<const float*>(r.v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int j = 2 * (i & 3), second = i >> 2;
+      z[i] = kHalves ? pack2(f[8 * second + j], f[8 * second + j + 1]) : pack2(f[2 * j + second], f[2 * j + 2 + second]);
+    }
+  } else {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(r.v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float a, b, c, d;
+      split<T>(w[2 * i], a, b);
+      split<T>(w[2 * i + 1], c, d);
+      if (kHalves) {                                   // words 0 .. 3 first channels, 4 .. 7 second ones
+        z[2 * i] = pack2(a, b);
+        z[2 * i + 1] = pack2(c, d);
+      } else {                                         // every word holds a pair
+        z[i] = pack2(a, c);
+        z[4 + i] = pack2(b, d);
+      }
+    }
   }
-  __device__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ void get(float* f) const {
-    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+}
+template <typename T, bool kHalves>
+__device__ __forceinline__ void pack(const uint64_t* z, Raw<T>& r) {
+  if constexpr (sizeof(T) == 4) {
+    float* f = reinterpret_cast<float*>(r.v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int j = 2 * (i & 3), second = i >> 2;
+      unpack2(z[i], f[kHalves ? 8 * second + j : 2 * j + second], f[kHalves ? 8 * second + j + 1 : 2 * j + 2 + second]);
+    }
+  } else {
+    uint32_t* w = reinterpret_cast<uint32_t*>(r.v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float a, b, c, d;
+      unpack2(z[kHalves ? 2 * i : i], a, b);
+      unpack2(z[kHalves ? 2 * i + 1 : 4 + i], c, d);
+      w[2 * i] = kHalves ? join<T>(a, b) : join<T>(a, c);
+      w[2 * i + 1] = kHalves ? join<T>(c, d) : join<T>(b, d);
+    }
   }
-  static __device__ void store(float* p, const float* f) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-  }
-};
+}
+
+__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t both(float x) { return pack2(x, x); }
+__device__ __forceinline__ float sum2(uint64_t v) {
+  float a, b;
+  unpack2(v, a, b);
+  return a + b;
+}
 
 // Sum over the threads of a row (a power of two of neighbouring lanes).
 __device__ __forceinline__ float row_sum(float s, int lanes) {
   for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   return s;
 }
+__device__ __forceinline__ float sum_of(const uint64_t* z) {
+  return sum2(fadd2(fadd2(fadd2(z[0], z[1]), fadd2(z[2], z[3])), fadd2(fadd2(z[4], z[5]), fadd2(z[6], z[7]))));
+}
+__device__ __forceinline__ float dot_of(const uint64_t* a, const uint64_t* b) {
+  uint64_t s = fmul2(a[0], b[0]), t = fmul2(a[1], b[1]);
+#pragma unroll
+  for (int i = 2; i < 8; i += 2) {
+    s = ffma2(a[i], b[i], s);
+    t = ffma2(a[i + 1], b[i + 1], t);
+  }
+  return sum2(fadd2(s, t));
+}
+
+// Four floats per lane and step q, the lanes' side by side: conflict-free 16-byte reads.
+__device__ __forceinline__ void load_pairs(const float* table, int q, int lanes, int lane, uint64_t& a, uint64_t& b) {
+  const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(table + (q * lanes + lane) * 4);
+  a = v.x;
+  b = v.y;
+}
+// turns the pairs by their angle, or back
+template <bool kBack>
+__device__ __forceinline__ void turn_pairs(uint64_t* z, const float* cs, const float* sn, int lanes, int lane) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    uint64_t c[2], s[2];
+    load_pairs(cs, q, lanes, lane, c[0], c[1]);
+    load_pairs(sn, q, lanes, lane, s[0], s[1]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint64_t& a = z[2 * q + i];
+      uint64_t& b = z[4 + 2 * q + i];
+      const uint64_t minus = s[i] ^ 0x8000000080000000ull;
+      const uint64_t ta = ffma2(a, c[i], fmul2(b, kBack ? s[i] : minus));
+      const uint64_t tb = ffma2(b, c[i], fmul2(a, kBack ? minus : s[i]));
+      a = ta;
+      b = tb;
+    }
+  }
+}
 
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_float(float x) { return x; }
-// z[0 .. 7] times, or plus, eight values in shared memory
-__device__ __forceinline__ void times8(float* z, const float* s) {
-  const float4 a = reinterpret_cast<const float4*>(s)[0], b = reinterpret_cast<const float4*>(s)[1];
-  z[0] *= a.x, z[1] *= a.y, z[2] *= a.z, z[3] *= a.w, z[4] *= b.x, z[5] *= b.y, z[6] *= b.z, z[7] *= b.w;
-}
-__device__ __forceinline__ void plus8(float* z, const float* s) {
-  const float4 a = reinterpret_cast<const float4*>(s)[0], b = reinterpret_cast<const float4*>(s)[1];
-  z[0] += a.x, z[1] += a.y, z[2] += a.z, z[3] += a.w, z[4] += b.x, z[5] += b.y, z[6] += b.z, z[7] += b.w;
-}
 
-// Channel c of the thread's sixteen: 0 .. 7 in the lower half of the row, 8 .. 15 in the upper half.  Pair j (0 .. 7) of the
-// thread: (j, j + 8) when channels pair across the halves, (2 j, 2 j + 1) otherwise.  cs, sn: the token's cosines and sines
-// by pair, in shared memory.
+// Channel of entry i (0 .. 15) of a lane's z, and pair of entry j (0 .. 7).
 template <bool kHalves>
-__device__ __forceinline__ void turn_pairs(float* z, const float* cs, const float* sn, int c_lo, int c_hi, float sign) {
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int pair = kHalves ? c_lo + 4 * q : (q ? c_hi : c_lo) / 2;
-    const float4 c4 = *reinterpret_cast<const float4*>(cs + pair), s4 = *reinterpret_cast<const float4*>(sn + pair);
-    const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int j = 4 * q + i;
-      float& x = z[kHalves ? j : 2 * j];
-      float& y = z[kHalves ? j + 8 : 2 * j + 1];
-      const float si = sign * s[i];
-      const float tx = x * c[i] - y * si, ty = x * si + y * c[i];
-      x = tx;
-      y = ty;
-    }
-  }
+__device__ __forceinline__ int channel_of(int d, int lane, int i) {
+  if (kHalves) return (i < 8 ? 0 : d / 2 - 8) + lane * 8 + i;
+  const int j = i & 7;
+  return (j < 4 ? 0 : d / 2 - 8) + lane * 8 + 2 * j + (i >> 3);
+}
+template <bool kHalves>
+__device__ __forceinline__ int pair_of(int d, int lane, int j) {
+  return kHalves ? lane * 8 + j : (j < 4 ? 0 : d / 4 - 4) + lane * 4 + j;
 }
 
 // The token a thread works on: its index in the batch entry on the attention side (ordered) and on the projection side.
@@ -186,34 +260,44 @@ template <typename T, int kNorm, bool kHalves, bool kBackward>
 __global__ void __launch_bounds__(kThreads, kBackward && kNorm != TRA_NORM_NONE ? 2 : 4)
 tra_rotary_kernel(const __grid_constant__ RotArgs p) {
   constexpr bool kSums = kBackward && kNorm != TRA_NORM_NONE;
-  // [buffer][cosines, then sines][token of the group][pair]: tokens_per_block * d / 2 <= 8 * kThreads
+  // per lane four floats and step, see load_pairs: [buffer][cosines, then sines][token of the group], 8 per lane
   __shared__ __align__(16) float s_turn[2][16 * kThreads];
   __shared__ __align__(16) float s_weight[kNorm != TRA_NORM_NONE ? 3 * kMaxD : 4], s_bias[kNorm == TRA_NORM_LAYER ? 3 * kMaxD : 4];
-  const int tid = threadIdx.x;
-  const int lane = tid % p.lanes, slot = tid / p.lanes;
+  __shared__ uint64_t s_freq[kMaxD / 2];
+  __shared__ uint8_t s_axis[kMaxD / 2];
+  const int tid = threadIdx.x, lanes = p.lanes;
+  const int lane = tid & (lanes - 1), slot = tid >> p.lanes_log2;
   const bool on = lane * 16 < p.d;                     // d / 16 need not be a power of two
   const int c_lo = lane * 8, c_hi = p.d / 2 + lane * 8;
-  const int head0 = slot % p.head_slots, token_slot = slot / p.head_slots;
-  const int tokens_per_block = kThreads / p.lanes / p.head_slots;
-  const int pairs = p.d / 2, sines = tokens_per_block * pairs;
+  const int head0 = slot & (p.head_slots - 1), token_slot = slot >> p.head_slots_log2;
+  const int tokens_per_block = kThreads >> (p.lanes_log2 + p.head_slots_log2);
+  const int sines = tokens_per_block * lanes * 8;
   const int t_first = p.one_tensor ? (int)blockIdx.y : 0, t_end = p.one_tensor ? t_first + 1 : p.n_tensors;
   const bool by_source = p.one_tensor ? p.t[t_first].tile_major != 0 : p.by_source != 0;
   const bool turns_any = !p.one_tensor || p.t[t_first].rotate;
 
+  for (int i = tid; i < p.d / 2; i += kThreads) {
+    s_freq[i] = p.turn[i];
+    s_axis[i] = p.axis[i];
+  }
   if (kNorm != TRA_NORM_NONE) {
-    for (int i = tid; i < 3 * p.d; i += kThreads) {
-      const int k = i / p.d, c = i - k * p.d;
-      if (k < t_first || k >= t_end) continue;
-      if (p.t[k].weight) s_weight[k * kMaxD + c] = to_float(((const T*)p.t[k].weight)[c]);
-      if (kNorm == TRA_NORM_LAYER && !kBackward && p.t[k].bias) s_bias[k * kMaxD + c] = to_float(((const T*)p.t[k].bias)[c]);
+    for (int i = tid; i < 16 * lanes; i += kThreads) {
+      const int l = (i >> 2) & (lanes - 1), e = (i >> (2 + p.lanes_log2)) * 4 + (i & 3);
+      const int c = channel_of<kHalves>(p.d, l, e);
+      for (int k = t_first; k < t_end; ++k) {
+        const RotTensor& t = p.t[k];
+        const bool has = l * 16 < p.d;
+        s_weight[k * kMaxD + i] = has && t.weight ? to_float(((const T*)t.weight)[c]) : 1.f;
+        if (kNorm == TRA_NORM_LAYER) s_bias[k * kMaxD + i] = has && !kBackward && t.bias ? to_float(((const T*)t.bias)[c]) : 0.f;
+      }
     }
   }
-  float acc_w[kSums ? 16 : 1], acc_b[kSums && kNorm == TRA_NORM_LAYER ? 16 : 1];
+  uint64_t acc_w[kSums ? 8 : 1], acc_b[kSums && kNorm == TRA_NORM_LAYER ? 8 : 1];
   if (kSums) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      acc_w[i] = 0.f;
-      if (kNorm == TRA_NORM_LAYER) acc_b[i] = 0.f;
+    for (int i = 0; i < 8; ++i) {
+      acc_w[i] = 0ull;
+      if (kNorm == TRA_NORM_LAYER) acc_b[i] = 0ull;
     }
   }
 
@@ -232,7 +316,7 @@ tra_rotary_kernel(const __grid_constant__ RotArgs p) {
   };
   // cosines and sines of a token, shared out over its threads
   auto angles = [&](const Token& k, float* turn) {
-    if (!k.there || !turns_any) return;
+    if (!turns_any) return;
     // positions belong to the projection side, which is the ordered index of a tensor that is not tile-major
     const int tok = by_source ? k.source : k.ordered;
     int frame = 0, y = 0, x = 0;
@@ -243,48 +327,53 @@ tra_rotary_kernel(const __grid_constant__ RotArgs p) {
       y = in_frame / p.W;
       x = in_frame - y * p.W;
     }
-    const bool turned = p.pos != nullptr || tok < p.n_video;           // text keeps its channels
-    for (int pair = head0 * p.lanes + lane; pair < pairs; pair += p.head_slots * p.lanes) {
+    // text keeps its channels; a token that does not exist turns its zeros by nothing
+    const bool turned = k.there && (p.pos != nullptr || tok < p.n_video);
+    float* const out = turn + token_slot * lanes * 8;
+    for (int e = (head0 << p.lanes_log2) + lane; e < lanes * 8; e += lanes << p.head_slots_log2) {
+      const int l = (e >> 2) & (lanes - 1), pair = pair_of<kHalves>(p.d, l, (e >> (2 + p.lanes_log2)) * 4 + (e & 3));
       float c = 1.f, sine = 0.f;
-      if (turned) {
-        const int axis = p.axis[pair];
+      if (turned && l * 16 < p.d) {
+        const int axis = s_axis[pair];
         const int v = p.pos != nullptr ? __ldg(p.pos + (long long)tok * p.n_axes + axis) : axis == 0 ? frame : axis == 1 ? y : x;
-        const uint64_t turns = (uint64_t)(int64_t)v * p.turn[pair];
+        const uint64_t turns = (uint64_t)(int64_t)v * s_freq[pair];
         sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f /* 2^-31 */, &sine, &c);
       }
-      turn[token_slot * pairs + pair] = c;
-      turn[sines + token_slot * pairs + pair] = sine;
+      out[e] = c;
+      out[sines + e] = sine;
     }
   };
 
-  Piece<T> lo, hi, xlo, xhi;
-  auto fetch = [&](const Token& k, int ti, int h) {
+  // the row whose loads are in flight
+  Raw<T> raw, xraw;
+  const T *in = nullptr, *xin = nullptr;
+  bool in_on = false;
+  auto load = [&](bool there, bool with_x) {
+    if (there) {
+      raw.load(in + c_lo, in + c_hi);
+      if (kSums && with_x) xraw.load(xin + c_lo, xin + c_hi);
+    } else {
+      raw.zero();
+      if (kSums) xraw.zero();
+    }
+  };
+  auto fetch_first = [&](const Token& k, int ti) {      // a token's first row of a tensor
     const RotTensor& t = p.t[ti];
-    if (k.there && on && h < t.heads) {
+    in_on = k.there && on;
+    if (in_on) {
       // forward reads at the source row and writes at the ordered one, backward the other way round
       const int source = t.tile_major ? k.source : k.ordered;
-      const T* in = (const T*)t.src + k.batch * t.src_stride[0] + (kBackward ? k.ordered : source) * t.src_stride[1] + h * t.src_stride[2];
-      lo.load(in + c_lo);
-      hi.load(in + c_hi);
-      if (kSums && t.rotate) {
-        const T* x = (const T*)t.x + k.batch * t.x_stride[0] + source * t.x_stride[1] + h * t.x_stride[2];
-        xlo.load(x + c_lo);
-        xhi.load(x + c_hi);
-      }
-    } else {
-      lo.zero();
-      hi.zero();
-      if (kSums) {
-        xlo.zero();
-        xhi.zero();
-      }
+      in = (const T*)t.src + k.batch * t.src_stride[0] + (kBackward ? k.ordered : source) * t.src_stride[1] + head0 * t.src_stride[2];
+      if (kSums && t.rotate) xin = (const T*)t.x + k.batch * t.x_stride[0] + source * t.x_stride[1] + head0 * t.x_stride[2];
     }
+    load(in_on && head0 < t.heads, t.rotate);
   };
 
   const int stride = (int)gridDim.x * tokens_per_block;
   int base = (int)blockIdx.x * tokens_per_block;
   Token cur = locate(base);
-  fetch(cur, t_first, head0);
+  fetch_first(cur, t_first);
+  __syncthreads();
   angles(cur, s_turn[0]);
   __syncthreads();
   int buffer = 0;
@@ -293,102 +382,99 @@ tra_rotary_kernel(const __grid_constant__ RotArgs p) {
   while (true) {
     const bool more = p.rows - base > stride;          // base + stride < rows
     const Token next = more ? locate(base + stride) : Token{0, 0, 0, false};
-    const float* const cs = s_turn[buffer] + token_slot * pairs;
+    const float* const cs = s_turn[buffer] + token_slot * lanes * 8;
     const float* const sn = cs + sines;
     for (int ti = t_first; ti < t_end; ++ti) {
       const RotTensor& t = p.t[ti];
-      const bool rotate = t.rotate != 0, normed = kNorm != TRA_NORM_NONE && rotate;
-      const bool has_w = normed && t.weight != nullptr;
-      const bool has_b = !kBackward && kNorm == TRA_NORM_LAYER && normed && t.bias != nullptr;
-      const int heads = t.heads;
-      for (int h = head0; h - head0 < heads; h += p.head_slots) {
-        const bool row_on = cur.there && on && h < heads;
-        float z[16];
-        lo.get(z);
-        hi.get(z + 8);
-        float n[kSums ? 16 : 1];
-        if constexpr (kSums) {
-          xlo.get(n);
-          xhi.get(n + 8);
-        }
+      const int heads = t.heads, hs = p.head_slots;
+      const bool rotate = t.rotate != 0;
+      const long long in_step = t.src_stride[2] << p.head_slots_log2, x_step = t.x_stride[2] << p.head_slots_log2,
+                      out_step = t.dst_stride[2] << p.head_slots_log2;
+      const bool out_on = cur.there && on;
+      T* out = (T*)t.dst + cur.batch * t.dst_stride[0] +
+               (kBackward && t.tile_major ? cur.source : cur.ordered) * t.dst_stride[1] + head0 * t.dst_stride[2];
+      for (int h = head0; h - head0 < heads; h += hs, out += out_step) {
+        const bool row_on = out_on && h < heads;
+        const Raw<T> row = raw, xrow = xraw;
         // the next row, while this one is worked on
-        if (h - head0 + p.head_slots < heads)
-          fetch(cur, ti, h + p.head_slots);
-        else if (ti + 1 < t_end)
-          fetch(cur, ti + 1, head0);
-        else
-          fetch(next, t_first, head0);
+        if (h - head0 + hs < heads) {
+          in += in_step;
+          if (kSums) xin += x_step;
+          load(in_on && h + hs < heads, rotate);
+        } else if (ti + 1 < t_end) {
+          fetch_first(cur, ti + 1);
+        } else {
+          fetch_first(next, t_first);
+        }
+        if (!rotate) {                                 // only moved
+          if (row_on) row.store(out + c_lo, out + c_hi);
+          continue;
+        }
+        uint64_t z[8];
+        unpack<T, kHalves>(row, z);
         if (!kBackward) {
-          if (normed) {
+          if (kNorm != TRA_NORM_NONE) {
             if (kNorm == TRA_NORM_LAYER) {
-              float s = 0.f;
+              const float total = row_sum(sum_of(z), lanes);       // every lane shuffles
+              const uint64_t mean = both(on ? -total * p.inv_d : 0.f);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) s += z[i];
-              const float mean = row_sum(s, p.lanes) * p.inv_d;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) z[i] = on ? z[i] - mean : 0.f;
+              for (int i = 0; i < 8; ++i) z[i] = fadd2(z[i], mean);
             }
-            float q = 0.f;
+            const uint64_t r = both(rsqrtf(fmaf(row_sum(dot_of(z, z), lanes), p.inv_d, p.eps)));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) q = fmaf(z[i], z[i], q);
-            const float r = rsqrtf(fmaf(row_sum(q, p.lanes), p.inv_d, p.eps));
+            for (int q = 0; q < 4; ++q) {
+              uint64_t w[2], b[2] = {0ull, 0ull};
+              load_pairs(s_weight + ti * kMaxD, q, lanes, lane, w[0], w[1]);
+              if (kNorm == TRA_NORM_LAYER) load_pairs(s_bias + ti * kMaxD, q, lanes, lane, b[0], b[1]);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] *= r;
-            if (has_w && on) {
-              times8(z, s_weight + ti * kMaxD + c_lo);
-              times8(z + 8, s_weight + ti * kMaxD + c_hi);
-            }
-            if (has_b && on) {
-              plus8(z, s_bias + ti * kMaxD + c_lo);
-              plus8(z + 8, s_bias + ti * kMaxD + c_hi);
+              for (int i = 0; i < 2; ++i) {
+                uint64_t& v = z[2 * q + i];
+                v = fmul2(v, r);
+                v = kNorm == TRA_NORM_LAYER ? ffma2(v, w[i], b[i]) : fmul2(v, w[i]);
+              }
             }
           }
-          if (rotate && on) turn_pairs<kHalves>(z, cs, sn, c_lo, c_hi, 1.f);
+          turn_pairs<false>(z, cs, sn, lanes, lane);
         } else {
-          if (rotate && on) turn_pairs<kHalves>(z, cs, sn, c_lo, c_hi, -1.f);      // z = u
+          turn_pairs<true>(z, cs, sn, lanes, lane);    // z = u
           if constexpr (kSums) {
-            if (normed) {
-              if (kNorm == TRA_NORM_LAYER) {
-                float s = 0.f;
+            uint64_t n[8];
+            unpack<T, kHalves>(xrow, n);
+            if (kNorm == TRA_NORM_LAYER) {
+              const float total = row_sum(sum_of(n), lanes);
+              const uint64_t mean = both(on ? -total * p.inv_d : 0.f);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s += n[i];
-                const float mean = row_sum(s, p.lanes) * p.inv_d;
+              for (int i = 0; i < 8; ++i) n[i] = fadd2(n[i], mean);
+            }
+            // a row that does not exist is left out (eps = 0 would make 0 * inf of it)
+            const float squares = row_sum(dot_of(n, n), lanes);
+            const uint64_t r = both(row_on ? rsqrtf(fmaf(squares, p.inv_d, p.eps)) : 0.f);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) n[i] = on ? n[i] - mean : 0.f;
-              }
-              float q = 0.f;
+            for (int i = 0; i < 8; ++i) {
+              n[i] = fmul2(n[i], r);
+              acc_w[i] = ffma2(z[i], n[i], acc_w[i]);
+              if (kNorm == TRA_NORM_LAYER) acc_b[i] = fadd2(acc_b[i], z[i]);
+            }
 #pragma unroll
-              for (int i = 0; i < 16; ++i) q = fmaf(n[i], n[i], q);
-              const float r = rsqrtf(fmaf(row_sum(q, p.lanes), p.inv_d, p.eps));
-              float sg = 0.f, sgn = 0.f;
+            for (int q = 0; q < 4; ++q) {              // z = g
+              uint64_t w[2];
+              load_pairs(s_weight + ti * kMaxD, q, lanes, lane, w[0], w[1]);
+              z[2 * q] = fmul2(z[2 * q], w[0]);
+              z[2 * q + 1] = fmul2(z[2 * q + 1], w[1]);
+            }
+            const uint64_t mgn = both(-row_sum(dot_of(z, n), lanes) * p.inv_d);
+            const uint64_t mg = both(kNorm == TRA_NORM_LAYER ? -row_sum(sum_of(z), lanes) * p.inv_d : 0.f);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                n[i] *= r;
-                // a row that does not exist is left out (eps = 0 would make 0 * inf of it)
-                acc_w[i] += row_on ? z[i] * n[i] : 0.f;
-                if (kNorm == TRA_NORM_LAYER) acc_b[i] += row_on ? z[i] : 0.f;
-              }
-              if (has_w && on) {                                     // g
-                times8(z, s_weight + ti * kMaxD + c_lo);
-                times8(z + 8, s_weight + ti * kMaxD + c_hi);
-              }
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                sg += z[i];
-                sgn = fmaf(z[i], n[i], sgn);
-              }
-              const float mgn = row_sum(sgn, p.lanes) * p.inv_d;
-              const float mg = kNorm == TRA_NORM_LAYER ? row_sum(sg, p.lanes) * p.inv_d : 0.f;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) z[i] = r * (z[i] - mg - n[i] * mgn);
+            for (int i = 0; i < 8; ++i) {
+              const uint64_t g = kNorm == TRA_NORM_LAYER ? fadd2(z[i], mg) : z[i];
+              z[i] = fmul2(r, ffma2(n[i], mgn, g));
             }
           }
         }
         if (row_on) {
-          const int source = t.tile_major ? cur.source : cur.ordered;
-          T* out = (T*)t.dst + cur.batch * t.dst_stride[0] + (kBackward ? source : cur.ordered) * t.dst_stride[1] + h * t.dst_stride[2];
-          Piece<T>::store(out + c_lo, z);
-          Piece<T>::store(out + c_hi, z + 8);
+          Raw<T> y;
+          pack<T, kHalves>(z, y);
+          y.store(out + c_lo, out + c_hi);
         }
       }
     }
@@ -410,12 +496,16 @@ tra_rotary_kernel(const __grid_constant__ RotArgs p) {
 #pragma unroll
     for (int which = 0; which < (kNorm == TRA_NORM_LAYER ? 2 : 1); ++which) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float v = acc_w[i];
+      for (int i = 0; i < 8; ++i) {
+        float v[2];
+        unpack2(acc_w[i], v[0], v[1]);
         if constexpr (kNorm == TRA_NORM_LAYER)
-          if (which == 1) v = acc_b[i];
-        for (int o = p.lanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if ((tid & 31) < p.lanes && on) s_red[warp * p.d + (i < 8 ? c_lo + i : c_hi + i - 8)] = v;
+          if (which == 1) unpack2(acc_b[i], v[0], v[1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          for (int o = lanes; o < 32; o <<= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+          if ((tid & 31) < lanes && on) s_red[warp * p.d + channel_of<kHalves>(p.d, lane, 2 * i + k)] = v[k];
+        }
       }
       __syncthreads();
       for (int c = tid; c < p.d; c += kThreads) {
@@ -453,6 +543,12 @@ __global__ void __launch_bounds__(kReduceRows * kReduceCols) tra_rotary_reduce_k
 int lanes_of(int d) {
   int l = 1;
   while (l * 16 < d) l *= 2;
+  return l;
+}
+
+int log2_of(int n) {
+  int l = 0;
+  while ((1 << l) < n) ++l;
   return l;
 }
 
@@ -547,6 +643,8 @@ int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const
   if (few)
     while (hs < slots && hs < most_heads) hs *= 2;
   a.head_slots = hs;
+  a.head_slots_log2 = log2_of(hs);
+  a.lanes_log2 = log2_of(lanes);
   // the weights' sums of a backward launch stay in registers: one tensor per block
   a.one_tensor = few || mixed || (backward && rot->norm != TRA_NORM_NONE);
   if (any_rotate && !pos && !plan) return TRA_ERR_INVALID_ARG;
