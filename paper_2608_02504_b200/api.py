@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 
 import torch
 
@@ -433,6 +434,18 @@ class HostPipeline:
 
 _DTYPES = {torch.bfloat16: TRA_BF16, torch.float16: TRA_FP16, torch.float32: TRA_FP32}
 
+# The calls below are made for every layer and token, on a few microseconds of kernel: descriptors are packed by one
+# struct call each (the layouts of tra_rotary_tensor_t, tra_packed_args_t and tra_packed_grads_t), devices are compared by index.
+_ROTARY_TENSOR = struct.Struct("7Q9qiI")
+_PACKED_ARGS = struct.Struct("5Q8q3Q5if")
+_PACKED_GRADS = struct.Struct("4Q8q")
+assert (_ROTARY_TENSOR.size, _PACKED_ARGS.size, _PACKED_GRADS.size) == tuple(
+    ctypes.sizeof(t) for t in (tra_rotary_tensor_t, tra_packed_args_t, tra_packed_grads_t))
+
+
+def _raw_stream(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
 
 class Rotary:
     """Head norm, rotary positions with several axes, and token order: what Q, K and V go through between a
@@ -493,44 +506,45 @@ class Rotary:
     def _tile_major(plan, name):
         """Which tensors the plan's attention calls take in tile-major order."""
         if plan is None or plan.flags & TRA_ORDER_RASTER:
-            return False
-        return name != "q" or not plan.flags & TRA_ORDER_RASTER_QO
+            return 0
+        return TRA_ROTARY_TILE_MAJOR if name != "q" or not plan.flags & TRA_ORDER_RASTER_QO else 0
 
-    def _param(self, t, name, like):
+    def _param(self, t, name, dtype, index):
         if t is None:
-            return None
-        if t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != (self.head_dim,) or \
-                not t.is_contiguous():
+            return 0
+        if t.dtype != dtype or t.get_device() != index or t.shape != (self.head_dim,) or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous [head_dim] tensor of the tensors' type and device")
         return t.data_ptr()
 
-    def _strides(self, t, name, like, shape, heads_first):
+    @staticmethod
+    def _strides(t, name, shape, dtype, index, heads_first=False):
         """Strides (batch, token, head) of a tensor [B, tokens, heads, d] or, heads first, [B, heads, tokens, d]."""
-        if not t.is_cuda or t.device != like.device or t.dtype != like.dtype or tuple(t.shape) != shape or \
-                (t.stride(3) != 1 and t.shape[3] > 1):
-            raise ValueError(f"{name}: expected a CUDA tensor of shape {shape}, type {like.dtype}, on {like.device}, "
-                             "with contiguous channels")
         s = t.stride()
-        return (s[0], s[2], s[1]) if heads_first else (s[0], s[1], s[2])
+        if t.get_device() != index or t.dtype != dtype or t.shape != shape or s[3] != 1:
+            raise ValueError(f"{name}: expected a CUDA tensor of shape {shape}, type {dtype}, on device {index}, "
+                             "with contiguous channels")
+        return (s[0], s[2], s[1]) if heads_first else s[:3]
 
     def _begin(self, first, plan, pos, heads_first):
-        if first.dim() != 4 or first.shape[3] != self.head_dim or first.dtype not in _DTYPES or not first.is_cuda:
+        shape = first.shape
+        if len(shape) != 4 or shape[3] != self.head_dim or first.dtype not in _DTYPES or not first.is_cuda:
             raise ValueError("expected CUDA tensors [B, tokens, heads, head_dim] "
                              "([B, heads, tokens, head_dim] on the attention side of a plan), bf16, fp16 or fp32")
-        if first.device.index != torch.cuda.current_device():
+        index = first.get_device()
+        if index != torch.cuda.current_device():
             raise ValueError("the tensors' device must be the current one")
-        B, tokens = first.shape[0], first.shape[2 if heads_first else 1]
+        B, tokens = shape[0], shape[2 if heads_first else 1]
         if plan is not None and tokens != plan.N:
             raise ValueError(f"expected {plan.N} tokens, the plan's")
         if plan is None and pos is None:
             raise ValueError("expected a plan or pos")
         pos_ptr = None
         if pos is not None:
-            if not pos.is_cuda or pos.device != first.device or pos.dtype != torch.int32 or \
-                    tuple(pos.shape) != (tokens, self.n_axes) or not pos.is_contiguous():
+            if pos.get_device() != index or pos.dtype != torch.int32 or pos.shape != (tokens, self.n_axes) or \
+                    not pos.is_contiguous():
                 raise ValueError("pos: expected a contiguous int32 CUDA tensor [tokens, n_axes]")
             pos_ptr = pos.data_ptr()
-        return B, tokens, pos_ptr
+        return B, tokens, index, pos_ptr
 
     def forward(self, q, k=None, v=None, *, plan=None, pos=None, q_weight=None, k_weight=None, q_bias=None, k_bias=None,
                 out=None):
@@ -541,33 +555,34 @@ class Rotary:
         given) and the outputs are [B, heads, tokens, d] in the order its attention calls take; without it,
         ``pos`` int32 [tokens, n_axes] names every token's position and outputs keep the inputs' layout.
         V is only moved: without a plan it comes back as a copy.  ``out``: output tensors instead of new ones."""
-        tensors = [("q", q, q_weight, q_bias), ("k", k, k_weight, k_bias), ("v", v, None, None)]
         if k is None and (k_weight is not None or k_bias is not None):
             raise ValueError("k_weight, k_bias: given without k")
-        B, tokens, pos_ptr = self._begin(q, plan, pos, False)
-        on_plan = plan is not None
-        args, outs, n = (tra_rotary_tensor_t * 3)(), [], 0
-        for i, (name, x, w, b) in enumerate(tensors):
+        B, tokens, index, pos_ptr = self._begin(q, plan, pos, False)
+        on_plan, dtype, d = plan is not None, q.dtype, self.head_dim
+        desc, outs, n = bytearray(3 * _ROTARY_TENSOR.size), [], 0
+        for i, (name, x, w, b) in enumerate((("q", q, q_weight, q_bias), ("k", k, k_weight, k_bias), ("v", v, None, None))):
             if x is None:
                 outs.append(None)
                 continue
-            heads = x.shape[2] if x.dim() == 4 else 0
-            src = self._strides(x, name, q, (B, tokens, heads, self.head_dim), False)
-            y = out[i] if out is not None else None
-            shape = (B, heads, tokens, self.head_dim) if on_plan else (B, tokens, heads, self.head_dim)
-            if y is None:
-                y = torch.empty(shape, dtype=x.dtype, device=x.device)
-            a = args[n]
-            a.src, a.dst = x.data_ptr(), y.data_ptr()
-            a.src_stride[:], a.dst_stride[:] = src, self._strides(y, "out " + name, q, shape, on_plan)
-            a.weight, a.bias = self._param(w, name + "_weight", q), self._param(b, name + "_bias", q)
-            a.heads = heads
-            a.flags = (TRA_ROTARY_ROTATE if name != "v" else 0) | \
-                (TRA_ROTARY_TILE_MAJOR if self._tile_major(plan, name) else 0)
+            if x.dim() != 4:
+                raise ValueError(f"{name}: expected [B, tokens, heads, head_dim]")
+            heads = x.shape[2]
+            src = self._strides(x, name, (B, tokens, heads, d), dtype, index)
+            shape = (B, heads, tokens, d) if on_plan else (B, tokens, heads, d)
+            y = torch.empty(shape, dtype=dtype, device=x.device) if out is None or out[i] is None else out[i]
+            dst = self._strides(y, "out " + name, shape, dtype, index, on_plan)
+            flags = self._tile_major(plan, name)
+            if name != "v":
+                flags |= TRA_ROTARY_ROTATE
+                w, b = self._param(w, name + "_weight", dtype, index), self._param(b, name + "_bias", dtype, index)
+            else:
+                w = b = 0
+            _ROTARY_TENSOR.pack_into(desc, n * _ROTARY_TENSOR.size, x.data_ptr(), y.data_ptr(), 0, w, b, 0, 0, *src, *dst,
+                                     0, 0, 0, heads, flags)
             outs.append(y)
             n += 1
-        _check(_lib.tra_rotary_forward(self._h, plan._h if on_plan else None, pos_ptr, ctypes.byref(args), n, B, tokens,
-                                       _DTYPES[q.dtype], _stream()), "tra_rotary_forward")
+        _check(_lib.tra_rotary_forward(self._h, plan._h if on_plan else None, pos_ptr, bytes(desc), n, B, tokens,
+                                       _DTYPES[dtype], _raw_stream(index)), "tra_rotary_forward")
         return tuple(outs)
 
     def backward(self, dq, dk=None, dv=None, *, q=None, k=None, plan=None, pos=None, q_weight=None, k_weight=None,
@@ -577,43 +592,48 @@ class Rotary:
         ``q``, ``k``: the forward's inputs, needed (and only taken) with a norm.  ``grads``: fp32 [d] tensors
         "q_weight", "k_weight" (and "q_bias", "k_bias" of a layer norm), summed over all rows, whether or not a
         weight was passed; empty without a norm or with ``want_weight_grads=False``."""
-        on_plan = plan is not None
+        on_plan, d = plan is not None, self.head_dim
         if k is not None and dk is None:
             raise ValueError("k: given without dk")
-        B, tokens, pos_ptr = self._begin(dq, plan, pos, on_plan)
-        args, outs, grads, n = (tra_rotary_tensor_t * 3)(), [], {}, 0
+        B, tokens, index, pos_ptr = self._begin(dq, plan, pos, on_plan)
+        dtype, device = dq.dtype, dq.device
+        desc, outs, grads, n = bytearray(3 * _ROTARY_TENSOR.size), [], {}, 0
         for i, (name, dy, x, w) in enumerate((("q", dq, q, q_weight), ("k", dk, k, k_weight), ("v", dv, None, None))):
             if dy is None:
                 outs.append(None)
                 continue
-            heads = dy.shape[1 if on_plan else 2] if dy.dim() == 4 else 0
-            y_shape = (B, heads, tokens, self.head_dim) if on_plan else (B, tokens, heads, self.head_dim)
-            x_shape = (B, tokens, heads, self.head_dim)
-            a = args[n]
-            a.src, a.src_stride[:] = dy.data_ptr(), self._strides(dy, "d" + name, dq, y_shape, on_plan)
-            dx = out[i] if out is not None else None
-            if dx is None:
-                dx = torch.empty(x_shape, dtype=dy.dtype, device=dy.device)
-            a.dst, a.dst_stride[:] = dx.data_ptr(), self._strides(dx, "out d" + name, dq, x_shape, False)
+            if dy.dim() != 4:
+                raise ValueError(f"d{name}: expected four dimensions")
+            heads = dy.shape[1 if on_plan else 2]
+            x_shape = (B, tokens, heads, d)
+            src = self._strides(dy, "d" + name, (B, heads, tokens, d) if on_plan else x_shape, dtype, index, on_plan)
+            dx = torch.empty(x_shape, dtype=dtype, device=device) if out is None or out[i] is None else out[i]
+            dst = self._strides(dx, "out d" + name, x_shape, dtype, index)
+            flags = self._tile_major(plan, name)
+            xp, x_strides, w_grad, b_grad = 0, (0, 0, 0), 0, 0
             if name != "v":
+                flags |= TRA_ROTARY_ROTATE
                 if (x is not None) != (self.norm is not None):
                     raise ValueError(f"{name}: the forward's input is needed with a norm and only with one")
                 if x is not None:
-                    a.x, a.x_stride[:] = x.data_ptr(), self._strides(x, name, dq, x_shape, False)
+                    xp, x_strides = x.data_ptr(), self._strides(x, name, x_shape, dtype, index)
                     if want_weight_grads:
-                        for end in ("weight", "bias")[:2 if self.norm == "layer" else 1]:
-                            g = grads[f"{name}_{end}"] = torch.empty(self.head_dim, dtype=torch.float32, device=dq.device)
-                            setattr(a, end + "_grad", g.data_ptr())
-                a.weight = self._param(w, name + "_weight", dq)
-            a.heads = heads
-            a.flags = (TRA_ROTARY_ROTATE if name != "v" else 0) | \
-                (TRA_ROTARY_TILE_MAJOR if self._tile_major(plan, name) else 0)
+                        g = grads[name + "_weight"] = torch.empty(d, dtype=torch.float32, device=device)
+                        w_grad = g.data_ptr()
+                        if self.norm == "layer":
+                            g = grads[name + "_bias"] = torch.empty(d, dtype=torch.float32, device=device)
+                            b_grad = g.data_ptr()
+                w = self._param(w, name + "_weight", dtype, index)
+            else:
+                w = 0
+            _ROTARY_TENSOR.pack_into(desc, n * _ROTARY_TENSOR.size, dy.data_ptr(), dx.data_ptr(), xp, w, 0, w_grad, b_grad,
+                                     *src, *dst, *x_strides, heads, flags)
             outs.append(dx)
             n += 1
-        ws = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dq.device) if grads else None
-        _check(_lib.tra_rotary_backward(self._h, plan._h if on_plan else None, pos_ptr, ctypes.byref(args), n, B, tokens,
-                                        _DTYPES[dq.dtype], ws.data_ptr() if grads else None,
-                                        self.workspace_bytes if grads else 0, _stream()), "tra_rotary_backward")
+        ws = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device) if grads else None
+        _check(_lib.tra_rotary_backward(self._h, plan._h if on_plan else None, pos_ptr, bytes(desc), n, B, tokens,
+                                        _DTYPES[dtype], ws.data_ptr() if grads else None,
+                                        self.workspace_bytes if grads else 0, _raw_stream(index)), "tra_rotary_backward")
         return tuple(outs), grads
 
 
@@ -632,7 +652,8 @@ class PackedAttn:
         self._h = ctypes.c_void_p()
         _check(_lib.tra_packed_create(ctypes.byref(self._h), ctypes.byref(cfg)), "tra_packed_create")
         self.heads, self.kv_heads, self.head_dim, self.dtype, self.causal = heads, kv_heads, head_dim, dtype, bool(causal)
-        self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = torch.cuda.current_device()
+        self.device = torch.device("cuda", self._index)
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -652,44 +673,43 @@ class PackedAttn:
         _check(self.status(stream), "tra_packed_status")
 
     def _tensor(self, t, name, total, heads):
-        if t.device != self.device or t.dtype != self.dtype or tuple(t.shape) != (total, heads, self.head_dim) or \
-                t.stride(2) != 1:
+        s = t.stride()
+        if t.get_device() != self._index or t.dtype != self.dtype or t.shape != (total, heads, self.head_dim) or s[2] != 1:
             raise ValueError(f"{name}: expected {self.dtype} [{total}, {heads}, {self.head_dim}] on {self.device} with "
                              "contiguous channels")
-        return t.data_ptr(), t.stride()[:2]
+        return t.data_ptr(), s[0], s[1]
 
     def _ints(self, t, name, n):
-        if t.device != self.device or t.dtype != torch.int32 or tuple(t.shape) != (n,) or not t.is_contiguous():
+        if t.get_device() != self._index or t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous int32 tensor of {n} entries on {self.device}")
         return t.data_ptr()
 
     def _args(self, q, k, v, o, lse, cu_q, cu_k, k_range, max_q, max_k, sm_scale):
         if q.dim() != 3 or k.dim() != 3 or cu_q.dim() != 1 or cu_q.shape[0] < 2:
             raise ValueError("expected q, k, v [tokens, heads, head_dim] and cu_q [n_seq + 1]")
-        if torch.cuda.current_device() != self.device.index:
+        if torch.cuda.current_device() != self._index:
             raise ValueError(f"the current device must be {self.device}")
-        a = tra_packed_args_t()
         tq, tk, n = q.shape[0], k.shape[0], cu_q.shape[0] - 1
-        a.q, a.q_stride[:] = self._tensor(q, "q", tq, self.heads)
-        a.k, a.k_stride[:] = self._tensor(k, "k", tk, self.kv_heads)
-        a.v, a.v_stride[:] = self._tensor(v, "v", tk, self.kv_heads)
-        a.o, a.o_stride[:] = self._tensor(o, "o", tq, self.heads)
+        qp, q0, q1 = self._tensor(q, "q", tq, self.heads)
+        kp, k0, k1 = self._tensor(k, "k", tk, self.kv_heads)
+        vp, v0, v1 = self._tensor(v, "v", tk, self.kv_heads)
+        op, o0, o1 = self._tensor(o, "o", tq, self.heads)
+        lp = 0
         if lse is not None:
-            if lse.device != self.device or lse.dtype != torch.float32 or tuple(lse.shape) != (tq, self.heads) or \
+            if lse.get_device() != self._index or lse.dtype != torch.float32 or lse.shape != (tq, self.heads) or \
                     not lse.is_contiguous():
                 raise ValueError("lse: expected a contiguous fp32 tensor [total_q, heads]")
-            a.lse = lse.data_ptr()
-        a.cu_q = self._ints(cu_q, "cu_q", n + 1)
+            lp = lse.data_ptr()
+        cq = self._ints(cu_q, "cu_q", n + 1)
         if k_range is not None:
             if cu_k is not None:
                 raise ValueError("expected cu_k or k_range, not both")
-            a.k_begin, a.k_end = self._ints(k_range[0], "k_range", n), self._ints(k_range[1], "k_range", n)
+            begin, end = self._ints(k_range[0], "k_range", n), self._ints(k_range[1], "k_range", n)
         else:
-            a.k_begin = a.cu_q if cu_k is None else self._ints(cu_k, "cu_k", n + 1)
-            a.k_end = a.k_begin + 4
-        a.n_seq, a.total_q, a.total_k, a.max_q, a.max_k = n, tq, tk, max_q, max_k
-        a.sm_scale = self.head_dim ** -0.5 if sm_scale is None else sm_scale
-        return a
+            begin = cq if cu_k is None else self._ints(cu_k, "cu_k", n + 1)
+            end = begin + 4
+        return _PACKED_ARGS.pack(qp, kp, vp, op, lp, q0, q1, k0, k1, v0, v1, o0, o1, cq, begin, end, n, tq, tk, max_q, max_k,
+                                 self.head_dim ** -0.5 if sm_scale is None else sm_scale)
 
     def forward(self, q, k, v, cu_q, cu_k=None, *, k_range=None, max_q, max_k, o=None, lse=None, want_lse=False,
                 sm_scale=None):
@@ -698,13 +718,13 @@ class PackedAttn:
         sequences' queries and keys (a longer one is cut and reported by ``check_status``).  Rows of o and lse that
         belong to no sequence are not written."""
         if o is None:
-            o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            o = torch.empty(q.shape, dtype=self.dtype, device=self.device)
         if lse is None and want_lse:
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
         a = self._args(q, k, v, o, lse, cu_q, cu_k, k_range, max_q, max_k, sm_scale)
-        n = _lib.tra_packed_attn_workspace_bytes(self._h, a.n_seq, a.total_q, max_q, max_k)
-        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-        _check(_lib.tra_packed_attn(self._h, ctypes.byref(a), ws.data_ptr() if n else None, n, _stream()), "tra_packed_attn")
+        n = _lib.tra_packed_attn_workspace_bytes(self._h, cu_q.shape[0] - 1, q.shape[0], max_q, max_k)
+        ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+        _check(_lib.tra_packed_attn(self._h, a, ws.data_ptr() if n else None, n, _raw_stream(self._index)), "tra_packed_attn")
         return o, lse
 
     def backward(self, do, q, k, v, o, lse, cu_q, cu_k=None, *, max_q, max_k, dq=None, dk=None, dv=None, sm_scale=None):
@@ -716,13 +736,12 @@ class PackedAttn:
         if lse is None:
             raise ValueError("lse: the forward call's, made with want_lse")
         a = self._args(q, k, v, o, lse, cu_q, cu_k, None, max_q, max_k, sm_scale)
-        g = tra_packed_grads_t()
-        g.d_o, g.do_stride[:] = self._tensor(do, "do", a.total_q, self.heads)
-        g.dq, g.dq_stride[:] = self._tensor(dq, "dq", a.total_q, self.heads)
-        g.dk, g.dk_stride[:] = self._tensor(dk, "dk", a.total_k, self.kv_heads)
-        g.dv, g.dv_stride[:] = self._tensor(dv, "dv", a.total_k, self.kv_heads)
-        n = _lib.tra_packed_attn_backward_workspace_bytes(self._h, a.total_q)
-        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-        _check(_lib.tra_packed_attn_backward(self._h, ctypes.byref(a), ctypes.byref(g), ws.data_ptr() if n else None, n,
-                                             _stream()), "tra_packed_attn_backward")
+        tq, tk = q.shape[0], k.shape[0]
+        ptrs, strides = zip(*((p, s) for p, *s in (self._tensor(do, "do", tq, self.heads), self._tensor(dq, "dq", tq, self.heads),
+                                                   self._tensor(dk, "dk", tk, self.kv_heads), self._tensor(dv, "dv", tk, self.kv_heads))))
+        g = _PACKED_GRADS.pack(*ptrs, *(x for s in strides for x in s))
+        n = _lib.tra_packed_attn_backward_workspace_bytes(self._h, tq)
+        ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+        _check(_lib.tra_packed_attn_backward(self._h, a, g, ws.data_ptr() if n else None, n, _raw_stream(self._index)),
+               "tra_packed_attn_backward")
         return dq, dk, dv
