@@ -60,20 +60,34 @@ __device__ __forceinline__ tra_seq_range tra_clamp_range(int begin, int end, int
   return {b, len};
 }
 
-// Which (sequence, unit) a thread block works on, units numbered sequence by sequence, ceil(length / unit_tokens)
-// each; one warp calls it.  seq = -1: past the last unit.  Lengths are read 32 sequences at a time.
-__device__ __forceinline__ void tra_find_unit(const int32_t* begin, const int32_t* end, int n_seq, int total, int max_len,
-                                              int unit_tokens, int unit, int* status, int& seq, int& index) {
+// What a thread block works on: unit `index` of a sequence and the sequence's token ranges.
+struct tra_unit {
+  int seq, index;          // seq = -1: nothing
+  tra_seq_range q, k;
+};
+
+// Finds the block's unit, units numbered sequence by sequence, ceil(length / unit_tokens) each, length in queries or
+// (by_keys) in keys; one_each: unit s is the whole of sequence s.  One warp calls it; every lane gets the result.  32 sequences are
+// read at a time, the ranges of both sides with them, so that the block waits for one load in most launches.
+__device__ __forceinline__ tra_unit tra_find_unit(const tra_packed_launch& p, bool by_keys, bool one_each, int unit_tokens,
+                                                  int unit) {
   const int lane = threadIdx.x & 31;
-  seq = -1;
-  index = 0;
+  tra_unit u = {-1, 0, {0, 0}, {0, 0}};
+  if (one_each) {
+    u.seq = unit;
+    u.q = tra_clamp_range(p.cu_q[unit], p.cu_q[unit + 1], p.total_q, p.max_q, p.status);
+    u.k = tra_clamp_range(p.k_begin[unit], p.k_end[unit], p.total_k, p.max_k, p.status);
+    return u;
+  }
   int before = 0;
-  for (int s0 = 0; s0 < n_seq; s0 += 32) {
-    int n = 0;
-    if (s0 + lane < n_seq) {
-      const tra_seq_range r = tra_clamp_range(begin[s0 + lane], end[s0 + lane], total, max_len, status);
-      n = (r.len + unit_tokens - 1) / unit_tokens;
+  for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
+    tra_seq_range q = {0, 0}, k = {0, 0};
+    if (s0 + lane < p.n_seq) {
+      const int s = s0 + lane, q0 = p.cu_q[s], q1 = p.cu_q[s + 1], k0 = p.k_begin[s], k1 = p.k_end[s];
+      q = tra_clamp_range(q0, q1, p.total_q, p.max_q, p.status);
+      k = tra_clamp_range(k0, k1, p.total_k, p.max_k, p.status);
     }
+    const int n = ((by_keys ? k.len : q.len) + unit_tokens - 1) / unit_tokens;
     int incl = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -84,12 +98,17 @@ __device__ __forceinline__ void tra_find_unit(const int32_t* begin, const int32_
     const unsigned hit = __ballot_sync(0xffffffffu, unit >= excl && unit < before + incl);
     if (hit) {
       const int l = __ffs(hit) - 1;
-      seq = s0 + l;
-      index = unit - __shfl_sync(0xffffffffu, excl, l);
-      return;
+      u.seq = s0 + l;
+      u.index = unit - __shfl_sync(0xffffffffu, excl, l);
+      u.q.begin = __shfl_sync(0xffffffffu, q.begin, l);
+      u.q.len = __shfl_sync(0xffffffffu, q.len, l);
+      u.k.begin = __shfl_sync(0xffffffffu, k.begin, l);
+      u.k.len = __shfl_sync(0xffffffffu, k.len, l);
+      return u;
     }
     before += __shfl_sync(0xffffffffu, incl, 31);
   }
+  return u;
 }
 
 }  // namespace

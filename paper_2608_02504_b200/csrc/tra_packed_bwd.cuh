@@ -55,7 +55,7 @@ struct BwdCtl {
   uint64_t drain;
   uint32_t tmem_base;
   int abort_flag;
-  int seq, unit;
+  tra_unit unit;
 };
 static_assert(sizeof(BwdCtl) <= 512, "control block");
 
@@ -82,7 +82,6 @@ __device__ __forceinline__ void bwd_init(BwdCtl* ctl) {
   mbar_init(smem_u32(&ctl->drain), 1);
   ctl->abort_flag = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
 __device__ __forceinline__ void bwd_teardown(BwdCtl* ctl, uint32_t tmem, int warp) {
@@ -95,7 +94,7 @@ __device__ __forceinline__ void bwd_teardown(BwdCtl* ctl, uint32_t tmem, int war
       while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
     }
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    tmem_free_all(tmem);
   }
 }
 
@@ -147,26 +146,36 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int kvh = blockIdx.y;
 
+  const int tile_tokens = p.tile_tokens, box_rows = tile_tokens * p.group;
+
+  // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    int seq = blockIdx.x, unit = 0;
-    if (p.max_k > kTileM)
-      tra_find_unit(p.k_begin, p.k_end, p.n_seq, p.total_k, p.max_k, kTileM, (int)blockIdx.x, p.status, seq, unit);
-    if (lane == 0) {
-      ctl->seq = seq;
-      ctl->unit = unit;
-    }
+    const tra_unit u = tra_find_unit(p, true, p.max_k <= kTileM, kTileM, (int)blockIdx.x);
+    if (lane == 0) ctl->unit = u;
+  } else if (warp == 9) {
+    tmem_alloc_all(&ctl->tmem_base);
   } else if (tid == 32) {
     bwd_init(ctl);
+  } else if (tid == 64) {
+    prefetch_map(&p.map_q);
+    prefetch_map(&p.map_do);
+    prefetch_map(&p.map_k);
+    prefetch_map(&p.map_v);
   }
+  if (box_rows < kTileM && warp >= 2 && warp < 8)        // rows that no box fills
+    zero_tile_rows(sStage, box_rows, kTileM, 2 * kBwdStages * C::kAtoms, C::kAtomBytes, tid - 64, 192);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  tc_fence_before();
   __syncthreads();
-  if (ctl->seq < 0) return;
-  const int seq = ctl->seq;
-  const tra_seq_range qr = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
-  const tra_seq_range kr = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
-  const int key0 = ctl->unit * kTileM;
-  if (key0 >= kr.len) return;
+  tc_fence_after();
+  const uint32_t tmem = ctl->tmem_base;
+  const tra_seq_range qr = ctl->unit.q, kr = ctl->unit.k;
+  const int key0 = ctl->unit.index * kTileM;
+  if (ctl->unit.seq < 0 || key0 >= kr.len) {
+    if (warp == 9) tmem_free_all(tmem);
+    return;
+  }
   const int ahead = kr.len - qr.len;
-  const int tile_tokens = p.tile_tokens, box_rows = tile_tokens * p.group;
   const int n_tiles_all = (qr.len + tile_tokens - 1) / tile_tokens;
   // causal: key j is seen by the tokens from j - ahead on
   const int first_tile = kCausal ? max(key0 - ahead, 0) / tile_tokens : 0;
@@ -174,20 +183,6 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
   const int tail_rows = (qr.len - (n_tiles_all - 1) * tile_tokens) * p.group;      // rows of the last tile
   const bool tail = n > 0 && tail_rows < box_rows;
   volatile int* abort_flag = &ctl->abort_flag;
-
-  if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&ctl->tmem_base))
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  if (box_rows < kTileM) {        // rows that no box fills
-    zero_tile_rows(sStage, box_rows, kTileM, 2 * kBwdStages * C::kAtoms, C::kAtomBytes, tid, kBwdThreads);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = ctl->tmem_base;
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBwdRegsControl));
@@ -431,45 +426,40 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __g
   const int kvh = blockIdx.y;
   const int tile_tokens = p.tile_tokens, box_rows = tile_tokens * p.group;
 
+  // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    const int want = (int)gridDim.x - 1 - (int)blockIdx.x;   // the last tiles of a causal sequence are the longest
-    int seq = want, unit = 0;
-    if (p.max_q > tile_tokens)
-      tra_find_unit(p.cu_q, p.cu_q + 1, p.n_seq, p.total_q, p.max_q, tile_tokens, want, p.status, seq, unit);
-    if (lane == 0) {
-      ctl->seq = seq;
-      ctl->unit = unit;
-    }
+    // the last tiles of a causal sequence are the longest: launched first
+    const tra_unit u = tra_find_unit(p, false, p.max_q <= tile_tokens, tile_tokens, (int)gridDim.x - 1 - (int)blockIdx.x);
+    if (lane == 0) ctl->unit = u;
+  } else if (warp == 9) {
+    tmem_alloc_all(&ctl->tmem_base);
   } else if (tid == 32) {
     bwd_init(ctl);
+  } else if (tid == 64) {
+    prefetch_map(&p.map_q);
+    prefetch_map(&p.map_do);
+    prefetch_map(&p.map_k);
+    prefetch_map(&p.map_v);
   }
+  if (box_rows < kTileM && warp >= 2 && warp < 8)        // rows that no box fills
+    zero_tile_rows(sQ, box_rows, kTileM, 2 * C::kAtoms, C::kAtomBytes, tid - 64, 192);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  tc_fence_before();
   __syncthreads();
-  if (ctl->seq < 0) return;
-  const int seq = ctl->seq;
-  const tra_seq_range qr = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
-  const tra_seq_range kr = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
-  const int tok0 = ctl->unit * tile_tokens;
-  if (tok0 >= qr.len) return;
+  tc_fence_after();
+  const uint32_t tmem = ctl->tmem_base;
+  const tra_seq_range qr = ctl->unit.q, kr = ctl->unit.k;
+  const int tok0 = ctl->unit.index * tile_tokens;
+  if (ctl->unit.seq < 0 || tok0 >= qr.len) {
+    if (warp == 9) tmem_free_all(tmem);
+    return;
+  }
   const int ahead = kr.len - qr.len;
   const int last_tok = min(tok0 + tile_tokens, qr.len) - 1;
   const int keys = kCausal ? min(max(last_tok + 1 + ahead, 0), kr.len) : kr.len;
   const int n = (keys + kTileM - 1) / kTileM;
   const bool tail = n > 0 && n * kTileM > kr.len;
   volatile int* abort_flag = &ctl->abort_flag;
-
-  if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&ctl->tmem_base))
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  if (box_rows < kTileM) {
-    zero_tile_rows(sQ, box_rows, kTileM, 2 * C::kAtoms, C::kAtomBytes, tid, kBwdThreads);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = ctl->tmem_base;
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBwdRegsControl));

@@ -53,7 +53,7 @@ struct FwdCtl {
   uint64_t drain;
   uint32_t tmem_base;
   int abort_flag;
-  int seq, pair;
+  tra_unit unit;
 };
 static_assert(sizeof(FwdCtl) <= 512, "control block");
 
@@ -70,14 +70,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
   // the last tiles of a causal sequence are the longest: launched first
   const int unit = p.n_units - 1 - (int)blockIdx.x;
 
+  const int box_rows = p.tile_tokens * p.group;
+  // set-up in parallel, one barrier: the block's unit, the mbarriers, tensor memory, and zeros in the rows of the query tiles
+  // that no box fills (group does not divide 128), so that they stay harmless
   if (warp == 0) {
-    int seq = unit, pair = 0;
-    if (p.max_q > 2 * p.tile_tokens)       // else one pair per sequence
-      tra_find_unit(p.cu_q, p.cu_q + 1, p.n_seq, p.total_q, p.max_q, 2 * p.tile_tokens, unit, p.status, seq, pair);
-    if (lane == 0) {
-      ctl->seq = seq;
-      ctl->pair = pair;
-    }
+    const tra_unit u = tra_find_unit(p, false, p.max_q <= 2 * p.tile_tokens, 2 * p.tile_tokens, unit);
+    if (lane == 0) ctl->unit = u;
+  } else if (warp == 9) {
+    tmem_alloc_all(&ctl->tmem_base);
   } else if (tid == 32) {
     mbar_init(smem_u32(&ctl->q_full), 1);
     for (int i = 0; i < C::kSlots; ++i) mbar_init(smem_u32(&ctl->kv_full[i]), 1);
@@ -92,15 +92,23 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
     mbar_init(smem_u32(&ctl->drain), 1);
     ctl->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  } else if (tid == 64) {
+    prefetch_map(&p.map_q);
+    prefetch_map(&p.map_k);
+    prefetch_map(&p.map_v);
   }
+  if (box_rows < kTileM && warp >= 2 && warp < 8) zero_tile_rows(sQ, box_rows, kTileM, 2 * C::kAtoms, C::kAtomBytes, tid - 64, 192);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  tc_fence_before();
   __syncthreads();
-  if (ctl->seq < 0) return;
-  const int seq = ctl->seq;
-  const tra_seq_range qr = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
-  const tra_seq_range kr = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
-  const int tok0 = ctl->pair * 2 * p.tile_tokens;         // first token of tile 0, inside the sequence
-  if (tok0 >= qr.len) return;                             // a sequence without queries
+  tc_fence_after();
+  const uint32_t tmem = ctl->tmem_base;
+  const tra_seq_range qr = ctl->unit.q, kr = ctl->unit.k;
+  const int tok0 = ctl->unit.index * 2 * p.tile_tokens;   // first token of tile 0, inside the sequence
+  if (ctl->unit.seq < 0 || tok0 >= qr.len) {              // past the last unit, or a sequence without queries
+    if (warp == 9) tmem_free_all(tmem);
+    return;
+  }
   const int ahead = kr.len - qr.len;                      // causal: token i sees keys 0 .. i + ahead
   // keys the last token of a tile sees, and the tile's key blocks
   auto tile_keys = [&](int k) -> int {
@@ -118,22 +126,6 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
   const int n_own[2] = {max(min(nb0, v_end) - v_begin, 0), max(min(nb1, v_end) - v_begin, 0)};
   const bool tail = n_entries > 0 && v_end * kKeyTile > kr.len;      // the last V tile reaches past the sequence
   volatile int* abort_flag = &ctl->abort_flag;
-
-  if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&ctl->tmem_base))
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  // rows of the query tiles that no box fills (group does not divide 128): zeros, so that they stay harmless
-  const int box_rows = p.tile_tokens * p.group;
-  if (box_rows < kTileM) {
-    zero_tile_rows(sQ, box_rows, kTileM, 2 * C::kAtoms, C::kAtomBytes, tid, kFwdThreads);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = ctl->tmem_base;
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFwdRegsControl));
@@ -269,37 +261,40 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kFwdRegsSoftmax));
     // ================================================================== softmax + epilogue
     const int k = warp >> 2;
-    const int r = tid & (kTileM - 1);
-    const int r_tok = r / p.group, r_head = r - r_tok * p.group;
-    const int tok = tok0 + k * p.tile_tokens + r_tok;             // inside the sequence
-    const bool row_valid = r < box_rows && tok < qr.len;
-    // rows that hold no query follow the tile's last one, so that they force no mask on their warp
-    const int mask_tok = min(tok, min(tok0 + (k + 1) * p.tile_tokens, qr.len) - 1);
-    const int seen = kCausal ? min(max(mask_tok + 1 + ahead, 0), kr.len) : kr.len;
-    const bool warp_on = __any_sync(0xffffffffu, row_valid);
+    int r = tid & (kTileM - 1);
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_o = tmem + lane_base + 256 + k * 128, t_s = tmem + lane_base + k * 128;
-    const float scale_log2 = p.sm_scale * kLog2e;
-
+    const int n = n_own[k];
     float m = -INFINITY, l = 0.f, l_exact = 0.f;
     bool alive = true;
-    const int n = n_own[k];
-    for (int e = 0; e < n; ++e) {
-      if (!mbar_wait_warp(smem_u32(&ctl->s_full[k]), (uint32_t)e & 1u, abort_flag, p.status)) {
-        alive = false;
-        break;
+    if ((warp & 3) * 32 >= box_rows || tok0 + k * p.tile_tokens + (warp & 3) * 32 / p.group >= qr.len) {
+      // a warp without a row keeps up with the barriers; what its lanes multiply stays in its own, unstored rows
+      for (int e = 0; e < n && alive; ++e) {
+        alive = mbar_wait_warp(smem_u32(&ctl->s_full[k]), (uint32_t)e & 1u, abort_flag, p.status);
+        if (alive && lane == 0) {
+          mbar_arrive(smem_u32(&ctl->p_ready[k][0]));
+          mbar_arrive(smem_u32(&ctl->p_ready[k][1]));
+        }
+        __syncwarp();
       }
-      tc_fence_after();
-      float alpha = 1.f;
-      uint32_t sb[128];
-      bool row_on = false;
-      if (warp_on) {
+    } else {
+      const float scale_log2 = p.sm_scale * kLog2e;
+      // columns of the first block that the row sees; rows that hold no query follow the tile's last one, so that they force
+      // no mask on their warp
+      const int mask_tok = min(tok0 + k * p.tile_tokens + r / p.group, min(tok0 + (k + 1) * p.tile_tokens, qr.len) - 1);
+      int col_limit = (kCausal ? min(max(mask_tok + 1 + ahead, 0), kr.len) : kr.len) - v_begin * kKeyTile;
+      for (int e = 0; e < n; ++e, col_limit -= kKeyTile) {
+        if (!mbar_wait_warp(smem_u32(&ctl->s_full[k]), (uint32_t)e & 1u, abort_flag, p.status)) {
+          alive = false;
+          break;
+        }
+        tc_fence_after();
+        uint32_t sb[128];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, &sb[c * 32]);
         tmem_wait_ld(&sb[0]);
 #pragma unroll
         for (int c = 1; c < 4; ++c) reg_fence32(&sb[c * 32]);
-        const int col_limit = seen - (v_begin + e) * kKeyTile;       // columns at and past it are not seen
         if (__any_sync(0xffffffffu, col_limit < kKeyTile)) {
 #pragma unroll
           for (int j = 0; j < 128; ++j)
@@ -313,33 +308,31 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         }
         mx0 = fmax3(mx0, __uint_as_float(sb[126]), __uint_as_float(sb[127]));
         const float m_blk = fmaxf(mx0, mx1) * scale_log2;
-        row_on = m_blk > -INFINITY || m > -INFINITY;
+        float alpha = 1.f;
         if (m_blk > m + kRescaleThreshold) {          // also the first block that holds a key (m = -inf)
           alpha = ex2(m - m_blk);
           l *= alpha;
           l_exact *= alpha;
           m = m_blk;
         }
-      }
-      if (__any_sync(0xffffffffu, alpha != 1.f) && e > 0) {
+        if (__any_sync(0xffffffffu, alpha != 1.f) && e > 0) {
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t o[32];
-          tmem_ld32(t_o + c * 32, o);
-          tmem_wait_ld(o);
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld32(t_o + c * 32, o);
+            tmem_wait_ld(o);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-          tmem_st32(t_o + c * 32, o);
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+            tmem_st32(t_o + c * 32, o);
+          }
         }
-      }
-      const float neg_m = row_on ? -m : 0.f;
-      const uint64_t scale2 = pack2(scale_log2, scale_log2), neg_m2 = pack2(neg_m, neg_m);
-      float l_lo = 0.f, l_hi = 0.f;
-      uint64_t e2 = 0ull;
+        const float neg_m = m > -INFINITY ? -m : 0.f;       // no key seen so far: every score is -inf
+        const uint64_t scale2 = pack2(scale_log2, scale_log2), neg_m2 = pack2(neg_m, neg_m);
+        float l_lo = 0.f, l_hi = 0.f;
+        uint64_t e2 = 0ull;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t pk[16];
-        if (warp_on) {
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pk[16];
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
             const uint64_t t2 =
@@ -354,32 +347,38 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
             if (kExact) e2 = fadd2(e2, pack2(x0, x1));
             pk[j >> 1] = packed;
           }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) pk[j] = 0u;
+          tmem_st16(t_s + c * 16, pk);
+          if (c & 1) {
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[k][c >> 1]));
+          }
         }
-        tmem_st16(t_s + c * 16, pk);
-        if (c & 1) {
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[k][c >> 1]));
+        l += l_lo + l_hi;
+        if (kExact) {
+          float a, b;
+          unpack2(e2, a, b);
+          l_exact += a + b;
         }
-      }
-      l += l_lo + l_hi;
-      if (kExact) {
-        float a, b;
-        unpack2(e2, a, b);
-        l_exact += a + b;
       }
     }
 
     // ---- epilogue --------------------------------------------------------------------------
     if (alive && n > 0) alive = mbar_wait_warp(smem_u32(&ctl->drain), 0u, abort_flag, p.status);
-    if (alive && (k == 0 || tile1_on)) {
+    // Read again from shared memory and the thread index: the loop above needs every register for the score row.
+    asm volatile("" : "+r"(r));
+    tra_unit own;
+    own.index = *(volatile int*)&ctl->unit.index;
+    own.q.begin = *(volatile int*)&ctl->unit.q.begin;
+    own.q.len = *(volatile int*)&ctl->unit.q.len;
+    const int tok = own.index * 2 * p.tile_tokens + k * p.tile_tokens + r / p.group;     // inside the sequence
+    const int r_head = r % p.group;
+    const bool row_valid = r < p.tile_tokens * p.group && tok < own.q.len;
+    if (alive) {
       tc_fence_after();
       const float inv_l = l > 0.f ? 1.f / l : 0.f;
-      const long long tok_g = qr.begin + (row_valid ? tok : 0);
+      const long long tok_g = own.q.begin + (row_valid ? tok : 0);
       const int head = kvh * p.group + (row_valid ? r_head : 0);
       const long long row_g = tok_g * p.heads + head;
       T* orow = (T*)p.o + tok_g * p.o_stride[0] + head * p.o_stride[1];
@@ -433,7 +432,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
     }
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    tmem_free_all(tmem);
   }
 }
 
