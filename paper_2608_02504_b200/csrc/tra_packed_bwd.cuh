@@ -30,26 +30,36 @@ namespace {
 constexpr int kBwdThreads = 384;
 constexpr int kBwdRegsSoftmax = 216;     // 2 * 216 + 72 = 3 * 168, the registers of the launch
 constexpr int kBwdRegsControl = 72;
-constexpr int kBwdStages = 2;
+constexpr int kStatStages = 2;           // of the query rows' lse and delta (dkv)
 
 template <int D>
 struct BwdCfg {
   static constexpr int kAtoms = D / 64;
   static constexpr int kAtomBytes = kTileM * 128;
   static constexpr int kTileBytes = kAtoms * kAtomBytes;
-  static constexpr int kSmemData = (2 + 2 * kBwdStages) * kTileBytes;      // two resident tiles, stages of two tiles
-  static constexpr int kSmemNeeded = kSmemData + 1024 + 512 + 2 * kBwdStages * kTileM * 4;
+  // Rings of streamed tiles.  A = Q (dkv) or K (dq), which two products use, the second one a step later; B = dO or V, done
+  // with earlier.  A ring of two A tiles left the tensor pipe waiting for its loads (440 cycles of 3,750 per step, dkv).
+  static constexpr int kA = D == 128 ? 3 : 4;
+  static constexpr int kB = D == 128 ? 2 : 4;
+  static constexpr int kSmemData = (2 + kA + kB) * kTileBytes;             // and two resident tiles
+  static constexpr int kSmemNeeded = kSmemData + 512 + 2 * kStatStages * kTileM * 4;
   // at least 120 KB so that one block owns an SM and its whole tensor memory
   static constexpr int kSmemBytes = kSmemNeeded > 120 * 1024 ? kSmemNeeded : 120 * 1024;
+  static_assert(kSmemBytes <= 232448, "shared memory of a block");
+  // tensor memory: with D = 64 there is room for P and dS of their own, and the next S and dP need not wait for the
+  // products that read them
+  static constexpr bool kApart = D == 64;
+  static constexpr int kSum0 = 256, kSum1 = kApart ? 320 : 384;            // dV, dK
+  static constexpr int kP = kApart ? 384 : 0, kDs = kApart ? 448 : 128;
+  static constexpr int kPStep = kApart ? 32 : 64;                          // columns from one half's P to the other's
 };
 
 struct BwdCtl {
   uint64_t own_full;                     // the resident tiles
-  uint64_t a_full[kBwdStages], b_full[kBwdStages];   // streamed tiles: Q / dO (dkv), K / V (dq)
-  uint64_t stage_free[kBwdStages];
-  uint64_t stat_full[kBwdStages], stat_free[kBwdStages];
+  uint64_t a_full[4], b_full[4], a_free[4], b_free[4];       // streamed tiles
+  uint64_t stat_full[kStatStages], stat_free[kStatStages];
   uint64_t s_full, dp_full;
-  uint64_t s_read, dp_read;              // dq: the threads hold S / dP in registers
+  uint64_t s_read, dp_read;              // the threads hold S / dP in registers
   uint64_t p_ready[2], ds_ready[2];      // per 64-column half
   uint64_t tail_full, tail_ready;
   uint64_t drain;
@@ -62,10 +72,13 @@ static_assert(sizeof(BwdCtl) <= 512, "control block");
 // Set-up shared by the two kernels: barriers and the block's (sequence, unit).
 __device__ __forceinline__ void bwd_init(BwdCtl* ctl) {
   mbar_init(smem_u32(&ctl->own_full), 1);
-  for (int i = 0; i < kBwdStages; ++i) {
+  for (int i = 0; i < 4; ++i) {
     mbar_init(smem_u32(&ctl->a_full[i]), 1);
     mbar_init(smem_u32(&ctl->b_full[i]), 1);
-    mbar_init(smem_u32(&ctl->stage_free[i]), 1);
+    mbar_init(smem_u32(&ctl->a_free[i]), 1);
+    mbar_init(smem_u32(&ctl->b_free[i]), 1);
+  }
+  for (int i = 0; i < kStatStages; ++i) {
     mbar_init(smem_u32(&ctl->stat_full[i]), 1);
     mbar_init(smem_u32(&ctl->stat_free[i]), 8);
   }
@@ -95,6 +108,50 @@ __device__ __forceinline__ void bwd_teardown(BwdCtl* ctl, uint32_t tmem, int war
     }
     tc_fence_after();
     tmem_free_all(tmem);
+  }
+}
+
+// Position in a ring: tile i lies in slot i % N and is the (i / N)-th of its slot.
+template <int N>
+struct RingPos {
+  int slot = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++slot == N) {
+      slot = 0;
+      phase ^= 1u;
+    }
+  }
+};
+
+// The producer's loop of either kernel: tile i of each ring as soon as its slot is free.  The
+// last pair goes to tail_full when rows past the sequence's end have to be zeroed in it.
+template <int D, typename LoadA, typename LoadB>
+__device__ __forceinline__ void bwd_produce(BwdCtl* ctl, int n, bool tail, uint32_t bytes, volatile int* abort_flag, int* status,
+                                            LoadA load_a, LoadB load_b) {
+  using C = BwdCfg<D>;
+  RingPos<C::kA> a;
+  RingPos<C::kB> b;
+  for (int i = 0; i < n; ++i) {
+    const bool last = tail && i == n - 1;
+    const uint32_t abar = smem_u32(last ? &ctl->tail_full : &ctl->a_full[a.slot]);
+    const uint32_t bbar = smem_u32(last ? &ctl->tail_full : &ctl->b_full[b.slot]);
+    if (last) mbar_expect_tx(abar, 2 * bytes);
+    auto do_a = [&]() -> bool {
+      if (i >= C::kA && !mbar_wait(smem_u32(&ctl->a_free[a.slot]), a.phase ^ 1u, abort_flag, status)) return false;
+      if (!last) mbar_expect_tx(abar, bytes);
+      load_a(i, a.slot, abar);
+      return true;
+    };
+    auto do_b = [&]() -> bool {
+      if (i >= C::kB && !mbar_wait(smem_u32(&ctl->b_free[b.slot]), b.phase ^ 1u, abort_flag, status)) return false;
+      if (!last) mbar_expect_tx(bbar, bytes);
+      load_b(i, b.slot, bbar);
+      return true;
+    };
+    if (!(do_a() && do_b())) break;
+    a.next();
+    b.next();
   }
 }
 
@@ -135,14 +192,14 @@ __device__ __forceinline__ void store32(T* dst, const uint32_t* bits, float mul)
 template <typename T, int D, bool kCausal>
 __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __grid_constant__ tra_packed_launch p) {
   using C = BwdCfg<D>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
   uint8_t* sK = smem;
   uint8_t* sV = smem + C::kTileBytes;
-  uint8_t* sStage = smem + 2 * C::kTileBytes;               // [stage][Q, dO]
+  uint8_t* sA = smem + 2 * C::kTileBytes;                   // Q tiles
+  uint8_t* sB = sA + C::kA * C::kTileBytes;                 // dO tiles
   BwdCtl* ctl = (BwdCtl*)(smem + C::kSmemData);
   float* s_lse2 = (float*)(smem + C::kSmemData + 512);       // [stage][128], then delta
-  float* s_delta = s_lse2 + kBwdStages * kTileM;
+  float* s_delta = s_lse2 + kStatStages * kTileM;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int kvh = blockIdx.y;
 
@@ -163,7 +220,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
     prefetch_map(&p.map_v);
   }
   if (box_rows < kTileM && warp >= 2 && warp < 8)        // rows that no box fills
-    zero_tile_rows(sStage, box_rows, kTileM, 2 * kBwdStages * C::kAtoms, C::kAtomBytes, tid - 64, 192);
+    zero_tile_rows(sA, box_rows, kTileM, (C::kA + C::kB) * C::kAtoms, C::kAtomBytes, tid - 64, 192);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   tc_fence_before();
   __syncthreads();
@@ -195,33 +252,23 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
           tma_load_3d(smem_u32(sK + a * C::kAtomBytes), &p.map_k, own, a * 64, kvh, kr.begin + key0);
           tma_load_3d(smem_u32(sV + a * C::kAtomBytes), &p.map_v, own, a * 64, kvh, kr.begin + key0);
         }
-        for (int i = 0; i < n; ++i) {
-          const int st = i % kBwdStages;
-          if (i >= kBwdStages && !mbar_wait(smem_u32(&ctl->stage_free[st]), (uint32_t)(i / kBwdStages - 1) & 1u, abort_flag, p.status))
-            break;
-          const bool last_tail = tail && i == n - 1;
-          const uint32_t qbar = smem_u32(last_tail ? &ctl->tail_full : &ctl->a_full[st]);
-          const uint32_t obar = smem_u32(last_tail ? &ctl->tail_full : &ctl->b_full[st]);
-          const uint32_t bytes = C::kAtoms * box_rows * 128;
-          const int tok = qr.begin + (first_tile + i) * tile_tokens;
-          uint8_t* dst = sStage + st * 2 * C::kTileBytes;
-          if (last_tail) {
-            mbar_expect_tx(qbar, 2 * bytes);
-          } else {
-            mbar_expect_tx(qbar, bytes);
-            mbar_expect_tx(obar, bytes);
-          }
-          for (int a = 0; a < C::kAtoms; ++a)
-            tma_load_3d(smem_u32(dst + a * C::kAtomBytes), &p.map_q, qbar, a * 64, kvh * p.group, tok);
-          for (int a = 0; a < C::kAtoms; ++a)
-            tma_load_3d(smem_u32(dst + C::kTileBytes + a * C::kAtomBytes), &p.map_do, obar, a * 64, kvh * p.group, tok);
-        }
+        const int tok0 = qr.begin + first_tile * tile_tokens;
+        bwd_produce<D>(
+            ctl, n, tail, C::kAtoms * box_rows * 128, abort_flag, p.status,
+            [&](int i, int slot, uint32_t bar) {
+              for (int a = 0; a < C::kAtoms; ++a)
+                tma_load_3d(smem_u32(sA + slot * C::kTileBytes + a * C::kAtomBytes), &p.map_q, bar, a * 64, kvh * p.group, tok0 + i * tile_tokens);
+            },
+            [&](int i, int slot, uint32_t bar) {
+              for (int a = 0; a < C::kAtoms; ++a)
+                tma_load_3d(smem_u32(sB + slot * C::kTileBytes + a * C::kAtomBytes), &p.map_do, bar, a * 64, kvh * p.group, tok0 + i * tile_tokens);
+            });
       }
     } else if (warp == 10) {
       // ================================================================== rows past the sequence's end
       if (tail && mbar_wait_warp(smem_u32(&ctl->tail_full), 0u, abort_flag, p.status)) {
-        uint8_t* st = sStage + ((n - 1) % kBwdStages) * 2 * C::kTileBytes;
-        zero_tile_rows(st, tail_rows, box_rows, 2 * C::kAtoms, C::kAtomBytes, lane, 32);
+        zero_tile_rows(sA + ((n - 1) % C::kA) * C::kTileBytes, tail_rows, box_rows, C::kAtoms, C::kAtomBytes, lane, 32);
+        zero_tile_rows(sB + ((n - 1) % C::kB) * C::kTileBytes, tail_rows, box_rows, C::kAtoms, C::kAtomBytes, lane, 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->tail_ready));
@@ -229,8 +276,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
     } else if (warp == 11) {
       // ================================================================== lse and delta of the query rows
       for (int i = 0; i < n; ++i) {
-        const int st = i % kBwdStages;
-        if (i >= kBwdStages && !mbar_wait_warp(smem_u32(&ctl->stat_free[st]), (uint32_t)(i / kBwdStages - 1) & 1u, abort_flag, p.status))
+        const int st = i % kStatStages;
+        if (i >= kStatStages && !mbar_wait_warp(smem_u32(&ctl->stat_free[st]), (uint32_t)(i / kStatStages - 1) & 1u, abort_flag, p.status))
           break;
         const int tok0 = (first_tile + i) * tile_tokens;
 #pragma unroll
@@ -244,8 +291,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
             lse2 = v == -INFINITY ? INFINITY : v;
             delta = p.delta[row];
           }
-          s_lse2[st * kTileM + r] = lse2;
-          s_delta[st * kTileM + r] = delta;
+          s_lse2[st * kTileM + r] = -lse2;               // negated for the packed multiply-add
+          s_delta[st * kTileM + r] = -delta;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->stat_full[st]));
@@ -256,29 +303,32 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
       constexpr uint32_t kIdescD = make_idesc_t<T>(D, true);
       constexpr uint32_t kHi = desc_hi(1024);
       const uint32_t k_lo = desc_lo(smem_u32(sK), 16), v_lo = desc_lo(smem_u32(sV), 16);
-      const uint32_t stage_k = desc_lo(smem_u32(sStage), 16);                  // K-major views of Q; dO one tile behind
-      const uint32_t stage_mn = desc_lo(smem_u32(sStage), C::kAtomBytes);      // MN-major views
+      const uint32_t a_k = desc_lo(smem_u32(sA), 16), a_mn = desc_lo(smem_u32(sA), C::kAtomBytes);     // K-major and MN-major views
+      const uint32_t b_k = desc_lo(smem_u32(sB), 16), b_mn = desc_lo(smem_u32(sB), C::kAtomBytes);
       constexpr uint32_t kTile = C::kTileBytes >> 4;
+      RingPos<C::kA> qs, qd;                 // Q of the next S, of the next dK
+      RingPos<C::kB> os, od;                 // dO of the next dP, of the next dV
       bool alive = mbar_wait(smem_u32(&ctl->own_full), 0u, abort_flag, p.status);
-      auto wait_q = [&](int i) -> bool {
-        if (tail && i == n - 1) return mbar_wait(smem_u32(&ctl->tail_ready), 0u, abort_flag, p.status);
-        return mbar_wait(smem_u32(&ctl->a_full[i % kBwdStages]), (uint32_t)(i / kBwdStages) & 1u, abort_flag, p.status);
-      };
-      auto wait_do = [&](int i) -> bool {
-        if (tail && i == n - 1) return true;                                   // came with Q
-        return mbar_wait(smem_u32(&ctl->b_full[i % kBwdStages]), (uint32_t)(i / kBwdStages) & 1u, abort_flag, p.status);
-      };
-      auto issue_s = [&](int i) {
+      auto issue_s = [&](int i) -> bool {
+        if (!(tail && i == n - 1 ? mbar_wait(smem_u32(&ctl->tail_ready), 0u, abort_flag, p.status)
+                                 : mbar_wait(smem_u32(&ctl->a_full[qs.slot]), qs.phase, abort_flag, p.status)))
+          return false;
         tc_fence_after();
-        mma_tiles<D>(tmem, k_lo, stage_k + (uint32_t)(i % kBwdStages) * 2 * kTile, kIdescS);
+        mma_tiles<D>(tmem, k_lo, a_k + (uint32_t)qs.slot * kTile, kIdescS);
         tc_commit(smem_u32(&ctl->s_full));
+        qs.next();
+        return true;
       };
-      auto issue_dp = [&](int i) {
+      auto issue_dp = [&](int i) -> bool {
+        // (the last pair of a tail came with Q)
+        if (!(tail && i == n - 1) && !mbar_wait(smem_u32(&ctl->b_full[os.slot]), os.phase, abort_flag, p.status)) return false;
         tc_fence_after();
-        mma_tiles<D>(tmem + 128, v_lo, stage_k + ((uint32_t)(i % kBwdStages) * 2 + 1) * kTile, kIdescS);
+        mma_tiles<D>(tmem + 128, v_lo, b_k + (uint32_t)os.slot * kTile, kIdescS);
         tc_commit(smem_u32(&ctl->dp_full));
+        os.next();
+        return true;
       };
-      // sum[tmem] += A[tmem, its 128 rows per half] * B[MN-major tile]
+      // sum[tmem] += A[tmem] * B[MN-major tile], each 64-row half as soon as it is announced
       auto issue_sum = [&](uint32_t d, uint32_t a, uint32_t b_lo, uint64_t* ready, int i) -> bool {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -286,29 +336,25 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
           tc_fence_after();
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
-            tc_mma_ts(d, a + h * 64 + kk * 8, b_lo + (h * 4 + kk) * (2048 >> 4), kHi, kIdescD, h + kk > 0 ? 1u : (i > 0 ? 1u : 0u));
+            tc_mma_ts(d, a + h * C::kPStep + kk * 8, b_lo + (h * 4 + kk) * (2048 >> 4), kHi, kIdescD, h + kk > 0 ? 1u : (i > 0 ? 1u : 0u));
         }
         return true;
       };
-      if (alive && n > 0) {
-        alive = wait_q(0);
-        if (alive) issue_s(0);
-        if (alive) alive = wait_do(0);
-        if (alive) issue_dp(0);
-      }
+      alive = alive && n > 0 && issue_s(0) && issue_dp(0);
       for (int i = 0; i < n && alive; ++i) {
-        const uint32_t st = (uint32_t)(i % kBwdStages) * 2;
-        if (!(alive = issue_sum(tmem + 256, tmem, stage_mn + (st + 1) * kTile, ctl->p_ready, i))) break;      // dV += P^T dO
-        if (i + 1 < n) {
-          if (!(alive = wait_q(i + 1))) break;
-          issue_s(i + 1);
-        }
-        if (!(alive = issue_sum(tmem + 384, tmem + 128, stage_mn + st * kTile, ctl->ds_ready, i))) break;     // dK += dS^T Q
-        tc_commit(smem_u32(&ctl->stage_free[i % kBwdStages]));
-        if (i + 1 < n) {
-          if (!(alive = wait_do(i + 1))) break;
-          issue_dp(i + 1);
-        }
+        const bool next = i + 1 < n;
+        if (C::kApart && next)
+          if (!(alive = mbar_wait(smem_u32(&ctl->s_read), (uint32_t)i & 1u, abort_flag, p.status) && issue_s(i + 1))) break;
+        if (!(alive = issue_sum(tmem + C::kSum0, tmem + C::kP, b_mn + (uint32_t)od.slot * kTile, ctl->p_ready, i))) break;     // dV += P^T dO
+        tc_commit(smem_u32(&ctl->b_free[od.slot]));
+        od.next();
+        if (C::kApart && next)
+          if (!(alive = mbar_wait(smem_u32(&ctl->dp_read), (uint32_t)i & 1u, abort_flag, p.status) && issue_dp(i + 1))) break;
+        if (!C::kApart && next && !(alive = issue_s(i + 1))) break;
+        if (!(alive = issue_sum(tmem + C::kSum1, tmem + C::kDs, a_mn + (uint32_t)qd.slot * kTile, ctl->ds_ready, i))) break;   // dK += dS^T Q
+        tc_commit(smem_u32(&ctl->a_free[qd.slot]));
+        qd.next();
+        if (!C::kApart && next && !(alive = issue_dp(i + 1))) break;
       }
       tc_commit(smem_u32(&ctl->drain));
       mbar_wait(smem_u32(&ctl->drain), 0u, abort_flag, p.status);
@@ -320,13 +366,17 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
     const int r = tid & (kTileM - 1);                        // key inside the tile
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lane_base + h * 64, t_dp = t_s + 128;
+    const uint32_t t_p = tmem + lane_base + C::kP + h * C::kPStep, t_ds = tmem + lane_base + C::kDs + h * C::kPStep;
+    RingPos<C::kA> qd;                                       // Q and dO of the step before: their freeing tells that the
+    RingPos<C::kB> od;                                       // products that read dS and P have retired
     const float scale_log2 = p.sm_scale * kLog2e;
+    const uint64_t scale2 = pack2(scale_log2, scale_log2);
     bool alive = true;
     for (int i = 0; i < n; ++i) {
-      const int st = i % kBwdStages;
-      const float4* lse4 = reinterpret_cast<const float4*>(s_lse2 + st * kTileM + h * 64);
-      const float4* delta4 = reinterpret_cast<const float4*>(s_delta + st * kTileM + h * 64);
-      if (!mbar_wait_warp(smem_u32(&ctl->stat_full[st]), (uint32_t)(i / kBwdStages) & 1u, abort_flag, p.status) ||
+      const int st = i % kStatStages;
+      const ulonglong2* lse4 = reinterpret_cast<const ulonglong2*>(s_lse2 + st * kTileM + h * 64);        // negated
+      const ulonglong2* delta4 = reinterpret_cast<const ulonglong2*>(s_delta + st * kTileM + h * 64);
+      if (!mbar_wait_warp(smem_u32(&ctl->stat_full[st]), (uint32_t)(i / kStatStages) & 1u, abort_flag, p.status) ||
           !mbar_wait_warp(smem_u32(&ctl->s_full), (uint32_t)i & 1u, abort_flag, p.status)) {
         alive = false;
         break;
@@ -335,13 +385,19 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
       uint32_t s[64];
       float pr[64];
       tmem_ld64(t_s, s);
+      if (C::kApart) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->s_read));
+      }
 #pragma unroll
       for (int c4 = 0; c4 < 16; ++c4) {
-        const float4 v = lse4[c4];
-        pr[c4 * 4] = ex2(fmaf(__uint_as_float(s[c4 * 4]), scale_log2, -v.x));
-        pr[c4 * 4 + 1] = ex2(fmaf(__uint_as_float(s[c4 * 4 + 1]), scale_log2, -v.y));
-        pr[c4 * 4 + 2] = ex2(fmaf(__uint_as_float(s[c4 * 4 + 2]), scale_log2, -v.z));
-        pr[c4 * 4 + 3] = ex2(fmaf(__uint_as_float(s[c4 * 4 + 3]), scale_log2, -v.w));
+        const ulonglong2 v = lse4[c4];
+        float t[4];
+        unpack2(ffma2(pack2(__uint_as_float(s[c4 * 4]), __uint_as_float(s[c4 * 4 + 1])), scale2, v.x), t[0], t[1]);
+        unpack2(ffma2(pack2(__uint_as_float(s[c4 * 4 + 2]), __uint_as_float(s[c4 * 4 + 3])), scale2, v.y), t[2], t[3]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pr[c4 * 4 + j] = ex2(t[j]);
       }
       // causal: columns of tokens in front of key - ahead do not see this key
       const int blind = kCausal ? max(key0 + r - ahead - (first_tile + i) * tile_tokens, 0) * p.group - h * 64 : 0;
@@ -354,7 +410,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
         uint32_t pk[32];
 #pragma unroll
         for (int c = 0; c < 32; ++c) pk[c] = pack_pair<T>(pr[2 * c], pr[2 * c + 1]);
-        tmem_st32(t_s, pk);
+        if (C::kApart && i > 0) {
+          if (!mbar_wait_warp(smem_u32(&ctl->b_free[od.slot]), od.phase, abort_flag, p.status)) {
+            alive = false;
+            break;
+          }
+          tc_fence_after();
+          od.next();
+        }
+        tmem_st32(t_p, pk);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -366,15 +430,31 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
       }
       tc_fence_after();
       tmem_ld64(t_dp, s);
+      if (C::kApart) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->dp_read));
+      }
       {
         uint32_t pk[32];
 #pragma unroll
         for (int c4 = 0; c4 < 16; ++c4) {
-          const float4 v = delta4[c4];
-          pk[c4 * 2] = pack_pair<T>(pr[c4 * 4] * (__uint_as_float(s[c4 * 4]) - v.x), pr[c4 * 4 + 1] * (__uint_as_float(s[c4 * 4 + 1]) - v.y));
-          pk[c4 * 2 + 1] = pack_pair<T>(pr[c4 * 4 + 2] * (__uint_as_float(s[c4 * 4 + 2]) - v.z), pr[c4 * 4 + 3] * (__uint_as_float(s[c4 * 4 + 3]) - v.w));
+          const ulonglong2 v = delta4[c4];
+          float t[4];
+          unpack2(fmul2(pack2(pr[c4 * 4], pr[c4 * 4 + 1]), fadd2(pack2(__uint_as_float(s[c4 * 4]), __uint_as_float(s[c4 * 4 + 1])), v.x)), t[0], t[1]);
+          unpack2(fmul2(pack2(pr[c4 * 4 + 2], pr[c4 * 4 + 3]), fadd2(pack2(__uint_as_float(s[c4 * 4 + 2]), __uint_as_float(s[c4 * 4 + 3])), v.y)), t[2], t[3]);
+          pk[c4 * 2] = pack_pair<T>(t[0], t[1]);
+          pk[c4 * 2 + 1] = pack_pair<T>(t[2], t[3]);
         }
-        tmem_st32(t_dp, pk);
+        if (C::kApart && i > 0) {
+          if (!mbar_wait_warp(smem_u32(&ctl->a_free[qd.slot]), qd.phase, abort_flag, p.status)) {
+            alive = false;
+            break;
+          }
+          tc_fence_after();
+          qd.next();
+        }
+        tmem_st32(t_ds, pk);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -398,7 +478,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
           const int col = h * (D / 2) + c * 32;
           uint32_t bits[32];
           if (n > 0) {
-            tmem_ld32(tmem + lane_base + 256 + which * 128 + col, bits);
+            tmem_ld32(tmem + lane_base + (which ? C::kSum1 : C::kSum0) + col, bits);
             tmem_wait_ld(bits);
           } else {
 #pragma unroll
@@ -416,11 +496,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
 template <typename T, int D, bool kCausal>
 __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __grid_constant__ tra_packed_launch p) {
   using C = BwdCfg<D>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
   uint8_t* sQ = smem;
   uint8_t* sDO = smem + C::kTileBytes;
-  uint8_t* sStage = smem + 2 * C::kTileBytes;               // [stage][K, V]
+  uint8_t* sA = smem + 2 * C::kTileBytes;                   // K tiles
+  uint8_t* sB = sA + C::kA * C::kTileBytes;                 // V tiles
   BwdCtl* ctl = (BwdCtl*)(smem + C::kSmemData);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int kvh = blockIdx.y;
@@ -472,31 +552,23 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __g
           tma_load_3d(smem_u32(sQ + a * C::kAtomBytes), &p.map_q, own, a * 64, kvh * p.group, qr.begin + tok0);
           tma_load_3d(smem_u32(sDO + a * C::kAtomBytes), &p.map_do, own, a * 64, kvh * p.group, qr.begin + tok0);
         }
-        for (int i = 0; i < n; ++i) {
-          const int st = i % kBwdStages;
-          if (i >= kBwdStages && !mbar_wait(smem_u32(&ctl->stage_free[st]), (uint32_t)(i / kBwdStages - 1) & 1u, abort_flag, p.status))
-            break;
-          const bool last_tail = tail && i == n - 1;
-          const uint32_t kbar = smem_u32(last_tail ? &ctl->tail_full : &ctl->a_full[st]);
-          const uint32_t vbar = smem_u32(last_tail ? &ctl->tail_full : &ctl->b_full[st]);
-          uint8_t* dst = sStage + st * 2 * C::kTileBytes;
-          if (last_tail) {
-            mbar_expect_tx(kbar, 2 * C::kTileBytes);
-          } else {
-            mbar_expect_tx(kbar, C::kTileBytes);
-            mbar_expect_tx(vbar, C::kTileBytes);
-          }
-          for (int a = 0; a < C::kAtoms; ++a)
-            tma_load_3d(smem_u32(dst + a * C::kAtomBytes), &p.map_k, kbar, a * 64, kvh, kr.begin + i * kTileM);
-          for (int a = 0; a < C::kAtoms; ++a)
-            tma_load_3d(smem_u32(dst + C::kTileBytes + a * C::kAtomBytes), &p.map_v, vbar, a * 64, kvh, kr.begin + i * kTileM);
-        }
+        bwd_produce<D>(
+            ctl, n, tail, C::kTileBytes, abort_flag, p.status,
+            [&](int i, int slot, uint32_t bar) {
+              for (int a = 0; a < C::kAtoms; ++a)
+                tma_load_3d(smem_u32(sA + slot * C::kTileBytes + a * C::kAtomBytes), &p.map_k, bar, a * 64, kvh, kr.begin + i * kTileM);
+            },
+            [&](int i, int slot, uint32_t bar) {
+              for (int a = 0; a < C::kAtoms; ++a)
+                tma_load_3d(smem_u32(sB + slot * C::kTileBytes + a * C::kAtomBytes), &p.map_v, bar, a * 64, kvh, kr.begin + i * kTileM);
+            });
       }
     } else if (warp == 10) {
       // ================================================================== rows past the sequence's end
       if (tail && mbar_wait_warp(smem_u32(&ctl->tail_full), 0u, abort_flag, p.status)) {
-        uint8_t* st = sStage + ((n - 1) % kBwdStages) * 2 * C::kTileBytes;
-        zero_tile_rows(st, kr.len - (n - 1) * kTileM, kTileM, 2 * C::kAtoms, C::kAtomBytes, lane, 32);
+        const int row0 = kr.len - (n - 1) * kTileM;
+        zero_tile_rows(sA + ((n - 1) % C::kA) * C::kTileBytes, row0, kTileM, C::kAtoms, C::kAtomBytes, lane, 32);
+        zero_tile_rows(sB + ((n - 1) % C::kB) * C::kTileBytes, row0, kTileM, C::kAtoms, C::kAtomBytes, lane, 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->tail_ready));
@@ -507,53 +579,50 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __g
       constexpr uint32_t kIdescD = make_idesc_t<T>(D, true);
       constexpr uint32_t kHi = desc_hi(1024);
       const uint32_t q_lo = desc_lo(smem_u32(sQ), 16), do_lo = desc_lo(smem_u32(sDO), 16);
-      const uint32_t stage_k = desc_lo(smem_u32(sStage), 16);
-      const uint32_t stage_mn = desc_lo(smem_u32(sStage), C::kAtomBytes);
+      const uint32_t a_k = desc_lo(smem_u32(sA), 16), a_mn = desc_lo(smem_u32(sA), C::kAtomBytes), b_k = desc_lo(smem_u32(sB), 16);
       constexpr uint32_t kTile = C::kTileBytes >> 4;
+      RingPos<C::kA> ks, kd;                 // K of the next S, of the next dQ
+      RingPos<C::kB> vs;
       bool alive = mbar_wait(smem_u32(&ctl->own_full), 0u, abort_flag, p.status);
-      auto wait_k = [&](int i) -> bool {
-        if (tail && i == n - 1) return mbar_wait(smem_u32(&ctl->tail_ready), 0u, abort_flag, p.status);
-        return mbar_wait(smem_u32(&ctl->a_full[i % kBwdStages]), (uint32_t)(i / kBwdStages) & 1u, abort_flag, p.status);
-      };
-      auto wait_v = [&](int i) -> bool {
-        if (tail && i == n - 1) return true;                                   // came with K
-        return mbar_wait(smem_u32(&ctl->b_full[i % kBwdStages]), (uint32_t)(i / kBwdStages) & 1u, abort_flag, p.status);
-      };
-      auto issue_s = [&](int i) {
+      auto issue_s = [&](int i) -> bool {
+        if (!(tail && i == n - 1 ? mbar_wait(smem_u32(&ctl->tail_ready), 0u, abort_flag, p.status)
+                                 : mbar_wait(smem_u32(&ctl->a_full[ks.slot]), ks.phase, abort_flag, p.status)))
+          return false;
         tc_fence_after();
-        mma_tiles<D>(tmem, q_lo, stage_k + (uint32_t)(i % kBwdStages) * 2 * kTile, kIdescS);
+        mma_tiles<D>(tmem, q_lo, a_k + (uint32_t)ks.slot * kTile, kIdescS);
         tc_commit(smem_u32(&ctl->s_full));
+        ks.next();
+        return true;
       };
-      auto issue_dp = [&](int i) {
+      auto issue_dp = [&](int i) -> bool {
+        // (the last pair of a tail came with K)
+        if (!(tail && i == n - 1) && !mbar_wait(smem_u32(&ctl->b_full[vs.slot]), vs.phase, abort_flag, p.status)) return false;
         tc_fence_after();
-        mma_tiles<D>(tmem + 128, do_lo, stage_k + ((uint32_t)(i % kBwdStages) * 2 + 1) * kTile, kIdescS);
+        mma_tiles<D>(tmem + 128, do_lo, b_k + (uint32_t)vs.slot * kTile, kIdescS);
         tc_commit(smem_u32(&ctl->dp_full));
+        tc_commit(smem_u32(&ctl->b_free[vs.slot]));
+        vs.next();
+        return true;
       };
-      if (alive && n > 0) {
-        alive = wait_k(0);
-        if (alive) issue_s(0);
-        if (alive) alive = wait_v(0);
-        if (alive) issue_dp(0);
-      }
+      alive = alive && n > 0 && issue_s(0) && issue_dp(0);
       for (int i = 0; i < n && alive; ++i) {
         if (i + 1 < n) {
-          if (!(alive = mbar_wait(smem_u32(&ctl->s_read), (uint32_t)i & 1u, abort_flag, p.status) && wait_k(i + 1))) break;
-          issue_s(i + 1);
-          if (!(alive = mbar_wait(smem_u32(&ctl->dp_read), (uint32_t)i & 1u, abort_flag, p.status) && wait_v(i + 1))) break;
-          issue_dp(i + 1);
+          if (!(alive = mbar_wait(smem_u32(&ctl->s_read), (uint32_t)i & 1u, abort_flag, p.status) && issue_s(i + 1))) break;
+          if (!(alive = mbar_wait(smem_u32(&ctl->dp_read), (uint32_t)i & 1u, abort_flag, p.status) && issue_dp(i + 1))) break;
         }
-        const uint32_t b_lo = stage_mn + (uint32_t)(i % kBwdStages) * 2 * kTile;        // dQ += dS K
+        const uint32_t k_mn = a_mn + (uint32_t)kd.slot * kTile;           // dQ += dS K
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (!(alive = mbar_wait(smem_u32(&ctl->ds_ready[h]), (uint32_t)i & 1u, abort_flag, p.status))) break;
           tc_fence_after();
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
-            tc_mma_ts(tmem + 256, tmem + 384 + (h * 4 + kk) * 8, b_lo + (h * 4 + kk) * (2048 >> 4), kHi, kIdescD,
+            tc_mma_ts(tmem + 256, tmem + 384 + (h * 4 + kk) * 8, k_mn + (h * 4 + kk) * (2048 >> 4), kHi, kIdescD,
                       h + kk > 0 ? 1u : (i > 0 ? 1u : 0u));
         }
         if (!alive) break;
-        tc_commit(smem_u32(&ctl->stage_free[i % kBwdStages]));
+        tc_commit(smem_u32(&ctl->a_free[kd.slot]));
+        kd.next();
       }
       tc_commit(smem_u32(&ctl->drain));
       mbar_wait(smem_u32(&ctl->drain), 0u, abort_flag, p.status);
@@ -576,6 +645,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __g
       delta = p.delta[tok_g * p.heads + head];
     }
     const int seen = kCausal ? min(max(min(tok, last_tok) + 1 + ahead, 0), kr.len) : kr.len;
+    RingPos<C::kA> kd;                                       // K of the step before
     bool alive = true;
     for (int i = 0; i < n; ++i) {
       if (!mbar_wait_warp(smem_u32(&ctl->s_full), (uint32_t)i & 1u, abort_flag, p.status)) {
@@ -611,10 +681,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __g
       for (int c = 0; c < 32; ++c)
         pk[c] = pack_pair<T>(pr[2 * c] * (__uint_as_float(s[2 * c]) - delta), pr[2 * c + 1] * (__uint_as_float(s[2 * c + 1]) - delta));
       // the product that read the last dS has retired (it also freed that stage)
-      if (i > 0 && !mbar_wait_warp(smem_u32(&ctl->stage_free[(i - 1) % kBwdStages]), (uint32_t)((i - 1) / kBwdStages) & 1u,
-                                   abort_flag, p.status)) {
-        alive = false;
-        break;
+      if (i > 0) {
+        if (!mbar_wait_warp(smem_u32(&ctl->a_free[kd.slot]), kd.phase, abort_flag, p.status)) {
+          alive = false;
+          break;
+        }
+        kd.next();
       }
       tc_fence_after();
       tmem_st32(tmem + lane_base + 384 + h * 32, pk);
