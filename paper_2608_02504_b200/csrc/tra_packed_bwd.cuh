@@ -275,24 +275,34 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
       }
     } else if (warp == 11) {
       // ================================================================== lse and delta of the query rows
+      // read before the wait for the slot, so that the loads' latency is not added to it
+      int r_tok[4], r_row[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = k * 32 + lane;
+        r_tok[k] = r < box_rows ? r / p.group : 1 << 30;             // past every sequence: a row no box fills
+        r_row[k] = r % p.group;
+      }
       for (int i = 0; i < n; ++i) {
         const int st = i % kStatStages;
+        const int tok0 = (first_tile + i) * tile_tokens;
+        float lse2[4], delta[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          lse2[k] = INFINITY;                             // a row that is not there, or sees no key: probability 0
+          delta[k] = 0.f;
+          if (r_tok[k] < qr.len - tok0) {
+            const long long row = (long long)(qr.begin + tok0 + r_tok[k]) * p.heads + kvh * p.group + r_row[k];
+            lse2[k] = p.lse[row];
+            delta[k] = p.delta[row];
+          }
+        }
         if (i >= kStatStages && !mbar_wait_warp(smem_u32(&ctl->stat_free[st]), (uint32_t)(i / kStatStages - 1) & 1u, abort_flag, p.status))
           break;
-        const int tok0 = (first_tile + i) * tile_tokens;
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          const int r = r4 * 32 + lane;
-          const int tok = tok0 + r / p.group;
-          float lse2 = INFINITY, delta = 0.f;           // a row that is not there, or sees no key: probability 0
-          if (r < box_rows && tok < qr.len) {
-            const long long row = (long long)(qr.begin + tok) * p.heads + kvh * p.group + r % p.group;
-            const float v = p.lse[row] * kLog2e;
-            lse2 = v == -INFINITY ? INFINITY : v;
-            delta = p.delta[row];
-          }
-          s_lse2[st * kTileM + r] = -lse2;               // negated for the packed multiply-add
-          s_delta[st * kTileM + r] = -delta;
+        for (int k = 0; k < 4; ++k) {                     // negated for the packed multiply-add
+          s_lse2[st * kTileM + k * 32 + lane] = lse2[k] == -INFINITY ? -INFINITY : -lse2[k] * kLog2e;
+          s_delta[st * kTileM + k * 32 + lane] = -delta[k];
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->stat_full[st]));
@@ -376,8 +386,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
       const int st = i % kStatStages;
       const ulonglong2* lse4 = reinterpret_cast<const ulonglong2*>(s_lse2 + st * kTileM + h * 64);        // negated
       const ulonglong2* delta4 = reinterpret_cast<const ulonglong2*>(s_delta + st * kTileM + h * 64);
-      if (!mbar_wait_warp(smem_u32(&ctl->stat_full[st]), (uint32_t)(i / kStatStages) & 1u, abort_flag, p.status) ||
-          !mbar_wait_warp(smem_u32(&ctl->s_full), (uint32_t)i & 1u, abort_flag, p.status)) {
+      if (!mbar_wait_warp(smem_u32(&ctl->s_full), (uint32_t)i & 1u, abort_flag, p.status) ||
+          !mbar_wait_warp(smem_u32(&ctl->stat_full[st]), (uint32_t)(i / kStatStages) & 1u, abort_flag, p.status)) {
         alive = false;
         break;
       }
