@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBwdRegsSoftmax));
     // ================================================================== probabilities and their gradients
     const int h = warp >> 2;                                 // columns 64 h .. 64 h + 63
-    const int r = tid & (kTileM - 1);                        // key inside the tile
+    int r = tid & (kTileM - 1);                              // key inside the tile
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lane_base + h * 64, t_dp = t_s + 128;
     const uint32_t t_p = tmem + lane_base + C::kP + h * C::kPStep, t_ds = tmem + lane_base + C::kDs + h * C::kPStep;
@@ -381,6 +381,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
     RingPos<C::kB> od;                                       // products that read dS and P have retired
     const float scale_log2 = p.sm_scale * kLog2e;
     const uint64_t scale2 = pack2(scale_log2, scale_log2);
+    int blind_tok = key0 + r - ahead - first_tile * tile_tokens;         // tokens of the first tile in front of the first seer
     bool alive = true;
     for (int i = 0; i < n; ++i) {
       const int st = i % kStatStages;
@@ -410,7 +411,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
         for (int j = 0; j < 4; ++j) pr[c4 * 4 + j] = ex2(t[j]);
       }
       // causal: columns of tokens in front of key - ahead do not see this key
-      const int blind = kCausal ? max(key0 + r - ahead - (first_tile + i) * tile_tokens, 0) * p.group - h * 64 : 0;
+      const int blind = kCausal ? max(blind_tok, 0) * p.group - h * 64 : 0;
+      blind_tok -= p.tile_tokens;
       if (kCausal && __any_sync(0xffffffffu, blind > 0)) {
 #pragma unroll
         for (int c = 0; c < 64; ++c)
@@ -478,8 +480,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
     if (alive && n > 0) alive = mbar_wait_warp(smem_u32(&ctl->drain), 0u, abort_flag, p.status);
     if (alive) {
       tc_fence_after();
-      const bool row_valid = key0 + r < kr.len;
-      const long long row = kr.begin + key0 + (row_valid ? r : 0);
+      // read again from shared memory and the thread index: the loop above needs the registers
+      asm volatile("" : "+r"(r));
+      const int key = *(volatile int*)&ctl->unit.index * kTileM + r;
+      const bool row_valid = key < *(volatile int*)&ctl->unit.k.len;
+      const long long row = *(volatile int*)&ctl->unit.k.begin + (row_valid ? key : 0);
       T* out[2] = {(T*)p.dv + row * p.dv_stride[0] + kvh * p.dv_stride[1], (T*)p.dk + row * p.dk_stride[0] + kvh * p.dk_stride[1]};
 #pragma unroll
       for (int which = 0; which < 2; ++which) {

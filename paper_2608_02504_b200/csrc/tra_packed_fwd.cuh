@@ -117,7 +117,6 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
     const int last = min(first + p.tile_tokens, qr.len) - 1;
     return kCausal ? min(max(last + 1 + ahead, 0), kr.len) : kr.len;
   };
-  const bool tile1_on = tok0 + p.tile_tokens < qr.len;
   const int nb0 = (tile_keys(0) + kKeyTile - 1) / kKeyTile, nb1 = (tile_keys(1) + kKeyTile - 1) / kKeyTile;
   const int nb = max(nb0, nb1);                           // nb0 <= nb1 when there is a second tile
   const int per_split = (nb + (int)gridDim.z - 1) / (int)gridDim.z;
