@@ -20,6 +20,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) tra_packed_join_kernel(const 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long row = blockIdx.x, stride = (long long)p.total_q * p.heads;
   const int tok = (int)(row / p.heads), head = (int)(row - (long long)tok * p.heads);
+  wait_last_launch();
   // rows in front of the first and behind the last sequence stay as they are
   if (tok < p.cu_q[0] || tok >= p.cu_q[p.n_seq]) return;
   float top = -INFINITY, sum = 0.f, etop = -INFINITY, esum = 0.f, o[kPer];
@@ -171,12 +172,10 @@ int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_lau
 }
 
 template <typename T>
-void launch_join(const tra_packed* h, const tra_packed_launch& p, cudaStream_t stream) {
-  const unsigned blocks = (unsigned)((long long)p.total_q * p.heads);
-  if (h->cfg.head_dim == 128)
-    tra_packed_join_kernel<T, 128><<<blocks, 32 * kJoinWarps, 0, stream>>>(p);
-  else
-    tra_packed_join_kernel<T, 64><<<blocks, 32 * kJoinWarps, 0, stream>>>(p);
+int launch_join(const tra_packed* h, const tra_packed_launch& p, cudaStream_t stream) {
+  const dim3 blocks((unsigned)((long long)p.total_q * p.heads));
+  return h->cfg.head_dim == 128 ? tra_launch(tra_packed_join_kernel<T, 128>, blocks, 32 * kJoinWarps, 0, stream, true, p)
+                                : tra_launch(tra_packed_join_kernel<T, 64>, blocks, 32 * kJoinWarps, 0, stream, true, p);
 }
 
 }  // namespace
@@ -262,12 +261,7 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
     rc = h->cfg.head_dim == 128 ? tra_packed_fwd_d128(ctx, p) : tra_packed_fwd_d64(ctx, p);
   }
   if (rc != TRA_OK || c.splits == 1) return rc;
-  if (h->cfg.dtype == TRA_BF16)
-    launch_join<__nv_bfloat16>(h, p, ctx.stream);
-  else
-    launch_join<__half>(h, p, ctx.stream);
-  TRA_CUDA_CHECK(cudaGetLastError());
-  return TRA_OK;
+  return h->cfg.dtype == TRA_BF16 ? launch_join<__nv_bfloat16>(h, p, ctx.stream) : launch_join<__half>(h, p, ctx.stream);
 }
 
 extern "C" size_t tra_packed_attn_backward_workspace_bytes(const tra_packed_t* h, int total_q) {

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "tra.h"
 
 struct tra_packed {
@@ -47,6 +49,33 @@ int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chu
 
 #ifdef __CUDACC__
 namespace {
+
+// Allows a kernel its dynamic shared memory, once per kernel and device (the attribute stays with the device's context).
+template <auto kernel>
+int tra_allow_smem(int bytes, int device) {
+  static std::atomic<uint64_t> done{0};
+  const uint64_t bit = device < 64 ? 1ull << device : 0ull;
+  if (done.load(std::memory_order_relaxed) & bit) return TRA_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return TRA_ERR_CUDA;
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return TRA_OK;
+}
+
+// Launch; after_last: may start while the stream's last kernel ends (see wait_last_launch).
+template <typename... Params, typename... Args>
+int tra_launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, bool after_last, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = after_last ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? TRA_OK : TRA_ERR_CUDA;
+}
 
 // The token range of a sequence, brought inside the tensor and the stated maximum; what had to be cut is recorded.
 struct tra_seq_range {

@@ -1,13 +1,13 @@
-// Gradients of attention over packed sequences: two kernels that recompute the probabilities from lse and keep every sum
-// inside one thread block (no atomics: the same bits every time).
+// Gradients of attention over packed sequences: one launch of two kinds of blocks that recompute the probabilities from lse
+// and keep every sum inside one thread block (no atomics: the same bits every time).
 //
-// P = exp(S - lse), dP = dO V^T, dS = P (dP - delta), delta = rowsum(dO O) (a small kernel of its own).
-//   tra_packed_dkv_kernel: one block per 128 keys of a (sequence, key/value head), walks the query tiles that see them:
+// P = exp(S - lse), dP = dO V^T, dS = P (dP - delta), delta = rowsum(dO O) (a small kernel in front).
+//   dkv_block: one block per 128 keys of a (sequence, key/value head), walks the query tiles that see them:
 //     S^T = K Q^T and dP^T = V dO^T (tcgen05, both operands in shared memory), the softmax threads (one key per
 //     lane, 64 query rows per thread) write P^T and dS^T back to tensor memory in the 16-bit type, where they are the
 //     A operands of dV += P^T dO and dK += dS^T Q.  A query tile holds all heads of the group, so the sum over the heads that
 //     share a key/value head is the product's own.
-//   tra_packed_dq_kernel: one block per 128-row query tile, walks its key blocks: S = Q K^T, dP = dO V^T, dQ += dS K.
+//   dq_block: one block per 128-row query tile, walks its key blocks: S = Q K^T, dP = dO V^T, dQ += dS K.
 // Seven products instead of the five that one pass over the pairs needs: the fifth sum, dQ, would have to leave the
 // block through memory (fp32 atomics whose order changes the result, or 4 bytes per row, channel and key block).
 //
@@ -190,9 +190,8 @@ __device__ __forceinline__ void store32(T* dst, const uint32_t* bits, float mul)
 
 // ------------------------------------------------------------------------------------ dK, dV
 template <typename T, int D, bool kCausal>
-__global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __grid_constant__ tra_packed_launch p) {
+__device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
   using C = BwdCfg<D>;
-  extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
   uint8_t* sK = smem;
   uint8_t* sV = smem + C::kTileBytes;
   uint8_t* sA = smem + 2 * C::kTileBytes;                   // Q tiles
@@ -201,13 +200,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
   float* s_lse2 = (float*)(smem + C::kSmemData + 512);       // [stage][128], then delta
   float* s_delta = s_lse2 + kStatStages * kTileM;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int kvh = blockIdx.y;
 
   const int tile_tokens = p.tile_tokens, box_rows = tile_tokens * p.group;
 
   // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    const tra_unit u = tra_find_unit(p, true, p.max_k <= kTileM, kTileM, (int)blockIdx.x);
+    const tra_unit u = tra_find_unit(p, true, p.max_k <= kTileM, kTileM, unit);
     if (lane == 0) ctl->unit = u;
   } else if (warp == 9) {
     tmem_alloc_all(&ctl->tmem_base);
@@ -230,6 +228,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
   const int key0 = ctl->unit.index * kTileM;
   if (ctl->unit.seq < 0 || key0 >= kr.len) {
     if (warp == 9) tmem_free_all(tmem);
+    wait_last_launch();          // no block ends before the launch in front of it
     return;
   }
   const int ahead = kr.len - qr.len;
@@ -275,6 +274,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
       }
     } else if (warp == 11) {
       // ================================================================== lse and delta of the query rows
+      wait_last_launch();                                 // delta
       // read before the wait for the slot, so that the loads' latency is not added to it
       int r_tok[4], r_row[4];
 #pragma unroll
@@ -509,22 +509,19 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dkv_kernel(const __
 
 // ------------------------------------------------------------------------------------ dQ
 template <typename T, int D, bool kCausal>
-__global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __grid_constant__ tra_packed_launch p) {
+__device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
   using C = BwdCfg<D>;
-  extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
   uint8_t* sQ = smem;
   uint8_t* sDO = smem + C::kTileBytes;
   uint8_t* sA = smem + 2 * C::kTileBytes;                   // K tiles
   uint8_t* sB = sA + C::kA * C::kTileBytes;                 // V tiles
   BwdCtl* ctl = (BwdCtl*)(smem + C::kSmemData);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int kvh = blockIdx.y;
   const int tile_tokens = p.tile_tokens, box_rows = tile_tokens * p.group;
 
   // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    // the last tiles of a causal sequence are the longest: launched first
-    const tra_unit u = tra_find_unit(p, false, p.max_q <= tile_tokens, tile_tokens, (int)gridDim.x - 1 - (int)blockIdx.x);
+    const tra_unit u = tra_find_unit(p, false, p.max_q <= tile_tokens, tile_tokens, unit);
     if (lane == 0) ctl->unit = u;
   } else if (warp == 9) {
     tmem_alloc_all(&ctl->tmem_base);
@@ -547,6 +544,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __g
   const int tok0 = ctl->unit.index * tile_tokens;
   if (ctl->unit.seq < 0 || tok0 >= qr.len) {
     if (warp == 9) tmem_free_all(tmem);
+    wait_last_launch();          // no block ends before the launch in front of it
     return;
   }
   const int ahead = kr.len - qr.len;
@@ -654,6 +652,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __g
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const float scale_log2 = p.sm_scale * kLog2e;
     float lse2 = INFINITY, delta = 0.f;                      // a row that is not there, or sees no key: probability 0
+    wait_last_launch();                                      // delta
     if (row_valid) {
       const float v = p.lse[tok_g * p.heads + head] * kLog2e;
       lse2 = v == -INFINITY ? INFINITY : v;
@@ -732,11 +731,26 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_dq_kernel(const __g
   bwd_teardown(ctl, tmem, warp);
 }
 
+// ------------------------------------------------------------------------------------ both
+// Blocks of either kind in one launch, so that the shorter dQ blocks fill the SMs that the last dK/dV blocks leave: first
+// dkv_units per key/value head, then dq_units.  Of a causal sequence the first keys and the last queries have most to
+// do, and come first.
+template <typename T, int D, bool kCausal>
+__global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_bwd_kernel(const __grid_constant__ tra_packed_launch p, int dkv_units, int dq_units) {
+  extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
+  const int n_dkv = dkv_units * p.kv_heads, b = blockIdx.x;
+  if (b < n_dkv)
+    dkv_block<T, D, kCausal>(p, smem, b % dkv_units, b / dkv_units);
+  else
+    dq_block<T, D, kCausal>(p, smem, dq_units - 1 - (b - n_dkv) % dq_units, (b - n_dkv) / dq_units);
+}
+
 // ------------------------------------------------------------------------------------ delta
 // delta = sum over the channels of dO O, d / 8 threads per (token, head), 16 bytes each.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) tra_packed_delta_kernel(const __grid_constant__ tra_packed_launch p) {
   constexpr int kLanes = D / 8;
+  allow_next_launch();
   const long long row = (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
   const int lane = threadIdx.x % kLanes;
   const long long rows = (long long)p.total_q * p.heads;
@@ -764,26 +778,20 @@ __global__ void __launch_bounds__(256) tra_packed_delta_kernel(const __grid_cons
 template <typename T, int D, bool kCausal>
 int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   const long long rows = (long long)a.total_q * a.heads;
+  int rc = TRA_OK;
   if (rows > 0) {
     constexpr int kRows = 256 / (D / 8);
-    tra_packed_delta_kernel<T, D><<<(unsigned)((rows + kRows - 1) / kRows), 256, 0, c.stream>>>(a);
-    TRA_CUDA_CHECK(cudaGetLastError());
+    if ((rc = tra_launch(tra_packed_delta_kernel<T, D>, dim3((unsigned)((rows + kRows - 1) / kRows)), 256, 0, c.stream, false, a)) != TRA_OK)
+      return rc;
   }
-  if (a.max_k > 0) {
-    auto dkv = tra_packed_dkv_kernel<T, D, kCausal>;
-    TRA_CUDA_CHECK(cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdCfg<D>::kSmemBytes));
-    const unsigned units = (unsigned)((a.max_k <= kTileM ? 0 : a.total_k / kTileM) + a.n_seq);
-    dkv<<<dim3(units, (unsigned)a.kv_heads), kBwdThreads, BwdCfg<D>::kSmemBytes, c.stream>>>(a);
-    TRA_CUDA_CHECK(cudaGetLastError());
-  }
-  if (a.max_q > 0) {
-    auto dq = tra_packed_dq_kernel<T, D, kCausal>;
-    TRA_CUDA_CHECK(cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdCfg<D>::kSmemBytes));
-    const unsigned units = (unsigned)((a.max_q <= a.tile_tokens ? 0 : a.total_q / a.tile_tokens) + a.n_seq);
-    dq<<<dim3(units, (unsigned)a.kv_heads), kBwdThreads, BwdCfg<D>::kSmemBytes, c.stream>>>(a);
-    TRA_CUDA_CHECK(cudaGetLastError());
-  }
-  return TRA_OK;
+  const int dkv_units = a.max_k > 0 ? (a.max_k <= kTileM ? 0 : a.total_k / kTileM) + a.n_seq : 0;
+  const int dq_units = a.max_q > 0 ? (a.max_q <= a.tile_tokens ? 0 : a.total_q / a.tile_tokens) + a.n_seq : 0;
+  const long long blocks = ((long long)dkv_units + dq_units) * a.kv_heads;
+  if (blocks == 0) return TRA_OK;
+  if (blocks > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
+  constexpr auto kern = tra_packed_bwd_kernel<T, D, kCausal>;
+  if ((rc = tra_allow_smem<kern>(BwdCfg<D>::kSmemBytes, c.h->device)) != TRA_OK) return rc;
+  return tra_launch(kern, dim3((unsigned)blocks), kBwdThreads, BwdCfg<D>::kSmemBytes, c.stream, rows > 0, a, dkv_units, dq_units);
 }
 
 template <int D>

@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (gridDim.z > 1) allow_next_launch();                 // the join of the parts
   const uint32_t tmem = ctl->tmem_base;
   const tra_seq_range qr = ctl->unit.q, kr = ctl->unit.k;
   const int tok0 = ctl->unit.index * 2 * p.tile_tokens;   // first token of tile 0, inside the sequence
@@ -437,12 +438,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
 
 template <typename T, int D, bool kCausal, bool kExact>
 int launch_fwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
-  auto kern = tra_packed_fwd_kernel<T, D, kCausal, kExact>;
-  TRA_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdCfg<D>::kSmemBytes));
-  kern<<<dim3((unsigned)a.n_units, (unsigned)a.kv_heads, (unsigned)a.splits), kFwdThreads, FwdCfg<D>::kSmemBytes,
-         c.stream>>>(a);
-  TRA_CUDA_CHECK(cudaGetLastError());
-  return TRA_OK;
+  constexpr auto kern = tra_packed_fwd_kernel<T, D, kCausal, kExact>;
+  const int rc = tra_allow_smem<kern>(FwdCfg<D>::kSmemBytes, c.h->device);
+  if (rc != TRA_OK) return rc;
+  return tra_launch(kern, dim3((unsigned)a.n_units, (unsigned)a.kv_heads, (unsigned)a.splits), kFwdThreads, FwdCfg<D>::kSmemBytes,
+                    c.stream, false, a);
 }
 
 template <int D>

@@ -76,6 +76,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
   const int seq = blockIdx.x, kvh = blockIdx.y;
   const tra_seq_range qr = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
   const tra_seq_range kr = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
+  if (gridDim.z > 1) allow_next_launch();                    // the join of the parts
   const int n_rows = qr.len * p.group;                       // <= 16
   if (n_rows == 0) return;
   const int ahead = kr.len - qr.len;
@@ -317,11 +318,11 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
 
 template <typename T, int D>
 int launch_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk) {
-  auto kern = tra_packed_rows_kernel<T, D>;
-  TRA_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsCfg<D>::kSmemBytes));
-  kern<<<dim3((unsigned)a.n_seq, (unsigned)a.kv_heads, (unsigned)a.splits), kRowsThreads, RowsCfg<D>::kSmemBytes, c.stream>>>(a, chunk);
-  TRA_CUDA_CHECK(cudaGetLastError());
-  return TRA_OK;
+  constexpr auto kern = tra_packed_rows_kernel<T, D>;
+  const int rc = tra_allow_smem<kern>(RowsCfg<D>::kSmemBytes, c.h->device);
+  if (rc != TRA_OK) return rc;
+  return tra_launch(kern, dim3((unsigned)a.n_seq, (unsigned)a.kv_heads, (unsigned)a.splits), kRowsThreads, RowsCfg<D>::kSmemBytes, c.stream,
+                    false, a, chunk);
 }
 
 }  // namespace
