@@ -400,7 +400,7 @@ int tra_packed_status(tra_packed_t* packed, void* stream);
 
 /* Forward.  The launch follows from the sizes alone: sequences of at most 16 rows (max_q * group) go to a kernel for few
  * rows over many keys, others to 128-row tensor-core tiles; either splits the keys over thread blocks when there
- * are too few rows to fill the GPU, and a second launch joins the parts, which lie in `workspace`: device memory of
+ * are too few rows to fill the GPU.  Many parts are joined by a second launch and lie in `workspace`: device memory of
  * tra_packed_attn_workspace_bytes (0: none needed, pass NULL), 16-byte aligned, owned by the caller and free to reuse once
  * `stream` has passed the call.  The current device must be the handle's.
  * Errors: TRA_ERR_INVALID_ARG, TRA_ERR_UNSUPPORTED, TRA_ERR_CAPACITY (workspace too small), TRA_ERR_CUDA. */

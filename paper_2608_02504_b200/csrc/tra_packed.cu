@@ -9,103 +9,147 @@
 namespace {
 
 constexpr int kJoinWarps = 4;
+constexpr int kMaxSplits = 256;       // parts of a split launch
 
 // O = sum_s w_s O_s, w_s = 2^(lse2_s - lse2), lse2 = log2 sum_s 2^lse2_s over the parts of a split launch; lse from the
-// unrounded sums in the same way.  One block per (token, head), its warps take every fourth part.
+// unrounded sums in the same way.  One block per (token, head): first the weights, all parts' logarithms read at once, then
+// its warps take every fourth part, four loads in flight each.
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kJoinWarps) tra_packed_join_kernel(const __grid_constant__ tra_packed_launch p) {
   constexpr int kPer = D / 32;
-  __shared__ float s_o[kJoinWarps][D];
-  __shared__ float s_max[kJoinWarps], s_sum[kJoinWarps], s_emax[kJoinWarps], s_esum[kJoinWarps];
+  __shared__ __align__(16) float s_o[kJoinWarps][D];
+  __shared__ float s_w[kMaxSplits];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long row = blockIdx.x, stride = (long long)p.total_q * p.heads;
   const int tok = (int)(row / p.heads), head = (int)(row - (long long)tok * p.heads);
   wait_last_launch();
   // rows in front of the first and behind the last sequence stay as they are
   if (tok < p.cu_q[0] || tok >= p.cu_q[p.n_seq]) return;
-  float top = -INFINITY, sum = 0.f, etop = -INFINITY, esum = 0.f, o[kPer];
+  // every warp forms the same sums (kMaxSplits / 32 logarithms per lane)
+  float v[kMaxSplits / 32], top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / 32; ++i) {
+    const int s = i * 32 + lane;
+    v[i] = s < p.splits ? p.part_lse2[s * stride + row] : -INFINITY;
+    top = v[i] != v[i] ? v[i] : fmaxf(top, v[i]);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float other = __shfl_xor_sync(0xffffffffu, top, o);
+    top = top != top ? top : other != other ? other : fmaxf(top, other);
+  }
+  const float ref = top == -INFINITY ? 0.f : top;        // no part holds a key: every weight is 0
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / 32; ++i) {
+    v[i] = ex2(v[i] - ref);                              // parts without a key: 0
+    sum += v[i];
+    if (warp == 0) s_w[i * 32 + lane] = v[i];
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  __syncthreads();
+  float o[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) o[i] = 0.f;
-  for (int s = warp; s < p.splits; s += kJoinWarps) {
-    const float v = p.part_lse2[s * stride + row];
-    if (v == -INFINITY) continue;                    // the part held no key this row sees
-    const float up = fmaxf(top, v), f = ex2(top - up), g = ex2(v - up);
-    const float* src = p.part_o + (s * stride + row) * D + lane * kPer;
+  const float* src = p.part_o + row * D + lane * kPer;
+  for (int s0 = warp; s0 < p.splits; s0 += 4 * kJoinWarps) {
+    float part[4][kPer], w[4];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) o[i] = o[i] * f + g * src[i];
-    sum = sum * f + g;
-    top = up;
-    if (p.part_exact) {
-      const float e = p.part_exact[s * stride + row], eup = fmaxf(etop, e);
-      esum = esum * ex2(etop - eup) + ex2(e - eup);
-      etop = eup;
+    for (int j = 0; j < 4; ++j) {
+      const int s = s0 + j * kJoinWarps;
+      w[j] = s < p.splits ? s_w[s] : 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) part[j][i] = 0.f;
+      if (w[j] != 0.f) {                                 // a part without a key has no row to read
+        if constexpr (kPer == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(src + s * stride * D);
+          part[j][0] = x.x, part[j][1] = x.y, part[j][2] = x.z, part[j][3] = x.w;
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(src + s * stride * D);
+          part[j][0] = x.x, part[j][1] = x.y;
+        }
+      }
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) o[i] = fmaf(w[j], part[j][i], o[i]);
   }
 #pragma unroll
   for (int i = 0; i < kPer; ++i) s_o[warp][lane * kPer + i] = o[i];
-  if (lane == 0) {
-    s_max[warp] = top, s_sum[warp] = sum, s_emax[warp] = etop, s_esum[warp] = esum;
-  }
   __syncthreads();
-  float all = -INFINITY, eall = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) {
-    all = fmaxf(all, s_max[w]);
-    eall = fmaxf(eall, s_emax[w]);
-  }
-  const float ref = all > -INFINITY ? all : 0.f, eref = eall > -INFINITY ? eall : 0.f;
-  float den = 0.f, eden = 0.f;
-#pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) {
-    den += s_sum[w] * ex2(s_max[w] - ref);
-    eden += s_esum[w] * ex2(s_emax[w] - eref);
-  }
-  const float inv = den != 0.f ? 1.f / den : 0.f;
+  const float inv = sum != 0.f ? 1.f / sum : 0.f;
   T* dst = (T*)p.o + tok * p.o_stride[0] + head * p.o_stride[1];
   if (threadIdx.x < D / 2) {
-    const int c = 2 * threadIdx.x;
-    float a = 0.f, b = 0.f;
+    float2 a = make_float2(0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) {
-      const float f = ex2(s_max[w] - ref);
-      a += f * s_o[w][c];
-      b += f * s_o[w][c + 1];
+      const float2 x = reinterpret_cast<const float2*>(s_o[w])[threadIdx.x];
+      a.x += x.x;
+      a.y += x.y;
     }
-    reinterpret_cast<uint32_t*>(dst)[threadIdx.x] = pack_pair<T>(a * inv, b * inv);
+    reinterpret_cast<uint32_t*>(dst)[threadIdx.x] = pack_pair<T>(a.x * inv, a.y * inv);
   }
-  if (threadIdx.x == 0 && p.lse) p.lse[row] = eden != 0.f ? (eref + log2f(eden)) * kLn2 : -INFINITY;
+  if (p.lse && warp == kJoinWarps - 1) {
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 32; ++i) {
+      const int s = i * 32 + lane;
+      if (s < p.splits) total += ex2(p.part_exact[s * stride + row] - ref);
+    }
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) total += __shfl_xor_sync(0xffffffffu, total, k);
+    if (lane == 0) p.lse[row] = total != 0.f ? (ref + log2f(total)) * kLn2 : -INFINITY;
+  }
 }
 
 // How a call runs: rows = the kernel for few rows (at most 16 per sequence and key/value head), with `splits` parts
-// of `chunk` keys; else the 128-row tiles, with `splits` ranges of key blocks.
+// of `chunk` keys, joined inside a thread-block cluster (clustered) or by the join kernel; else the 128-row tiles, with
+// `splits` ranges of key blocks and the join kernel.
 struct Choice {
-  bool rows;
+  bool rows, clustered;
   int splits, chunk;
 };
 
+constexpr int kClusterMax = 8;        // the largest portable cluster
+
 Choice choose(const tra_packed* h, int n_seq, int total_q, int max_q, int max_k) {
   const int group = h->cfg.heads / h->cfg.kv_heads;
-  Choice c = {(long long)max_q * group <= 16, 1, 0};
+  Choice c = {(long long)max_q * group <= 16, false, 1, 0};
   if (c.rows) {
-    const long long units = (long long)n_seq * h->cfg.kv_heads, target = 8ll * h->sm_count;
-    const long long want = (target + units - 1) / units;
-    long long chunk = (max_k + want - 1) / want;
-    if (chunk < 256) chunk = 256;
-    c.chunk = (int)((chunk + 63) / 64 * 64);
-    c.splits = max_k > 0 ? (max_k + c.chunk - 1) / c.chunk : 1;
+    // Two blocks fit an SM: as many parts as fill them once (a second wave costs its ramp-up: 1,024 blocks of 256 keys
+    // took 41 us over a 32K cache of eight heads, 128 blocks of 2,048 keys 27 us), each of at least 128 keys.
+    const long long units = (long long)n_seq * h->cfg.kv_heads;
+    long long parts = 2ll * h->sm_count / units;
+    const long long most = ((long long)max_k + 127) / 128;
+    if (parts > most) parts = most;
+    // More parts than a cluster holds pay off only over long caches, where the join's launch and workspace are small.
+    if (parts > kClusterMax && max_k <= 512 * kClusterMax) parts = kClusterMax;
+    if (parts > kClusterMax) {
+      parts = h->sm_count / units;                          // one block per SM: fewer and longer parts for the join
+      if (parts < kClusterMax) parts = kClusterMax;
+    }
+    if (parts > kMaxSplits) parts = kMaxSplits;
+    if (parts < 1) parts = 1;
+    c.chunk = (int)(((max_k + parts - 1) / parts + 63) / 64 * 64);
+    if (c.chunk < 64) c.chunk = 64;
+    c.splits = max_k > 0 ? (int)(((long long)max_k + c.chunk - 1) / c.chunk) : 1;
+    c.clustered = c.splits > 1 && c.splits <= kClusterMax;
   } else {
     const int tile = kTileM / group;
     const long long blocks = ((max_q <= 2 * tile ? 0 : total_q / (2 * tile)) + n_seq) * (long long)h->cfg.kv_heads;
     const long long nb = (max_k + 127) / 128;
     long long s = h->sm_count / blocks;
     if (s > nb / 4) s = nb / 4;
+    if (s > kMaxSplits) s = kMaxSplits;
     c.splits = s > 1 ? (int)s : 1;
   }
   return c;
 }
 
 size_t workspace_of(const tra_packed* h, const Choice& c, int total_q) {
-  return c.splits > 1 ? sizeof(float) * (size_t)c.splits * total_q * h->cfg.heads * (h->cfg.head_dim + 2) : 0;
+  return c.splits > 1 && !c.clustered ? sizeof(float) * (size_t)c.splits * total_q * h->cfg.heads * (h->cfg.head_dim + 2) : 0;
 }
 
 bool bad_sizes(const tra_packed* h, int n_seq, int total_q, int max_q, int max_k) {
@@ -174,8 +218,8 @@ int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_lau
 template <typename T>
 int launch_join(const tra_packed* h, const tra_packed_launch& p, cudaStream_t stream) {
   const dim3 blocks((unsigned)((long long)p.total_q * p.heads));
-  return h->cfg.head_dim == 128 ? tra_launch(tra_packed_join_kernel<T, 128>, blocks, 32 * kJoinWarps, 0, stream, true, p)
-                                : tra_launch(tra_packed_join_kernel<T, 64>, blocks, 32 * kJoinWarps, 0, stream, true, p);
+  return h->cfg.head_dim == 128 ? tra_launch(tra_packed_join_kernel<T, 128>, blocks, 32 * kJoinWarps, 0, stream, true, 1, p)
+                                : tra_launch(tra_packed_join_kernel<T, 64>, blocks, 32 * kJoinWarps, 0, stream, true, 1, p);
 }
 
 }  // namespace
@@ -235,9 +279,9 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
   const tra_packed_ctx ctx = {h, (cudaStream_t)stream_};
   p.o = a->o;
   const Choice c = choose(h, a->n_seq, a->total_q, a->max_q, a->max_k);
-  if (c.splits > 65535) return TRA_ERR_UNSUPPORTED;
   p.splits = c.splits;
-  if (c.splits > 1) {
+  const bool join = c.splits > 1 && !c.clustered;
+  if (join) {
     if ((long long)a->total_q * p.heads > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
     if (!workspace || ((uintptr_t)workspace & 15)) return TRA_ERR_INVALID_ARG;
     if (workspace_bytes < workspace_of(h, c, a->total_q)) return TRA_ERR_CAPACITY;
@@ -254,13 +298,13 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
   if ((rc = make_packed_map(&p.map_k, h, kk, ks, p.kv_heads, tk, 1, key_box)) != TRA_OK) return rc;
   if ((rc = make_packed_map(&p.map_v, h, vv, vs, p.kv_heads, tk, 1, key_box)) != TRA_OK) return rc;
   if (c.rows) {
-    rc = tra_packed_rows(ctx, p, c.chunk);
+    rc = tra_packed_rows(ctx, p, c.chunk, c.clustered);
   } else {
     if ((rc = make_packed_map(&p.map_q, h, a->q, a->q_stride, p.heads, a->total_q, p.group, p.tile_tokens)) != TRA_OK) return rc;
     p.n_units = (a->max_q <= 2 * p.tile_tokens ? 0 : a->total_q / (2 * p.tile_tokens)) + a->n_seq;
     rc = h->cfg.head_dim == 128 ? tra_packed_fwd_d128(ctx, p) : tra_packed_fwd_d64(ctx, p);
   }
-  if (rc != TRA_OK || c.splits == 1) return rc;
+  if (rc != TRA_OK || !join) return rc;
   return h->cfg.dtype == TRA_BF16 ? launch_join<__nv_bfloat16>(h, p, ctx.stream) : launch_join<__half>(h, p, ctx.stream);
 }
 

@@ -45,7 +45,7 @@ int tra_packed_fwd_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_fwd_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
-int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk);
+int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered);
 
 #ifdef __CUDACC__
 namespace {
@@ -61,19 +61,27 @@ int tra_allow_smem(int bytes, int device) {
   return TRA_OK;
 }
 
-// Launch; after_last: may start while the stream's last kernel ends (see wait_last_launch).
+// Launch; after_last: may start while the stream's last kernel ends (see wait_last_launch); cluster: blocks along z that form
+// a thread-block cluster.
 template <typename... Params, typename... Args>
-int tra_launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, bool after_last, const Args&... args) {
+int tra_launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, bool after_last, int cluster,
+               const Args&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = after_last ? 1 : 0;
+  cudaLaunchAttribute attr[2];
+  cfg.attrs = attr;
+  if (after_last) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = attr[cfg.numAttrs].val.clusterDim.y = 1;
+    attr[cfg.numAttrs++].val.clusterDim.z = (unsigned)cluster;
+  }
   return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? TRA_OK : TRA_ERR_CUDA;
 }
 

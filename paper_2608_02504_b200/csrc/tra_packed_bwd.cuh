@@ -781,7 +781,7 @@ int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   int rc = TRA_OK;
   if (rows > 0) {
     constexpr int kRows = 256 / (D / 8);
-    if ((rc = tra_launch(tra_packed_delta_kernel<T, D>, dim3((unsigned)((rows + kRows - 1) / kRows)), 256, 0, c.stream, false, a)) != TRA_OK)
+    if ((rc = tra_launch(tra_packed_delta_kernel<T, D>, dim3((unsigned)((rows + kRows - 1) / kRows)), 256, 0, c.stream, false, 1, a)) != TRA_OK)
       return rc;
   }
   const int dkv_units = a.max_k > 0 ? (a.max_k <= kTileM ? 0 : a.total_k / kTileM) + a.n_seq : 0;
@@ -791,7 +791,7 @@ int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   if (blocks > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
   constexpr auto kern = tra_packed_bwd_kernel<T, D, kCausal>;
   if ((rc = tra_allow_smem<kern>(BwdCfg<D>::kSmemBytes, c.h->device)) != TRA_OK) return rc;
-  return tra_launch(kern, dim3((unsigned)blocks), kBwdThreads, BwdCfg<D>::kSmemBytes, c.stream, rows > 0, a, dkv_units, dq_units);
+  return tra_launch(kern, dim3((unsigned)blocks), kBwdThreads, BwdCfg<D>::kSmemBytes, c.stream, rows > 0, 1, a, dkv_units, dq_units);
 }
 
 template <int D>

@@ -442,7 +442,7 @@ int launch_fwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   const int rc = tra_allow_smem<kern>(FwdCfg<D>::kSmemBytes, c.h->device);
   if (rc != TRA_OK) return rc;
   return tra_launch(kern, dim3((unsigned)a.n_units, (unsigned)a.kv_heads, (unsigned)a.splits), kFwdThreads, FwdCfg<D>::kSmemBytes,
-                    c.stream, false, a);
+                    c.stream, false, 1, a);
 }
 
 template <int D>

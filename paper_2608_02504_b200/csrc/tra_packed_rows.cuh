@@ -6,8 +6,10 @@
 // loads (96 KB in flight per block, two blocks per SM), and four warps take sixteen keys of every tile each, with a running
 // maximum and sum of their own, joined at the end through shared memory.  The products are 16 x 16 x 16 mma.sync steps:
 // a 128-row tcgen05 tile would spend its softmax on 112 rows that are not there (128 threads walk 128 score columns per key
-// block whatever the rows hold), and the tensor pipe is idle either way.  The parts of a sequence are joined by
-// tra_packed_join_kernel.
+// block whatever the rows hold), and the tensor pipe is idle either way.
+//
+// The parts of a sequence: up to eight are one thread-block cluster and are joined through distributed shared memory, without
+// a workspace or a second launch; more go through a workspace and tra_packed_join_kernel.
 #pragma once
 #include "tra_packed.h"
 #include "tra_packed_ptx.cuh"
@@ -29,8 +31,8 @@ struct RowsCfg {
   static constexpr int kSmemBytes = kSmemData + 1024 + 256;
 };
 // the join of the warps' parts reuses the ring
-static_assert(kRowsWarps * kRowsMax * (128 + 4) * 4 <= RowsCfg<128>::kSmemData, "join area");
-static_assert(kRowsWarps * kRowsMax * (64 + 4) * 4 <= RowsCfg<64>::kSmemData, "join area");
+static_assert((kRowsWarps + 1) * kRowsMax * (128 + 4) * 4 <= RowsCfg<128>::kSmemData, "join area");
+static_assert((kRowsWarps + 1) * kRowsMax * (64 + 4) * 4 <= RowsCfg<64>::kSmemData, "join area");
 
 struct RowsCtl {
   uint64_t full[6], empty[6];
@@ -65,9 +67,21 @@ __device__ __forceinline__ void mma16816<__half>(float* c, const uint32_t* a, ui
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// ---- thread-block clusters: a barrier over the cluster, and 16 bytes of another block's shared memory
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float4 cluster_ld4(const void* own_address, uint32_t rank) {
+  uint32_t addr;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_u32(own_address)), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 // sequence = blockIdx.x, key/value head = blockIdx.y, part = blockIdx.z (keys [part * chunk, ...)); chunk is a multiple of 64
 template <typename T, int D>
-__global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const __grid_constant__ tra_packed_launch p, int chunk) {
+__global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const __grid_constant__ tra_packed_launch p, int chunk, int clustered) {
   using C = RowsCfg<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -76,13 +90,13 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
   const int seq = blockIdx.x, kvh = blockIdx.y;
   const tra_seq_range qr = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
   const tra_seq_range kr = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
-  if (gridDim.z > 1) allow_next_launch();                    // the join of the parts
+  const bool parts = gridDim.z > 1 && !clustered;
+  if (parts) allow_next_launch();                            // the join of the parts
   const int n_rows = qr.len * p.group;                       // <= 16
   if (n_rows == 0) return;
   const int ahead = kr.len - qr.len;
   const int key0 = (int)blockIdx.z * chunk, key1 = min(key0 + chunk, kr.len);     // chunk * parts fits an int
   const int n_tiles = key1 > key0 ? (key1 - key0 + kRowsTile - 1) / kRowsTile : 0;
-  const bool parts = gridDim.z > 1;
   const long long part_base = (long long)blockIdx.z * p.total_q * p.heads;
   auto row_token = [&](int r) -> long long { return qr.begin + r / p.group; };
   auto row_head = [&](int r) -> int { return kvh * p.group + r % p.group; };
@@ -254,14 +268,17 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
     }
   }
   __syncthreads();                                           // every tile has been read: the ring becomes the join area
-  if (ctl->abort_flag) {
-    // a wait ran out: copies in flight land before the block ends; nothing is written
+  const bool gave_up = ctl->abort_flag != 0;
+  if (gave_up) {
+    // a wait ran out: copies in flight land before the block ends; nothing is written (and nothing added to a cluster's rows)
     const unsigned long long t0 = globaltimer_ns();
     while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-    return;
+    if (!clustered) return;
   }
   float* part = (float*)smem;                                // [warp][row][D], then [warp][row][4]: m, l, le
   float* stat = part + kRowsWarps * kRowsMax * D;
+  float* mine = stat + kRowsWarps * kRowsMax * 4;            // the block's rows: [row][D], then [row][4]
+  float* mine_stat = mine + kRowsMax * D;
   if (warp < kRowsWarps) {
     const int g = lane >> 2, tig = lane & 3;
 #pragma unroll
@@ -273,56 +290,82 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
         *reinterpret_cast<float2*>(dst + i * 8 + tig * 2) = make_float2(o[i][half * 2], o[i][half * 2 + 1]);
       if (tig == 0) {
         float* st = stat + (warp * kRowsMax + r) * 4;
-        st[0] = m[half];
+        st[0] = gave_up ? -INFINITY : m[half];
         st[1] = l[half];
         st[2] = le[half];
       }
     }
   }
   __syncthreads();
-  // four channels of a row per step
-  for (int i = tid; i < n_rows * (D / 4); i += kRowsThreads) {
-    const int r = i / (D / 4), c = (i % (D / 4)) * 4;
+  // rows of the parts `st(w)`, `row(w)` of n (warps of a block, then blocks of a cluster) on one reference
+  auto join = [](int n, auto st, auto row, float& ref, float& sl, float& se, float4& acc) {
     float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kRowsWarps; ++w) top = fmaxf(top, stat[(w * kRowsMax + r) * 4]);
-    const float ref = top > -INFINITY ? top : 0.f;
-    float sl = 0.f, se = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kRowsWarps; ++w) {
-      const float* st = stat + (w * kRowsMax + r) * 4;
-      const float f = ex2(st[0] - ref);
-      const float4 v = *reinterpret_cast<const float4*>(part + (w * kRowsMax + r) * D + c);
-      sl += f * st[1];
-      se += f * st[2];
-      acc[0] += f * v.x;
-      acc[1] += f * v.y;
-      acc[2] += f * v.z;
-      acc[3] += f * v.w;
+    for (int w = 0; w < n; ++w) top = fmaxf(top, st(w).x);
+    ref = top > -INFINITY ? top : 0.f;
+    sl = se = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w = 0; w < n; ++w) {
+      const float4 t = st(w), v = row(w);
+      const float f = ex2(t.x - ref);
+      if (t.x == -INFINITY) continue;                        // nothing seen there
+      sl += f * t.y;
+      se += f * t.z;
+      acc.x += f * v.x;
+      acc.y += f * v.y;
+      acc.z += f * v.z;
+      acc.w += f * v.w;
     }
+  };
+  auto finish = [&](int r, int c, float ref, float sl, float se, const float4& acc) {
     const float inv = sl != 0.f ? 1.f / sl : 0.f;
     const long long tok = row_token(r), row = tok * p.heads + row_head(r);
     if (parts) {
-      *reinterpret_cast<float4*>(p.part_o + (part_base + row) * D + c) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      *reinterpret_cast<float4*>(p.part_o + (part_base + row) * D + c) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
       if (c == 0) {
         p.part_lse2[part_base + row] = sl != 0.f ? ref + log2f(sl) : -INFINITY;
         if (p.part_exact) p.part_exact[part_base + row] = se != 0.f ? ref + log2f(se) : -INFINITY;
       }
     } else {
       T* dst = (T*)p.o + tok * p.o_stride[0] + row_head(r) * p.o_stride[1] + c;
-      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_pair<T>(acc[0] * inv, acc[1] * inv), pack_pair<T>(acc[2] * inv, acc[3] * inv));
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_pair<T>(acc.x * inv, acc.y * inv), pack_pair<T>(acc.z * inv, acc.w * inv));
       if (c == 0 && p.lse) p.lse[row] = se != 0.f ? (ref + log2f(se)) * kLn2 : -INFINITY;
     }
+  };
+  // four channels of a row per step
+  for (int i = tid; i < n_rows * (D / 4); i += kRowsThreads) {
+    const int r = i / (D / 4), c = (i % (D / 4)) * 4;
+    float ref, sl, se;
+    float4 acc;
+    join(kRowsWarps, [&](int w) { return *reinterpret_cast<const float4*>(stat + (w * kRowsMax + r) * 4); },
+         [&](int w) { return *reinterpret_cast<const float4*>(part + (w * kRowsMax + r) * D + c); }, ref, sl, se, acc);
+    if (clustered) {
+      *reinterpret_cast<float4*>(mine + r * D + c) = acc;
+      if (c == 0) *reinterpret_cast<float4*>(mine_stat + r * 4) = make_float4(sl != 0.f ? ref : -INFINITY, sl, se, 0.f);
+    } else {
+      finish(r, c, ref, sl, se, acc);
+    }
+  }
+  if (clustered) {
+    cluster_sync();                                          // every block's rows are there
+    for (int i = (int)blockIdx.z * kRowsThreads + tid; i < n_rows * (D / 4); i += (int)gridDim.z * kRowsThreads) {
+      const int r = i / (D / 4), c = (i % (D / 4)) * 4;
+      float ref, sl, se;
+      float4 acc;
+      join((int)gridDim.z, [&](int w) { return cluster_ld4(mine_stat + r * 4, (uint32_t)w); },
+           [&](int w) { return cluster_ld4(mine + r * D + c, (uint32_t)w); }, ref, sl, se, acc);
+      finish(r, c, ref, sl, se, acc);
+    }
+    cluster_sync();                                          // nobody leaves while its rows are read
   }
 }
 
 template <typename T, int D>
-int launch_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk) {
+int launch_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered) {
   constexpr auto kern = tra_packed_rows_kernel<T, D>;
   const int rc = tra_allow_smem<kern>(RowsCfg<D>::kSmemBytes, c.h->device);
   if (rc != TRA_OK) return rc;
   return tra_launch(kern, dim3((unsigned)a.n_seq, (unsigned)a.kv_heads, (unsigned)a.splits), kRowsThreads, RowsCfg<D>::kSmemBytes, c.stream,
-                    false, a, chunk);
+                    false, clustered ? a.splits : 1, a, chunk, clustered ? 1 : 0);
 }
 
 }  // namespace
