@@ -103,11 +103,17 @@ struct tra_unit {
   tra_seq_range q, k;
 };
 
-// Finds the block's unit, units numbered sequence by sequence, ceil(length / unit_tokens) each, length in queries or
+// A lane's share of 32 sequences: their ranges, and the units before and in them.
+struct tra_seq_cache {
+  int s0 = -1, before = 0, total = 0, excl = 0, n = 0;
+  tra_seq_range q = {0, 0}, k = {0, 0};
+};
+
+// Finds a unit, units numbered sequence by sequence, ceil(length / unit_tokens) each, length in queries or
 // (by_keys) in keys; one_each: unit s is the whole of sequence s.  One warp calls it; every lane gets the result.  32 sequences are
-// read at a time, the ranges of both sides with them, so that the block waits for one load in most launches.
-__device__ __forceinline__ tra_unit tra_find_unit(const tra_packed_launch& p, bool by_keys, bool one_each, int unit_tokens,
-                                                  int unit) {
+// read at a time, the ranges of both sides with them, and kept for the next call.
+__device__ __forceinline__ tra_unit tra_find_unit(const tra_packed_launch& p, bool by_keys, bool one_each, int unit_tokens, int unit,
+                                                  tra_seq_cache& c) {
   const int lane = threadIdx.x & 31;
   tra_unit u = {-1, 0, {0, 0}, {0, 0}};
   if (one_each) {
@@ -116,35 +122,41 @@ __device__ __forceinline__ tra_unit tra_find_unit(const tra_packed_launch& p, bo
     u.k = tra_clamp_range(p.k_begin[unit], p.k_end[unit], p.total_k, p.max_k, p.status);
     return u;
   }
-  int before = 0;
-  for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
-    tra_seq_range q = {0, 0}, k = {0, 0};
-    if (s0 + lane < p.n_seq) {
-      const int s = s0 + lane, q0 = p.cu_q[s], q1 = p.cu_q[s + 1], k0 = p.k_begin[s], k1 = p.k_end[s];
-      q = tra_clamp_range(q0, q1, p.total_q, p.max_q, p.status);
-      k = tra_clamp_range(k0, k1, p.total_k, p.max_k, p.status);
+  if (c.s0 < 0 || unit < c.before) {         // nothing read yet, or the unit lies in front of what was
+    c.s0 = -32;
+    c.before = c.total = 0;
+  }
+  while (unit >= c.before + c.total) {
+    c.s0 += 32;
+    c.before += c.total;
+    if (c.s0 >= p.n_seq) {
+      c.s0 = -1;
+      return u;
     }
-    const int n = ((by_keys ? k.len : q.len) + unit_tokens - 1) / unit_tokens;
-    int incl = n;
+    c.q = c.k = {0, 0};
+    if (c.s0 + lane < p.n_seq) {
+      const int s = c.s0 + lane, q0 = p.cu_q[s], q1 = p.cu_q[s + 1], k0 = p.k_begin[s], k1 = p.k_end[s];
+      c.q = tra_clamp_range(q0, q1, p.total_q, p.max_q, p.status);
+      c.k = tra_clamp_range(k0, k1, p.total_k, p.max_k, p.status);
+    }
+    c.n = ((by_keys ? c.k.len : c.q.len) + unit_tokens - 1) / unit_tokens;
+    int incl = c.n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int up = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += up;
     }
-    const int excl = before + incl - n;
-    const unsigned hit = __ballot_sync(0xffffffffu, unit >= excl && unit < before + incl);
-    if (hit) {
-      const int l = __ffs(hit) - 1;
-      u.seq = s0 + l;
-      u.index = unit - __shfl_sync(0xffffffffu, excl, l);
-      u.q.begin = __shfl_sync(0xffffffffu, q.begin, l);
-      u.q.len = __shfl_sync(0xffffffffu, q.len, l);
-      u.k.begin = __shfl_sync(0xffffffffu, k.begin, l);
-      u.k.len = __shfl_sync(0xffffffffu, k.len, l);
-      return u;
-    }
-    before += __shfl_sync(0xffffffffu, incl, 31);
+    c.excl = incl - c.n;
+    c.total = __shfl_sync(0xffffffffu, incl, 31);
   }
+  const int at = unit - c.before;
+  const int l = __ffs(__ballot_sync(0xffffffffu, at >= c.excl && at < c.excl + c.n)) - 1;
+  u.seq = c.s0 + l;
+  u.index = at - __shfl_sync(0xffffffffu, c.excl, l);
+  u.q.begin = __shfl_sync(0xffffffffu, c.q.begin, l);
+  u.q.len = __shfl_sync(0xffffffffu, c.q.len, l);
+  u.k.begin = __shfl_sync(0xffffffffu, c.k.begin, l);
+  u.k.len = __shfl_sync(0xffffffffu, c.k.len, l);
   return u;
 }
 

@@ -174,17 +174,21 @@ __device__ __forceinline__ void mma_tiles(uint32_t d, uint32_t a_lo, uint32_t b_
   }
 }
 
-// Stores 32 channels of one row, scaled and rounded.
-template <typename T>
-__device__ __forceinline__ void store32(T* dst, const uint32_t* bits, float mul) {
-  uint4* out = reinterpret_cast<uint4*>(dst);
+// The warpgroup's half (D / 2 channels from h D / 2) of a sum in tensor memory, scaled and rounded, to the rows' memory.
+template <typename T, int D>
+__device__ __forceinline__ void store_half(const RowAddresses& rows, uint32_t taddr, int h, bool any, float mul) {
+#pragma unroll 1
+  for (int c = 0; c < D / 64; ++c) {
+    uint32_t v[32];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    uint32_t w[4];
+    for (int j = 0; j < 32; ++j) v[j] = 0u;
+    if (any) {
+      tmem_ld32(taddr + h * (D / 2) + c * 32, v);
+      tmem_wait_ld(v);
+    }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = pack_pair<T>(__uint_as_float(bits[q * 8 + 2 * j]) * mul, __uint_as_float(bits[q * 8 + 2 * j + 1]) * mul);
-    out[q] = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int j = 0; j < 16; ++j) v[j] = pack_pair<T>(__uint_as_float(v[2 * j]) * mul, __uint_as_float(v[2 * j + 1]) * mul);
+    rows.store64(v, h * D + c * 64);
   }
 }
 
@@ -205,7 +209,8 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
 
   // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    const tra_unit u = tra_find_unit(p, true, p.max_k <= kTileM, kTileM, unit);
+    tra_seq_cache seqs;
+    const tra_unit u = tra_find_unit(p, true, p.max_k <= kTileM, kTileM, unit, seqs);
     if (lane == 0) ctl->unit = u;
   } else if (warp == 9) {
     tmem_alloc_all(&ctl->tmem_base);
@@ -486,22 +491,10 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
       const bool row_valid = key < *(volatile int*)&ctl->unit.k.len;
       const long long row = *(volatile int*)&ctl->unit.k.begin + (row_valid ? key : 0);
       T* out[2] = {(T*)p.dv + row * p.dv_stride[0] + kvh * p.dv_stride[1], (T*)p.dk + row * p.dk_stride[0] + kvh * p.dk_stride[1]};
-#pragma unroll
-      for (int which = 0; which < 2; ++which) {
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          const int col = h * (D / 2) + c * 32;
-          uint32_t bits[32];
-          if (n > 0) {
-            tmem_ld32(tmem + lane_base + (which ? C::kSum1 : C::kSum0) + col, bits);
-            tmem_wait_ld(bits);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) bits[j] = 0u;
-          }
-          if (row_valid) store32<T>(out[which] + col, bits, which ? p.sm_scale : 1.f);
-        }
-      }
+#pragma unroll 1
+      for (int which = 0; which < 2; ++which)
+        store_half<T, D>(RowAddresses(row_valid ? out[which] : nullptr), tmem + lane_base + (which ? C::kSum1 : C::kSum0), h, n > 0,
+                         which ? p.sm_scale : 1.f);
     }
   }
   bwd_teardown(ctl, tmem, warp);
@@ -521,7 +514,8 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
 
   // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    const tra_unit u = tra_find_unit(p, false, p.max_q <= tile_tokens, tile_tokens, unit);
+    tra_seq_cache seqs;
+    const tra_unit u = tra_find_unit(p, false, p.max_q <= tile_tokens, tile_tokens, unit, seqs);
     if (lane == 0) ctl->unit = u;
   } else if (warp == 9) {
     tmem_alloc_all(&ctl->tmem_base);
@@ -713,19 +707,7 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
     if (alive) {
       tc_fence_after();
       T* out = (T*)p.dq + tok_g * p.dq_stride[0] + head * p.dq_stride[1];
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        const int col = h * (D / 2) + c * 32;
-        uint32_t bits[32];
-        if (n > 0) {
-          tmem_ld32(tmem + lane_base + 256 + col, bits);
-          tmem_wait_ld(bits);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) bits[j] = 0u;
-        }
-        if (row_valid) store32<T>(out + col, bits, p.sm_scale);
-      }
+      store_half<T, D>(RowAddresses(row_valid ? out : nullptr), tmem + lane_base + 256, h, n > 0, p.sm_scale);
     }
   }
   bwd_teardown(ctl, tmem, warp);

@@ -71,6 +71,28 @@ __device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
 __device__ __forceinline__ void allow_next_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_last_launch() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// Cluster launch control: asks for a block of this grid that has not been started yet; the 16-byte answer arrives on `bar`.
+// true: `block` is its blockIdx.x and the block will not be started; false: none left (no further request is made then).
+__device__ __forceinline__ void ask_for_launch(uint32_t answer, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ bool launch_answer(uint32_t answer, int& block) {
+  uint32_t yes, x = 0;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 a;\n\t"
+      "ld.shared.b128 a, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "mov.u32 %1, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, a;\n\t}"
+      : "=r"(yes), "=r"(x)
+      : "r"(answer)
+      : "memory");
+  if (yes) block = (int)x;
+  return yes != 0;
+}
+
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -81,6 +103,44 @@ __device__ __forceinline__ void tmem_alloc_all(uint32_t* base) {
 __device__ __forceinline__ void tmem_free_all(uint32_t tmem) {
   asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
+
+// Rows to memory.  A thread holds 64 bytes of its own row (tensor memory gives every lane a row); stored like that, each of a
+// warp's 16-byte stores touches 32 lines.  Groups of four lanes exchange 16-byte pieces first, v[4 u ..] = piece u of the own row ->
+// v[4 i ..] = piece (lane % 4) of the group's row i, and a store touches eight.  (Groups of eight and whole lines take three
+// times the instructions, and this code runs once per tile, out of a cold instruction cache: 7,600 cycles for two tiles
+// against 4,500 without any exchange.)
+struct RowAddresses {
+  uint64_t row[4];             // of the group's rows (0: not stored)
+  __device__ __forceinline__ explicit RowAddresses(const void* own) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) row[i] = __shfl_sync(0xffffffffu, (unsigned long long)own, (threadIdx.x & 28) + i);
+  }
+  // 64 bytes of every row, `offset` bytes from its start; all lanes of the warp call it
+  __device__ __forceinline__ void store64(uint32_t* v, int offset) const {
+    const int l = threadIdx.x & 3;
+#pragma unroll
+    for (int b = 1; b < 4; b <<= 1) {
+      const bool up = (l & b) != 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (u & b) continue;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t& lo = v[u * 4 + w];
+          uint32_t& hi = v[(u | b) * 4 + w];
+          const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? lo : hi, b);
+          if (up)
+            lo = got;
+          else
+            hi = got;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (row[i]) *reinterpret_cast<uint4*>(row[i] + offset + l * 16) = make_uint4(v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3]);
+  }
+};
 
 // Zeroes rows [row0, row1) of `atoms` 64-column pieces of a tile, rows 128 bytes apart (the 128-byte swizzle moves
 // 16-byte chunks inside a row only).
