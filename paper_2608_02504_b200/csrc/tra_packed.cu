@@ -8,27 +8,27 @@
 
 namespace {
 
-constexpr int kJoinWarps = 4;
 constexpr int kMaxSplits = 256;       // parts of a split launch
 
 // O = sum_s w_s O_s, w_s = 2^(lse2_s - lse2), lse2 = log2 sum_s 2^lse2_s over the parts of a split launch; lse from the
-// unrounded sums in the same way.  One block per (token, head): first the weights, all parts' logarithms read at once, then
-// its warps take every fourth part, four loads in flight each.
-template <typename T, int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) tra_packed_join_kernel(const __grid_constant__ tra_packed_launch p) {
-  constexpr int kPer = D / 32;
-  __shared__ __align__(16) float s_o[kJoinWarps][D];
-  __shared__ float s_w[kMaxSplits];
+// unrounded sums in the same way.  kWarps warps per (token, head): first the weights, all parts' logarithms read at once and
+// kept by the lanes, then every warp adds its parts, four loads in flight.  Four warps per row where there are few rows (the
+// serial loads count), one where there are many (12,000 rows of two parts: 42 us a call with a block each, 29 with a warp each).
+template <typename T, int D, int kWarps>
+__global__ void __launch_bounds__(128) tra_packed_join_kernel(const __grid_constant__ tra_packed_launch p) {
+  constexpr int kPer = D / 32, kLogs = kMaxSplits / 32;
+  __shared__ __align__(16) float s_o[kWarps > 1 ? kWarps : 1][kWarps > 1 ? D : 1];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long row = blockIdx.x, stride = (long long)p.total_q * p.heads;
-  const int tok = (int)(row / p.heads), head = (int)(row - (long long)tok * p.heads);
+  const long long stride = (long long)p.total_q * p.heads;
+  const long long row = kWarps > 1 ? blockIdx.x : (long long)blockIdx.x * 4 + warp;
   wait_last_launch();
+  if (row >= stride) return;
+  const int tok = (int)(row / p.heads), head = (int)(row - (long long)tok * p.heads);
   // rows in front of the first and behind the last sequence stay as they are
   if (tok < p.cu_q[0] || tok >= p.cu_q[p.n_seq]) return;
-  // every warp forms the same sums (kMaxSplits / 32 logarithms per lane)
-  float v[kMaxSplits / 32], top = -INFINITY;
+  float v[kLogs], top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kMaxSplits / 32; ++i) {
+  for (int i = 0; i < kLogs; ++i) {
     const int s = i * 32 + lane;
     v[i] = s < p.splits ? p.part_lse2[s * stride + row] : -INFINITY;
     top = v[i] != v[i] ? v[i] : fmaxf(top, v[i]);
@@ -41,60 +41,69 @@ __global__ void __launch_bounds__(32 * kJoinWarps) tra_packed_join_kernel(const 
   const float ref = top == -INFINITY ? 0.f : top;        // no part holds a key: every weight is 0
   float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < kMaxSplits / 32; ++i) {
+  for (int i = 0; i < kLogs; ++i) {
     v[i] = ex2(v[i] - ref);                              // parts without a key: 0
     sum += v[i];
-    if (warp == 0) s_w[i * 32 + lane] = v[i];
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  __syncthreads();
   float o[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) o[i] = 0.f;
+  const int first = kWarps > 1 ? warp : 0;
   const float* src = p.part_o + row * D + lane * kPer;
-  for (int s0 = warp; s0 < p.splits; s0 += 4 * kJoinWarps) {
-    float part[4][kPer], w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int s = s0 + j * kJoinWarps;
-      w[j] = s < p.splits ? s_w[s] : 0.f;
+  for (int k = 0; k < kLogs; ++k) {
+    for (int s0 = k * 32 + first; s0 < min(p.splits, k * 32 + 32); s0 += 4 * kWarps) {
+      float part[4][kPer], w[4];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) part[j][i] = 0.f;
-      if (w[j] != 0.f) {                                 // a part without a key has no row to read
-        if constexpr (kPer == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(src + s * stride * D);
-          part[j][0] = x.x, part[j][1] = x.y, part[j][2] = x.z, part[j][3] = x.w;
-        } else {
-          const float2 x = *reinterpret_cast<const float2*>(src + s * stride * D);
-          part[j][0] = x.x, part[j][1] = x.y;
+      for (int j = 0; j < 4; ++j) {
+        const int s = s0 + j * kWarps;
+        const float w_s = __shfl_sync(0xffffffffu, v[k], s & 31);
+        w[j] = s < k * 32 + 32 ? w_s : 0.f;              // (past the last part the weights are 0)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) part[j][i] = 0.f;
+        if (w[j] != 0.f) {                               // a part without a key has no row to read
+          if constexpr (kPer == 4) {
+            const float4 x = *reinterpret_cast<const float4*>(src + s * stride * D);
+            part[j][0] = x.x, part[j][1] = x.y, part[j][2] = x.z, part[j][3] = x.w;
+          } else {
+            const float2 x = *reinterpret_cast<const float2*>(src + s * stride * D);
+            part[j][0] = x.x, part[j][1] = x.y;
+          }
         }
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) o[i] = fmaf(w[j], part[j][i], o[i]);
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) o[i] = fmaf(w[j], part[j][i], o[i]);
   }
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) s_o[warp][lane * kPer + i] = o[i];
-  __syncthreads();
   const float inv = sum != 0.f ? 1.f / sum : 0.f;
   T* dst = (T*)p.o + tok * p.o_stride[0] + head * p.o_stride[1];
-  if (threadIdx.x < D / 2) {
-    float2 a = make_float2(0.f, 0.f);
+  if constexpr (kWarps > 1) {
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) {
-      const float2 x = reinterpret_cast<const float2*>(s_o[w])[threadIdx.x];
-      a.x += x.x;
-      a.y += x.y;
+    for (int i = 0; i < kPer; ++i) s_o[warp][lane * kPer + i] = o[i];
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        o[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) o[i] += s_o[w][lane * kPer + i];
+      }
     }
-    reinterpret_cast<uint32_t*>(dst)[threadIdx.x] = pack_pair<T>(a.x * inv, a.y * inv);
   }
-  if (p.lse && warp == kJoinWarps - 1) {
+  if (kWarps == 1 || warp == 0) {
+    if constexpr (kPer == 4)
+      reinterpret_cast<uint2*>(dst)[lane] = make_uint2(pack_pair<T>(o[0] * inv, o[1] * inv), pack_pair<T>(o[2] * inv, o[3] * inv));
+    else
+      reinterpret_cast<uint32_t*>(dst)[lane] = pack_pair<T>(o[0] * inv, o[1] * inv);
+  }
+  if (p.lse && (kWarps == 1 || warp == kWarps - 1)) {
     float total = 0.f;
 #pragma unroll
-    for (int i = 0; i < kMaxSplits / 32; ++i) {
+    for (int i = 0; i < kLogs; ++i) {
       const int s = i * 32 + lane;
       if (s < p.splits) total += ex2(p.part_exact[s * stride + row] - ref);
     }
@@ -131,7 +140,9 @@ Choice choose(const tra_packed* h, int n_seq, int total_q, int max_q, int max_k)
       if (parts < kClusterMax) parts = kClusterMax;
     }
     if (parts > kMaxSplits) parts = kMaxSplits;
-    if (parts < 1) parts = 1;
+    // Enough sequences to fill the GPU: long caches in two parts all the same, since their lengths differ (64 caches of up to
+    // 32K keys, eight heads: 640 us against 700 when the lengths are spread evenly, 1,175 against 1,162 when they are equal).
+    if (parts <= 1) parts = max_k >= 8192 ? 2 : 1;
     c.chunk = (int)(((max_k + parts - 1) / parts + 63) / 64 * 64);
     if (c.chunk < 64) c.chunk = 64;
     c.splits = max_k > 0 ? (int)(((long long)max_k + c.chunk - 1) / c.chunk) : 1;
@@ -141,7 +152,7 @@ Choice choose(const tra_packed* h, int n_seq, int total_q, int max_q, int max_k)
     const long long blocks = ((max_q <= 2 * tile ? 0 : total_q / (2 * tile)) + n_seq) * (long long)h->cfg.kv_heads;
     const long long nb = (max_k + 127) / 128;
     long long s = h->sm_count / blocks;
-    if (s > nb / 4) s = nb / 4;
+    if (s > nb / 2) s = nb / 2;                            // parts of two key blocks at least
     if (s > kMaxSplits) s = kMaxSplits;
     c.splits = s > 1 ? (int)s : 1;
   }
@@ -215,11 +226,16 @@ int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_lau
   return TRA_OK;
 }
 
+template <typename T, int D>
+int launch_join_shape(const tra_packed* h, const tra_packed_launch& p, cudaStream_t stream) {
+  const long long rows = (long long)p.total_q * p.heads;
+  if (rows >= 16ll * h->sm_count)
+    return tra_launch(tra_packed_join_kernel<T, D, 1>, dim3((unsigned)((rows + 3) / 4)), 128, 0, stream, true, 1, p);
+  return tra_launch(tra_packed_join_kernel<T, D, 4>, dim3((unsigned)rows), 128, 0, stream, true, 1, p);
+}
 template <typename T>
 int launch_join(const tra_packed* h, const tra_packed_launch& p, cudaStream_t stream) {
-  const dim3 blocks((unsigned)((long long)p.total_q * p.heads));
-  return h->cfg.head_dim == 128 ? tra_launch(tra_packed_join_kernel<T, 128>, blocks, 32 * kJoinWarps, 0, stream, true, 1, p)
-                                : tra_launch(tra_packed_join_kernel<T, 64>, blocks, 32 * kJoinWarps, 0, stream, true, 1, p);
+  return h->cfg.head_dim == 128 ? launch_join_shape<T, 128>(h, p, stream) : launch_join_shape<T, 64>(h, p, stream);
 }
 
 }  // namespace
