@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "tra.h"
 
 #define TRA_MAX_SEG 4       // bounding boxes kept per block
@@ -85,6 +87,19 @@ __host__ __device__ inline int tra_field_row_words(int W) { return 4 * (((W + 4)
 // Query blocks per 128-row query tile of the attention launches, for blocks of more than 32 tokens: a tile holds two
 // blocks of up to 64 tokens or one larger block (its first G * b rows are used).
 inline int tra_blocks_per_tile(int block) { return block <= 64 ? 2 : 1; }
+
+// Allows a kernel its dynamic shared memory, once per kernel and device (the attribute stays with the device's context).
+template <auto kernel>
+int tra_allow_smem(int bytes) {
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return TRA_ERR_CUDA;
+  static std::atomic<uint64_t> done{0};
+  const uint64_t bit = device < 64 ? 1ull << device : 0ull;
+  if (done.load(std::memory_order_relaxed) & bit) return TRA_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return TRA_ERR_CUDA;
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return TRA_OK;
+}
 
 // Plan time: the coarse table of the two-round radius search (tra_radius.cu).
 int tra_build_coarse_table(const uint32_t* counts, uint32_t* coarse, long long cells, int n_radii, int* status,

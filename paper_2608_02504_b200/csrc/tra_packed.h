@@ -6,9 +6,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include <atomic>
-
-#include "tra.h"
+#include "tra_common.cuh"
 
 struct tra_packed {
   tra_packed_config_t cfg;
@@ -49,17 +47,6 @@ int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chu
 
 #ifdef __CUDACC__
 namespace {
-
-// Allows a kernel its dynamic shared memory, once per kernel and device (the attribute stays with the device's context).
-template <auto kernel>
-int tra_allow_smem(int bytes, int device) {
-  static std::atomic<uint64_t> done{0};
-  const uint64_t bit = device < 64 ? 1ull << device : 0ull;
-  if (done.load(std::memory_order_relaxed) & bit) return TRA_OK;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return TRA_ERR_CUDA;
-  done.fetch_or(bit, std::memory_order_relaxed);
-  return TRA_OK;
-}
 
 // Launch; after_last: may start while the stream's last kernel ends (see wait_last_launch); cluster: blocks along z that form
 // a thread-block cluster.

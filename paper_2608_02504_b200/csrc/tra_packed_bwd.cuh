@@ -772,7 +772,7 @@ int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   if (blocks == 0) return TRA_OK;
   if (blocks > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
   constexpr auto kern = tra_packed_bwd_kernel<T, D, kCausal>;
-  if ((rc = tra_allow_smem<kern>(BwdCfg<D>::kSmemBytes, c.h->device)) != TRA_OK) return rc;
+  if ((rc = tra_allow_smem<kern>(BwdCfg<D>::kSmemBytes)) != TRA_OK) return rc;
   return tra_launch(kern, dim3((unsigned)blocks), kBwdThreads, BwdCfg<D>::kSmemBytes, c.stream, rows > 0, 1, a, dkv_units, dq_units);
 }
 

@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
 template <typename T, int D, bool kCausal, bool kExact>
 int launch_fwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   constexpr auto kern = tra_packed_fwd_kernel<T, D, kCausal, kExact>;
-  const int rc = tra_allow_smem<kern>(FwdCfg<D>::kSmemBytes, c.h->device);
+  const int rc = tra_allow_smem<kern>(FwdCfg<D>::kSmemBytes);
   if (rc != TRA_OK) return rc;
   const long long units = (long long)a.n_units * a.kv_heads * a.splits;
   if (units > 0x3fffffffll) return TRA_ERR_UNSUPPORTED;

@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
 template <typename T, int D>
 int launch_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered) {
   constexpr auto kern = tra_packed_rows_kernel<T, D>;
-  const int rc = tra_allow_smem<kern>(RowsCfg<D>::kSmemBytes, c.h->device);
+  const int rc = tra_allow_smem<kern>(RowsCfg<D>::kSmemBytes);
   if (rc != TRA_OK) return rc;
   return tra_launch(kern, dim3((unsigned)a.n_seq, (unsigned)a.kv_heads, (unsigned)a.splits), kRowsThreads, RowsCfg<D>::kSmemBytes, c.stream,
                     false, clustered ? a.splits : 1, a, chunk, clustered ? 1 : 0);

@@ -83,6 +83,10 @@ struct Raw {
       v[kVec + i] = reinterpret_cast<const uint4*>(hi)[i];
     }
   }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < 2 * kVec; ++i) v[i] = make_uint4(0u, 0u, 0u, 0u);
+  }
   __device__ __forceinline__ void store(T* lo, T* hi) const {
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
@@ -90,10 +94,29 @@ struct Raw {
       reinterpret_cast<uint4*>(hi)[i] = v[kVec + i];
     }
   }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int i = 0; i < 2 * kVec; ++i) v[i] = make_uint4(0u, 0u, 0u, 0u);
-  }
+};
+
+// Rows on their way.  One row ahead waits in registers, except in the norm's backward pass of the 16-bit types, whose registers
+// are taken: there every thread copies its own pieces into shared memory, [stage][piece][thread] 16 bytes each, kStages - 1
+// rows ahead, and reads nothing but them, so that waiting for its own copies is all the synchronisation there is.  (Measured on the
+// 32.7K-token shape: RMS backward 208 us with registers, 180 with the ring; fp32 308 and 397; forward 110 and 114.)
+__device__ __forceinline__ void copy16(uint4* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+
+template <typename T, int kNorm, bool kBackward>
+struct RotShape {
+  static constexpr bool kSums = kBackward && kNorm != TRA_NORM_NONE;
+  static constexpr bool kRing = kSums && sizeof(T) == 2;
+  static constexpr int kPieces = 4 * Raw<T>::kVec;              // of dy, and of x
+  static constexpr int kStages = kRing ? 4 : 2;                 // 2: one row ahead, in registers
+  static constexpr int kBlocksPerSm = kSums ? 2 : 4;            // as many as need no (or few) spills
+  static constexpr int kRingBytes = kRing ? kStages * kPieces * kThreads * 16 : 0;
 };
 
 // two neighbouring channels of a 16-bit type
@@ -187,6 +210,11 @@ __device__ __forceinline__ float sum2(uint64_t v) {
 
 // Sum over the threads of a row (a power of two of neighbouring lanes).
 __device__ __forceinline__ float row_sum(float s, int lanes) {
+  if (lanes == 8) {                                  // 128 channels
+    s += __shfl_xor_sync(0xffffffffu, s, 4);
+    s += __shfl_xor_sync(0xffffffffu, s, 2);
+    return s + __shfl_xor_sync(0xffffffffu, s, 1);
+  }
   for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   return s;
 }
@@ -253,15 +281,19 @@ struct Token {
 };
 
 // A block takes groups of tokens_per_block tokens: the same number of threads for every token, each walking every
-// head_slots-th head of the block's tensors (all of them one after the other, or the one blockIdx.y names).  Loads run one row
-// ahead of the arithmetic, across heads, tensors and groups; the angles of the next group go to the other half of s_turn
+// head_slots-th head of the block's tensors (all of them one after the other, or the one blockIdx.y names).  Loads run ahead
+// of the arithmetic, across heads, tensors and groups; the angles of the next group go to the other half of s_turn
 // behind the current group's rows, so that a group costs one barrier and no exposed load.
 template <typename T, int kNorm, bool kHalves, bool kBackward>
-__global__ void __launch_bounds__(kThreads, kBackward && kNorm != TRA_NORM_NONE ? 2 : 4)
+__global__ void __launch_bounds__(kThreads, RotShape<T, kNorm, kBackward>::kBlocksPerSm)
 tra_rotary_kernel(const __grid_constant__ RotArgs p) {
-  constexpr bool kSums = kBackward && kNorm != TRA_NORM_NONE;
+  using Shape = RotShape<T, kNorm, kBackward>;
+  constexpr bool kSums = Shape::kSums;
+  constexpr int kStages = Shape::kStages, kVec = Raw<T>::kVec;
+  extern __shared__ __align__(16) uint8_t smem[];
+  uint4* const ring = reinterpret_cast<uint4*>(smem) + threadIdx.x;       // [stage][piece] kThreads apart
   // per lane four floats and step, see load_pairs: [buffer][cosines, then sines][token of the group], 8 per lane
-  __shared__ __align__(16) float s_turn[2][16 * kThreads];
+  float* const s_turn = reinterpret_cast<float*>(smem + Shape::kRingBytes);
   __shared__ __align__(16) float s_weight[kNorm != TRA_NORM_NONE ? 3 * kMaxD : 4], s_bias[kNorm == TRA_NORM_LAYER ? 3 * kMaxD : 4];
   __shared__ uint64_t s_freq[kMaxD / 2];
   __shared__ uint8_t s_axis[kMaxD / 2];
@@ -302,7 +334,7 @@ tra_rotary_kernel(const __grid_constant__ RotArgs p) {
   }
 
   auto locate = [&](int base) -> Token {
-    Token k = {0, 0, 0, base + token_slot < p.rows};
+    Token k = {0, 0, 0, base < p.rows && base + token_slot < p.rows};
     if (k.there) {
       k.ordered = base + token_slot;
       if (p.tokens != p.rows) {
@@ -344,67 +376,128 @@ tra_rotary_kernel(const __grid_constant__ RotArgs p) {
     }
   };
 
-  // the row whose loads are in flight
+  const int stride = (int)gridDim.x * tokens_per_block;
+  int base = (int)blockIdx.x * tokens_per_block;
+  Token cur = locate(base);
+
+  // Ring: the row that is requested next, its token (and the one after it), tensor, head and addresses.
+  Token ask = cur, ask_next = cur;
+  int ask_base = base, ask_t = t_first, ask_h = head0, ask_stage = 0;
+  // otherwise: the row ahead
   Raw<T> raw, xraw;
-  const T *in = nullptr, *xin = nullptr;
   bool in_on = false;
-  auto load = [&](bool there, bool with_x) {
+  const T *in = nullptr, *xin = nullptr;                 // both: its address, at the thread's lower channels
+  auto aim = [&](const Token& k, int ti) {               // a token's first row of a tensor
+    const RotTensor& t = p.t[ti];
+    // forward reads at the source row and writes at the ordered one, backward the other way round
+    const int source = t.tile_major ? k.source : k.ordered;
+    in = (const T*)t.src + k.batch * t.src_stride[0] + (kBackward ? k.ordered : source) * t.src_stride[1] + head0 * t.src_stride[2] + c_lo;
+    if (kSums && t.rotate) xin = (const T*)t.x + k.batch * t.x_stride[0] + source * t.x_stride[1] + head0 * t.x_stride[2] + c_lo;
+  };
+  auto request = [&]() {                                 // ring
+    if (ask_base < p.rows) {
+      const RotTensor& t = p.t[ask_t];
+      uint4* dst = ring + ask_stage * Shape::kPieces * kThreads;
+      const bool with_x = t.rotate != 0;
+      if (ask.there && on && ask_h < t.heads) {
+        copy16(dst, in);
+        copy16(dst + kThreads, in + p.d / 2);
+        if (with_x) {
+          copy16(dst + 2 * kThreads, xin);
+          copy16(dst + 3 * kThreads, xin + p.d / 2);
+        }
+      } else {                                           // a row that is not there is zeros
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dst[i * kThreads] = make_uint4(0u, 0u, 0u, 0u);
+      }
+      ask_h += p.head_slots;
+      if (ask_h - head0 < t.heads) {
+        in += t.src_stride[2] << p.head_slots_log2;
+        xin += t.x_stride[2] << p.head_slots_log2;
+      } else {
+        ask_h = head0;
+        if (++ask_t == t_end) {
+          ask_t = t_first;
+          ask = ask_next;
+          ask_base += stride;
+          ask_next = locate(ask_base + stride);
+        }
+        aim(ask, ask_t);
+      }
+    }
+    copy_commit();                                       // an empty group at the end keeps the count
+    if (++ask_stage == kStages) ask_stage = 0;
+  };
+  auto load = [&](bool there, bool with_x) {             // no ring
     if (there) {
-      raw.load(in + c_lo, in + c_hi);
-      if (kSums && with_x) xraw.load(xin + c_lo, xin + c_hi);
+      raw.load(in, in + p.d / 2);
+      if (kSums && with_x) xraw.load(xin, xin + p.d / 2);
     } else {
       raw.zero();
       if (kSums) xraw.zero();
     }
   };
-  auto fetch_first = [&](const Token& k, int ti) {      // a token's first row of a tensor
-    const RotTensor& t = p.t[ti];
+  auto load_first = [&](const Token& k, int ti) {
     in_on = k.there && on;
-    if (in_on) {
-      // forward reads at the source row and writes at the ordered one, backward the other way round
-      const int source = t.tile_major ? k.source : k.ordered;
-      in = (const T*)t.src + k.batch * t.src_stride[0] + (kBackward ? k.ordered : source) * t.src_stride[1] + head0 * t.src_stride[2];
-      if (kSums && t.rotate) xin = (const T*)t.x + k.batch * t.x_stride[0] + source * t.x_stride[1] + head0 * t.x_stride[2];
-    }
-    load(in_on && head0 < t.heads, t.rotate);
+    if (in_on) aim(k, ti);
+    load(in_on && head0 < p.t[ti].heads, p.t[ti].rotate);
   };
+  if constexpr (Shape::kRing) {
+    ask_next = locate(base + stride);
+    aim(ask, ask_t);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) request();
+  } else {
+    load_first(cur, t_first);
+  }
 
-  const int stride = (int)gridDim.x * tokens_per_block;
-  int base = (int)blockIdx.x * tokens_per_block;
-  Token cur = locate(base);
-  fetch_first(cur, t_first);
   __syncthreads();
-  angles(cur, s_turn[0]);
+  angles(cur, s_turn);
   __syncthreads();
+  int stage = 0;
   int buffer = 0;
   // All threads of a warp walk the same number of rows (row sums are warp-wide shuffles): a thread whose token or head
   // does not exist takes part with zeros.
   while (true) {
     const bool more = p.rows - base > stride;          // base + stride < rows
     const Token next = more ? locate(base + stride) : Token{0, 0, 0, false};
-    const float* const cs = s_turn[buffer] + token_slot * lanes * 8;
+    const float* const cs = s_turn + buffer * 2 * sines + token_slot * lanes * 8;
     const float* const sn = cs + sines;
     for (int ti = t_first; ti < t_end; ++ti) {
       const RotTensor& t = p.t[ti];
       const int heads = t.heads, hs = p.head_slots;
       const bool rotate = t.rotate != 0;
-      const long long in_step = t.src_stride[2] << p.head_slots_log2, x_step = t.x_stride[2] << p.head_slots_log2,
-                      out_step = t.dst_stride[2] << p.head_slots_log2;
+      const long long out_step = t.dst_stride[2] << p.head_slots_log2;
       const bool out_on = cur.there && on;
       T* out = (T*)t.dst + cur.batch * t.dst_stride[0] +
                (kBackward && t.tile_major ? cur.source : cur.ordered) * t.dst_stride[1] + head0 * t.dst_stride[2];
       for (int h = head0; h - head0 < heads; h += hs, out += out_step) {
         const bool row_on = out_on && h < heads;
-        const Raw<T> row = raw, xrow = xraw;
-        // the next row, while this one is worked on
-        if (h - head0 + hs < heads) {
-          in += in_step;
-          if (kSums) xin += x_step;
+        Raw<T> row, xrow;
+        if constexpr (Shape::kRing) {
+          copy_wait<kStages - 2>();                    // this row's pieces are there
+          const uint4* src = ring + stage * Shape::kPieces * kThreads;
+#pragma unroll
+          for (int i = 0; i < 2 * kVec; ++i) {
+            row.v[i] = src[i * kThreads];
+            xrow.v[i] = src[(2 * kVec + i) * kThreads];
+          }
+          if (++stage == kStages) stage = 0;
+        } else {
+          row = raw;
+          if (kSums) xrow = xraw;
+        }
+        // the next row, while this one is worked on (ring: into the stage read one row ago)
+        if constexpr (Shape::kRing) {
+          request();
+        } else if (h - head0 + hs < heads) {
+          in += t.src_stride[2] << p.head_slots_log2;
+          if (kSums) xin += t.x_stride[2] << p.head_slots_log2;
           load(in_on && h + hs < heads, rotate);
         } else if (ti + 1 < t_end) {
-          fetch_first(cur, ti + 1);
+          load_first(cur, ti + 1);
         } else {
-          fetch_first(next, t_first);
+          load_first(next, t_first);
         }
         if (!rotate) {                                 // only moved
           if (row_on) row.store(out + c_lo, out + c_hi);
@@ -480,7 +573,7 @@ tra_rotary_kernel(const __grid_constant__ RotArgs p) {
     }
     if (!more) break;
     buffer ^= 1;
-    angles(next, s_turn[buffer]);
+    angles(next, s_turn + buffer * 2 * sines);
     __syncthreads();
     base += stride;
     cur = next;
@@ -490,7 +583,7 @@ tra_rotary_kernel(const __grid_constant__ RotArgs p) {
     const RotTensor& t = p.t[t_first];
     if (t.partial == nullptr) return;
     // threads of the same lane hold the same channels: add them over the warp, then over the block's warps in order
-    float* s_red = s_turn[0];                          // [warp][d], d <= 256
+    float* s_red = reinterpret_cast<float*>(smem);     // [warp][d], d <= 256: the ring is empty now, or s_turn is done with
     const int warp = tid >> 5;
     __syncthreads();
 #pragma unroll
@@ -552,9 +645,7 @@ int log2_of(int n) {
   return l;
 }
 
-// Blocks of a launch, per tensor of a backward launch: what fits 148 SMs at once.
-constexpr int kForwardBlocksMax = 4 * 148;
-constexpr int kBackwardBlocksMax = 2 * 148;
+constexpr int kBlocksMax = 4 * 148;
 
 int elem_bytes(int dtype) { return dtype == TRA_FP32 ? 4 : 2; }
 
@@ -564,21 +655,31 @@ bool aligned_strides(const int64_t* s, int dtype) {
   return true;
 }
 
+template <typename T, int kNorm, bool kHalves, bool kBackward>
+int launch_kernel(dim3 grid, const RotArgs& a, cudaStream_t stream) {
+  using Shape = RotShape<T, kNorm, kBackward>;
+  int bytes = Shape::kRingBytes + 2 * 16 * kThreads / a.head_slots * (int)sizeof(float);
+  if (bytes < kThreads / 32 * kMaxD * (int)sizeof(float)) bytes = kThreads / 32 * kMaxD * (int)sizeof(float);      // s_red
+  const int rc = tra_allow_smem<tra_rotary_kernel<T, kNorm, kHalves, kBackward>>(Shape::kRingBytes + 2 * 16 * kThreads * (int)sizeof(float));
+  if (rc != TRA_OK) return rc;
+  tra_rotary_kernel<T, kNorm, kHalves, kBackward><<<grid, kThreads, bytes, stream>>>(a);
+  return cudaGetLastError() == cudaSuccess ? TRA_OK : TRA_ERR_CUDA;
+}
 template <typename T, int kNorm, bool kBackward>
-void launch_halves(bool halves, dim3 grid, const RotArgs& a, cudaStream_t stream) {
-  if (halves)
-    tra_rotary_kernel<T, kNorm, true, kBackward><<<grid, kThreads, 0, stream>>>(a);
-  else
-    tra_rotary_kernel<T, kNorm, false, kBackward><<<grid, kThreads, 0, stream>>>(a);
+int launch_halves(bool halves, dim3 grid, const RotArgs& a, cudaStream_t stream) {
+  return halves ? launch_kernel<T, kNorm, true, kBackward>(grid, a, stream) : launch_kernel<T, kNorm, false, kBackward>(grid, a, stream);
 }
 template <typename T, bool kBackward>
-void launch_norm(int norm, bool halves, dim3 grid, const RotArgs& a, cudaStream_t stream) {
-  if (norm == TRA_NORM_RMS)
-    launch_halves<T, TRA_NORM_RMS, kBackward>(halves, grid, a, stream);
-  else if (norm == TRA_NORM_LAYER)
-    launch_halves<T, TRA_NORM_LAYER, kBackward>(halves, grid, a, stream);
-  else
-    launch_halves<T, TRA_NORM_NONE, kBackward>(halves, grid, a, stream);
+int launch_norm(int norm, bool halves, dim3 grid, const RotArgs& a, cudaStream_t stream) {
+  return norm == TRA_NORM_RMS     ? launch_halves<T, TRA_NORM_RMS, kBackward>(halves, grid, a, stream)
+         : norm == TRA_NORM_LAYER ? launch_halves<T, TRA_NORM_LAYER, kBackward>(halves, grid, a, stream)
+                                  : launch_halves<T, TRA_NORM_NONE, kBackward>(halves, grid, a, stream);
+}
+// Blocks of a launch (per tensor, when a block works on one): what fits the SMs at once.
+template <typename T>
+int wave_of(int norm, bool backward) {
+  if (!backward) return 148 * (norm == TRA_NORM_NONE ? RotShape<T, TRA_NORM_NONE, false>::kBlocksPerSm : RotShape<T, TRA_NORM_RMS, false>::kBlocksPerSm);
+  return 148 * (norm == TRA_NORM_NONE ? RotShape<T, TRA_NORM_NONE, true>::kBlocksPerSm : RotShape<T, TRA_NORM_RMS, true>::kBlocksPerSm);
 }
 
 int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const tra_rotary_tensor_t* tensors,
@@ -633,20 +734,22 @@ int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const
       any_rotate = true;
     }
   }
-  // Heads side by side in a block: a power of two that divides the heads of every tensor (no idle threads), at most 8, so
-  // that a token's angles serve many rows.  With few tokens one block per tensor and all heads side by side, so that the
-  // launch still fills the GPU (148 SMs of 1024 threads).
+  // Heads side by side in a block.  One: a token's set-up and angles serve all its rows, and 32 tokens share a barrier
+  // (the norm's backward pass on the 32.7K-token shape: 146 us, 171 with four); the forward pass, whose groups are cheap, takes four
+  // where that divides the heads of every tensor (75.6K-token layer: 752 us, 746 with one; 32.7K without a norm: 110 and
+  // 116).  More while the launch does not fill the GPU, and then a block per tensor.
   const int slots = kThreads / lanes;
+  const int wave = dtype == TRA_FP32 ? wave_of<float>(rot->norm, backward) : wave_of<__half>(rot->norm, backward);
+  const bool sums = backward && rot->norm != TRA_NORM_NONE;
+  auto groups = [&](int h) { return (rows + slots / h - 1) / (slots / h); };
   int hs = 1;
-  while (hs < 8 && hs < slots && common % (2 * hs) == 0) hs *= 2;
-  const bool few = (long long)rows * hs * lanes < 148 * 1024;
-  if (few)
-    while (hs < slots && hs < most_heads) hs *= 2;
+  while (!sums && hs < 4 && hs < slots && common % (2 * hs) == 0) hs *= 2;
+  while (hs < slots && hs < most_heads && groups(hs) < wave) hs *= 2;
   a.head_slots = hs;
   a.head_slots_log2 = log2_of(hs);
   a.lanes_log2 = log2_of(lanes);
-  // the weights' sums of a backward launch stay in registers: one tensor per block
-  a.one_tensor = few || mixed || (backward && rot->norm != TRA_NORM_NONE);
+  // the weights' sums stay in registers: one tensor per block
+  a.one_tensor = groups(hs) < wave || mixed || sums;
   if (any_rotate && !pos && !plan) return TRA_ERR_INVALID_ARG;
   memcpy(a.turn, rot->turn, sizeof(a.turn));
   memcpy(a.axis, rot->axis, sizeof(a.axis));
@@ -664,10 +767,7 @@ int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const
   a.rows = rows;
   a.tokens = tokens;
 
-  // blocks that stay: one wave of the four (backward with a norm: two) that fit an SM
-  const int tokens_per_block = kThreads / lanes / hs;
-  const int wave = backward && rot->norm != TRA_NORM_NONE ? kBackwardBlocksMax : kForwardBlocksMax;
-  int blocks = (rows + tokens_per_block - 1) / tokens_per_block;
+  int blocks = groups(hs);             // blocks that stay: one wave
   if (blocks > wave) blocks = wave;
   ReduceArgs red;
   memset(&red, 0, sizeof(red));
@@ -693,17 +793,13 @@ int run(const tra_rotary* rot, const tra_plan_t* plan, const int32_t* pos, const
   }
   const dim3 grid((unsigned)blocks, a.one_tensor ? (unsigned)n_tensors : 1u);
   const bool halves = rot->halves != 0;
-  if (dtype == TRA_BF16) {
-    backward ? launch_norm<__nv_bfloat16, true>(rot->norm, halves, grid, a, stream)
-             : launch_norm<__nv_bfloat16, false>(rot->norm, halves, grid, a, stream);
-  } else if (dtype == TRA_FP16) {
-    backward ? launch_norm<__half, true>(rot->norm, halves, grid, a, stream)
-             : launch_norm<__half, false>(rot->norm, halves, grid, a, stream);
-  } else {
-    backward ? launch_norm<float, true>(rot->norm, halves, grid, a, stream)
-             : launch_norm<float, false>(rot->norm, halves, grid, a, stream);
-  }
-  TRA_CUDA_CHECK(cudaGetLastError());
+  const int rc = dtype == TRA_BF16   ? (backward ? launch_norm<__nv_bfloat16, true>(rot->norm, halves, grid, a, stream)
+                                                 : launch_norm<__nv_bfloat16, false>(rot->norm, halves, grid, a, stream))
+                 : dtype == TRA_FP16 ? (backward ? launch_norm<__half, true>(rot->norm, halves, grid, a, stream)
+                                                 : launch_norm<__half, false>(rot->norm, halves, grid, a, stream))
+                                     : (backward ? launch_norm<float, true>(rot->norm, halves, grid, a, stream)
+                                                 : launch_norm<float, false>(rot->norm, halves, grid, a, stream));
+  if (rc != TRA_OK) return rc;
   if (n_red) {
     tra_rotary_reduce_kernel<<<dim3((rot->head_dim + kReduceCols - 1) / kReduceCols, n_red), kReduceRows * kReduceCols, 0,
                                stream>>>(red);
@@ -750,7 +846,7 @@ extern "C" int tra_rotary_destroy(tra_rotary_t* rot) {
 }
 
 extern "C" size_t tra_rotary_backward_workspace_bytes(const tra_rotary_t* rot) {
-  return rot ? sizeof(float) * 3 * 2 * (size_t)kBackwardBlocksMax * rot->head_dim : 0;
+  return rot ? sizeof(float) * 3 * 2 * (size_t)kBlocksMax * rot->head_dim : 0;
 }
 
 extern "C" int tra_rotary_forward(const tra_rotary_t* rot, const tra_plan_t* plan, const int32_t* pos,
