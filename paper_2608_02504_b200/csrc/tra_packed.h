@@ -84,67 +84,49 @@ __device__ __forceinline__ tra_seq_range tra_clamp_range(int begin, int end, int
   return {b, len};
 }
 
-// What a thread block works on: unit `index` of a sequence and the sequence's token ranges.
+// What a thread block works on: unit `index` of a sequence, of its `count`, and the sequence's token ranges.
 struct tra_unit {
-  int seq, index;          // seq = -1: nothing
+  int seq, index, count;   // seq = -1: nothing
   tra_seq_range q, k;
 };
 
-// A lane's share of 32 sequences: their ranges, and the units before and in them.
-struct tra_seq_cache {
-  int s0 = -1, before = 0, total = 0, excl = 0, n = 0;
-  tra_seq_range q = {0, 0}, k = {0, 0};
-};
-
-// Finds a unit, units numbered sequence by sequence, ceil(length / unit_tokens) each, length in queries or
-// (by_keys) in keys; one_each: unit s is the whole of sequence s.  One warp calls it; every lane gets the result.  32 sequences are
-// read at a time, the ranges of both sides with them, and kept for the next call.
-__device__ __forceinline__ tra_unit tra_find_unit(const tra_packed_launch& p, bool by_keys, bool one_each, int unit_tokens, int unit,
-                                                  tra_seq_cache& c) {
+// Finds a unit: `unit_tokens` consecutive queries, or (by_keys) keys, of a sequence.  The units of sequence s are numbered from
+// first(s) = floor(begin(s) / unit_tokens) + s on, which leaves room for all of them (some numbers mean nothing), and makes the
+// sequence of a number a search in the ascending bounds, 32 at a time.  one_each: unit s is the whole of sequence s.
+// One warp calls it; every lane gets the result.
+__device__ __forceinline__ tra_unit tra_find_unit(const tra_packed_launch& p, bool by_keys, bool one_each, int unit_tokens, int unit) {
   const int lane = threadIdx.x & 31;
-  tra_unit u = {-1, 0, {0, 0}, {0, 0}};
+  tra_unit u = {-1, 0, 1, {0, 0}, {0, 0}};
   if (one_each) {
-    u.seq = unit;
     u.q = tra_clamp_range(p.cu_q[unit], p.cu_q[unit + 1], p.total_q, p.max_q, p.status);
     u.k = tra_clamp_range(p.k_begin[unit], p.k_end[unit], p.total_k, p.max_k, p.status);
+    if ((by_keys ? u.k.len : u.q.len) > 0) u.seq = unit;
     return u;
   }
-  if (c.s0 < 0 || unit < c.before) {         // nothing read yet, or the unit lies in front of what was
-    c.s0 = -32;
-    c.before = c.total = 0;
-  }
-  while (unit >= c.before + c.total) {
-    c.s0 += 32;
-    c.before += c.total;
-    if (c.s0 >= p.n_seq) {
-      c.s0 = -1;
+  int lo = 0, hi = p.n_seq;
+  while (true) {
+    const int stride = (hi - lo + 31) / 32;
+    const int s = lo + lane * stride;
+    int first = 0, q0 = 0, q1 = 0, k0 = 0, k1 = 0;
+    if (s < hi) {
+      if (stride == 1) q0 = p.cu_q[s], q1 = p.cu_q[s + 1], k0 = p.k_begin[s], k1 = p.k_end[s];
+      const int begin = stride == 1 ? (by_keys ? k0 : q0) : (by_keys ? p.k_begin[s] : p.cu_q[s]);
+      first = min(max(begin, 0), by_keys ? p.total_k : p.total_q) / unit_tokens + s;
+    }
+    const unsigned hits = __ballot_sync(0xffffffffu, s < hi && first <= unit);
+    if (!hits) return u;                       // in front of the first sequence
+    const int l = 31 - __clz(hits);
+    if (stride == 1) {
+      u.q = tra_clamp_range(__shfl_sync(0xffffffffu, q0, l), __shfl_sync(0xffffffffu, q1, l), p.total_q, p.max_q, p.status);
+      u.k = tra_clamp_range(__shfl_sync(0xffffffffu, k0, l), __shfl_sync(0xffffffffu, k1, l), p.total_k, p.max_k, p.status);
+      u.index = unit - __shfl_sync(0xffffffffu, first, l);
+      u.count = ((by_keys ? u.k.len : u.q.len) + unit_tokens - 1) / unit_tokens;
+      if (u.index < u.count) u.seq = lo + l;
       return u;
     }
-    c.q = c.k = {0, 0};
-    if (c.s0 + lane < p.n_seq) {
-      const int s = c.s0 + lane, q0 = p.cu_q[s], q1 = p.cu_q[s + 1], k0 = p.k_begin[s], k1 = p.k_end[s];
-      c.q = tra_clamp_range(q0, q1, p.total_q, p.max_q, p.status);
-      c.k = tra_clamp_range(k0, k1, p.total_k, p.max_k, p.status);
-    }
-    c.n = ((by_keys ? c.k.len : c.q.len) + unit_tokens - 1) / unit_tokens;
-    int incl = c.n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += up;
-    }
-    c.excl = incl - c.n;
-    c.total = __shfl_sync(0xffffffffu, incl, 31);
+    hi = min(lo + (l + 1) * stride, hi);
+    lo += l * stride;
   }
-  const int at = unit - c.before;
-  const int l = __ffs(__ballot_sync(0xffffffffu, at >= c.excl && at < c.excl + c.n)) - 1;
-  u.seq = c.s0 + l;
-  u.index = at - __shfl_sync(0xffffffffu, c.excl, l);
-  u.q.begin = __shfl_sync(0xffffffffu, c.q.begin, l);
-  u.q.len = __shfl_sync(0xffffffffu, c.q.len, l);
-  u.k.begin = __shfl_sync(0xffffffffu, c.k.begin, l);
-  u.k.len = __shfl_sync(0xffffffffu, c.k.len, l);
-  return u;
 }
 
 }  // namespace

@@ -209,8 +209,7 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
 
   // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    tra_seq_cache seqs;
-    const tra_unit u = tra_find_unit(p, true, p.max_k <= kTileM, kTileM, unit, seqs);
+    const tra_unit u = tra_find_unit(p, true, p.max_k <= kTileM, kTileM, unit);
     if (lane == 0) ctl->unit = u;
   } else if (warp == 9) {
     tmem_alloc_all(&ctl->tmem_base);
@@ -231,7 +230,7 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
   const uint32_t tmem = ctl->tmem_base;
   const tra_seq_range qr = ctl->unit.q, kr = ctl->unit.k;
   const int key0 = ctl->unit.index * kTileM;
-  if (ctl->unit.seq < 0 || key0 >= kr.len) {
+  if (ctl->unit.seq < 0) {
     if (warp == 9) tmem_free_all(tmem);
     wait_last_launch();          // no block ends before the launch in front of it
     return;
@@ -514,8 +513,7 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
 
   // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    tra_seq_cache seqs;
-    const tra_unit u = tra_find_unit(p, false, p.max_q <= tile_tokens, tile_tokens, unit, seqs);
+    const tra_unit u = tra_find_unit(p, false, p.max_q <= tile_tokens, tile_tokens, unit);
     if (lane == 0) ctl->unit = u;
   } else if (warp == 9) {
     tmem_alloc_all(&ctl->tmem_base);
@@ -535,8 +533,9 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
   tc_fence_after();
   const uint32_t tmem = ctl->tmem_base;
   const tra_seq_range qr = ctl->unit.q, kr = ctl->unit.k;
-  const int tok0 = ctl->unit.index * tile_tokens;
-  if (ctl->unit.seq < 0 || tok0 >= qr.len) {
+  // the last tiles, the longest of a causal sequence, come first
+  const int tok0 = (ctl->unit.count - 1 - ctl->unit.index) * tile_tokens;
+  if (ctl->unit.seq < 0) {
     if (warp == 9) tmem_free_all(tmem);
     wait_last_launch();          // no block ends before the launch in front of it
     return;
@@ -724,7 +723,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_bwd_kernel(const __
   if (b < n_dkv)
     dkv_block<T, D, kCausal>(p, smem, b % dkv_units, b / dkv_units);
   else
-    dq_block<T, D, kCausal>(p, smem, dq_units - 1 - (b - n_dkv) % dq_units, (b - n_dkv) / dq_units);
+    dq_block<T, D, kCausal>(p, smem, (b - n_dkv) % dq_units, (b - n_dkv) / dq_units);
 }
 
 // ------------------------------------------------------------------------------------ delta

@@ -219,12 +219,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFwdRegsControl));
     if (warp == 11) {
       // ================================================================== scheduler
-      // The grid has a block per unit, in launch order: within a key/value head the last tiles come first, which of a causal
-      // sequence are the longest.  A running block takes over blocks that have not been started yet, one at a time (cluster
+      // The grid has a block per unit, in launch order: a sequence's last tiles come first, which are the longest of a causal one.  A running block takes over blocks that have not been started yet, one at a time (cluster
       // launch control), and so balances units of different lengths without a counter in memory.
       // The request is made when the producer is about to run out of loads: units taken over early are units that an idle block
       // cannot have.
-      tra_seq_cache seqs;
       int n = 0, unit = blockIdx.x;
       uint32_t asked = 0;
       bool alive = true, more = true;
@@ -233,8 +231,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         FwdWork w;
         w.split = unit - j * p.splits;
         w.kvh = j / p.n_units;
-        w.unit = tra_find_unit(p, false, p.max_q <= 2 * p.tile_tokens, 2 * p.tile_tokens, p.n_units - 1 - (j - w.kvh * p.n_units), seqs);
-        if (w.unit.seq >= 0 && w.unit.index * 2 * p.tile_tokens < w.unit.q.len) {      // there is something to do
+        w.unit = tra_find_unit(p, false, p.max_q <= 2 * p.tile_tokens, 2 * p.tile_tokens, j - w.kvh * p.n_units);
+        w.unit.index = w.unit.count - 1 - w.unit.index;
+        if (w.unit.seq >= 0) {                                // there is something to do
           if (n >= 2) alive = mbar_wait_warp(smem_u32(&ctl->work_free[n & 1]), (uint32_t)((n >> 1) - 1) & 1u, abort_flag, p.status);
           if (!alive) break;
           if (lane == 0) {

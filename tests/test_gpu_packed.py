@@ -223,3 +223,50 @@ def test_prefill_then_tokens_match_the_whole_prompt(api):
         at += step
     check(whole, want["o"], want["o_tol"], "o")
     attn.check_status()
+
+
+def test_binding_refusals(api):
+    d, n = 64, 40
+    attn = api.PackedAttn(4, 2, d, causal=True)
+    q, k, v = randn((n, 4, d), BF, 1), randn((n, 2, d), BF, 2), randn((n, 2, d), BF, 3)
+    cu = i32([0, n])
+    kw = dict(max_q=n, max_k=n)
+    bad = [
+        lambda: attn.forward(q.half(), k, v, cu, **kw), lambda: attn.forward(q.cpu(), k, v, cu, **kw),
+        lambda: attn.forward(q, k, v[:-1], cu, **kw), lambda: attn.forward(k, k, v, cu, **kw),
+        lambda: attn.forward(q[..., ::2], k, v, cu, **kw), lambda: attn.forward(q, k, v, cu.long(), **kw),
+        lambda: attn.forward(q, k, v, cu[:1], **kw), lambda: attn.forward(q, k, v, cu, cu[:1], **kw),
+        lambda: attn.forward(q, k, v, cu, cu, k_range=(cu[:1], cu[1:]), **kw),
+        lambda: attn.forward(q, k, v, cu, lse=torch.empty(n, 4, device="cuda", dtype=torch.float64), **kw),
+        lambda: attn.forward(q[0], k, v, cu, **kw), lambda: api.PackedAttn(4, 2, d, dtype=torch.float32),
+    ]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: attn.forward(q, k, v, cu, max_q=n + 1, max_k=n), lambda: attn.forward(q, k, v, cu, max_q=n, max_k=n + 1),
+                 lambda: attn.forward(q, k, v, cu, sm_scale=0.0, **kw), lambda: api.PackedAttn(4, 3, d), lambda: api.PackedAttn(4, 2, 80),
+                 lambda: attn.forward(q, k[:, :1].expand(n, 2, d), v, cu, **kw)):      # a stride of zero
+        with pytest.raises(api.TraError):
+            call()
+    o, lse = attn.forward(q, k, v, cu, want_lse=True, **kw)
+    with pytest.raises(ValueError):
+        attn.backward(q, q, k, v, o, None, cu, **kw)
+    with pytest.raises(ValueError):
+        attn.backward(q[:-1], q, k, v, o, lse, cu, **kw)
+    attn.check_status()
+    torch.cuda.synchronize()
+
+
+def test_many_sequences(api):
+    """More sequences than one search step reads, long ones among short and empty ones; keys shared by two sequences."""
+    lens = [(7 * i) % 5 for i in range(1100)]
+    lens[3], lens[600], lens[1099] = 700, 301, 260
+    run(api, BF, 64, 2, 1, True, lens)
+    lens = [0] * 40 + [300] + [0] * 33 + [1]
+    run(api, HALF, 64, 1, 1, False, lens)
+    d, n, m = 64, 90, 500
+    attn = api.PackedAttn(2, 2, d, causal=True)
+    q, k, v = randn((2 * n, 2, d), BF, 1), randn((m, 2, d), BF, 2), randn((m, 2, d), BF, 3)
+    o, _ = attn.forward(q, k, v, i32([0, n, 2 * n]), k_range=(i32([0, 0]), i32([m, m - 77])), max_q=n, max_k=m)
+    want = reference(q, k, v, [0, n, 2 * n], [0, 0], [m, m - 77], True, d ** -0.5)
+    check(o, want["o"], want["o_tol"], "o")

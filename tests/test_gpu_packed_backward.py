@@ -73,6 +73,12 @@ def test_more_or_fewer_keys_than_queries(api, causal, dtype, d):
     run(api, dtype, d, 2, 2, causal, [0], [150])
 
 
+def test_many_sequences(api):
+    lens = [(7 * i) % 4 for i in range(1050)]
+    lens[2], lens[700] = 400, 130
+    run(api, BF, 64, 2, 1, True, lens)
+
+
 def test_scales(api):
     run(api, BF, 128, 2, 2, True, [200], sm_scale=0.5)
     run(api, HALF, 64, 2, 2, False, [300], sm_scale=1e-4)
@@ -210,5 +216,5 @@ def test_layer_around_it(api):
     # every stage rounds to fp16 (2^-11): q, k (scores of up to about 5 move by their sum), P, dS, dq, dk, dx: below 32
     # roundings of the size of the result, in the relative norm
     for name, got, want in (("o", o, out), ("dx", dfused, gx), ("wq", wg["q_weight"], gq), ("wk", wg["k_weight"], gk)):
-        rel = float((got.double() - want).norm() / want.norm())
+        rel = float(((got.double() - want).norm() / want.norm()).detach())
         assert rel <= 32 * 2.0 ** -11, (name, rel)
