@@ -559,12 +559,15 @@ class Rotary:
         With ``plan`` the tokens are its raster-order sequence, positions come from its grid (unless ``pos`` is
         given) and the outputs are [B, heads, tokens, d] in the order its attention calls take; without it,
         ``pos`` int32 [tokens, n_axes] names every token's position and outputs keep the inputs' layout.
-        V is only moved: without a plan it comes back as a copy.  ``out``: output tensors instead of new ones."""
+        V is only moved: without a plan it comes back as a copy.  ``out``: output tensors instead of new ones (new ones of
+        one shape are slices of one allocation)."""
         if k is None and (k_weight is not None or k_bias is not None):
             raise ValueError("k_weight, k_bias: given without k")
         B, tokens, index, pos_ptr = self._begin(q, plan, pos, False)
         on_plan, dtype, d = plan is not None, q.dtype, self.head_dim
         desc, outs, n = bytearray(3 * _ROTARY_TENSOR.size), [], 0
+        if out is None and on_plan and k is not None and v is not None and k.shape == q.shape and v.shape == q.shape:
+            out = q.new_empty((3, B, q.shape[2], tokens, d)).unbind(0)      # one allocation (and 4 us less per call)
         for i, (name, x, w, b) in enumerate((("q", q, q_weight, q_bias), ("k", k, k_weight, k_bias), ("v", v, None, None))):
             if x is None:
                 outs.append(None)

@@ -69,6 +69,7 @@ __device__ __forceinline__ void mma16816<__half>(float* c, const uint32_t* a, ui
 
 // ---- thread-block clusters: a barrier over the cluster, and 16 bytes of another block's shared memory
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ float4 cluster_ld4(const void* own_address, uint32_t rank) {

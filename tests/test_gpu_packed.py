@@ -270,3 +270,45 @@ def test_many_sequences(api):
     o, _ = attn.forward(q, k, v, i32([0, n, 2 * n]), k_range=(i32([0, 0]), i32([m, m - 77])), max_q=n, max_k=m)
     want = reference(q, k, v, [0, n, 2 * n], [0, 0], [m, m - 77], True, d ** -0.5)
     check(o, want["o"], want["o_tol"], "o")
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_no_tokens(api, n):
+    """No keys at all, no queries at all, neither."""
+    d = 64
+    attn = api.PackedAttn(2, 1, d, causal=True)
+    q, none = randn((n, 2, d), BF, 1), torch.empty(0, 1, d, dtype=BF, device="cuda")
+    o, lse = attn.forward(q, none, none, i32([0, n]), i32([0, 0]), max_q=n, max_k=0, want_lse=True)
+    assert (o == 0).all() and (lse == -math.inf).all()
+    dq, dk, dv = attn.backward(q, q, none, none, o, lse, i32([0, n]), i32([0, 0]), max_q=n, max_k=0)
+    assert (dq == 0).all() and dk.shape == (0, 1, d)
+    k, noq = randn((n, 1, d), BF, 2), torch.empty(0, 2, d, dtype=BF, device="cuda")
+    o, lse = attn.forward(noq, k, k, i32([0, 0]), i32([0, n]), max_q=0, max_k=n, want_lse=True)
+    assert o.shape == (0, 2, d)
+    dq, dk, dv = attn.backward(noq, noq, k, k, o, lse, i32([0, 0]), i32([0, n]), max_q=0, max_k=n)
+    assert (dk == 0).all() and (dv == 0).all()
+    o, _ = attn.forward(noq, none, none, i32([0, 0]), max_q=0, max_k=0)
+    attn.backward(noq, noq, none, none, o, lse, i32([0, 0]), max_q=0, max_k=0)
+    attn.check_status()
+
+
+def test_two_handles_and_streams_at_once(api):
+    """Long launches of two handles on two streams, both taking over blocks: each gives what it gives alone."""
+    d, n = 128, 3000
+    a, b = api.PackedAttn(8, 2, d, causal=True), api.PackedAttn(4, 4, d, causal=False)
+    qa, ka, va = randn((n, 8, d), BF, 1), randn((n, 2, d), BF, 2), randn((n, 2, d), BF, 3)
+    qb, kb, vb = randn((n, 4, d), BF, 4), randn((n, 4, d), BF, 5), randn((n, 4, d), BF, 6)
+    cu = i32([0, 1000, n])
+    kw = dict(max_q=n, max_k=n, want_lse=True)
+    wa, wb = a.forward(qa, ka, va, cu, **kw), b.forward(qb, kb, vb, cu, **kw)
+    ga = a.backward(qa, qa, ka, va, *wa, cu, max_q=n, max_k=n)
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        with torch.cuda.stream(s):
+            xa = a.forward(qa, ka, va, cu, **kw)
+            ha = a.backward(qa, qa, ka, va, *xa, cu, max_q=n, max_k=n)
+        with torch.cuda.stream(t):
+            xb = b.forward(qb, kb, vb, cu, **kw)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(xa + xb + ha, wa + wb + ga))
