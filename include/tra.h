@@ -389,6 +389,10 @@ typedef struct {
   int n_seq, total_q, total_k;
   int max_q, max_k;       /* upper bounds of the sequences' queries and keys                      */
   float sm_scale;
+  void* o_rest;           /* what rounding took from o, in o's type, [total_q, heads, d] contiguous, 16-byte aligned,   */
+                          /* or NULL.  Forward, with lse only: written.  Backward: read; the sums of dO O are then those */
+                          /* of the unrounded o, without which the gradients of a short or peaked row are mostly the     */
+                          /* rounding of o                                                                             */
 } tra_packed_args_t;
 
 /* Creates the handle on the current device (allocates its status word). */

@@ -81,7 +81,8 @@ class tra_packed_args_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "o", "lse")] + \
         [(n, ctypes.c_int64 * 2) for n in ("q_stride", "k_stride", "v_stride", "o_stride")] + \
         [(n, ctypes.c_void_p) for n in ("cu_q", "k_begin", "k_end")] + \
-        [(n, ctypes.c_int) for n in ("n_seq", "total_q", "total_k", "max_q", "max_k")] + [("sm_scale", ctypes.c_float)]
+        [(n, ctypes.c_int) for n in ("n_seq", "total_q", "total_k", "max_q", "max_k")] + [("sm_scale", ctypes.c_float)] + \
+        [("o_rest", ctypes.c_void_p)]
 
 
 class tra_packed_grads_t(ctypes.Structure):
@@ -437,7 +438,7 @@ _DTYPES = {torch.bfloat16: TRA_BF16, torch.float16: TRA_FP16, torch.float32: TRA
 # The calls below are made for every layer and token, on a few microseconds of kernel: descriptors are packed by one
 # struct call each (the layouts of tra_rotary_tensor_t, tra_packed_args_t and tra_packed_grads_t), devices are compared by index.
 _ROTARY_TENSOR = struct.Struct("7Q9qiI")
-_PACKED_ARGS = struct.Struct("5Q8q3Q5if")
+_PACKED_ARGS = struct.Struct("5Q8q3Q5ifQ")
 _PACKED_GRADS = struct.Struct("4Q8q")
 assert (_ROTARY_TENSOR.size, _PACKED_ARGS.size, _PACKED_GRADS.size) == tuple(
     ctypes.sizeof(t) for t in (tra_rotary_tensor_t, tra_packed_args_t, tra_packed_grads_t))
@@ -692,7 +693,7 @@ class PackedAttn:
             raise ValueError(f"{name}: expected a contiguous int32 tensor of {n} entries on {self.device}")
         return t.data_ptr()
 
-    def _args(self, q, k, v, o, lse, cu_q, cu_k, k_range, max_q, max_k, sm_scale):
+    def _args(self, q, k, v, o, lse, rest, cu_q, cu_k, k_range, max_q, max_k, sm_scale):
         if q.dim() != 3 or k.dim() != 3 or cu_q.dim() != 1 or cu_q.shape[0] < 2:
             raise ValueError("expected q, k, v [tokens, heads, head_dim] and cu_q [n_seq + 1]")
         if torch.cuda.current_device() != self._index:
@@ -717,19 +718,30 @@ class PackedAttn:
             begin = cq if cu_k is None else self._ints(cu_k, "cu_k", n + 1)
             end = begin + 4
         return _PACKED_ARGS.pack(qp, kp, vp, op, lp, q0, q1, k0, k1, v0, v1, o0, o1, cq, begin, end, n, tq, tk, max_q, max_k,
-                                 self.head_dim ** -0.5 if sm_scale is None else sm_scale)
+                                 self.head_dim ** -0.5 if sm_scale is None else sm_scale, 0 if rest is None else rest.data_ptr())
+
+    @staticmethod
+    def _rest(lse, q):
+        """What rounding took from o, kept beside an lse that ``forward`` made (``lse.o_rest``), for the gradients."""
+        rest = getattr(lse, "o_rest", None)
+        if rest is not None and (rest.shape != q.shape or rest.dtype != q.dtype or rest.device != q.device or
+                                 not rest.is_contiguous()):
+            raise ValueError("lse.o_rest: does not belong to this q")
+        return rest
 
     def forward(self, q, k, v, cu_q, cu_k=None, *, k_range=None, max_q, max_k, o=None, lse=None, want_lse=False,
                 sm_scale=None):
         """-> (o, lse).  Keys: packed like the queries (``cu_k``, default ``cu_q``), or ``k_range`` = (begin, end), two
         int32 [n_seq] tensors, e.g. the filled parts of a cache's slots.  ``max_q``, ``max_k``: upper bounds of the
         sequences' queries and keys (a longer one is cut and reported by ``check_status``).  Rows of o and lse that
-        belong to no sequence are not written."""
+        belong to no sequence are not written.  An lse made here (``want_lse``) also keeps what rounding took from o, as
+        ``lse.o_rest``, a tensor like o that ``backward`` uses when it is there; drop it where no gradient is needed."""
         if o is None:
             o = _empty_like(q)
         if lse is None and want_lse:
             lse = q.new_empty((q.shape[0], self.heads), dtype=torch.float32)
-        a = self._args(q, k, v, o, lse, cu_q, cu_k, k_range, max_q, max_k, sm_scale)
+            lse.o_rest = _empty_like(q)
+        a = self._args(q, k, v, o, lse, self._rest(lse, q), cu_q, cu_k, k_range, max_q, max_k, sm_scale)
         n = _lib.tra_packed_attn_workspace_bytes(self._h, cu_q.shape[0] - 1, q.shape[0], max_q, max_k)
         ws = q.new_empty((n,), dtype=torch.uint8) if n else None
         _check(_lib.tra_packed_attn(self._h, a, ws.data_ptr() if n else None, n, _raw_stream(self._index)), "tra_packed_attn")
@@ -743,7 +755,7 @@ class PackedAttn:
         dv = _empty_like(v) if dv is None else dv
         if lse is None:
             raise ValueError("lse: the forward call's, made with want_lse")
-        a = self._args(q, k, v, o, lse, cu_q, cu_k, None, max_q, max_k, sm_scale)
+        a = self._args(q, k, v, o, lse, self._rest(lse, q), cu_q, cu_k, None, max_q, max_k, sm_scale)
         tq, tk = q.shape[0], k.shape[0]
         ptrs, strides = zip(*((p, s) for p, *s in (self._tensor(do, "do", tq, self.heads), self._tensor(dq, "dq", tq, self.heads),
                                                    self._tensor(dk, "dk", tk, self.kv_heads), self._tensor(dv, "dv", tk, self.kv_heads))))

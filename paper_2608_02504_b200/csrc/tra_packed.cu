@@ -95,10 +95,20 @@ __global__ void __launch_bounds__(128) tra_packed_join_kernel(const __grid_const
     }
   }
   if (kWarps == 1 || warp == 0) {
-    if constexpr (kPer == 4)
-      reinterpret_cast<uint2*>(dst)[lane] = make_uint2(pack_pair<T>(o[0] * inv, o[1] * inv), pack_pair<T>(o[2] * inv, o[3] * inv));
-    else
-      reinterpret_cast<uint32_t*>(dst)[lane] = pack_pair<T>(o[0] * inv, o[1] * inv);
+    uint32_t y[kPer / 2], rest[kPer / 2];
+#pragma unroll
+    for (int i = 0; i < kPer / 2; ++i) {
+      y[i] = pack_pair<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
+      rest[i] = rest_pair<T>(o[2 * i] * inv, o[2 * i + 1] * inv, y[i]);
+    }
+    T* dst_rest = p.o_rest ? (T*)p.o_rest + row * D : nullptr;
+    if constexpr (kPer == 4) {
+      reinterpret_cast<uint2*>(dst)[lane] = make_uint2(y[0], y[1]);
+      if (dst_rest) reinterpret_cast<uint2*>(dst_rest)[lane] = make_uint2(rest[0], rest[1]);
+    } else {
+      reinterpret_cast<uint32_t*>(dst)[lane] = y[0];
+      if (dst_rest) reinterpret_cast<uint32_t*>(dst_rest)[lane] = rest[0];
+    }
   }
   if (p.lse && (kWarps == 1 || warp == kWarps - 1)) {
     float total = 0.f;
@@ -199,6 +209,7 @@ int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_lau
     return TRA_ERR_INVALID_ARG;
   if (!a->cu_q || !a->k_begin || !a->k_end || !(a->sm_scale > 0.f) || a->sm_scale > 1e30f) return TRA_ERR_INVALID_ARG;
   if (((uintptr_t)a->cu_q | (uintptr_t)a->k_begin | (uintptr_t)a->k_end | (uintptr_t)a->lse) & 3) return TRA_ERR_INVALID_ARG;
+  if (((uintptr_t)a->o_rest & 15) || (a->o_rest && !a->lse)) return TRA_ERR_INVALID_ARG;
   if (a->total_q > (1 << 30) || a->total_k > (1 << 30)) return TRA_ERR_UNSUPPORTED;
   const int heads = h->cfg.heads, kv = h->cfg.kv_heads;
   if (bad_tensor(a->q, a->q_stride, a->total_q, heads) || bad_tensor(a->o, a->o_stride, a->total_q, heads) ||
@@ -210,6 +221,7 @@ int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_lau
   memset(p, 0, sizeof(*p));
   p->q = a->q, p->k = a->k, p->v = a->v;
   p->lse = a->lse;
+  p->o_rest = a->o_rest;
   for (int i = 0; i < 2; ++i) {
     p->q_stride[i] = a->q_stride[i];
     p->k_stride[i] = a->k_stride[i];

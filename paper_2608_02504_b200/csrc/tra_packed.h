@@ -21,6 +21,7 @@ struct tra_packed_launch {
   const void *q, *k, *v, *o_in, *d_o;
   void *o, *dq, *dk, *dv;
   float* lse;                  // forward: written or NULL; backward: read
+  void* o_rest;                // [total_q][heads][d] o minus its rounding, or NULL; forward: written (with lse); backward: read
   float* part_o;               // forward, split over the keys: [splits][total_q][heads][d]
   float* part_lse2;            //   [splits][total_q][heads] base-2 log of the sum the part was divided by
   float* part_exact;           //   [splits][total_q][heads] base-2 log of the unrounded sum (lse asked for) or NULL

@@ -727,7 +727,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_bwd_kernel(const __
 }
 
 // ------------------------------------------------------------------------------------ delta
-// delta = sum over the channels of dO O, d / 8 threads per (token, head), 16 bytes each.
+// delta = sum over the channels of dO O, d / 8 threads per (token, head), 16 bytes each.  O with what its rounding took, when the
+// forward call kept it: P (dP - delta) cancels where a row sees few keys or one dominates, and there the rounding of O is
+// the larger part of what is left (two tokens, bf16: 9.4e-3 of a gradient, 3.3e-3 with the remainder).
 template <typename T, int D>
 __global__ void __launch_bounds__(256) tra_packed_delta_kernel(const __grid_constant__ tra_packed_launch p) {
   constexpr int kLanes = D / 8;
@@ -741,12 +743,16 @@ __global__ void __launch_bounds__(256) tra_packed_delta_kernel(const __grid_cons
     const int head = (int)(row - tok * p.heads);
     const uint4 a = *reinterpret_cast<const uint4*>((const T*)p.o_in + tok * p.o_stride[0] + head * p.o_stride[1] + lane * 8);
     const uint4 b = *reinterpret_cast<const uint4*>((const T*)p.d_o + tok * p.do_stride[0] + head * p.do_stride[1] + lane * 8);
-    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    const uint4 c = p.o_rest ? *reinterpret_cast<const uint4*>((const T*)p.o_rest + row * D + lane * 8) : make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w}, z[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float x0, x1, y0, y1;
+      float x0, x1, y0, y1, z0, z1;
       unpack_pair<T>(x[i], x0, x1);
       unpack_pair<T>(y[i], y0, y1);
+      unpack_pair<T>(z[i], z0, z1);
+      x0 += z0;
+      x1 += z1;
       s = fmaf(x0, y0, s);
       s = fmaf(x1, y1, s);
     }

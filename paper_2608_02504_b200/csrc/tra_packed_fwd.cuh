@@ -119,6 +119,7 @@ __device__ __forceinline__ void store_unit(const tra_packed_launch& p, FwdCtl* c
   const RowAddresses rows(!row_valid ? nullptr
                           : parts ? (void*)(p.part_o + part_row * D)
                                   : (void*)((T*)p.o + tok_g * p.o_stride[0] + head * p.o_stride[1]));
+  const RowAddresses rests(kExact && p.o_rest && row_valid && !parts ? (void*)((T*)p.o_rest + row_g * D) : nullptr);
 #pragma unroll 1
   for (int c = 0; c < D / 32; ++c) {
     uint32_t o[32];
@@ -139,9 +140,15 @@ __device__ __forceinline__ void store_unit(const tra_packed_launch& p, FwdCtl* c
       rows.store64(o, c * 128);
       rows.store64(o + 16, c * 128 + 64);
     } else {
+      uint32_t y[16];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) o[j] = pack_pair<T>(__uint_as_float(o[2 * j]), __uint_as_float(o[2 * j + 1]));
-      rows.store64(o, c * 64);
+      for (int j = 0; j < 16; ++j) {
+        const float a = __uint_as_float(o[2 * j]), b = __uint_as_float(o[2 * j + 1]);
+        y[j] = pack_pair<T>(a, b);
+        if (kExact) o[j] = rest_pair<T>(a, b, y[j]);
+      }
+      rows.store64(y, c * 64);
+      if (kExact && p.o_rest) rests.store64(o, c * 64);
     }
   }
   if (row_valid) {

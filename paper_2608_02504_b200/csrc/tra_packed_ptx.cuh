@@ -60,6 +60,14 @@ __device__ __forceinline__ void unpack_pair<__half>(uint32_t packed, float& lo, 
   lo = f.x;
   hi = f.y;
 }
+// what rounding to the pair took from two values, rounded itself
+template <typename T>
+__device__ __forceinline__ uint32_t rest_pair(float lo, float hi, uint32_t packed) {
+  float a, b;
+  unpack_pair<T>(packed, a, b);
+  return pack_pair<T>(lo - a, hi - b);
+}
+
 
 __device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
   uint64_t d;

@@ -328,7 +328,11 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
       }
     } else {
       T* dst = (T*)p.o + tok * p.o_stride[0] + row_head(r) * p.o_stride[1] + c;
-      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_pair<T>(acc.x * inv, acc.y * inv), pack_pair<T>(acc.z * inv, acc.w * inv));
+      const float y[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+      const uint2 packed = make_uint2(pack_pair<T>(y[0], y[1]), pack_pair<T>(y[2], y[3]));
+      *reinterpret_cast<uint2*>(dst) = packed;
+      if (p.o_rest)
+        *reinterpret_cast<uint2*>((T*)p.o_rest + row * D + c) = make_uint2(rest_pair<T>(y[0], y[1], packed.x), rest_pair<T>(y[2], y[3], packed.y));
       if (c == 0 && p.lse) p.lse[row] = se != 0.f ? (ref + log2f(se)) * kLn2 : -INFINITY;
     }
   };

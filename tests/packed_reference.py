@@ -23,9 +23,11 @@ def sequences(cu_q, k_begin, k_end):
         yield s, cu_q[s], cu_q[s + 1], k_begin[s], k_end[s]
 
 
-def reference(q, k, v, cu_q, k_begin, k_end, causal, scale, do=None):
+def reference(q, k, v, cu_q, k_begin, k_end, causal, scale, do=None, o_rest=False):
     """All tensors in fp64 on their device; returns a dict of fp64 results and tolerances (rows outside the sequences
-    are zero with tolerance zero).  Lists on the host."""
+    are zero with tolerance zero).  Lists on the host.  o_rest: delta is formed from O and the remainder of its
+    rounding (off by u^2 |o|), and its other errors are bounded as they arise, u sum_j p_j |v_j - o|, not by the sums of
+    magnitudes: small sequences only."""
     dtype = q.dtype
     u = torch.finfo(dtype).eps / 2
     fp16 = dtype == torch.float16
@@ -73,6 +75,11 @@ def reference(q, k, v, cu_q, k_begin, k_end, causal, scale, do=None):
             dP = dO @ V.T
             dS = p * (dP - delta)
             ep = (e + lse_tol)[..., None] + UNIT                                # relative error of P
+            if o_rest:
+                spread = (p[..., None] * (V[None, None] - o[:, :, None]).abs()).sum(-2)
+                tol = (u + e)[..., None] * spread * (1 + 4 * u) + (m + 16) * UNIT * absv + 2 * u * u * o.abs() + tiny
+                if fp16:
+                    tol = tol + m * 2.0 ** -25 * V.abs().max()
             # error of dP - delta: products, and delta's: the rounding of O (u |o| and what came before it)
             size = dO.norm(dim=-1, keepdim=True)
             edp = (d + 8) * UNIT * size * V.norm(dim=-1).max() + (dO.abs() * tol).sum(-1, keepdim=True) \

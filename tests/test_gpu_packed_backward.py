@@ -73,6 +73,33 @@ def test_more_or_fewer_keys_than_queries(api, causal, dtype, d):
     run(api, dtype, d, 2, 2, causal, [0], [150])
 
 
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("lens", [[2], [2, 3, 1, 2], [17, 5], [40, 130], [300]], ids=str)
+@pytest.mark.parametrize("d,hq,hk", [(128, 4, 2), (64, 3, 3), (64, 16, 1)])
+def test_rows_that_cancel(api, dtype, lens, d, hq, hk):
+    """Short sequences and peaked rows, where P (dP - delta) cancels: the remainder of o that ``want_lse`` keeps takes the
+    rounding of o out of the gradients."""
+    cu = packed(lens)
+    n = cu[-1]
+    q, k, v, do = (randn((n, h, d), dtype, i, 2.5 if i == 0 else 1.0) for i, h in enumerate((hq, hk, hk, hq)))
+    attn = api.PackedAttn(hq, hk, d, dtype=dtype, causal=True)
+    kw = dict(max_q=max(lens), max_k=max(lens))
+    o, lse = attn.forward(q, k, v, i32(cu), want_lse=True, **kw)
+    want = reference(q, k, v, cu, cu[:-1], cu[1:], True, d ** -0.5, do=do, o_rest=True)
+    u = torch.finfo(dtype).eps / 2
+    # O and its remainder together: the rounding of the remainder, u^2 |o|, and the errors that come before
+    both = o.double() + lse.o_rest.double()
+    check(both, want["o"], want["o_tol"] - u * want["o"].abs() * (1 + u) + 2.0 ** -24, "o + rest")
+    for name, t in zip(("dq", "dk", "dv"), attn.backward(do, q, k, v, o, lse, i32(cu), **kw)):
+        check(t, want[name], want[name + "_tol"], name)
+    o2 = torch.empty_like(o)
+    attn.forward(q * 0.5, k, v, i32(cu), o=o2, lse=lse, **kw)            # an lse used again keeps its remainder up to date
+    alone = attn.forward(q * 0.5, k, v, i32(cu), want_lse=True, **kw)
+    assert torch.equal(o2, alone[0]) and torch.equal(lse.o_rest, alone[1].o_rest)
+    with pytest.raises(ValueError):
+        attn.backward(do[1:], q[1:], k, v, o[1:], lse, i32(cu), **kw)
+
+
 def test_many_sequences(api):
     lens = [(7 * i) % 4 for i in range(1050)]
     lens[2], lens[700] = 400, 130

@@ -91,6 +91,7 @@ def test_null_handles():
 def test_good_arguments_reach_the_device_check():
     assert passed(forward(arguments()))
     assert passed(forward(arguments(lse=None)))
+    assert passed(forward(arguments(o_rest=A))) and forward(arguments(o_rest=A, lse=None)) == BAD
     assert passed(backward(arguments(), grads()))
     assert passed(forward(arguments(total_k=0, max_k=0, k=None, v=None)))
     # a dimension of one entry has no stride
@@ -100,7 +101,7 @@ def test_good_arguments_reach_the_device_check():
 @pytest.mark.parametrize("kw,rc", [
     (dict(q=None), BAD), (dict(k=None), BAD), (dict(v=None), BAD), (dict(o=None), BAD), (dict(q=A + 8), BAD),
     (dict(o=A + 2), BAD), (dict(cu_q=None), BAD), (dict(k_begin=None), BAD), (dict(k_end=None), BAD), (dict(cu_q=A + 2), BAD),
-    (dict(lse=A + 1), BAD), (dict(n_seq=0), BAD), (dict(total_q=-1), BAD), (dict(total_k=-1), BAD), (dict(max_q=-1), BAD),
+    (dict(lse=A + 1), BAD), (dict(o_rest=A + 8), BAD), (dict(n_seq=0), BAD), (dict(total_q=-1), BAD), (dict(total_k=-1), BAD), (dict(max_q=-1), BAD),
     (dict(max_q=101), BAD), (dict(max_k=121), BAD), (dict(sm_scale=0.0), BAD), (dict(sm_scale=-1.0), BAD),
     (dict(sm_scale=float("nan")), BAD), (dict(sm_scale=float("inf")), BAD), (dict(q_stride=(256, 60)), BAD),
     (dict(k_stride=(0, 64)), BAD), (dict(v_stride=(128, -64)), BAD), (dict(o_stride=(1 << 38, 64)), BAD),
