@@ -115,7 +115,10 @@ struct RotShape {
   static constexpr bool kRing = kSums && sizeof(T) == 2;
   static constexpr int kPieces = 4 * Raw<T>::kVec;              // of dy, and of x
   static constexpr int kStages = kRing ? 4 : 2;                 // 2: one row ahead, in registers
-  static constexpr int kBlocksPerSm = kSums ? 2 : 4;            // as many as need no (or few) spills
+  // As many as need no (or few) spills.  16-bit forward, 75,600 tokens with 40 + 40 + 40 heads of 128: 4 blocks 750 us, 3 827,
+  // 5 811.  fp32, 32,837 tokens with 12 + 12 + 12 heads of 128, 3 blocks against 4: forward 221 against 244 us, with
+  // layer norm 213 against 226, backward without a norm 212 against 264.
+  static constexpr int kBlocksPerSm = kSums ? 2 : sizeof(T) == 4 ? 3 : 4;
   static constexpr int kRingBytes = kRing ? kStages * kPieces * kThreads * 16 : 0;
 };
 
