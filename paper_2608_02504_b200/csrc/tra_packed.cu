@@ -365,20 +365,26 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
     p.dk_stride[i] = g->dk_stride[i];
     p.dv_stride[i] = g->dv_stride[i];
   }
+  // Streamed tiles of 64 rows let two blocks share an SM where head_dim leaves the room; not where they would hold less than
+  // nine tenths of the rows of 128 (groups of 22 heads and more that do not divide 64).
+  const int half = 64 / p.group;
+  p.stream_rows = h->cfg.head_dim == 64 && 20 * half >= 9 * p.tile_tokens ? 64 : 128;
+  p.stream_tokens = p.stream_rows / p.group;
   // a side without tokens is never loaded; its maps then describe the other side
   const bool q = a->total_q > 0, k = a->total_k > 0;
-  if ((rc = make_packed_map(&p.map_q, h, q ? a->q : a->k, q ? a->q_stride : a->k_stride, q ? p.heads : p.kv_heads,
-                            q ? a->total_q : a->total_k, q ? p.group : 1, p.tile_tokens)) != TRA_OK)
-    return rc;
-  if ((rc = make_packed_map(&p.map_do, h, q ? g->d_o : a->k, q ? g->do_stride : a->k_stride, q ? p.heads : p.kv_heads,
-                            q ? a->total_q : a->total_k, q ? p.group : 1, p.tile_tokens)) != TRA_OK)
-    return rc;
-  if ((rc = make_packed_map(&p.map_k, h, k ? a->k : a->q, k ? a->k_stride : a->q_stride, p.kv_heads, k ? a->total_k : a->total_q, 1,
-                            kTileM)) != TRA_OK)
-    return rc;
-  if ((rc = make_packed_map(&p.map_v, h, k ? a->v : a->q, k ? a->v_stride : a->q_stride, p.kv_heads, k ? a->total_k : a->total_q, 1,
-                            kTileM)) != TRA_OK)
-    return rc;
+  const void *qq = q ? a->q : a->k, *oo = q ? g->d_o : a->k, *kk = k ? a->k : a->q, *vv = k ? a->v : a->q;
+  const int64_t *qs = q ? a->q_stride : a->k_stride, *os = q ? g->do_stride : a->k_stride;
+  const int64_t *ks = k ? a->k_stride : a->q_stride, *vs = k ? a->v_stride : a->q_stride;
+  const int q_heads = q ? p.heads : p.kv_heads, q_box = q ? p.group : 1, nq = q ? a->total_q : a->total_k, nk = k ? a->total_k : a->total_q;
+  if ((rc = make_packed_map(&p.map_q, h, qq, qs, q_heads, nq, q_box, p.tile_tokens)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p.map_do, h, oo, os, q_heads, nq, q_box, p.tile_tokens)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p.map_k, h, kk, ks, p.kv_heads, nk, 1, p.stream_rows)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p.map_v, h, vv, vs, p.kv_heads, nk, 1, p.stream_rows)) != TRA_OK) return rc;
+  p.map_q_stream = p.map_q, p.map_do_stream = p.map_do;
+  if (p.stream_rows != kTileM) {
+    if ((rc = make_packed_map(&p.map_q_stream, h, qq, qs, q_heads, nq, q_box, p.stream_tokens)) != TRA_OK) return rc;
+    if ((rc = make_packed_map(&p.map_do_stream, h, oo, os, q_heads, nq, q_box, p.stream_tokens)) != TRA_OK) return rc;
+  }
   const tra_packed_ctx ctx = {h, (cudaStream_t)stream_};
   return h->cfg.head_dim == 128 ? tra_packed_bwd_d128(ctx, p) : tra_packed_bwd_d64(ctx, p);
 }

@@ -18,6 +18,7 @@ struct tra_packed {
 // heads that share the key/value head, token-major: row r of a tile is token r / group, head r % group.
 struct tra_packed_launch {
   CUtensorMap map_q, map_k, map_v, map_do;   // boxes: 64 channels x (group heads x tile tokens | 1 head x 128 tokens)
+  CUtensorMap map_q_stream, map_do_stream;   // backward, streamed tiles of stream_rows rows (then K and V boxes have that many, too)
   const void *q, *k, *v, *o_in, *d_o;
   void *o, *dq, *dk, *dv;
   float* lse;                  // forward: written or NULL; backward: read
@@ -30,6 +31,7 @@ struct tra_packed_launch {
   const int32_t *cu_q, *k_begin, *k_end;
   int n_seq, total_q, total_k, max_q, max_k;
   int heads, kv_heads, group, tile_tokens;   // tile_tokens = 128 / group: query tokens of a 128-row tile
+  int stream_rows, stream_tokens;            // backward: rows of a streamed tile, 128 or 64, and stream_rows / group
   int causal, splits, n_units;               // n_units: query-tile pairs (forward) or key / query tiles (backward) launched
   float sm_scale;
   int* status;

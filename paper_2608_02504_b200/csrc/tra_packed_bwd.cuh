@@ -12,12 +12,13 @@
 // block through memory (fp32 atomics whose order changes the result, or 4 bytes per row, channel and key block).
 //
 // Order on the tensor pipe, so that it always has a product that waits for nobody:
-//   dkv: dV(i), S(i+1), dK(i), dP(i+1): the threads turn dP(i) into dS(i) under the first two and S(i+1) into P(i+1)
-//        under the last two;
+//   dkv: S(i+1) as soon as the threads hold dP(i) in registers, dV(i), then dK(i), dP(i+1): the threads turn dP(i) into dS(i)
+//        under the first two and S(i+1) into P(i+1) under the last two;
 //   dq : S(i+1) as soon as the threads hold S(i) in registers, dP(i+1) likewise, then dQ(i).
-// Tensor memory: S [0, 128), dP [128, 256), two sums of D columns from 256 and 384 (dkv) or one and dS (dq).  P and dS of the
-// warpgroup that owns columns 64 h .. 64 h + 63 overwrite the first 32 of those columns, which only its own threads
-// read (dkv); dq keeps dS apart, because dP(i+1) is issued before dQ(i) has read it.
+// Tensor memory: two places of a step's columns, then the sums.  dkv: S(i) in one place, dP(i) in the other; P and dS of the
+// warpgroup that owns columns 64 h .. 64 h + 63 overwrite its scores (the first and the last 32 of those columns), which only its
+// own threads read; so dP's place is free for S(i+1) before the products have read P(i) and dS(i), and theirs takes dP(i+1).
+// dq: S, dP, dQ, and dS apart, because dP(i+1) is issued before dQ(i) has read it.
 //
 // Rows past a sequence's end (another sequence's, or anything) meet zero probabilities, but 0 * NaN is NaN where such a row is on the
 // summed side of a product: an idle warp zeroes them in shared memory (dkv: rows of Q and dO; dq: rows of K and V).
@@ -27,31 +28,41 @@
 
 namespace {
 
-constexpr int kBwdThreads = 384;
-constexpr int kBwdRegsSoftmax = 216;     // 2 * 216 + 72 = 3 * 168, the registers of the launch
-constexpr int kBwdRegsControl = 72;
 constexpr int kStatStages = 2;           // of the query rows' lse and delta (dkv)
 
-template <int D>
+// kHalves: groups of 64 columns that a step walks, with one warpgroup of softmax threads each.
+//   2: streamed tiles of 128 rows, one block per SM.
+//   1: streamed tiles of 64 rows, half of the tensor memory, two blocks per SM: where the products are short (D = 64) the serial
+//      part of a step and the blocks' starts and ends are hidden by the other block.
+template <int D, int kHalves>
 struct BwdCfg {
   static constexpr int kAtoms = D / 64;
-  static constexpr int kAtomBytes = kTileM * 128;
+  static constexpr int kAtomBytes = kTileM * 128;                          // resident tiles
   static constexpr int kTileBytes = kAtoms * kAtomBytes;
+  static constexpr int kStream = 64 * kHalves;                             // rows of a streamed tile
+  static constexpr int kStreamAtom = kStream * 128;
+  static constexpr int kStreamBytes = kAtoms * kStreamAtom;
   // Rings of streamed tiles.  A = Q (dkv) or K (dq), which two products use, the second one a step later; B = dO or V, done
   // with earlier.  A ring of two A tiles left the tensor pipe waiting for its loads (440 cycles of 3,750 per step, dkv).
   static constexpr int kA = D == 128 ? 3 : 4;
   static constexpr int kB = D == 128 ? 2 : 4;
-  static constexpr int kSmemData = (2 + kA + kB) * kTileBytes;             // and two resident tiles
-  static constexpr int kSmemNeeded = kSmemData + 512 + 2 * kStatStages * kTileM * 4;
-  // at least 120 KB so that one block owns an SM and its whole tensor memory
-  static constexpr int kSmemBytes = kSmemNeeded > 120 * 1024 ? kSmemNeeded : 120 * 1024;
-  static_assert(kSmemBytes <= 232448, "shared memory of a block");
-  // tensor memory: with D = 64 there is room for P and dS of their own, and the next S and dP need not wait for the
-  // products that read them
-  static constexpr bool kApart = D == 64;
-  static constexpr int kSum0 = 256, kSum1 = kApart ? 320 : 384;            // dV, dK
-  static constexpr int kP = kApart ? 384 : 0, kDs = kApart ? 448 : 128;
-  static constexpr int kPStep = kApart ? 32 : 64;                          // columns from one half's P to the other's
+  static constexpr int kSmemData = 2 * kTileBytes + (kA + kB) * kStreamBytes;
+  static constexpr int kSmemNeeded = kSmemData + 512 + 2 * kStatStages * kStream * 4;
+  // At least 120 KB so that one block owns an SM and its whole tensor memory; with halves 113 KB, so that two fit and neither shares
+  // the SM with a block that wants all of it.
+  static constexpr int kSmemLeast = kHalves == 2 ? 120 * 1024 : 113 * 1024;
+  static constexpr int kSmemBytes = kSmemNeeded > kSmemLeast ? kSmemNeeded : kSmemLeast;
+  static_assert(kSmemBytes <= (kHalves == 2 ? 232448 : kSmemLeast), "shared memory of a block");
+  static constexpr int kSoftWarps = 4 * kHalves;
+  static constexpr int kThreads = 32 * kSoftWarps + 128;
+  static constexpr int kBlocks = kHalves == 2 ? 1 : 2;                     // per SM
+  static constexpr int kRegsSoftmax = kHalves == 2 ? 216 : 200;            // 2 * 216 + 72 = 3 * 168, the registers of the launch;
+  static constexpr int kRegsControl = kHalves == 2 ? 72 : 56;              // 200 + 56 = 2 * 128
+  // Tensor memory: two places of a step's width, for the scores and dP, and the sums; P and dS over the scores (dkv), dS apart (dq).
+  static constexpr int kColumns = 256 * kHalves;
+  static constexpr int kDp = kStream;
+  static constexpr int kSum0 = 2 * kStream, kSum1 = 3 * kStream;           // dV and dK; dQ and dS
+  static_assert(D <= kStream, "the sums' columns");
 };
 
 struct BwdCtl {
@@ -59,8 +70,8 @@ struct BwdCtl {
   uint64_t a_full[4], b_full[4], a_free[4], b_free[4];       // streamed tiles
   uint64_t stat_full[kStatStages], stat_free[kStatStages];
   uint64_t s_full, dp_full;
-  uint64_t s_read, dp_read;              // the threads hold S / dP in registers
-  uint64_t p_ready[2], ds_ready[2];      // per 64-column half
+  uint64_t s_read, dp_read;              // the threads hold S / dP in registers (dkv: and have stored P, before dp_read)
+  uint64_t ds_ready;
   uint64_t tail_full, tail_ready;
   uint64_t drain;
   uint32_t tmem_base;
@@ -70,6 +81,7 @@ struct BwdCtl {
 static_assert(sizeof(BwdCtl) <= 512, "control block");
 
 // Set-up shared by the two kernels: barriers and the block's (sequence, unit).
+template <int kHalves>
 __device__ __forceinline__ void bwd_init(BwdCtl* ctl) {
   mbar_init(smem_u32(&ctl->own_full), 1);
   for (int i = 0; i < 4; ++i) {
@@ -80,16 +92,13 @@ __device__ __forceinline__ void bwd_init(BwdCtl* ctl) {
   }
   for (int i = 0; i < kStatStages; ++i) {
     mbar_init(smem_u32(&ctl->stat_full[i]), 1);
-    mbar_init(smem_u32(&ctl->stat_free[i]), 8);
+    mbar_init(smem_u32(&ctl->stat_free[i]), 4 * kHalves);
   }
   mbar_init(smem_u32(&ctl->s_full), 1);
   mbar_init(smem_u32(&ctl->dp_full), 1);
-  mbar_init(smem_u32(&ctl->s_read), 8);
-  mbar_init(smem_u32(&ctl->dp_read), 8);
-  for (int h = 0; h < 2; ++h) {
-    mbar_init(smem_u32(&ctl->p_ready[h]), 4);
-    mbar_init(smem_u32(&ctl->ds_ready[h]), 4);
-  }
+  mbar_init(smem_u32(&ctl->s_read), 4 * kHalves);
+  mbar_init(smem_u32(&ctl->dp_read), 4 * kHalves);
+  mbar_init(smem_u32(&ctl->ds_ready), 4 * kHalves);
   mbar_init(smem_u32(&ctl->tail_full), 1);
   mbar_init(smem_u32(&ctl->tail_ready), 1);
   mbar_init(smem_u32(&ctl->drain), 1);
@@ -97,17 +106,18 @@ __device__ __forceinline__ void bwd_init(BwdCtl* ctl) {
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
 
+template <class C>
 __device__ __forceinline__ void bwd_teardown(BwdCtl* ctl, uint32_t tmem, int warp) {
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == C::kSoftWarps + 1) {
     if (ctl->abort_flag) {
       // let copies and MMAs that were in flight when the block gave up land before releasing
       const unsigned long long t0 = globaltimer_ns();
       while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
     }
     tc_fence_after();
-    tmem_free_all(tmem);
+    tmem_free<C::kColumns>(tmem);
   }
 }
 
@@ -126,10 +136,9 @@ struct RingPos {
 
 // The producer's loop of either kernel: tile i of each ring as soon as its slot is free.  The
 // last pair goes to tail_full when rows past the sequence's end have to be zeroed in it.
-template <int D, typename LoadA, typename LoadB>
+template <class C, typename LoadA, typename LoadB>
 __device__ __forceinline__ void bwd_produce(BwdCtl* ctl, int n, bool tail, uint32_t bytes, volatile int* abort_flag, int* status,
                                             LoadA load_a, LoadB load_b) {
-  using C = BwdCfg<D>;
   RingPos<C::kA> a;
   RingPos<C::kB> b;
   for (int i = 0; i < n; ++i) {
@@ -163,66 +172,66 @@ __device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t* r) {
   reg_fence32(r + 32);
 }
 
-// Product of two K-major tiles in shared memory: D[tmem] = A B^T over the D channels.
+// Product of two K-major tiles in shared memory: D[tmem] = A B^T over the D channels (atoms of 128 rows where there are two).
 template <int D>
 __device__ __forceinline__ void mma_tiles(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
   constexpr uint32_t kHi = desc_hi(1024);
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
-    const uint32_t off = ((kk >> 2) * BwdCfg<D>::kAtomBytes + (kk & 3) * 32) >> 4;
+    const uint32_t off = ((kk >> 2) * kTileM * 128 + (kk & 3) * 32) >> 4;
     tc_mma_ss(d, a_lo + off, kHi, b_lo + off, kHi, idesc, kk > 0 ? 1u : 0u);
   }
 }
 
-// The warpgroup's half (D / 2 channels from h D / 2) of a sum in tensor memory, scaled and rounded, to the rows' memory.
-template <typename T, int D>
-__device__ __forceinline__ void store_half(const RowAddresses& rows, uint32_t taddr, int h, bool any, float mul) {
+// The warpgroup's share (kChannels from h kChannels on) of a sum in tensor memory, scaled and rounded, to the rows' memory.
+template <typename T, int kChannels>
+__device__ __forceinline__ void store_share(const RowAddresses& rows, uint32_t taddr, int h, bool any, float mul) {
 #pragma unroll 1
-  for (int c = 0; c < D / 64; ++c) {
+  for (int c = 0; c < kChannels / 32; ++c) {
     uint32_t v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = 0u;
     if (any) {
-      tmem_ld32(taddr + h * (D / 2) + c * 32, v);
+      tmem_ld32(taddr + h * kChannels + c * 32, v);
       tmem_wait_ld(v);
     }
 #pragma unroll
     for (int j = 0; j < 16; ++j) v[j] = pack_pair<T>(__uint_as_float(v[2 * j]) * mul, __uint_as_float(v[2 * j + 1]) * mul);
-    rows.store64(v, h * D + c * 64);
+    rows.store64(v, h * kChannels * 2 + c * 64);
   }
 }
 
 // ------------------------------------------------------------------------------------ dK, dV
-template <typename T, int D, bool kCausal>
+template <typename T, int D, int kHalves, bool kCausal>
 __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
-  using C = BwdCfg<D>;
+  using C = BwdCfg<D, kHalves>;
   uint8_t* sK = smem;
   uint8_t* sV = smem + C::kTileBytes;
   uint8_t* sA = smem + 2 * C::kTileBytes;                   // Q tiles
-  uint8_t* sB = sA + C::kA * C::kTileBytes;                 // dO tiles
+  uint8_t* sB = sA + C::kA * C::kStreamBytes;                 // dO tiles
   BwdCtl* ctl = (BwdCtl*)(smem + C::kSmemData);
-  float* s_lse2 = (float*)(smem + C::kSmemData + 512);       // [stage][128], then delta
-  float* s_delta = s_lse2 + kStatStages * kTileM;
+  float* s_lse2 = (float*)(smem + C::kSmemData + 512);       // [stage][streamed row], then delta
+  float* s_delta = s_lse2 + kStatStages * C::kStream;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-  const int tile_tokens = p.tile_tokens, box_rows = tile_tokens * p.group;
+  const int tile_tokens = p.stream_tokens, box_rows = tile_tokens * p.group;
 
   // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
     const tra_unit u = tra_find_unit(p, true, p.max_k <= kTileM, kTileM, unit);
     if (lane == 0) ctl->unit = u;
-  } else if (warp == 9) {
-    tmem_alloc_all(&ctl->tmem_base);
+  } else if (warp == C::kSoftWarps + 1) {
+    tmem_alloc<C::kColumns>(&ctl->tmem_base);
   } else if (tid == 32) {
-    bwd_init(ctl);
+    bwd_init<kHalves>(ctl);
   } else if (tid == 64) {
-    prefetch_map(&p.map_q);
-    prefetch_map(&p.map_do);
+    prefetch_map(&p.map_q_stream);
+    prefetch_map(&p.map_do_stream);
     prefetch_map(&p.map_k);
     prefetch_map(&p.map_v);
   }
-  if (box_rows < kTileM && warp >= 2 && warp < 8)        // rows that no box fills
-    zero_tile_rows(sA, box_rows, kTileM, (C::kA + C::kB) * C::kAtoms, C::kAtomBytes, tid - 64, 192);
+  if (box_rows < C::kStream && warp >= 2 && warp < C::kSoftWarps)        // rows that no box fills
+    zero_tile_rows(sA, box_rows, C::kStream, (C::kA + C::kB) * C::kAtoms, C::kStreamAtom, tid - 64, 32 * (C::kSoftWarps - 2));
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   tc_fence_before();
   __syncthreads();
@@ -231,7 +240,7 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
   const tra_seq_range qr = ctl->unit.q, kr = ctl->unit.k;
   const int key0 = ctl->unit.index * kTileM;
   if (ctl->unit.seq < 0) {
-    if (warp == 9) tmem_free_all(tmem);
+    if (warp == C::kSoftWarps + 1) tmem_free<C::kColumns>(tmem);
     wait_last_launch();          // no block ends before the launch in front of it
     return;
   }
@@ -244,45 +253,47 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
   const bool tail = n > 0 && tail_rows < box_rows;
   volatile int* abort_flag = &ctl->abort_flag;
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBwdRegsControl));
-    if (warp == 8) {
+  if (warp >= C::kSoftWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsControl));
+    if (warp == C::kSoftWarps) {
       // ================================================================== TMA producer
       if (lane == 0) {
         const uint32_t own = smem_u32(&ctl->own_full);
         mbar_expect_tx(own, 2 * C::kTileBytes);
-        for (int a = 0; a < C::kAtoms; ++a) {
-          tma_load_3d(smem_u32(sK + a * C::kAtomBytes), &p.map_k, own, a * 64, kvh, kr.begin + key0);
-          tma_load_3d(smem_u32(sV + a * C::kAtomBytes), &p.map_v, own, a * 64, kvh, kr.begin + key0);
-        }
+        for (int a = 0; a < C::kAtoms; ++a)
+          for (int b = 0; b < kTileM; b += C::kStream) {
+            tma_load_3d(smem_u32(sK + a * C::kAtomBytes + b * 128), &p.map_k, own, a * 64, kvh, kr.begin + key0 + b);
+            tma_load_3d(smem_u32(sV + a * C::kAtomBytes + b * 128), &p.map_v, own, a * 64, kvh, kr.begin + key0 + b);
+          }
         const int tok0 = qr.begin + first_tile * tile_tokens;
-        bwd_produce<D>(
+        bwd_produce<C>(
             ctl, n, tail, C::kAtoms * box_rows * 128, abort_flag, p.status,
             [&](int i, int slot, uint32_t bar) {
               for (int a = 0; a < C::kAtoms; ++a)
-                tma_load_3d(smem_u32(sA + slot * C::kTileBytes + a * C::kAtomBytes), &p.map_q, bar, a * 64, kvh * p.group, tok0 + i * tile_tokens);
+                tma_load_3d(smem_u32(sA + slot * C::kStreamBytes + a * C::kStreamAtom), &p.map_q_stream, bar, a * 64, kvh * p.group, tok0 + i * tile_tokens);
             },
             [&](int i, int slot, uint32_t bar) {
               for (int a = 0; a < C::kAtoms; ++a)
-                tma_load_3d(smem_u32(sB + slot * C::kTileBytes + a * C::kAtomBytes), &p.map_do, bar, a * 64, kvh * p.group, tok0 + i * tile_tokens);
+                tma_load_3d(smem_u32(sB + slot * C::kStreamBytes + a * C::kStreamAtom), &p.map_do_stream, bar, a * 64, kvh * p.group, tok0 + i * tile_tokens);
             });
       }
-    } else if (warp == 10) {
+    } else if (warp == C::kSoftWarps + 2) {
       // ================================================================== rows past the sequence's end
       if (tail && mbar_wait_warp(smem_u32(&ctl->tail_full), 0u, abort_flag, p.status)) {
-        zero_tile_rows(sA + ((n - 1) % C::kA) * C::kTileBytes, tail_rows, box_rows, C::kAtoms, C::kAtomBytes, lane, 32);
-        zero_tile_rows(sB + ((n - 1) % C::kB) * C::kTileBytes, tail_rows, box_rows, C::kAtoms, C::kAtomBytes, lane, 32);
+        zero_tile_rows(sA + ((n - 1) % C::kA) * C::kStreamBytes, tail_rows, box_rows, C::kAtoms, C::kStreamAtom, lane, 32);
+        zero_tile_rows(sB + ((n - 1) % C::kB) * C::kStreamBytes, tail_rows, box_rows, C::kAtoms, C::kStreamAtom, lane, 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->tail_ready));
       }
-    } else if (warp == 11) {
+    } else if (warp == C::kSoftWarps + 3) {
       // ================================================================== lse and delta of the query rows
       wait_last_launch();                                 // delta
       // read before the wait for the slot, so that the loads' latency is not added to it
-      int r_tok[4], r_row[4];
+      constexpr int kPer = C::kStream / 32;
+      int r_tok[kPer], r_row[kPer];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kPer; ++k) {
         const int r = k * 32 + lane;
         r_tok[k] = r < box_rows ? r / p.group : 1 << 30;             // past every sequence: a row no box fills
         r_row[k] = r % p.group;
@@ -290,9 +301,9 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
       for (int i = 0; i < n; ++i) {
         const int st = i % kStatStages;
         const int tok0 = (first_tile + i) * tile_tokens;
-        float lse2[4], delta[4];
+        float lse2[kPer], delta[kPer];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kPer; ++k) {
           lse2[k] = INFINITY;                             // a row that is not there, or sees no key: probability 0
           delta[k] = 0.f;
           if (r_tok[k] < qr.len - tok0) {
@@ -304,93 +315,90 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
         if (i >= kStatStages && !mbar_wait_warp(smem_u32(&ctl->stat_free[st]), (uint32_t)(i / kStatStages - 1) & 1u, abort_flag, p.status))
           break;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {                     // negated for the packed multiply-add
-          s_lse2[st * kTileM + k * 32 + lane] = lse2[k] == -INFINITY ? -INFINITY : -lse2[k] * kLog2e;
-          s_delta[st * kTileM + k * 32 + lane] = -delta[k];
+        for (int k = 0; k < kPer; ++k) {                     // negated for the packed multiply-add
+          s_lse2[st * C::kStream + k * 32 + lane] = lse2[k] == -INFINITY ? -INFINITY : -lse2[k] * kLog2e;
+          s_delta[st * C::kStream + k * 32 + lane] = -delta[k];
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->stat_full[st]));
       }
-    } else if (warp == 9) {
+    } else if (warp == C::kSoftWarps + 1) {
       // ================================================================== MMA issuer
-      constexpr uint32_t kIdescS = make_idesc_t<T>(kTileM, false);
+      constexpr uint32_t kIdescS = make_idesc_t<T>(C::kStream, false);
       constexpr uint32_t kIdescD = make_idesc_t<T>(D, true);
       constexpr uint32_t kHi = desc_hi(1024);
       const uint32_t k_lo = desc_lo(smem_u32(sK), 16), v_lo = desc_lo(smem_u32(sV), 16);
-      const uint32_t a_k = desc_lo(smem_u32(sA), 16), a_mn = desc_lo(smem_u32(sA), C::kAtomBytes);     // K-major and MN-major views
-      const uint32_t b_k = desc_lo(smem_u32(sB), 16), b_mn = desc_lo(smem_u32(sB), C::kAtomBytes);
-      constexpr uint32_t kTile = C::kTileBytes >> 4;
+      const uint32_t a_k = desc_lo(smem_u32(sA), 16), a_mn = desc_lo(smem_u32(sA), C::kStreamAtom);     // K-major and MN-major views
+      const uint32_t b_k = desc_lo(smem_u32(sB), 16), b_mn = desc_lo(smem_u32(sB), C::kStreamAtom);
+      constexpr uint32_t kTile = C::kStreamBytes >> 4;
       RingPos<C::kA> qs, qd;                 // Q of the next S, of the next dK
       RingPos<C::kB> os, od;                 // dO of the next dP, of the next dV
       bool alive = mbar_wait(smem_u32(&ctl->own_full), 0u, abort_flag, p.status);
-      auto issue_s = [&](int i) -> bool {
-        if (!(tail && i == n - 1 ? mbar_wait(smem_u32(&ctl->tail_ready), 0u, abort_flag, p.status)
-                                 : mbar_wait(smem_u32(&ctl->a_full[qs.slot]), qs.phase, abort_flag, p.status)))
-          return false;
-        tc_fence_after();
-        mma_tiles<D>(tmem, k_lo, a_k + (uint32_t)qs.slot * kTile, kIdescS);
+      // Q and dO of the next scores and dP are in shared memory
+      auto tiles_here = [&](int i) -> bool {
+        if (tail && i == n - 1) return mbar_wait(smem_u32(&ctl->tail_ready), 0u, abort_flag, p.status);
+        return mbar_wait(smem_u32(&ctl->a_full[qs.slot]), qs.phase, abort_flag, p.status) &&
+               mbar_wait(smem_u32(&ctl->b_full[os.slot]), os.phase, abort_flag, p.status);
+      };
+      auto issue_s = [&](int i) {
+        mma_tiles<D>(tmem + (i & 1 ? C::kDp : 0), k_lo, a_k + (uint32_t)qs.slot * kTile, kIdescS);
         tc_commit(smem_u32(&ctl->s_full));
         qs.next();
-        return true;
       };
-      auto issue_dp = [&](int i) -> bool {
-        // (the last pair of a tail came with Q)
-        if (!(tail && i == n - 1) && !mbar_wait(smem_u32(&ctl->b_full[os.slot]), os.phase, abort_flag, p.status)) return false;
-        tc_fence_after();
-        mma_tiles<D>(tmem + 128, v_lo, b_k + (uint32_t)os.slot * kTile, kIdescS);
+      auto issue_dp = [&](int i) {
+        mma_tiles<D>(tmem + (i & 1 ? 0 : C::kDp), v_lo, b_k + (uint32_t)os.slot * kTile, kIdescS);
         tc_commit(smem_u32(&ctl->dp_full));
         os.next();
-        return true;
       };
-      // sum[tmem] += A[tmem] * B[MN-major tile], each 64-row half as soon as it is announced
-      auto issue_sum = [&](uint32_t d, uint32_t a, uint32_t b_lo, uint64_t* ready, int i) -> bool {
+      // sum[tmem] += A[tmem] * B[MN-major tile]
+      auto issue_sum = [&](uint32_t d, uint32_t a, uint32_t b_lo, int i) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!mbar_wait(smem_u32(&ready[h]), (uint32_t)i & 1u, abort_flag, p.status)) return false;
-          tc_fence_after();
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            tc_mma_ts(d, a + h * C::kPStep + kk * 8, b_lo + (h * 4 + kk) * (2048 >> 4), kHi, kIdescD, h + kk > 0 ? 1u : (i > 0 ? 1u : 0u));
-        }
-        return true;
+        for (int kk = 0; kk < 4 * kHalves; ++kk)
+          tc_mma_ts(d, a + (kk >> 2) * 64 + (kk & 3) * 8, b_lo + kk * (2048 >> 4), kHi, kIdescD, kk > 0 ? 1u : (i > 0 ? 1u : 0u));
       };
-      alive = alive && n > 0 && issue_s(0) && issue_dp(0);
+      alive = alive && n > 0 && tiles_here(0);
+      if (alive) {
+        tc_fence_after();
+        issue_s(0);
+        issue_dp(0);
+      }
+      // Every wait costs this warp about 120 cycles, met or not, and the threads wait for the scores: so the tiles are waited for
+      // while the threads compute P, P needs no barrier of its own (dp_read comes behind its stores), and the scores go first.
       for (int i = 0; i < n && alive; ++i) {
         const bool next = i + 1 < n;
-        if (C::kApart && next)
-          if (!(alive = mbar_wait(smem_u32(&ctl->s_read), (uint32_t)i & 1u, abort_flag, p.status) && issue_s(i + 1))) break;
-        if (!(alive = issue_sum(tmem + C::kSum0, tmem + C::kP, b_mn + (uint32_t)od.slot * kTile, ctl->p_ready, i))) break;     // dV += P^T dO
+        const uint32_t t_p = tmem + (i & 1 ? C::kDp : 0);
+        if (next && !(alive = tiles_here(i + 1))) break;
+        if (!(alive = mbar_wait(smem_u32(&ctl->dp_read), (uint32_t)i & 1u, abort_flag, p.status))) break;
+        tc_fence_after();
+        if (next) issue_s(i + 1);                                                   // in dP's place
+        issue_sum(tmem + C::kSum0, t_p, b_mn + (uint32_t)od.slot * kTile, i);       // dV += P^T dO
         tc_commit(smem_u32(&ctl->b_free[od.slot]));
         od.next();
-        if (C::kApart && next)
-          if (!(alive = mbar_wait(smem_u32(&ctl->dp_read), (uint32_t)i & 1u, abort_flag, p.status) && issue_dp(i + 1))) break;
-        if (!C::kApart && next && !(alive = issue_s(i + 1))) break;
-        if (!(alive = issue_sum(tmem + C::kSum1, tmem + C::kDs, a_mn + (uint32_t)qd.slot * kTile, ctl->ds_ready, i))) break;   // dK += dS^T Q
+        if (!(alive = mbar_wait(smem_u32(&ctl->ds_ready), (uint32_t)i & 1u, abort_flag, p.status))) break;
+        tc_fence_after();
+        issue_sum(tmem + C::kSum1, t_p + 32, a_mn + (uint32_t)qd.slot * kTile, i);  // dK += dS^T Q
         tc_commit(smem_u32(&ctl->a_free[qd.slot]));
         qd.next();
-        if (!C::kApart && next && !(alive = issue_dp(i + 1))) break;
+        if (next) issue_dp(i + 1);                                                  // in the place of P and dS
       }
       tc_commit(smem_u32(&ctl->drain));
       mbar_wait(smem_u32(&ctl->drain), 0u, abort_flag, p.status);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBwdRegsSoftmax));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
     // ================================================================== probabilities and their gradients
     const int h = warp >> 2;                                 // columns 64 h .. 64 h + 63
     int r = tid & (kTileM - 1);                              // key inside the tile
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t t_s = tmem + lane_base + h * 64, t_dp = t_s + 128;
-    const uint32_t t_p = tmem + lane_base + C::kP + h * C::kPStep, t_ds = tmem + lane_base + C::kDs + h * C::kPStep;
-    RingPos<C::kA> qd;                                       // Q and dO of the step before: their freeing tells that the
-    RingPos<C::kB> od;                                       // products that read dS and P have retired
     const float scale_log2 = p.sm_scale * kLog2e;
     const uint64_t scale2 = pack2(scale_log2, scale_log2);
     int blind_tok = key0 + r - ahead - first_tile * tile_tokens;         // tokens of the first tile in front of the first seer
     bool alive = true;
     for (int i = 0; i < n; ++i) {
       const int st = i % kStatStages;
-      const ulonglong2* lse4 = reinterpret_cast<const ulonglong2*>(s_lse2 + st * kTileM + h * 64);        // negated
-      const ulonglong2* delta4 = reinterpret_cast<const ulonglong2*>(s_delta + st * kTileM + h * 64);
+      const uint32_t t_s = tmem + lane_base + h * 64 + (i & 1 ? C::kDp : 0), t_dp = tmem + lane_base + h * 64 + (i & 1 ? 0 : C::kDp);
+      const ulonglong2* lse4 = reinterpret_cast<const ulonglong2*>(s_lse2 + st * C::kStream + h * 64);        // negated
+      const ulonglong2* delta4 = reinterpret_cast<const ulonglong2*>(s_delta + st * C::kStream + h * 64);
       if (!mbar_wait_warp(smem_u32(&ctl->s_full), (uint32_t)i & 1u, abort_flag, p.status) ||
           !mbar_wait_warp(smem_u32(&ctl->stat_full[st]), (uint32_t)(i / kStatStages) & 1u, abort_flag, p.status)) {
         alive = false;
@@ -400,11 +408,6 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
       uint32_t s[64];
       float pr[64];
       tmem_ld64(t_s, s);
-      if (C::kApart) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&ctl->s_read));
-      }
 #pragma unroll
       for (int c4 = 0; c4 < 16; ++c4) {
         const ulonglong2 v = lse4[c4];
@@ -416,7 +419,7 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
       }
       // causal: columns of tokens in front of key - ahead do not see this key
       const int blind = kCausal ? max(blind_tok, 0) * p.group - h * 64 : 0;
-      blind_tok -= p.tile_tokens;
+      blind_tok -= tile_tokens;
       if (kCausal && __any_sync(0xffffffffu, blind > 0)) {
 #pragma unroll
         for (int c = 0; c < 64; ++c)
@@ -426,19 +429,8 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
         uint32_t pk[32];
 #pragma unroll
         for (int c = 0; c < 32; ++c) pk[c] = pack_pair<T>(pr[2 * c], pr[2 * c + 1]);
-        if (C::kApart && i > 0) {
-          if (!mbar_wait_warp(smem_u32(&ctl->b_free[od.slot]), od.phase, abort_flag, p.status)) {
-            alive = false;
-            break;
-          }
-          tc_fence_after();
-          od.next();
-        }
-        tmem_st32(t_p, pk);
+        tmem_st32(t_s, pk);
         tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&ctl->p_ready[h]));
       }
       if (!mbar_wait_warp(smem_u32(&ctl->dp_full), (uint32_t)i & 1u, abort_flag, p.status)) {
         alive = false;
@@ -446,11 +438,9 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
       }
       tc_fence_after();
       tmem_ld64(t_dp, s);
-      if (C::kApart) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&ctl->dp_read));
-      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&ctl->dp_read));
       {
         uint32_t pk[32];
 #pragma unroll
@@ -462,20 +452,12 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
           pk[c4 * 2] = pack_pair<T>(t[0], t[1]);
           pk[c4 * 2 + 1] = pack_pair<T>(t[2], t[3]);
         }
-        if (C::kApart && i > 0) {
-          if (!mbar_wait_warp(smem_u32(&ctl->a_free[qd.slot]), qd.phase, abort_flag, p.status)) {
-            alive = false;
-            break;
-          }
-          tc_fence_after();
-          qd.next();
-        }
-        tmem_st32(t_ds, pk);
+        tmem_st32(t_s + 32, pk);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(smem_u32(&ctl->ds_ready[h]));
+          mbar_arrive(smem_u32(&ctl->ds_ready));
           mbar_arrive(smem_u32(&ctl->stat_free[st]));
         }
       }
@@ -492,21 +474,21 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
       T* out[2] = {(T*)p.dv + row * p.dv_stride[0] + kvh * p.dv_stride[1], (T*)p.dk + row * p.dk_stride[0] + kvh * p.dk_stride[1]};
 #pragma unroll 1
       for (int which = 0; which < 2; ++which)
-        store_half<T, D>(RowAddresses(row_valid ? out[which] : nullptr), tmem + lane_base + (which ? C::kSum1 : C::kSum0), h, n > 0,
+        store_share<T, D / kHalves>(RowAddresses(row_valid ? out[which] : nullptr), tmem + lane_base + (which ? C::kSum1 : C::kSum0), h, n > 0,
                          which ? p.sm_scale : 1.f);
     }
   }
-  bwd_teardown(ctl, tmem, warp);
+  bwd_teardown<C>(ctl, tmem, warp);
 }
 
 // ------------------------------------------------------------------------------------ dQ
-template <typename T, int D, bool kCausal>
+template <typename T, int D, int kHalves, bool kCausal>
 __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
-  using C = BwdCfg<D>;
+  using C = BwdCfg<D, kHalves>;
   uint8_t* sQ = smem;
   uint8_t* sDO = smem + C::kTileBytes;
   uint8_t* sA = smem + 2 * C::kTileBytes;                   // K tiles
-  uint8_t* sB = sA + C::kA * C::kTileBytes;                 // V tiles
+  uint8_t* sB = sA + C::kA * C::kStreamBytes;                 // V tiles
   BwdCtl* ctl = (BwdCtl*)(smem + C::kSmemData);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int tile_tokens = p.tile_tokens, box_rows = tile_tokens * p.group;
@@ -515,18 +497,18 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
   if (warp == 0) {
     const tra_unit u = tra_find_unit(p, false, p.max_q <= tile_tokens, tile_tokens, unit);
     if (lane == 0) ctl->unit = u;
-  } else if (warp == 9) {
-    tmem_alloc_all(&ctl->tmem_base);
+  } else if (warp == C::kSoftWarps + 1) {
+    tmem_alloc<C::kColumns>(&ctl->tmem_base);
   } else if (tid == 32) {
-    bwd_init(ctl);
+    bwd_init<kHalves>(ctl);
   } else if (tid == 64) {
     prefetch_map(&p.map_q);
     prefetch_map(&p.map_do);
     prefetch_map(&p.map_k);
     prefetch_map(&p.map_v);
   }
-  if (box_rows < kTileM && warp >= 2 && warp < 8)        // rows that no box fills
-    zero_tile_rows(sQ, box_rows, kTileM, 2 * C::kAtoms, C::kAtomBytes, tid - 64, 192);
+  if (box_rows < kTileM && warp >= 2 && warp < C::kSoftWarps)        // rows that no box fills
+    zero_tile_rows(sQ, box_rows, kTileM, 2 * C::kAtoms, C::kAtomBytes, tid - 64, 32 * (C::kSoftWarps - 2));
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   tc_fence_before();
   __syncthreads();
@@ -536,20 +518,20 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
   // the last tiles, the longest of a causal sequence, come first
   const int tok0 = (ctl->unit.count - 1 - ctl->unit.index) * tile_tokens;
   if (ctl->unit.seq < 0) {
-    if (warp == 9) tmem_free_all(tmem);
+    if (warp == C::kSoftWarps + 1) tmem_free<C::kColumns>(tmem);
     wait_last_launch();          // no block ends before the launch in front of it
     return;
   }
   const int ahead = kr.len - qr.len;
   const int last_tok = min(tok0 + tile_tokens, qr.len) - 1;
   const int keys = kCausal ? min(max(last_tok + 1 + ahead, 0), kr.len) : kr.len;
-  const int n = (keys + kTileM - 1) / kTileM;
-  const bool tail = n > 0 && n * kTileM > kr.len;
+  const int n = (keys + C::kStream - 1) / C::kStream;
+  const bool tail = n > 0 && n * C::kStream > kr.len;
   volatile int* abort_flag = &ctl->abort_flag;
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBwdRegsControl));
-    if (warp == 8) {
+  if (warp >= C::kSoftWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsControl));
+    if (warp == C::kSoftWarps) {
       // ================================================================== TMA producer
       if (lane == 0) {
         const uint32_t own = smem_u32(&ctl->own_full);
@@ -558,75 +540,76 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
           tma_load_3d(smem_u32(sQ + a * C::kAtomBytes), &p.map_q, own, a * 64, kvh * p.group, qr.begin + tok0);
           tma_load_3d(smem_u32(sDO + a * C::kAtomBytes), &p.map_do, own, a * 64, kvh * p.group, qr.begin + tok0);
         }
-        bwd_produce<D>(
-            ctl, n, tail, C::kTileBytes, abort_flag, p.status,
+        bwd_produce<C>(
+            ctl, n, tail, C::kStreamBytes, abort_flag, p.status,
             [&](int i, int slot, uint32_t bar) {
               for (int a = 0; a < C::kAtoms; ++a)
-                tma_load_3d(smem_u32(sA + slot * C::kTileBytes + a * C::kAtomBytes), &p.map_k, bar, a * 64, kvh, kr.begin + i * kTileM);
+                tma_load_3d(smem_u32(sA + slot * C::kStreamBytes + a * C::kStreamAtom), &p.map_k, bar, a * 64, kvh, kr.begin + i * C::kStream);
             },
             [&](int i, int slot, uint32_t bar) {
               for (int a = 0; a < C::kAtoms; ++a)
-                tma_load_3d(smem_u32(sB + slot * C::kTileBytes + a * C::kAtomBytes), &p.map_v, bar, a * 64, kvh, kr.begin + i * kTileM);
+                tma_load_3d(smem_u32(sB + slot * C::kStreamBytes + a * C::kStreamAtom), &p.map_v, bar, a * 64, kvh, kr.begin + i * C::kStream);
             });
       }
-    } else if (warp == 10) {
+    } else if (warp == C::kSoftWarps + 2) {
       // ================================================================== rows past the sequence's end
       if (tail && mbar_wait_warp(smem_u32(&ctl->tail_full), 0u, abort_flag, p.status)) {
-        const int row0 = kr.len - (n - 1) * kTileM;
-        zero_tile_rows(sA + ((n - 1) % C::kA) * C::kTileBytes, row0, kTileM, C::kAtoms, C::kAtomBytes, lane, 32);
-        zero_tile_rows(sB + ((n - 1) % C::kB) * C::kTileBytes, row0, kTileM, C::kAtoms, C::kAtomBytes, lane, 32);
+        const int row0 = kr.len - (n - 1) * C::kStream;
+        zero_tile_rows(sA + ((n - 1) % C::kA) * C::kStreamBytes, row0, C::kStream, C::kAtoms, C::kStreamAtom, lane, 32);
+        zero_tile_rows(sB + ((n - 1) % C::kB) * C::kStreamBytes, row0, C::kStream, C::kAtoms, C::kStreamAtom, lane, 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->tail_ready));
       }
-    } else if (warp == 9) {
+    } else if (warp == C::kSoftWarps + 1) {
       // ================================================================== MMA issuer
-      constexpr uint32_t kIdescS = make_idesc_t<T>(kTileM, false);
+      constexpr uint32_t kIdescS = make_idesc_t<T>(C::kStream, false);
       constexpr uint32_t kIdescD = make_idesc_t<T>(D, true);
       constexpr uint32_t kHi = desc_hi(1024);
       const uint32_t q_lo = desc_lo(smem_u32(sQ), 16), do_lo = desc_lo(smem_u32(sDO), 16);
-      const uint32_t a_k = desc_lo(smem_u32(sA), 16), a_mn = desc_lo(smem_u32(sA), C::kAtomBytes), b_k = desc_lo(smem_u32(sB), 16);
-      constexpr uint32_t kTile = C::kTileBytes >> 4;
+      const uint32_t a_k = desc_lo(smem_u32(sA), 16), a_mn = desc_lo(smem_u32(sA), C::kStreamAtom), b_k = desc_lo(smem_u32(sB), 16);
+      constexpr uint32_t kTile = C::kStreamBytes >> 4;
       RingPos<C::kA> ks, kd;                 // K of the next S, of the next dQ
       RingPos<C::kB> vs;
       bool alive = mbar_wait(smem_u32(&ctl->own_full), 0u, abort_flag, p.status);
-      auto issue_s = [&](int i) -> bool {
-        if (!(tail && i == n - 1 ? mbar_wait(smem_u32(&ctl->tail_ready), 0u, abort_flag, p.status)
-                                 : mbar_wait(smem_u32(&ctl->a_full[ks.slot]), ks.phase, abort_flag, p.status)))
-          return false;
-        tc_fence_after();
+      // K and V of the next scores and dP are in shared memory
+      auto tiles_here = [&](int i) -> bool {
+        if (tail && i == n - 1) return mbar_wait(smem_u32(&ctl->tail_ready), 0u, abort_flag, p.status);
+        return mbar_wait(smem_u32(&ctl->a_full[ks.slot]), ks.phase, abort_flag, p.status) &&
+               mbar_wait(smem_u32(&ctl->b_full[vs.slot]), vs.phase, abort_flag, p.status);
+      };
+      auto issue_s = [&]() {
         mma_tiles<D>(tmem, q_lo, a_k + (uint32_t)ks.slot * kTile, kIdescS);
         tc_commit(smem_u32(&ctl->s_full));
         ks.next();
-        return true;
       };
-      auto issue_dp = [&](int i) -> bool {
-        // (the last pair of a tail came with K)
-        if (!(tail && i == n - 1) && !mbar_wait(smem_u32(&ctl->b_full[vs.slot]), vs.phase, abort_flag, p.status)) return false;
-        tc_fence_after();
-        mma_tiles<D>(tmem + 128, do_lo, b_k + (uint32_t)vs.slot * kTile, kIdescS);
+      auto issue_dp = [&]() {
+        mma_tiles<D>(tmem + C::kDp, do_lo, b_k + (uint32_t)vs.slot * kTile, kIdescS);
         tc_commit(smem_u32(&ctl->dp_full));
         tc_commit(smem_u32(&ctl->b_free[vs.slot]));
         vs.next();
-        return true;
       };
-      alive = alive && n > 0 && issue_s(0) && issue_dp(0);
+      alive = alive && n > 0 && tiles_here(0);
+      if (alive) {
+        tc_fence_after();
+        issue_s();
+        issue_dp();
+      }
       for (int i = 0; i < n && alive; ++i) {
         if (i + 1 < n) {
-          if (!(alive = mbar_wait(smem_u32(&ctl->s_read), (uint32_t)i & 1u, abort_flag, p.status) && issue_s(i + 1))) break;
-          if (!(alive = mbar_wait(smem_u32(&ctl->dp_read), (uint32_t)i & 1u, abort_flag, p.status) && issue_dp(i + 1))) break;
+          if (!(alive = tiles_here(i + 1) && mbar_wait(smem_u32(&ctl->s_read), (uint32_t)i & 1u, abort_flag, p.status))) break;
+          tc_fence_after();
+          issue_s();
+          if (!(alive = mbar_wait(smem_u32(&ctl->dp_read), (uint32_t)i & 1u, abort_flag, p.status))) break;
+          tc_fence_after();
+          issue_dp();
         }
+        if (!(alive = mbar_wait(smem_u32(&ctl->ds_ready), (uint32_t)i & 1u, abort_flag, p.status))) break;
+        tc_fence_after();
         const uint32_t k_mn = a_mn + (uint32_t)kd.slot * kTile;           // dQ += dS K
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!(alive = mbar_wait(smem_u32(&ctl->ds_ready[h]), (uint32_t)i & 1u, abort_flag, p.status))) break;
-          tc_fence_after();
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            tc_mma_ts(tmem + 256, tmem + 384 + (h * 4 + kk) * 8, k_mn + (h * 4 + kk) * (2048 >> 4), kHi, kIdescD,
-                      h + kk > 0 ? 1u : (i > 0 ? 1u : 0u));
-        }
-        if (!alive) break;
+        for (int kk = 0; kk < 4 * kHalves; ++kk)
+          tc_mma_ts(tmem + C::kSum0, tmem + C::kSum1 + kk * 8, k_mn + kk * (2048 >> 4), kHi, kIdescD, kk > 0 ? 1u : (i > 0 ? 1u : 0u));
         tc_commit(smem_u32(&ctl->a_free[kd.slot]));
         kd.next();
       }
@@ -634,7 +617,7 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
       mbar_wait(smem_u32(&ctl->drain), 0u, abort_flag, p.status);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBwdRegsSoftmax));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
     const int h = warp >> 2;                                 // key columns 64 h .. 64 h + 63 of a block
     const int r = tid & (kTileM - 1);                        // query row
     const int r_tok = r / p.group, r_head = r - r_tok * p.group;
@@ -651,6 +634,7 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
       lse2 = v == -INFINITY ? INFINITY : v;
       delta = p.delta[tok_g * p.heads + head];
     }
+    const uint64_t scale2 = pack2(scale_log2, scale_log2), neg_lse2 = pack2(-lse2, -lse2), neg_delta2 = pack2(-delta, -delta);
     const int seen = kCausal ? min(max(min(tok, last_tok) + 1 + ahead, 0), kr.len) : kr.len;
     RingPos<C::kA> kd;                                       // K of the step before
     bool alive = true;
@@ -667,8 +651,12 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctl->s_read));
 #pragma unroll
-      for (int c = 0; c < 64; ++c) pr[c] = ex2(fmaf(__uint_as_float(s[c]), scale_log2, -lse2));
-      const int limit = seen - i * kTileM - h * 64;          // columns at and past it are not seen
+      for (int c = 0; c < 64; c += 2) {
+        float t0, t1;
+        unpack2(ffma2(pack2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, neg_lse2), t0, t1);
+        pr[c] = ex2(t0), pr[c + 1] = ex2(t1);
+      }
+      const int limit = seen - i * C::kStream - h * 64;          // columns at and past it are not seen
       if (__any_sync(0xffffffffu, limit < 64)) {
 #pragma unroll
         for (int c = 0; c < 64; ++c)
@@ -679,14 +667,17 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
         break;
       }
       tc_fence_after();
-      tmem_ld64(tmem + lane_base + 128 + h * 64, s);
+      tmem_ld64(tmem + lane_base + C::kDp + h * 64, s);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctl->dp_read));
       uint32_t pk[32];
 #pragma unroll
-      for (int c = 0; c < 32; ++c)
-        pk[c] = pack_pair<T>(pr[2 * c] * (__uint_as_float(s[2 * c]) - delta), pr[2 * c + 1] * (__uint_as_float(s[2 * c + 1]) - delta));
+      for (int c = 0; c < 32; ++c) {
+        float t0, t1;
+        unpack2(fmul2(pack2(pr[2 * c], pr[2 * c + 1]), fadd2(pack2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), neg_delta2)), t0, t1);
+        pk[c] = pack_pair<T>(t0, t1);
+      }
       // the product that read the last dS has retired (it also freed that stage)
       if (i > 0) {
         if (!mbar_wait_warp(smem_u32(&ctl->a_free[kd.slot]), kd.phase, abort_flag, p.status)) {
@@ -696,34 +687,35 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
         kd.next();
       }
       tc_fence_after();
-      tmem_st32(tmem + lane_base + 384 + h * 32, pk);
+      tmem_st32(tmem + lane_base + C::kSum1 + h * 32, pk);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready[h]));
+      if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
     }
     if (alive && n > 0) alive = mbar_wait_warp(smem_u32(&ctl->drain), 0u, abort_flag, p.status);
     if (alive) {
       tc_fence_after();
       T* out = (T*)p.dq + tok_g * p.dq_stride[0] + head * p.dq_stride[1];
-      store_half<T, D>(RowAddresses(row_valid ? out : nullptr), tmem + lane_base + 256, h, n > 0, p.sm_scale);
+      store_share<T, D / kHalves>(RowAddresses(row_valid ? out : nullptr), tmem + lane_base + C::kSum0, h, n > 0, p.sm_scale);
     }
   }
-  bwd_teardown(ctl, tmem, warp);
+  bwd_teardown<C>(ctl, tmem, warp);
 }
 
 // ------------------------------------------------------------------------------------ both
 // Blocks of either kind in one launch, so that the shorter dQ blocks fill the SMs that the last dK/dV blocks leave: first
 // dkv_units per key/value head, then dq_units.  Of a causal sequence the first keys and the last queries have most to
 // do, and come first.
-template <typename T, int D, bool kCausal>
-__global__ void __launch_bounds__(kBwdThreads, 1) tra_packed_bwd_kernel(const __grid_constant__ tra_packed_launch p, int dkv_units, int dq_units) {
+template <typename T, int D, int kHalves, bool kCausal>
+__global__ void __launch_bounds__(BwdCfg<D, kHalves>::kThreads, BwdCfg<D, kHalves>::kBlocks)
+    tra_packed_bwd_kernel(const __grid_constant__ tra_packed_launch p, int dkv_units, int dq_units) {
   extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
   const int n_dkv = dkv_units * p.kv_heads, b = blockIdx.x;
   if (b < n_dkv)
-    dkv_block<T, D, kCausal>(p, smem, b % dkv_units, b / dkv_units);
+    dkv_block<T, D, kHalves, kCausal>(p, smem, b % dkv_units, b / dkv_units);
   else
-    dq_block<T, D, kCausal>(p, smem, (b - n_dkv) % dq_units, (b - n_dkv) / dq_units);
+    dq_block<T, D, kHalves, kCausal>(p, smem, (b - n_dkv) % dq_units, (b - n_dkv) / dq_units);
 }
 
 // ------------------------------------------------------------------------------------ delta
@@ -762,7 +754,7 @@ __global__ void __launch_bounds__(256) tra_packed_delta_kernel(const __grid_cons
   if (row < rows && lane == 0) p.delta[row] = s;
 }
 
-template <typename T, int D, bool kCausal>
+template <typename T, int D, int kHalves, bool kCausal>
 int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   const long long rows = (long long)a.total_q * a.heads;
   int rc = TRA_OK;
@@ -776,16 +768,17 @@ int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   const long long blocks = ((long long)dkv_units + dq_units) * a.kv_heads;
   if (blocks == 0) return TRA_OK;
   if (blocks > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
-  constexpr auto kern = tra_packed_bwd_kernel<T, D, kCausal>;
-  if ((rc = tra_allow_smem<kern>(BwdCfg<D>::kSmemBytes)) != TRA_OK) return rc;
-  return tra_launch(kern, dim3((unsigned)blocks), kBwdThreads, BwdCfg<D>::kSmemBytes, c.stream, rows > 0, 1, a, dkv_units, dq_units);
+  using C = BwdCfg<D, kHalves>;
+  constexpr auto kern = tra_packed_bwd_kernel<T, D, kHalves, kCausal>;
+  if ((rc = tra_allow_smem<kern>(C::kSmemBytes)) != TRA_OK) return rc;
+  return tra_launch(kern, dim3((unsigned)blocks), C::kThreads, C::kSmemBytes, c.stream, rows > 0, 1, a, dkv_units, dq_units);
 }
 
-template <int D>
+template <int D, int kHalves>
 int launch_bwd_shape(const tra_packed_ctx& c, const tra_packed_launch& a) {
   if (c.h->cfg.dtype == TRA_BF16)
-    return a.causal ? launch_bwd<__nv_bfloat16, D, true>(c, a) : launch_bwd<__nv_bfloat16, D, false>(c, a);
-  return a.causal ? launch_bwd<__half, D, true>(c, a) : launch_bwd<__half, D, false>(c, a);
+    return a.causal ? launch_bwd<__nv_bfloat16, D, kHalves, true>(c, a) : launch_bwd<__nv_bfloat16, D, kHalves, false>(c, a);
+  return a.causal ? launch_bwd<__half, D, kHalves, true>(c, a) : launch_bwd<__half, D, kHalves, false>(c, a);
 }
 
 }  // namespace

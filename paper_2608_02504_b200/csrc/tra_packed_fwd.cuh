@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
   volatile int* abort_flag = &ctl->abort_flag;
 
   if (warp == 9) {
-    tmem_alloc_all(&ctl->tmem_base);
+    tmem_alloc<512>(&ctl->tmem_base);
   } else if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&ctl->work_full[i]), 1);
@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
     }
     tc_fence_after();
-    tmem_free_all(tmem);
+    tmem_free<512>(tmem);
   }
 }
 
