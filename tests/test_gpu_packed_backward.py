@@ -65,6 +65,16 @@ def test_groups(api, group):
 
 
 @pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("group", [1, 4, 12, 13, 20, 22, 32, 33])
+def test_streamed_tiles(api, causal, group):
+    """Lengths about the tiles that the blocks stream: 64 keys or 64 rows (64 / group tokens) at head_dim 64, 128 where that
+    would leave rows empty."""
+    t = 64 // group
+    run(api, BF, 64, group, 1, causal, [63, 64, 65, 1, 127, 128, 129, 191, 193])
+    run(api, HALF, 64, 2 * group, 2, causal, [t, 2 * t + 1, 3 * t, 1], [65, 64 + t, 320, 63])
+
+
+@pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (HALF, 64)])
 def test_more_or_fewer_keys_than_queries(api, causal, dtype, d):
     run(api, dtype, d, 4, 2, causal, [100, 40, 60, 300, 20], [1000, 40, 25, 7, 0])
