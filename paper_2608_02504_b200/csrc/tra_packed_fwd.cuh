@@ -42,6 +42,10 @@ struct FwdCfg {
   static constexpr int kSmemNeeded = kSmemData + 512 /*barriers*/;
   // at least 120 KB so that one block owns an SM and its whole tensor memory
   static constexpr int kSmemBytes = kSmemNeeded > 120 * 1024 ? kSmemNeeded : 120 * 1024;
+  // The issuing warp's values in uniform registers (see uniform() and the gradients' kernel).  D = 128 is bound by the tensor pipe: four
+  // causal sequences of 4,096 tokens, 40 / 8 heads, 0.752 -> 0.669 ms.  D = 64 is bound by the softmax warps, and the votes
+  // cost more than they give: 0.42 -> 0.45 ms with 16 heads.
+  static constexpr bool kUniform = D == 128;
 };
 
 // One unit of work: a pair of query tiles of a (sequence, key/value head), over one part of its key blocks.
@@ -171,7 +175,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
   uint8_t* sQ = smem;
   uint8_t* sKV = smem + 2 * C::kTileBytes;
   FwdCtl* ctl = (FwdCtl*)(smem + C::kSmemData);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = uniform_if<C::kUniform>(tid >> 5), lane = tid & 31;
   const int box_rows = p.tile_tokens * p.group;
   volatile int* abort_flag = &ctl->abort_flag;
 
@@ -339,6 +343,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       }
     } else if (warp == 9) {
       // ================================================================== MMA issuer
+      auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+        return C::kUniform ? mbar_wait_warp(bar, parity, abort_flag, p.status) : mbar_wait(bar, parity, abort_flag, p.status);
+      };
+      const uint32_t tmem = uniform_if<C::kUniform>(ctl->tmem_base);
       constexpr uint32_t kIdescQK = make_idesc_t<T>(kKeyTile, false);
       constexpr uint32_t kIdescPV = make_idesc_t<T>(D, true);
       constexpr uint32_t kHi = desc_hi(1024);
@@ -359,7 +367,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         const uint32_t d = tmem + 256 + k * 128, pa = tmem + k * 128;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          if (!mbar_wait(smem_u32(&ctl->p_ready[k][half]), parity, abort_flag, p.status)) return false;
+          if (!wait(smem_u32(&ctl->p_ready[k][half]), parity)) return false;
           tc_fence_after();
 #pragma unroll
           for (int kk = half * 4; kk < half * 4 + 4; ++kk)
@@ -379,13 +387,17 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       uint32_t entries[2] = {0u, 0u};        // key blocks of a tile so far
       uint32_t sums[2] = {0u, 0u};           // units in which the tile had any
       bool alive = true;
-      for (int n = 0; alive && next_work(n); ++n) {
+      for (int n = 0; alive && uniform_if<C::kUniform>(next_work(n)); ++n) {
         const FwdWork w = ctl->work[n & 1];
         done_with_work(n);
-        const FwdPlan<kCausal> u(w, p);
+        FwdPlan<kCausal> u(w, p);
+        u.n_entries = uniform_if<C::kUniform>(u.n_entries);
+        u.n_own[0] = uniform_if<C::kUniform>(u.n_own[0]);
+        u.n_own[1] = uniform_if<C::kUniform>(u.n_own[1]);
+        u.tail = uniform_if<C::kUniform>(u.tail);
         if (u.n_entries == 0) continue;
-        alive = mbar_wait(smem_u32(&ctl->q_full), units & 1u, abort_flag, p.status) &&
-                mbar_wait(smem_u32(&ctl->kv_full[slot]), phase, abort_flag, p.status);       // first K tile
+        alive = wait(smem_u32(&ctl->q_full), units & 1u) &&
+                wait(smem_u32(&ctl->kv_full[slot]), phase);       // first K tile
         if (!alive) break;
         tc_fence_after();
 #pragma unroll
@@ -397,9 +409,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         for (int e = 0; e < u.n_entries; ++e) {
           const int vslot = slot;
           const bool have_next = e + 1 < u.n_entries;
-          alive = mbar_wait(smem_u32(&ctl->kv_full[vslot]), phase, abort_flag, p.status);
+          alive = wait(smem_u32(&ctl->kv_full[vslot]), phase);
           if (alive && u.tail && !have_next) {
-            alive = mbar_wait(smem_u32(&ctl->tail_ready[tails & 1]), (tails >> 1) & 1u, abort_flag, p.status);
+            alive = wait(smem_u32(&ctl->tail_ready[tails & 1]), (tails >> 1) & 1u);
             ++tails;
           }
           advance();
@@ -409,7 +421,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
             if (!alive || e >= u.n_own[k]) continue;
             if (e == 0) {
               // the sum of the tile's last unit has been read
-              if (sums[k] > 0 && !(alive = mbar_wait(smem_u32(&ctl->o_free[k]), (sums[k] - 1) & 1u, abort_flag, p.status))) continue;
+              if (sums[k] > 0 && !(alive = wait(smem_u32(&ctl->o_free[k]), (sums[k] - 1) & 1u))) continue;
               ++sums[k];
             }
             if (!(alive = issue_pv(k, vslot, entries[k] & 1u, e > 0 ? 1u : 0u))) continue;
@@ -418,7 +430,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
               tc_commit(smem_u32(&ctl->o_full[k]));
             } else {
               if (!k_ready) {
-                alive = mbar_wait(smem_u32(&ctl->kv_full[slot]), phase, abort_flag, p.status);
+                alive = wait(smem_u32(&ctl->kv_full[slot]), phase);
                 k_ready = true;
                 if (!alive) continue;
                 tc_fence_after();
@@ -435,7 +447,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       }
       // every MMA has retired before tensor memory is released
       tc_commit(smem_u32(&ctl->drain));
-      mbar_wait(smem_u32(&ctl->drain), 0u, abort_flag, p.status);
+      wait(smem_u32(&ctl->drain), 0u);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kFwdRegsSoftmax));

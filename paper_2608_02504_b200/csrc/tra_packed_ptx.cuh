@@ -74,6 +74,21 @@ __device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+// A value that all lanes hold, in a form that the compiler knows to be the same in all of them (a warp reduction's or a vote's
+// result).  tcgen05.mma takes its descriptors from uniform registers; where the compiler cannot tell that they are uniform (values
+// read from shared memory, or computed under a condition that a lane's own wait decided) every product spends 70 to 85 cycles on
+// moving them there, more than a product of 64 columns takes.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
+__device__ __forceinline__ int uniform(int x) { return (int)__reduce_or_sync(0xffffffffu, (unsigned)x); }
+__device__ __forceinline__ bool uniform(bool x) { return __any_sync(0xffffffffu, x) != 0; }
+template <bool kYes, typename V>
+__device__ __forceinline__ V uniform_if(V x) {
+  if constexpr (kYes)
+    return uniform(x);
+  else
+    return x;
+}
+
 // A launch that follows another one in the stream starts while it ends: the first one allows it (once all its blocks run),
 // the second waits where it needs the first one's results.
 __device__ __forceinline__ void allow_next_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
