@@ -11,6 +11,9 @@
 // Seven products instead of the five that one pass over the pairs needs: the fifth sum, dQ, would have to leave the
 // block through memory (fp32 atomics whose order changes the result, or 4 bytes per row, channel and key block).
 //
+// 4,096 tokens, 16 heads, d 128: 0.36 ms (957 TFLOP/s of the five products that the gradients need, 1,340 of the seven); four causal
+// sequences of them, 40 / 8 heads: 2.13 ms (807); four, 16 heads, d 64: 1.09 ms (630); nine of 1,560, 12 heads, d 64: 0.40 ms.
+//
 // Order on the tensor pipe, so that it always has a product that waits for nobody:
 //   dkv: S(i+1) as soon as the threads hold dP(i) in registers, dV(i), then dK(i), dP(i+1): the threads turn dP(i) into dS(i)
 //        under the first two and S(i+1) into P(i+1) under the last two;
@@ -32,8 +35,8 @@ constexpr int kStatStages = 2;           // of the query rows' lse and delta (dk
 
 // kHalves: groups of 64 columns that a step walks, with one warpgroup of softmax threads each.
 //   2: streamed tiles of 128 rows, one block per SM.
-//   1: streamed tiles of 64 rows, half of the tensor memory, two blocks per SM: where the products are short (D = 64) the serial
-//      part of a step and the blocks' starts and ends are hidden by the other block.
+//   1: streamed tiles of 64 rows, half of the tensor memory, two blocks per SM: where the products are short (D = 64) one block's
+//      start and end are hidden by the other (nine sequences of 1,560 tokens, 12 heads: 0.46 -> 0.40 ms; of 4,096: level).
 template <int D, int kHalves>
 struct BwdCfg {
   static constexpr int kAtoms = D / 64;

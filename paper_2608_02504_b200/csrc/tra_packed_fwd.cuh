@@ -17,7 +17,8 @@
 // Split launches give every unit a range of the key blocks; the parts O / l and log2 l go to a
 // workspace and tra_packed_join_kernel adds them.
 //
-// Bound: tensor cores, at the power cap (see tra_attn_kernel.cuh), for long sequences.
+// Bound: tensor cores, at the power cap (see tra_attn_kernel.cuh), for long sequences: two of 32,760 tokens and one of 10,921, 12 heads, d
+// 128, 11.1 ms (1,250 TFLOP/s); eight causal prompts of 1 to 8,192 tokens, 40 / 8 heads, 775 us (1,180 TFLOP/s), 0.9 ms back to back.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -42,10 +43,6 @@ struct FwdCfg {
   static constexpr int kSmemNeeded = kSmemData + 512 /*barriers*/;
   // at least 120 KB so that one block owns an SM and its whole tensor memory
   static constexpr int kSmemBytes = kSmemNeeded > 120 * 1024 ? kSmemNeeded : 120 * 1024;
-  // The issuing warp's values in uniform registers (see uniform() and the gradients' kernel).  D = 128 is bound by the tensor pipe: four
-  // causal sequences of 4,096 tokens, 40 / 8 heads, 0.752 -> 0.669 ms.  D = 64 is bound by the softmax warps, and the votes
-  // cost more than they give: 0.42 -> 0.45 ms with 16 heads.
-  static constexpr bool kUniform = D == 128;
 };
 
 // One unit of work: a pair of query tiles of a (sequence, key/value head), over one part of its key blocks.
@@ -175,7 +172,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
   uint8_t* sQ = smem;
   uint8_t* sKV = smem + 2 * C::kTileBytes;
   FwdCtl* ctl = (FwdCtl*)(smem + C::kSmemData);
-  const int tid = threadIdx.x, warp = uniform_if<C::kUniform>(tid >> 5), lane = tid & 31;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int box_rows = p.tile_tokens * p.group;
   volatile int* abort_flag = &ctl->abort_flag;
 
@@ -230,8 +227,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFwdRegsControl));
     if (warp == 11) {
       // ================================================================== scheduler
-      // The grid has a block per unit, in launch order: a sequence's last tiles come first, which are the longest of a causal one.  A running block takes over blocks that have not been started yet, one at a time (cluster
-      // launch control), and so balances units of different lengths without a counter in memory.
+      // The grid has a block per unit, in launch order: a sequence's last tiles come first, which are the longest of a causal
+      // one.  A running block takes over blocks that have not been started yet, one at a time (cluster launch control), and so balances units of different lengths without a counter in memory.
       // The request is made when the producer is about to run out of loads: units taken over early are units that an idle block
       // cannot have.
       int n = 0, unit = blockIdx.x;
@@ -343,10 +340,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       }
     } else if (warp == 9) {
       // ================================================================== MMA issuer
-      auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-        return C::kUniform ? mbar_wait_warp(bar, parity, abort_flag, p.status) : mbar_wait(bar, parity, abort_flag, p.status);
-      };
-      const uint32_t tmem = uniform_if<C::kUniform>(ctl->tmem_base);
+      // Waits end in a vote and values from shared memory in a reduction, so that descriptors stay in uniform registers (four
+      // sequences of 4,096 tokens: causal, 40 / 8 heads, d 128 0.750 -> 0.675 ms; 16 heads, d 64 0.389 -> 0.373, causal 0.273 -> 0.250).
+      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_flag, p.status); };
+      const uint32_t tmem = uniform(ctl->tmem_base);
       constexpr uint32_t kIdescQK = make_idesc_t<T>(kKeyTile, false);
       constexpr uint32_t kIdescPV = make_idesc_t<T>(D, true);
       constexpr uint32_t kHi = desc_hi(1024);
@@ -387,14 +384,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       uint32_t entries[2] = {0u, 0u};        // key blocks of a tile so far
       uint32_t sums[2] = {0u, 0u};           // units in which the tile had any
       bool alive = true;
-      for (int n = 0; alive && uniform_if<C::kUniform>(next_work(n)); ++n) {
+      for (int n = 0; alive && uniform(next_work(n)); ++n) {
         const FwdWork w = ctl->work[n & 1];
         done_with_work(n);
         FwdPlan<kCausal> u(w, p);
-        u.n_entries = uniform_if<C::kUniform>(u.n_entries);
-        u.n_own[0] = uniform_if<C::kUniform>(u.n_own[0]);
-        u.n_own[1] = uniform_if<C::kUniform>(u.n_own[1]);
-        u.tail = uniform_if<C::kUniform>(u.tail);
+        u.n_entries = uniform(u.n_entries);
+        u.n_own[0] = uniform(u.n_own[0]);
+        u.n_own[1] = uniform(u.n_own[1]);
+        u.tail = uniform(u.tail);
         if (u.n_entries == 0) continue;
         alive = wait(smem_u32(&ctl->q_full), units & 1u) &&
                 wait(smem_u32(&ctl->kv_full[slot]), phase);       // first K tile

@@ -81,13 +81,6 @@ __device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
 __device__ __forceinline__ int uniform(int x) { return (int)__reduce_or_sync(0xffffffffu, (unsigned)x); }
 __device__ __forceinline__ bool uniform(bool x) { return __any_sync(0xffffffffu, x) != 0; }
-template <bool kYes, typename V>
-__device__ __forceinline__ V uniform_if(V x) {
-  if constexpr (kYes)
-    return uniform(x);
-  else
-    return x;
-}
 
 // A launch that follows another one in the stream starts while it ends: the first one allows it (once all its blocks run),
 // the second waits where it needs the first one's results.

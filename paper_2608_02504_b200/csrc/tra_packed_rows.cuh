@@ -8,6 +8,9 @@
 // a 128-row tcgen05 tile would spend its softmax on 112 rows that are not there (128 threads walk 128 score columns per key
 // block whatever the rows hold), and the tensor pipe is idle either way.
 //
+// 64 caches of 700 to 32,768 keys, 40 / 8 heads, d 128: 686 us, 6.4 TB/s (98 % of the copy rate).  One cache of 777 keys, 12 heads, d 64:
+// 5.5 us on the GPU.
+//
 // The parts of a sequence: up to eight are one thread-block cluster and are joined through distributed shared memory, without
 // a workspace or a second launch; more go through a workspace and tra_packed_join_kernel.
 #pragma once
