@@ -368,8 +368,8 @@ int tra_rotary_backward(const tra_rotary_t* rot, const tra_plan_t* plan, const i
  *   O = softmax(sm_scale Q K^T) V,  lse = log sum exp of the scores a query sees, fp32 [total_q, heads].
  * A query that sees no key gets O = 0 and lse = -inf.  Rows of O and lse in front of cu_q[0] and behind cu_q[n_seq] are
  * left as they were.  What lies in K and V outside a sequence's range, or in Q outside of all, is never used and may be
- * anything, NaN too.  (Inside a sequence a hidden key's weight is 0, but 0 * NaN is NaN: a value that is not finite can reach
- * queries that do not see its key.) */
+ * anything, NaN too.  (Inside a sequence a NaN among the scores that a query sees makes its O and lse NaN; a hidden key's weight is
+ * 0, but 0 * NaN is NaN: a value that is not finite can reach queries that do not see its key.) */
 typedef struct tra_packed tra_packed_t; /* opaque: head layout, type, order, a device status word */
 
 typedef struct {

@@ -294,14 +294,16 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
         *reinterpret_cast<float2*>(dst + i * 8 + tig * 2) = make_float2(o[i][half * 2], o[i][half * 2 + 1]);
       if (tig == 0) {
         float* st = stat + (warp * kRowsMax + r) * 4;
-        st[0] = gave_up ? -INFINITY : m[half];
-        st[1] = l[half];
+        st[0] = m[half];
+        st[1] = gave_up ? 0.f : l[half];
         st[2] = le[half];
       }
     }
   }
   __syncthreads();
-  // rows of the parts `st(w)`, `row(w)` of n (warps of a block, then blocks of a cluster) on one reference
+  // Rows of the parts `st(w)`, `row(w)` of n (warps of a block, then blocks of a cluster) on one reference.  A part has seen nothing
+  // when its sum is 0, not when its maximum is -inf: scores of NaN leave the maximum where it is, and their NaN in the sums
+  // has to reach the result (0 * NaN is NaN).
   auto join = [](int n, auto st, auto row, float& ref, float& sl, float& se, float4& acc) {
     float top = -INFINITY;
     for (int w = 0; w < n; ++w) top = fmaxf(top, st(w).x);
@@ -311,7 +313,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
     for (int w = 0; w < n; ++w) {
       const float4 t = st(w), v = row(w);
       const float f = ex2(t.x - ref);
-      if (t.x == -INFINITY) continue;                        // nothing seen there
+      if (t.y == 0.f) continue;                              // nothing seen there
       sl += f * t.y;
       se += f * t.z;
       acc.x += f * v.x;
