@@ -416,7 +416,9 @@ int tra_packed_attn(const tra_packed_t* packed, const tra_packed_args_t* args, v
 /* Gradients of a forward call over PACKED keys (args->k_end must be args->k_begin + 1: ascending bounds, so that no key
  * belongs to two sequences).  args as in the forward call, with its o and lse.  dq, dk, dv are written for the rows of the
  * sequences (zeros where nothing is seen) and left alone elsewhere; sums of gradients that heads share are formed in fp32
- * inside one thread block: no atomics, the same bits every time.  d_o outside the sequences may be anything.
+ * inside one thread block: the same bits every time.  d_o outside the sequences may be anything.
+ * fp16: the probabilities and their gradients are rounded for their products as multiples by powers of two that follow the
+ * largest rows of d_o and v of a key/value head, so that the relative precision does not depend on the size of d_o.
  *   workspace: device memory of tra_packed_attn_backward_workspace_bytes, as for the forward call. */
 typedef struct {
   const void* d_o;        /* the gradient of o */

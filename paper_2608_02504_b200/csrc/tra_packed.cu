@@ -337,7 +337,9 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
 }
 
 extern "C" size_t tra_packed_attn_backward_workspace_bytes(const tra_packed_t* h, int total_q) {
-  return h && total_q > 0 ? sizeof(float) * (size_t)total_q * h->cfg.heads : 0;
+  if (!h || total_q <= 0) return 0;
+  // delta, and (fp16) the largest norms behind it
+  return sizeof(float) * ((size_t)total_q * h->cfg.heads + (h->cfg.dtype == TRA_FP16 ? 2 * (size_t)h->cfg.kv_heads : 0));
 }
 
 extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_args_t* a, const tra_packed_grads_t* g,
@@ -357,6 +359,7 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
     if (workspace_bytes < tra_packed_attn_backward_workspace_bytes(h, a->total_q)) return TRA_ERR_CAPACITY;
   }
   p.delta = (float*)workspace;
+  p.norms = (uint32_t*)workspace + (long long)a->total_q * p.heads;
   p.o_in = a->o, p.d_o = g->d_o;
   p.dq = g->dq, p.dk = g->dk, p.dv = g->dv;
   for (int i = 0; i < 2; ++i) {

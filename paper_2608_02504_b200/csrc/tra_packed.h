@@ -27,6 +27,7 @@ struct tra_packed_launch {
   float* part_lse2;            //   [splits][total_q][heads] base-2 log of the sum the part was divided by
   float* part_exact;           //   [splits][total_q][heads] base-2 log of the unrounded sum (lse asked for) or NULL
   float* delta;                // backward: [total_q][heads] sum of dO O
+  uint32_t* norms;             // backward, fp16: [2][kv_heads] bits of the largest squared norm of a row of dO, of V
   long long q_stride[2], k_stride[2], v_stride[2], o_stride[2], do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2];
   const int32_t *cu_q, *k_begin, *k_end;
   int n_seq, total_q, total_k, max_q, max_k;

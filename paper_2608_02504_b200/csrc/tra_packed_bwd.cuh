@@ -33,6 +33,24 @@ namespace {
 
 constexpr int kStatStages = 2;           // of the query rows' lse and delta (dkv)
 
+// fp16 holds P and dS = P (dP - delta) for their products only where they are not small: below 2^-14 its steps stop shrinking, and
+// a long row's P, or any row's dS under a small dO, lies there (4,096 keys seen evenly, |dO| 1e-4: dS off by 6 %, at 1e-5 all of it 0).
+// So both are rounded in fp16 as multiples, by powers of two that the epilogue's fp32 factor takes out again:
+//   P 2^12: P <= 1 up to the error of its exponent, so 2^12 leaves four binades for that; full precision down to P = 2^-26;
+//   dP - delta times tau, the power of two that brings its bound 2 max|dO row| max|V row| into (1/2, 2] (|delta| is a mean of the dP):
+//   dS 2^12 tau <= 2^13, full precision 27 binades down.  The maxima, over the rows of a key/value head's sequences, are formed beside
+//   delta (atomic maxima: the same bits in any order).  bf16 has the range of fp32 and needs none of it.
+template <typename T>
+constexpr bool kScaled = std::is_same<T, __half>::value;
+constexpr float kProbLog2 = 12.f, kProbMul = 4096.f;
+
+__device__ __forceinline__ float grad_tau(const tra_packed_launch& p, int kvh) {
+  const float x = __uint_as_float(p.norms[kvh]) * __uint_as_float(p.norms[p.kv_heads + kvh]);      // 2^-96 .. 2^78, or 0
+  if (!(x > 0.f)) return 1.f;
+  const int e = (int)(__float_as_uint(x) >> 23) - 127;               // 2 sqrt(x) < 2^(1 + (e + 1) / 2)
+  return __uint_as_float((uint32_t)(127 - ((e + 2) >> 1)) << 23);
+}
+
 // kHalves: groups of 64 columns that a step walks, with one warpgroup of softmax threads each.
 //   2: streamed tiles of 128 rows, one block per SM.
 //   1: streamed tiles of 64 rows, half of the tensor memory, two blocks per SM: where the products are short (D = 64) one block's
@@ -79,6 +97,7 @@ struct BwdCtl {
   uint64_t drain;
   uint32_t tmem_base;
   int abort_flag;
+  float tau;                             // fp16: see kScaled (dkv)
   tra_unit unit;
 };
 static_assert(sizeof(BwdCtl) <= 512, "control block");
@@ -292,6 +311,11 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
     } else if (warp == C::kSoftWarps + 3) {
       // ================================================================== lse and delta of the query rows
       wait_last_launch();                                 // delta
+      float tau = 1.f;
+      if (kScaled<T> && n > 0) {
+        tau = grad_tau(p, kvh);
+        if (lane == 0) ctl->tau = tau;                    // read behind the first stat_full
+      }
       // read before the wait for the slot, so that the loads' latency is not added to it
       constexpr int kPer = C::kStream / 32;
       int r_tok[kPer], r_row[kPer];
@@ -319,8 +343,9 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
           break;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {                     // negated for the packed multiply-add
-          s_lse2[st * C::kStream + k * 32 + lane] = lse2[k] == -INFINITY ? -INFINITY : -lse2[k] * kLog2e;
-          s_delta[st * C::kStream + k * 32 + lane] = -delta[k];
+          s_lse2[st * C::kStream + k * 32 + lane] =
+              lse2[k] == -INFINITY ? -INFINITY : kScaled<T> ? fmaf(-lse2[k], kLog2e, kProbLog2) : -lse2[k] * kLog2e;
+          s_delta[st * C::kStream + k * 32 + lane] = -delta[k] * tau;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->stat_full[st]));
@@ -450,13 +475,16 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctl->dp_read));
       {
+        const float tau = kScaled<T> ? *(volatile float*)&ctl->tau : 1.f;
+        const uint64_t tau2 = pack2(tau, tau);
+        auto minus_delta = [&](uint64_t dp, uint64_t neg_delta) { return kScaled<T> ? ffma2(dp, tau2, neg_delta) : fadd2(dp, neg_delta); };
         uint32_t pk[32];
 #pragma unroll
         for (int c4 = 0; c4 < 16; ++c4) {
           const ulonglong2 v = delta4[c4];
           float t[4];
-          unpack2(fmul2(pack2(pr[c4 * 4], pr[c4 * 4 + 1]), fadd2(pack2(__uint_as_float(s[c4 * 4]), __uint_as_float(s[c4 * 4 + 1])), v.x)), t[0], t[1]);
-          unpack2(fmul2(pack2(pr[c4 * 4 + 2], pr[c4 * 4 + 3]), fadd2(pack2(__uint_as_float(s[c4 * 4 + 2]), __uint_as_float(s[c4 * 4 + 3])), v.y)), t[2], t[3]);
+          unpack2(fmul2(pack2(pr[c4 * 4], pr[c4 * 4 + 1]), minus_delta(pack2(__uint_as_float(s[c4 * 4]), __uint_as_float(s[c4 * 4 + 1])), v.x)), t[0], t[1]);
+          unpack2(fmul2(pack2(pr[c4 * 4 + 2], pr[c4 * 4 + 3]), minus_delta(pack2(__uint_as_float(s[c4 * 4 + 2]), __uint_as_float(s[c4 * 4 + 3])), v.y)), t[2], t[3]);
           pk[c4 * 2] = pack_pair<T>(t[0], t[1]);
           pk[c4 * 2 + 1] = pack_pair<T>(t[2], t[3]);
         }
@@ -479,11 +507,13 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
       const int key = *(volatile int*)&ctl->unit.index * kTileM + r;
       const bool row_valid = key < *(volatile int*)&ctl->unit.k.len;
       const long long row = *(volatile int*)&ctl->unit.k.begin + (row_valid ? key : 0);
+      const float mul = kScaled<T> && n > 0 ? 1.f / kProbMul : 1.f;
+      const float mul_k = kScaled<T> && n > 0 ? p.sm_scale / (kProbMul * *(volatile float*)&ctl->tau) : p.sm_scale;
       T* out[2] = {(T*)p.dv + row * p.dv_stride[0] + kvh * p.dv_stride[1], (T*)p.dk + row * p.dk_stride[0] + kvh * p.dk_stride[1]};
 #pragma unroll 1
       for (int which = 0; which < 2; ++which)
         store_share<T, D / kHalves>(RowAddresses(row_valid ? out[which] : nullptr), tmem + lane_base + (which ? C::kSum1 : C::kSum0), h, n > 0,
-                         which ? p.sm_scale : 1.f);
+                         which ? mul_k : mul);
     }
   }
   bwd_teardown<C>(ctl, tmem, warp);
@@ -645,7 +675,10 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
       lse2 = v == -INFINITY ? INFINITY : v;
       delta = p.delta[tok_g * p.heads + head];
     }
+    const float tau = kScaled<T> && n > 0 ? grad_tau(p, kvh) * kProbMul : 1.f;      // dS times it, as in dkv_block
+    delta *= tau;
     const uint64_t scale2 = pack2(scale_log2, scale_log2), neg_lse2 = pack2(-lse2, -lse2), neg_delta2 = pack2(-delta, -delta);
+    const uint64_t tau2 = pack2(tau, tau);
     const int seen = kCausal ? min(max(min(tok, last_tok) + 1 + ahead, 0), kr.len) : kr.len;
     RingPos<C::kA> kd;                                       // K of the step before
     bool alive = true;
@@ -686,7 +719,8 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
 #pragma unroll
       for (int c = 0; c < 32; ++c) {
         float t0, t1;
-        unpack2(fmul2(pack2(pr[2 * c], pr[2 * c + 1]), fadd2(pack2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), neg_delta2)), t0, t1);
+        const uint64_t dp = pack2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
+        unpack2(fmul2(pack2(pr[2 * c], pr[2 * c + 1]), kScaled<T> ? ffma2(dp, tau2, neg_delta2) : fadd2(dp, neg_delta2)), t0, t1);
         pk[c] = pack_pair<T>(t0, t1);
       }
       // the product that read the last dS has retired (it also freed that stage)
@@ -708,7 +742,7 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
     if (alive) {
       tc_fence_after();
       T* out = (T*)p.dq + tok_g * p.dq_stride[0] + head * p.dq_stride[1];
-      store_share<T, D / kHalves>(RowAddresses(row_valid ? out : nullptr), tmem + lane_base + C::kSum0, h, n > 0, p.sm_scale);
+      store_share<T, D / kHalves>(RowAddresses(row_valid ? out : nullptr), tmem + lane_base + C::kSum0, h, n > 0, kScaled<T> ? p.sm_scale / tau : p.sm_scale);
     }
   }
   bwd_teardown<C>(ctl, tmem, warp);
@@ -733,6 +767,37 @@ __global__ void __launch_bounds__(BwdCfg<D, kHalves>::kThreads, BwdCfg<D, kHalve
 // delta = sum over the channels of dO O, d / 8 threads per (token, head), 16 bytes each.  O with what its rounding took, when the
 // forward call kept it: P (dP - delta) cancels where a row sees few keys or one dominates, and there the rounding of O is
 // the larger part of what is left (two tokens, bf16: 9.4e-3 of a gradient, 3.3e-3 with the remainder).
+// One thread's share of a row: eight channels of dO (o and its remainder).
+template <typename T, int D>
+__device__ __forceinline__ float delta_share(const tra_packed_launch& p, long long tok, int head, int lane, const uint4& d_o) {
+  const uint4 a = *reinterpret_cast<const uint4*>((const T*)p.o_in + tok * p.o_stride[0] + head * p.o_stride[1] + lane * 8);
+  const uint4 c = p.o_rest ? *reinterpret_cast<const uint4*>((const T*)p.o_rest + (tok * p.heads + head) * D + lane * 8) : make_uint4(0u, 0u, 0u, 0u);
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {d_o.x, d_o.y, d_o.z, d_o.w}, z[4] = {c.x, c.y, c.z, c.w};
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x0, x1, y0, y1, z0, z1;
+    unpack_pair<T>(x[i], x0, x1);
+    unpack_pair<T>(y[i], y0, y1);
+    unpack_pair<T>(z[i], z0, z1);
+    x0 += z0;
+    x1 += z1;
+    s = fmaf(x0, y0, s);
+    s = fmaf(x1, y1, s);
+  }
+  return s;
+}
+template <int kLanes>
+__device__ __forceinline__ float sum_lanes(float s) {
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
+}
+template <typename T>
+__device__ __forceinline__ const uint4& row_piece(const void* base, const long long* stride, long long tok, int head, int lane) {
+  return *reinterpret_cast<const uint4*>((const T*)base + tok * stride[0] + head * stride[1] + lane * 8);
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(256) tra_packed_delta_kernel(const __grid_constant__ tra_packed_launch p) {
   constexpr int kLanes = D / 8;
@@ -744,25 +809,70 @@ __global__ void __launch_bounds__(256) tra_packed_delta_kernel(const __grid_cons
   if (row < rows) {
     const long long tok = row / p.heads;
     const int head = (int)(row - tok * p.heads);
-    const uint4 a = *reinterpret_cast<const uint4*>((const T*)p.o_in + tok * p.o_stride[0] + head * p.o_stride[1] + lane * 8);
-    const uint4 b = *reinterpret_cast<const uint4*>((const T*)p.d_o + tok * p.do_stride[0] + head * p.do_stride[1] + lane * 8);
-    const uint4 c = p.o_rest ? *reinterpret_cast<const uint4*>((const T*)p.o_rest + row * D + lane * 8) : make_uint4(0u, 0u, 0u, 0u);
-    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w}, z[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float x0, x1, y0, y1, z0, z1;
-      unpack_pair<T>(x[i], x0, x1);
-      unpack_pair<T>(y[i], y0, y1);
-      unpack_pair<T>(z[i], z0, z1);
-      x0 += z0;
-      x1 += z1;
-      s = fmaf(x0, y0, s);
-      s = fmaf(x1, y1, s);
-    }
+    s = delta_share<T, D>(p, tok, head, lane, row_piece<T>(p.d_o, p.do_stride, tok, head, lane));
   }
-#pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  s = sum_lanes<kLanes>(s);
   if (row < rows && lane == 0) p.delta[row] = s;
+}
+
+// fp16: delta, and the largest squared norms behind grad_tau, of the rows of dO and of V that belong to a sequence and are finite.  A block
+// takes `steps` times 256 / (d / 8) tokens of one head, first the heads of dO, then those of V, and leaves one atomic maximum behind (rows
+// of mixed heads, as above, would leave one each: 12 -> 25 us at 14,040 tokens, 12 heads, d 64).
+template <int D>
+__global__ void __launch_bounds__(256) tra_packed_delta_norms_kernel(const __grid_constant__ tra_packed_launch p, int q_blocks, int steps) {
+  using T = __half;
+  constexpr int kLanes = D / 8, kRows = 256 / kLanes;
+  __shared__ uint32_t s_largest[8];
+  allow_next_launch();
+  const int lane = threadIdx.x % kLanes;
+  const bool of_v = (int)blockIdx.x >= q_blocks;
+  const int heads = of_v ? p.kv_heads : p.heads, total = of_v ? p.total_k : p.total_q;
+  const int b = (int)blockIdx.x - (of_v ? q_blocks : 0), head = b % heads;
+  const int from = of_v ? p.k_begin[0] : p.cu_q[0], to = of_v ? p.k_end[p.n_seq - 1] : p.cu_q[p.n_seq];
+  long long tok = (long long)(b / heads) * steps * kRows + threadIdx.x / kLanes;
+  float largest = 0.f;
+  for (int i = 0; i < steps; ++i, tok += kRows) {
+    const bool there = tok < total, counts = there && tok >= from && tok < to;
+    uint4 x = make_uint4(0u, 0u, 0u, 0u);
+    float dot = 0.f, squares = 0.f;
+    if (of_v) {
+      if (counts) x = row_piece<T>(p.v, p.v_stride, tok, head, lane);
+    } else if (there) {
+      x = row_piece<T>(p.d_o, p.do_stride, tok, head, lane);
+      dot = delta_share<T, D>(p, tok, head, lane, x);
+    }
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float lo, hi;
+      unpack_pair<T>(w[k], lo, hi);
+      squares = fmaf(lo, lo, fmaf(hi, hi, squares));
+    }
+    squares = sum_lanes<kLanes>(squares);
+    if (!of_v) {
+      dot = sum_lanes<kLanes>(dot);
+      if (there && lane == 0) p.delta[tok * p.heads + head] = dot;
+    }
+    if (counts && squares < INFINITY) largest = fmaxf(largest, squares);
+  }
+  const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(largest));
+  if ((threadIdx.x & 31) == 0) s_largest[threadIdx.x >> 5] = most;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    const uint32_t all = __reduce_max_sync(0xffffffffu, threadIdx.x < 8 ? s_largest[threadIdx.x] : 0u);
+    if (threadIdx.x == 0 && all) atomicMax(p.norms + (of_v ? p.kv_heads + head : head / p.group), all);
+  }
+}
+
+template <int D>
+int launch_delta_norms(const tra_packed_ctx& c, const tra_packed_launch& a) {
+  constexpr int kRows = 256 / (D / 8);
+  const long long q = ((long long)a.total_q + kRows - 1) / kRows, v = ((long long)a.total_k + kRows - 1) / kRows;
+  const long long most = 32ll * c.h->sm_count;           // four times what runs at once
+  const long long steps = (q * a.heads + v * a.kv_heads + most - 1) / most;
+  const long long q_blocks = (q + steps - 1) / steps * a.heads, v_blocks = (v + steps - 1) / steps * a.kv_heads;
+  if (cudaMemsetAsync(a.norms, 0, 2 * sizeof(uint32_t) * a.kv_heads, c.stream) != cudaSuccess) return TRA_ERR_CUDA;
+  return tra_launch(tra_packed_delta_norms_kernel<D>, dim3((unsigned)(q_blocks + v_blocks)), 256, 0, c.stream, false, 1, a, (int)q_blocks, (int)steps);
 }
 
 template <typename T, int D, int kHalves, bool kCausal>
@@ -771,8 +881,11 @@ int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   int rc = TRA_OK;
   if (rows > 0) {
     constexpr int kRows = 256 / (D / 8);
-    if ((rc = tra_launch(tra_packed_delta_kernel<T, D>, dim3((unsigned)((rows + kRows - 1) / kRows)), 256, 0, c.stream, false, 1, a)) != TRA_OK)
-      return rc;
+    if constexpr (kScaled<T>)
+      rc = launch_delta_norms<D>(c, a);
+    else
+      rc = tra_launch(tra_packed_delta_kernel<T, D>, dim3((unsigned)((rows + kRows - 1) / kRows)), 256, 0, c.stream, false, 1, a);
+    if (rc != TRA_OK) return rc;
   }
   const int dkv_units = a.max_k > 0 ? (a.max_k <= kTileM ? 0 : a.total_k / kTileM) + a.n_seq : 0;
   const int dq_units = a.max_q > 0 ? (a.max_q <= a.tile_tokens ? 0 : a.total_q / a.tile_tokens) + a.n_seq : 0;
