@@ -387,7 +387,7 @@ typedef struct {
   const int32_t *cu_q;    /* device [n_seq + 1], ascending                                        */
   const int32_t *k_begin, *k_end; /* device [n_seq]; packed keys: cu_k and cu_k + 1               */
   int n_seq, total_q, total_k;
-  int max_q, max_k;       /* upper bounds of the sequences' queries and keys                      */
+  int max_q, max_k;       /* upper bounds of the sequences' queries and keys, at most total_q and total_k */
   float sm_scale;
   void* o_rest;           /* what rounding took from o, in o's type, [total_q, heads, d] contiguous, 16-byte aligned,   */
                           /* or NULL.  Forward, with lse only: written.  Backward: read; the sums of dO O are then those */

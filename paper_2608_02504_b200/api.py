@@ -733,7 +733,7 @@ class PackedAttn:
                 sm_scale=None):
         """-> (o, lse).  Keys: packed like the queries (``cu_k``, default ``cu_q``), or ``k_range`` = (begin, end), two
         int32 [n_seq] tensors, e.g. the filled parts of a cache's slots.  ``max_q``, ``max_k``: upper bounds of the
-        sequences' queries and keys (a longer one is cut and reported by ``check_status``).  Rows of o and lse that
+        sequences' queries and keys, at most the tensors' tokens (a longer sequence is cut and reported by ``check_status``).  Rows of o and lse that
         belong to no sequence are not written.  An lse made here (``want_lse``) also keeps what rounding took from o, as
         ``lse.o_rest``, a tensor like o that ``backward`` uses when it is there; drop it where no gradient is needed."""
         if o is None:

@@ -135,7 +135,8 @@ constexpr int kClusterMax = 8;        // the largest portable cluster
 
 Choice choose(const tra_packed* h, int n_seq, int total_q, int max_q, int max_k) {
   const int group = h->cfg.heads / h->cfg.kv_heads;
-  Choice c = {(long long)max_q * group <= 16, false, 1, 0};
+  Choice c = {(long long)max_q * group <= 16, false, 1, 64};
+  if (max_q == 0) return c;                                // nothing to attend to: the launch looks at the ranges alone
   if (c.rows) {
     // Two blocks fit an SM: as many parts as fill them once (a second wave costs its ramp-up: 1,024 blocks of 256 keys
     // took 41 us over a 32K cache of eight heads, 128 blocks of 2,048 keys 27 us), each of at least 128 keys.
@@ -303,7 +304,6 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
   tra_packed_launch p;
   int rc = begin_launch(h, a, &p);
   if (rc != TRA_OK) return rc;
-  if (a->max_q == 0) return TRA_OK;                        // no query at all
   const tra_packed_ctx ctx = {h, (cudaStream_t)stream_};
   p.o = a->o;
   const Choice c = choose(h, a->n_seq, a->total_q, a->max_q, a->max_k);
@@ -318,6 +318,7 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
     p.part_lse2 = p.part_o + rows * h->cfg.head_dim;
     p.part_exact = a->lse ? p.part_lse2 + rows : nullptr;
   }
+  if (a->max_q == 0) return tra_packed_rows(ctx, p, c.chunk, false);       // (no row, no tile: the maps stay empty)
   const int key_box = c.rows ? 64 : 128;
   // without keys no tile is loaded; the maps then describe the queries
   const void *kk = a->total_k > 0 ? a->k : a->q, *vv = a->total_k > 0 ? a->v : a->q;
@@ -353,7 +354,8 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
       bad_tensor(g->dk, g->dk_stride, a->total_k, p.kv_heads) || bad_tensor(g->dv, g->dv_stride, a->total_k, p.kv_heads))
     return TRA_ERR_INVALID_ARG;
   if ((long long)a->total_q * p.heads > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
-  if (a->total_q == 0 && a->total_k == 0) return TRA_OK;
+  const tra_packed_ctx ctx = {h, (cudaStream_t)stream_};
+  if (a->max_q == 0 && a->max_k == 0) return tra_packed_rows(ctx, p, 64, false);      // nothing to do: the ranges are looked at
   if (a->total_q > 0) {
     if (!workspace || ((uintptr_t)workspace & 15)) return TRA_ERR_INVALID_ARG;
     if (workspace_bytes < tra_packed_attn_backward_workspace_bytes(h, a->total_q)) return TRA_ERR_CAPACITY;
@@ -388,6 +390,5 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
     if ((rc = make_packed_map(&p.map_q_stream, h, qq, qs, q_heads, nq, q_box, p.stream_tokens)) != TRA_OK) return rc;
     if ((rc = make_packed_map(&p.map_do_stream, h, oo, os, q_heads, nq, q_box, p.stream_tokens)) != TRA_OK) return rc;
   }
-  const tra_packed_ctx ctx = {h, (cudaStream_t)stream_};
   return h->cfg.head_dim == 128 ? tra_packed_bwd_d128(ctx, p) : tra_packed_bwd_d64(ctx, p);
 }

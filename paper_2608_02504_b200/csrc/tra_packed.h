@@ -97,7 +97,8 @@ struct tra_unit {
 // Finds a unit: `unit_tokens` consecutive queries, or (by_keys) keys, of a sequence.  The units of sequence s are numbered from
 // first(s) = floor(begin(s) / unit_tokens) + s on, which leaves room for all of them (some numbers mean nothing), and makes the
 // sequence of a number a search in the ascending bounds, 32 at a time.  one_each: unit s is the whole of sequence s.
-// One warp calls it; every lane gets the result.
+// One warp calls it; every lane gets the result.  There are at least as many numbers as sequences, and number s looks at the ranges of
+// sequence s too, so that each is reported that runs backwards, which the search might never meet.
 __device__ __forceinline__ tra_unit tra_find_unit(const tra_packed_launch& p, bool by_keys, bool one_each, int unit_tokens, int unit) {
   const int lane = threadIdx.x & 31;
   tra_unit u = {-1, 0, 1, {0, 0}, {0, 0}};
@@ -106,6 +107,10 @@ __device__ __forceinline__ tra_unit tra_find_unit(const tra_packed_launch& p, bo
     u.k = tra_clamp_range(p.k_begin[unit], p.k_end[unit], p.total_k, p.max_k, p.status);
     if ((by_keys ? u.k.len : u.q.len) > 0) u.seq = unit;
     return u;
+  }
+  if (unit < p.n_seq) {
+    tra_clamp_range(p.cu_q[unit], p.cu_q[unit + 1], p.total_q, p.max_q, p.status);
+    tra_clamp_range(p.k_begin[unit], p.k_end[unit], p.total_k, p.max_k, p.status);
   }
   int lo = 0, hi = p.n_seq;
   while (true) {
