@@ -721,41 +721,71 @@ class PackedAttn:
                                  self.head_dim ** -0.5 if sm_scale is None else sm_scale, 0 if rest is None else rest.data_ptr())
 
     @staticmethod
-    def _rest(lse, q):
-        """What rounding took from o, kept beside an lse that ``forward`` made (``lse.o_rest``), for the gradients."""
-        rest = getattr(lse, "o_rest", None)
-        if rest is not None and (rest.shape != q.shape or rest.dtype != q.dtype or rest.device != q.device or
-                                 not rest.is_contiguous()):
-            raise ValueError("lse.o_rest: does not belong to this q")
-        return rest
+    def _version(t):
+        """Counts what torch writes into a tensor (the kernels' own writes are not counted)."""
+        return None if t.is_inference() else t._version
+
+    @staticmethod
+    def _rest_fits(rest, q):
+        return rest.shape == q.shape and rest.dtype == q.dtype and rest.device == q.device and rest.is_contiguous()
 
     def forward(self, q, k, v, cu_q, cu_k=None, *, k_range=None, max_q, max_k, o=None, lse=None, want_lse=False,
-                sm_scale=None):
+                sm_scale=None, o_rest=None):
         """-> (o, lse).  Keys: packed like the queries (``cu_k``, default ``cu_q``), or ``k_range`` = (begin, end), two
         int32 [n_seq] tensors, e.g. the filled parts of a cache's slots.  ``max_q``, ``max_k``: upper bounds of the
         sequences' queries and keys, at most the tensors' tokens (a longer sequence is cut and reported by ``check_status``).  Rows of o and lse that
-        belong to no sequence are not written.  An lse made here (``want_lse``) also keeps what rounding took from o, as
-        ``lse.o_rest``, a tensor like o that ``backward`` uses when it is there; drop it where no gradient is needed."""
+        belong to no sequence are not written.
+
+        ``o_rest``: what rounding took from o, for ``backward``: a contiguous tensor like q to write it to, or False for
+        none.  By default an lse made here (``want_lse``) gets one, and one that an lse passed in carries is written again.
+        The one that was written is also kept as ``lse.o_rest``; a copy or a slice of lse does not carry it along."""
         if o is None:
             o = _empty_like(q)
+        if o_rest is None:
+            if lse is not None:
+                o_rest = getattr(lse, "o_rest", None)
+                if o_rest is not None and not self._rest_fits(o_rest, q):
+                    o_rest = None                        # of a call on other tensors
+            elif want_lse:
+                o_rest = _empty_like(q)
+        elif o_rest is False:
+            o_rest = None
+        elif not self._rest_fits(o_rest, q) or (lse is None and not want_lse):
+            raise ValueError("o_rest: expected a contiguous tensor like q, beside an lse")
         if lse is None and want_lse:
             lse = q.new_empty((q.shape[0], self.heads), dtype=torch.float32)
-            lse.o_rest = _empty_like(q)
-        a = self._args(q, k, v, o, lse, self._rest(lse, q), cu_q, cu_k, k_range, max_q, max_k, sm_scale)
+        a = self._args(q, k, v, o, lse, o_rest, cu_q, cu_k, k_range, max_q, max_k, sm_scale)
         n = _lib.tra_packed_attn_workspace_bytes(self._h, cu_q.shape[0] - 1, q.shape[0], max_q, max_k)
         ws = q.new_empty((n,), dtype=torch.uint8) if n else None
         _check(_lib.tra_packed_attn(self._h, a, ws.data_ptr() if n else None, n, _raw_stream(self._index)), "tra_packed_attn")
+        if lse is not None:
+            lse.o_rest, lse.o_rest_version = o_rest, self._version(lse)
         return o, lse
 
-    def backward(self, do, q, k, v, o, lse, cu_q, cu_k=None, *, max_q, max_k, dq=None, dk=None, dv=None, sm_scale=None):
+    def backward(self, do, q, k, v, o, lse, cu_q, cu_k=None, *, max_q, max_k, dq=None, dk=None, dv=None, sm_scale=None,
+                 o_rest=None):
         """Gradients (dq, dk, dv) of ``forward`` over packed keys, from its o and lse.  Rows that belong to no sequence
-        are not written."""
+        are not written.
+
+        ``o_rest``: what rounding took from o, as ``forward`` wrote it; without it the gradients of rows that see few keys,
+        or one above all, are mostly the rounding of o.  Default: the one kept beside the lse, if it carries one, and an error when
+        something else has been written into that lse since; False: none."""
         dq = _empty_like(q) if dq is None else dq
         dk = _empty_like(k) if dk is None else dk
         dv = _empty_like(v) if dv is None else dv
         if lse is None:
             raise ValueError("lse: the forward call's, made with want_lse")
-        a = self._args(q, k, v, o, lse, self._rest(lse, q), cu_q, cu_k, None, max_q, max_k, sm_scale)
+        if o_rest is None:
+            o_rest = getattr(lse, "o_rest", None)
+            if o_rest is not None:
+                version = self._version(lse)
+                if getattr(lse, "o_rest_version", version) != version:
+                    raise ValueError("lse.o_rest: the lse was written since; pass o_rest (False: none)")
+        elif o_rest is False:
+            o_rest = None
+        if o_rest is not None and not self._rest_fits(o_rest, q):
+            raise ValueError("o_rest: expected a contiguous tensor like q")
+        a = self._args(q, k, v, o, lse, o_rest, cu_q, cu_k, None, max_q, max_k, sm_scale)
         tq, tk = q.shape[0], k.shape[0]
         ptrs, strides = zip(*((p, s) for p, *s in (self._tensor(do, "do", tq, self.heads), self._tensor(dq, "dq", tq, self.heads),
                                                    self._tensor(dk, "dk", tk, self.kv_heads), self._tensor(dv, "dv", tk, self.kv_heads))))
