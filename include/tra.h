@@ -287,7 +287,7 @@ int tra_hot_path_host(tra_plan_t* plan, const void* Q_host, const void* K_host, 
  *   rotary  : d / 2 channel pairs, pair p = channels (2p, 2p + 1), or (p, p + d/2) with `halves`; pair p belongs to
  *             axis axis[p] and turns by the angle pos[axis[p]] * inv_freq[p]:
  *             (z1, z2) -> (z1 cos - z2 sin, z1 sin + z2 cos).  inv_freq[p] = 0 leaves a pair as it is.
- *             Angles are reduced exactly for every int32 position.
+ *             Angles are reduced by whole turns before they are rounded: off by 2^-23 at most for every int32 position.
  *   order   : see TRA_ROTARY_TILE_MAJOR.
  * All arithmetic is fp32 and rounded once, to the tensors' type. */
 #define TRA_ROTARY_MAX_HEAD_DIM 256
@@ -307,7 +307,7 @@ typedef struct {
   int head_dim;           /* d: a multiple of 16, 16 .. 256                               */
   int n_axes;             /* 1 .. 4                                                       */
   const int* axis;        /* HOST [d / 2]: 0 .. n_axes - 1                                */
-  const double* inv_freq; /* HOST [d / 2]: radians per position, finite                   */
+  const double* inv_freq; /* HOST [d / 2]: radians per position, finite, below 2^64 in magnitude */
   int halves;             /* how channels pair: 0 = (2p, 2p + 1), 1 = (p, p + d/2)        */
   int norm;               /* TRA_NORM_*                                                   */
   double eps;             /* of the norm, >= 0                                            */

@@ -9,10 +9,10 @@
 //   dx = r (g - n mean(g n))            RMS norm
 //   dx = r (g - mean g - n mean(g n))   layer norm.
 //
-// Angles.  F_p = f_p / 2 pi modulo one turn, as a 64-bit binary fraction (rounded once, on the host, from long
-// double).  pos * F_p modulo 2^64 is then the angle in turns with its whole turns already gone, whatever the
-// position: an integer product in place of a range reduction, off by pos * 2^-65 turns.  Its high word, as a
-// signed number of half turns, goes to sincospif.
+// Angles.  F_p = f_p / 2 pi modulo one turn, as a 64-bit binary fraction (rounded once, on the host, from an integer
+// product with 192 bits of 1 / 2 pi).  pos * F_p modulo 2^64 is then the angle in turns with its whole turns already gone, whatever the
+// position: an integer product in place of a range reduction, off by pos * 2^-65 turns.  Its high word (2^-32 turns
+// at most are cut), as a signed number of half turns rounded to fp32 (2^-25 half turns), goes to sincospif.
 //
 // Bound: HBM.  Every element is read once and written once (the norm's backward pass reads x too); a row stays
 // in the registers of d / 16 neighbouring threads, 16 channels each (a 16-byte piece of either half of the row
@@ -651,6 +651,35 @@ int log2_of(int n) {
 
 constexpr int kBlocksMax = 4 * 148;
 
+// f / 2 pi modulo one turn as a 64-bit binary fraction, |f| < 2^64.  f = m 2^e with a 53-bit m, so the fraction is m times
+// floor(2^192 / 2 pi), shifted right by 128 - e >= 117 bits and rounded; the digits that the constant lacks weigh less than 2^-64 of its
+// last bit.
+uint64_t turn_of(double f) {
+  constexpr uint64_t kInvTwoPi[3] = {0x36d8a5664f10e410ull, 0x7f09d5f47d4d3770ull, 0x28be60db9391054aull};
+  int exponent = 0;
+  const uint64_t m = (uint64_t)ldexp(frexp(fabs(f), &exponent), 53);
+  const int shift = 128 + 53 - exponent;
+  if (m == 0 || shift >= 245) return 0;                // the product is below 2^243: rounds to 0
+  uint64_t w[5] = {0, 0, 0, 0, 0};
+  unsigned __int128 carry = 0;
+  for (int i = 0; i < 3; ++i) {
+    carry += (unsigned __int128)m * kInvTwoPi[i];
+    w[i] = (uint64_t)carry;
+    carry >>= 64;
+  }
+  w[3] = (uint64_t)carry;
+  const int half = shift - 1;                          // rounding: half of the last bit kept
+  carry = 1ull << (half & 63);
+  for (int i = half >> 6; i < 4; ++i) {
+    carry += w[i];
+    w[i] = (uint64_t)carry;
+    carry >>= 64;
+  }
+  const int word = shift >> 6, bit = shift & 63;
+  const uint64_t turns = bit ? w[word] >> bit | w[word + 1] << (64 - bit) : w[word];
+  return f < 0 ? 0 - turns : turns;
+}
+
 int elem_bytes(int dtype) { return dtype == TRA_FP32 ? 4 : 2; }
 
 bool aligned_strides(const int64_t* s, int dtype) {
@@ -823,6 +852,8 @@ extern "C" int tra_rotary_create(tra_rotary_t** out, const tra_rotary_config_t* 
   if (cfg->head_dim < 16 || cfg->head_dim > kMaxD || cfg->head_dim % 16) return TRA_ERR_UNSUPPORTED;
   for (int i = 0; i < cfg->head_dim / 2; ++i)
     if (cfg->axis[i] < 0 || cfg->axis[i] >= cfg->n_axes || !isfinite(cfg->inv_freq[i])) return TRA_ERR_INVALID_ARG;
+  for (int i = 0; i < cfg->head_dim / 2; ++i)
+    if (fabs(cfg->inv_freq[i]) >= 18446744073709551616.0) return TRA_ERR_UNSUPPORTED;
   tra_rotary* r = new (std::nothrow) tra_rotary;
   if (!r) return TRA_ERR_CAPACITY;
   memset(r, 0, sizeof(*r));
@@ -831,12 +862,8 @@ extern "C" int tra_rotary_create(tra_rotary_t** out, const tra_rotary_config_t* 
   r->halves = cfg->halves != 0;
   r->norm = cfg->norm;
   r->eps = (float)cfg->eps;
-  const long double two_pi = 6.283185307179586476925286766559005768L;
   for (int i = 0; i < cfg->head_dim / 2; ++i) {
-    long double turns = (long double)cfg->inv_freq[i] / two_pi;
-    turns -= floorl(turns);                                       // in [0, 1]
-    const long double scaled = floorl(turns * 18446744073709551616.0L + 0.5L);
-    r->turn[i] = scaled >= 18446744073709551616.0L ? 0ull : (uint64_t)scaled;
+    r->turn[i] = turn_of(cfg->inv_freq[i]);
     r->axis[i] = (uint8_t)cfg->axis[i];
   }
   *out = r;
