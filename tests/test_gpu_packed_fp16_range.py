@@ -117,3 +117,63 @@ def test_scale_ignores_what_lies_outside(api):
         assert all(torch.equal(a, b[inside]) for a, b in zip(base, got))
     do.zero_()
     assert all((t[inside] == 0).all() for t in gradients(attn, q, k, v, do, cu, None, 150, 150, None))
+
+
+def test_replays_follow_the_size_of_do(api):
+    """The scale belongs to a call: replays of a captured one with a large dO, then a small one, give what calls of their own give."""
+    d, n = 64, 300
+    q, k, v = (randn((n, h, d), HALF, i) for i, h in enumerate((4, 2, 2)))
+    do, unit = torch.empty(n, 4, d, dtype=HALF, device="cuda"), unit_do((n, 4, d), 4)
+    attn = api.PackedAttn(4, 2, d, dtype=HALF, causal=True)
+    cu = i32([0, 100, n])
+    o, lse = attn.forward(q, k, v, cu, max_q=200, max_k=200, want_lse=True)
+    step = lambda: attn.backward(do, q, k, v, o, lse, cu, max_q=200, max_k=200)
+    do.copy_(unit)
+    step()
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step()
+        graphs.append((graph, out))
+    first = None
+    for power in (12, -12, 0, 12):
+        do.copy_(unit * 2.0 ** power)
+        for graph, _ in graphs:
+            graph.replay()
+        want = step()
+        for _, out in graphs:
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            there = step()
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(there, want))
+        first = [t.clone() for t in want] if first is None else first
+    assert all(torch.equal(a, b) for a, b in zip(first, want))
+    attn.check_status()
+
+
+@pytest.mark.parametrize("d,group,hk", [(64, 1, 5), (64, 3, 2), (128, 5, 3), (128, 1, 2), (64, 22, 2)])
+def test_heads_of_different_sizes(api, d, group, hk):
+    """Every key/value head has a scale of its own: the gradients are those of calls with one such head, bit by bit, whatever the other
+    heads hold; slices of fused tensors among them."""
+    lens = [70, 1, 333]
+    cu, n = packed(lens), sum(lens)
+    sizes = torch.tensor([2.0 ** (-8 + 7 * (i % 3)) for i in range(hk)], device="cuda", dtype=HALF)
+    fused = randn((n, (group + 2) * hk, d), HALF, 1)
+    q, k, v = fused[:, :group * hk], fused[:, group * hk:-hk], fused[:, -hk:]
+    v *= sizes[:, None]
+    do = unit_do((group * hk, n, d), 4).transpose(0, 1) * sizes.flip(0).repeat_interleave(group)[:, None]
+    attn, one = api.PackedAttn(group * hk, hk, d, dtype=HALF), api.PackedAttn(group, 1, d, dtype=HALF)
+    kw = dict(max_q=max(lens), max_k=max(lens))
+    o, lse = attn.forward(q, k, v, i32(cu), want_lse=True, **kw)
+    dq, dk, dv = attn.backward(do, q, k, v, o, lse, i32(cu), **kw)
+    for h in range(hk):
+        mine, kv = slice(h * group, (h + 1) * group), slice(h, h + 1)
+        got = one.backward(do[:, mine], q[:, mine], k[:, kv], v[:, kv], o[:, mine], lse[:, mine].contiguous(), i32(cu),
+                           o_rest=lse.o_rest[:, mine].contiguous(), **kw)
+        assert torch.equal(got[0], dq[:, mine]) and torch.equal(got[1], dk[:, kv]) and torch.equal(got[2], dv[:, kv]), h
+    attn.check_status()
