@@ -461,7 +461,8 @@ class Rotary:
     an axis with c channels turns by ``scale[axis] * theta ** (-2 k / c)`` radians per position.  Any other
     layout of frequencies: pass ``axis`` and ``inv_freq``, one entry per channel pair, instead.
     ``halves``: channels p and p + d/2 form a pair (default: 2p and 2p + 1).
-    ``norm``: None, "rms" or "layer", over the channels of every head.
+    ``norm``: None, "rms" or "layer", over the channels of each head by itself.  A model that norms over the channels of all heads
+    together does that before the split into heads and calls with None.
     """
 
     def __init__(self, head_dim, axis_dims=None, theta=10000.0, scale=None, axis=None, inv_freq=None, halves=False,

@@ -2,7 +2,8 @@
 
 Every ``.cu`` file is compiled to an object of its own (in parallel) and the objects are linked
 into ``libtra_b200.so`` next to this file.  ``-DTRA_DEBUG`` builds (``build(debug=True)``) go to
-``libtra_b200_debug.so``: the same sources with every global index checked on the device.
+``libtra_b200_debug.so``: the same sources with the global indexes of the sparse path's kernels (plan, mask, dense and
+block-sparse attention) checked on the device; the rotary and packed-attention kernels are the same in both.
 """
 from __future__ import annotations
 

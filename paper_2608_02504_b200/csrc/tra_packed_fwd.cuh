@@ -14,6 +14,9 @@
 // replaced before they are looked at; their V rows would still meet the zero probabilities in the product (0 * NaN), so an
 // idle warp zeroes them in shared memory before the tensor pipe reads that last tile.
 //
+// P is rounded to the 16-bit type, the only operand type of the product with V that keeps its rate; the sum that divides O is
+// taken over the rounded values, so that what is left of the rounding is u sum p |v - o|.
+//
 // Split launches give every unit a range of the key blocks; the parts O / l and log2 l go to a
 // workspace and tra_packed_join_kernel adds them.
 //
