@@ -341,8 +341,8 @@ int tra_rotary_destroy(tra_rotary_t* rot);
  *   pos  : int32 [tokens, n_axes], the position of every token in the order of the projection side, shared by the
  *          batch entries; or NULL: video token (t*H + y)*W + x of the plan has position (t, y, x) (n_axes = 3) and
  *          text tokens are normed and not turned.
- * Pointers 16-byte aligned.  src and dst must not overlap, except that a tensor that is not TILE_MAJOR may be worked
- * on in place (dst = src with the same strides).
+ * Pointers 16-byte aligned.  B and tokens are at least 1.  src (and x) and dst must not overlap, except that a tensor
+ * that is not TILE_MAJOR may be worked on in place (dst = src with the same strides).
  * Errors: TRA_ERR_INVALID_ARG, TRA_ERR_UNSUPPORTED, TRA_ERR_CUDA. */
 int tra_rotary_forward(const tra_rotary_t* rot, const tra_plan_t* plan, const int32_t* pos,
                        const tra_rotary_tensor_t* tensors, int n_tensors, int B, int tokens, int dtype,
@@ -366,10 +366,11 @@ int tra_rotary_backward(const tra_rotary_t* rot, const tra_plan_t* plan, const i
  * (device int32; ranges of keys may leave gaps and may be shared).  With `causal`, query i of a sequence sees its keys
  * 0 .. i + (number of keys - number of queries): the last query sees every key.
  *   O = softmax(sm_scale Q K^T) V,  lse = log sum exp of the scores a query sees, fp32 [total_q, heads].
- * A query that sees no key gets O = 0 and lse = -inf.  Rows of O and lse in front of cu_q[0] and behind cu_q[n_seq] are
- * left as they were.  What lies in K and V outside a sequence's range, or in Q outside of all, is never used and may be
+ * A query that sees no key, or only scores of -inf, gets O = 0 and lse = -inf.  Rows of O and lse in front of cu_q[0]
+ * and behind cu_q[n_seq] are left as they were.  What lies in K and V outside a sequence's range, or in Q outside of all, is never used and may be
  * anything, NaN too.  (Inside a sequence a NaN among the scores that a query sees makes its O and lse NaN; a hidden key's weight is
- * 0, but 0 * NaN is NaN: a value that is not finite can reach queries that do not see its key.) */
+ * 0, but 0 * NaN is NaN: a value that is not finite can reach queries that do not see its key.)
+ * What a call writes overlaps neither what it reads nor its other results. */
 typedef struct tra_packed tra_packed_t; /* opaque: head layout, type, order, a device status word */
 
 typedef struct {

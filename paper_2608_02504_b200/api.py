@@ -722,13 +722,14 @@ class PackedAttn:
                                  self.head_dim ** -0.5 if sm_scale is None else sm_scale, 0 if rest is None else rest.data_ptr())
 
     @staticmethod
-    def _version(t):
-        """Counts what torch writes into a tensor (the kernels' own writes are not counted)."""
-        return None if t.is_inference() else t._version
+    def _writes(lse, rest):
+        """How often torch has written into lse more than into its remainder (the kernels' own writes are not counted): the
+        same as when a call made them as long as both are as they were, or were written or copied together."""
+        return None if rest is None or lse.is_inference() or rest.is_inference() else lse._version - rest._version
 
     @staticmethod
     def _rest_fits(rest, q):
-        return rest.shape == q.shape and rest.dtype == q.dtype and rest.device == q.device and rest.is_contiguous()
+        return isinstance(rest, torch.Tensor) and rest.shape == q.shape and rest.dtype == q.dtype and rest.device == q.device and rest.is_contiguous()
 
     def forward(self, q, k, v, cu_q, cu_k=None, *, k_range=None, max_q, max_k, o=None, lse=None, want_lse=False,
                 sm_scale=None, o_rest=None):
@@ -760,7 +761,7 @@ class PackedAttn:
         ws = q.new_empty((n,), dtype=torch.uint8) if n else None
         _check(_lib.tra_packed_attn(self._h, a, ws.data_ptr() if n else None, n, _raw_stream(self._index)), "tra_packed_attn")
         if lse is not None:
-            lse.o_rest, lse.o_rest_version = o_rest, self._version(lse)
+            lse.o_rest, lse.o_rest_writes = o_rest, self._writes(lse, o_rest)
         return o, lse
 
     def backward(self, do, q, k, v, o, lse, cu_q, cu_k=None, *, max_q, max_k, dq=None, dk=None, dv=None, sm_scale=None,
@@ -770,7 +771,7 @@ class PackedAttn:
 
         ``o_rest``: what rounding took from o, as ``forward`` wrote it; without it the gradients of rows that see few keys,
         or one above all, are mostly the rounding of o.  Default: the one kept beside the lse, if it carries one, and an error when
-        something else has been written into that lse since; False: none."""
+        torch has written into one of the two since and not into the other; False: none."""
         dq = _empty_like(q) if dq is None else dq
         dk = _empty_like(k) if dk is None else dk
         dv = _empty_like(v) if dv is None else dv
@@ -779,8 +780,8 @@ class PackedAttn:
         if o_rest is None:
             o_rest = getattr(lse, "o_rest", None)
             if o_rest is not None:
-                version = self._version(lse)
-                if getattr(lse, "o_rest_version", version) != version:
+                writes = self._writes(lse, o_rest)
+                if getattr(lse, "o_rest_writes", writes) != writes:
                     raise ValueError("lse.o_rest: the lse was written since; pass o_rest (False: none)")
         elif o_rest is False:
             o_rest = None

@@ -1,5 +1,8 @@
 """What rounding took from o (``o_rest``): passed explicitly, kept beside an lse that the call made, refused where it no longer
 belongs to the lse, left out on request."""
+import copy
+import io
+
 import pytest
 import torch
 
@@ -105,3 +108,24 @@ def test_lse_used_by_other_handles(api, case):
     with pytest.raises(api.TraError):
         attn.forward(q, k, v, cu, lse=lse, o_rest=False, max_q=10 ** 6, max_k=125)
     assert lse.o_rest is rest
+
+
+def test_copies_that_carry_the_remainder_along(case):
+    """Deep copies, stored and loaded tensors, and buffers into which both are copied keep lse and remainder together."""
+    attn, (q, k, v), do, cu, kw = case
+    o, lse = attn.forward(q, k, v, cu, want_lse=True, **kw)
+    want = attn.backward(do, q, k, v, o, lse, cu, **kw)
+    stored = io.BytesIO()
+    torch.save(lse, stored)
+    stored.seek(0)
+    for other in (copy.deepcopy(lse), torch.load(stored, weights_only=False)):
+        assert torch.equal(other.o_rest, lse.o_rest)
+        assert same(want, attn.backward(do, q, k, v, o, other, cu, **kw))
+    _, buffer = attn.forward(q * 0.5, k, v, cu, want_lse=True, **kw)
+    buffer.copy_(lse)
+    with pytest.raises(ValueError):
+        attn.backward(do, q, k, v, o, buffer, cu, **kw)
+    buffer.o_rest.copy_(lse.o_rest)
+    assert same(want, attn.backward(do, q, k, v, o, buffer, cu, **kw))
+    with pytest.raises(ValueError):
+        attn.forward(q, k, v, cu, want_lse=True, o_rest=True, **kw)
