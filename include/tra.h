@@ -378,6 +378,9 @@ typedef struct {
   int head_dim;        /* 64 or 128                                  */
   int dtype;           /* TRA_BF16 or TRA_FP16                       */
   int causal;
+  int window;          /* 0: none.  Else (with causal) a query sees the last `window` keys up to its own position and the   */
+  int sinks;           /* first `sinks` keys of its sequence (0: none): at position p = i + keys - queries, key j with      */
+                       /* j <= p and (j > p - window or j < sinks).  Keys that no query of a call sees are not read         */
 } tra_packed_config_t;
 
 typedef struct {

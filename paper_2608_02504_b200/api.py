@@ -74,7 +74,7 @@ class tra_rotary_tensor_t(ctypes.Structure):
 
 
 class tra_packed_config_t(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int) for n in ("heads", "kv_heads", "head_dim", "dtype", "causal")]
+    _fields_ = [(n, ctypes.c_int) for n in ("heads", "kv_heads", "head_dim", "dtype", "causal", "window", "sinks")]
 
 
 class tra_packed_args_t(ctypes.Structure):
@@ -653,15 +653,18 @@ class PackedAttn:
 
     Tensors: q, o [total_q, heads, head_dim], k, v [total_k, kv_heads, head_dim], any strides (multiples of 8
     elements) with contiguous channels.  ``cu_q`` int32 [n_seq + 1]: sequence s has the queries cu_q[s] .. cu_q[s+1] - 1.
+    ``window`` (with ``causal``; 0: none): a query sees the last ``window`` keys up to its own position, and the first ``sinks``
+    keys of its sequence whatever the distance.
     """
 
-    def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, causal=True):
+    def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, causal=True, window=0, sinks=0):
         if dtype not in (torch.bfloat16, torch.float16):
             raise ValueError("dtype: expected bf16 or fp16")
-        cfg = tra_packed_config_t(heads, kv_heads, head_dim, _DTYPES[dtype], int(causal))
+        cfg = tra_packed_config_t(heads, kv_heads, head_dim, _DTYPES[dtype], int(causal), window, sinks)
         self._h = ctypes.c_void_p()
         _check(_lib.tra_packed_create(ctypes.byref(self._h), ctypes.byref(cfg)), "tra_packed_create")
         self.heads, self.kv_heads, self.head_dim, self.dtype, self.causal = heads, kv_heads, head_dim, dtype, bool(causal)
+        self.window, self.sinks = window, sinks
         self._index = torch.cuda.current_device()
         self.device = torch.device("cuda", self._index)
 

@@ -133,10 +133,22 @@ struct Choice {
 
 constexpr int kClusterMax = 8;        // the largest portable cluster
 
+// Whether a window hides anything from sequences of up to max_k keys: the last position has all but `window` in front of it, and the first
+// tokens stay.
+bool window_hides(const tra_packed* h, int max_k) { return h->cfg.window > 0 && (long long)h->cfg.window + h->cfg.sinks < max_k; }
+
+// Keys that a tile of `tokens` queries walks at most (tra_key_axis).
+int longest_axis(const tra_packed* h, int max_k, int tokens) {
+  if (!window_hides(h, max_k)) return max_k;
+  const long long n = (long long)(h->cfg.sinks + 7) / 8 * 8 + h->cfg.window + tokens - 1;
+  return n < max_k ? (int)n : max_k;
+}
+
 Choice choose(const tra_packed* h, int n_seq, int total_q, int max_q, int max_k) {
   const int group = h->cfg.heads / h->cfg.kv_heads;
   Choice c = {(long long)max_q * group <= 16, false, 1, 64};
   if (max_q == 0) return c;                                // nothing to attend to: the launch looks at the ranges alone
+  max_k = longest_axis(h, max_k, c.rows ? max_q : 2 * (kTileM / group));
   if (c.rows) {
     // Two blocks fit an SM: as many parts as fill them once (a second wave costs its ramp-up: 1,024 blocks of 256 keys
     // took 41 us over a 32K cache of eight heads, 128 blocks of 2,048 keys 27 us), each of at least 128 keys.
@@ -233,10 +245,26 @@ int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_lau
   p->n_seq = a->n_seq, p->total_q = a->total_q, p->total_k = a->total_k, p->max_q = a->max_q, p->max_k = a->max_k;
   p->heads = h->cfg.heads, p->kv_heads = h->cfg.kv_heads, p->group = h->cfg.heads / h->cfg.kv_heads;
   p->tile_tokens = kTileM / p->group;
-  p->causal = h->cfg.causal, p->splits = 1;
+  p->order = !h->cfg.causal ? kOrderNone : window_hides(h, a->max_k) ? kOrderWindow : kOrderCausal;
+  p->window = h->cfg.window, p->sinks = h->cfg.sinks, p->sink_rows = (h->cfg.sinks + 7) / 8 * 8;
+  p->splits = 1;
   p->sm_scale = a->sm_scale;
   p->status = h->d_status;
   return TRA_OK;
+}
+
+// The maps of K and V, in boxes of `rows` keys and, for the tile where the first tokens end, of its two parts.
+int make_key_maps(tra_packed_launch* p, const tra_packed* h, const void* k, const int64_t* ks, const void* v, const int64_t* vs, long long tokens,
+                  int rows) {
+  int rc;
+  if ((rc = make_packed_map(&p->map_k, h, k, ks, p->kv_heads, tokens, 1, rows)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p->map_v, h, v, vs, p->kv_heads, tokens, 1, rows)) != TRA_OK) return rc;
+  const int first = p->order == kOrderWindow ? p->sink_rows % rows : 0;
+  if (first == 0) return TRA_OK;
+  if ((rc = make_packed_map(&p->map_k_first, h, k, ks, p->kv_heads, tokens, 1, first)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p->map_v_first, h, v, vs, p->kv_heads, tokens, 1, first)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p->map_k_rest, h, k, ks, p->kv_heads, tokens, 1, rows - first)) != TRA_OK) return rc;
+  return make_packed_map(&p->map_v_rest, h, v, vs, p->kv_heads, tokens, 1, rows - first);
 }
 
 template <typename T, int D>
@@ -259,6 +287,9 @@ extern "C" int tra_packed_create(tra_packed_t** out, const tra_packed_config_t* 
   if (cfg->heads < 1 || cfg->kv_heads < 1 || cfg->heads % cfg->kv_heads) return TRA_ERR_INVALID_ARG;
   if (cfg->dtype != TRA_BF16 && cfg->dtype != TRA_FP16) return TRA_ERR_INVALID_ARG;
   if (cfg->head_dim != 64 && cfg->head_dim != 128) return TRA_ERR_UNSUPPORTED;
+  if (cfg->window < 0 || cfg->sinks < 0 || (cfg->sinks > 0 && cfg->window == 0)) return TRA_ERR_INVALID_ARG;
+  if (cfg->window > 0 && !cfg->causal) return TRA_ERR_UNSUPPORTED;
+  if (cfg->window > (1 << 30) || cfg->sinks > (1 << 30)) return TRA_ERR_UNSUPPORTED;
   if (cfg->heads > 4096 || cfg->heads / cfg->kv_heads > kTileM) return TRA_ERR_UNSUPPORTED;
   tra_packed* h = new (std::nothrow) tra_packed;
   if (!h) return TRA_ERR_CAPACITY;
@@ -324,14 +355,16 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
   const void *kk = a->total_k > 0 ? a->k : a->q, *vv = a->total_k > 0 ? a->v : a->q;
   const int64_t *ks = a->total_k > 0 ? a->k_stride : a->q_stride, *vs = a->total_k > 0 ? a->v_stride : a->q_stride;
   const long long tk = a->total_k > 0 ? a->total_k : a->total_q;
-  if ((rc = make_packed_map(&p.map_k, h, kk, ks, p.kv_heads, tk, 1, key_box)) != TRA_OK) return rc;
-  if ((rc = make_packed_map(&p.map_v, h, vv, vs, p.kv_heads, tk, 1, key_box)) != TRA_OK) return rc;
+  if ((rc = make_key_maps(&p, h, kk, ks, vv, vs, tk, key_box)) != TRA_OK) return rc;
   if (c.rows) {
     rc = tra_packed_rows(ctx, p, c.chunk, c.clustered);
   } else {
     if ((rc = make_packed_map(&p.map_q, h, a->q, a->q_stride, p.heads, a->total_q, p.group, p.tile_tokens)) != TRA_OK) return rc;
     p.n_units = (a->max_q <= 2 * p.tile_tokens ? 0 : a->total_q / (2 * p.tile_tokens)) + a->n_seq;
-    rc = h->cfg.head_dim == 128 ? tra_packed_fwd_d128(ctx, p) : tra_packed_fwd_d64(ctx, p);
+    if (p.order == kOrderWindow)
+      rc = h->cfg.head_dim == 128 ? tra_packed_fwd_window_d128(ctx, p) : tra_packed_fwd_window_d64(ctx, p);
+    else
+      rc = h->cfg.head_dim == 128 ? tra_packed_fwd_d128(ctx, p) : tra_packed_fwd_d64(ctx, p);
   }
   if (rc != TRA_OK || !join) return rc;
   return h->cfg.dtype == TRA_BF16 ? launch_join<__nv_bfloat16>(h, p, ctx.stream) : launch_join<__half>(h, p, ctx.stream);
@@ -383,12 +416,12 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
   const int q_heads = q ? p.heads : p.kv_heads, q_box = q ? p.group : 1, nq = q ? a->total_q : a->total_k, nk = k ? a->total_k : a->total_q;
   if ((rc = make_packed_map(&p.map_q, h, qq, qs, q_heads, nq, q_box, p.tile_tokens)) != TRA_OK) return rc;
   if ((rc = make_packed_map(&p.map_do, h, oo, os, q_heads, nq, q_box, p.tile_tokens)) != TRA_OK) return rc;
-  if ((rc = make_packed_map(&p.map_k, h, kk, ks, p.kv_heads, nk, 1, p.stream_rows)) != TRA_OK) return rc;
-  if ((rc = make_packed_map(&p.map_v, h, vv, vs, p.kv_heads, nk, 1, p.stream_rows)) != TRA_OK) return rc;
+  if ((rc = make_key_maps(&p, h, kk, ks, vv, vs, nk, p.stream_rows)) != TRA_OK) return rc;
   p.map_q_stream = p.map_q, p.map_do_stream = p.map_do;
   if (p.stream_rows != kTileM) {
     if ((rc = make_packed_map(&p.map_q_stream, h, qq, qs, q_heads, nq, q_box, p.stream_tokens)) != TRA_OK) return rc;
     if ((rc = make_packed_map(&p.map_do_stream, h, oo, os, q_heads, nq, q_box, p.stream_tokens)) != TRA_OK) return rc;
   }
+  if (p.order == kOrderWindow) return h->cfg.head_dim == 128 ? tra_packed_bwd_window_d128(ctx, p) : tra_packed_bwd_window_d64(ctx, p);
   return h->cfg.head_dim == 128 ? tra_packed_bwd_d128(ctx, p) : tra_packed_bwd_d64(ctx, p);
 }

@@ -19,6 +19,8 @@ struct tra_packed {
 struct tra_packed_launch {
   CUtensorMap map_q, map_k, map_v, map_do;   // boxes: 64 channels x (group heads x tile tokens | 1 head x 128 tokens)
   CUtensorMap map_q_stream, map_do_stream;   // backward, streamed tiles of stream_rows rows (then K and V boxes have that many, too)
+  // window with first tokens: the key tile that holds the last of them and, behind them, the first keys of the window
+  CUtensorMap map_k_first, map_v_first, map_k_rest, map_v_rest;
   const void *q, *k, *v, *o_in, *d_o;
   void *o, *dq, *dk, *dv;
   float* lse;                  // forward: written or NULL; backward: read
@@ -33,10 +35,15 @@ struct tra_packed_launch {
   int n_seq, total_q, total_k, max_q, max_k;
   int heads, kv_heads, group, tile_tokens;   // tile_tokens = 128 / group: query tokens of a 128-row tile
   int stream_rows, stream_tokens;            // backward: rows of a streamed tile, 128 or 64, and stream_rows / group
-  int causal, splits, n_units;               // n_units: query-tile pairs (forward) or key / query tiles (backward) launched
+  int order, splits, n_units;                // n_units: query-tile pairs (forward) or key / query tiles (backward) launched
+  int window, sinks, sink_rows;              // kOrderWindow; sink_rows: sinks rounded up to whole 8-row pieces of a tile
   float sm_scale;
   int* status;
 };
+
+// Which keys a query at position p of its sequence's key axis sees (p of the last query = the last key): all; keys 0 .. p; of these, the
+// last `window` and the first `sinks`.
+constexpr int kOrderNone = 0, kOrderCausal = 1, kOrderWindow = 2;
 
 struct tra_packed_ctx {
   const tra_packed_t* h;
@@ -47,6 +54,10 @@ int tra_packed_fwd_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_fwd_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_fwd_window_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_fwd_window_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_bwd_window_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_bwd_window_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered);
 
 #ifdef __CUDACC__
@@ -86,6 +97,36 @@ __device__ __forceinline__ tra_seq_range tra_clamp_range(int begin, int end, int
   const int len = min(e - b, max_len);
   if (b != begin || b + len != end) atomicCAS(status, 0, TRA_ERR_INVALID_ARG);
   return {b, len};
+}
+
+// The keys that a tile of queries walks.  With a window these are not one range: its first keys, [0, sink_rows), and the window's, from
+// that of the tile's first query on.  They are walked as one axis v, closed up: key v below sink_rows, v + gap from there on, and a
+// tile of keys may hold both.  (Tiles of their own for the first tokens and tiles that start at multiples of 128 keys take two more tiles
+// per query tile.)  A query at position p sees v < p + 1 - gap, of these v < sinks and v > p - gap - window: gap > 0 only
+// where the tile's first window starts behind sink_rows, and then every window of the tile does.
+template <int kOrder>
+struct tra_key_axis {
+  int gap, len;                // len: of the axis, the sequence's last key included
+  __device__ __forceinline__ tra_key_axis(const tra_packed_launch& p, int first_position, int k_len) {
+    gap = kOrder == kOrderWindow ? max(first_position + 1 - p.window - p.sink_rows, 0) : 0;
+    len = k_len - gap;
+  }
+};
+
+// Loads `rows` keys from v0 on (a multiple of `rows`) into a tile of kAtoms 64-channel pieces, `atom_bytes` apart.
+template <int kOrder, int kAtoms, typename Load>
+__device__ __forceinline__ void tra_load_keys(const tra_packed_launch& p, int v0, int rows, int gap, bool v_side, uint32_t dst, int atom_bytes,
+                                              Load load) {
+  const CUtensorMap* whole = v_side ? &p.map_v : &p.map_k;
+  if (kOrder == kOrderWindow && v0 < p.sink_rows && v0 + rows > p.sink_rows) {        // the last of the first tokens, and the window
+    for (int a = 0; a < kAtoms; ++a) {
+      load(dst + a * atom_bytes, v_side ? &p.map_v_first : &p.map_k_first, a * 64, v0);
+      load(dst + a * atom_bytes + (p.sink_rows - v0) * 128, v_side ? &p.map_v_rest : &p.map_k_rest, a * 64, p.sink_rows + gap);
+    }
+    return;
+  }
+  const int key = kOrder == kOrderWindow && v0 >= p.sink_rows ? v0 + gap : v0;
+  for (int a = 0; a < kAtoms; ++a) load(dst + a * atom_bytes, whole, a * 64, key);
 }
 
 // What a thread block works on: unit `index` of a sequence, of its `count`, and the sequence's token ranges.

@@ -227,9 +227,10 @@ __device__ __forceinline__ void store_share(const RowAddresses& rows, uint32_t t
 }
 
 // ------------------------------------------------------------------------------------ dK, dV
-template <typename T, int D, int kHalves, bool kCausal>
+template <typename T, int D, int kHalves, int kOrder>
 __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
   using C = BwdCfg<D, kHalves>;
+  constexpr bool kCausal = kOrder != kOrderNone;
   uint8_t* sK = smem;
   uint8_t* sV = smem + C::kTileBytes;
   uint8_t* sA = smem + 2 * C::kTileBytes;                   // Q tiles
@@ -273,9 +274,13 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
   const int n_tiles_all = (qr.len + tile_tokens - 1) / tile_tokens;
   // causal: key j is seen by the tokens from j - ahead on
   const int first_tile = kCausal ? max(key0 - ahead, 0) / tile_tokens : 0;
-  const int n_all = max(n_tiles_all - first_tile, 0), n = n_all;
+  // window: key j is seen by the tokens up to j + window - 1 - ahead, one of the first tokens by all behind it
+  int end_tile = n_tiles_all;
+  if (kOrder == kOrderWindow && key0 >= p.sinks)
+    end_tile = (int)min((long long)end_tile, max((long long)key0 + kTileM - 1 + p.window - ahead + tile_tokens - 1, 0ll) / tile_tokens);
+  const int n_all = max(end_tile - first_tile, 0), n = n_all;
   const int tail_rows = (qr.len - (n_tiles_all - 1) * tile_tokens) * p.group;      // rows of the last tile
-  const bool tail_all = n > 0 && tail_rows < box_rows, tail = tail_all;
+  const bool tail_all = n > 0 && end_tile == n_tiles_all && tail_rows < box_rows, tail = tail_all;
   volatile int* abort_flag = &ctl->abort_flag;
 
   if (warp >= C::kSoftWarps) {
@@ -429,6 +434,9 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
     const float scale_log2 = p.sm_scale * kLog2e;
     const uint64_t scale2 = pack2(scale_log2, scale_log2);
     int blind_tok = key0 + r - ahead - first_tile * tile_tokens;         // tokens of the first tile in front of the first seer
+    // window: tokens of the first tile in front of the last seer's successor
+    int gone_tok = kOrder == kOrderWindow ? (int)min((long long)blind_tok + p.window, 1ll << 30) : 0;
+    const bool stays = kOrder == kOrderWindow && key0 + r < p.sinks;
     bool alive = true;
     for (int i = 0; i < n; ++i) {
       const int st = i % kStatStages;
@@ -460,6 +468,15 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
 #pragma unroll
         for (int c = 0; c < 64; ++c)
           if (c < blind) pr[c] = 0.f;
+      }
+      if (kOrder == kOrderWindow) {                          // columns from `gone` on have left this key behind
+        const int gone = stays ? kTileM : max(min(gone_tok, kTileM), 0) * p.group - h * 64;
+        gone_tok -= tile_tokens;
+        if (__any_sync(0xffffffffu, gone < 64)) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c >= gone) pr[c] = 0.f;
+        }
       }
       {
         uint32_t pk[32];
@@ -523,9 +540,10 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
 }
 
 // ------------------------------------------------------------------------------------ dQ
-template <typename T, int D, int kHalves, bool kCausal>
+template <typename T, int D, int kHalves, int kOrder>
 __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
   using C = BwdCfg<D, kHalves>;
+  constexpr bool kCausal = kOrder != kOrderNone;
   uint8_t* sQ = smem;
   uint8_t* sDO = smem + C::kTileBytes;
   uint8_t* sA = smem + 2 * C::kTileBytes;                   // K tiles
@@ -565,9 +583,10 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
   }
   const int ahead = kr.len - qr.len;
   const int last_tok = min(tok0 + tile_tokens, qr.len) - 1;
-  const int keys = kCausal ? min(max(last_tok + 1 + ahead, 0), kr.len) : kr.len;
+  const tra_key_axis<kOrder> axis(p, tok0 + ahead, kr.len);
+  const int keys = kCausal ? min(max(last_tok + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
   const int n_all = (keys + C::kStream - 1) / C::kStream, n = n_all;
-  const bool tail_all = n > 0 && n * C::kStream > kr.len, tail = tail_all;
+  const bool tail_all = n > 0 && n * C::kStream > axis.len, tail = tail_all;
   volatile int* abort_flag = &ctl->abort_flag;
 
   if (warp >= C::kSoftWarps) {
@@ -584,18 +603,22 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
         bwd_produce<C>(
             ctl, n, tail, C::kStreamBytes, abort_flag, p.status,
             [&](int i, int slot, uint32_t bar) {
-              for (int a = 0; a < C::kAtoms; ++a)
-                tma_load_3d(smem_u32(sA + slot * C::kStreamBytes + a * C::kStreamAtom), &p.map_k, bar, a * 64, kvh, kr.begin + i * C::kStream);
+              tra_load_keys<kOrder, C::kAtoms>(p, i * C::kStream, C::kStream, axis.gap, false, smem_u32(sA + slot * C::kStreamBytes), C::kStreamAtom,
+                                               [&](uint32_t dst, const CUtensorMap* map, int channel, int key) {
+                                                 tma_load_3d(dst, map, bar, channel, kvh, kr.begin + key);
+                                               });
             },
             [&](int i, int slot, uint32_t bar) {
-              for (int a = 0; a < C::kAtoms; ++a)
-                tma_load_3d(smem_u32(sB + slot * C::kStreamBytes + a * C::kStreamAtom), &p.map_v, bar, a * 64, kvh, kr.begin + i * C::kStream);
+              tra_load_keys<kOrder, C::kAtoms>(p, i * C::kStream, C::kStream, axis.gap, true, smem_u32(sB + slot * C::kStreamBytes), C::kStreamAtom,
+                                               [&](uint32_t dst, const CUtensorMap* map, int channel, int key) {
+                                                 tma_load_3d(dst, map, bar, channel, kvh, kr.begin + key);
+                                               });
             });
       }
     } else if (warp == C::kSoftWarps + 2) {
       // ================================================================== rows past the sequence's end
       if (tail && mbar_wait_warp(smem_u32(&ctl->tail_full), 0u, abort_flag, p.status)) {
-        const int row0 = kr.len - (n - 1) * C::kStream;
+        const int row0 = axis.len - (n - 1) * C::kStream;
         zero_tile_rows(sA + ((n - 1) % C::kA) * C::kStreamBytes, row0, C::kStream, C::kAtoms, C::kStreamAtom, lane, 32);
         zero_tile_rows(sB + ((n - 1) % C::kB) * C::kStreamBytes, row0, C::kStream, C::kAtoms, C::kStreamAtom, lane, 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -682,7 +705,7 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
     delta *= tau;
     const uint64_t scale2 = pack2(scale_log2, scale_log2), neg_lse2 = pack2(-lse2, -lse2), neg_delta2 = pack2(-delta, -delta);
     const uint64_t tau2 = pack2(tau, tau);
-    const int seen = kCausal ? min(max(min(tok, last_tok) + 1 + ahead, 0), kr.len) : kr.len;
+    const int seen = kCausal ? min(max(min(tok, last_tok) + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
     RingPos<C::kA> kd;                                       // K of the step before
     bool alive = true;
     for (int i = 0; i < n; ++i) {
@@ -708,6 +731,14 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
 #pragma unroll
         for (int c = 0; c < 64; ++c)
           if (c >= limit) pr[c] = 0.f;
+      }
+      if (kOrder == kOrderWindow) {                          // columns in front of `old` are out of the window but for the first tokens
+        const int old = limit - p.window, first = p.sinks - i * C::kStream - h * 64;
+        if (__any_sync(0xffffffffu, old > max(first, 0))) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c < old && c >= first) pr[c] = 0.f;
+        }
       }
       if (!mbar_wait_warp(smem_u32(&ctl->dp_full), (uint32_t)i & 1u, abort_flag, p.status)) {
         alive = false;
@@ -755,15 +786,15 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
 // Blocks of either kind in one launch, so that the shorter dQ blocks fill the SMs that the last dK/dV blocks leave: first
 // dkv_units per key/value head, then dq_units.  Of a causal sequence the first keys and the last queries have most to
 // do, and come first.
-template <typename T, int D, int kHalves, bool kCausal>
+template <typename T, int D, int kHalves, int kOrder>
 __global__ void __launch_bounds__(BwdCfg<D, kHalves>::kThreads, BwdCfg<D, kHalves>::kBlocks)
     tra_packed_bwd_kernel(const __grid_constant__ tra_packed_launch p, int dkv_units, int dq_units) {
   extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
   const int n_dkv = dkv_units * p.kv_heads, b = blockIdx.x;
   if (b < n_dkv)
-    dkv_block<T, D, kHalves, kCausal>(p, smem, b % dkv_units, b / dkv_units);
+    dkv_block<T, D, kHalves, kOrder>(p, smem, b % dkv_units, b / dkv_units);
   else
-    dq_block<T, D, kHalves, kCausal>(p, smem, (b - n_dkv) % dq_units, (b - n_dkv) / dq_units);
+    dq_block<T, D, kHalves, kOrder>(p, smem, (b - n_dkv) % dq_units, (b - n_dkv) / dq_units);
 }
 
 // ------------------------------------------------------------------------------------ delta
@@ -878,7 +909,7 @@ int launch_delta_norms(const tra_packed_ctx& c, const tra_packed_launch& a) {
   return tra_launch(tra_packed_delta_norms_kernel<D>, dim3((unsigned)(q_blocks + v_blocks)), 256, 0, c.stream, false, 1, a, (int)q_blocks, (int)steps);
 }
 
-template <typename T, int D, int kHalves, bool kCausal>
+template <typename T, int D, int kHalves, int kOrder>
 int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   const long long rows = (long long)a.total_q * a.heads;
   int rc = TRA_OK;
@@ -896,7 +927,7 @@ int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   if (blocks == 0) return TRA_OK;
   if (blocks > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
   using C = BwdCfg<D, kHalves>;
-  constexpr auto kern = tra_packed_bwd_kernel<T, D, kHalves, kCausal>;
+  constexpr auto kern = tra_packed_bwd_kernel<T, D, kHalves, kOrder>;
   if ((rc = tra_allow_smem<kern>(C::kSmemBytes)) != TRA_OK) return rc;
   return tra_launch(kern, dim3((unsigned)blocks), C::kThreads, C::kSmemBytes, c.stream, rows > 0, 1, a, dkv_units, dq_units);
 }
@@ -904,8 +935,12 @@ int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
 template <int D, int kHalves>
 int launch_bwd_shape(const tra_packed_ctx& c, const tra_packed_launch& a) {
   if (c.h->cfg.dtype == TRA_BF16)
-    return a.causal ? launch_bwd<__nv_bfloat16, D, kHalves, true>(c, a) : launch_bwd<__nv_bfloat16, D, kHalves, false>(c, a);
-  return a.causal ? launch_bwd<__half, D, kHalves, true>(c, a) : launch_bwd<__half, D, kHalves, false>(c, a);
+    return a.order == kOrderCausal ? launch_bwd<__nv_bfloat16, D, kHalves, kOrderCausal>(c, a) : launch_bwd<__nv_bfloat16, D, kHalves, kOrderNone>(c, a);
+  return a.order == kOrderCausal ? launch_bwd<__half, D, kHalves, kOrderCausal>(c, a) : launch_bwd<__half, D, kHalves, kOrderNone>(c, a);
+}
+template <int D, int kHalves>
+int launch_bwd_window(const tra_packed_ctx& c, const tra_packed_launch& a) {
+  return c.h->cfg.dtype == TRA_BF16 ? launch_bwd<__nv_bfloat16, D, kHalves, kOrderWindow>(c, a) : launch_bwd<__half, D, kHalves, kOrderWindow>(c, a);
 }
 
 }  // namespace

@@ -76,22 +76,25 @@ struct FwdCtl {
 static_assert(sizeof(FwdCtl) <= 512, "control block");
 
 // What a unit asks of every role.
-template <bool kCausal>
+template <int kOrder>
 struct FwdPlan {
   int tok0;                   // first token of tile 0, inside the sequence
-  int v_begin, n_entries;     // key blocks v_begin .. v_begin + n_entries - 1
+  int gap;                    // of the key axis (tra_key_axis)
+  int v_begin, n_entries;     // key blocks v_begin .. v_begin + n_entries - 1 of it
   int n_own[2];               // entries of each tile (n_own[0] <= n_own[1] where there is a second tile)
   bool tail;                  // the last V tile reaches past the sequence
   __device__ __forceinline__ FwdPlan(const FwdWork& w, const tra_packed_launch& p) {
     const int q_len = w.unit.q.len, k_len = w.unit.k.len;
     tok0 = w.unit.index * 2 * p.tile_tokens;
     const int ahead = k_len - q_len;                      // causal: token i sees keys 0 .. i + ahead
+    const tra_key_axis<kOrder> axis(p, tok0 + ahead, k_len);
+    gap = axis.gap;
     int blocks[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int first = tok0 + k * p.tile_tokens;
       const int last = min(first + p.tile_tokens, q_len) - 1;
-      const int keys = first >= q_len ? 0 : kCausal ? min(max(last + 1 + ahead, 0), k_len) : k_len;
+      const int keys = first >= q_len ? 0 : kOrder ? min(max(last + 1 + ahead - gap, 0), axis.len) : k_len;
       blocks[k] = (keys + kKeyTile - 1) / kKeyTile;
     }
     const int nb = max(blocks[0], blocks[1]);
@@ -101,7 +104,7 @@ struct FwdPlan {
     n_entries = v_end - v_begin;
 #pragma unroll
     for (int k = 0; k < 2; ++k) n_own[k] = max(min(blocks[k], v_end) - v_begin, 0);
-    tail = n_entries > 0 && v_end * kKeyTile > k_len;
+    tail = n_entries > 0 && v_end * kKeyTile > axis.len;
   }
 };
 
@@ -168,9 +171,10 @@ __device__ __forceinline__ void store_unit(const tra_packed_launch& p, FwdCtl* c
 
 // Blocks that stay, one per SM: while the softmax warps finish a unit, the loads and the first scores of the next one are under
 // way already (a block per unit spent about 10 us on set-up, first loads and epilogue: as much as five key blocks).
-template <typename T, int D, bool kCausal, bool kExact>
+template <typename T, int D, int kOrder, bool kExact>
 __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __grid_constant__ tra_packed_launch p) {
   using C = FwdCfg<D>;
+  constexpr bool kCausal = kOrder != kOrderNone;
   extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
   uint8_t* sQ = smem;
   uint8_t* sKV = smem + 2 * C::kTileBytes;
@@ -279,7 +283,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       for (int n = 0; alive && next_work(n); ++n) {
         const FwdWork w = ctl->work[n & 1];
         done_with_work(n);
-        const FwdPlan<kCausal> u(w, p);
+        const FwdPlan<kOrder> u(w, p);
         if (u.n_entries <= kAskAhead && lane == 0) mbar_arrive(smem_u32(&ctl->want));
         if (u.n_entries == 0) continue;
         if (lane == 0) {
@@ -312,9 +316,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
                 bar = smem_u32(&ctl->tail_full[tails & 1]);
               }
               mbar_expect_tx(bar, C::kTileBytes);
-              for (int a = 0; a < C::kAtoms; ++a)
-                tma_load_3d(smem_u32(sKV + slot * C::kTileBytes + a * C::kAtomBytes), kv == 0 ? &p.map_k : &p.map_v, bar,
-                            a * 64, w.kvh, w.unit.k.begin + (u.v_begin + e) * kKeyTile);
+              tra_load_keys<kOrder, C::kAtoms>(p, (u.v_begin + e) * kKeyTile, kKeyTile, u.gap, kv == 1, smem_u32(sKV + slot * C::kTileBytes), C::kAtomBytes,
+                                               [&](uint32_t dst, const CUtensorMap* map, int channel, int key) {
+                                                 tma_load_3d(dst, map, bar, channel, w.kvh, w.unit.k.begin + key);
+                                               });
               if (++slot == C::kSlots) slot = 0;
             }
           }
@@ -330,11 +335,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       for (int n = 0; next_work(n); ++n) {
         const FwdWork w = ctl->work[n & 1];
         done_with_work(n);
-        const FwdPlan<kCausal> u(w, p);
+        const FwdPlan<kOrder> u(w, p);
         if (!u.tail) continue;
         if (!mbar_wait_warp(smem_u32(&ctl->tail_full[tails & 1]), (uint32_t)(tails >> 1) & 1u, abort_flag, p.status)) break;
         const int slot = *(volatile int*)&ctl->tail_slot[tails & 1];
-        zero_tile_rows(sKV + slot * C::kTileBytes, w.unit.k.len - (u.v_begin + u.n_entries - 1) * kKeyTile, kKeyTile, C::kAtoms,
+        zero_tile_rows(sKV + slot * C::kTileBytes, w.unit.k.len - u.gap - (u.v_begin + u.n_entries - 1) * kKeyTile, kKeyTile, C::kAtoms,
                        C::kAtomBytes, lane, 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -390,7 +395,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       for (int n = 0; alive && uniform(next_work(n)); ++n) {
         const FwdWork w = ctl->work[n & 1];
         done_with_work(n);
-        FwdPlan<kCausal> u(w, p);
+        FwdPlan<kOrder> u(w, p);
         u.n_entries = uniform(u.n_entries);
         u.n_own[0] = uniform(u.n_own[0]);
         u.n_own[1] = uniform(u.n_own[1]);
@@ -459,11 +464,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
     bool alive = true;
     for (int it = 0; alive && next_work(it); ++it) {
       float m = -INFINITY, l = 0.f, l_exact = 0.f;
-      int n, col_limit;
+      int n, col_limit, first_cols = 0;       // first_cols: columns in front of it are seen whatever the window
       bool rows_here;
       {
         const FwdWork w = ctl->work[it & 1];
-        const FwdPlan<kCausal> u(w, p);
+        const FwdPlan<kOrder> u(w, p);
         n = u.n_own[k];
         const int tile_tok = u.tok0 + k * p.tile_tokens;
         // (opaque to the compiler: what follows from the thread index alone would be kept in registers through all units)
@@ -474,7 +479,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         // columns of the first block that the row sees; rows that hold no query follow the tile's last one, so that they
         // force no mask on their warp
         const int mask_tok = min(tile_tok + r / p.group, min(tile_tok + p.tile_tokens, w.unit.q.len) - 1);
-        col_limit = (kCausal ? min(max(mask_tok + 1 + w.unit.k.len - w.unit.q.len, 0), w.unit.k.len) : w.unit.k.len) - u.v_begin * kKeyTile;
+        col_limit = (kCausal ? min(max(mask_tok + 1 + w.unit.k.len - w.unit.q.len - u.gap, 0), w.unit.k.len) : w.unit.k.len) - u.v_begin * kKeyTile;
+        if (kOrder == kOrderWindow) first_cols = p.sinks - u.v_begin * kKeyTile;
       }
       if (!rows_here) {
         // a warp without a row keeps up with the barriers; what its lanes multiply stays in its own, unstored rows
@@ -502,6 +508,20 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
           tmem_wait_ld(&sb[0]);
 #pragma unroll
           for (int c = 1; c < 4; ++c) reg_fence32(&sb[c * 32]);
+          if constexpr (kOrder == kOrderWindow) {
+            // columns from `old` on are in the window, those below first_cols are seen all the same
+            const int old = col_limit - p.window;
+            if (__any_sync(0xffffffffu, old > max(first_cols, 0))) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                if (!__any_sync(0xffffffffu, old > max(first_cols, c * 32) && first_cols < c * 32 + 32)) continue;
+#pragma unroll
+                for (int j = c * 32; j < c * 32 + 32; ++j)
+                  if (j < old && j >= first_cols) sb[j] = 0xff800000u;      // -inf
+              }
+            }
+            first_cols -= kKeyTile;
+          }
           if (__any_sync(0xffffffffu, col_limit < kKeyTile)) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -600,9 +620,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
   }
 }
 
-template <typename T, int D, bool kCausal, bool kExact>
+template <typename T, int D, int kOrder, bool kExact>
 int launch_fwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
-  constexpr auto kern = tra_packed_fwd_kernel<T, D, kCausal, kExact>;
+  constexpr auto kern = tra_packed_fwd_kernel<T, D, kOrder, kExact>;
   const int rc = tra_allow_smem<kern>(FwdCfg<D>::kSmemBytes);
   if (rc != TRA_OK) return rc;
   const long long units = (long long)a.n_units * a.kv_heads * a.splits;
@@ -611,15 +631,21 @@ int launch_fwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
                     1, a);
 }
 
+template <typename T, int D, int kOrder>
+int launch_fwd_order(const tra_packed_ctx& c, const tra_packed_launch& a) {
+  return a.lse ? launch_fwd<T, D, kOrder, true>(c, a) : launch_fwd<T, D, kOrder, false>(c, a);
+}
+
+// The two orders without a window, and the one with (translation units of their own).
 template <int D>
 int launch_fwd_shape(const tra_packed_ctx& c, const tra_packed_launch& a) {
-  const bool exact = a.lse != nullptr;
-  if (c.h->cfg.dtype == TRA_BF16) {
-    if (a.causal) return exact ? launch_fwd<__nv_bfloat16, D, true, true>(c, a) : launch_fwd<__nv_bfloat16, D, true, false>(c, a);
-    return exact ? launch_fwd<__nv_bfloat16, D, false, true>(c, a) : launch_fwd<__nv_bfloat16, D, false, false>(c, a);
-  }
-  if (a.causal) return exact ? launch_fwd<__half, D, true, true>(c, a) : launch_fwd<__half, D, true, false>(c, a);
-  return exact ? launch_fwd<__half, D, false, true>(c, a) : launch_fwd<__half, D, false, false>(c, a);
+  if (c.h->cfg.dtype == TRA_BF16)
+    return a.order == kOrderCausal ? launch_fwd_order<__nv_bfloat16, D, kOrderCausal>(c, a) : launch_fwd_order<__nv_bfloat16, D, kOrderNone>(c, a);
+  return a.order == kOrderCausal ? launch_fwd_order<__half, D, kOrderCausal>(c, a) : launch_fwd_order<__half, D, kOrderNone>(c, a);
+}
+template <int D>
+int launch_fwd_window(const tra_packed_ctx& c, const tra_packed_launch& a) {
+  return c.h->cfg.dtype == TRA_BF16 ? launch_fwd_order<__nv_bfloat16, D, kOrderWindow>(c, a) : launch_fwd_order<__half, D, kOrderWindow>(c, a);
 }
 
 }  // namespace

@@ -1,6 +1,8 @@
 // Attention of few rows over many keys: one new token of every sequence (or a few), over a key/value cache split along
 // its length.  At most 16 rows (tokens times the heads of a group) per sequence and key/value head.
 //
+// With a window the keys in front of it are not read, but for the first tokens (tra_key_axis).
+//
 // Bound: HBM, every key and value is read once and used for at most 16 rows.  A thread block takes `chunk` keys of one
 // (sequence, key/value head): a producer warp streams 64-key tiles of K and V through a ring of TMA
 // loads (96 KB in flight per block, two blocks per SM), and four warps take sixteen keys of every tile each, with a running
@@ -83,8 +85,8 @@ __device__ __forceinline__ float4 cluster_ld4(const void* own_address, uint32_t 
   return v;
 }
 
-// sequence = blockIdx.x, key/value head = blockIdx.y, part = blockIdx.z (keys [part * chunk, ...)); chunk is a multiple of 64
-template <typename T, int D>
+// sequence = blockIdx.x, key/value head = blockIdx.y, part = blockIdx.z (keys [part * chunk, ...) of the key axis); chunk is a multiple of 64
+template <typename T, int D, bool kWindow>
 __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const __grid_constant__ tra_packed_launch p, int chunk, int clustered) {
   using C = RowsCfg<D>;
   extern __shared__ uint8_t smem_raw[];
@@ -99,7 +101,8 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
   const int n_rows = qr.len * p.group;                       // <= 16
   if (n_rows == 0) return;
   const int ahead = kr.len - qr.len;
-  const int key0 = (int)blockIdx.z * chunk, key1 = min(key0 + chunk, kr.len);     // chunk * parts fits an int
+  const tra_key_axis<kWindow ? kOrderWindow : kOrderCausal> axis(p, ahead, kr.len);
+  const int key0 = (int)blockIdx.z * chunk, key1 = min(key0 + chunk, axis.len);     // chunk * parts fits an int
   const int n_tiles = key1 > key0 ? (key1 - key0 + kRowsTile - 1) / kRowsTile : 0;
   const long long part_base = (long long)blockIdx.z * p.total_q * p.heads;
   auto row_token = [&](int r) -> long long { return qr.begin + r / p.group; };
@@ -141,9 +144,9 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
         const uint32_t bar = smem_u32(&ctl->full[slot]);
         mbar_expect_tx(bar, 2 * C::kTileBytes);
         for (int kv = 0; kv < 2; ++kv)
-          for (int a = 0; a < C::kAtoms; ++a)
-            tma_load_3d(smem_u32(smem + (2 * slot + kv) * C::kTileBytes + a * C::kAtomBytes), kv == 0 ? &p.map_k : &p.map_v,
-                        bar, a * 64, kvh, kr.begin + key0 + t * kRowsTile);
+          tra_load_keys<kWindow ? kOrderWindow : kOrderCausal, C::kAtoms>(
+              p, key0 + t * kRowsTile, kRowsTile, axis.gap, kv == 1, smem_u32(smem + (2 * slot + kv) * C::kTileBytes), C::kAtomBytes,
+              [&](uint32_t dst, const CUtensorMap* map, int channel, int key) { tma_load_3d(dst, map, bar, channel, kvh, kr.begin + key); });
         if (++slot == C::kStages) {
           slot = 0;
           phase ^= 1u;
@@ -169,9 +172,10 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int t = min((g + 8 * half) / p.group, qr.len - 1);
-      seen[half] = p.causal ? min(max(t + 1 + ahead, 0), kr.len) : kr.len;
+      seen[half] = p.order ? min(max(t + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
     }
-    const int seen_min = p.causal ? min(max(1 + ahead, 0), kr.len) : kr.len;       // of the first token
+    const int seen_min = p.order ? min(max(1 + ahead - axis.gap, 0), axis.len) : kr.len;       // of the first token
+    const int old_max = kWindow ? qr.len + ahead - axis.gap - p.window : 0;        // keys that have left the last token's window
     const int row_in_tile = warp * 16;
     int slot = 0;
     uint32_t phase = 0u;
@@ -200,6 +204,15 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
             mma16816<T>(s[0], qa[kk], b[0], b[1]);
             mma16816<T>(s[1], qa[kk], b[2], b[3]);
           }
+        }
+        if (kWindow && k0 < old_max && k0 + 16 > p.sinks) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int v = k0 + (j >> 1) * 8 + tig * 2 + (j & 1);
+              if (v < seen[half] - p.window && v >= p.sinks) s[j >> 1][half * 2 + (j & 1)] = -INFINITY;
+            }
         }
         if (k0 + 16 > min(seen_min, key1)) {
 #pragma unroll
@@ -369,13 +382,18 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
   }
 }
 
-template <typename T, int D>
-int launch_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered) {
-  constexpr auto kern = tra_packed_rows_kernel<T, D>;
+template <typename T, int D, bool kWindow>
+int launch_rows_kernel(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered) {
+  constexpr auto kern = tra_packed_rows_kernel<T, D, kWindow>;
   const int rc = tra_allow_smem<kern>(RowsCfg<D>::kSmemBytes);
   if (rc != TRA_OK) return rc;
   return tra_launch(kern, dim3((unsigned)a.n_seq, (unsigned)a.kv_heads, (unsigned)a.splits), kRowsThreads, RowsCfg<D>::kSmemBytes, c.stream,
                     false, clustered ? a.splits : 1, a, chunk, clustered ? 1 : 0);
+}
+
+template <typename T, int D>
+int launch_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered) {
+  return a.order == kOrderWindow ? launch_rows_kernel<T, D, true>(c, a, chunk, clustered) : launch_rows_kernel<T, D, false>(c, a, chunk, clustered);
 }
 
 }  // namespace
