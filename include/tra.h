@@ -434,6 +434,41 @@ size_t tra_packed_attn_backward_workspace_bytes(const tra_packed_t* packed, int 
 int tra_packed_attn_backward(const tra_packed_t* packed, const tra_packed_args_t* args, const tra_packed_grads_t* grads,
                              void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- a cache of 4 bits: keys and values quantised as they are written, read back, and attended over (long streams whose
+ * cache would not fit, or whose reading bounds every new token) ---- */
+
+/* Heads, head_dim and type are those of a tra_packed_t.  A row (one token of one key/value head) is held in groups of 32 channels:
+ *   low = the group's smallest element, step = the smallest number of the type with 15 step >= largest - low,
+ *   code = floor((x - low) / step + 1/2) in 0 .. 15; it stands for low + code step, so that it is off by step / 2 at most.
+ * A group that holds a NaN or an infinity reads back as NaN.  Where the codes lie inside a row is the library's affair: rows are
+ * written and read by these calls.  A row takes d / 2 + d / 8 bytes, for keys and for values each. */
+typedef struct {
+  void *k, *v;             /* [kv_heads, tokens, d / 2] bytes, 16-byte aligned                                          */
+  void *k_step, *v_step;   /* [kv_heads, tokens, 2, d / 32] of the type: steps, then lowest values; 16-byte aligned     */
+  int tokens;              /* rows of every head: even, at most 2^30                                                   */
+} tra_cache4_t;
+
+/* Token i of k and v ([n, kv_heads, d] behind strides (token, head), elements, multiples of 8; 16-byte aligned) goes to row slots[i] of the
+ * cache (device int32 [n]); a negative slot is left out, one past the cache is left out and reported (tra_packed_status:
+ * TRA_ERR_INVALID_ARG).  The slots of one call are distinct; what a slot that is named twice holds afterwards is not specified.
+ * Errors: TRA_ERR_INVALID_ARG, TRA_ERR_UNSUPPORTED, TRA_ERR_CUDA. */
+int tra_cache4_write(const tra_packed_t* packed, const tra_cache4_t* cache, const void* k, const void* v, const int64_t* k_stride,
+                     const int64_t* v_stride, const int32_t* slots, int n, void* stream);
+
+/* The way back: rows slots[i] of the cache, rounded once to the type, to token i of k and v.  Tokens of slots that are left out stay as
+ * they are.  A slot may be named several times. */
+int tra_cache4_read(const tra_packed_t* packed, const tra_cache4_t* cache, void* k, void* v, const int64_t* k_stride, const int64_t* v_stride,
+                    const int32_t* slots, int n, void* stream);
+
+/* Attention over the cache: tra_packed_attn with the values that the codes stand for as keys and values (not rounded to the type; where a
+ * sequence has more than 64 rows per key/value head, they are read back, rounded, into the workspace first, half a gigabyte or one sequence
+ * at a time).  k_begin, k_end: rows of the cache.  args->k, v and their strides are not used, total_k is the cache's tokens; o_rest must be
+ * NULL (there are no gradients with respect to a cache).  What lies in rows outside the sequences' ranges may be anything.  Workspace,
+ * status and errors as for tra_packed_attn. */
+size_t tra_packed_attn_cache4_workspace_bytes(const tra_packed_t* packed, int n_seq, int total_q, int max_q, int max_k);
+int tra_packed_attn_cache4(const tra_packed_t* packed, const tra_packed_args_t* args, const tra_cache4_t* cache, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

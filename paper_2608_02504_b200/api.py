@@ -41,6 +41,7 @@ EXPORTS = [
     "tra_rotary_backward",
     "tra_packed_create", "tra_packed_destroy", "tra_packed_status", "tra_packed_attn_workspace_bytes",
     "tra_packed_attn", "tra_packed_attn_backward_workspace_bytes", "tra_packed_attn_backward",
+    "tra_cache4_write", "tra_cache4_read", "tra_packed_attn_cache4_workspace_bytes", "tra_packed_attn_cache4",
 ]
 
 
@@ -90,6 +91,10 @@ class tra_packed_grads_t(ctypes.Structure):
         [(n, ctypes.c_int64 * 2) for n in ("do_stride", "dq_stride", "dk_stride", "dv_stride")]
 
 
+class tra_cache4_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_step", "v_step")] + [("tokens", ctypes.c_int)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -133,6 +138,11 @@ def _load():
     lib.tra_packed_attn_backward_workspace_bytes.argtypes = [vp, i32]
     lib.tra_packed_attn_backward_workspace_bytes.restype = ctypes.c_size_t
     lib.tra_packed_attn_backward.argtypes = [vp, vp, vp, vp, ctypes.c_size_t, vp]
+    for name in ("tra_cache4_write", "tra_cache4_read"):
+        getattr(lib, name).argtypes = [vp, vp, vp, vp, ctypes.c_int64 * 2, ctypes.c_int64 * 2, vp, i32, vp]
+    lib.tra_packed_attn_cache4_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
+    lib.tra_packed_attn_cache4_workspace_bytes.restype = ctypes.c_size_t
+    lib.tra_packed_attn_cache4.argtypes = [vp, vp, vp, vp, ctypes.c_size_t, vp]
     return lib
 
 
@@ -697,15 +707,18 @@ class PackedAttn:
             raise ValueError(f"{name}: expected a contiguous int32 tensor of {n} entries on {self.device}")
         return t.data_ptr()
 
-    def _args(self, q, k, v, o, lse, rest, cu_q, cu_k, k_range, max_q, max_k, sm_scale):
-        if q.dim() != 3 or k.dim() != 3 or cu_q.dim() != 1 or cu_q.shape[0] < 2:
+    def _args(self, q, k, v, o, lse, rest, cu_q, cu_k, k_range, max_q, max_k, sm_scale, cached=None):
+        if q.dim() != 3 or (cached is None and k.dim() != 3) or cu_q.dim() != 1 or cu_q.shape[0] < 2:
             raise ValueError("expected q, k, v [tokens, heads, head_dim] and cu_q [n_seq + 1]")
         if torch.cuda.current_device() != self._index:
             raise ValueError(f"the current device must be {self.device}")
-        tq, tk, n = q.shape[0], k.shape[0], cu_q.shape[0] - 1
+        tq, tk, n = q.shape[0], k.shape[0] if cached is None else cached, cu_q.shape[0] - 1
         qp, q0, q1 = self._tensor(q, "q", tq, self.heads)
-        kp, k0, k1 = self._tensor(k, "k", tk, self.kv_heads)
-        vp, v0, v1 = self._tensor(v, "v", tk, self.kv_heads)
+        if cached is None:
+            kp, k0, k1 = self._tensor(k, "k", tk, self.kv_heads)
+            vp, v0, v1 = self._tensor(v, "v", tk, self.kv_heads)
+        else:
+            kp = k0 = k1 = vp = v0 = v1 = 0
         op, o0, o1 = self._tensor(o, "o", tq, self.heads)
         lp = 0
         if lse is not None:
@@ -800,3 +813,69 @@ class PackedAttn:
         _check(_lib.tra_packed_attn_backward(self._h, a, g, ws.data_ptr() if n else None, n, _raw_stream(self._index)),
                "tra_packed_attn_backward")
         return dq, dk, dv
+
+    def forward_cache4(self, q, cache, cu_q, *, k_range, max_q, max_k, o=None, lse=None, want_lse=False, sm_scale=None):
+        """``forward`` over a ``Cache4``: sequence s attends to the rows k_range[0][s] .. k_range[1][s] - 1 of the cache -> (o, lse).
+        ``max_k``: upper bound of the sequences' keys, at most the cache's tokens."""
+        cache._fits(self)
+        if o is None:
+            o = _empty_like(q)
+        if lse is None and want_lse:
+            lse = q.new_empty((q.shape[0], self.heads), dtype=torch.float32)
+        if k_range is None:
+            raise ValueError("k_range: expected (begin, end)")
+        a = self._args(q, None, None, o, lse, None, cu_q, None, k_range, max_q, max_k, sm_scale, cached=cache.tokens)
+        n = _lib.tra_packed_attn_cache4_workspace_bytes(self._h, cu_q.shape[0] - 1, q.shape[0], max_q, max_k)
+        ws = q.new_empty((n,), dtype=torch.uint8) if n else None
+        _check(_lib.tra_packed_attn_cache4(self._h, a, cache._desc, ws.data_ptr() if n else None, n, _raw_stream(self._index)),
+               "tra_packed_attn_cache4")
+        return o, lse
+
+
+class Cache4:
+    """Keys and values in 4 bits, groups of 32 channels with a step and a lowest value each (``tra_cache4_write``): 0.625 bytes a
+    channel.  ``attn``: the ``PackedAttn`` whose heads, head_dim, type and device it has; it may be used with others like it.
+    ``tokens``: rows, rounded up to an even number (``cache.tokens``).
+
+    Rows are written and read by slot; ``PackedAttn.forward_cache4`` attends over ranges of them.  Contents start undefined:
+    ranges name written rows only."""
+
+    def __init__(self, attn, tokens):
+        if tokens < 0:
+            raise ValueError("tokens: expected a number of rows")
+        self.attn, self.tokens = attn, tokens + tokens % 2
+        heads, d = attn.kv_heads, attn.head_dim
+        self.k, self.v = (torch.empty((heads, self.tokens, d // 2), dtype=torch.uint8, device=attn.device) for _ in range(2))
+        self.k_step, self.v_step = (torch.empty((heads, self.tokens, 2, d // 32), dtype=attn.dtype, device=attn.device) for _ in range(2))
+        self._desc = bytes(tra_cache4_t(*(t.data_ptr() for t in (self.k, self.v, self.k_step, self.v_step)), self.tokens))
+
+    def _fits(self, attn):
+        a = self.attn
+        if attn is not a and (attn.kv_heads, attn.head_dim, attn.dtype, attn._index) != (a.kv_heads, a.head_dim, a.dtype, a._index):
+            raise ValueError("cache: made for other heads, another head_dim, type or device")
+
+    def _rows(self, call, name, k, v, slots):
+        attn = self.attn
+        if slots.dim() != 1 or k.dim() != 3 or v.dim() != 3:
+            raise ValueError("expected k, v [n, kv_heads, head_dim] and slots [n]")
+        if torch.cuda.current_device() != attn._index:
+            raise ValueError(f"the current device must be {attn.device}")
+        n = slots.shape[0]
+        at = attn._ints(slots, "slots", n)
+        (kp, *ks), (vp, *vs) = attn._tensor(k, "k", n, attn.kv_heads), attn._tensor(v, "v", n, attn.kv_heads)
+        stride = ctypes.c_int64 * 2
+        _check(call(attn._h, self._desc, kp, vp, stride(*ks), stride(*vs), at, n, _raw_stream(attn._index)), name)
+
+    def write(self, k, v, slots):
+        """Tokens k, v [n, kv_heads, head_dim] (any strides, multiples of 8 elements, with contiguous channels) into the rows ``slots``
+        (int32 [n], distinct; negative: not written; past the cache: not written and reported by ``attn.check_status``)."""
+        self._rows(_lib.tra_cache4_write, "tra_cache4_write", k, v, slots)
+
+    def read(self, slots, k=None, v=None):
+        """The rows ``slots`` -> (k, v) [n, kv_heads, head_dim], rounded to the type; rows of slots that are negative or past the cache
+        are left as they are (new tensors: undefined)."""
+        shape = (slots.shape[0], self.attn.kv_heads, self.attn.head_dim)
+        k = torch.empty(shape, dtype=self.attn.dtype, device=self.attn.device) if k is None else k
+        v = torch.empty(shape, dtype=self.attn.dtype, device=self.attn.device) if v is None else v
+        self._rows(_lib.tra_cache4_read, "tra_cache4_read", k, v, slots)
+        return k, v

@@ -1,0 +1,497 @@
+// The cache of 4 bits: keys and values are quantised as they are written, read back, and attended over.
+#include <string.h>
+
+#include "tra_cache4.h"
+#include "tra_packed_ptx.cuh"
+
+namespace {
+
+struct Cache4Rows {
+  const void *k, *v;                    // write: [n][kv_heads][d] behind strides; read: written
+  long long k_stride[2], v_stride[2];
+  uint8_t *k_codes, *v_codes;
+  void *k_step, *v_step;
+  const int32_t* slots;
+  int n, tokens;
+  int* status;
+};
+
+template <typename T>
+struct Pair;
+template <>
+struct Pair<__half> {
+  using type = __half2;
+};
+template <>
+struct Pair<__nv_bfloat16> {
+  using type = __nv_bfloat162;
+};
+template <typename T>
+__device__ __forceinline__ typename Pair<T>::type as_pair(uint32_t x) {
+  return *reinterpret_cast<typename Pair<T>::type*>(&x);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t as_bits(typename Pair<T>::type x) {
+  return *reinterpret_cast<uint32_t*>(&x);
+}
+
+// ------------------------------------------------------------------------------------ write
+// Of a group of 32 channels x: low = min x, step = the smallest number of the type with 15 step >= max x - low, code = floor((x - low) / step + 1/2)
+// (so that |x - (low + code step)| <= step / 2).  A group that holds a NaN or an infinity gets a step and a lowest value of NaN.
+//
+// The rounding is decided exactly (for x - low in fp32): the product with the reciprocal, taken a little too large so that halves go up,
+// gives a candidate that is right or one too high, and its remainder says which.
+//
+// Bound: HBM.  A thread takes one group, G = d / 32 neighbouring lanes a row; the codes' order inside a row needs words of all its groups side
+// by side, so that the lanes of a row exchange them.
+template <typename T>
+struct Group {
+  uint32_t x[16];              // pairs of channels
+  float mul, neg_low, inv, s;  // t = x mul - low mul, of steps s; inv a little above 1 / s, or 0
+  uint32_t packed;             // step, lowest value
+
+  __device__ __forceinline__ void measure() {
+    using P = typename Pair<T>::type;
+    P lo = as_pair<T>(x[0]), hi = lo;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) {
+      lo = __hmin2_nan(lo, as_pair<T>(x[i]));
+      hi = __hmax2_nan(hi, as_pair<T>(x[i]));
+    }
+    float lo0, lo1, hi0, hi1;
+    unpack_pair<T>(as_bits<T>(lo), lo0, lo1);
+    unpack_pair<T>(as_bits<T>(hi), hi0, hi1);
+    const bool finite = fabsf(lo0) < INFINITY && fabsf(lo1) < INFINITY && fabsf(hi0) < INFINITY && fabsf(hi1) < INFINITY;
+    const float l = fminf(lo0, lo1), h = fmaxf(hi0, hi1);
+    // in halves, so that a range past fp32 stays one
+    const float half_range = fmaf(h, 0.5f, -0.5f * l);
+    uint32_t bits = pack_pair<T>(half_range * (1.f / 7.5f), l);         // step (low half), lowest value
+    float st, unused;
+    unpack_pair<T>(bits, st, unused);
+    // (the product is within two units of the quotient, far less than a step of the type: at most one up or down)
+    if (7.5f * st < half_range) {
+      bits += 1u;
+    } else if (st > 0.f) {
+      float below, high;
+      unpack_pair<T>((bits & 0xffffu) - 1u, below, high);
+      if (7.5f * below >= half_range) bits -= 1u;
+    }
+    unpack_pair<T>(bits, st, unused);
+    if (!finite) bits = std::is_same<T, __half>::value ? 0x7e007e00u : 0x7fc07fc0u;
+    // steps of 2^-60 and less (bf16 only) are brought up first, so that their reciprocal is a number
+    mul = !std::is_same<T, __half>::value && st < 0x1p-60f ? 0x1p60f : 0.5f;
+    s = st * mul;
+    inv = finite && st > 0.f ? __frcp_rn(s) * (1.f + 0x1p-22f) : 0.f;
+    if (inv == 0.f) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0u;
+    }
+    neg_low = inv == 0.f ? 0.f : -l * mul;
+    packed = bits;
+  }
+  // code of one element, as a float
+  __device__ __forceinline__ float code(float v) const {
+    constexpr float kMagic = 12582912.f;                       // 1.5 2^23: the sum's last bit is 1
+    const float t = fmaf(v, mul, neg_low);
+    const float k = fmaf(t, inv, kMagic) - kMagic;
+    return fmaf(-k, s, t) < -0.5f * s ? k - 1.f : k;
+  }
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) tra_cache4_write_kernel(const __grid_constant__ Cache4Rows a) {
+  constexpr int G = D / kCacheGroup, kRowsPerBlock = 256 / G;
+  const int j = threadIdx.x % G, head = blockIdx.y;
+  const long long i = (long long)blockIdx.x * kRowsPerBlock + threadIdx.x / G;
+  const bool of_v = blockIdx.z != 0;
+  int slot = i < a.n ? a.slots[i] : -1;
+  if (slot >= a.tokens) {
+    tra_set_status(a.status, TRA_ERR_INVALID_ARG);
+    slot = -1;
+  }
+  if (!__any_sync(0xffffffffu, slot >= 0)) return;
+  Group<T> q;
+  const long long* stride = of_v ? a.v_stride : a.k_stride;
+  const T* src = (const T*)(of_v ? a.v : a.k) + (slot < 0 ? 0 : i * stride[0] + head * stride[1] + j * kCacheGroup);
+  if (slot >= 0) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint4 w = *reinterpret_cast<const uint4*>(src + c * 8);
+      q.x[4 * c] = w.x, q.x[4 * c + 1] = w.y, q.x[4 * c + 2] = w.z, q.x[4 * c + 3] = w.w;
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < 16; ++c) q.x[c] = 0u;
+  }
+  q.measure();
+  uint32_t out[4];             // words 4 j .. 4 j + 3 of the row
+  // four codes, as one number, 4 bits each
+  auto four = [](float a, float b, float c, float d) -> uint32_t { return (uint32_t)(int)fmaf(d, 4096.f, fmaf(c, 256.f, fmaf(b, 16.f, a))); };
+  if (!of_v) {
+    // word t of the group: channels 8 (n % 4) + 2 t + n / 4
+    uint32_t w[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      float lo[4], hi[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float x0, x1;
+        unpack_pair<T>(q.x[4 * c + t], x0, x1);
+        lo[c] = q.code(x0);
+        hi[c] = q.code(x1);
+      }
+      w[t] = four(lo[0], lo[1], lo[2], lo[3]) | four(hi[0], hi[1], hi[2], hi[3]) << 16;
+    }
+    // word t of group j lies at G t + j: a transposition among the row's lanes
+    if constexpr (G == 4) {
+#pragma unroll
+      for (int b = 1; b < 4; b <<= 1) {
+        const bool up = (j & b) != 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (u & b) continue;
+          const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[u] : w[u | b], b);
+          if (up)
+            w[u] = got;
+          else
+            w[u | b] = got;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) out[u] = w[u];
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, j ? w[u] : w[u + 2], 1);
+        out[2 * u] = j ? got : w[u];
+        out[2 * u + 1] = j ? w[u + 2] : got;
+      }
+    }
+  } else {
+    // half a word for every g: channels 8 n + g of the group; the other half is the neighbouring group's
+    uint32_t h[8];
+#pragma unroll
+    for (int g = 0; g < 8; g += 2) {
+      float c0[4], c1[4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        float x0, x1;
+        unpack_pair<T>(q.x[4 * n + g / 2], x0, x1);
+        c0[n] = q.code(x0);
+        c1[n] = q.code(x1);
+      }
+      h[g] = four(c0[0], c0[1], c0[2], c0[3]);
+      h[g + 1] = four(c1[0], c1[1], c1[2], c1[3]);
+    }
+    // lane pairs join halves: the even lane takes g = 0, 1, 4, 5 (d 64: 0 .. 3), the odd one the others
+    uint32_t w[4];
+    const bool odd = j & 1;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int mine = G == 4 ? (u & 1) + (u & 2) * 2 : u, other = G == 4 ? mine + 2 : u + 4;
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? h[mine] : h[other], 1);
+      w[u] = odd ? got | h[other] << 16 : h[mine] | got << 16;
+    }
+    if constexpr (G == 4) {
+      // words 2 g + w: lanes 0, 1 hold w = 0 of g = (0, 1, 4, 5), (2, 3, 6, 7), lanes 2, 3 hold w = 1 of them
+      const bool up = j & 2;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[u] : w[u + 2], 2);
+        out[2 * u] = up ? got : w[u];
+        out[2 * u + 1] = up ? w[u + 2] : got;
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) out[u] = w[u];
+    }
+  }
+  if (slot < 0) return;
+  const long long row = (long long)head * a.tokens + slot;
+  *reinterpret_cast<uint4*>((of_v ? a.v_codes : a.k_codes) + row * (D / 2) + j * 16) = make_uint4(out[0], out[1], out[2], out[3]);
+  uint16_t* st = (uint16_t*)(of_v ? a.v_step : a.k_step) + row * (2 * G);
+  st[j] = (uint16_t)q.packed;
+  st[G + j] = (uint16_t)(q.packed >> 16);
+}
+
+// ------------------------------------------------------------------------------------ read
+// A group's values, rounded once: code * step + low is one fused multiply-add of the type.  Pairs of codes become pairs of numbers by an OR
+// with a power of two that is taken off again (fp16: 1024 + n, bf16: 128 + n, both exact).
+template <typename T>
+__device__ __forceinline__ uint32_t value_pair(uint32_t codes, uint32_t step2, uint32_t low2) {
+  constexpr bool kHalf = std::is_same<T, __half>::value;
+  const auto n = __hsub2(as_pair<T>(codes | (kHalf ? 0x64006400u : 0x43004300u)), as_pair<T>(kHalf ? 0x64006400u : 0x43004300u));
+  return as_bits<T>(__hfma2(n, as_pair<T>(step2), as_pair<T>(low2)));
+}
+
+// Group j of a row: 32 channels, 16 pairs.
+template <typename T, int D>
+__device__ __forceinline__ void read_group(const uint8_t* codes, const void* steps, long long row, int j, bool of_v, uint32_t* out) {
+  constexpr int G = D / kCacheGroup;
+  const uint16_t* st = (const uint16_t*)steps + row * (2 * G);
+  const uint32_t step2 = st[j] * 0x10001u, low2 = st[G + j] * 0x10001u;
+  const uint32_t* w = (const uint32_t*)(codes + row * (D / 2));
+  if (!of_v) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const uint32_t x = w[G * t + j];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) out[4 * n + t] = value_pair<T>((x >> (4 * n)) & 0x000f000fu, step2, low2);
+    }
+  } else {
+    const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+#pragma unroll
+    for (int g = 0; g < 8; g += 2) {
+      const uint32_t x = __byte_perm(w[(G / 2) * g + (j >> 1)], w[(G / 2) * (g + 1) + (j >> 1)], sel);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) out[4 * n + g / 2] = value_pair<T>((x >> (4 * n)) & 0x000f000fu, step2, low2);
+    }
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) tra_cache4_read_kernel(const __grid_constant__ Cache4Rows a) {
+  constexpr int G = D / kCacheGroup, kRowsPerBlock = 256 / G;
+  const int j = threadIdx.x % G, head = blockIdx.y;
+  const long long i = (long long)blockIdx.x * kRowsPerBlock + threadIdx.x / G;
+  const bool of_v = blockIdx.z != 0;
+  const int slot = i < a.n ? a.slots[i] : -1;
+  if (slot < 0) return;
+  if (slot >= a.tokens) {
+    tra_set_status(a.status, TRA_ERR_INVALID_ARG);
+    return;
+  }
+  uint32_t v[16];
+  read_group<T, D>(of_v ? a.v_codes : a.k_codes, of_v ? a.v_step : a.k_step, (long long)head * a.tokens + slot, j, of_v, v);
+  const long long* stride = of_v ? a.v_stride : a.k_stride;
+  T* dst = (T*)(of_v ? a.v : a.k) + i * stride[0] + head * stride[1] + j * kCacheGroup;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) reinterpret_cast<uint4*>(dst)[c] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+}
+
+// ------------------------------------------------------------------------------------ many rows: the keys read back first
+// Sequence s of a pass gets the rows s * stride .. of two 16-bit tensors [rows][kv_heads][d]: the keys of its axis (tra_key_axis), as
+// their ranges say, which the attention launch behind it reads as begin / end.
+struct Cache4Expand {
+  tra_packed_launch a;
+  const uint8_t *k_codes, *v_codes;
+  const void *k_step, *v_step;
+  void *k, *v;
+  int32_t *begin, *end;
+  int stride;
+};
+
+template <typename T, int D, int kOrder>
+__global__ void __launch_bounds__(256) tra_cache4_expand_kernel(const __grid_constant__ Cache4Expand e) {
+  constexpr int G = D / kCacheGroup, kRowsPerBlock = 256 / G;
+  const tra_packed_launch& p = e.a;
+  const int j = threadIdx.x % G, head = blockIdx.y, seq = blockIdx.z >> 1;
+  const bool of_v = blockIdx.z & 1;
+  const int v0 = blockIdx.x * kRowsPerBlock + threadIdx.x / G;
+  const tra_seq_range q = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
+  const tra_seq_range k = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
+  const tra_key_axis<kOrder> axis(p, k.len - q.len, k.len);
+  const int len = q.len > 0 ? min(axis.len, e.stride) : 0;
+  if (head == 0 && blockIdx.z == 2 * seq && blockIdx.x == 0 && threadIdx.x == 0) {
+    e.begin[seq] = seq * e.stride;
+    e.end[seq] = seq * e.stride + len;
+  }
+  if (v0 >= len) return;
+  const int key = kOrder == kOrderWindow && v0 >= p.sink_rows ? v0 + axis.gap : v0;
+  uint32_t v[16];
+  read_group<T, D>(of_v ? e.v_codes : e.k_codes, of_v ? e.v_step : e.k_step, (long long)head * p.total_k + k.begin + key, j, of_v, v);
+  T* dst = (T*)(of_v ? e.v : e.k) + (((long long)seq * e.stride + v0) * p.kv_heads + head) * D + j * kCacheGroup;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) reinterpret_cast<uint4*>(dst)[c] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+}
+
+// ------------------------------------------------------------------------------------ host side
+constexpr int kMaxSplits = 256, kClusterMax = 8;
+constexpr int kRowsDirect = 64;                  // rows per key/value head up to which the codes are read by the products' kernel
+constexpr size_t kExpandBytes = 512u << 20;      // keys and values read back at a time (one sequence at least)
+
+bool bad_cache(const tra_packed_t* h, const tra_cache4_t* c) {
+  if (!h || !c || c->tokens < 0 || (c->tokens & 1)) return true;
+  if (c->tokens == 0) return false;
+  const uintptr_t all = (uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->k_step | (uintptr_t)c->v_step;
+  return !c->k || !c->v || !c->k_step || !c->v_step || (all & 15);
+}
+
+// How a call runs: `direct` (few rows) in `splits` parts of `chunk` keys, or in passes of `seqs` sequences whose keys are read back.
+struct Choice4 {
+  bool direct, clustered;
+  int splits, chunk, row_tiles;
+  int seqs, stride;
+};
+
+Choice4 choose4(const tra_packed_t* h, int n_seq, int max_q, int max_k) {
+  const int group = h->cfg.heads / h->cfg.kv_heads;
+  Choice4 c = {};
+  const long long rows = (long long)max_q * group;
+  c.direct = rows <= kRowsDirect;
+  c.splits = 1, c.chunk = 128, c.row_tiles = 1;
+  if (max_q == 0) return c;
+  if (c.direct) {
+    c.row_tiles = (int)((rows + 15) / 16);
+    int longest = tra_packed_longest_axis(h, max_k, max_q);
+    if (longest < max_k) {                       // first tokens take whole tiles here
+      const long long more = (long long)longest + 127;
+      longest = more < max_k ? (int)more : max_k;
+    }
+    // as tra_packed_attn: as many parts as fill the GPU once, two parts of long caches of many sequences
+    const int per_sm = rows <= 8 ? 3 : 2;
+    const long long units = (long long)n_seq * h->cfg.kv_heads * c.row_tiles;
+    long long parts = (long long)per_sm * h->sm_count / units;
+    const long long most = ((long long)longest + 255) / 256;
+    if (parts > most) parts = most;
+    if (parts > kClusterMax && longest <= 1024 * kClusterMax) parts = kClusterMax;
+    if (parts > kClusterMax) {
+      parts = h->sm_count / units;
+      if (parts < kClusterMax) parts = kClusterMax;
+    }
+    if (parts > kMaxSplits) parts = kMaxSplits;
+    if (parts <= 1) parts = longest >= 8192 ? 2 : 1;
+    c.chunk = (int)(((longest + parts - 1) / parts + 127) / 128 * 128);
+    if (c.chunk < 128) c.chunk = 128;
+    c.splits = longest > 0 ? (int)(((long long)longest + c.chunk - 1) / c.chunk) : 1;
+    c.clustered = c.splits > 1 && c.splits <= kClusterMax;
+  } else {
+    c.stride = (tra_packed_longest_axis(h, max_k, max_q) + 7) / 8 * 8;
+    const size_t one = (size_t)c.stride * h->cfg.kv_heads * h->cfg.head_dim * 4;
+    const size_t most = one ? kExpandBytes / one : n_seq;
+    c.seqs = (int)(most < 1 ? 1 : most > (size_t)n_seq ? n_seq : most > 16384 ? 16384 : most);
+    while ((long long)c.seqs * c.stride > (1 << 30)) --c.seqs;
+  }
+  return c;
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+size_t workspace4(const tra_packed_t* h, const Choice4& c, int n_seq, int total_q, int max_q) {
+  if (max_q == 0) return 0;
+  if (c.direct) return c.splits > 1 && !c.clustered ? sizeof(float) * (size_t)c.splits * total_q * h->cfg.heads * (h->cfg.head_dim + 2) : 0;
+  const size_t keys = round256((size_t)c.seqs * c.stride * h->cfg.kv_heads * h->cfg.head_dim * 2);
+  return 2 * keys + round256(sizeof(int32_t) * 2 * (size_t)c.seqs) + tra_packed_attn_workspace_bytes(h, c.seqs, total_q, max_q, c.stride);
+}
+
+template <typename T, int D>
+int launch_rows_io(const Cache4Rows& a, int kv_heads, bool write, cudaStream_t stream) {
+  constexpr int kRows = 256 / (D / kCacheGroup);
+  const dim3 grid((unsigned)(((long long)a.n + kRows - 1) / kRows), (unsigned)kv_heads, 2);
+  return write ? tra_launch(tra_cache4_write_kernel<T, D>, grid, 256, 0, stream, false, 1, a)
+               : tra_launch(tra_cache4_read_kernel<T, D>, grid, 256, 0, stream, false, 1, a);
+}
+
+// The stride of a dimension of one entry is never used; the others are positive multiples of 16 bytes.
+bool bad_rows(const void* ptr, const int64_t* stride, long long tokens, int heads) {
+  if (!ptr || ((uintptr_t)ptr & 15)) return true;
+  const long long n[2] = {tokens, heads};
+  for (int i = 0; i < 2; ++i)
+    if (n[i] > 1 && (stride[i] < 8 || (stride[i] & 7) || stride[i] >= (1ll << 38))) return true;
+  return false;
+}
+
+int rows_io(const tra_packed_t* h, const tra_cache4_t* c, const void* k, const void* v, const int64_t* ks, const int64_t* vs, const int32_t* slots, int n,
+            bool write, void* stream) {
+  if (bad_cache(h, c) || n < 0) return TRA_ERR_INVALID_ARG;
+  if (c->tokens > (1 << 30) || n > (1 << 30)) return TRA_ERR_UNSUPPORTED;
+  if (n == 0) return TRA_OK;
+  const int kv = h->cfg.kv_heads;
+  if (!ks || !vs || !slots || ((uintptr_t)slots & 3) || bad_rows(k, ks, n, kv) || bad_rows(v, vs, n, kv)) return TRA_ERR_INVALID_ARG;
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return TRA_ERR_CUDA;
+  if (device != h->device) return TRA_ERR_INVALID_ARG;
+  Cache4Rows a = {k, v, {ks[0], ks[1]}, {vs[0], vs[1]}, (uint8_t*)c->k, (uint8_t*)c->v, c->k_step, c->v_step, slots, n, c->tokens, h->d_status};
+  cudaStream_t s = (cudaStream_t)stream;
+  if (h->cfg.head_dim == 128)
+    return h->cfg.dtype == TRA_BF16 ? launch_rows_io<__nv_bfloat16, 128>(a, kv, write, s) : launch_rows_io<__half, 128>(a, kv, write, s);
+  return h->cfg.dtype == TRA_BF16 ? launch_rows_io<__nv_bfloat16, 64>(a, kv, write, s) : launch_rows_io<__half, 64>(a, kv, write, s);
+}
+
+template <typename T, int D>
+int launch_expand(const tra_packed_ctx& c, const Cache4Expand& e, int seqs) {
+  constexpr int kRows = 256 / (D / kCacheGroup);
+  const int blocks = e.stride > 0 ? (e.stride + kRows - 1) / kRows : 1;
+  const dim3 grid((unsigned)blocks, (unsigned)e.a.kv_heads, (unsigned)(2 * seqs));
+  return e.a.order == kOrderWindow ? tra_launch(tra_cache4_expand_kernel<T, D, kOrderWindow>, grid, 256, 0, c.stream, false, 1, e)
+                                   : tra_launch(tra_cache4_expand_kernel<T, D, kOrderCausal>, grid, 256, 0, c.stream, false, 1, e);
+}
+
+}  // namespace
+
+extern "C" int tra_cache4_write(const tra_packed_t* h, const tra_cache4_t* c, const void* k, const void* v, const int64_t* k_stride,
+                                const int64_t* v_stride, const int32_t* slots, int n, void* stream) {
+  return rows_io(h, c, k, v, k_stride, v_stride, slots, n, true, stream);
+}
+
+extern "C" int tra_cache4_read(const tra_packed_t* h, const tra_cache4_t* c, void* k, void* v, const int64_t* k_stride, const int64_t* v_stride,
+                               const int32_t* slots, int n, void* stream) {
+  return rows_io(h, c, k, v, k_stride, v_stride, slots, n, false, stream);
+}
+
+extern "C" size_t tra_packed_attn_cache4_workspace_bytes(const tra_packed_t* h, int n_seq, int total_q, int max_q, int max_k) {
+  if (!h || n_seq < 1 || total_q < 0 || max_q < 0 || max_k < 0 || max_q > total_q) return 0;
+  return workspace4(h, choose4(h, n_seq, max_q, max_k), n_seq, total_q, max_q);
+}
+
+extern "C" int tra_packed_attn_cache4(const tra_packed_t* h, const tra_packed_args_t* args, const tra_cache4_t* cache, void* workspace,
+                                      size_t workspace_bytes, void* stream_) {
+  if (!args || bad_cache(h, cache)) return TRA_ERR_INVALID_ARG;
+  tra_packed_args_t a = *args;
+  if (a.o_rest) return TRA_ERR_INVALID_ARG;                  // there is no backward call that would read it
+  a.total_k = cache->tokens;
+  tra_cache4_launch q;
+  memset(&q, 0, sizeof(q));
+  int rc = tra_packed_begin(h, &a, false, &q.a);
+  if (rc != TRA_OK) return rc;
+  const tra_packed_ctx ctx = {h, (cudaStream_t)stream_};
+  const Choice4 c = choose4(h, a.n_seq, a.max_q, a.max_k);
+  const size_t need = workspace4(h, c, a.n_seq, a.total_q, a.max_q);
+  if (need && (!workspace || ((uintptr_t)workspace & 15))) return TRA_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return TRA_ERR_CAPACITY;
+  if (c.direct) {
+    if (c.splits > 1 && !c.clustered && (long long)a.total_q * q.a.heads > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
+    q.a.o = a.o;
+    q.a.splits = c.splits;
+    q.a.sink_rows = (int)(((long long)h->cfg.sinks + 127) / 128 * 128);
+    q.k = (const uint8_t*)cache->k, q.v = (const uint8_t*)cache->v, q.k_step = cache->k_step, q.v_step = cache->v_step;
+    q.row_tiles = c.row_tiles;
+    if (need) {
+      const long long rows = (long long)c.splits * a.total_q * q.a.heads;
+      q.a.part_o = (float*)workspace;
+      q.a.part_lse2 = q.a.part_o + rows * h->cfg.head_dim;
+      q.a.part_exact = a.lse ? q.a.part_lse2 + rows : nullptr;
+    }
+    if ((long long)q.a.kv_heads * c.row_tiles > 65535) return TRA_ERR_UNSUPPORTED;
+    rc = tra_cache4_rows(ctx, q, c.chunk, c.clustered);
+    return rc != TRA_OK || !need ? rc : tra_packed_join(ctx, q.a);
+  }
+  // many rows: passes over sequences, keys read back into the workspace
+  const int kv = h->cfg.kv_heads, d = h->cfg.head_dim;
+  const size_t keys = round256((size_t)c.seqs * c.stride * kv * d * 2);
+  Cache4Expand e;
+  e.a = q.a;
+  e.k_codes = (const uint8_t*)cache->k, e.v_codes = (const uint8_t*)cache->v, e.k_step = cache->k_step, e.v_step = cache->v_step;
+  e.k = workspace, e.v = (uint8_t*)workspace + keys;
+  e.begin = (int32_t*)((uint8_t*)workspace + 2 * keys), e.end = e.begin + c.seqs;
+  e.stride = c.stride;
+  uint8_t* rest = (uint8_t*)workspace + 2 * keys + round256(sizeof(int32_t) * 2 * (size_t)c.seqs);
+  for (int s = 0; s < a.n_seq; s += c.seqs) {
+    const int n = a.n_seq - s < c.seqs ? a.n_seq - s : c.seqs;
+    e.a.cu_q = a.cu_q + s, e.a.k_begin = a.k_begin + s, e.a.k_end = a.k_end + s;
+    e.a.n_seq = n;
+    if (h->cfg.dtype == TRA_BF16)
+      rc = d == 128 ? launch_expand<__nv_bfloat16, 128>(ctx, e, n) : launch_expand<__nv_bfloat16, 64>(ctx, e, n);
+    else
+      rc = d == 128 ? launch_expand<__half, 128>(ctx, e, n) : launch_expand<__half, 64>(ctx, e, n);
+    if (rc != TRA_OK) return rc;
+    tra_packed_args_t b = a;
+    b.k = e.k, b.v = e.v;
+    b.k_stride[0] = b.v_stride[0] = (int64_t)kv * d, b.k_stride[1] = b.v_stride[1] = d;
+    b.cu_q = a.cu_q + s, b.k_begin = e.begin, b.k_end = e.end;
+    b.n_seq = n, b.total_k = c.seqs * c.stride, b.max_k = c.stride;
+    rc = tra_packed_attn(h, &b, rest, workspace_bytes - (size_t)(rest - (uint8_t*)workspace), stream_);
+    if (rc != TRA_OK) return rc;
+  }
+  return TRA_OK;
+}

@@ -3,7 +3,7 @@
 
 #include <new>
 
-#include "tra_packed.h"
+#include "tra_cache4.h"
 #include "tra_packed_ptx.cuh"
 
 namespace {
@@ -217,7 +217,7 @@ bool bad_tensor(const void* ptr, const int64_t* stride, long long tokens, int he
 }
 
 // Checks what the forward and the backward call share and fills the launch.
-int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_launch* p) {
+int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_launch* p, bool keys = true) {
   if (!h || !a || bad_sizes(h, a->n_seq, a->total_q, a->max_q, a->max_k) || a->total_k < 0 || a->max_k > a->total_k)
     return TRA_ERR_INVALID_ARG;
   if (!a->cu_q || !a->k_begin || !a->k_end || !(a->sm_scale > 0.f) || a->sm_scale > 1e30f) return TRA_ERR_INVALID_ARG;
@@ -226,7 +226,7 @@ int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_lau
   if (a->total_q > (1 << 30) || a->total_k > (1 << 30)) return TRA_ERR_UNSUPPORTED;
   const int heads = h->cfg.heads, kv = h->cfg.kv_heads;
   if (bad_tensor(a->q, a->q_stride, a->total_q, heads) || bad_tensor(a->o, a->o_stride, a->total_q, heads) ||
-      bad_tensor(a->k, a->k_stride, a->total_k, kv) || bad_tensor(a->v, a->v_stride, a->total_k, kv))
+      (keys && (bad_tensor(a->k, a->k_stride, a->total_k, kv) || bad_tensor(a->v, a->v_stride, a->total_k, kv))))
     return TRA_ERR_INVALID_ARG;
   int device = 0;
   if (cudaGetDevice(&device) != cudaSuccess) return TRA_ERR_CUDA;
@@ -280,6 +280,12 @@ int launch_join(const tra_packed* h, const tra_packed_launch& p, cudaStream_t st
 }
 
 }  // namespace
+
+int tra_packed_join(const tra_packed_ctx& c, const tra_packed_launch& p) {
+  return c.h->cfg.dtype == TRA_BF16 ? launch_join<__nv_bfloat16>(c.h, p, c.stream) : launch_join<__half>(c.h, p, c.stream);
+}
+int tra_packed_begin(const tra_packed_t* h, const tra_packed_args_t* a, bool keys, tra_packed_launch* p) { return begin_launch(h, a, p, keys); }
+int tra_packed_longest_axis(const tra_packed_t* h, int max_k, int tokens) { return longest_axis(h, max_k, tokens); }
 
 extern "C" int tra_packed_create(tra_packed_t** out, const tra_packed_config_t* cfg) {
   if (!out || !cfg) return TRA_ERR_INVALID_ARG;
@@ -367,7 +373,7 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
       rc = h->cfg.head_dim == 128 ? tra_packed_fwd_d128(ctx, p) : tra_packed_fwd_d64(ctx, p);
   }
   if (rc != TRA_OK || !join) return rc;
-  return h->cfg.dtype == TRA_BF16 ? launch_join<__nv_bfloat16>(h, p, ctx.stream) : launch_join<__half>(h, p, ctx.stream);
+  return tra_packed_join(ctx, p);
 }
 
 extern "C" size_t tra_packed_attn_backward_workspace_bytes(const tra_packed_t* h, int total_q) {

@@ -18,10 +18,10 @@
 #pragma once
 #include "tra_packed.h"
 #include "tra_packed_ptx.cuh"
+#include "tra_rows_join.cuh"
 
 namespace {
 
-constexpr int kRowsMax = 16;
 constexpr int kRowsTile = 64;             // keys per ring slot
 constexpr int kRowsWarps = 4;
 constexpr int kRowsThreads = 32 * (kRowsWarps + 1);
@@ -36,8 +36,8 @@ struct RowsCfg {
   static constexpr int kSmemBytes = kSmemData + 1024 + 256;
 };
 // the join of the warps' parts reuses the ring
-static_assert((kRowsWarps + 1) * kRowsMax * (128 + 4) * 4 <= RowsCfg<128>::kSmemData, "join area");
-static_assert((kRowsWarps + 1) * kRowsMax * (64 + 4) * 4 <= RowsCfg<64>::kSmemData, "join area");
+static_assert(rows_join_bytes<128>(kRowsWarps) <= RowsCfg<128>::kSmemData, "join area");
+static_assert(rows_join_bytes<64>(kRowsWarps) <= RowsCfg<64>::kSmemData, "join area");
 
 struct RowsCtl {
   uint64_t full[6], empty[6];
@@ -57,34 +57,6 @@ __device__ __forceinline__ void ldsm4_trans(uint32_t addr, uint32_t* r) {
                : "r"(addr)
                : "memory");
 }
-template <typename T>
-__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1);
-template <>
-__device__ __forceinline__ void mma16816<__nv_bfloat16>(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-template <>
-__device__ __forceinline__ void mma16816<__half>(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// ---- thread-block clusters: a barrier over the cluster, and 16 bytes of another block's shared memory
-__device__ __forceinline__ void cluster_sync() {
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float4 cluster_ld4(const void* own_address, uint32_t rank) {
-  uint32_t addr;
-  float4 v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_u32(own_address)), "r"(rank));
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
-}
-
 // sequence = blockIdx.x, key/value head = blockIdx.y, part = blockIdx.z (keys [part * chunk, ...) of the key axis); chunk is a multiple of 64
 template <typename T, int D, bool kWindow>
 __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const __grid_constant__ tra_packed_launch p, int chunk, int clustered) {
@@ -292,11 +264,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
     while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
     if (!clustered) return;
   }
-  float* part = (float*)smem;                                // [warp][row][D], then [warp][row][4]: m, l, le
-  float* stat = part + kRowsWarps * kRowsMax * D;
-  float* mine = stat + kRowsWarps * kRowsMax * 4;            // the block's rows: [row][D], then [row][4]
-  float* mine_stat = mine + kRowsMax * D;
-  if (warp < kRowsWarps) {
+  rows_join<T, D, kRowsWarps>(p, {qr, kvh, 0, n_rows, parts, clustered != 0}, (float*)smem, [&](float* part, float* stat) {
     const int g = lane >> 2, tig = lane & 3;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -312,74 +280,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
         st[2] = le[half];
       }
     }
-  }
-  __syncthreads();
-  // Rows of the parts `st(w)`, `row(w)` of n (warps of a block, then blocks of a cluster) on one reference.  A part has seen nothing
-  // when its sum is 0, not when its maximum is -inf: scores of NaN leave the maximum where it is, and their NaN in the sums
-  // has to reach the result (0 * NaN is NaN).
-  auto join = [](int n, auto st, auto row, float& ref, float& sl, float& se, float4& acc) {
-    float top = -INFINITY;
-    for (int w = 0; w < n; ++w) top = fmaxf(top, st(w).x);
-    ref = top > -INFINITY ? top : 0.f;
-    sl = se = 0.f;
-    acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int w = 0; w < n; ++w) {
-      const float4 t = st(w), v = row(w);
-      const float f = ex2(t.x - ref);
-      if (t.y == 0.f) continue;                              // nothing seen there
-      sl += f * t.y;
-      se += f * t.z;
-      acc.x += f * v.x;
-      acc.y += f * v.y;
-      acc.z += f * v.z;
-      acc.w += f * v.w;
-    }
-  };
-  auto finish = [&](int r, int c, float ref, float sl, float se, const float4& acc) {
-    const float inv = sl != 0.f ? 1.f / sl : 0.f;
-    const long long tok = row_token(r), row = tok * p.heads + row_head(r);
-    if (parts) {
-      *reinterpret_cast<float4*>(p.part_o + (part_base + row) * D + c) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-      if (c == 0) {
-        p.part_lse2[part_base + row] = sl != 0.f ? ref + log2f(sl) : -INFINITY;
-        if (p.part_exact) p.part_exact[part_base + row] = se != 0.f ? ref + log2f(se) : -INFINITY;
-      }
-    } else {
-      T* dst = (T*)p.o + tok * p.o_stride[0] + row_head(r) * p.o_stride[1] + c;
-      const float y[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
-      const uint2 packed = make_uint2(pack_pair<T>(y[0], y[1]), pack_pair<T>(y[2], y[3]));
-      *reinterpret_cast<uint2*>(dst) = packed;
-      if (p.o_rest)
-        *reinterpret_cast<uint2*>((T*)p.o_rest + row * D + c) = make_uint2(rest_pair<T>(y[0], y[1], packed.x), rest_pair<T>(y[2], y[3], packed.y));
-      if (c == 0 && p.lse) p.lse[row] = se != 0.f ? (ref + log2f(se)) * kLn2 : -INFINITY;
-    }
-  };
-  // four channels of a row per step
-  for (int i = tid; i < n_rows * (D / 4); i += kRowsThreads) {
-    const int r = i / (D / 4), c = (i % (D / 4)) * 4;
-    float ref, sl, se;
-    float4 acc;
-    join(kRowsWarps, [&](int w) { return *reinterpret_cast<const float4*>(stat + (w * kRowsMax + r) * 4); },
-         [&](int w) { return *reinterpret_cast<const float4*>(part + (w * kRowsMax + r) * D + c); }, ref, sl, se, acc);
-    if (clustered) {
-      *reinterpret_cast<float4*>(mine + r * D + c) = acc;
-      if (c == 0) *reinterpret_cast<float4*>(mine_stat + r * 4) = make_float4(sl != 0.f ? ref : -INFINITY, sl, se, 0.f);
-    } else {
-      finish(r, c, ref, sl, se, acc);
-    }
-  }
-  if (clustered) {
-    cluster_sync();                                          // every block's rows are there
-    for (int i = (int)blockIdx.z * kRowsThreads + tid; i < n_rows * (D / 4); i += (int)gridDim.z * kRowsThreads) {
-      const int r = i / (D / 4), c = (i % (D / 4)) * 4;
-      float ref, sl, se;
-      float4 acc;
-      join((int)gridDim.z, [&](int w) { return cluster_ld4(mine_stat + r * 4, (uint32_t)w); },
-           [&](int w) { return cluster_ld4(mine + r * D + c, (uint32_t)w); }, ref, sl, se, acc);
-      finish(r, c, ref, sl, se, acc);
-    }
-    cluster_sync();                                          // nobody leaves while its rows are read
-  }
+  });
 }
 
 template <typename T, int D, bool kWindow>
