@@ -334,27 +334,27 @@ Choice4 choose4(const tra_packed_t* h, int n_seq, int max_q, int max_k) {
   if (c.direct) {
     c.row_tiles = (int)((rows + 15) / 16);
     int longest = tra_packed_longest_axis(h, max_k, max_q);
-    if (longest < max_k) {                       // first tokens take whole tiles here
-      const long long more = (long long)longest + 127;
+    if (longest < max_k) {                       // first tokens take whole pieces here
+      const long long more = (long long)longest + 31;
       longest = more < max_k ? (int)more : max_k;
     }
-    // as tra_packed_attn: as many parts as fill the GPU once, two parts of long caches of many sequences
-    const int per_sm = rows <= 8 ? 3 : 2;
+    // Blocks that fit the GPU at once.  Few units: as many parts as fill it once, each of at least 256 keys, in a cluster where eight
+    // are enough or the cache is short (see choose in tra_packed.cu).  Many units: parts of about 3,072 keys, so that blocks of different
+    // lengths spread evenly, and no clusters, whose blocks start and end together (64 caches of up to 32K keys, eight heads: 510 us
+    // whole, 555 in two clustered parts, 405 in two, 335 in eight to eleven).
+    const long long slots = (long long)(rows <= 8 ? 3 : 2) * h->sm_count;
     const long long units = (long long)n_seq * h->cfg.kv_heads * c.row_tiles;
-    long long parts = (long long)per_sm * h->sm_count / units;
+    const bool many = 2 * units > slots;
+    long long parts = many ? (longest + 1535) / 3072 : slots / units;
     const long long most = ((long long)longest + 255) / 256;
     if (parts > most) parts = most;
-    if (parts > kClusterMax && longest <= 1024 * kClusterMax) parts = kClusterMax;
-    if (parts > kClusterMax) {
-      parts = h->sm_count / units;
-      if (parts < kClusterMax) parts = kClusterMax;
-    }
+    if (!many && parts > kClusterMax && longest <= 1024 * kClusterMax) parts = kClusterMax;
     if (parts > kMaxSplits) parts = kMaxSplits;
-    if (parts <= 1) parts = longest >= 8192 ? 2 : 1;
+    if (parts < 1) parts = 1;
     c.chunk = (int)(((longest + parts - 1) / parts + 127) / 128 * 128);
     if (c.chunk < 128) c.chunk = 128;
     c.splits = longest > 0 ? (int)(((long long)longest + c.chunk - 1) / c.chunk) : 1;
-    c.clustered = c.splits > 1 && c.splits <= kClusterMax;
+    c.clustered = !many && c.splits > 1 && c.splits <= kClusterMax;
   } else {
     c.stride = (tra_packed_longest_axis(h, max_k, max_q) + 7) / 8 * 8;
     const size_t one = (size_t)c.stride * h->cfg.kv_heads * h->cfg.head_dim * 4;
@@ -453,7 +453,7 @@ extern "C" int tra_packed_attn_cache4(const tra_packed_t* h, const tra_packed_ar
     if (c.splits > 1 && !c.clustered && (long long)a.total_q * q.a.heads > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
     q.a.o = a.o;
     q.a.splits = c.splits;
-    q.a.sink_rows = (int)(((long long)h->cfg.sinks + 127) / 128 * 128);
+    q.a.sink_rows = (int)(((long long)h->cfg.sinks + 31) / 32 * 32);
     q.k = (const uint8_t*)cache->k, q.v = (const uint8_t*)cache->v, q.k_step = cache->k_step, q.v_step = cache->v_step;
     q.row_tiles = c.row_tiles;
     if (need) {

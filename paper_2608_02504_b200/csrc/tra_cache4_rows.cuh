@@ -1,30 +1,37 @@
 // Attention of few rows over a cache of 4 bits: one new token of every sequence (or a few), the codes turned into operands of the
 // products in registers.  At most 16 rows (tokens times the heads of a group) per block; more rows take more blocks.
 //
-// Mathematics.  A key is k_c = m_j + s_j n_c for the channels c of group j, n = 0 .. 15, so
-//   q k = sum_j (s_j sum_(c in j) q_c n_c + m_j sum_(c in j) q_c):
-// the products run over the codes themselves, and steps and lowest values come in fp32 behind them (the second sum is one more product, of
-// the lowest values with the queries' group sums in two or three pieces).  Likewise o_c = sum_i (p_i s_ij) n_ic + sum_i p_i m_ij: a step is
-// multiplied into the probability.  Nothing is rounded to the type of the tensors on the way.
+// Mathematics.  A key is k_c = low_j + step_j n_c for the channels c of group j, n = 0 .. 15, so
+//   q k = sum_j (step_j sum_(c in j) q_c n_c + low_j sum_(c in j) q_c):
+// the products run over the codes themselves, and the steps come in fp32 behind them (the second sum is one more product, of the lowest
+// values with the queries' group sums in two or three pieces).  A value is mid_j + step_j (n_c - 7.5), mid = low + 7.5 step, so
+//   o_c = sum_i (p_i step_ij) n_ic - 7.5 sum_i (p_i step_ij) + sum_i p_i mid_ij:
+// the steps go to the probabilities, and the last two sums, the same for the channels of a group, are rows of one more product.
+//
+// Rounding.  p step is rounded to fp16, once, and meets n - 7.5, which is as large as what a value differs from its group's middle: that is
+// the rounding of the probabilities of any attention kernel.  (Probabilities rounded first and multiplied by the steps in fp16, against n and
+// low: 4.5e-4 off on a cache of 777 fp16 keys, where rounding the result alone makes 2.0e-4; so: 2.8e-4.)  p mid has p rounded to fp16.  Everything
+// else is exact or fp32.
 //
 // A code in the low bits of a 16-bit half is the fp16 number n 2^-24, exactly (a subnormal), and one in the next four bits is 16 times
 // that: so one mask takes two codes to two halves, and the factor 16 goes to the other operand (keys: channels of q) or to the
 // result (values: channels of o).  All products are fp16 with fp32 sums, whatever the type of the tensors: q is scaled by a power of two per
-// row that brings its largest element to 2^10, and steps and lowest values of the values by one, 2^-e, that follows the largest of them so
+// row that brings its largest element to 2^10, and steps and middles of the values by one, 2^-e, that follows the largest of them so
 // far, so that fp16's range is not an issue: elements 2^-24 times the largest lose precision, which no 16-bit tensor shows.  The probabilities are
 // held times 2^6 for the same reason.
 //
-// Bound: HBM (0.625 bytes a channel, against 2), with about 1.4 instructions per code between them.  A producer warp streams 128-key tiles
-// through a ring of bulk copies (a tile is four runs of bytes); four warps take 32 keys of every tile each.
+// Bound: HBM (0.625 bytes a channel, against 2) beside instruction issue.  A block is four warps that each walk pieces of 32 keys, every fourth
+// one, through a ring of bulk copies of their own (a piece is four runs of bytes): no warp waits for another before the join.
 #pragma once
 #include "tra_cache4.h"
 #include "tra_rows_join.cuh"
 
 namespace {
 
-constexpr int kC4Tile = 128;              // keys per ring slot
+constexpr int kC4Piece = 32;              // keys of a ring slot: one per lane
 constexpr int kC4Warps = 4;
-constexpr int kC4Threads = 32 * (kC4Warps + 1);
+constexpr int kC4Threads = 32 * kC4Warps;
+constexpr int kC4Tile = kC4Piece * kC4Warps;
 constexpr int kC4ProbLog2 = 6;            // probabilities are held times 2^6
 constexpr int kC4QLog2 = 10;              // rows of q: largest element in [2^9, 2^10)
 
@@ -32,19 +39,21 @@ template <int D>
 struct C4Cfg {
   static constexpr int kGroups = D / kCacheGroup;
   static constexpr int kRow = D / 2, kStepRow = D / 8;                    // bytes
-  static constexpr int kCodes = kC4Tile * kRow;
-  static constexpr int kSteps = (kC4Tile * kStepRow + 16 + 15) / 16 * 16;   // a tile may start in the middle of 16 bytes (d 64)
+  static constexpr int kCodes = kC4Piece * kRow;
+  static constexpr int kSteps = kC4Piece * kStepRow + 16;                 // a piece may start in the middle of 16 bytes (d 64)
   static constexpr int kStageBytes = 2 * (kCodes + kSteps);
-  static constexpr int kStages = D == 128 ? 3 : 6;
-  static constexpr int kSmemData = kStages * kStageBytes;
-  static constexpr int kScratch = kC4Warps * 2 * kGroups * 32 * 2;        // scaled steps and lowest values of a warp's 32 values
-  static constexpr int kSmemBytes = kSmemData + kScratch + 256;
+  static constexpr int kStages = D == 128 ? 3 : 4;
+  static constexpr int kRing = kStages * kStageBytes;                     // of a warp
+  // a warp's steps in fp32, [32 keys][groups] of the keys and of the values, and middles in fp16, [groups][32 keys]
+  static constexpr int kScratch = kC4Piece * kGroups * (4 + 4 + 2);
+  static constexpr int kSmemData = kC4Warps * (kRing + kScratch);
+  static constexpr int kSmemBytes = kSmemData + 256;
 };
 static_assert(rows_join_bytes<128>(kC4Warps) <= C4Cfg<128>::kSmemData, "join area");
 static_assert(rows_join_bytes<64>(kC4Warps) <= C4Cfg<64>::kSmemData, "join area");
 
 struct C4Ctl {
-  uint64_t full[6], empty[6];
+  uint64_t full[kC4Warps][4];
   int abort_flag;
 };
 static_assert(sizeof(C4Ctl) <= 256, "control block");
@@ -59,10 +68,21 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
+__device__ __forceinline__ uint32_t sub_half2(uint32_t a, uint32_t b) {
   uint32_t d;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
+}
+// Codes to operands: of the four codes in either half of x, those of bits 0 and 4 and those of bits 8 and 12 (the second of a pair times
+// 16).  The low code of the upper byte is what is left of the byte, an fp16 number itself: a subtraction on the pipe that has less to do.
+__device__ __forceinline__ void low_codes(uint32_t x, uint32_t& c0, uint32_t& c1) {
+  c0 = x & 0x000f000fu;
+  c1 = x & 0x00f000f0u;
+}
+__device__ __forceinline__ void high_codes(uint32_t x, uint32_t& c0, uint32_t& c1) {
+  const uint32_t bytes = __byte_perm(x, 0u, 0x4341);
+  c1 = bytes & 0x00f000f0u;
+  c0 = sub_half2(bytes, c1);
 }
 // 2^e, -126 <= e <= 127
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
@@ -72,17 +92,20 @@ __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t
 __device__ __forceinline__ int c4_row(int x) { return x ^ ((x >> 1) & 1); }
 
 // sequence = blockIdx.x, (row tile, key/value head) = blockIdx.y, part = blockIdx.z (keys [part * chunk, ...) of the key axis); chunk is a
-// multiple of 128.  NT: groups of eight rows.
-template <typename T, int D, int NT, bool kWindow>
-__global__ void __launch_bounds__(kC4Threads, NT == 1 ? 3 : 2)
+// multiple of 128.  NB: groups of eight rows.
+template <typename T, int D, int NB, bool kWindow>
+__global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
     tra_cache4_rows_kernel(const __grid_constant__ tra_cache4_launch args, int chunk, int clustered) {
   using C = C4Cfg<D>;
   constexpr int G = C::kGroups;
   const tra_packed_launch& p = args.a;
   extern __shared__ __align__(128) uint8_t smem[];
-  uint8_t* scratch = smem + C::kSmemData;
-  C4Ctl* ctl = (C4Ctl*)(smem + C::kSmemData + C::kScratch);
+  C4Ctl* ctl = (C4Ctl*)(smem + C::kSmemData);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint8_t* ring = smem + warp * C::kRing;
+  float* k_step = (float*)(smem + kC4Warps * C::kRing + warp * C::kScratch);
+  float* v_step = k_step + kC4Piece * G;
+  __half* v_mid = (__half*)(v_step + kC4Piece * G);
   const int seq = blockIdx.x, kvh = blockIdx.y / args.row_tiles, row0 = (blockIdx.y % args.row_tiles) * kRowsMax;
   const tra_seq_range qr = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
   const tra_seq_range kr = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
@@ -92,15 +115,14 @@ __global__ void __launch_bounds__(kC4Threads, NT == 1 ? 3 : 2)
   if (n_rows <= 0) return;
   const int ahead = kr.len - qr.len;
   const int tok0 = row0 / p.group, tok1 = (row0 + n_rows - 1) / p.group;        // tokens of this tile
-  // (sink_rows is a multiple of the tile here: a tile holds first tokens or the window's)
+  // (sink_rows is a multiple of a piece here: a piece holds first tokens or the window's)
   const tra_key_axis<kWindow ? kOrderWindow : kOrderCausal> axis(p, ahead + tok0, kr.len);
   const int walk = p.order ? min(max(tok1 + 1 + ahead - axis.gap, 0), axis.len) : kr.len;       // keys that the last token sees
   const int key0 = (int)blockIdx.z * chunk, key1 = min(key0 + chunk, walk);
-  const int n_tiles = key1 > key0 ? (key1 - key0 + kC4Tile - 1) / kC4Tile : 0;
   auto row_token = [&](int r) -> long long { return qr.begin + (row0 + r) / p.group; };
   auto row_head = [&](int r) -> int { return kvh * p.group + (row0 + r) % p.group; };
 
-  if (n_tiles == 0 && parts) {                               // nothing here: the join skips the part
+  if (key1 <= key0 && parts) {                               // nothing here: the join skips the part
     if (tid < n_rows) {
       const long long row = (long long)blockIdx.z * p.total_q * p.heads + row_token(tid) * p.heads + row_head(tid);
       p.part_lse2[row] = -INFINITY;
@@ -108,354 +130,384 @@ __global__ void __launch_bounds__(kC4Threads, NT == 1 ? 3 : 2)
     }
     return;
   }
-  if (tid == 0) {
-    for (int i = 0; i < C::kStages; ++i) {
-      mbar_init(smem_u32(&ctl->full[i]), 1);
-      mbar_init(smem_u32(&ctl->empty[i]), kC4Warps);
-    }
-    ctl->abort_flag = 0;
+  if (tid == 0) ctl->abort_flag = 0;
+  if (lane == 0) {
+    for (int i = 0; i < C::kStages; ++i) mbar_init(smem_u32(&ctl->full[warp][i]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   __syncthreads();
   volatile int* abort_flag = &ctl->abort_flag;
-  // Tile from axis position v on: its first row of the cache and how many rows are loaded.  Of the first tokens' tiles only those are (where
+  // Piece from axis position v on: its first row of the cache and how many rows are loaded.  Of the first tokens' pieces only those are (where
   // a gap follows, nobody sees the rows behind them).
-  auto tile_row = [&](int v) -> int { return kr.begin + (kWindow && v >= p.sink_rows ? v + axis.gap : v); };
-  auto tile_count = [&](int v) -> int {
-    const int n = min(kC4Tile, key1 - v);
-    return kWindow && axis.gap > 0 && v < p.sink_rows ? max(min(n, p.sinks - v), 0) : n;
+  auto piece_row = [&](int v) -> int { return kr.begin + (kWindow && v >= p.sink_rows ? v + axis.gap : v); };
+  auto piece_count = [&](int v) -> int {
+    const int n = min(kC4Piece, key1 - v);
+    return kWindow && axis.gap > 0 && v < p.sink_rows ? min(n, p.sinks - v) : n;
   };
+  const int first_piece = key0 + warp * kC4Piece;
+  const int n_pieces = key1 > first_piece ? (key1 - first_piece + kC4Tile - 1) / kC4Tile : 0;
+  // Lanes 0 .. 3 issue a copy each: codes of keys, of values, steps of keys, of values.
+  const bool of_steps = lane & 2;
+  const uint8_t* src = (lane & 1) ? (of_steps ? (const uint8_t*)args.v_step : args.v) : (of_steps ? (const uint8_t*)args.k_step : args.k);
+  src += (long long)kvh * p.total_k * (of_steps ? C::kStepRow : C::kRow);
+  const uint32_t dst = smem_u32(ring) + (of_steps ? 2 * C::kCodes + (lane & 1) * C::kSteps : (lane & 1) * C::kCodes);
+  const uint32_t row_bytes = of_steps ? C::kStepRow : C::kRow;
+  const uint32_t bars = smem_u32(&ctl->full[warp][0]);
+  auto load_piece = [&](int i, int slot) {
+    const int v = first_piece + i * kC4Tile, n = piece_count(v);
+    int row = piece_row(v), count = n;
+    uint32_t bytes = (uint32_t)n * (2 * (C::kRow + C::kStepRow));
+    if (D == 64) {                                           // rows of 8 bytes of steps, two of them per 16 (the cache holds an even number of rows)
+      const int first = row & ~1, more = ((row + n + 1) & ~1) - first;
+      bytes += (uint32_t)(more - n) * (2 * C::kStepRow);
+      if (of_steps) row = first, count = more;
+    }
+    const uint32_t bar = bars + slot * 8;
+    if (n <= 0) {
+      if (lane == 0) mbar_arrive(bar);
+    } else {
+      if (lane == 0) mbar_expect_tx(bar, bytes);
+      __syncwarp();
+      if (lane < 4) bulk_load(dst + slot * C::kStageBytes, src + (long long)row * row_bytes, count * row_bytes, bar);
+    }
+  };
+  for (int i = 0; i < C::kStages && i < n_pieces; ++i) load_piece(i, i);
 
-  float m[NT][2], l[NT][2], le[NT][2];                       // rows nt * 8 + 2 tig, + 1
-  float o[D / 16][NT][4], om[NT][4];                         // channels 16 i + g, + 8 (times 16); groups' lowest values
+  const int g = lane >> 2, tig = lane & 3;
+  float m[NB][2], l[NB][2];                                  // rows 8 nb + 2 tig, + 1
+  float o[D / 16][NB][4], om[NB][4];                         // [channels 16 i + g, + 8 (times 16)][rows 8 nb + 2 tig, + 1]; groups' share
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+  for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) m[nt][c] = -INFINITY, l[nt][c] = le[nt][c] = 0.f;
+    for (int c = 0; c < 2; ++c) m[nb][c] = -INFINITY, l[nb][c] = 0.f;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      om[nt][c] = 0.f;
+      om[nb][c] = 0.f;
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) o[i][nt][c] = 0.f;
+      for (int i = 0; i < D / 16; ++i) o[i][nb][c] = 0.f;
     }
   }
   int e_run = -120;                                          // values are held times 2^-e_run
-  const int g = lane >> 2, tig = lane & 3;
 
-  if (warp == kC4Warps) {
-    if (lane == 0) {
-      const long long head = (long long)kvh * p.total_k;
-      int slot = 0;
-      uint32_t phase = 1u;                                   // the first pass over the ring finds every slot free
-      for (int t = 0; t < n_tiles; ++t) {
-        if (!mbar_wait(smem_u32(&ctl->empty[slot]), phase, abort_flag, p.status)) break;
-        const int v = key0 + t * kC4Tile, row = tile_row(v), n = tile_count(v);
-        // d 64: rows of 8 bytes of steps, two of them per 16 (the cache holds an even number of rows)
-        const int first = D == 64 ? row & ~1 : row, last = D == 64 ? (row + n + 1) & ~1 : row + n;
-        const uint32_t codes = (uint32_t)n * C::kRow, steps = (uint32_t)(last - first) * C::kStepRow;
-        const uint32_t bar = smem_u32(&ctl->full[slot]), dst = smem_u32(smem + slot * C::kStageBytes);
-        if (n > 0) {
-          mbar_expect_tx(bar, 2 * (codes + steps));
-          bulk_load(dst, args.k + (head + row) * C::kRow, codes, bar);
-          bulk_load(dst + 2 * C::kCodes, (const uint8_t*)args.k_step + (head + first) * C::kStepRow, steps, bar);
-          bulk_load(dst + C::kCodes, args.v + (head + row) * C::kRow, codes, bar);
-          bulk_load(dst + 2 * C::kCodes + C::kSteps, (const uint8_t*)args.v_step + (head + first) * C::kStepRow, steps, bar);
-        } else {
-          mbar_arrive(bar);
-        }
-        if (++slot == C::kStages) {
-          slot = 0;
-          phase ^= 1u;
-        }
-      }
+  // ---- queries as the second operand: column g of a product is row 8 nb + g
+  constexpr int kPieces = std::is_same<T, __nv_bfloat16>::value ? 3 : 2;        // of the group sums, in T
+  uint32_t qb[D / 16][NB][2], qs[NB][2];
+  float row_mul[NB][2];                                      // to scores in base 2, codes' factor 2^24 included
+  int hi[NB][2];                                             // keys in front of it are seen by the row
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int r = nb * 8 + g;
+    const bool there = r < n_rows;
+    const T* qrow = (const T*)p.q + row_token(there ? r : 0) * p.q_stride[0] + row_head(there ? r : 0) * p.q_stride[1];
+    uint32_t raw[D / 8];
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      raw[i] = there ? *reinterpret_cast<const uint32_t*>(qrow + i * 8 + tig * 2) : 0u;
+      float a, b;
+      unpack_pair<T>(raw[i], a, b);
+      top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
     }
-  } else {
-    // ---- queries as the second operand: column g of a product is row nt * 8 + g
-    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
-    constexpr int kPieces = kBf16 ? 3 : 2;                   // of the group sums, in T
-    uint32_t qb[D / 16][NT][2], qs[NT][2];
-    float col_mul[NT][2];
-    int hi[NT][2];                                           // keys in front of it are seen by the row
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int e = min(max((int)(__float_as_uint(top) >> 23) - 126, -90), 128);        // |q| < 2^e
+    const float mul = pow2i(kC4QLog2 - e);
+    qs[nb][0] = qs[nb][1] = 0u;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int r = nt * 8 + g;
-      const bool there = r < n_rows;
-      const T* qrow = (const T*)p.q + row_token(there ? r : 0) * p.q_stride[0] + row_head(there ? r : 0) * p.q_stride[1];
-      uint32_t raw[D / 8];
-      float top = 0.f;
+    for (int j = 0; j < G; ++j) {
+      float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        raw[i] = there ? *reinterpret_cast<const uint32_t*>(qrow + i * 8 + tig * 2) : 0u;
+      for (int i = 4 * j; i < 4 * j + 4; ++i) {
         float a, b;
         unpack_pair<T>(raw[i], a, b);
-        top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
+        a *= mul, b *= mul;
+        sum += a + b;
+        const float f = i & 1 ? 0.0625f : 1.f;               // its codes are held times 16
+        qb[i >> 1][nb][i & 1] = pack_pair<__half>(a * f, b * f);
       }
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int e = min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 128);       // |q| < 2^e
-      const float mul = pow2i(kC4QLog2 - e);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      // piece x of group j is row x G + j of the operand: rows 2 tig, 2 tig + 1 in one register, 8 more in the other
+      float left = sum;
 #pragma unroll
-      for (int j = 0; j < G; ++j) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 4 * j; i < 4 * j + 4; ++i) {
-          float a, b;
-          unpack_pair<T>(raw[i], a, b);
-          a *= mul, b *= mul;
-          sum += a + b;
-          const float f = i & 1 ? 0.0625f : 1.f;             // its codes are held times 16
-          qb[i >> 1][nt][i & 1] = pack_pair<__half>(a * f, b * f);
-        }
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        // piece x of group j is row x G + j of the operand: rows 2 tig, 2 tig + 1 in register 0, 8 more in register 1
-        float left = sum;
-#pragma unroll
-        for (int x = 0; x < kPieces; ++x) {
-          const int at = x * G + j;
-          const uint32_t piece = pack_pair<T>(left, 0.f) & 0xffffu;
-          float a, b;
-          unpack_pair<T>(piece, a, b);
-          left -= a;
-          if (at == 0) qs[nt][0] = qs[nt][1] = 0u;
-          if (((at & 7) >> 1) == tig) qs[nt][at >> 3] |= piece << ((at & 1) * 16);
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        col_mul[nt][c] = p.sm_scale * kLog2e * pow2i(__shfl_sync(0xffffffffu, e, (2 * tig + c) * 4) - kC4QLog2);
-        const int t = min((row0 + nt * 8 + 2 * tig + c) / p.group, tok1);
-        hi[nt][c] = p.order ? min(max(t + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
+      for (int x = 0; x < kPieces; ++x) {
+        const int at = x * G + j;
+        const uint32_t piece = pack_pair<T>(left, 0.f) & 0xffffu;
+        float a, b;
+        unpack_pair<T>(piece, a, b);
+        left -= a;
+        if (((at & 7) >> 1) == tig) qs[nb][at >> 3] |= piece << ((at & 1) * 16);
       }
     }
-    const int hi_min = p.order ? min(max(tok0 + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
-    const int old_max = kWindow ? walk - p.window : 0;       // keys that have left the last token's window
-    uint8_t* warp_scratch = scratch + warp * (C::kScratch / kC4Warps);
-    int slot = 0;
-    uint32_t phase = 0u;
-    for (int t = 0; t < n_tiles; ++t) {
-      if (!mbar_wait_warp(smem_u32(&ctl->full[slot]), phase, abort_flag, p.status)) break;
-      const int v0 = key0 + t * kC4Tile, there = tile_count(v0), in_tile = warp * 32;
-      const int k0 = v0 + in_tile;                           // axis position of this warp's first key
-      if (in_tile < there) {
-        const uint8_t* stage = smem + slot * C::kStageBytes;
-        const int shift = D == 64 ? tile_row(v0) & 1 : 0;
-        const uint8_t *kc = stage + in_tile * C::kRow, *vc = kc + C::kCodes;
-        const uint8_t* ks = stage + 2 * C::kCodes + (in_tile + shift) * C::kStepRow;
-        const uint8_t* vs = ks + C::kSteps;
-        // ---- steps and lowest values of the values: lane = key
-        {
-          float x[2 * G];
-          uint32_t raw[G];
-          const uint8_t* at = vs + lane * C::kStepRow;
-          if constexpr (G == 4) {
-            const uint4 w = *reinterpret_cast<const uint4*>(at);
-            raw[0] = w.x, raw[1] = w.y, raw[2] = w.z, raw[3] = w.w;
-          } else {
-            const uint2 w = *reinterpret_cast<const uint2*>(at);
-            raw[0] = w.x, raw[1] = w.y;
-          }
-          float top = 0.f;
 #pragma unroll
-          for (int i = 0; i < G; ++i) {
-            if (in_tile + lane >= there) raw[i] = 0u;        // behind the sequence's end: anything
-            unpack_pair<T>(raw[i], x[2 * i], x[2 * i + 1]);
-            const float f = i < G / 2 ? 16.f : 1.f;
-            top = fmaxf(top, f * fmaxf(fabsf(x[2 * i]), fabsf(x[2 * i + 1])));
-          }
-          const int e = min((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23) - 126, 126);     // all below 2^e
-          if (e > e_run) {
-            const float f = ex2((float)(e_run - e));
-            e_run = e;
+    for (int c = 0; c < 2; ++c) {
+      row_mul[nb][c] = p.sm_scale * kLog2e * 0x1p24f * pow2i(__shfl_sync(0xffffffffu, e, (2 * tig + c) * 4) - kC4QLog2);
+      const int tok = min((row0 + nb * 8 + 2 * tig + c) / p.group, tok1);
+      hi[nb][c] = p.order ? min(max(tok + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
+    }
+  }
+  const int hi_min = p.order ? min(max(tok0 + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
+  const int old_max = kWindow ? walk - p.window : 0;         // keys that have left the last token's window
+  // -7.5 / 16 in row j of a product (rows from 8 on are nobody's)
+  uint32_t middle[G][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+  for (int j = 0; j < G; ++j)
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                om[nt][c] *= f;
+    for (int i = 0; i < 4; ++i) {
+      middle[j][i] = g == j ? 0xb780b780u : 0u;
+      asm volatile("" : "+r"(middle[j][i]));                 // kept, not made again for every product
+    }
+  auto scale_sums = [&](float f0, float f1, int nb) {
+    om[nb][0] *= f0, om[nb][1] *= f1;
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) o[i][nt][c] *= f;
-              }
-          }
-          const float mul = pow2i(-e_run);
-          const int r = lane & 7, logical = c4_row(r), half = (lane >> 3) & 1, sub = lane >> 4;
-          __half* dst = (__half*)warp_scratch + (sub * 4 + (logical >> 1)) * 4 + half * 2 + (logical & 1);
-#pragma unroll
-          for (int i = 0; i < 2 * G; ++i) dst[i * 32] = __float2half_rn(x[i] * (i < G ? 16.f * mul : mul));
-          __syncwarp();
+    for (int i = 0; i < D / 16; ++i) o[i][nb][0] *= f0, o[i][nb][1] *= f1, o[i][nb][2] *= f0, o[i][nb][3] *= f1;
+  };
+
+  int slot = 0;
+  uint32_t phase = 0u;
+#pragma unroll 1
+  for (int piece = 0; piece < n_pieces; ++piece) {
+    if (!mbar_wait_warp(smem_u32(&ctl->full[warp][slot]), phase, abort_flag, p.status)) break;
+    const int k0 = first_piece + piece * kC4Tile, there = piece_count(k0);        // axis position of the first key; keys
+    if (there > 0) {
+      const uint8_t* kc = ring + slot * C::kStageBytes;
+      const uint8_t* vc = kc + C::kCodes;
+      const uint8_t* ks = kc + 2 * C::kCodes + (D == 64 ? (piece_row(k0) & 1) * C::kStepRow : 0);
+      const uint8_t* vs = ks + C::kSteps;
+      // ---- steps and lowest values, lane = key: what the lanes need of each other's keys goes through scratch
+      {
+        uint32_t kw[G / 2], vw[G];
+        if constexpr (G == 4) {
+          const uint2 a = *reinterpret_cast<const uint2*>(ks + lane * 16);
+          const uint4 b = *reinterpret_cast<const uint4*>(vs + lane * 16);
+          kw[0] = a.x, kw[1] = a.y;
+          vw[0] = b.x, vw[1] = b.y, vw[2] = b.z, vw[3] = b.w;
+        } else {
+          const uint2 b = *reinterpret_cast<const uint2*>(vs + lane * 8);
+          kw[0] = *reinterpret_cast<const uint32_t*>(ks + lane * 8);
+          vw[0] = b.x, vw[1] = b.y;
         }
-        uint32_t pb[2][NT][2];                               // probabilities as the second operand: [16 keys][rows]
-        float s[2][NT][4];
+        float kf[G], st[G], mid[G], top = 0.f;
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-          const int r0 = sub * 16 + c4_row(g), r1 = r0 + 8;
-          // the lowest values' share
-          uint32_t am[4];
-          {
-            constexpr int kPairs = G / 2;
-            const int pair = tig % kPairs;
-            am[0] = *reinterpret_cast<const uint32_t*>(ks + r0 * C::kStepRow + G * 2 + pair * 4);
-            am[1] = *reinterpret_cast<const uint32_t*>(ks + r1 * C::kStepRow + G * 2 + pair * 4);
-            am[2] = am[0], am[3] = am[1];
+        for (int i = 0; i < G / 2; ++i) {
+          unpack_pair<T>(kw[i], kf[2 * i], kf[2 * i + 1]);
+          const bool in = lane < there;                      // behind the last key: anything
+          unpack_pair<T>(in ? vw[i] : 0u, st[2 * i], st[2 * i + 1]);
+          unpack_pair<T>(in ? vw[G / 2 + i] : 0u, mid[2 * i], mid[2 * i + 1]);
+        }
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+          st[j] *= 16.f;
+          top = fmax3(top, fabsf(mid[j]), fabsf(st[j]));
+          mid[j] = fmaf(st[j], 0.46875f, mid[j]);            // low + 7.5 step
+          st[j] = fmaxf(st[j], 0.f);                         // NaN (a group that is not finite) stays in the middle alone
+        }
+        const int e = min((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23) - 126, 126);       // all below 2^e
+        if (e > e_run) {
+          const float f = ex2((float)(e_run - e));
+          e_run = e;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) scale_sums(f, f, nb);
+        }
+        const float mul = pow2i(-e_run);
+        const int r = lane & 7, logical = c4_row(r), half = (lane >> 3) & 1, sub = lane >> 4;
+        __half* mid_at = v_mid + (sub * 4 + (logical >> 1)) * 4 + half * 2 + (logical & 1);
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+          st[j] *= mul;
+          mid_at[j * kC4Piece] = __float2half_rn(mid[j] * mul);
+        }
+        // in the order of the products' rows
+        const int at = ((lane & ~7) + logical) * G;
+        if constexpr (G == 4) {
+          *reinterpret_cast<float4*>(k_step + at) = make_float4(kf[0], kf[1], kf[2], kf[3]);
+          *reinterpret_cast<float4*>(v_step + at) = make_float4(st[0], st[1], st[2], st[3]);
+        } else {
+          *reinterpret_cast<float2*>(k_step + at) = make_float2(kf[0], kf[1]);
+          *reinterpret_cast<float2*>(v_step + at) = make_float2(st[0], st[1]);
+        }
+        __syncwarp();
+      }
+      // ---- scores: s[sub][nb][i] = key 16 sub + g + 8 (i / 2) (of the products' order), row 8 nb + 2 tig + i % 2
+      float s[2][NB][4];
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const int r0 = sub * 16 + c4_row(g), r1 = r0 + 8;
+        uint32_t w[2][G];
+        float st[2][G];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint8_t* at = kc + (half ? r1 : r0) * C::kRow + tig * (G * 4);
+          const float* step_at = k_step + (sub * 16 + half * 8 + g) * G;
+          if constexpr (G == 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(at);
+            w[half][0] = x.x, w[half][1] = x.y, w[half][2] = x.z, w[half][3] = x.w;
+            const float4 y = *reinterpret_cast<const float4*>(step_at);
+            st[half][0] = y.x, st[half][1] = y.y, st[half][2] = y.z, st[half][3] = y.w;
+          } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(at);
+            w[half][0] = x.x, w[half][1] = x.y;
+            const float2 y = *reinterpret_cast<const float2*>(step_at);
+            st[half][0] = y.x, st[half][1] = y.y;
           }
-          float st[2][G];
+        }
+        {
+          const uint8_t* at = ks + G * 2 + (tig % (G / 2)) * 4;
+          const uint32_t low0 = *reinterpret_cast<const uint32_t*>(at + r0 * C::kStepRow), low1 = *reinterpret_cast<const uint32_t*>(at + r1 * C::kStepRow);
 #pragma unroll
-          for (int half = 0; half < 2; ++half)
+          for (int nb = 0; nb < NB; ++nb) {
+            float c[4] = {0.f, 0.f, 0.f, 0.f};
+            mma1688<T>(c, low0, low1, qs[nb][0]);
+            if (kPieces * G > 8) mma1688<T>(c, low0, low1, qs[nb][1]);
 #pragma unroll
-            for (int i = 0; i < G / 2; ++i)
-              unpack_pair<T>(*reinterpret_cast<const uint32_t*>(ks + (half ? r1 : r0) * C::kStepRow + i * 4), st[half][2 * i], st[half][2 * i + 1]);
-          uint32_t w[2][G];
+            for (int i = 0; i < 4; ++i) s[sub][nb][i] = c[i] * 0x1p-24f;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+          uint32_t a0[4], a1[4];
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const uint8_t* at = kc + (half ? r1 : r0) * C::kRow + tig * (G * 4);
-            if constexpr (G == 4) {
-              const uint4 x = *reinterpret_cast<const uint4*>(at);
-              w[half][0] = x.x, w[half][1] = x.y, w[half][2] = x.z, w[half][3] = x.w;
-            } else {
-              const uint2 x = *reinterpret_cast<const uint2*>(at);
-              w[half][0] = x.x, w[half][1] = x.y;
-            }
+            low_codes(w[half][j], a0[half], a0[half + 2]);
+            high_codes(w[half][j], a1[half], a1[half + 2]);
           }
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float c[4] = {0.f, 0.f, 0.f, 0.f};
-            mma16816<T>(c, am, qs[nt][0], qs[nt][1]);
+          for (int nb = 0; nb < NB; ++nb) {
+            float c[4];
+            mma16816_first<__half>(c, a0, qb[2 * j][nb][0], qb[2 * j][nb][1]);
+            mma16816<__half>(c, a1, qb[2 * j + 1][nb][0], qb[2 * j + 1][nb][1]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[sub][nt][i] = c[i] * 0x1p-24f;
-          }
-#pragma unroll
-          for (int j = 0; j < G; ++j) {
-            const uint32_t a0[4] = {w[0][j] & 0x000f000fu, w[1][j] & 0x000f000fu, w[0][j] & 0x00f000f0u, w[1][j] & 0x00f000f0u};
-            const uint32_t h0 = w[0][j] >> 8, h1 = w[1][j] >> 8;
-            const uint32_t a1[4] = {h0 & 0x000f000fu, h1 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x00f000f0u};
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              float c[4] = {0.f, 0.f, 0.f, 0.f};
-              mma16816<__half>(c, a0, qb[2 * j][nt][0], qb[2 * j][nt][1]);
-              mma16816<__half>(c, a1, qb[2 * j + 1][nt][0], qb[2 * j + 1][nt][1]);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) s[sub][nt][i] = fmaf(st[i >> 1][j], c[i], s[sub][nt][i]);
-            }
-          }
-          // scores in base 2: the codes' factor 2^24 and the row's own
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[sub][nt][i] *= 0x1p24f * col_mul[nt][i & 1];
-          const int v = k0 + sub * 16 + c4_row(g);
-          if (k0 + 32 > min(hi_min, key1) || in_tile + 32 > there) {
-            const int end = min(key1, v0 + there);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (v + (i >> 1) * 8 >= min(hi[nt][i & 1], end)) s[sub][nt][i] = -INFINITY;
-          }
-          if (kWindow && k0 < old_max && k0 + 32 > p.sinks) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int x = v + (i >> 1) * 8;
-                if (x < hi[nt][i & 1] - p.window && x >= p.sinks) s[sub][nt][i] = -INFINITY;
-              }
+            for (int i = 0; i < 4; ++i) s[sub][nb][i] = fmaf(st[i >> 1][j], c[i], s[sub][nb][i]);
           }
         }
-        // ---- probabilities
+      }
+      if (k0 + kC4Piece > min(hi_min, key1) || there < kC4Piece) {
+        const int end = k0 + there;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (k0 + sub * 16 + (i >> 1) * 8 + c4_row(g) >= min(hi[nb][i & 1], end)) s[sub][nb][i] = -INFINITY;
+      }
+      if (kWindow && k0 < old_max && k0 + kC4Piece > p.sinks) {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int v = k0 + sub * 16 + (i >> 1) * 8 + c4_row(g);
+              if (v < hi[nb][i & 1] - p.window && v >= p.sinks) s[sub][nb][i] = -INFINITY;
+            }
+      }
+      // ---- probabilities
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float mx[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          mx[c] = fmaxf(fmaxf(s[0][nb][c], s[0][nb][c + 2]), fmaxf(s[1][nb][c], s[1][nb][c + 2]));
+          mx[c] = fmaxf(mx[c], __shfl_xor_sync(0xffffffffu, mx[c], 4));
+          mx[c] = fmaxf(mx[c], __shfl_xor_sync(0xffffffffu, mx[c], 8));
+          mx[c] = fmaxf(mx[c], __shfl_xor_sync(0xffffffffu, mx[c], 16)) * row_mul[nb][c];
+        }
+        // exact whatever the reference is, as long as all terms share it: raised only when it is 8 (2^8) behind
+        if (mx[0] > m[nb][0] + kRescaleThreshold || mx[1] > m[nb][1] + kRescaleThreshold) {
+          float alpha[2];
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float mx = fmaxf(fmaxf(s[0][nt][c], s[0][nt][c + 2]), fmaxf(s[1][nt][c], s[1][nt][c + 2]));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-            // exact whatever the reference is, as long as all terms share it: raised only when it is 8 (2^8) behind
-            if (mx > m[nt][c] + kRescaleThreshold) {
-              const float alpha = ex2(m[nt][c] - mx);
-              l[nt][c] *= alpha;
-              le[nt][c] *= alpha;
-              m[nt][c] = mx;
-#pragma unroll
-              for (int i = 0; i < D / 16; ++i) {
-                o[i][nt][c] *= alpha;
-                o[i][nt][c + 2] *= alpha;
-              }
-              om[nt][c] *= alpha;
-            }
+            const float top = fmaxf(m[nb][c], mx[c]);
+            alpha[c] = top > -INFINITY ? ex2(m[nb][c] - top) : 1.f;
+            m[nb][c] = top;
+            l[nb][c] *= alpha[c];
           }
-          const float ref[2] = {m[nt][0] > -INFINITY ? m[nt][0] - kC4ProbLog2 : 0.f, m[nt][1] > -INFINITY ? m[nt][1] - kC4ProbLog2 : 0.f};
-#pragma unroll
-          for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const float x0 = ex2(s[sub][nt][2 * half] - ref[0]), x1 = ex2(s[sub][nt][2 * half + 1] - ref[1]);
-              le[nt][0] += x0;
-              le[nt][1] += x1;
-              const uint32_t packed = pack_pair<__half>(x0, x1);
-              add_pair<__half>(l[nt][0], l[nt][1], packed);  // the sum that divides O: of the rounded probabilities
-              pb[sub][nt][half] = transpose8x8(packed);
-            }
+          scale_sums(alpha[0], alpha[1], nb);
         }
-        // ---- values
+        const float neg_ref[2] = {m[nb][0] > -INFINITY ? kC4ProbLog2 - m[nb][0] : 0.f, m[nb][1] > -INFINITY ? kC4ProbLog2 - m[nb][1] : 0.f};
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-          const int r0 = sub * 16 + c4_row(2 * tig), r1 = sub * 16 + c4_row(2 * tig + 1);
-          const uint8_t* sc = warp_scratch + (sub * 4 + tig) * 8;
-          {
-            uint2 x = make_uint2(0u, 0u);
-            if (g < G) x = *reinterpret_cast<const uint2*>(sc + (G + g) * 64);
-            const uint32_t a[4] = {x.x, 0u, x.y, 0u};
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma16816<__half>(om[nt], a, pb[sub][nt][0], pb[sub][nt][1]);
-          }
-          uint32_t w[4][G / 2];
+        for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint8_t* at = vc + ((i & 1 ? r1 : r0) + (i >> 1) * 8) * C::kRow + g * (G * 2);
-            if constexpr (G == 4) {
-              const uint2 x = *reinterpret_cast<const uint2*>(at);
-              w[i][0] = x.x, w[i][1] = x.y;
-            } else {
-              w[i][0] = *reinterpret_cast<const uint32_t*>(at);
-            }
+            s[sub][nb][i] = ex2(fmaf(s[sub][nb][i], row_mul[nb][i & 1], neg_ref[i & 1]));
+            l[nb][i & 1] += s[sub][nb][i];
           }
+      }
+      // ---- values
 #pragma unroll
-          for (int j = 0; j < G; ++j) {
-            // the four codes of group j in two neighbouring keys, side by side
-            const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-            const uint32_t x = __byte_perm(w[0][j >> 1], w[1][j >> 1], sel), y = __byte_perm(w[2][j >> 1], w[3][j >> 1], sel);
-            const uint32_t xh = x >> 8, yh = y >> 8;
-            const uint32_t a0[4] = {x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u};
-            const uint32_t a1[4] = {xh & 0x000f000fu, xh & 0x00f000f0u, yh & 0x000f000fu, yh & 0x00f000f0u};
-            const uint2 step = *reinterpret_cast<const uint2*>(sc + j * 64);
+      for (int sub = 0; sub < 2; ++sub) {
+        uint32_t w[4][G / 2];                                // keys 2 tig, + 1, 2 tig + 8, + 9
+        const int r0 = sub * 16 + c4_row(2 * tig), r1 = sub * 16 + c4_row(2 * tig + 1);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              const uint32_t b0 = mul_half2(pb[sub][nt][0], step.x), b1 = mul_half2(pb[sub][nt][1], step.y);
-              mma16816<__half>(o[2 * j][nt], a0, b0, b1);
-              mma16816<__half>(o[2 * j + 1][nt], a1, b0, b1);
-            }
+        for (int i = 0; i < 4; ++i) {
+          const uint8_t* at = vc + ((i & 1 ? r1 : r0) + (i >> 1) * 8) * C::kRow + g * (G * 2);
+          if constexpr (G == 4) {
+            const uint2 x = *reinterpret_cast<const uint2*>(at);
+            w[i][0] = x.x, w[i][1] = x.y;
+          } else {
+            w[i][0] = *reinterpret_cast<const uint32_t*>(at);
           }
         }
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ctl->empty[slot]));
-      if (++slot == C::kStages) {
-        slot = 0;
-        phase ^= 1u;
+        float st[2][G];                                      // keys g, g + 8
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const float* at = v_step + (sub * 16 + half * 8 + g) * G;
+          if constexpr (G == 4) {
+            const float4 y = *reinterpret_cast<const float4*>(at);
+            st[half][0] = y.x, st[half][1] = y.y, st[half][2] = y.z, st[half][3] = y.w;
+          } else {
+            const float2 y = *reinterpret_cast<const float2*>(at);
+            st[half][0] = y.x, st[half][1] = y.y;
+          }
+        }
+        {
+          // (rows from 8 on are nobody's: any group's middles do, and so they do for the rows behind the last group)
+          const uint2 v = *reinterpret_cast<const uint2*>(v_mid + (g % G) * kC4Piece + (sub * 4 + tig) * 4);
+          const uint32_t a[4] = {v.x, v.x, v.y, v.y};
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            const float* x = s[sub][nb];
+            mma16816<__half>(om[nb], a, transpose8x8(pack_pair<__half>(x[0], x[1])), transpose8x8(pack_pair<__half>(x[2], x[3])));
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+          // the four codes of group j in two neighbouring keys, side by side
+          const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+          const uint32_t x = __byte_perm(w[0][j >> 1], w[1][j >> 1], sel), y = __byte_perm(w[2][j >> 1], w[3][j >> 1], sel);
+          uint32_t a0[4], a1[4];
+          low_codes(x, a0[0], a0[1]);
+          low_codes(y, a0[2], a0[3]);
+          high_codes(x, a1[0], a1[1]);
+          high_codes(y, a1[2], a1[3]);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            const float* q = s[sub][nb];
+            const uint32_t b0 = transpose8x8(pack_pair<__half>(q[0] * st[0][j], q[1] * st[0][j]));
+            const uint32_t b1 = transpose8x8(pack_pair<__half>(q[2] * st[1][j], q[3] * st[1][j]));
+            mma16816<__half>(o[2 * j][nb], a0, b0, b1);
+            mma16816<__half>(o[2 * j + 1][nb], a1, b0, b1);
+            mma16816<__half>(om[nb], middle[j], b0, b1);
+          }
+        }
       }
     }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int i = 4; i < 32; i <<= 1) {
-          l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], i);
-          le[nt][c] += __shfl_xor_sync(0xffffffffu, le[nt][c], i);
-        }
+    __syncwarp();
+    if (piece + C::kStages < n_pieces) load_piece(piece + C::kStages, slot);
+    if (++slot == C::kStages) {
+      slot = 0;
+      phase ^= 1u;
+    }
   }
-  __syncthreads();                                           // every tile has been read: the ring becomes the join area
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 4; i < 32; i <<= 1) l[nb][c] += __shfl_xor_sync(0xffffffffu, l[nb][c], i);
+  __syncthreads();                                           // every piece has been read: the rings become the join area
   const bool gave_up = ctl->abort_flag != 0;
   if (gave_up) {
     // a wait ran out: copies in flight land before the block ends; nothing is written (and nothing added to a cluster's rows)
@@ -463,36 +515,36 @@ __global__ void __launch_bounds__(kC4Threads, NT == 1 ? 3 : 2)
     while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
     if (!clustered) return;
   }
-  rows_join<T, D, kC4Warps>(p, {qr, kvh, row0, n_rows, parts, clustered != 0}, (float*)smem, [&](float* part, float* stat) {
+  rows_join<T, D, kC4Warps, kC4Threads, 8 * NB>(p, {qr, kvh, row0, n_rows, parts, clustered != 0}, (float*)smem, [&](float* part, float* stat) {
     const float f = pow2i(e_run);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const int r = nt * 8 + 2 * tig + c;
-        float* dst = part + (warp * kRowsMax + r) * D;
+        const int r = warp * 8 * NB + nb * 8 + 2 * tig + c;
+        float* dst = part + r * D;
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-          const float low = __shfl_sync(0xffffffffu, om[nt][c], j * 4 + tig) * f;      // of group j
+          const float low = __shfl_sync(0xffffffffu, om[nb][c], j * 4 + tig) * f;        // row j
 #pragma unroll
           for (int i = 2 * j; i < 2 * j + 2; ++i) {
-            dst[i * 16 + g] = fmaf(o[i][nt][c] * 0x1p20f, f, low);      // codes 2^24, steps 2^-4
-            dst[i * 16 + g + 8] = fmaf(o[i][nt][c + 2] * 0x1p16f, f, low);
+            dst[i * 16 + g] = fmaf(o[i][nb][c] * 0x1p20f, f, low);        // codes 2^24, steps 2^-4
+            dst[i * 16 + g + 8] = fmaf(o[i][nb][c + 2] * 0x1p16f, f, low);
           }
         }
         if (g == 0) {
-          float* st = stat + (warp * kRowsMax + r) * 4;
-          st[0] = m[nt][c] - kC4ProbLog2;
-          st[1] = gave_up ? 0.f : l[nt][c];
-          st[2] = le[nt][c];
+          float* st = stat + r * 4;
+          st[0] = m[nb][c] - kC4ProbLog2;
+          st[1] = gave_up ? 0.f : l[nb][c];
+          st[2] = l[nb][c];
         }
       }
   });
 }
 
-template <typename T, int D, int NT, bool kWindow>
+template <typename T, int D, int NB, bool kWindow>
 int launch_cache4_kernel(const tra_packed_ctx& c, const tra_cache4_launch& a, int chunk, bool clustered) {
-  constexpr auto kern = tra_cache4_rows_kernel<T, D, NT, kWindow>;
+  constexpr auto kern = tra_cache4_rows_kernel<T, D, NB, kWindow>;
   const int rc = tra_allow_smem<kern>(C4Cfg<D>::kSmemBytes);
   if (rc != TRA_OK) return rc;
   return tra_launch(kern, dim3((unsigned)a.a.n_seq, (unsigned)(a.a.kv_heads * a.row_tiles), (unsigned)a.a.splits), kC4Threads, C4Cfg<D>::kSmemBytes,

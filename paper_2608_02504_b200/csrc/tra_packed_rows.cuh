@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) tra_packed_rows_kernel(const 
     while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
     if (!clustered) return;
   }
-  rows_join<T, D, kRowsWarps>(p, {qr, kvh, 0, n_rows, parts, clustered != 0}, (float*)smem, [&](float* part, float* stat) {
+  rows_join<T, D, kRowsWarps, kRowsThreads, kRowsMax>(p, {qr, kvh, 0, n_rows, parts, clustered != 0}, (float*)smem, [&](float* part, float* stat) {
     const int g = lane >> 2, tig = lane & 3;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {

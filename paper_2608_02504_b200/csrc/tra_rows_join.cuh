@@ -6,7 +6,7 @@
 
 namespace {
 
-constexpr int kRowsMax = 16;              // rows of a block
+constexpr int kRowsMax = 16;              // rows of a block at most
 
 template <typename T>
 __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1);
@@ -21,6 +21,38 @@ __device__ __forceinline__ void mma16816<__half>(float* c, const uint32_t* a, ui
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// the same onto zeros (written so, the zeros take no registers)
+template <typename T>
+__device__ __forceinline__ void mma16816_first(float* d, const uint32_t* a, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16816_first<__nv_bfloat16>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+template <>
+__device__ __forceinline__ void mma16816_first<__half>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+// 16 x 8 x 8: the first operand's rows g, g + 8 in two registers
+template <typename T>
+__device__ __forceinline__ void mma1688(float* c, uint32_t a0, uint32_t a1, uint32_t b);
+template <>
+__device__ __forceinline__ void mma1688<__nv_bfloat16>(float* c, uint32_t a0, uint32_t a1, uint32_t b) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(b));
+}
+template <>
+__device__ __forceinline__ void mma1688<__half>(float* c, uint32_t a0, uint32_t a1, uint32_t b) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(b));
 }
 
 // ---- thread-block clusters: a barrier over the cluster, and 16 bytes of another block's shared memory
@@ -44,20 +76,19 @@ struct rows_place {
 };
 
 template <int D>
-constexpr int rows_join_bytes(int warps) { return (warps + 1) * kRowsMax * (D + 4) * 4; }
+constexpr int rows_join_bytes(int warps, int rows = kRowsMax) { return (warps + 1) * rows * (D + 4) * 4; }
 
-// store(part, stat): every warp's sums to part [warp][row][D] and its maximum, the sum that divides O and the unrounded sum to stat
-// [warp][row][4].  All threads call it.
-template <typename T, int D, int kWarps, typename Store>
+// store(part, stat): the sums of every of kWarps warps to part [warp][row][D] and its maximum, the sum that divides O and the unrounded
+// sum to stat [warp][row][4], kRows rows each.  All kThreads threads call it.
+template <typename T, int D, int kWarps, int kThreads, int kRows, typename Store>
 __device__ __forceinline__ void rows_join(const tra_packed_launch& p, const rows_place& at, float* part, Store store) {
-  constexpr int kThreads = 32 * (kWarps + 1);
   const int tid = threadIdx.x, n_rows = at.n_rows;
   const long long part_base = (long long)blockIdx.z * p.total_q * p.heads;
   auto row_token = [&](int r) -> long long { return at.q.begin + (at.row0 + r) / p.group; };
   auto row_head = [&](int r) -> int { return at.kvh * p.group + (at.row0 + r) % p.group; };
-  float* stat = part + kWarps * kRowsMax * D;
-  float* mine = stat + kWarps * kRowsMax * 4;                // the block's rows: [row][D], then [row][4]
-  float* mine_stat = mine + kRowsMax * D;
+  float* stat = part + kWarps * kRows * D;
+  float* mine = stat + kWarps * kRows * 4;                // the block's rows: [row][D], then [row][4]
+  float* mine_stat = mine + kRows * D;
   if (tid < 32 * kWarps) store(part, stat);
   __syncthreads();
   // Rows of the parts `st(w)`, `row(w)` of n (warps of a block, then blocks of a cluster) on one reference.  A part has seen nothing
@@ -105,8 +136,8 @@ __device__ __forceinline__ void rows_join(const tra_packed_launch& p, const rows
     const int r = i / (D / 4), c = (i % (D / 4)) * 4;
     float ref, sl, se;
     float4 acc;
-    join(kWarps, [&](int w) { return *reinterpret_cast<const float4*>(stat + (w * kRowsMax + r) * 4); },
-         [&](int w) { return *reinterpret_cast<const float4*>(part + (w * kRowsMax + r) * D + c); }, ref, sl, se, acc);
+    join(kWarps, [&](int w) { return *reinterpret_cast<const float4*>(stat + (w * kRows + r) * 4); },
+         [&](int w) { return *reinterpret_cast<const float4*>(part + (w * kRows + r) * D + c); }, ref, sl, se, acc);
     if (at.clustered) {
       *reinterpret_cast<float4*>(mine + r * D + c) = acc;
       if (c == 0) *reinterpret_cast<float4*>(mine_stat + r * 4) = make_float4(sl != 0.f ? ref : -INFINITY, sl, se, 0.f);
