@@ -270,8 +270,11 @@ __global__ void __launch_bounds__(256) tra_cache4_read_kernel(const __grid_const
 }
 
 // ------------------------------------------------------------------------------------ many rows: the keys read back first
-// Sequence s of a pass gets the rows s * stride .. of two 16-bit tensors [rows][kv_heads][d]: the keys of its axis (tra_key_axis), as
-// their ranges say, which the attention launch behind it reads as begin / end.
+// Sequence s of a pass gets the rows s * stride .. of two 16-bit tensors [rows][2][kv_heads][d]: the keys of its axis (tra_key_axis), as
+// their ranges say, which the attention launch behind it reads as begin / end.  An element low + step n has up to 4 bits more than the type,
+// and more where low and step are of different sizes; rounded to the type alone, keys and values would each add as much error as
+// the rounding of the result (bf16, 97 queries over 65,500 keys: 3.8e-3 off, against 1.7e-3 for the result's rounding; with the pieces 2.4e-3).  So what
+// rounding took is kept as a second piece.
 struct Cache4Expand {
   tra_packed_launch a;
   const uint8_t *k_codes, *v_codes;
@@ -280,6 +283,46 @@ struct Cache4Expand {
   int32_t *begin, *end;
   int stride;
 };
+
+// A group's values in two pieces.
+template <typename T, int D>
+__device__ __forceinline__ void read_group_pieces(const uint8_t* codes, const void* steps, long long row, int j, bool of_v, uint32_t* out, uint32_t* rest) {
+  constexpr int G = D / kCacheGroup;
+  const uint16_t* st = (const uint16_t*)steps + row * (2 * G);
+  float step, low, unused;
+  unpack_pair<T>(st[j], step, unused);
+  unpack_pair<T>(st[G + j], low, unused);
+  const uint32_t* w = (const uint32_t*)(codes + row * (D / 2));
+  // codes n and n + 4 of x (keys: of a word; values: of halves of two words)
+  auto two = [&](uint32_t x, int n, int at) {
+    // 2^23 + code is a float; that power of two is taken off again, exactly
+    const float a = __uint_as_float(0x4b000000u | ((x >> (4 * n)) & 15u)) - 8388608.f, b = __uint_as_float(0x4b000000u | ((x >> (4 * n + 16)) & 15u)) - 8388608.f;
+    const float y = fmaf(a, step, low), z = fmaf(b, step, low);
+    out[at] = pack_pair<T>(y, z);
+    if (std::is_same<T, __half>::value) {                    // (low + 15 step may pass the type's range by a step's rounding)
+      float p, q;
+      unpack_pair<T>(out[at], p, q);
+      if (fabsf(p) == INFINITY || fabsf(q) == INFINITY) out[at] = pack_pair<T>(fminf(fmaxf(y, -65504.f), 65504.f), fminf(fmaxf(z, -65504.f), 65504.f));
+    }
+    rest[at] = rest_pair<T>(y, z, out[at]);
+  };
+  if (!of_v) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const uint32_t x = w[G * t + j];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) two(x, n, 4 * n + t);
+    }
+  } else {
+    const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+#pragma unroll
+    for (int g = 0; g < 8; g += 2) {
+      const uint32_t x = __byte_perm(w[(G / 2) * g + (j >> 1)], w[(G / 2) * (g + 1) + (j >> 1)], sel);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) two(x, n, 4 * n + g / 2);
+    }
+  }
+}
 
 template <typename T, int D, int kOrder>
 __global__ void __launch_bounds__(256) tra_cache4_expand_kernel(const __grid_constant__ Cache4Expand e) {
@@ -298,11 +341,15 @@ __global__ void __launch_bounds__(256) tra_cache4_expand_kernel(const __grid_con
   }
   if (v0 >= len) return;
   const int key = kOrder == kOrderWindow && v0 >= p.sink_rows ? v0 + axis.gap : v0;
-  uint32_t v[16];
-  read_group<T, D>(of_v ? e.v_codes : e.k_codes, of_v ? e.v_step : e.k_step, (long long)head * p.total_k + k.begin + key, j, of_v, v);
-  T* dst = (T*)(of_v ? e.v : e.k) + (((long long)seq * e.stride + v0) * p.kv_heads + head) * D + j * kCacheGroup;
+  uint32_t v[16], rest[16];
+  read_group_pieces<T, D>(of_v ? e.v_codes : e.k_codes, of_v ? e.v_step : e.k_step, (long long)head * p.total_k + k.begin + key, j, of_v, v, rest);
+  T* dst = (T*)(of_v ? e.v : e.k) + (((long long)seq * e.stride + v0) * 2 * p.kv_heads + head) * D + j * kCacheGroup;
+  T* dst_rest = dst + (long long)p.kv_heads * D;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) reinterpret_cast<uint4*>(dst)[c] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+  for (int c = 0; c < 4; ++c) {
+    reinterpret_cast<uint4*>(dst)[c] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+    reinterpret_cast<uint4*>(dst_rest)[c] = make_uint4(rest[4 * c], rest[4 * c + 1], rest[4 * c + 2], rest[4 * c + 3]);
+  }
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -357,7 +404,7 @@ Choice4 choose4(const tra_packed_t* h, int n_seq, int max_q, int max_k) {
     c.clustered = !many && c.splits > 1 && c.splits <= kClusterMax;
   } else {
     c.stride = (tra_packed_longest_axis(h, max_k, max_q) + 7) / 8 * 8;
-    const size_t one = (size_t)c.stride * h->cfg.kv_heads * h->cfg.head_dim * 4;
+    const size_t one = (size_t)c.stride * h->cfg.kv_heads * h->cfg.head_dim * 8;
     const size_t most = one ? kExpandBytes / one : n_seq;
     c.seqs = (int)(most < 1 ? 1 : most > (size_t)n_seq ? n_seq : most > 16384 ? 16384 : most);
     while ((long long)c.seqs * c.stride > (1 << 30)) --c.seqs;
@@ -370,7 +417,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 size_t workspace4(const tra_packed_t* h, const Choice4& c, int n_seq, int total_q, int max_q) {
   if (max_q == 0) return 0;
   if (c.direct) return c.splits > 1 && !c.clustered ? sizeof(float) * (size_t)c.splits * total_q * h->cfg.heads * (h->cfg.head_dim + 2) : 0;
-  const size_t keys = round256((size_t)c.seqs * c.stride * h->cfg.kv_heads * h->cfg.head_dim * 2);
+  const size_t keys = round256((size_t)c.seqs * c.stride * h->cfg.kv_heads * h->cfg.head_dim * 4);
   return 2 * keys + round256(sizeof(int32_t) * 2 * (size_t)c.seqs) + tra_packed_attn_workspace_bytes(h, c.seqs, total_q, max_q, c.stride);
 }
 
@@ -468,7 +515,7 @@ extern "C" int tra_packed_attn_cache4(const tra_packed_t* h, const tra_packed_ar
   }
   // many rows: passes over sequences, keys read back into the workspace
   const int kv = h->cfg.kv_heads, d = h->cfg.head_dim;
-  const size_t keys = round256((size_t)c.seqs * c.stride * kv * d * 2);
+  const size_t keys = round256((size_t)c.seqs * c.stride * kv * d * 4);
   Cache4Expand e;
   e.a = q.a;
   e.k_codes = (const uint8_t*)cache->k, e.v_codes = (const uint8_t*)cache->v, e.k_step = cache->k_step, e.v_step = cache->v_step;
@@ -487,10 +534,10 @@ extern "C" int tra_packed_attn_cache4(const tra_packed_t* h, const tra_packed_ar
     if (rc != TRA_OK) return rc;
     tra_packed_args_t b = a;
     b.k = e.k, b.v = e.v;
-    b.k_stride[0] = b.v_stride[0] = (int64_t)kv * d, b.k_stride[1] = b.v_stride[1] = d;
+    b.k_stride[0] = b.v_stride[0] = (int64_t)2 * kv * d, b.k_stride[1] = b.v_stride[1] = d;
     b.cu_q = a.cu_q + s, b.k_begin = e.begin, b.k_end = e.end;
     b.n_seq = n, b.total_k = c.seqs * c.stride, b.max_k = c.stride;
-    rc = tra_packed_attn(h, &b, rest, workspace_bytes - (size_t)(rest - (uint8_t*)workspace), stream_);
+    rc = tra_packed_attn_pieces(h, &b, rest, workspace_bytes - (size_t)(rest - (uint8_t*)workspace), stream_);
     if (rc != TRA_OK) return rc;
   }
   return TRA_OK;

@@ -25,5 +25,7 @@ int tra_cache4_rows(const tra_packed_ctx& c, const tra_cache4_launch& a, int chu
 int tra_packed_join(const tra_packed_ctx& c, const tra_packed_launch& p);
 // Checks what every attention call shares and fills the launch; a->k and a->v are looked at when `keys`.
 int tra_packed_begin(const tra_packed_t* h, const tra_packed_args_t* a, bool keys, tra_packed_launch* p);
+// tra_packed_attn over K and V of twice the heads: rounded elements, then what rounding took from them.  At more than 16 rows per key/value head.
+int tra_packed_attn_pieces(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes, void* stream);
 // Keys that `tokens` queries walk at most.
 int tra_packed_longest_axis(const tra_packed_t* h, int max_k, int tokens);

@@ -255,16 +255,17 @@ int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_lau
 
 // The maps of K and V, in boxes of `rows` keys and, for the tile where the first tokens end, of its two parts.
 int make_key_maps(tra_packed_launch* p, const tra_packed* h, const void* k, const int64_t* ks, const void* v, const int64_t* vs, long long tokens,
-                  int rows) {
+                  int rows, int pieces = 1) {
   int rc;
-  if ((rc = make_packed_map(&p->map_k, h, k, ks, p->kv_heads, tokens, 1, rows)) != TRA_OK) return rc;
-  if ((rc = make_packed_map(&p->map_v, h, v, vs, p->kv_heads, tokens, 1, rows)) != TRA_OK) return rc;
+  const int heads = p->kv_heads * pieces;
+  if ((rc = make_packed_map(&p->map_k, h, k, ks, heads, tokens, 1, rows)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p->map_v, h, v, vs, heads, tokens, 1, rows)) != TRA_OK) return rc;
   const int first = p->order == kOrderWindow ? p->sink_rows % rows : 0;
   if (first == 0) return TRA_OK;
-  if ((rc = make_packed_map(&p->map_k_first, h, k, ks, p->kv_heads, tokens, 1, first)) != TRA_OK) return rc;
-  if ((rc = make_packed_map(&p->map_v_first, h, v, vs, p->kv_heads, tokens, 1, first)) != TRA_OK) return rc;
-  if ((rc = make_packed_map(&p->map_k_rest, h, k, ks, p->kv_heads, tokens, 1, rows - first)) != TRA_OK) return rc;
-  return make_packed_map(&p->map_v_rest, h, v, vs, p->kv_heads, tokens, 1, rows - first);
+  if ((rc = make_packed_map(&p->map_k_first, h, k, ks, heads, tokens, 1, first)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p->map_v_first, h, v, vs, heads, tokens, 1, first)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p->map_k_rest, h, k, ks, heads, tokens, 1, rows - first)) != TRA_OK) return rc;
+  return make_packed_map(&p->map_v_rest, h, v, vs, heads, tokens, 1, rows - first);
 }
 
 template <typename T, int D>
@@ -336,8 +337,7 @@ extern "C" size_t tra_packed_attn_workspace_bytes(const tra_packed_t* h, int n_s
   return workspace_of(h, choose(h, n_seq, total_q, max_q, max_k), total_q);
 }
 
-extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes,
-                               void* stream_) {
+static int attend(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes, void* stream_, int pieces) {
   tra_packed_launch p;
   int rc = begin_launch(h, a, &p);
   if (rc != TRA_OK) return rc;
@@ -361,13 +361,16 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
   const void *kk = a->total_k > 0 ? a->k : a->q, *vv = a->total_k > 0 ? a->v : a->q;
   const int64_t *ks = a->total_k > 0 ? a->k_stride : a->q_stride, *vs = a->total_k > 0 ? a->v_stride : a->q_stride;
   const long long tk = a->total_k > 0 ? a->total_k : a->total_q;
-  if ((rc = make_key_maps(&p, h, kk, ks, vv, vs, tk, key_box)) != TRA_OK) return rc;
+  if ((rc = make_key_maps(&p, h, kk, ks, vv, vs, tk, key_box, pieces)) != TRA_OK) return rc;
   if (c.rows) {
     rc = tra_packed_rows(ctx, p, c.chunk, c.clustered);
   } else {
     if ((rc = make_packed_map(&p.map_q, h, a->q, a->q_stride, p.heads, a->total_q, p.group, p.tile_tokens)) != TRA_OK) return rc;
     p.n_units = (a->max_q <= 2 * p.tile_tokens ? 0 : a->total_q / (2 * p.tile_tokens)) + a->n_seq;
-    if (p.order == kOrderWindow)
+    if (pieces == 2) {
+      if (p.order != kOrderWindow) p.window = 1 << 30, p.sinks = p.sink_rows = 0;
+      rc = h->cfg.head_dim == 128 ? tra_packed_fwd_pieces_d128(ctx, p) : tra_packed_fwd_pieces_d64(ctx, p);
+    } else if (p.order == kOrderWindow)
       rc = h->cfg.head_dim == 128 ? tra_packed_fwd_window_d128(ctx, p) : tra_packed_fwd_window_d64(ctx, p);
     else
       rc = h->cfg.head_dim == 128 ? tra_packed_fwd_d128(ctx, p) : tra_packed_fwd_d64(ctx, p);
@@ -376,10 +379,60 @@ extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a
   return tra_packed_join(ctx, p);
 }
 
+extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes, void* stream) {
+  return attend(h, a, workspace, workspace_bytes, stream, 1);
+}
+int tra_packed_attn_pieces(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes, void* stream) {
+  return attend(h, a, workspace, workspace_bytes, stream, 2);
+}
+
+namespace {
+
+// Streamed tiles of 64 rows let two blocks share an SM where head_dim leaves the room; not where they would hold less than
+// nine tenths of the rows of 128 (groups of 22 heads and more that do not divide 64).
+int backward_stream_rows(const tra_packed* h) {
+  const int group = h->cfg.heads / h->cfg.kv_heads;
+  return h->cfg.head_dim == 64 && 20 * (64 / group) >= 9 * (kTileM / group) ? 64 : 128;
+}
+
+// Units of the first keys' gradients (tra_find_sink_unit): as many streamed tiles as another key tile walks, 16 at least, or a 32nd of all
+// queries, or more where the sums would take over a quarter of a gigabyte.  slots = 0: not cut.
+struct SinkPlan {
+  int steps;
+  long long slots;
+};
+SinkPlan sink_plan(const tra_packed* h, int total_q) {
+  SinkPlan s = {0, 0};
+  if (h->cfg.window == 0 || h->cfg.sinks == 0) return s;
+  const long long tokens = backward_stream_rows(h) / (h->cfg.heads / h->cfg.kv_heads);
+  long long steps = ((long long)h->cfg.window + kTileM) / tokens;
+  if (steps > 64) steps = 64;
+  if (steps < 16) steps = 16;
+  if (steps < total_q / (32 * tokens)) steps = total_q / (32 * tokens);
+  // not where one block that walks all queries is done before the others: these walk a window each, and the dQ blocks about as much
+  const long long tiles = (total_q + kTileM - 1) / kTileM, sink_tiles = ((long long)h->cfg.sinks + kTileM - 1) / kTileM, walk = total_q / tokens;
+  const long long blocks = h->cfg.head_dim == 64 ? 2 : 1;
+  if (10 * walk * blocks * h->sm_count < 6 * h->cfg.kv_heads * (2 * tiles * (h->cfg.window + kTileM) / tokens + sink_tiles * walk)) return s;
+  for (; steps * tokens < total_q; steps *= 2) {
+    const long long slots = 2 * (total_q / (steps * tokens)) + 2;
+    if (slots * h->cfg.kv_heads * h->cfg.sinks > (256ll << 20) / (8 * h->cfg.head_dim)) continue;
+    s.steps = (int)steps, s.slots = slots;
+    break;
+  }
+  return s;
+}
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+// delta, and (fp16) the largest norms behind it
+size_t delta_bytes(const tra_packed* h, int total_q) {
+  return sizeof(float) * ((size_t)total_q * h->cfg.heads + (h->cfg.dtype == TRA_FP16 ? 2 * (size_t)h->cfg.kv_heads : 0));
+}
+
+}  // namespace
+
 extern "C" size_t tra_packed_attn_backward_workspace_bytes(const tra_packed_t* h, int total_q) {
   if (!h || total_q <= 0) return 0;
-  // delta, and (fp16) the largest norms behind it
-  return sizeof(float) * ((size_t)total_q * h->cfg.heads + (h->cfg.dtype == TRA_FP16 ? 2 * (size_t)h->cfg.kv_heads : 0));
+  const size_t n = delta_bytes(h, total_q), slots = (size_t)sink_plan(h, total_q).slots;
+  return slots == 0 ? n : round16(n) + sizeof(float) * slots * h->cfg.kv_heads * (size_t)h->cfg.sinks * 2 * h->cfg.head_dim;
 }
 
 extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_args_t* a, const tra_packed_grads_t* g,
@@ -409,11 +462,13 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
     p.dk_stride[i] = g->dk_stride[i];
     p.dv_stride[i] = g->dv_stride[i];
   }
-  // Streamed tiles of 64 rows let two blocks share an SM where head_dim leaves the room; not where they would hold less than
-  // nine tenths of the rows of 128 (groups of 22 heads and more that do not divide 64).
-  const int half = 64 / p.group;
-  p.stream_rows = h->cfg.head_dim == 64 && 20 * half >= 9 * p.tile_tokens ? 64 : 128;
+  p.stream_rows = backward_stream_rows(h);
   p.stream_tokens = p.stream_rows / p.group;
+  const SinkPlan sinks = sink_plan(h, a->total_q);
+  if (p.order == kOrderWindow && sinks.slots > 0) {
+    p.sink_steps = sinks.steps, p.sink_slots = (int)sinks.slots;
+    p.sink_part = (float*)((uint8_t*)workspace + round16(delta_bytes(h, a->total_q)));
+  }
   // a side without tokens is never loaded; its maps then describe the other side
   const bool q = a->total_q > 0, k = a->total_k > 0;
   const void *qq = q ? a->q : a->k, *oo = q ? g->d_o : a->k, *kk = k ? a->k : a->q, *vv = k ? a->v : a->q;

@@ -37,6 +37,8 @@ struct tra_packed_launch {
   int stream_rows, stream_tokens;            // backward: rows of a streamed tile, 128 or 64, and stream_rows / group
   int order, splits, n_units;                // n_units: query-tile pairs (forward) or key / query tiles (backward) launched
   int window, sinks, sink_rows;              // kOrderWindow; sink_rows: sinks rounded up to whole 8-row pieces of a tile
+  int sink_steps, sink_slots;                // backward: see tra_find_sink_unit; 0: the first keys' tiles walk all their queries
+  float* sink_part;                          //   [slot][kv_heads][sinks][dK, dV][d] fp32
   float sm_scale;
   int* status;
 };
@@ -56,6 +58,8 @@ int tra_packed_bwd_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_fwd_window_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_fwd_window_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_fwd_pieces_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_fwd_pieces_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_window_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_window_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered);
@@ -177,6 +181,35 @@ __device__ __forceinline__ tra_unit tra_find_unit(const tra_packed_launch& p, bo
     hi = min(lo + (l + 1) * stride, hi);
     lo += l * stride;
   }
+}
+
+// Backward with a window: the first keys are seen by all queries behind them, the others by a window's.  So that their tiles do not
+// walk on when all others are done, the queries of a sequence of more than sink_steps streamed tiles are cut into units of that many, whose
+// sums of the first keys' gradients go to `sink_part` and are added by a kernel of their own, in order.  Unit c of a sequence from token b on has
+// slot 2 floor(b / unit) + c, unit in tokens: a sequence longer than a unit ends in front of the next one's slots, and there are at most
+// 2 floor(total_q / unit) + 2, however many sequences there are.
+__device__ __forceinline__ int tra_sink_unit_tokens(const tra_packed_launch& p) { return p.sink_steps * p.stream_tokens; }
+
+// The unit of a slot (seq = -1: none).  One warp calls it; every lane gets the result.
+__device__ __forceinline__ tra_unit tra_find_sink_unit(const tra_packed_launch& p, int slot) {
+  const int lane = threadIdx.x & 31, unit = tra_sink_unit_tokens(p);
+  tra_unit u = {-1, 0, 1, {0, 0}, {0, 0}};
+  int lo = 0, hi = p.n_seq;                    // the last sequence whose first slot is not behind this one
+  while (hi - lo > 1) {
+    const int stride = (hi - lo + 31) / 32, s = lo + lane * stride;
+    const bool in = s < hi && 2 * (min(max(p.cu_q[s], 0), p.total_q) / unit) <= slot;
+    const unsigned hits = __ballot_sync(0xffffffffu, in);
+    if (!hits) return u;
+    const int l = 31 - __clz(hits);
+    hi = min(lo + (l + 1) * stride, hi);
+    lo += l * stride;
+  }
+  u.q = tra_clamp_range(p.cu_q[lo], p.cu_q[lo + 1], p.total_q, p.max_q, p.status);
+  u.k = tra_clamp_range(p.k_begin[lo], p.k_end[lo], p.total_k, p.max_k, p.status);
+  u.index = slot - 2 * (u.q.begin / unit);
+  u.count = (u.q.len + unit - 1) / unit;
+  if (u.q.len > unit && u.index >= 0 && u.index < u.count) u.seq = lo;
+  return u;
 }
 
 }  // namespace

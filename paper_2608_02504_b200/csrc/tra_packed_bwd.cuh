@@ -226,9 +226,28 @@ __device__ __forceinline__ void store_share(const RowAddresses& rows, uint32_t t
   }
 }
 
+// The same, not rounded.
+template <int kChannels>
+__device__ __forceinline__ void store_share_fp32(const RowAddresses& rows, uint32_t taddr, int h, bool any, float mul) {
+#pragma unroll 1
+  for (int c = 0; c < kChannels / 32; ++c) {
+    uint32_t v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = 0u;
+    if (any) {
+      tmem_ld32(taddr + h * kChannels + c * 32, v);
+      tmem_wait_ld(v);
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * mul);
+    rows.store64(v, h * kChannels * 4 + c * 128);
+    rows.store64(v + 16, h * kChannels * 4 + c * 128 + 64);
+  }
+}
+
 // ------------------------------------------------------------------------------------ dK, dV
 template <typename T, int D, int kHalves, int kOrder>
-__device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
+__device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh, const int sink_tile = -1) {
   using C = BwdCfg<D, kHalves>;
   constexpr bool kCausal = kOrder != kOrderNone;
   uint8_t* sK = smem;
@@ -244,7 +263,9 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
 
   // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    const tra_unit u = tra_find_unit(p, true, p.max_k <= kTileM, kTileM, unit);
+    tra_unit u = kOrder == kOrderWindow && sink_tile >= 0 ? tra_find_sink_unit(p, unit) : tra_find_unit(p, true, p.max_k <= kTileM, kTileM, unit);
+    if (kOrder == kOrderWindow && sink_tile < 0 && p.sink_steps > 0 && u.q.len > tra_sink_unit_tokens(p) && (u.index + 1) * kTileM <= p.sinks)
+      u.seq = -1;                                            // first keys alone: units of their own have them
     if (lane == 0) ctl->unit = u;
   } else if (warp == C::kSoftWarps + 1) {
     tmem_alloc<C::kColumns>(&ctl->tmem_base);
@@ -264,7 +285,8 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
   tc_fence_after();
   const uint32_t tmem = ctl->tmem_base;
   const tra_seq_range qr = ctl->unit.q, kr = ctl->unit.k;
-  const int key0 = ctl->unit.index * kTileM;
+  const bool of_sinks = kOrder == kOrderWindow && sink_tile >= 0;
+  const int key0 = (of_sinks ? sink_tile : ctl->unit.index) * kTileM;
   if (ctl->unit.seq < 0) {
     if (warp == C::kSoftWarps + 1) tmem_free<C::kColumns>(tmem);
     wait_last_launch();          // no block ends before the launch in front of it
@@ -272,11 +294,15 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
   }
   const int ahead = kr.len - qr.len;
   const int n_tiles_all = (qr.len + tile_tokens - 1) / tile_tokens;
+  // keys in front of it are seen whatever the distance, and others have their sums (of_sinks) or nobody does
+  const bool cut = kOrder == kOrderWindow && p.sink_steps > 0 && qr.len > tra_sink_unit_tokens(p);
+  const int staying = kOrder != kOrderWindow || (cut && !of_sinks) ? 0 : p.sinks;
   // causal: key j is seen by the tokens from j - ahead on
-  const int first_tile = kCausal ? max(key0 - ahead, 0) / tile_tokens : 0;
+  const int first_tile = max(kCausal ? max(key0 - ahead, 0) / tile_tokens : 0, of_sinks ? ctl->unit.index * p.sink_steps : 0);
   // window: key j is seen by the tokens up to j + window - 1 - ahead, one of the first tokens by all behind it
   int end_tile = n_tiles_all;
-  if (kOrder == kOrderWindow && key0 >= p.sinks)
+  if (of_sinks) end_tile = min(end_tile, (ctl->unit.index + 1) * p.sink_steps);
+  if (kOrder == kOrderWindow && key0 >= staying)
     end_tile = (int)min((long long)end_tile, max((long long)key0 + kTileM - 1 + p.window - ahead + tile_tokens - 1, 0ll) / tile_tokens);
   const int n_all = max(end_tile - first_tile, 0), n = n_all;
   const int tail_rows = (qr.len - (n_tiles_all - 1) * tile_tokens) * p.group;      // rows of the last tile
@@ -436,7 +462,7 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
     int blind_tok = key0 + r - ahead - first_tile * tile_tokens;         // tokens of the first tile in front of the first seer
     // window: tokens of the first tile in front of the last seer's successor
     int gone_tok = kOrder == kOrderWindow ? (int)min((long long)blind_tok + p.window, 1ll << 30) : 0;
-    const bool stays = kOrder == kOrderWindow && key0 + r < p.sinks;
+    const bool stays = kOrder == kOrderWindow && key0 + r < staying;
     bool alive = true;
     for (int i = 0; i < n; ++i) {
       const int st = i % kStatStages;
@@ -524,11 +550,20 @@ __device__ __forceinline__ void dkv_block(const tra_packed_launch& p, uint8_t* s
       tc_fence_after();
       // read again from shared memory and the thread index: the loop above needs the registers
       asm volatile("" : "+r"(r));
-      const int key = *(volatile int*)&ctl->unit.index * kTileM + r;
-      const bool row_valid = key < *(volatile int*)&ctl->unit.k.len;
+      const int key = (of_sinks ? sink_tile : *(volatile int*)&ctl->unit.index) * kTileM + r;
+      const bool row_valid = key < *(volatile int*)&ctl->unit.k.len && (kOrder != kOrderWindow || (of_sinks ? key < p.sinks : !cut || key >= p.sinks));
       const long long row = *(volatile int*)&ctl->unit.k.begin + (row_valid ? key : 0);
       const float mul = kScaled<T> && n > 0 ? 1.f / kProbMul : 1.f;
       const float mul_k = kScaled<T> && n > 0 ? p.sm_scale / (kProbMul * *(volatile float*)&ctl->tau) : p.sm_scale;
+      if (of_sinks) {
+        float* part = p.sink_part + (((long long)unit * p.kv_heads + kvh) * p.sinks + (row_valid ? key : 0)) * (2 * D);
+#pragma unroll 1
+        for (int which = 0; which < 2; ++which)
+          store_share_fp32<D / kHalves>(RowAddresses(row_valid ? part + (which ? 0 : D) : nullptr), tmem + lane_base + (which ? C::kSum1 : C::kSum0), h,
+                                        n > 0, which ? mul_k : mul);
+        bwd_teardown<C>(ctl, tmem, warp);
+        return;
+      }
       T* out[2] = {(T*)p.dv + row * p.dv_stride[0] + kvh * p.dv_stride[1], (T*)p.dk + row * p.dk_stride[0] + kvh * p.dk_stride[1]};
 #pragma unroll 1
       for (int which = 0; which < 2; ++which)
@@ -790,7 +825,16 @@ template <typename T, int D, int kHalves, int kOrder>
 __global__ void __launch_bounds__(BwdCfg<D, kHalves>::kThreads, BwdCfg<D, kHalves>::kBlocks)
     tra_packed_bwd_kernel(const __grid_constant__ tra_packed_launch p, int dkv_units, int dq_units) {
   extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
-  const int n_dkv = dkv_units * p.kv_heads, b = blockIdx.x;
+  int b = blockIdx.x;
+  if constexpr (kOrder == kOrderWindow) {
+    const int n_sink = p.sink_slots * p.kv_heads * ((min(p.sinks, p.max_k) + kTileM - 1) / kTileM);
+    if (b < n_sink) {
+      dkv_block<T, D, kHalves, kOrder>(p, smem, b % p.sink_slots, b / p.sink_slots % p.kv_heads, b / p.sink_slots / p.kv_heads);
+      return;
+    }
+    b -= n_sink;
+  }
+  const int n_dkv = dkv_units * p.kv_heads;
   if (b < n_dkv)
     dkv_block<T, D, kHalves, kOrder>(p, smem, b % dkv_units, b / dkv_units);
   else
@@ -909,6 +953,36 @@ int launch_delta_norms(const tra_packed_ctx& c, const tra_packed_launch& a) {
   return tra_launch(tra_packed_delta_norms_kernel<D>, dim3((unsigned)(q_blocks + v_blocks)), 256, 0, c.stream, false, 1, a, (int)q_blocks, (int)steps);
 }
 
+// The first keys' gradients of cut sequences (tra_find_sink_unit): sums over their units, in order, rounded.  A warp per key.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) tra_packed_sinks_kernel(const __grid_constant__ tra_packed_launch p) {
+  const int seq = blockIdx.x, kvh = blockIdx.y, lane = threadIdx.x & 31, unit = tra_sink_unit_tokens(p);
+  const tra_seq_range q = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
+  const tra_seq_range k = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
+  if (q.len <= unit) return;
+  const int count = (q.len + unit - 1) / unit, slot = 2 * (q.begin / unit);
+  constexpr int kPer = 2 * D / 32;             // of dK, then dV
+  const bool of_v = lane >= 16;
+  const int channel = (lane & 15) * kPer;
+  for (int key = blockIdx.z * 8 + (threadIdx.x >> 5); key < min(p.sinks, k.len); key += gridDim.z * 8) {
+    float sum[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sum[i] = 0.f;
+    for (int c = 0; c < count; ++c) {
+      const float* part = p.sink_part + (((long long)(slot + c) * p.kv_heads + kvh) * p.sinks + key) * (2 * D) + lane * kPer;
+#pragma unroll
+      for (int i = 0; i < kPer; i += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(part + i);
+        sum[i] += x.x, sum[i + 1] += x.y, sum[i + 2] += x.z, sum[i + 3] += x.w;
+      }
+    }
+    const long long row = k.begin + key;
+    T* out = of_v ? (T*)p.dv + row * p.dv_stride[0] + kvh * p.dv_stride[1] : (T*)p.dk + row * p.dk_stride[0] + kvh * p.dk_stride[1];
+#pragma unroll
+    for (int i = 0; i < kPer; i += 2) *reinterpret_cast<uint32_t*>(out + channel + i) = pack_pair<T>(sum[i], sum[i + 1]);
+  }
+}
+
 template <typename T, int D, int kHalves, int kOrder>
 int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   const long long rows = (long long)a.total_q * a.heads;
@@ -923,13 +997,18 @@ int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
   }
   const int dkv_units = a.max_k > 0 ? (a.max_k <= kTileM ? 0 : a.total_k / kTileM) + a.n_seq : 0;
   const int dq_units = a.max_q > 0 ? (a.max_q <= a.tile_tokens ? 0 : a.total_q / a.tile_tokens) + a.n_seq : 0;
-  const long long blocks = ((long long)dkv_units + dq_units) * a.kv_heads;
+  const long long sink_units = kOrder == kOrderWindow ? (long long)a.sink_slots * (((a.sinks < a.max_k ? a.sinks : a.max_k) + kTileM - 1) / kTileM) : 0;
+  const long long blocks = (sink_units + dkv_units + dq_units) * a.kv_heads;
   if (blocks == 0) return TRA_OK;
   if (blocks > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
   using C = BwdCfg<D, kHalves>;
   constexpr auto kern = tra_packed_bwd_kernel<T, D, kHalves, kOrder>;
   if ((rc = tra_allow_smem<kern>(C::kSmemBytes)) != TRA_OK) return rc;
-  return tra_launch(kern, dim3((unsigned)blocks), C::kThreads, C::kSmemBytes, c.stream, rows > 0, 1, a, dkv_units, dq_units);
+  rc = tra_launch(kern, dim3((unsigned)blocks), C::kThreads, C::kSmemBytes, c.stream, rows > 0, 1, a, dkv_units, dq_units);
+  if (rc != TRA_OK || sink_units == 0) return rc;
+  const int keys = a.sinks < a.max_k ? a.sinks : a.max_k;
+  return tra_launch(tra_packed_sinks_kernel<T, D>, dim3((unsigned)a.n_seq, (unsigned)a.kv_heads, (unsigned)(keys < 512 ? (keys + 7) / 8 : 64)), 256, 0,
+                    c.stream, false, 1, a);
 }
 
 template <int D, int kHalves>

@@ -36,10 +36,13 @@ constexpr int kFwdRegsControl = 72;
 constexpr int kKeyTile = 128;
 constexpr int kAskAhead = 1;             // key blocks a unit's producer has left to load when the next unit is asked for
 
-template <int D>
+// kPieces: numbers of the 16-bit type that a key's or a value's element is the sum of; 2: a cache of 4 bits, whose elements have
+// more bits than the type, read back as the rounded element and what rounding took from it (heads kv_heads .. of K and V), with
+// two products where there was one.
+template <int D, int kPieces>
 struct FwdCfg {
   static constexpr int kTileBytes = kTileM * D * 2;
-  static constexpr int kSlots = D == 128 ? 5 : 6;
+  static constexpr int kSlots = D == 128 ? 5 : kPieces == 1 ? 6 : 10;
   static constexpr int kAtoms = D / 64;
   static constexpr int kAtomBytes = kTileM * 128;
   static constexpr int kSmemData = (2 + kSlots) * kTileBytes;
@@ -60,15 +63,15 @@ struct FwdCtl {
   uint64_t want;              // the producer nears the end of its unit
   uint64_t work_full[2], work_free[2];
   uint64_t q_full, q_free;
-  uint64_t kv_full[6];
+  uint64_t kv_full[10];
   uint64_t kv_release[8];
   uint64_t s_full[2];
   uint64_t p_ready[2][2];     // [tile][64-key half]
   uint64_t o_full[2], o_free[2];    // [tile]: the last product of a unit has retired / its sum has been read
   uint64_t tail_full[2], tail_ready[2];   // V tiles that reach past the sequence's end: loaded; their foreign rows zeroed
   uint64_t drain;
-  int freed_by[6];            // release event that frees a slot's tile (producer only)
-  int tail_slot[2];
+  int freed_by[10];           // release event that frees a slot's tile (producer only)
+  int tail_slot[2][2];
   uint32_t tmem_base;
   int abort_flag;
   FwdWork work[2];
@@ -76,7 +79,7 @@ struct FwdCtl {
 static_assert(sizeof(FwdCtl) <= 512, "control block");
 
 // What a unit asks of every role.
-template <int kOrder>
+template <int kOrder, int kPieces>
 struct FwdPlan {
   int tok0;                   // first token of tile 0, inside the sequence
   int gap;                    // of the key axis (tra_key_axis)
@@ -87,14 +90,16 @@ struct FwdPlan {
     const int q_len = w.unit.q.len, k_len = w.unit.k.len;
     tok0 = w.unit.index * 2 * p.tile_tokens;
     const int ahead = k_len - q_len;                      // causal: token i sees keys 0 .. i + ahead
-    const tra_key_axis<kOrder> axis(p, tok0 + ahead, k_len);
+    // (two pieces: this order alone is compiled, with a window without end where there is none; not causal: every query sits at the end)
+    const bool all = kPieces == 2 && p.order == kOrderNone;
+    const tra_key_axis<kOrder> axis(p, all ? k_len - 1 : tok0 + ahead, k_len);
     gap = axis.gap;
     int blocks[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int first = tok0 + k * p.tile_tokens;
       const int last = min(first + p.tile_tokens, q_len) - 1;
-      const int keys = first >= q_len ? 0 : kOrder ? min(max(last + 1 + ahead - gap, 0), axis.len) : k_len;
+      const int keys = first >= q_len ? 0 : kOrder ? min(max((all ? k_len : last + 1 + ahead) - gap, 0), axis.len) : k_len;
       blocks[k] = (keys + kKeyTile - 1) / kKeyTile;
     }
     const int nb = max(blocks[0], blocks[1]);
@@ -171,9 +176,9 @@ __device__ __forceinline__ void store_unit(const tra_packed_launch& p, FwdCtl* c
 
 // Blocks that stay, one per SM: while the softmax warps finish a unit, the loads and the first scores of the next one are under
 // way already (a block per unit spent about 10 us on set-up, first loads and epilogue: as much as five key blocks).
-template <typename T, int D, int kOrder, bool kExact>
+template <typename T, int D, int kOrder, bool kExact, int kPieces>
 __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __grid_constant__ tra_packed_launch p) {
-  using C = FwdCfg<D>;
+  using C = FwdCfg<D, kPieces>;
   constexpr bool kCausal = kOrder != kOrderNone;
   extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
   uint8_t* sQ = smem;
@@ -201,7 +206,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
     mbar_init(smem_u32(&ctl->want), 1);
     mbar_init(smem_u32(&ctl->q_full), 1);
     mbar_init(smem_u32(&ctl->q_free), 1);
-    for (int i = 0; i < 6; ++i) mbar_init(smem_u32(&ctl->kv_full[i]), 1);
+    for (int i = 0; i < C::kSlots; ++i) mbar_init(smem_u32(&ctl->kv_full[i]), 1);
     for (int i = 0; i < 8; ++i) mbar_init(smem_u32(&ctl->kv_release[i]), 1);
     mbar_init(smem_u32(&ctl->drain), 1);
     ctl->abort_flag = 0;
@@ -283,7 +288,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       for (int n = 0; alive && next_work(n); ++n) {
         const FwdWork w = ctl->work[n & 1];
         done_with_work(n);
-        const FwdPlan<kOrder> u(w, p);
+        const FwdPlan<kOrder, kPieces> u(w, p);
         if (u.n_entries <= kAskAhead && lane == 0) mbar_arrive(smem_u32(&ctl->want));
         if (u.n_entries == 0) continue;
         if (lane == 0) {
@@ -300,25 +305,29 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
           // per unit: the first frees K0, event e + 1 frees V_e and K_(e+1).  Event r arrives on kv_release[r % 8].
           for (int e = 0; e < u.n_entries && alive; ++e) {
             if (e + kAskAhead + 1 == u.n_entries) mbar_arrive(smem_u32(&ctl->want));
-            for (int kv = 0; kv < 2; ++kv) {
+            for (int kv = 0; kv < 2 * kPieces && alive; ++kv) {
+              const bool of_v = kv >= kPieces;
+              const int piece = of_v ? kv - kPieces : kv;
               if (n_load >= C::kSlots) {
                 const int r = ctl->freed_by[slot];
                 if (!(alive = mbar_wait(smem_u32(&ctl->kv_release[r & 7]), (uint32_t)(r >> 3) & 1u, abort_flag, p.status))) break;
               } else {
                 ++n_load;
               }
-              ctl->freed_by[slot] = event0 + e + kv;
+              ctl->freed_by[slot] = event0 + e + of_v;
               uint32_t bar = smem_u32(&ctl->kv_full[slot]);
-              if (kv == 1 && u.tail && e == u.n_entries - 1) {
+              if (of_v && u.tail && e == u.n_entries - 1) {
                 // rows of it are zeroed first: it is announced by tail_ready, and the slot's barrier only keeps its count
                 mbar_arrive(bar);
-                ctl->tail_slot[tails & 1] = slot;
+                ctl->tail_slot[tails & 1][piece] = slot;
                 bar = smem_u32(&ctl->tail_full[tails & 1]);
+                if (piece == 0) mbar_expect_tx(bar, kPieces * C::kTileBytes);
+              } else {
+                mbar_expect_tx(bar, C::kTileBytes);
               }
-              mbar_expect_tx(bar, C::kTileBytes);
-              tra_load_keys<kOrder, C::kAtoms>(p, (u.v_begin + e) * kKeyTile, kKeyTile, u.gap, kv == 1, smem_u32(sKV + slot * C::kTileBytes), C::kAtomBytes,
+              tra_load_keys<kOrder, C::kAtoms>(p, (u.v_begin + e) * kKeyTile, kKeyTile, u.gap, of_v, smem_u32(sKV + slot * C::kTileBytes), C::kAtomBytes,
                                                [&](uint32_t dst, const CUtensorMap* map, int channel, int key) {
-                                                 tma_load_3d(dst, map, bar, channel, w.kvh, w.unit.k.begin + key);
+                                                 tma_load_3d(dst, map, bar, channel, w.kvh + piece * p.kv_heads, w.unit.k.begin + key);
                                                });
               if (++slot == C::kSlots) slot = 0;
             }
@@ -335,12 +344,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       for (int n = 0; next_work(n); ++n) {
         const FwdWork w = ctl->work[n & 1];
         done_with_work(n);
-        const FwdPlan<kOrder> u(w, p);
+        const FwdPlan<kOrder, kPieces> u(w, p);
         if (!u.tail) continue;
         if (!mbar_wait_warp(smem_u32(&ctl->tail_full[tails & 1]), (uint32_t)(tails >> 1) & 1u, abort_flag, p.status)) break;
-        const int slot = *(volatile int*)&ctl->tail_slot[tails & 1];
-        zero_tile_rows(sKV + slot * C::kTileBytes, w.unit.k.len - u.gap - (u.v_begin + u.n_entries - 1) * kKeyTile, kKeyTile, C::kAtoms,
-                       C::kAtomBytes, lane, 32);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+          zero_tile_rows(sKV + *(volatile int*)&ctl->tail_slot[tails & 1][i] * C::kTileBytes,
+                         w.unit.k.len - u.gap - (u.v_begin + u.n_entries - 1) * kKeyTile, kKeyTile, C::kAtoms, C::kAtomBytes, lane, 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->tail_ready[tails & 1]));
@@ -357,26 +367,33 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       constexpr uint32_t kHi = desc_hi(1024);
       const uint32_t q_lo0 = desc_lo(smem_u32(sQ), 16), q_lo1 = desc_lo(smem_u32(sQ + C::kTileBytes), 16);
       const uint32_t k_lo0 = desc_lo(smem_u32(sKV), 16), v_lo0 = desc_lo(smem_u32(sKV), C::kAtomBytes);
-      auto issue_s = [&](int k, int kslot) {
-        const uint32_t qa = k ? q_lo1 : q_lo0, ka = k_lo0 + (uint32_t)kslot * (C::kTileBytes >> 4);
+      auto issue_s = [&](int k, const int* kslot) {
+        const uint32_t qa = k ? q_lo1 : q_lo0;
         const uint32_t d = tmem + k * 128;
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t off = ((kk >> 2) * C::kAtomBytes + (kk & 3) * 32) >> 4;
-          tc_mma_ss(d, qa + off, kHi, ka + off, kHi, kIdescQK, kk > 0 ? 1u : 0u);
+        for (int i = 0; i < kPieces; ++i) {
+          const uint32_t ka = k_lo0 + (uint32_t)kslot[i] * (C::kTileBytes >> 4);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t off = ((kk >> 2) * C::kAtomBytes + (kk & 3) * 32) >> 4;
+            tc_mma_ss(d, qa + off, kHi, ka + off, kHi, kIdescQK, kk > 0 || i > 0 ? 1u : 0u);
+          }
         }
         tc_commit(smem_u32(&ctl->s_full[k]));
       };
-      auto issue_pv = [&](int k, int vslot, uint32_t parity, uint32_t started) -> bool {
-        const uint32_t va = v_lo0 + (uint32_t)vslot * (C::kTileBytes >> 4);
+      auto issue_pv = [&](int k, const int* vslot, uint32_t parity, uint32_t started) -> bool {
         const uint32_t d = tmem + 256 + k * 128, pa = tmem + k * 128;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           if (!wait(smem_u32(&ctl->p_ready[k][half]), parity)) return false;
           tc_fence_after();
 #pragma unroll
-          for (int kk = half * 4; kk < half * 4 + 4; ++kk)
-            tc_mma_ts(d, pa + kk * 8, va + kk * (2048 >> 4), kHi, kIdescPV, kk > 0 ? 1u : started);
+          for (int i = 0; i < kPieces; ++i) {
+            const uint32_t va = v_lo0 + (uint32_t)vslot[i] * (C::kTileBytes >> 4);
+#pragma unroll
+            for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+              tc_mma_ts(d, pa + kk * 8, va + kk * (2048 >> 4), kHi, kIdescPV, kk > 0 || i > 0 ? 1u : started);
+          }
         }
         return true;
       };
@@ -388,6 +405,16 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
           phase ^= 1u;
         }
       };
+      // the next tile's slots, once it is there
+      auto take = [&](int* slots) -> bool {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          slots[i] = slot;
+          if (!wait(smem_u32(&ctl->kv_full[slot]), phase)) return false;
+          advance();
+        }
+        return true;
+      };
       uint32_t event = 0, units = 0, tails = 0;
       uint32_t entries[2] = {0u, 0u};        // key blocks of a tile so far
       uint32_t sums[2] = {0u, 0u};           // units in which the tile had any
@@ -395,31 +422,28 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       for (int n = 0; alive && uniform(next_work(n)); ++n) {
         const FwdWork w = ctl->work[n & 1];
         done_with_work(n);
-        FwdPlan<kOrder> u(w, p);
+        FwdPlan<kOrder, kPieces> u(w, p);
         u.n_entries = uniform(u.n_entries);
         u.n_own[0] = uniform(u.n_own[0]);
         u.n_own[1] = uniform(u.n_own[1]);
         u.tail = uniform(u.tail);
         if (u.n_entries == 0) continue;
-        alive = wait(smem_u32(&ctl->q_full), units & 1u) &&
-                wait(smem_u32(&ctl->kv_full[slot]), phase);       // first K tile
+        int kslot[kPieces], vslot[kPieces];
+        alive = wait(smem_u32(&ctl->q_full), units & 1u) && take(kslot);        // first K tile
         if (!alive) break;
         tc_fence_after();
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          if (u.n_own[k] > 0) issue_s(k, slot);
+          if (u.n_own[k] > 0) issue_s(k, kslot);
         tc_commit(smem_u32(&ctl->kv_release[event++ & 7u]));
         if (u.n_entries == 1) tc_commit(smem_u32(&ctl->q_free));
-        advance();
         for (int e = 0; e < u.n_entries; ++e) {
-          const int vslot = slot;
           const bool have_next = e + 1 < u.n_entries;
-          alive = wait(smem_u32(&ctl->kv_full[vslot]), phase);
+          alive = take(vslot);
           if (alive && u.tail && !have_next) {
             alive = wait(smem_u32(&ctl->tail_ready[tails & 1]), (tails >> 1) & 1u);
             ++tails;
           }
-          advance();
           bool k_ready = false;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
@@ -435,18 +459,17 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
               tc_commit(smem_u32(&ctl->o_full[k]));
             } else {
               if (!k_ready) {
-                alive = wait(smem_u32(&ctl->kv_full[slot]), phase);
+                alive = take(kslot);
                 k_ready = true;
                 if (!alive) continue;
                 tc_fence_after();
               }
-              issue_s(k, slot);
+              issue_s(k, kslot);
             }
           }
           if (!alive) break;
           tc_commit(smem_u32(&ctl->kv_release[event++ & 7u]));       // V of this block and K of the next
           if (e + 2 == u.n_entries) tc_commit(smem_u32(&ctl->q_free));
-          if (have_next) advance();
         }
         ++units;
       }
@@ -468,7 +491,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       bool rows_here;
       {
         const FwdWork w = ctl->work[it & 1];
-        const FwdPlan<kOrder> u(w, p);
+        const FwdPlan<kOrder, kPieces> u(w, p);
         n = u.n_own[k];
         const int tile_tok = u.tok0 + k * p.tile_tokens;
         // (opaque to the compiler: what follows from the thread index alone would be kept in registers through all units)
@@ -479,7 +502,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         // columns of the first block that the row sees; rows that hold no query follow the tile's last one, so that they
         // force no mask on their warp
         const int mask_tok = min(tile_tok + r / p.group, min(tile_tok + p.tile_tokens, w.unit.q.len) - 1);
-        col_limit = (kCausal ? min(max(mask_tok + 1 + w.unit.k.len - w.unit.q.len - u.gap, 0), w.unit.k.len) : w.unit.k.len) - u.v_begin * kKeyTile;
+        col_limit = (kCausal && !(kPieces == 2 && p.order == kOrderNone) ? min(max(mask_tok + 1 + w.unit.k.len - w.unit.q.len - u.gap, 0), w.unit.k.len)
+                                                                         : w.unit.k.len) - u.v_begin * kKeyTile;
         if (kOrder == kOrderWindow) first_cols = p.sinks - u.v_begin * kKeyTile;
       }
       if (!rows_here) {
@@ -620,23 +644,23 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
   }
 }
 
-template <typename T, int D, int kOrder, bool kExact>
+template <typename T, int D, int kOrder, bool kExact, int kPieces>
 int launch_fwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
-  constexpr auto kern = tra_packed_fwd_kernel<T, D, kOrder, kExact>;
-  const int rc = tra_allow_smem<kern>(FwdCfg<D>::kSmemBytes);
+  constexpr auto kern = tra_packed_fwd_kernel<T, D, kOrder, kExact, kPieces>;
+  constexpr int kSmem = FwdCfg<D, kPieces>::kSmemBytes;
+  const int rc = tra_allow_smem<kern>(kSmem);
   if (rc != TRA_OK) return rc;
   const long long units = (long long)a.n_units * a.kv_heads * a.splits;
   if (units > 0x3fffffffll) return TRA_ERR_UNSUPPORTED;
-  return tra_launch(kern, dim3((unsigned)units), kFwdThreads, FwdCfg<D>::kSmemBytes, c.stream, false,
-                    1, a);
+  return tra_launch(kern, dim3((unsigned)units), kFwdThreads, kSmem, c.stream, false, 1, a);
 }
 
-template <typename T, int D, int kOrder>
+template <typename T, int D, int kOrder, int kPieces = 1>
 int launch_fwd_order(const tra_packed_ctx& c, const tra_packed_launch& a) {
-  return a.lse ? launch_fwd<T, D, kOrder, true>(c, a) : launch_fwd<T, D, kOrder, false>(c, a);
+  return a.lse ? launch_fwd<T, D, kOrder, true, kPieces>(c, a) : launch_fwd<T, D, kOrder, false, kPieces>(c, a);
 }
 
-// The two orders without a window, and the one with (translation units of their own).
+// The two orders without a window, the one with, and keys and values in two pieces (translation units of their own).
 template <int D>
 int launch_fwd_shape(const tra_packed_ctx& c, const tra_packed_launch& a) {
   if (c.h->cfg.dtype == TRA_BF16)
@@ -646,6 +670,10 @@ int launch_fwd_shape(const tra_packed_ctx& c, const tra_packed_launch& a) {
 template <int D>
 int launch_fwd_window(const tra_packed_ctx& c, const tra_packed_launch& a) {
   return c.h->cfg.dtype == TRA_BF16 ? launch_fwd_order<__nv_bfloat16, D, kOrderWindow>(c, a) : launch_fwd_order<__half, D, kOrderWindow>(c, a);
+}
+template <int D>
+int launch_fwd_pieces(const tra_packed_ctx& c, const tra_packed_launch& a) {
+  return c.h->cfg.dtype == TRA_BF16 ? launch_fwd_order<__nv_bfloat16, D, kOrderWindow, 2>(c, a) : launch_fwd_order<__half, D, kOrderWindow, 2>(c, a);
 }
 
 }  // namespace

@@ -10,6 +10,8 @@ h = 2^-11 of fp16, in which the products over codes run:
   - fp16 numbers below 2^-14: steps and lowest values are off by 2^-24 of the largest of them, top = max (|low|, 16 step) times 2; probabilities, held
     times 2^6 and at most 2^8 above the reference, by 2^-25 in sums that are at least 2^-2: 2^-22 top per key;
   - sums over n keys: n + 16 units 2^-23 of sum p (|low| + 15 step).
+Calls of more than 64 rows per key/value head (`pieces`) take keys and values as two numbers of the type each, off by u^2 of an element, and
+round probabilities to the type as the other kernels do: u sum p |v - o|, and in fp16 2^-25 per key of the largest value.
 lse: as in packed_reference.py."""
 import math
 
@@ -48,7 +50,7 @@ def sizes(x):
     return each, float(torch.maximum(low.abs(), 16 * step).max()) if x.numel() else 0.0
 
 
-def attention(q, k, v, cu_q, k_begin, k_end, window, sinks, scale):
+def attention(q, k, v, cu_q, k_begin, k_end, window, sinks, scale, pieces=False, causal=True):
     """k, v: the 16-bit tensors that were written.  -> dict of o, lse and tolerances."""
     u = torch.finfo(q.dtype).eps / 2
     h = 2.0 ** -11
@@ -61,7 +63,7 @@ def attention(q, k, v, cu_q, k_begin, k_end, window, sinks, scale):
         n, m = q1 - q0, k1 - k0
         if n == 0 or m == 0:
             continue
-        mask = seen(n, m, window, sinks, q.device)
+        mask = seen(n, m, window, sinks, q.device) if causal else torch.ones(n, m, dtype=torch.bool, device=q.device)
         for i in range(hk):
             rows, heads = slice(q0, q1), slice(i * g, (i + 1) * g)
             Q = q[rows, heads].double().transpose(0, 1)
@@ -75,6 +77,12 @@ def attention(q, k, v, cu_q, k_begin, k_end, window, sinks, scale):
             e = scale * Q.norm(dim=-1) * Ks.norm(dim=-1).max() * (d + 16) * UNIT + 2.0 ** -21
             tol = u * o.abs() * (1 + 2 * u) + h * o.abs() + (2 * h + e)[..., None] * size * (1 + 4 * h) + e[..., None] * o.abs() \
                 + (m + 16) * UNIT * size + (2.0 ** -23 + m * 2.0 ** -22) * top * (p.sum(-1, keepdim=True) > 0) + tiny
+            if pieces:
+                e = e + scale * Q.norm(dim=-1) * K.norm(dim=-1).max() * 2 * u * u
+                absv = p @ V.abs()
+                tol = u * o.abs() * (1 + 2 * u) + (u + e)[..., None] * (absv + o.abs()) * (1 + 4 * u) + 2 * u * u * absv + (m + 16) * UNIT * absv + tiny
+                if q.dtype == torch.float16:
+                    tol = tol + m * 2.0 ** -25 * V.abs().max()
             r["o"][rows, heads], r["o_tol"][rows, heads] = o.transpose(0, 1), tol.transpose(0, 1)
             lse_tol = e + (m + 64) * UNIT / 2 + lse.abs().nan_to_num(posinf=0) * UNIT
             r["lse"][rows, heads] = lse.transpose(0, 1)

@@ -152,7 +152,7 @@ def run(api, dtype, d, hq, hk, lens_q, lens_k, window=0, sinks=0, slots=None, se
     cache.v_step.fill_(float("nan"))
     for b, e in zip(kb, ke):
         cache.write(k[b:e], v[b:e], torch.arange(b, e, dtype=torch.int32, device="cuda"))
-    want = attention(q, k, v, cu, kb, ke, window, sinks, d ** -0.5)
+    want = attention(q, k, v, cu, kb, ke, window, sinks, d ** -0.5, max(lens_q) * hq // hk > 64, causal)
     kw = dict(k_range=(i32(kb), i32(ke)), max_q=max(lens_q), max_k=max(lens_k))
     o = torch.full((total_q, hq, d), 77.0, dtype=dtype, device="cuda")
     lse = torch.full((total_q, hq), 55.0, device="cuda")
@@ -192,6 +192,27 @@ def test_few_tokens(api, window, sinks):
     run(api, BF, 64, 1, 1, [16, 15], [16, 4000], window, sinks)
     run(api, HALF, 128, 6, 2, [10, 3, 20], [400, 33, 1000], window, sinks)          # more than one tile of rows
     run(api, BF, 128, 2, 1, [32, 1], [130, 700], window, sinks)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (100, 5), (700, 130), (300, 256)])
+@pytest.mark.parametrize("dtype,d,hq,hk", [(BF, 128, 10, 2), (HALF, 64, 3, 1), (BF, 64, 4, 4), (HALF, 128, 8, 1)])
+def test_chunks(api, dtype, d, hq, hk, window, sinks):
+    """More than 64 rows per key/value head: keys and values read back in two pieces."""
+    run(api, dtype, d, hq, hk, [100, 40, 60, 300, 20, 0, 1], [1000, 40, 25, 301, 0, 50, 1300], window, sinks)
+    run(api, dtype, d, hq, hk, [97], [5000], window, sinks)
+    run(api, dtype, d, hq, hk, [130, 77], [2000, 131], window, sinks, slots=2048)
+
+
+def test_chunks_that_are_not_causal(api):
+    run(api, BF, 128, 4, 2, [100, 1, 70], [300, 1000, 12], causal=False)
+    run(api, HALF, 64, 4, 2, [100, 1, 70], [300, 1000, 12], causal=False)
+    run(api, BF, 64, 4, 2, [3, 1], [300, 1000], causal=False)
+
+
+def test_groups(api):
+    for group in (1, 3, 7, 16, 43, 100, 128):
+        run(api, BF, 64, group, 1, [70, 9, 2], [90, 700, 1030], 200, 9)
+        run(api, HALF, 128, 2 * group, 2, [1, 1], [700, 33])
 
 
 def test_many_splits(api):

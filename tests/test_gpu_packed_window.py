@@ -267,3 +267,11 @@ def test_refusals(api):
         with pytest.raises(api.TraError) as e:
             api.PackedAttn(4, 2, 64, **kw)
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("dtype,d,hq,hk", [(BF, 128, 4, 1), (HALF, 64, 5, 1), (HALF, 128, 12, 2)])
+@pytest.mark.parametrize("window,sinks", [(40, 3), (200, 140)])
+def test_first_keys_of_long_sequences(api, dtype, d, hq, hk, window, sinks):
+    """Sequences whose queries are cut into units for the first keys' gradients, among others that are not; more keys than queries."""
+    backward(api, dtype, d, hq, hk, window, sinks, [3, 2500, 0, 130, 1, 1200, 511])
+    backward(api, dtype, d, hq, hk, window, sinks, [900, 0, 1500, 20], [1900, 10, 1400, 20])
