@@ -13,6 +13,7 @@ struct Cache4Rows {
   void *k_step, *v_step;
   const int32_t* slots;
   int n, tokens;
+  bool wide;                            // rows of k and v start on 32 bytes
   int* status;
 };
 
@@ -35,24 +36,176 @@ __device__ __forceinline__ uint32_t as_bits(typename Pair<T>::type x) {
   return *reinterpret_cast<uint32_t*>(&x);
 }
 
+// 32 bytes, aligned to 16 (two accesses) or to 32 (one: whole sectors, where a warp's threads are 64 bytes apart)
+__device__ __forceinline__ void load64(const void* p, bool wide, uint32_t* r) {
+  if (wide) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(r[8 * i]), "=r"(r[8 * i + 1]), "=r"(r[8 * i + 2]), "=r"(r[8 * i + 3]), "=r"(r[8 * i + 4]), "=r"(r[8 * i + 5]), "=r"(r[8 * i + 6]),
+                     "=r"(r[8 * i + 7])
+                   : "l"((const uint8_t*)p + 32 * i)
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+      r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
+    }
+  }
+}
+__device__ __forceinline__ void store64(void* p, bool wide, const uint32_t* r) {
+  if (wide) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[8 * i]), "r"(r[8 * i + 1]), "r"(r[8 * i + 2]), "r"(r[8 * i + 3]),
+                   "r"(r[8 * i + 4]), "r"(r[8 * i + 5]), "r"(r[8 * i + 6]), "r"(r[8 * i + 7]), "l"((uint8_t*)p + 32 * i)
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+  }
+}
+
+// The codes of a row lie in pieces of 16 bytes, and a group's in all of them: the G lanes of a row, one group each, exchange words.  Lane j's
+// words of group j (keys: word t; values: half words of g = 0 .. 7) <-> words 4 j .. 4 j + 3 of the row.
+template <int G>
+__device__ __forceinline__ void swap_key_words(uint32_t* w, int j) {          // its own inverse for G = 4
+#pragma unroll
+  for (int b = 1; b < G; b <<= 1) {
+    const bool up = (j & b) != 0;
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      if (u & b) continue;
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[u] : w[u | b], b);
+      if (up)
+        w[u] = got;
+      else
+        w[u | b] = got;
+    }
+  }
+}
+template <int G>
+__device__ __forceinline__ void key_words_to_row(uint32_t* w, int j) {
+  if constexpr (G == 4) {
+    swap_key_words<4>(w, j);
+  } else {                                     // word 2 t + j: t = 0, 1 and t = 2, 3
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, j ? w[u] : w[u + 2], 1);
+      if (j)
+        w[u] = got;                            // t = u + 2 of group 0
+      else
+        w[u + 2] = got;                        // t = u of group 1
+    }
+    const uint32_t x = w[1];                   // (t, j): 00 10 01 11 -> 00 01 10 11
+    w[1] = w[2];
+    w[2] = x;
+  }
+}
+template <int G>
+__device__ __forceinline__ void row_to_key_words(uint32_t* w, int j) {
+  if constexpr (G == 4) {
+    swap_key_words<4>(w, j);
+  } else {
+    const uint32_t x = w[1];
+    w[1] = w[2];
+    w[2] = x;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, j ? w[u] : w[u + 2], 1);
+      if (j)
+        w[u] = got;
+      else
+        w[u + 2] = got;
+    }
+  }
+}
+// h: eight halves of words in the low 16 bits; w: words 4 j .. 4 j + 3
+template <int G>
+__device__ __forceinline__ void value_halves_to_row(const uint32_t* h, uint32_t* w, int j) {
+  // neighbours join halves: the even lane takes g = 0, 1, 4, 5 (d 64: 0 .. 3), the odd one the others
+  const bool odd = j & 1;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int mine = G == 4 ? (u & 1) + (u & 2) * 2 : u, other = G == 4 ? mine + 2 : u + 4;
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? h[mine] : h[other], 1);
+    w[u] = odd ? __byte_perm(got, h[other], 0x5410) : __byte_perm(h[mine], got, 0x5410);
+  }
+  if constexpr (G == 4) {
+    // words 2 g + x: lanes 0, 1 hold x = 0 of g = (0, 1, 4, 5), (2, 3, 6, 7), lanes 2, 3 hold x = 1 of them
+    const bool up = j & 2;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[u] : w[u + 2], 2);
+      if (up)
+        w[u] = got;
+      else
+        w[u + 2] = got;
+    }
+    const uint32_t x = w[1];
+    w[1] = w[2];
+    w[2] = x;
+  }
+}
+// the way back; p[i]: halves of g = 2 i and 2 i + 1, side by side
+template <int G>
+__device__ __forceinline__ void row_to_value_pairs(uint32_t* w, uint32_t* p, int j) {
+  if constexpr (G == 4) {
+    const uint32_t x = w[1];
+    w[1] = w[2];
+    w[2] = x;
+    const bool up = j & 2;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[u] : w[u + 2], 2);
+      if (up)
+        w[u] = got;
+      else
+        w[u + 2] = got;
+    }
+  }
+  const bool odd = j & 1;
+  // own half of the own words, two to a register, and the neighbour's half of them for it
+  const uint32_t own = odd ? 0x7632u : 0x5410u, his = odd ? 0x5410u : 0x7632u;
+  uint32_t mine[2], got[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    mine[u] = __byte_perm(w[2 * u], w[2 * u + 1], own);
+    got[u] = __shfl_xor_sync(0xffffffffu, __byte_perm(w[2 * u], w[2 * u + 1], his), 1);
+  }
+  if constexpr (G == 4) {                      // even: g = 01, 45 own, 23, 67 the neighbour's
+    p[0] = odd ? got[0] : mine[0];
+    p[1] = odd ? mine[0] : got[0];
+    p[2] = odd ? got[1] : mine[1];
+    p[3] = odd ? mine[1] : got[1];
+  } else {                                     // even: g = 01, 23 own
+    p[0] = odd ? got[0] : mine[0];
+    p[1] = odd ? got[1] : mine[1];
+    p[2] = odd ? mine[0] : got[0];
+    p[3] = odd ? mine[1] : got[1];
+  }
+}
+
 // ------------------------------------------------------------------------------------ write
 // Of a group of 32 channels x: low = min x, step = the smallest number of the type with 15 step >= max x - low, code = floor((x - low) / step + 1/2)
 // (so that |x - (low + code step)| <= step / 2).  A group that holds a NaN or an infinity gets a step and a lowest value of NaN.
 //
-// The rounding is decided exactly (for x - low in fp32): the product with the reciprocal, taken a little too large so that halves go up,
-// gives a candidate that is right or one too high, and its remainder says which.
+// The quotient is a product with the reciprocal, taken 2^-22 too large so that halves go up, added to 1.5 2^23, where the last bit is 1 and the
+// rounding to a whole number is the addition's.  (A quotient less than 2^-22 of itself below a half goes up as well.  Differences and
+// steps of a 16-bit type lie that close to a half only where x is 2^-13 and less of the range: one element in 10^8 of normal ones.)  The sums'
+// bits, shifted to their places, add up to the codes and a constant.
 //
-// Bound: HBM.  A thread takes one group, G = d / 32 neighbouring lanes a row; the codes' order inside a row needs words of all its groups side
-// by side, so that the lanes of a row exchange them.
+// Bound: HBM.  A thread takes one group, G = d / 32 neighbouring lanes a row.  16,381 tokens of eight heads, d 128, keys and values: see
+// tra_cache4_write_kernel.
 template <typename T>
 struct Group {
   uint32_t x[16];              // pairs of channels
-  float mul, neg_low, inv, s;  // t = x mul - low mul, of steps s; inv a little above 1 / s, or 0
+  float mul, neg_low, inv;     // t = x mul - low mul, of steps of 1 / inv; inv 0: every code is 0
   uint32_t packed;             // step, lowest value
 
   __device__ __forceinline__ void measure() {
-    using P = typename Pair<T>::type;
-    P lo = as_pair<T>(x[0]), hi = lo;
+    typename Pair<T>::type lo = as_pair<T>(x[0]), hi = lo;
 #pragma unroll
     for (int i = 1; i < 16; ++i) {
       lo = __hmin2_nan(lo, as_pair<T>(x[i]));
@@ -66,35 +219,35 @@ struct Group {
     // in halves, so that a range past fp32 stays one
     const float half_range = fmaf(h, 0.5f, -0.5f * l);
     uint32_t bits = pack_pair<T>(half_range * (1.f / 7.5f), l);         // step (low half), lowest value
-    float st, unused;
+    float st, below, unused;
     unpack_pair<T>(bits, st, unused);
+    unpack_pair<T>((bits & 0xffffu) - 1u, below, unused);
     // (the product is within two units of the quotient, far less than a step of the type: at most one up or down)
-    if (7.5f * st < half_range) {
+    if (7.5f * st < half_range)
       bits += 1u;
-    } else if (st > 0.f) {
-      float below, high;
-      unpack_pair<T>((bits & 0xffffu) - 1u, below, high);
-      if (7.5f * below >= half_range) bits -= 1u;
-    }
+    else if (st > 0.f && 7.5f * below >= half_range)
+      bits -= 1u;
     unpack_pair<T>(bits, st, unused);
     if (!finite) bits = std::is_same<T, __half>::value ? 0x7e007e00u : 0x7fc07fc0u;
+    packed = bits;
     // steps of 2^-60 and less (bf16 only) are brought up first, so that their reciprocal is a number
     mul = !std::is_same<T, __half>::value && st < 0x1p-60f ? 0x1p60f : 0.5f;
-    s = st * mul;
-    inv = finite && st > 0.f ? __frcp_rn(s) * (1.f + 0x1p-22f) : 0.f;
+    inv = finite && st > 0.f ? __frcp_rn(st * mul) * (1.f + 0x1p-22f) : 0.f;
+    neg_low = inv == 0.f ? 0.f : -l * mul;
     if (inv == 0.f) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = 0u;
     }
-    neg_low = inv == 0.f ? 0.f : -l * mul;
-    packed = bits;
   }
-  // code of one element, as a float
-  __device__ __forceinline__ float code(float v) const {
-    constexpr float kMagic = 12582912.f;                       // 1.5 2^23: the sum's last bit is 1
-    const float t = fmaf(v, mul, neg_low);
-    const float k = fmaf(t, inv, kMagic) - kMagic;
-    return fmaf(-k, s, t) < -0.5f * s ? k - 1.f : k;
+  static constexpr float kMagic = 12582912.f;        // 1.5 2^23
+  static constexpr uint32_t kMagicBits = 0x4b400000u;
+  // kMagicBits plus the codes of a pair
+  __device__ __forceinline__ void codes(uint32_t pair, uint32_t& a, uint32_t& b) const {
+    float v0, v1;
+    unpack_pair<T>(pair, v0, v1);
+    unpack2(ffma2(ffma2(pack2(v0, v1), pack2(mul, mul), pack2(neg_low, neg_low)), pack2(inv, inv), pack2(kMagic, kMagic)), v0, v1);
+    a = __float_as_uint(v0);
+    b = __float_as_uint(v1);
   }
 };
 
@@ -109,102 +262,45 @@ __global__ void __launch_bounds__(256) tra_cache4_write_kernel(const __grid_cons
     tra_set_status(a.status, TRA_ERR_INVALID_ARG);
     slot = -1;
   }
-  if (!__any_sync(0xffffffffu, slot >= 0)) return;
   Group<T> q;
   const long long* stride = of_v ? a.v_stride : a.k_stride;
-  const T* src = (const T*)(of_v ? a.v : a.k) + (slot < 0 ? 0 : i * stride[0] + head * stride[1] + j * kCacheGroup);
-  if (slot >= 0) {
+  const T* src = (const T*)(of_v ? a.v : a.k) + (i * stride[0] + head * stride[1] + j * kCacheGroup);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint4 w = *reinterpret_cast<const uint4*>(src + c * 8);
-      q.x[4 * c] = w.x, q.x[4 * c + 1] = w.y, q.x[4 * c + 2] = w.z, q.x[4 * c + 3] = w.w;
-    }
-  } else {
-#pragma unroll
-    for (int c = 0; c < 16; ++c) q.x[c] = 0u;
-  }
+  for (int c = 0; c < 16; ++c) q.x[c] = 0u;
+  if (slot >= 0) load64(src, a.wide, q.x);
   q.measure();
   uint32_t out[4];             // words 4 j .. 4 j + 3 of the row
-  // four codes, as one number, 4 bits each
-  auto four = [](float a, float b, float c, float d) -> uint32_t { return (uint32_t)(int)fmaf(d, 4096.f, fmaf(c, 256.f, fmaf(b, 16.f, a))); };
+  constexpr uint32_t kFour = Group<T>::kMagicBits * 0x1111u;       // what four of them in a half word leave besides the codes
   if (!of_v) {
     // word t of the group: channels 8 (n % 4) + 2 t + n / 4
-    uint32_t w[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      float lo[4], hi[4];
+      uint32_t lo = 0u - kFour, hi = 0u - kFour;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        float x0, x1;
-        unpack_pair<T>(q.x[4 * c + t], x0, x1);
-        lo[c] = q.code(x0);
-        hi[c] = q.code(x1);
+        uint32_t x0, x1;
+        q.codes(q.x[4 * c + t], x0, x1);
+        lo += x0 << (4 * c);
+        hi += x1 << (4 * c);
       }
-      w[t] = four(lo[0], lo[1], lo[2], lo[3]) | four(hi[0], hi[1], hi[2], hi[3]) << 16;
+      out[t] = __byte_perm(lo, hi, 0x5410);
     }
-    // word t of group j lies at G t + j: a transposition among the row's lanes
-    if constexpr (G == 4) {
-#pragma unroll
-      for (int b = 1; b < 4; b <<= 1) {
-        const bool up = (j & b) != 0;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          if (u & b) continue;
-          const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[u] : w[u | b], b);
-          if (up)
-            w[u] = got;
-          else
-            w[u | b] = got;
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) out[u] = w[u];
-    } else {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint32_t got = __shfl_xor_sync(0xffffffffu, j ? w[u] : w[u + 2], 1);
-        out[2 * u] = j ? got : w[u];
-        out[2 * u + 1] = j ? w[u + 2] : got;
-      }
-    }
+    key_words_to_row<G>(out, j);
   } else {
     // half a word for every g: channels 8 n + g of the group; the other half is the neighbouring group's
     uint32_t h[8];
 #pragma unroll
     for (int g = 0; g < 8; g += 2) {
-      float c0[4], c1[4];
+      h[g] = h[g + 1] = 0u - kFour;
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        float x0, x1;
-        unpack_pair<T>(q.x[4 * n + g / 2], x0, x1);
-        c0[n] = q.code(x0);
-        c1[n] = q.code(x1);
+        uint32_t x0, x1;
+        q.codes(q.x[4 * n + g / 2], x0, x1);
+        h[g] += x0 << (4 * n);
+        h[g + 1] += x1 << (4 * n);
       }
-      h[g] = four(c0[0], c0[1], c0[2], c0[3]);
-      h[g + 1] = four(c1[0], c1[1], c1[2], c1[3]);
     }
-    // lane pairs join halves: the even lane takes g = 0, 1, 4, 5 (d 64: 0 .. 3), the odd one the others
-    uint32_t w[4];
-    const bool odd = j & 1;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int mine = G == 4 ? (u & 1) + (u & 2) * 2 : u, other = G == 4 ? mine + 2 : u + 4;
-      const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? h[mine] : h[other], 1);
-      w[u] = odd ? got | h[other] << 16 : h[mine] | got << 16;
-    }
-    if constexpr (G == 4) {
-      // words 2 g + w: lanes 0, 1 hold w = 0 of g = (0, 1, 4, 5), (2, 3, 6, 7), lanes 2, 3 hold w = 1 of them
-      const bool up = j & 2;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[u] : w[u + 2], 2);
-        out[2 * u] = up ? got : w[u];
-        out[2 * u + 1] = up ? w[u + 2] : got;
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) out[u] = w[u];
-    }
+    value_halves_to_row<G>(h, out, j);
   }
   if (slot < 0) return;
   const long long row = (long long)head * a.tokens + slot;
@@ -224,30 +320,36 @@ __device__ __forceinline__ uint32_t value_pair(uint32_t codes, uint32_t step2, u
   return as_bits<T>(__hfma2(n, as_pair<T>(step2), as_pair<T>(low2)));
 }
 
-// Group j of a row: 32 channels, 16 pairs.
-template <typename T, int D>
-__device__ __forceinline__ void read_group(const uint8_t* codes, const void* steps, long long row, int j, bool of_v, uint32_t* out) {
-  constexpr int G = D / kCacheGroup;
-  const uint16_t* st = (const uint16_t*)steps + row * (2 * G);
-  const uint32_t step2 = st[j] * 0x10001u, low2 = st[G + j] * 0x10001u;
-  const uint32_t* w = (const uint32_t*)(codes + row * (D / 2));
-  if (!of_v) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const uint32_t x = w[G * t + j];
-#pragma unroll
-      for (int n = 0; n < 4; ++n) out[4 * n + t] = value_pair<T>((x >> (4 * n)) & 0x000f000fu, step2, low2);
-    }
-  } else {
-    const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-#pragma unroll
-    for (int g = 0; g < 8; g += 2) {
-      const uint32_t x = __byte_perm(w[(G / 2) * g + (j >> 1)], w[(G / 2) * (g + 1) + (j >> 1)], sel);
-#pragma unroll
-      for (int n = 0; n < 4; ++n) out[4 * n + g / 2] = value_pair<T>((x >> (4 * n)) & 0x000f000fu, step2, low2);
-    }
+// A lane's share of a row: codes 16 j .. of the row, and group j's step and lowest value.
+template <int D>
+struct RowShare {
+  uint32_t w[4], step, low;
+  __device__ __forceinline__ RowShare() : w{0u, 0u, 0u, 0u}, step(0u), low(0u) {}
+  __device__ __forceinline__ void load(const uint8_t* codes, const void* steps, long long row, int j) {
+    constexpr int G = D / kCacheGroup;
+    const uint4 v = *reinterpret_cast<const uint4*>(codes + row * (D / 2) + j * 16);
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    const uint16_t* st = (const uint16_t*)steps + row * (2 * G);
+    step = st[j], low = st[G + j];
   }
-}
+  // use(x, n, at): codes n (low half of x) and n + 4 (high half) are those of the pair of channels 2 at, 2 at + 1 of group j
+  template <typename Use>
+  __device__ __forceinline__ void each_pair(int j, bool of_v, Use use) {
+    constexpr int G = D / kCacheGroup;
+    uint32_t x[4];
+    if (of_v) {
+      row_to_value_pairs<G>(w, x, j);
+    } else {
+      row_to_key_words<G>(w, j);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) x[t] = w[t];
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) use(x[t], n, 4 * n + t);
+  }
+};
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256) tra_cache4_read_kernel(const __grid_constant__ Cache4Rows a) {
@@ -255,18 +357,19 @@ __global__ void __launch_bounds__(256) tra_cache4_read_kernel(const __grid_const
   const int j = threadIdx.x % G, head = blockIdx.y;
   const long long i = (long long)blockIdx.x * kRowsPerBlock + threadIdx.x / G;
   const bool of_v = blockIdx.z != 0;
-  const int slot = i < a.n ? a.slots[i] : -1;
-  if (slot < 0) return;
+  int slot = i < a.n ? a.slots[i] : -1;
   if (slot >= a.tokens) {
     tra_set_status(a.status, TRA_ERR_INVALID_ARG);
-    return;
+    slot = -1;
   }
+  RowShare<D> s;
+  if (slot >= 0) s.load(of_v ? a.v_codes : a.k_codes, of_v ? a.v_step : a.k_step, (long long)head * a.tokens + slot, j);
   uint32_t v[16];
-  read_group<T, D>(of_v ? a.v_codes : a.k_codes, of_v ? a.v_step : a.k_step, (long long)head * a.tokens + slot, j, of_v, v);
+  const uint32_t step2 = s.step * 0x10001u, low2 = s.low * 0x10001u;
+  s.each_pair(j, of_v, [&](uint32_t x, int n, int at) { v[at] = value_pair<T>((x >> (4 * n)) & 0x000f000fu, step2, low2); });
+  if (slot < 0) return;
   const long long* stride = of_v ? a.v_stride : a.k_stride;
-  T* dst = (T*)(of_v ? a.v : a.k) + i * stride[0] + head * stride[1] + j * kCacheGroup;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) reinterpret_cast<uint4*>(dst)[c] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+  store64((T*)(of_v ? a.v : a.k) + i * stride[0] + head * stride[1] + j * kCacheGroup, a.wide, v);
 }
 
 // ------------------------------------------------------------------------------------ many rows: the keys read back first
@@ -284,46 +387,6 @@ struct Cache4Expand {
   int stride;
 };
 
-// A group's values in two pieces.
-template <typename T, int D>
-__device__ __forceinline__ void read_group_pieces(const uint8_t* codes, const void* steps, long long row, int j, bool of_v, uint32_t* out, uint32_t* rest) {
-  constexpr int G = D / kCacheGroup;
-  const uint16_t* st = (const uint16_t*)steps + row * (2 * G);
-  float step, low, unused;
-  unpack_pair<T>(st[j], step, unused);
-  unpack_pair<T>(st[G + j], low, unused);
-  const uint32_t* w = (const uint32_t*)(codes + row * (D / 2));
-  // codes n and n + 4 of x (keys: of a word; values: of halves of two words)
-  auto two = [&](uint32_t x, int n, int at) {
-    // 2^23 + code is a float; that power of two is taken off again, exactly
-    const float a = __uint_as_float(0x4b000000u | ((x >> (4 * n)) & 15u)) - 8388608.f, b = __uint_as_float(0x4b000000u | ((x >> (4 * n + 16)) & 15u)) - 8388608.f;
-    const float y = fmaf(a, step, low), z = fmaf(b, step, low);
-    out[at] = pack_pair<T>(y, z);
-    if (std::is_same<T, __half>::value) {                    // (low + 15 step may pass the type's range by a step's rounding)
-      float p, q;
-      unpack_pair<T>(out[at], p, q);
-      if (fabsf(p) == INFINITY || fabsf(q) == INFINITY) out[at] = pack_pair<T>(fminf(fmaxf(y, -65504.f), 65504.f), fminf(fmaxf(z, -65504.f), 65504.f));
-    }
-    rest[at] = rest_pair<T>(y, z, out[at]);
-  };
-  if (!of_v) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const uint32_t x = w[G * t + j];
-#pragma unroll
-      for (int n = 0; n < 4; ++n) two(x, n, 4 * n + t);
-    }
-  } else {
-    const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-#pragma unroll
-    for (int g = 0; g < 8; g += 2) {
-      const uint32_t x = __byte_perm(w[(G / 2) * g + (j >> 1)], w[(G / 2) * (g + 1) + (j >> 1)], sel);
-#pragma unroll
-      for (int n = 0; n < 4; ++n) two(x, n, 4 * n + g / 2);
-    }
-  }
-}
-
 template <typename T, int D, int kOrder>
 __global__ void __launch_bounds__(256) tra_cache4_expand_kernel(const __grid_constant__ Cache4Expand e) {
   constexpr int G = D / kCacheGroup, kRowsPerBlock = 256 / G;
@@ -339,17 +402,29 @@ __global__ void __launch_bounds__(256) tra_cache4_expand_kernel(const __grid_con
     e.begin[seq] = seq * e.stride;
     e.end[seq] = seq * e.stride + len;
   }
-  if (v0 >= len) return;
+  RowShare<D> r;
   const int key = kOrder == kOrderWindow && v0 >= p.sink_rows ? v0 + axis.gap : v0;
+  if (v0 < len) r.load(of_v ? e.v_codes : e.k_codes, of_v ? e.v_step : e.k_step, (long long)head * p.total_k + k.begin + key, j);
   uint32_t v[16], rest[16];
-  read_group_pieces<T, D>(of_v ? e.v_codes : e.k_codes, of_v ? e.v_step : e.k_step, (long long)head * p.total_k + k.begin + key, j, of_v, v, rest);
+  float step, low, unused;
+  unpack_pair<T>(r.step, step, unused);
+  unpack_pair<T>(r.low, low, unused);
+  r.each_pair(j, of_v, [&](uint32_t x, int n, int at) {
+    // 2^23 + code is a float; that power of two is taken off again, exactly
+    const float a = __uint_as_float(0x4b000000u | ((x >> (4 * n)) & 15u)) - 8388608.f, b = __uint_as_float(0x4b000000u | ((x >> (4 * n + 16)) & 15u)) - 8388608.f;
+    const float y = fmaf(a, step, low), z = fmaf(b, step, low);
+    v[at] = pack_pair<T>(y, z);
+    if (std::is_same<T, __half>::value) {                    // (low + 15 step may pass the type's range by a step's rounding)
+      float f, g;
+      unpack_pair<T>(v[at], f, g);
+      if (fabsf(f) == INFINITY || fabsf(g) == INFINITY) v[at] = pack_pair<T>(fminf(fmaxf(y, -65504.f), 65504.f), fminf(fmaxf(z, -65504.f), 65504.f));
+    }
+    rest[at] = rest_pair<T>(y, z, v[at]);
+  });
+  if (v0 >= len) return;
   T* dst = (T*)(of_v ? e.v : e.k) + (((long long)seq * e.stride + v0) * 2 * p.kv_heads + head) * D + j * kCacheGroup;
-  T* dst_rest = dst + (long long)p.kv_heads * D;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    reinterpret_cast<uint4*>(dst)[c] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-    reinterpret_cast<uint4*>(dst_rest)[c] = make_uint4(rest[4 * c], rest[4 * c + 1], rest[4 * c + 2], rest[4 * c + 3]);
-  }
+  store64(dst, true, v);
+  store64(dst + (long long)p.kv_heads * D, true, rest);
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -448,7 +523,8 @@ int rows_io(const tra_packed_t* h, const tra_cache4_t* c, const void* k, const v
   int device = 0;
   if (cudaGetDevice(&device) != cudaSuccess) return TRA_ERR_CUDA;
   if (device != h->device) return TRA_ERR_INVALID_ARG;
-  Cache4Rows a = {k, v, {ks[0], ks[1]}, {vs[0], vs[1]}, (uint8_t*)c->k, (uint8_t*)c->v, c->k_step, c->v_step, slots, n, c->tokens, h->d_status};
+  const bool wide = !(((uintptr_t)k | (uintptr_t)v | (n > 1 ? (uintptr_t)(ks[0] | vs[0]) * 2 : 0) | (kv > 1 ? (uintptr_t)(ks[1] | vs[1]) * 2 : 0)) & 31);
+  Cache4Rows a = {k, v, {ks[0], ks[1]}, {vs[0], vs[1]}, (uint8_t*)c->k, (uint8_t*)c->v, c->k_step, c->v_step, slots, n, c->tokens, wide, h->d_status};
   cudaStream_t s = (cudaStream_t)stream;
   if (h->cfg.head_dim == 128)
     return h->cfg.dtype == TRA_BF16 ? launch_rows_io<__nv_bfloat16, 128>(a, kv, write, s) : launch_rows_io<__half, 128>(a, kv, write, s);
