@@ -373,11 +373,13 @@ __global__ void __launch_bounds__(256) tra_cache4_read_kernel(const __grid_const
 }
 
 // ------------------------------------------------------------------------------------ many rows: the keys read back first
-// Sequence s of a pass gets the rows s * stride .. of two 16-bit tensors [rows][2][kv_heads][d]: the keys of its axis (tra_key_axis), as
-// their ranges say, which the attention launch behind it reads as begin / end.  An element low + step n has up to 4 bits more than the type,
-// and more where low and step are of different sizes; rounded to the type alone, keys and values would each add as much error as
-// the rounding of the result (bf16, 97 queries over 65,500 keys: 3.8e-3 off, against 1.7e-3 for the result's rounding; with the pieces 2.4e-3).  So what
-// rounding took is kept as a second piece.
+// Sequence s of a pass gets the rows s * stride .. of two 16-bit tensors: the keys of its axis (tra_key_axis), as their ranges say, which the
+// attention launch behind it reads as begin / end.  An element low + step n has up to 4 bits more than the type, and more where low and
+// step are of different sizes; rounded to the type alone, keys and values would each add as much error as the rounding of the
+// result (bf16, 97 queries over 65,500 keys: 3.8e-3 off, against 1.7e-3 for the result's rounding alone).  So
+//   fp16: [rows][2][kv_heads][d], the rounded element and, as a second piece, what rounding took;
+//   bf16: [rows][kv_heads][d] in fp16, of multiples that keep the largest of a sequence and head below 2^15 (kv_top), beside Q in fp16 by multiples of
+//         its rows (q_mul): one product instead of two (four chunks, 40 / 8 heads, window 4,096: 385 us in pieces, 223 so).
 struct Cache4Expand {
   tra_packed_launch a;
   const uint8_t *k_codes, *v_codes;
@@ -385,7 +387,85 @@ struct Cache4Expand {
   void *k, *v;
   int32_t *begin, *end;
   int stride;
+  uint32_t* top;               // bf16: [K, V][n_seq][kv_heads], cleared
+  __half* q;                   //       [total_q][heads][d]
+  float* q_mul;                //       [total_q][heads]
+  int step_blocks;             //       blocks of a (sequence, head, side) that look at its steps
 };
+
+// A sequence's keys as the launches of a pass see them.
+struct ExpandRange {
+  tra_seq_range q, k;
+  int gap, len;
+  template <int kOrder>
+  __device__ __forceinline__ static ExpandRange of(const Cache4Expand& e, int seq) {
+    const tra_packed_launch& p = e.a;
+    ExpandRange r;
+    r.q = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
+    r.k = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
+    const tra_key_axis<kOrder> axis(p, r.k.len - r.q.len, r.k.len);
+    r.gap = axis.gap;
+    r.len = r.q.len > 0 ? min(axis.len, e.stride) : 0;
+    return r;
+  }
+  __device__ __forceinline__ long long key(const tra_packed_launch& p, int v) const { return (long long)k.begin + (v >= p.sink_rows ? v + gap : v); }
+};
+
+// bf16: the largest size of what a sequence's keys and values of a head may stand for (blocks z < 2 n_seq), from steps and lowest values
+// alone, and Q in fp16 (the other blocks: 256 / (d / 8) rows each, d / 8 threads a row).
+template <int D, int kOrder>
+__global__ void __launch_bounds__(256) tra_cache4_multiples_kernel(const __grid_constant__ Cache4Expand e) {
+  using T = __nv_bfloat16;
+  constexpr int G = D / kCacheGroup;
+  const tra_packed_launch& p = e.a;
+  allow_next_launch();
+  const int n_top = e.step_blocks * p.kv_heads * 2 * p.n_seq;
+  if ((int)blockIdx.x < n_top) {
+    const int block = blockIdx.x % e.step_blocks, rest = blockIdx.x / e.step_blocks, head = rest % p.kv_heads, side = rest / p.kv_heads;
+    const bool of_v = side & 1;
+    const ExpandRange r = ExpandRange::of<kOrder>(e, side >> 1);
+    float top = 0.f;
+    for (int v = block * 256 + threadIdx.x; v < r.len; v += e.step_blocks * 256) {
+      const uint32_t* w = (const uint32_t*)((const T*)(of_v ? e.v_step : e.k_step) + ((long long)head * p.total_k + r.key(p, v)) * (2 * G));
+#pragma unroll
+      for (int i = 0; i < G / 2; ++i) {
+        float s0, s1, l0, l1;
+        unpack_pair<T>(w[i], s0, s1);
+        unpack_pair<T>(w[G / 2 + i], l0, l1);
+        top = fmaxf(top, fmaxf(fmaf(15.f, s0, fabsf(l0)), fmaf(15.f, s1, fabsf(l1))));        // (NaN, of a group that is not finite, is left out)
+      }
+    }
+    top = fminf(top, 3e38f);
+    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+    if ((threadIdx.x & 31) == 0 && most) atomicMax(e.top + ((of_v ? p.n_seq : 0) + (side >> 1)) * p.kv_heads + head, most);
+    return;
+  }
+  constexpr int kLanes = D / 8;
+  const long long row = (long long)((int)blockIdx.x - n_top) * (256 / kLanes) + threadIdx.x / kLanes, rows = (long long)p.total_q * p.heads;
+  const int lane = threadIdx.x % kLanes;
+  uint4 x = make_uint4(0u, 0u, 0u, 0u);
+  if (row < rows) x = *reinterpret_cast<const uint4*>((const T*)p.q + row / p.heads * p.q_stride[0] + row % p.heads * p.q_stride[1] + lane * 8);
+  uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a, b;
+    unpack_pair<T>(w[i], a, b);
+    top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
+  }
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float mul = tra_fp16_mul(top);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a, b;
+    unpack_pair<T>(w[i], a, b);
+    w[i] = pack_pair<__half>(a * mul, b * mul);
+  }
+  if (row >= rows) return;
+  reinterpret_cast<uint4*>(e.q + row * D)[lane] = make_uint4(w[0], w[1], w[2], w[3]);
+  if (lane == 0) e.q_mul[row] = tra_inverse_pow2(mul);
+}
 
 template <typename T, int D, int kOrder>
 __global__ void __launch_bounds__(256) tra_cache4_expand_kernel(const __grid_constant__ Cache4Expand e) {
@@ -394,37 +474,40 @@ __global__ void __launch_bounds__(256) tra_cache4_expand_kernel(const __grid_con
   const int j = threadIdx.x % G, head = blockIdx.y, seq = blockIdx.z >> 1;
   const bool of_v = blockIdx.z & 1;
   const int v0 = blockIdx.x * kRowsPerBlock + threadIdx.x / G;
-  const tra_seq_range q = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
-  const tra_seq_range k = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
-  const tra_key_axis<kOrder> axis(p, k.len - q.len, k.len);
-  const int len = q.len > 0 ? min(axis.len, e.stride) : 0;
+  const ExpandRange range = ExpandRange::of<kOrder>(e, seq);
   if (head == 0 && blockIdx.z == 2 * seq && blockIdx.x == 0 && threadIdx.x == 0) {
     e.begin[seq] = seq * e.stride;
-    e.end[seq] = seq * e.stride + len;
+    e.end[seq] = seq * e.stride + range.len;
   }
   RowShare<D> r;
-  const int key = kOrder == kOrderWindow && v0 >= p.sink_rows ? v0 + axis.gap : v0;
-  if (v0 < len) r.load(of_v ? e.v_codes : e.k_codes, of_v ? e.v_step : e.k_step, (long long)head * p.total_k + k.begin + key, j);
+  if (v0 < range.len) r.load(of_v ? e.v_codes : e.k_codes, of_v ? e.v_step : e.k_step, (long long)head * p.total_k + range.key(p, v0), j);
   uint32_t v[16], rest[16];
   float step, low, unused;
   unpack_pair<T>(r.step, step, unused);
   unpack_pair<T>(r.low, low, unused);
+  constexpr bool kFp16 = std::is_same<T, __half>::value;
+  if constexpr (!kFp16) {
+    wait_last_launch();
+    const float mul = tra_fp16_mul(__uint_as_float(e.top[((of_v ? p.n_seq : 0) + seq) * p.kv_heads + head]));
+    step *= mul;
+    low *= mul;
+  }
   r.each_pair(j, of_v, [&](uint32_t x, int n, int at) {
     // 2^23 + code is a float; that power of two is taken off again, exactly
     const float a = __uint_as_float(0x4b000000u | ((x >> (4 * n)) & 15u)) - 8388608.f, b = __uint_as_float(0x4b000000u | ((x >> (4 * n + 16)) & 15u)) - 8388608.f;
     const float y = fmaf(a, step, low), z = fmaf(b, step, low);
-    v[at] = pack_pair<T>(y, z);
-    if (std::is_same<T, __half>::value) {                    // (low + 15 step may pass the type's range by a step's rounding)
+    v[at] = pack_pair<__half>(y, z);
+    if constexpr (kFp16) {                                   // (low + 15 step may pass the type's range by a step's rounding)
       float f, g;
       unpack_pair<T>(v[at], f, g);
       if (fabsf(f) == INFINITY || fabsf(g) == INFINITY) v[at] = pack_pair<T>(fminf(fmaxf(y, -65504.f), 65504.f), fminf(fmaxf(z, -65504.f), 65504.f));
+      rest[at] = rest_pair<T>(y, z, v[at]);
     }
-    rest[at] = rest_pair<T>(y, z, v[at]);
   });
-  if (v0 >= len) return;
-  T* dst = (T*)(of_v ? e.v : e.k) + (((long long)seq * e.stride + v0) * 2 * p.kv_heads + head) * D + j * kCacheGroup;
+  if (v0 >= range.len) return;
+  T* dst = (T*)(of_v ? e.v : e.k) + (((long long)seq * e.stride + v0) * (kFp16 ? 2 : 1) * p.kv_heads + head) * D + j * kCacheGroup;
   store64(dst, true, v);
-  store64(dst + (long long)p.kv_heads * D, true, rest);
+  if constexpr (kFp16) store64(dst + (long long)p.kv_heads * D, true, rest);
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -479,7 +562,7 @@ Choice4 choose4(const tra_packed_t* h, int n_seq, int max_q, int max_k) {
     c.clustered = !many && c.splits > 1 && c.splits <= kClusterMax;
   } else {
     c.stride = (tra_packed_longest_axis(h, max_k, max_q) + 7) / 8 * 8;
-    const size_t one = (size_t)c.stride * h->cfg.kv_heads * h->cfg.head_dim * 8;
+    const size_t one = (size_t)c.stride * h->cfg.kv_heads * h->cfg.head_dim * (h->cfg.dtype == TRA_BF16 ? 4 : 8);
     const size_t most = one ? kExpandBytes / one : n_seq;
     c.seqs = (int)(most < 1 ? 1 : most > (size_t)n_seq ? n_seq : most > 16384 ? 16384 : most);
     while ((long long)c.seqs * c.stride > (1 << 30)) --c.seqs;
@@ -489,11 +572,28 @@ Choice4 choose4(const tra_packed_t* h, int n_seq, int max_q, int max_k) {
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
+// The workspace of a call that reads keys back.
+struct Layout4 {
+  size_t v, ranges, top, q_mul, q, attn, bytes;
+};
+Layout4 layout4(const tra_packed_t* h, const Choice4& c, int total_q, int max_q) {
+  const bool bf16 = h->cfg.dtype == TRA_BF16;
+  const size_t d = h->cfg.head_dim, kv = h->cfg.kv_heads, heads = h->cfg.heads;
+  Layout4 l;
+  l.v = round256((size_t)c.seqs * c.stride * kv * d * (bf16 ? 2 : 4));
+  l.ranges = 2 * l.v;
+  l.top = l.ranges + round256(sizeof(int32_t) * 2 * (size_t)c.seqs);
+  l.q_mul = l.top + (bf16 ? round256(sizeof(uint32_t) * 2 * c.seqs * kv) : 0);
+  l.q = l.q_mul + (bf16 ? round256(sizeof(float) * total_q * heads) : 0);
+  l.attn = l.q + (bf16 ? round256((size_t)total_q * heads * d * 2) : 0);
+  l.bytes = l.attn + tra_packed_attn_workspace_bytes(h, c.seqs, total_q, max_q, c.stride);
+  return l;
+}
+
 size_t workspace4(const tra_packed_t* h, const Choice4& c, int n_seq, int total_q, int max_q) {
   if (max_q == 0) return 0;
   if (c.direct) return c.splits > 1 && !c.clustered ? sizeof(float) * (size_t)c.splits * total_q * h->cfg.heads * (h->cfg.head_dim + 2) : 0;
-  const size_t keys = round256((size_t)c.seqs * c.stride * h->cfg.kv_heads * h->cfg.head_dim * 4);
-  return 2 * keys + round256(sizeof(int32_t) * 2 * (size_t)c.seqs) + tra_packed_attn_workspace_bytes(h, c.seqs, total_q, max_q, c.stride);
+  return layout4(h, c, total_q, max_q).bytes;
 }
 
 template <typename T, int D>
@@ -531,13 +631,30 @@ int rows_io(const tra_packed_t* h, const tra_cache4_t* c, const void* k, const v
   return h->cfg.dtype == TRA_BF16 ? launch_rows_io<__nv_bfloat16, 64>(a, kv, write, s) : launch_rows_io<__half, 64>(a, kv, write, s);
 }
 
-template <typename T, int D>
-int launch_expand(const tra_packed_ctx& c, const Cache4Expand& e, int seqs) {
+template <typename T, int D, int kOrder>
+int launch_expand_order(const tra_packed_ctx& c, Cache4Expand e, bool first) {
   constexpr int kRows = 256 / (D / kCacheGroup);
+  const int seqs = e.a.n_seq;
+  const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
+  if constexpr (bf16) {
+    if (cudaMemsetAsync(e.top, 0, sizeof(uint32_t) * 2 * seqs * e.a.kv_heads, c.stream) != cudaSuccess) return TRA_ERR_CUDA;
+    // about eight rounds of 256 keys per block, and enough blocks where there are few heads
+    long long blocks = ((long long)e.stride + 2047) / 2048;
+    const long long fill = 4ll * c.h->sm_count / (2ll * seqs * e.a.kv_heads) + 1, most = ((long long)e.stride + 255) / 256;
+    if (blocks < fill) blocks = fill;
+    e.step_blocks = (int)(blocks > most ? (most < 1 ? 1 : most) : blocks);
+    const long long rows = first ? ((long long)e.a.total_q * e.a.heads + 256 / (D / 8) - 1) / (256 / (D / 8)) : 0;
+    const long long grid = (long long)e.step_blocks * e.a.kv_heads * 2 * seqs + rows;
+    if (grid > 0x7fffffffll) return TRA_ERR_UNSUPPORTED;
+    const int rc = tra_launch(tra_cache4_multiples_kernel<D, kOrder>, dim3((unsigned)grid), 256, 0, c.stream, false, 1, e);
+    if (rc != TRA_OK) return rc;
+  }
   const int blocks = e.stride > 0 ? (e.stride + kRows - 1) / kRows : 1;
-  const dim3 grid((unsigned)blocks, (unsigned)e.a.kv_heads, (unsigned)(2 * seqs));
-  return e.a.order == kOrderWindow ? tra_launch(tra_cache4_expand_kernel<T, D, kOrderWindow>, grid, 256, 0, c.stream, false, 1, e)
-                                   : tra_launch(tra_cache4_expand_kernel<T, D, kOrderCausal>, grid, 256, 0, c.stream, false, 1, e);
+  return tra_launch(tra_cache4_expand_kernel<T, D, kOrder>, dim3((unsigned)blocks, (unsigned)e.a.kv_heads, (unsigned)(2 * seqs)), 256, 0, c.stream, bf16, 1, e);
+}
+template <typename T, int D>
+int launch_expand(const tra_packed_ctx& c, const Cache4Expand& e, bool first) {
+  return e.a.order == kOrderWindow ? launch_expand_order<T, D, kOrderWindow>(c, e, first) : launch_expand_order<T, D, kOrderCausal>(c, e, first);
 }
 
 }  // namespace
@@ -590,30 +707,35 @@ extern "C" int tra_packed_attn_cache4(const tra_packed_t* h, const tra_packed_ar
     return rc != TRA_OK || !need ? rc : tra_packed_join(ctx, q.a);
   }
   // many rows: passes over sequences, keys read back into the workspace
+  const bool bf16 = h->cfg.dtype == TRA_BF16;
   const int kv = h->cfg.kv_heads, d = h->cfg.head_dim;
-  const size_t keys = round256((size_t)c.seqs * c.stride * kv * d * 4);
+  const Layout4 l = layout4(h, c, a.total_q, a.max_q);
+  uint8_t* ws = (uint8_t*)workspace;
   Cache4Expand e;
+  memset(&e, 0, sizeof(e));
   e.a = q.a;
+  if (e.a.order != kOrderWindow) e.a.sink_rows = 0;
   e.k_codes = (const uint8_t*)cache->k, e.v_codes = (const uint8_t*)cache->v, e.k_step = cache->k_step, e.v_step = cache->v_step;
-  e.k = workspace, e.v = (uint8_t*)workspace + keys;
-  e.begin = (int32_t*)((uint8_t*)workspace + 2 * keys), e.end = e.begin + c.seqs;
+  e.k = ws, e.v = ws + l.v;
+  e.begin = (int32_t*)(ws + l.ranges), e.end = e.begin + c.seqs;
+  e.top = (uint32_t*)(ws + l.top), e.q_mul = (float*)(ws + l.q_mul), e.q = (__half*)(ws + l.q);
   e.stride = c.stride;
-  uint8_t* rest = (uint8_t*)workspace + 2 * keys + round256(sizeof(int32_t) * 2 * (size_t)c.seqs);
   for (int s = 0; s < a.n_seq; s += c.seqs) {
     const int n = a.n_seq - s < c.seqs ? a.n_seq - s : c.seqs;
     e.a.cu_q = a.cu_q + s, e.a.k_begin = a.k_begin + s, e.a.k_end = a.k_end + s;
     e.a.n_seq = n;
-    if (h->cfg.dtype == TRA_BF16)
-      rc = d == 128 ? launch_expand<__nv_bfloat16, 128>(ctx, e, n) : launch_expand<__nv_bfloat16, 64>(ctx, e, n);
+    if (bf16)
+      rc = d == 128 ? launch_expand<__nv_bfloat16, 128>(ctx, e, s == 0) : launch_expand<__nv_bfloat16, 64>(ctx, e, s == 0);
     else
-      rc = d == 128 ? launch_expand<__half, 128>(ctx, e, n) : launch_expand<__half, 64>(ctx, e, n);
+      rc = d == 128 ? launch_expand<__half, 128>(ctx, e, s == 0) : launch_expand<__half, 64>(ctx, e, s == 0);
     if (rc != TRA_OK) return rc;
     tra_packed_args_t b = a;
     b.k = e.k, b.v = e.v;
-    b.k_stride[0] = b.v_stride[0] = (int64_t)2 * kv * d, b.k_stride[1] = b.v_stride[1] = d;
+    b.k_stride[0] = b.v_stride[0] = (int64_t)(bf16 ? 1 : 2) * kv * d, b.k_stride[1] = b.v_stride[1] = d;
+    if (bf16) b.q = e.q, b.q_stride[0] = (int64_t)q.a.heads * d, b.q_stride[1] = d;
     b.cu_q = a.cu_q + s, b.k_begin = e.begin, b.k_end = e.end;
     b.n_seq = n, b.total_k = c.seqs * c.stride, b.max_k = c.stride;
-    rc = tra_packed_attn_pieces(h, &b, rest, workspace_bytes - (size_t)(rest - (uint8_t*)workspace), stream_);
+    rc = tra_packed_attn_read_back(h, &b, e.q_mul, e.top, ws + l.attn, workspace_bytes - l.attn, stream_);
     if (rc != TRA_OK) return rc;
   }
   return TRA_OK;

@@ -25,7 +25,9 @@ int tra_cache4_rows(const tra_packed_ctx& c, const tra_cache4_launch& a, int chu
 int tra_packed_join(const tra_packed_ctx& c, const tra_packed_launch& p);
 // Checks what every attention call shares and fills the launch; a->k and a->v are looked at when `keys`.
 int tra_packed_begin(const tra_packed_t* h, const tra_packed_args_t* a, bool keys, tra_packed_launch* p);
-// tra_packed_attn over K and V of twice the heads: rounded elements, then what rounding took from them.  At more than 16 rows per key/value head.
-int tra_packed_attn_pieces(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes, void* stream);
+// tra_packed_attn over keys and values that were read back, at more than 16 rows per key/value head (see FwdCfg).  fp16 tensors: K and V of twice
+// the heads, rounded elements, then what rounding took from them.  bf16: Q, K and V are fp16, with their multiples' q_mul and kv_top.
+int tra_packed_attn_read_back(const tra_packed_t* h, const tra_packed_args_t* a, const float* q_mul, const uint32_t* kv_top, void* workspace,
+                              size_t workspace_bytes, void* stream);
 // Keys that `tokens` queries walk at most.
 int tra_packed_longest_axis(const tra_packed_t* h, int max_k, int tokens);

@@ -192,7 +192,7 @@ bool bad_sizes(const tra_packed* h, int n_seq, int total_q, int max_q, int max_k
 
 // [tokens, heads, d] behind strides, viewed with the channels innermost; box = 64 channels x box_heads x box_tokens.
 int make_packed_map(CUtensorMap* map, const tra_packed* h, const void* base, const int64_t* stride, int heads, long long tokens,
-                    int box_heads, int box_tokens) {
+                    int box_heads, int box_tokens, bool fp16 = false) {
   encode_tiled_fn enc = get_encode_tiled();
   if (!enc) return TRA_ERR_CUDA;
   cuuint64_t dims[3] = {(cuuint64_t)h->cfg.head_dim, (cuuint64_t)heads, (cuuint64_t)tokens};
@@ -200,7 +200,7 @@ int make_packed_map(CUtensorMap* map, const tra_packed* h, const void* base, con
   cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)stride[1] * 2 : 128u, tokens > 1 ? (cuuint64_t)stride[0] * 2 : 128u};
   cuuint32_t box[3] = {64u, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
   cuuint32_t estr[3] = {1u, 1u, 1u};
-  const CUresult r = enc(map, h->cfg.dtype == TRA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+  const CUresult r = enc(map, h->cfg.dtype == TRA_BF16 && !fp16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
                          const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? TRA_OK : TRA_ERR_CUDA;
@@ -257,15 +257,16 @@ int begin_launch(const tra_packed* h, const tra_packed_args_t* a, tra_packed_lau
 int make_key_maps(tra_packed_launch* p, const tra_packed* h, const void* k, const int64_t* ks, const void* v, const int64_t* vs, long long tokens,
                   int rows, int pieces = 1) {
   int rc;
-  const int heads = p->kv_heads * pieces;
-  if ((rc = make_packed_map(&p->map_k, h, k, ks, heads, tokens, 1, rows)) != TRA_OK) return rc;
-  if ((rc = make_packed_map(&p->map_v, h, v, vs, heads, tokens, 1, rows)) != TRA_OK) return rc;
+  const int heads = p->kv_heads * (pieces == 2 ? 2 : 1);
+  const bool fp16 = pieces == 0;
+  if ((rc = make_packed_map(&p->map_k, h, k, ks, heads, tokens, 1, rows, fp16)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p->map_v, h, v, vs, heads, tokens, 1, rows, fp16)) != TRA_OK) return rc;
   const int first = p->order == kOrderWindow ? p->sink_rows % rows : 0;
   if (first == 0) return TRA_OK;
-  if ((rc = make_packed_map(&p->map_k_first, h, k, ks, heads, tokens, 1, first)) != TRA_OK) return rc;
-  if ((rc = make_packed_map(&p->map_v_first, h, v, vs, heads, tokens, 1, first)) != TRA_OK) return rc;
-  if ((rc = make_packed_map(&p->map_k_rest, h, k, ks, heads, tokens, 1, rows - first)) != TRA_OK) return rc;
-  return make_packed_map(&p->map_v_rest, h, v, vs, heads, tokens, 1, rows - first);
+  if ((rc = make_packed_map(&p->map_k_first, h, k, ks, heads, tokens, 1, first, fp16)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p->map_v_first, h, v, vs, heads, tokens, 1, first, fp16)) != TRA_OK) return rc;
+  if ((rc = make_packed_map(&p->map_k_rest, h, k, ks, heads, tokens, 1, rows - first, fp16)) != TRA_OK) return rc;
+  return make_packed_map(&p->map_v_rest, h, v, vs, heads, tokens, 1, rows - first, fp16);
 }
 
 template <typename T, int D>
@@ -337,7 +338,8 @@ extern "C" size_t tra_packed_attn_workspace_bytes(const tra_packed_t* h, int n_s
   return workspace_of(h, choose(h, n_seq, total_q, max_q, max_k), total_q);
 }
 
-static int attend(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes, void* stream_, int pieces) {
+static int attend(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes, void* stream_, int pieces,
+                  const float* q_mul = nullptr, const uint32_t* kv_top = nullptr) {
   tra_packed_launch p;
   int rc = begin_launch(h, a, &p);
   if (rc != TRA_OK) return rc;
@@ -365,11 +367,15 @@ static int attend(const tra_packed_t* h, const tra_packed_args_t* a, void* works
   if (c.rows) {
     rc = tra_packed_rows(ctx, p, c.chunk, c.clustered);
   } else {
-    if ((rc = make_packed_map(&p.map_q, h, a->q, a->q_stride, p.heads, a->total_q, p.group, p.tile_tokens)) != TRA_OK) return rc;
+    if ((rc = make_packed_map(&p.map_q, h, a->q, a->q_stride, p.heads, a->total_q, p.group, p.tile_tokens, pieces == 0)) != TRA_OK) return rc;
     p.n_units = (a->max_q <= 2 * p.tile_tokens ? 0 : a->total_q / (2 * p.tile_tokens)) + a->n_seq;
-    if (pieces == 2) {
+    if (pieces != 1) {
       if (p.order != kOrderWindow) p.window = 1 << 30, p.sinks = p.sink_rows = 0;
-      rc = h->cfg.head_dim == 128 ? tra_packed_fwd_pieces_d128(ctx, p) : tra_packed_fwd_pieces_d64(ctx, p);
+      p.q_mul = q_mul, p.kv_top = kv_top;
+      if (pieces == 2)
+        rc = h->cfg.head_dim == 128 ? tra_packed_fwd_pieces_d128(ctx, p) : tra_packed_fwd_pieces_d64(ctx, p);
+      else
+        rc = h->cfg.head_dim == 128 ? tra_packed_fwd_fp16_d128(ctx, p) : tra_packed_fwd_fp16_d64(ctx, p);
     } else if (p.order == kOrderWindow)
       rc = h->cfg.head_dim == 128 ? tra_packed_fwd_window_d128(ctx, p) : tra_packed_fwd_window_d64(ctx, p);
     else
@@ -382,8 +388,9 @@ static int attend(const tra_packed_t* h, const tra_packed_args_t* a, void* works
 extern "C" int tra_packed_attn(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes, void* stream) {
   return attend(h, a, workspace, workspace_bytes, stream, 1);
 }
-int tra_packed_attn_pieces(const tra_packed_t* h, const tra_packed_args_t* a, void* workspace, size_t workspace_bytes, void* stream) {
-  return attend(h, a, workspace, workspace_bytes, stream, 2);
+int tra_packed_attn_read_back(const tra_packed_t* h, const tra_packed_args_t* a, const float* q_mul, const uint32_t* kv_top, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  return attend(h, a, workspace, workspace_bytes, stream, h->cfg.dtype == TRA_BF16 ? 0 : 2, q_mul, kv_top);
 }
 
 namespace {

@@ -39,6 +39,9 @@ struct tra_packed_launch {
   int window, sinks, sink_rows;              // kOrderWindow; sink_rows: sinks rounded up to whole 8-row pieces of a tile
   int sink_steps, sink_slots;                // backward: see tra_find_sink_unit; 0: the first keys' tiles walk all their queries
   float* sink_part;                          //   [slot][kv_heads][sinks][dK, dV][d] fp32
+  // fp16 products for bf16 tensors (kPieces = 0 of the forward kernel): Q, K and V are fp16 multiples of the elements
+  const float* q_mul;                        // [total_q][heads]: Q's elements are these times what the map reads
+  const uint32_t* kv_top;                    // [K, V][n_seq][kv_heads]: bits of the largest size, of which the multiple follows
   float sm_scale;
   int* status;
 };
@@ -60,12 +63,21 @@ int tra_packed_fwd_window_d128(const tra_packed_ctx& c, const tra_packed_launch&
 int tra_packed_fwd_window_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_fwd_pieces_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_fwd_pieces_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_fwd_fp16_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_fwd_fp16_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_window_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_window_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered);
 
 #ifdef __CUDACC__
 namespace {
+
+// The power of two that brings numbers of up to `top` below 2^15, where fp16 holds the most of them.
+__device__ __forceinline__ float tra_fp16_mul(float top) {
+  const int e = min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 127);        // top < 2^e
+  return __uint_as_float((uint32_t)(127 + 15 - e) << 23);
+}
+__device__ __forceinline__ float tra_inverse_pow2(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
 
 // Launch; after_last: may start while the stream's last kernel ends (see wait_last_launch); cluster: blocks along z that form
 // a thread-block cluster.

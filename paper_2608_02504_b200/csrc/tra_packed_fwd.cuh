@@ -38,11 +38,14 @@ constexpr int kAskAhead = 1;             // key blocks a unit's producer has lef
 
 // kPieces: numbers of the 16-bit type that a key's or a value's element is the sum of; 2: a cache of 4 bits, whose elements have
 // more bits than the type, read back as the rounded element and what rounding took from it (heads kv_heads .. of K and V), with
-// two products where there was one.
+// two products where there was one.  0: such a cache of bf16, read back as fp16 multiples, whose 11 bits the bf16 result does not
+// tell from the exact elements (K and V by a power of two per sequence and head, Q by one per row): products and probabilities in fp16, the
+// powers of two go to the scores' scale and to the sum that divides O.
 template <int D, int kPieces>
 struct FwdCfg {
+  static constexpr int kTiles = kPieces == 2 ? 2 : 1;      // of a block of keys, and of its values
   static constexpr int kTileBytes = kTileM * D * 2;
-  static constexpr int kSlots = D == 128 ? 5 : kPieces == 1 ? 6 : 10;
+  static constexpr int kSlots = D == 128 ? 5 : kTiles == 1 ? 6 : 10;
   static constexpr int kAtoms = D / 64;
   static constexpr int kAtomBytes = kTileM * 128;
   static constexpr int kSmemData = (2 + kSlots) * kTileBytes;
@@ -90,8 +93,8 @@ struct FwdPlan {
     const int q_len = w.unit.q.len, k_len = w.unit.k.len;
     tok0 = w.unit.index * 2 * p.tile_tokens;
     const int ahead = k_len - q_len;                      // causal: token i sees keys 0 .. i + ahead
-    // (two pieces: this order alone is compiled, with a window without end where there is none; not causal: every query sits at the end)
-    const bool all = kPieces == 2 && p.order == kOrderNone;
+    // (but for 1 this order alone is compiled, with a window without end where there is none; not causal: every query sits at the end)
+    const bool all = kPieces != 1 && p.order == kOrderNone;
     const tra_key_axis<kOrder> axis(p, all ? k_len - 1 : tok0 + ahead, k_len);
     gap = axis.gap;
     int blocks[2];
@@ -114,7 +117,7 @@ struct FwdPlan {
 };
 
 // Stores a tile's rows of a finished unit, or their part of a split launch, and hands the sum's tensor memory back.
-template <typename T, int D, bool kExact>
+template <typename T, int D, bool kExact, int kPieces>
 __device__ __forceinline__ void store_unit(const tra_packed_launch& p, FwdCtl* ctl, int slot, int k, uint32_t t_o, bool any, float m, float l,
                                         float l_exact) {
   const FwdWork& w = ctl->work[slot];
@@ -124,7 +127,8 @@ __device__ __forceinline__ void store_unit(const tra_packed_launch& p, FwdCtl* c
   const long long tok_g = w.unit.q.begin + (row_valid ? tok : 0);
   const int head = w.kvh * p.group + r % p.group;
   const long long row_g = tok_g * p.heads + head;
-  const float inv_l = l > 0.f ? 1.f / l : 0.f;
+  float inv_l = l > 0.f ? 1.f / l : 0.f;
+  if constexpr (kPieces == 0) inv_l *= tra_inverse_pow2(tra_fp16_mul(__uint_as_float(p.kv_top[(p.n_seq + w.unit.seq) * p.kv_heads + w.kvh])));
   const bool seen = any && l != 0.f;
   const bool parts = p.splits > 1;
   const long long part_row = (long long)w.split * p.total_q * p.heads + row_g;
@@ -179,6 +183,8 @@ __device__ __forceinline__ void store_unit(const tra_packed_launch& p, FwdCtl* c
 template <typename T, int D, int kOrder, bool kExact, int kPieces>
 __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __grid_constant__ tra_packed_launch p) {
   using C = FwdCfg<D, kPieces>;
+  using TOut = typename std::conditional<kPieces == 0, __nv_bfloat16, T>::type;
+  constexpr int kTiles = C::kTiles;
   constexpr bool kCausal = kOrder != kOrderNone;
   extern __shared__ __align__(1024) uint8_t smem[];         // the swizzled tiles start on 1024-byte boundaries
   uint8_t* sQ = smem;
@@ -305,9 +311,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
           // per unit: the first frees K0, event e + 1 frees V_e and K_(e+1).  Event r arrives on kv_release[r % 8].
           for (int e = 0; e < u.n_entries && alive; ++e) {
             if (e + kAskAhead + 1 == u.n_entries) mbar_arrive(smem_u32(&ctl->want));
-            for (int kv = 0; kv < 2 * kPieces && alive; ++kv) {
-              const bool of_v = kv >= kPieces;
-              const int piece = of_v ? kv - kPieces : kv;
+            for (int kv = 0; kv < 2 * kTiles && alive; ++kv) {
+              const bool of_v = kv >= kTiles;
+              const int piece = of_v ? kv - kTiles : kv;
               if (n_load >= C::kSlots) {
                 const int r = ctl->freed_by[slot];
                 if (!(alive = mbar_wait(smem_u32(&ctl->kv_release[r & 7]), (uint32_t)(r >> 3) & 1u, abort_flag, p.status))) break;
@@ -321,7 +327,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
                 mbar_arrive(bar);
                 ctl->tail_slot[tails & 1][piece] = slot;
                 bar = smem_u32(&ctl->tail_full[tails & 1]);
-                if (piece == 0) mbar_expect_tx(bar, kPieces * C::kTileBytes);
+                if (piece == 0) mbar_expect_tx(bar, kTiles * C::kTileBytes);
               } else {
                 mbar_expect_tx(bar, C::kTileBytes);
               }
@@ -348,7 +354,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         if (!u.tail) continue;
         if (!mbar_wait_warp(smem_u32(&ctl->tail_full[tails & 1]), (uint32_t)(tails >> 1) & 1u, abort_flag, p.status)) break;
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i)
+        for (int i = 0; i < kTiles; ++i)
           zero_tile_rows(sKV + *(volatile int*)&ctl->tail_slot[tails & 1][i] * C::kTileBytes,
                          w.unit.k.len - u.gap - (u.v_begin + u.n_entries - 1) * kKeyTile, kKeyTile, C::kAtoms, C::kAtomBytes, lane, 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -371,7 +377,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         const uint32_t qa = k ? q_lo1 : q_lo0;
         const uint32_t d = tmem + k * 128;
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
+        for (int i = 0; i < kTiles; ++i) {
           const uint32_t ka = k_lo0 + (uint32_t)kslot[i] * (C::kTileBytes >> 4);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
@@ -388,7 +394,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
           if (!wait(smem_u32(&ctl->p_ready[k][half]), parity)) return false;
           tc_fence_after();
 #pragma unroll
-          for (int i = 0; i < kPieces; ++i) {
+          for (int i = 0; i < kTiles; ++i) {
             const uint32_t va = v_lo0 + (uint32_t)vslot[i] * (C::kTileBytes >> 4);
 #pragma unroll
             for (int kk = half * 4; kk < half * 4 + 4; ++kk)
@@ -408,7 +414,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
       // the next tile's slots, once it is there
       auto take = [&](int* slots) -> bool {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
+        for (int i = 0; i < kTiles; ++i) {
           slots[i] = slot;
           if (!wait(smem_u32(&ctl->kv_full[slot]), phase)) return false;
           advance();
@@ -428,7 +434,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         u.n_own[1] = uniform(u.n_own[1]);
         u.tail = uniform(u.tail);
         if (u.n_entries == 0) continue;
-        int kslot[kPieces], vslot[kPieces];
+        int kslot[kTiles], vslot[kTiles];
         alive = wait(smem_u32(&ctl->q_full), units & 1u) && take(kslot);        // first K tile
         if (!alive) break;
         tc_fence_after();
@@ -487,6 +493,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
     bool alive = true;
     for (int it = 0; alive && next_work(it); ++it) {
       float m = -INFINITY, l = 0.f, l_exact = 0.f;
+      float row_mul = 1.f;                    // kPieces 0: of the row's scores
       int n, col_limit, first_cols = 0;       // first_cols: columns in front of it are seen whatever the window
       bool rows_here;
       {
@@ -502,9 +509,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         // columns of the first block that the row sees; rows that hold no query follow the tile's last one, so that they
         // force no mask on their warp
         const int mask_tok = min(tile_tok + r / p.group, min(tile_tok + p.tile_tokens, w.unit.q.len) - 1);
-        col_limit = (kCausal && !(kPieces == 2 && p.order == kOrderNone) ? min(max(mask_tok + 1 + w.unit.k.len - w.unit.q.len - u.gap, 0), w.unit.k.len)
+        col_limit = (kCausal && !(kPieces != 1 && p.order == kOrderNone) ? min(max(mask_tok + 1 + w.unit.k.len - w.unit.q.len - u.gap, 0), w.unit.k.len)
                                                                          : w.unit.k.len) - u.v_begin * kKeyTile;
         if (kOrder == kOrderWindow) first_cols = p.sinks - u.v_begin * kKeyTile;
+        if constexpr (kPieces == 0) {
+          const int at = w.unit.seq * p.kv_heads + w.kvh, row = min(tile_tok + r / p.group, w.unit.q.len - 1);
+          row_mul = tra_inverse_pow2(tra_fp16_mul(__uint_as_float(p.kv_top[at]))) *
+                    p.q_mul[(long long)(w.unit.q.begin + row) * p.heads + w.kvh * p.group + r % p.group];
+        }
       }
       if (!rows_here) {
         // a warp without a row keeps up with the barriers; what its lanes multiply stays in its own, unstored rows
@@ -518,7 +530,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
           __syncwarp();
         }
       } else {
-        const float scale_log2 = p.sm_scale * kLog2e;
+        const float scale_log2 = kPieces == 0 ? p.sm_scale * kLog2e * row_mul : p.sm_scale * kLog2e;
         for (int e = 0; e < n; ++e, col_limit -= kKeyTile) {
           if (!mbar_wait_warp(smem_u32(&ctl->s_full[k]), entries & 1u, abort_flag, p.status)) {
             alive = false;
@@ -626,7 +638,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
         tc_fence_after();
       }
       if (!alive) break;
-      store_unit<T, D, kExact>(p, ctl, it & 1, k, t_o, n > 0, m, l, l_exact);
+      store_unit<TOut, D, kExact, kPieces>(p, ctl, it & 1, k, t_o, n > 0, m, l, l_exact);
       done_with_work(it);
     }
   }
@@ -660,7 +672,7 @@ int launch_fwd_order(const tra_packed_ctx& c, const tra_packed_launch& a) {
   return a.lse ? launch_fwd<T, D, kOrder, true, kPieces>(c, a) : launch_fwd<T, D, kOrder, false, kPieces>(c, a);
 }
 
-// The two orders without a window, the one with, and keys and values in two pieces (translation units of their own).
+// The two orders without a window, the one with, keys and values in two pieces, and fp16 products for bf16 (translation units of their own).
 template <int D>
 int launch_fwd_shape(const tra_packed_ctx& c, const tra_packed_launch& a) {
   if (c.h->cfg.dtype == TRA_BF16)
@@ -673,7 +685,12 @@ int launch_fwd_window(const tra_packed_ctx& c, const tra_packed_launch& a) {
 }
 template <int D>
 int launch_fwd_pieces(const tra_packed_ctx& c, const tra_packed_launch& a) {
-  return c.h->cfg.dtype == TRA_BF16 ? launch_fwd_order<__nv_bfloat16, D, kOrderWindow, 2>(c, a) : launch_fwd_order<__half, D, kOrderWindow, 2>(c, a);
+  return launch_fwd_order<__half, D, kOrderWindow, 2>(c, a);
+}
+
+template <int D>
+int launch_fwd_fp16(const tra_packed_ctx& c, const tra_packed_launch& a) {
+  return launch_fwd_order<__half, D, kOrderWindow, 0>(c, a);
 }
 
 }  // namespace

@@ -10,8 +10,9 @@ h = 2^-11 of fp16, in which the products over codes run:
   - fp16 numbers below 2^-14: steps and lowest values are off by 2^-24 of the largest of them, top = max (|low|, 16 step) times 2; probabilities, held
     times 2^6 and at most 2^8 above the reference, by 2^-25 in sums that are at least 2^-2: 2^-22 top per key;
   - sums over n keys: n + 16 units 2^-23 of sum p (|low| + 15 step).
-Calls of more than 64 rows per key/value head (`pieces`) take keys and values as two numbers of the type each, off by u^2 of an element, and
-round probabilities to the type as the other kernels do: u sum p |v - o|, and in fp16 2^-25 per key of the largest value.
+Calls of more than 64 rows per key/value head (`pieces`) round probabilities to fp16, h sum p |v - o|, and 2^-25 per key of the largest value
+below 2^-14; keys and values are in fp16 two numbers each, off by h^2 of an element, in bf16 one number of fp16, off by h of an element and by
+2^-39 of the largest (multiples below 2^15, subnormal steps of 2^-24); probabilities are then up to 2^8, so that 2^-25 is 2^-33 of what they may be.
 lse: as in packed_reference.py."""
 import math
 
@@ -78,12 +79,13 @@ def attention(q, k, v, cu_q, k_begin, k_end, window, sinks, scale, pieces=False,
             tol = u * o.abs() * (1 + 2 * u) + h * o.abs() + (2 * h + e)[..., None] * size * (1 + 4 * h) + e[..., None] * o.abs() \
                 + (m + 16) * UNIT * size + (2.0 ** -23 + m * 2.0 ** -22) * top * (p.sum(-1, keepdim=True) > 0) + tiny
             if pieces:
-                e = e + scale * Q.norm(dim=-1) * K.norm(dim=-1).max() * 2 * u * u
+                off = 2 * h * h if q.dtype == torch.float16 else h
+                e = e + scale * Q.norm(dim=-1) * (K.norm(dim=-1).max() * off + 2.0 ** -39 * d ** 0.5 * sizes(k[k0:k1, i])[1])
                 absv = p @ V.abs()
-                tol = u * o.abs() * (1 + 2 * u) + (u + e)[..., None] * (absv + o.abs()) * (1 + 4 * u) + 2 * u * u * absv + (m + 16) * UNIT * absv + tiny
-                if q.dtype == torch.float16:
-                    tol = tol + m * 2.0 ** -25 * V.abs().max()
+                tol = u * o.abs() * (1 + 2 * u) + (h + e)[..., None] * (absv + o.abs()) * (1 + 4 * h) + off * absv + (m + 16) * UNIT * absv + tiny \
+                    + (m * 2.0 ** -25 * V.abs().max() + 2.0 ** -39 * top) * (p.sum(-1, keepdim=True) > 0)
             r["o"][rows, heads], r["o_tol"][rows, heads] = o.transpose(0, 1), tol.transpose(0, 1)
+            # (the exponent's error, as above)
             lse_tol = e + (m + 64) * UNIT / 2 + lse.abs().nan_to_num(posinf=0) * UNIT
             r["lse"][rows, heads] = lse.transpose(0, 1)
             r["lse_tol"][rows, heads] = torch.where(none, torch.zeros_like(lse), lse_tol).transpose(0, 1)

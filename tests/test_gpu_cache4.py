@@ -229,17 +229,18 @@ def test_extreme_scores(api):
 
 @pytest.mark.parametrize("k_size,v_size", [(1e-6, 1e-5), (30.0, 1e4), (1e-3, 3e-2)])
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (HALF, 64)])
-def test_sizes_of_keys_and_values(api, dtype, d, k_size, v_size):
+@pytest.mark.parametrize("nq", [1, 70])
+def test_sizes_of_keys_and_values(api, dtype, d, k_size, v_size, nq):
     """Values far from 1, and rows of very different sizes in one cache: what is small is off by 2^-22 of what is large, per key."""
     n, hq, hk = 600, 4, 2
-    q = randn((1, hq, d), dtype, 1)
+    q = randn((nq, hq, d), dtype, 1) * torch.exp2(-torch.arange(nq, device="cuda") % 9).to(dtype)[:, None, None]
     k, v = randn((n, hk, d), dtype, 2, k_size), randn((n, hk, d), dtype, 3, v_size)
     v[300:] *= 2.0 ** -6
     attn = api.PackedAttn(hq, hk, d, dtype=dtype)
     cache = api.Cache4(attn, n)
     cache.write(k, v, torch.arange(n, dtype=torch.int32, device="cuda"))
-    o, lse = attn.forward_cache4(q, cache, i32([0, 1]), k_range=(i32([0]), i32([n])), max_q=1, max_k=n, want_lse=True)
-    want = attention(q, k, v, [0, 1], [0], [n], 0, 0, d ** -0.5)
+    o, lse = attn.forward_cache4(q, cache, i32([0, nq]), k_range=(i32([0]), i32([n])), max_q=nq, max_k=n, want_lse=True)
+    want = attention(q, k, v, [0, nq], [0], [n], 0, 0, d ** -0.5, nq > 32)
     check(lse, want["lse"], want["lse_tol"], "lse")
     check(o, want["o"], want["o_tol"], "o")
 
@@ -263,6 +264,27 @@ def test_nan_reaches_the_rows_that_see_it(api):
     q[0, 0, 3] = float("nan")
     o, lse = attn.forward_cache4(q, cache, i32([0, 1]), k_range=(i32([101]), i32([n])), max_q=1, max_k=n, want_lse=True)
     assert o[0, 0].isnan().all() and lse[0, 0].isnan() and o[0, 1].isfinite().all()
+
+
+def test_nan_in_chunks(api):
+    """More rows than the kernel for few takes: a NaN reaches the rows that see it, and nobody where no range holds it."""
+    d, n, nq = 64, 300, 100
+    for dtype in (BF, HALF):
+        attn = api.PackedAttn(2, 1, d, dtype=dtype)
+        cache = api.Cache4(attn, n)
+        k, v = randn((n, 1, d), dtype, 1), randn((n, 1, d), dtype, 2)
+        good = attn.forward_cache4
+        k[250, 0, 0] = float("nan")
+        cache.write(k, v, torch.arange(n, dtype=torch.int32, device="cuda"))
+        q = randn((nq, 2, d), dtype, 3)
+        o, lse = good(q, cache, i32([0, nq]), k_range=(i32([0]), i32([n])), max_q=nq, max_k=n, want_lse=True)
+        first = 250 - (n - nq)                                # the first query that sees key 250
+        assert o[first:].isnan().all() and lse[first:].isnan().all() and o[:first].isfinite().all()
+        o, lse = good(q, cache, i32([0, nq]), k_range=(i32([0]), i32([250])), max_q=nq, max_k=n, want_lse=True)
+        assert o.isfinite().all() and lse.isfinite().all()
+        q[5, 1, 3] = float("nan")
+        o, lse = good(q, cache, i32([0, nq]), k_range=(i32([0]), i32([250])), max_q=nq, max_k=n, want_lse=True)
+        assert o[5, 1].isnan().all() and o[5, 0].isfinite().all() and o[6:].isfinite().all()
 
 
 def test_offsets_past_32_bits(api):
