@@ -139,7 +139,7 @@ def _load():
     lib.tra_packed_attn_backward_workspace_bytes.restype = ctypes.c_size_t
     lib.tra_packed_attn_backward.argtypes = [vp, vp, vp, vp, ctypes.c_size_t, vp]
     for name in ("tra_cache4_write", "tra_cache4_read"):
-        getattr(lib, name).argtypes = [vp, vp, vp, vp, ctypes.c_int64 * 2, ctypes.c_int64 * 2, vp, i32, vp]
+        getattr(lib, name).argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp]
     lib.tra_packed_attn_cache4_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
     lib.tra_packed_attn_cache4_workspace_bytes.restype = ctypes.c_size_t
     lib.tra_packed_attn_cache4.argtypes = [vp, vp, vp, vp, ctypes.c_size_t, vp]
@@ -450,6 +450,7 @@ _DTYPES = {torch.bfloat16: TRA_BF16, torch.float16: TRA_FP16, torch.float32: TRA
 _ROTARY_TENSOR = struct.Struct("7Q9qiI")
 _PACKED_ARGS = struct.Struct("5Q8q3Q5ifQ")
 _PACKED_GRADS = struct.Struct("4Q8q")
+_STRIDES = struct.Struct("2q")
 assert (_ROTARY_TENSOR.size, _PACKED_ARGS.size, _PACKED_GRADS.size) == tuple(
     ctypes.sizeof(t) for t in (tra_rotary_tensor_t, tra_packed_args_t, tra_packed_grads_t))
 
@@ -862,9 +863,9 @@ class Cache4:
             raise ValueError(f"the current device must be {attn.device}")
         n = slots.shape[0]
         at = attn._ints(slots, "slots", n)
-        (kp, *ks), (vp, *vs) = attn._tensor(k, "k", n, attn.kv_heads), attn._tensor(v, "v", n, attn.kv_heads)
-        stride = ctypes.c_int64 * 2
-        _check(call(attn._h, self._desc, kp, vp, stride(*ks), stride(*vs), at, n, _raw_stream(attn._index)), name)
+        kp, k0, k1 = attn._tensor(k, "k", n, attn.kv_heads)
+        vp, v0, v1 = attn._tensor(v, "v", n, attn.kv_heads)
+        _check(call(attn._h, self._desc, kp, vp, _STRIDES.pack(k0, k1), _STRIDES.pack(v0, v1), at, n, _raw_stream(attn._index)), name)
 
     def write(self, k, v, slots):
         """Tokens k, v [n, kv_heads, head_dim] (any strides, multiples of 8 elements, with contiguous channels) into the rows ``slots``
@@ -873,9 +874,10 @@ class Cache4:
 
     def read(self, slots, k=None, v=None):
         """The rows ``slots`` -> (k, v) [n, kv_heads, head_dim], rounded to the type; rows of slots that are negative or past the cache
-        are left as they are (new tensors: undefined)."""
-        shape = (slots.shape[0], self.attn.kv_heads, self.attn.head_dim)
-        k = torch.empty(shape, dtype=self.attn.dtype, device=self.attn.device) if k is None else k
-        v = torch.empty(shape, dtype=self.attn.dtype, device=self.attn.device) if v is None else v
+        are left as they are (new tensors, which are slices of one allocation: undefined)."""
+        if k is None and v is None:
+            k, v = self.k_step.new_empty((2, slots.shape[0], self.attn.kv_heads, self.attn.head_dim)).unbind(0)      # one allocation
+        elif k is None or v is None:
+            raise ValueError("k, v: expected both or neither")
         self._rows(_lib.tra_cache4_read, "tra_cache4_read", k, v, slots)
         return k, v

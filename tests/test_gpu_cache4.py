@@ -346,7 +346,7 @@ def test_refusals(api):
     kr, kw = (i32([0]), i32([n])), dict(max_q=n, max_k=n)
     for call in (lambda: cache.write(k.half(), k, slots), lambda: cache.write(k, k[:-1], slots), lambda: cache.write(k, k, slots.long()),
                  lambda: cache.write(k.cpu(), k, slots), lambda: cache.write(k[..., ::2], k, slots), lambda: cache.write(k[0], k, slots),
-                 lambda: cache.read(slots.cpu()), lambda: cache.read(slots, k=k[1:]), lambda: api.Cache4(attn, -1),
+                 lambda: cache.read(slots.cpu()), lambda: cache.read(slots, k=k[1:]), lambda: cache.read(slots, k=k[1:], v=k), lambda: api.Cache4(attn, -1),
                  lambda: attn.forward_cache4(q.half(), cache, cu, k_range=kr, **kw), lambda: attn.forward_cache4(q, cache, cu, k_range=None, **kw),
                  lambda: attn.forward_cache4(q, cache, cu, k_range=(kr[0].long(), kr[1]), **kw),
                  lambda: api.PackedAttn(4, 4, d).forward_cache4(q, cache, cu, k_range=kr, **kw),
