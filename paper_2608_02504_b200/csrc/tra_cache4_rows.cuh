@@ -46,7 +46,8 @@ struct C4Cfg {
   static constexpr int kRing = kStages * kStageBytes;                     // of a warp
   // a warp's steps in fp32, [32 keys][groups] of the keys and of the values, and middles in fp16, [groups][32 keys]
   static constexpr int kScratch = kC4Piece * kGroups * (4 + 4 + 2);
-  static constexpr int kSmemData = kC4Warps * (kRing + kScratch);
+  static constexpr int kQueries = D / 16 * 8 * 32;                        // of eight rows: two registers per 16 channels and lane
+  static constexpr int kSmemData = kC4Warps * (kRing + kScratch) + 2 * kQueries;
   static constexpr int kSmemBytes = kSmemData + 256;
 };
 static_assert(rows_join_bytes<128>(kC4Warps) <= C4Cfg<128>::kSmemData, "join area");
@@ -106,6 +107,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
   float* k_step = (float*)(smem + kC4Warps * C::kRing + warp * C::kScratch);
   float* v_step = k_step + kC4Piece * G;
   __half* v_mid = (__half*)(v_step + kC4Piece * G);
+  uint4* queries = (uint4*)(smem + kC4Warps * (C::kRing + C::kScratch));      // [rows / 8][32 channels][lane]
   const int seq = blockIdx.x, kvh = blockIdx.y / args.row_tiles, row0 = (blockIdx.y % args.row_tiles) * kRowsMax;
   const tra_seq_range qr = tra_clamp_range(p.cu_q[seq], p.cu_q[seq + 1], p.total_q, p.max_q, p.status);
   const tra_seq_range kr = tra_clamp_range(p.k_begin[seq], p.k_end[seq], p.total_k, p.max_k, p.status);
@@ -176,14 +178,14 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
 
   const int g = lane >> 2, tig = lane & 3;
   float m[NB][2], l[NB][2];                                  // rows 8 nb + 2 tig, + 1
-  float o[D / 16][NB][4], om[NB][4];                         // [channels 16 i + g, + 8 (times 16)][rows 8 nb + 2 tig, + 1]; groups' share
+  float o[D / 16][NB][4], om[NB][4], om_odd[NB][4];          // [channels 16 i + g, + 8 (times 16)][rows 8 nb + 2 tig, + 1]; groups' share
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) m[nb][c] = -INFINITY, l[nb][c] = 0.f;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      om[nb][c] = 0.f;
+      om[nb][c] = om_odd[nb][c] = 0.f;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) o[i][nb][c] = 0.f;
     }
@@ -192,7 +194,8 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
 
   // ---- queries as the second operand: column g of a product is row 8 nb + g
   constexpr int kPieces = std::is_same<T, __nv_bfloat16>::value ? 3 : 2;        // of the group sums, in T
-  uint32_t qb[D / 16][NB][2], qs[NB][2];
+  // (in shared memory: registers are what limits the blocks of an SM)
+  uint32_t qs[NB][2];
   float row_mul[NB][2];                                      // to scores in base 2, codes' factor 2^24 included
   int hi[NB][2];                                             // keys in front of it are seen by the row
 #pragma unroll
@@ -217,6 +220,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
 #pragma unroll
     for (int j = 0; j < G; ++j) {
       float sum = 0.f;
+      uint32_t qb[4];
 #pragma unroll
       for (int i = 4 * j; i < 4 * j + 4; ++i) {
         float a, b;
@@ -224,8 +228,9 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
         a *= mul, b *= mul;
         sum += a + b;
         const float f = i & 1 ? 0.0625f : 1.f;               // its codes are held times 16
-        qb[i >> 1][nb][i & 1] = pack_pair<__half>(a * f, b * f);
+        qb[i & 3] = pack_pair<__half>(a * f, b * f);
       }
+      if (warp == 0) queries[(nb * G + j) * 32 + lane] = make_uint4(qb[0], qb[1], qb[2], qb[3]);
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
       // piece x of group j is row x G + j of the operand: rows 2 tig, 2 tig + 1 in one register, 8 more in the other
@@ -249,21 +254,21 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
   }
   const int hi_min = p.order ? min(max(tok0 + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
   const int old_max = kWindow ? walk - p.window : 0;         // keys that have left the last token's window
-  // -7.5 / 16 in row j of a product (rows from 8 on are nobody's)
-  uint32_t middle[G][4];
+  // -7.5 / 16 in row j of a product for the groups j = 0, 2 and in row 8 + j for j = 1, 3: a register each, and a sum for either half
+  uint32_t middle[G];
 #pragma unroll
-  for (int j = 0; j < G; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      middle[j][i] = g == j ? 0xb780b780u : 0u;
-      asm volatile("" : "+r"(middle[j][i]));                 // kept, not made again for every product
-    }
+  for (int j = 0; j < G; ++j) {
+    middle[j] = g == j ? 0xb780b780u : 0u;
+    asm volatile("" : "+r"(middle[j]));                      // kept, not made again for every product
+  }
   auto scale_sums = [&](float f0, float f1, int nb) {
     om[nb][0] *= f0, om[nb][1] *= f1;
+    om_odd[nb][2] *= f0, om_odd[nb][3] *= f1;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) o[i][nb][0] *= f0, o[i][nb][1] *= f1, o[i][nb][2] *= f0, o[i][nb][3] *= f1;
   };
 
+  __syncthreads();                                           // the queries are there
   int slot = 0;
   uint32_t phase = 0u;
 #pragma unroll 1
@@ -375,8 +380,9 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
             float c[4];
-            mma16816_first<__half>(c, a0, qb[2 * j][nb][0], qb[2 * j][nb][1]);
-            mma16816<__half>(c, a1, qb[2 * j + 1][nb][0], qb[2 * j + 1][nb][1]);
+            const uint4 q = queries[(nb * G + j) * 32 + lane];
+            mma16816_first<__half>(c, a0, q.x, q.y);
+            mma16816<__half>(c, a1, q.z, q.w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[sub][nb][i] = fmaf(st[i >> 1][j], c[i], s[sub][nb][i]);
           }
@@ -489,7 +495,8 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
             const uint32_t b1 = transpose8x8(pack_pair<__half>(q[2] * st[1][j], q[3] * st[1][j]));
             mma16816<__half>(o[2 * j][nb], a0, b0, b1);
             mma16816<__half>(o[2 * j + 1][nb], a1, b0, b1);
-            mma16816<__half>(om[nb], middle[j], b0, b1);
+            mma1688<__half>(j & 1 ? om_odd[nb] : om[nb], middle[j & ~1], middle[j | 1], b0);
+            mma1688<__half>(j & 1 ? om_odd[nb] : om[nb], middle[j & ~1], middle[j | 1], b1);
           }
         }
       }
@@ -525,7 +532,9 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
         float* dst = part + r * D;
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-          const float low = __shfl_sync(0xffffffffu, om[nb][c], j * 4 + tig) * f;        // row j
+          // row j: its middles and, of an even group, what the codes are above them; of an odd one the latter in row 8 + j
+          const float mine = om[nb][c] + (g & 1 ? om_odd[nb][c + 2] : 0.f);
+          const float low = __shfl_sync(0xffffffffu, mine, j * 4 + tig) * f;
 #pragma unroll
           for (int i = 2 * j; i < 2 * j + 2; ++i) {
             dst[i * 16 + g] = fmaf(o[i][nb][c] * 0x1p20f, f, low);        // codes 2^24, steps 2^-4
