@@ -471,6 +471,11 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
   }
   p.stream_rows = backward_stream_rows(h);
   p.stream_tokens = p.stream_rows / p.group;
+  // dQ blocks of about 24 steps, as long as there are three for every SM (times two where two share one)
+  const long long walked = ((long long)p.sink_rows + p.window + p.tile_tokens) / p.stream_rows + 1;
+  const long long tiles = ((long long)a->total_q / p.tile_tokens + 1) * p.kv_heads, three = 3ll * h->sm_count * (p.stream_rows == 64 ? 2 : 1);
+  p.dq_tiles = (int)(walked >= 24 ? 1 : 24 / walked);
+  while (p.dq_tiles > 1 && tiles / p.dq_tiles < three) --p.dq_tiles;
   const SinkPlan sinks = sink_plan(h, a->total_q);
   if (p.order == kOrderWindow && sinks.slots > 0) {
     p.sink_steps = sinks.steps, p.sink_slots = (int)sinks.slots;

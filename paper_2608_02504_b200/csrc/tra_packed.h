@@ -37,6 +37,7 @@ struct tra_packed_launch {
   int stream_rows, stream_tokens;            // backward: rows of a streamed tile, 128 or 64, and stream_rows / group
   int order, splits, n_units;                // n_units: query-tile pairs (forward) or key / query tiles (backward) launched
   int window, sinks, sink_rows;              // kOrderWindow; sink_rows: sinks rounded up to whole 8-row pieces of a tile
+  int dq_tiles;                              // backward with a window: query tiles of a dQ block, one after the other
   int sink_steps, sink_slots;                // backward: see tra_find_sink_unit; 0: the first keys' tiles walk all their queries
   float* sink_part;                          //   [slot][kv_heads][sinks][dK, dV][d] fp32
   // fp16 products for bf16 tensors (kPieces = 0 of the forward kernel): Q, K and V are fp16 multiples of the elements

@@ -98,6 +98,7 @@ struct BwdCtl {
   uint64_t ds_ready;
   uint64_t tail_full, tail_ready;
   uint64_t drain;
+  uint64_t own_free, sum_full, sum_free; // dq_tiles_block: the resident tiles may be overwritten; a tile's sum is there / has been read
   uint32_t tmem_base;
   int abort_flag;
   float tau;                             // fp16: see kScaled (dkv)
@@ -127,6 +128,9 @@ __device__ __forceinline__ void bwd_init(BwdCtl* ctl) {
   mbar_init(smem_u32(&ctl->tail_full), 1);
   mbar_init(smem_u32(&ctl->tail_ready), 1);
   mbar_init(smem_u32(&ctl->drain), 1);
+  mbar_init(smem_u32(&ctl->own_free), 1);
+  mbar_init(smem_u32(&ctl->sum_full), 1);
+  mbar_init(smem_u32(&ctl->sum_free), 4 * kHalves);
   ctl->abort_flag = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
@@ -618,10 +622,9 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
   }
   const int ahead = kr.len - qr.len;
   const int last_tok = min(tok0 + tile_tokens, qr.len) - 1;
-  const tra_key_axis<kOrder> axis(p, tok0 + ahead, kr.len);
-  const int keys = kCausal ? min(max(last_tok + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
+  const int keys = kCausal ? min(max(last_tok + 1 + ahead, 0), kr.len) : kr.len;
   const int n_all = (keys + C::kStream - 1) / C::kStream, n = n_all;
-  const bool tail_all = n > 0 && n * C::kStream > axis.len, tail = tail_all;
+  const bool tail_all = n > 0 && n * C::kStream > kr.len, tail = tail_all;
   volatile int* abort_flag = &ctl->abort_flag;
 
   if (warp >= C::kSoftWarps) {
@@ -638,22 +641,18 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
         bwd_produce<C>(
             ctl, n, tail, C::kStreamBytes, abort_flag, p.status,
             [&](int i, int slot, uint32_t bar) {
-              tra_load_keys<kOrder, C::kAtoms>(p, i * C::kStream, C::kStream, axis.gap, false, smem_u32(sA + slot * C::kStreamBytes), C::kStreamAtom,
-                                               [&](uint32_t dst, const CUtensorMap* map, int channel, int key) {
-                                                 tma_load_3d(dst, map, bar, channel, kvh, kr.begin + key);
-                                               });
+              for (int a = 0; a < C::kAtoms; ++a)
+                tma_load_3d(smem_u32(sA + slot * C::kStreamBytes + a * C::kStreamAtom), &p.map_k, bar, a * 64, kvh, kr.begin + i * C::kStream);
             },
             [&](int i, int slot, uint32_t bar) {
-              tra_load_keys<kOrder, C::kAtoms>(p, i * C::kStream, C::kStream, axis.gap, true, smem_u32(sB + slot * C::kStreamBytes), C::kStreamAtom,
-                                               [&](uint32_t dst, const CUtensorMap* map, int channel, int key) {
-                                                 tma_load_3d(dst, map, bar, channel, kvh, kr.begin + key);
-                                               });
+              for (int a = 0; a < C::kAtoms; ++a)
+                tma_load_3d(smem_u32(sB + slot * C::kStreamBytes + a * C::kStreamAtom), &p.map_v, bar, a * 64, kvh, kr.begin + i * C::kStream);
             });
       }
     } else if (warp == C::kSoftWarps + 2) {
       // ================================================================== rows past the sequence's end
       if (tail && mbar_wait_warp(smem_u32(&ctl->tail_full), 0u, abort_flag, p.status)) {
-        const int row0 = axis.len - (n - 1) * C::kStream;
+        const int row0 = kr.len - (n - 1) * C::kStream;
         zero_tile_rows(sA + ((n - 1) % C::kA) * C::kStreamBytes, row0, C::kStream, C::kAtoms, C::kStreamAtom, lane, 32);
         zero_tile_rows(sB + ((n - 1) % C::kB) * C::kStreamBytes, row0, C::kStream, C::kAtoms, C::kStreamAtom, lane, 32);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -740,7 +739,7 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
     delta *= tau;
     const uint64_t scale2 = pack2(scale_log2, scale_log2), neg_lse2 = pack2(-lse2, -lse2), neg_delta2 = pack2(-delta, -delta);
     const uint64_t tau2 = pack2(tau, tau);
-    const int seen = kCausal ? min(max(min(tok, last_tok) + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
+    const int seen = kCausal ? min(max(min(tok, last_tok) + 1 + ahead, 0), kr.len) : kr.len;
     RingPos<C::kA> kd;                                       // K of the step before
     bool alive = true;
     for (int i = 0; i < n; ++i) {
@@ -766,14 +765,6 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
 #pragma unroll
         for (int c = 0; c < 64; ++c)
           if (c >= limit) pr[c] = 0.f;
-      }
-      if (kOrder == kOrderWindow) {                          // columns in front of `old` are out of the window but for the first tokens
-        const int old = limit - p.window, first = p.sinks - i * C::kStream - h * 64;
-        if (__any_sync(0xffffffffu, old > max(first, 0))) {
-#pragma unroll
-          for (int c = 0; c < 64; ++c)
-            if (c < old && c >= first) pr[c] = 0.f;
-        }
       }
       if (!mbar_wait_warp(smem_u32(&ctl->dp_full), (uint32_t)i & 1u, abort_flag, p.status)) {
         alive = false;
@@ -817,6 +808,301 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
   bwd_teardown<C>(ctl, tmem, warp);
 }
 
+// With a window a query tile walks few keys, and a block per tile spends more on set-up, first loads, the last product and the stores than on its steps
+// (five of them: 5 us of 12.6).  So a block takes dq_tiles consecutive tiles of a sequence: the next one's Q and dO are loaded, and its
+// first scores formed, under the last steps and the stores of the one before.  Steps are counted through (g), so that every barrier keeps one phase per step
+// or per tile.  Prompts of up to 8,192 tokens, 40 / 8 heads, d 128, window 512: see launch_bwd.
+template <typename T, int D, int kHalves>
+__device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
+  using C = BwdCfg<D, kHalves>;
+  uint8_t* sQ = smem;
+  uint8_t* sDO = smem + C::kTileBytes;
+  uint8_t* sA = smem + 2 * C::kTileBytes;                   // K tiles
+  uint8_t* sB = sA + C::kA * C::kStreamBytes;                 // V tiles
+  BwdCtl* ctl = (BwdCtl*)(smem + C::kSmemData);
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+  const int tile_tokens = p.tile_tokens, box_rows = tile_tokens * p.group, unit_tokens = tile_tokens * p.dq_tiles;
+
+  // set-up in parallel, one barrier (see the forward kernel)
+  if (warp == 0) {
+    const tra_unit u = tra_find_unit(p, false, p.max_q <= unit_tokens, unit_tokens, unit);
+    if (lane == 0) ctl->unit = u;
+  } else if (warp == C::kSoftWarps + 1) {
+    tmem_alloc<C::kColumns>(&ctl->tmem_base);
+  } else if (tid == 32) {
+    bwd_init<kHalves>(ctl);
+  } else if (tid == 64) {
+    prefetch_map(&p.map_q);
+    prefetch_map(&p.map_do);
+    prefetch_map(&p.map_k);
+    prefetch_map(&p.map_v);
+  }
+  if (box_rows < kTileM && warp >= 2 && warp < C::kSoftWarps)        // rows that no box fills
+    zero_tile_rows(sQ, box_rows, kTileM, 2 * C::kAtoms, C::kAtomBytes, tid - 64, 32 * (C::kSoftWarps - 2));
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctl->tmem_base;
+  if (ctl->unit.seq < 0) {
+    if (warp == C::kSoftWarps + 1) tmem_free<C::kColumns>(tmem);
+    wait_last_launch();          // no block ends before the launch in front of it
+    return;
+  }
+  const int n_tiles = uniform(min(p.dq_tiles, (ctl->unit.q.len - ctl->unit.index * unit_tokens + tile_tokens - 1) / tile_tokens));
+  volatile int* abort_flag = &ctl->abort_flag;
+  // a tile's steps: read from shared memory, where they cost no registers
+  struct Tile {
+    int tok0, last_tok, ahead, gap, len, n;
+    bool tail;
+  };
+  auto tile_at = [&](int t) {
+    volatile tra_unit* u = &ctl->unit;
+    const int q_len = u->q.len, k_len = u->k.len;
+    Tile x;
+    x.tok0 = u->index * unit_tokens + t * tile_tokens;
+    x.last_tok = min(x.tok0 + tile_tokens, q_len) - 1;
+    x.ahead = k_len - q_len;
+    const tra_key_axis<kOrderWindow> axis(p, x.tok0 + x.ahead, k_len);
+    x.gap = axis.gap;
+    x.len = axis.len;
+    x.n = (min(max(x.last_tok + 1 + x.ahead - x.gap, 0), x.len) + C::kStream - 1) / C::kStream;
+    x.tail = x.n > 0 && x.n * C::kStream > x.len;
+    return x;
+  };
+
+  if (warp >= C::kSoftWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsControl));
+    if (warp == C::kSoftWarps) {
+      // ================================================================== TMA producer
+      if (lane == 0) {
+        const int q_begin = ctl->unit.q.begin, k_begin = ctl->unit.k.begin;
+        RingPos<C::kA> a;
+        RingPos<C::kB> b;
+        int loaded = 0;
+        bool alive = true;
+        for (int t = 0; t < n_tiles && alive; ++t) {
+          const Tile x = tile_at(t);
+          if (t > 0 && !(alive = mbar_wait(smem_u32(&ctl->own_free), (uint32_t)(t - 1) & 1u, abort_flag, p.status))) break;
+          const uint32_t own = smem_u32(&ctl->own_full);
+          mbar_expect_tx(own, 2 * C::kAtoms * box_rows * 128);
+          for (int c = 0; c < C::kAtoms; ++c) {
+            tma_load_3d(smem_u32(sQ + c * C::kAtomBytes), &p.map_q, own, c * 64, kvh * p.group, q_begin + x.tok0);
+            tma_load_3d(smem_u32(sDO + c * C::kAtomBytes), &p.map_do, own, c * 64, kvh * p.group, q_begin + x.tok0);
+          }
+          for (int i = 0; i < x.n; ++i, ++loaded) {
+            const bool last = x.tail && i == x.n - 1;
+            auto load = [&](bool v_side, uint64_t* full, uint64_t* free, uint32_t phase, bool wait, uint8_t* dst) -> bool {
+              if (wait && !mbar_wait(smem_u32(free), phase ^ 1u, abort_flag, p.status)) return false;
+              uint32_t bar = smem_u32(full);
+              if (last) {                                     // announced by tail_ready once rows of it are zeroed; its own barrier keeps its count
+                mbar_arrive(bar);
+                bar = smem_u32(&ctl->tail_full);
+                if (!v_side) mbar_expect_tx(bar, 2 * C::kStreamBytes);
+              } else {
+                mbar_expect_tx(bar, C::kStreamBytes);
+              }
+              tra_load_keys<kOrderWindow, C::kAtoms>(p, i * C::kStream, C::kStream, x.gap, v_side, smem_u32(dst), C::kStreamAtom,
+                                                     [&](uint32_t to, const CUtensorMap* map, int channel, int key) {
+                                                       tma_load_3d(to, map, bar, channel, kvh, k_begin + key);
+                                                     });
+              return true;
+            };
+            alive = load(false, &ctl->a_full[a.slot], &ctl->a_free[a.slot], a.phase, loaded >= C::kA, sA + a.slot * C::kStreamBytes) &&
+                    load(true, &ctl->b_full[b.slot], &ctl->b_free[b.slot], b.phase, loaded >= C::kB, sB + b.slot * C::kStreamBytes);
+            if (!alive) break;
+            a.next();
+            b.next();
+          }
+        }
+      }
+    } else if (warp == C::kSoftWarps + 2) {
+      // ================================================================== rows past the sequence's end
+      int steps = 0, tails = 0;
+      for (int t = 0; t < n_tiles; ++t) {
+        const Tile x = tile_at(t);
+        steps += x.n;
+        if (!x.tail) continue;
+        if (!mbar_wait_warp(smem_u32(&ctl->tail_full), (uint32_t)tails & 1u, abort_flag, p.status)) break;
+        const int row0 = x.len - (x.n - 1) * C::kStream;
+        zero_tile_rows(sA + ((steps - 1) % C::kA) * C::kStreamBytes, row0, C::kStream, C::kAtoms, C::kStreamAtom, lane, 32);
+        zero_tile_rows(sB + ((steps - 1) % C::kB) * C::kStreamBytes, row0, C::kStream, C::kAtoms, C::kStreamAtom, lane, 32);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->tail_ready));
+        ++tails;
+      }
+    } else if (warp == C::kSoftWarps + 1) {
+      // ================================================================== MMA issuer
+      constexpr uint32_t kIdescS = make_idesc_t<T>(C::kStream, false);
+      constexpr uint32_t kIdescD = make_idesc_t<T>(D, true);
+      constexpr uint32_t kHi = desc_hi(1024);
+      const uint32_t q_lo = desc_lo(smem_u32(sQ), 16), do_lo = desc_lo(smem_u32(sDO), 16);
+      const uint32_t a_k = desc_lo(smem_u32(sA), 16), a_mn = desc_lo(smem_u32(sA), C::kStreamAtom), b_k = desc_lo(smem_u32(sB), 16);
+      constexpr uint32_t kTile = C::kStreamBytes >> 4;
+      RingPos<C::kA> ks, kd;                 // K of the next S, of the next dQ
+      RingPos<C::kB> vs;
+      const uint32_t tmem = uniform(ctl->tmem_base);
+      auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(smem_u32(bar), parity & 1u, abort_flag, p.status); };
+      uint32_t g = 0, tails = 0;             // steps so far, tails so far
+      bool alive = true;
+      for (int t = 0; t < n_tiles && alive; ++t) {
+        const Tile x = tile_at(t);
+        const int n = uniform(x.n);
+        const bool tail = uniform(x.tail);
+        // K and V of step i are in shared memory
+        auto tiles_here = [&](int i) -> bool {
+          if (tail && i == n - 1) return wait(&ctl->tail_ready, tails++);
+          return wait(&ctl->a_full[ks.slot], ks.phase) && wait(&ctl->b_full[vs.slot], vs.phase);
+        };
+        // scores and dP of the step that follows step g - 1, whose columns they take
+        auto issue_next = [&](bool last, uint32_t before) -> bool {
+          if (before > 0 && !wait(&ctl->s_read, before - 1)) return false;
+          tc_fence_after();
+          mma_tiles<D>(tmem, q_lo, a_k + (uint32_t)ks.slot * kTile, kIdescS);
+          tc_commit(smem_u32(&ctl->s_full));
+          ks.next();
+          if (before > 0 && !wait(&ctl->dp_read, before - 1)) return false;
+          tc_fence_after();
+          mma_tiles<D>(tmem + C::kDp, do_lo, b_k + (uint32_t)vs.slot * kTile, kIdescS);
+          tc_commit(smem_u32(&ctl->dp_full));
+          tc_commit(smem_u32(&ctl->b_free[vs.slot]));
+          if (last) tc_commit(smem_u32(&ctl->own_free));
+          vs.next();
+          return true;
+        };
+        if (!(alive = wait(&ctl->own_full, t))) break;
+        if (n == 0) tc_commit(smem_u32(&ctl->own_free));
+        if (n > 0 && !(alive = tiles_here(0) && issue_next(n == 1, g))) break;
+        // the sum of the tile before has been read
+        if (t > 0 && !(alive = wait(&ctl->sum_free, t - 1))) break;
+        for (int i = 0; i < n; ++i, ++g) {
+          if (i + 1 < n && !(alive = tiles_here(i + 1) && issue_next(i + 2 == n, g + 1))) break;
+          if (!(alive = wait(&ctl->ds_ready, g))) break;
+          tc_fence_after();
+          const uint32_t k_mn = a_mn + (uint32_t)kd.slot * kTile;           // dQ += dS K
+#pragma unroll
+          for (int kk = 0; kk < 4 * kHalves; ++kk)
+            tc_mma_ts(tmem + C::kSum0, tmem + C::kSum1 + kk * 8, k_mn + kk * (2048 >> 4), kHi, kIdescD, kk > 0 ? 1u : (i > 0 ? 1u : 0u));
+          tc_commit(smem_u32(&ctl->a_free[kd.slot]));
+          kd.next();
+        }
+        if (!alive) break;
+        tc_commit(smem_u32(&ctl->sum_full));
+      }
+      tc_commit(smem_u32(&ctl->drain));
+      mbar_wait_warp(smem_u32(&ctl->drain), 0u, abort_flag, p.status);
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
+    const int h = warp >> 2;                                 // key columns 64 h .. 64 h + 63 of a block
+    int r = tid & (kTileM - 1);                              // query row
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const float scale_log2 = p.sm_scale * kLog2e;
+    const uint64_t scale2 = pack2(scale_log2, scale_log2);
+    RingPos<C::kA> kd;                                       // K of the step before
+    uint32_t g = 0;
+    bool alive = true;
+    wait_last_launch();                                      // delta
+    const float tau = kScaled<T> ? grad_tau(p, kvh) * kProbMul : 1.f;      // dS times it, as in dkv_block
+    const uint64_t tau2 = pack2(tau, tau);
+    for (int t = 0; t < n_tiles && alive; ++t) {
+      int n, limit0;
+      float lse2 = INFINITY, delta = 0.f;                    // a row that is not there, or sees no key: probability 0
+      asm volatile("" : "+r"(r));                            // (what follows from it alone would be kept in registers through all tiles)
+      {
+        const Tile x = tile_at(t);
+        n = x.n;
+        const int tok = x.tok0 + r / p.group;
+        limit0 = min(max(min(tok, x.last_tok) + 1 + x.ahead - x.gap, 0), x.len) - h * 64;
+        if (r < box_rows && tok <= x.last_tok) {
+          const long long row = (long long)(*(volatile int*)&ctl->unit.q.begin + tok) * p.heads + kvh * p.group + r % p.group;
+          const float v = p.lse[row] * kLog2e;
+          lse2 = v == -INFINITY ? INFINITY : v;
+          delta = p.delta[row] * tau;
+        }
+      }
+      const uint64_t neg_lse2 = pack2(-lse2, -lse2), neg_delta2 = pack2(-delta, -delta);
+      for (int i = 0; i < n; ++i, ++g) {
+        if (!mbar_wait_warp(smem_u32(&ctl->s_full), g & 1u, abort_flag, p.status)) {
+          alive = false;
+          break;
+        }
+        tc_fence_after();
+        uint32_t s[64];
+        float pr[64];
+        tmem_ld64(tmem + lane_base + h * 64, s);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->s_read));
+#pragma unroll
+        for (int c = 0; c < 64; c += 2) {
+          float t0, t1;
+          unpack2(ffma2(pack2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, neg_lse2), t0, t1);
+          pr[c] = ex2(t0), pr[c + 1] = ex2(t1);
+        }
+        const int limit = limit0 - i * C::kStream;           // columns at and past it are not seen
+        if (__any_sync(0xffffffffu, limit < 64)) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c >= limit) pr[c] = 0.f;
+        }
+        // columns in front of `old` are out of the window but for the first tokens
+        const int old = limit - p.window, first = p.sinks - i * C::kStream - h * 64;
+        if (__any_sync(0xffffffffu, old > max(first, 0))) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c < old && c >= first) pr[c] = 0.f;
+        }
+        if (!mbar_wait_warp(smem_u32(&ctl->dp_full), g & 1u, abort_flag, p.status)) {
+          alive = false;
+          break;
+        }
+        tc_fence_after();
+        tmem_ld64(tmem + lane_base + C::kDp + h * 64, s);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->dp_read));
+        uint32_t pk[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          float t0, t1;
+          const uint64_t dp = pack2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
+          unpack2(fmul2(pack2(pr[2 * c], pr[2 * c + 1]), kScaled<T> ? ffma2(dp, tau2, neg_delta2) : fadd2(dp, neg_delta2)), t0, t1);
+          pk[c] = pack_pair<T>(t0, t1);
+        }
+        // the product that read the last dS has retired (it also freed that stage)
+        if (g > 0) {
+          if (!mbar_wait_warp(smem_u32(&ctl->a_free[kd.slot]), kd.phase, abort_flag, p.status)) {
+            alive = false;
+            break;
+          }
+          kd.next();
+        }
+        tc_fence_after();
+        tmem_st32(tmem + lane_base + C::kSum1 + h * 32, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
+      }
+      if (alive) alive = mbar_wait_warp(smem_u32(&ctl->sum_full), (uint32_t)t & 1u, abort_flag, p.status);
+      if (!alive) break;
+      tc_fence_after();
+      asm volatile("" : "+r"(r));
+      const int tok = (*(volatile int*)&ctl->unit.index * p.dq_tiles + t) * tile_tokens + r / p.group;
+      const bool row_valid = r < box_rows && tok < *(volatile int*)&ctl->unit.q.len;
+      const long long tok_g = *(volatile int*)&ctl->unit.q.begin + (row_valid ? tok : 0);
+      T* out = (T*)p.dq + tok_g * p.dq_stride[0] + (kvh * p.group + r % p.group) * p.dq_stride[1];
+      store_share<T, D / kHalves>(RowAddresses(row_valid ? out : nullptr), tmem + lane_base + C::kSum0, h, n > 0, kScaled<T> ? p.sm_scale / tau : p.sm_scale);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_free));
+    }
+  }
+  bwd_teardown<C>(ctl, tmem, warp);
+}
+
 // ------------------------------------------------------------------------------------ both
 // Blocks of either kind in one launch, so that the shorter dQ blocks fill the SMs that the last dK/dV blocks leave: first
 // dkv_units per key/value head, then dq_units.  Of a causal sequence the first keys and the last queries have most to
@@ -837,6 +1123,8 @@ __global__ void __launch_bounds__(BwdCfg<D, kHalves>::kThreads, BwdCfg<D, kHalve
   const int n_dkv = dkv_units * p.kv_heads;
   if (b < n_dkv)
     dkv_block<T, D, kHalves, kOrder>(p, smem, b % dkv_units, b / dkv_units);
+  else if constexpr (kOrder == kOrderWindow)
+    dq_tiles_block<T, D, kHalves>(p, smem, (b - n_dkv) % dq_units, (b - n_dkv) / dq_units);
   else
     dq_block<T, D, kHalves, kOrder>(p, smem, (b - n_dkv) % dq_units, (b - n_dkv) / dq_units);
 }
@@ -996,7 +1284,8 @@ int launch_bwd(const tra_packed_ctx& c, const tra_packed_launch& a) {
     if (rc != TRA_OK) return rc;
   }
   const int dkv_units = a.max_k > 0 ? (a.max_k <= kTileM ? 0 : a.total_k / kTileM) + a.n_seq : 0;
-  const int dq_units = a.max_q > 0 ? (a.max_q <= a.tile_tokens ? 0 : a.total_q / a.tile_tokens) + a.n_seq : 0;
+  const int dq_tokens = a.tile_tokens * (kOrder == kOrderWindow ? a.dq_tiles : 1);
+  const int dq_units = a.max_q > 0 ? (a.max_q <= dq_tokens ? 0 : a.total_q / dq_tokens) + a.n_seq : 0;
   const long long sink_units = kOrder == kOrderWindow ? (long long)a.sink_slots * (((a.sinks < a.max_k ? a.sinks : a.max_k) + kTileM - 1) / kTileM) : 0;
   const long long blocks = (sink_units + dkv_units + dq_units) * a.kv_heads;
   if (blocks == 0) return TRA_OK;
