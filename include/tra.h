@@ -380,7 +380,8 @@ typedef struct {
   int causal;
   int window;          /* 0: none.  Else (with causal) a query sees the last `window` keys up to its own position and the   */
   int sinks;           /* first `sinks` keys of its sequence (0: none): at position p = i + keys - queries, key j with      */
-                       /* j <= p and (j > p - window or j < sinks).  Keys that no query of a call sees are not read         */
+                       /* j <= p and (j > p - window or j < sinks).  What lies behind the first tokens and in front of    */
+                       /* every window costs nothing                                                                     */
 } tra_packed_config_t;
 
 typedef struct {

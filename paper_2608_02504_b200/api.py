@@ -451,8 +451,9 @@ _ROTARY_TENSOR = struct.Struct("7Q9qiI")
 _PACKED_ARGS = struct.Struct("5Q8q3Q5ifQ")
 _PACKED_GRADS = struct.Struct("4Q8q")
 _STRIDES = struct.Struct("2q")
-assert (_ROTARY_TENSOR.size, _PACKED_ARGS.size, _PACKED_GRADS.size) == tuple(
-    ctypes.sizeof(t) for t in (tra_rotary_tensor_t, tra_packed_args_t, tra_packed_grads_t))
+_CACHE4 = struct.Struct("4Qi4x")
+assert (_ROTARY_TENSOR.size, _PACKED_ARGS.size, _PACKED_GRADS.size, _CACHE4.size) == tuple(
+    ctypes.sizeof(t) for t in (tra_rotary_tensor_t, tra_packed_args_t, tra_packed_grads_t, tra_cache4_t))
 
 
 # (torch.cuda.current_stream builds a Stream object for it: 1.3 us against 0.1)
@@ -828,7 +829,7 @@ class PackedAttn:
         a = self._args(q, None, None, o, lse, None, cu_q, None, k_range, max_q, max_k, sm_scale, cached=cache.tokens)
         n = _lib.tra_packed_attn_cache4_workspace_bytes(self._h, cu_q.shape[0] - 1, q.shape[0], max_q, max_k)
         ws = q.new_empty((n,), dtype=torch.uint8) if n else None
-        _check(_lib.tra_packed_attn_cache4(self._h, a, cache._desc, ws.data_ptr() if n else None, n, _raw_stream(self._index)),
+        _check(_lib.tra_packed_attn_cache4(self._h, a, cache._desc(), ws.data_ptr() if n else None, n, _raw_stream(self._index)),
                "tra_packed_attn_cache4")
         return o, lse
 
@@ -848,7 +849,9 @@ class Cache4:
         heads, d = attn.kv_heads, attn.head_dim
         self.k, self.v = (torch.empty((heads, self.tokens, d // 2), dtype=torch.uint8, device=attn.device) for _ in range(2))
         self.k_step, self.v_step = (torch.empty((heads, self.tokens, 2, d // 32), dtype=attn.dtype, device=attn.device) for _ in range(2))
-        self._desc = bytes(tra_cache4_t(*(t.data_ptr() for t in (self.k, self.v, self.k_step, self.v_step)), self.tokens))
+
+    def _desc(self):
+        return _CACHE4.pack(self.k.data_ptr(), self.v.data_ptr(), self.k_step.data_ptr(), self.v_step.data_ptr(), self.tokens)
 
     def _fits(self, attn):
         a = self.attn
@@ -865,7 +868,7 @@ class Cache4:
         at = attn._ints(slots, "slots", n)
         kp, k0, k1 = attn._tensor(k, "k", n, attn.kv_heads)
         vp, v0, v1 = attn._tensor(v, "v", n, attn.kv_heads)
-        _check(call(attn._h, self._desc, kp, vp, _STRIDES.pack(k0, k1), _STRIDES.pack(v0, v1), at, n, _raw_stream(attn._index)), name)
+        _check(call(attn._h, self._desc(), kp, vp, _STRIDES.pack(k0, k1), _STRIDES.pack(v0, v1), at, n, _raw_stream(attn._index)), name)
 
     def write(self, k, v, slots):
         """Tokens k, v [n, kv_heads, head_dim] (any strides, multiples of 8 elements, with contiguous channels) into the rows ``slots``

@@ -417,9 +417,10 @@ SinkPlan sink_plan(const tra_packed* h, int total_q) {
   if (steps < 16) steps = 16;
   if (steps < total_q / (32 * tokens)) steps = total_q / (32 * tokens);
   // not where one block that walks all queries is done before the others: these walk a window each, and the dQ blocks about as much
-  const long long tiles = (total_q + kTileM - 1) / kTileM, sink_tiles = ((long long)h->cfg.sinks + kTileM - 1) / kTileM, walk = total_q / tokens;
+  const long long tiles = (total_q + kTileM - 1) / kTileM, walk = total_q / tokens, window = h->cfg.window < total_q ? h->cfg.window : total_q;
+  const long long sink_tiles = ((h->cfg.sinks < total_q ? h->cfg.sinks : total_q) + kTileM - 1) / kTileM;
   const long long blocks = h->cfg.head_dim == 64 ? 2 : 1;
-  if (10 * walk * blocks * h->sm_count < 6 * h->cfg.kv_heads * (2 * tiles * (h->cfg.window + kTileM) / tokens + sink_tiles * walk)) return s;
+  if (10 * walk * blocks * h->sm_count < 6 * h->cfg.kv_heads * (2 * tiles * (window + kTileM) / tokens + sink_tiles * walk)) return s;
   for (; steps * tokens < total_q; steps *= 2) {
     const long long slots = 2 * (total_q / (steps * tokens)) + 2;
     if (slots * h->cfg.kv_heads * h->cfg.sinks > (256ll << 20) / (8 * h->cfg.head_dim)) continue;

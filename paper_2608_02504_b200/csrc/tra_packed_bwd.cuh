@@ -1006,23 +1006,25 @@ __device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8
     wait_last_launch();                                      // delta
     const float tau = kScaled<T> ? grad_tau(p, kvh) * kProbMul : 1.f;      // dS times it, as in dkv_block
     const uint64_t tau2 = pack2(tau, tau);
-    for (int t = 0; t < n_tiles && alive; ++t) {
-      int n, limit0;
-      float lse2 = INFINITY, delta = 0.f;                    // a row that is not there, or sees no key: probability 0
+    int n = 0, limit0 = 0;
+    float lse = INFINITY, delta = 0.f;                       // a row that is not there: probability 0
+    auto begin_tile = [&](int t) {
       asm volatile("" : "+r"(r));                            // (what follows from it alone would be kept in registers through all tiles)
-      {
-        const Tile x = tile_at(t);
-        n = x.n;
-        const int tok = x.tok0 + r / p.group;
-        limit0 = min(max(min(tok, x.last_tok) + 1 + x.ahead - x.gap, 0), x.len) - h * 64;
-        if (r < box_rows && tok <= x.last_tok) {
-          const long long row = (long long)(*(volatile int*)&ctl->unit.q.begin + tok) * p.heads + kvh * p.group + r % p.group;
-          const float v = p.lse[row] * kLog2e;
-          lse2 = v == -INFINITY ? INFINITY : v;
-          delta = p.delta[row] * tau;
-        }
+      const Tile x = tile_at(t);
+      n = x.n;
+      const int tok = x.tok0 + r / p.group;
+      limit0 = min(max(min(tok, x.last_tok) + 1 + x.ahead - x.gap, 0), x.len) - h * 64;
+      lse = INFINITY, delta = 0.f;
+      if (r < box_rows && tok <= x.last_tok) {
+        const long long row = (long long)(*(volatile int*)&ctl->unit.q.begin + tok) * p.heads + kvh * p.group + r % p.group;
+        lse = p.lse[row];
+        delta = p.delta[row];
       }
-      const uint64_t neg_lse2 = pack2(-lse2, -lse2), neg_delta2 = pack2(-delta, -delta);
+    };
+    begin_tile(0);
+    for (int t = 0; t < n_tiles && alive; ++t) {
+      const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;       // or sees no key
+      const uint64_t neg_lse2 = pack2(-lse2, -lse2), neg_delta2 = pack2(-delta * tau, -delta * tau);
       for (int i = 0; i < n; ++i, ++g) {
         if (!mbar_wait_warp(smem_u32(&ctl->s_full), g & 1u, abort_flag, p.status)) {
           alive = false;
@@ -1086,6 +1088,8 @@ __device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->ds_ready));
       }
+      const bool any = n > 0;
+      if (alive && t + 1 < n_tiles) begin_tile(t + 1);       // its loads travel while the sum is waited for and stored
       if (alive) alive = mbar_wait_warp(smem_u32(&ctl->sum_full), (uint32_t)t & 1u, abort_flag, p.status);
       if (!alive) break;
       tc_fence_after();
@@ -1094,7 +1098,7 @@ __device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8
       const bool row_valid = r < box_rows && tok < *(volatile int*)&ctl->unit.q.len;
       const long long tok_g = *(volatile int*)&ctl->unit.q.begin + (row_valid ? tok : 0);
       T* out = (T*)p.dq + tok_g * p.dq_stride[0] + (kvh * p.group + r % p.group) * p.dq_stride[1];
-      store_share<T, D / kHalves>(RowAddresses(row_valid ? out : nullptr), tmem + lane_base + C::kSum0, h, n > 0, kScaled<T> ? p.sm_scale / tau : p.sm_scale);
+      store_share<T, D / kHalves>(RowAddresses(row_valid ? out : nullptr), tmem + lane_base + C::kSum0, h, any, kScaled<T> ? p.sm_scale / tau : p.sm_scale);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctl->sum_free));

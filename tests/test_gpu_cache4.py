@@ -215,6 +215,12 @@ def test_groups(api):
         run(api, HALF, 128, 2 * group, 2, [1, 1], [700, 33])
 
 
+@pytest.mark.parametrize("nq", [1, 3])
+def test_many_sequences(api, nq):
+    run(api, BF, 64, 4, 2, [nq * (i % 3 > 0) for i in range(1100)], [(7 * i) % 97 + 3 for i in range(1100)])
+    run(api, HALF, 128, 2, 1, [nq] * 400, [(37 * i) % 700 for i in range(400)], 90, 5)
+
+
 def test_many_splits(api):
     run(api, BF, 128, 2, 2, [1], [40000])
     run(api, HALF, 64, 12, 2, [8], [30001])
