@@ -20,6 +20,11 @@
 // Split launches give every unit a range of the key blocks; the parts O / l and log2 l go to a
 // workspace and tra_packed_join_kernel adds them.
 //
+// With a window (kOrderWindow) a pair of tiles walks the first tokens' keys and the union of its tiles' windows as one closed-up axis
+// (tra_key_axis); what a row does not see of that is masked like the causal edge.  A window of 1,024, 40 / 8 heads, d 128, is nine key blocks per pair
+// of 50 tokens, of which 8.2 hold a key that some row sees: eight prompts of 1 to 16,384 tokens 616 us (880 TFLOP/s of what is seen).  What is left to the
+// rate of long sequences is the ends of the units: 7,000 cycles (last product, stores) of 40,000.
+//
 // Bound: tensor cores, at the power cap (see tra_attn_kernel.cuh), for long sequences: two of 32,760 tokens and one of 10,921, 12 heads, d
 // 128, 11.1 ms (1,250 TFLOP/s); eight causal prompts of 1 to 8,192 tokens, 40 / 8 heads, 775 us (1,180 TFLOP/s), 0.9 ms back to back.
 #pragma once
