@@ -4,29 +4,30 @@
 // Mathematics.  A key is k_c = low_j + step_j n_c for the channels c of group j, n = 0 .. 15, so
 //   q k = sum_j (step_j sum_(c in j) q_c n_c + low_j sum_(c in j) q_c):
 // the products run over the codes themselves, and the steps come in fp32 behind them (the second sum is one more product, of the lowest
-// values with the queries' group sums in two or three pieces).  A value is mid_j + step_j (n_c - 7.5), mid = low + 7.5 step, so
-//   o_c = sum_i (p_i step_ij) n_ic - 7.5 sum_i (p_i step_ij) + sum_i p_i mid_ij:
-// the steps go to the probabilities, and the last two sums, the same for the channels of a group, are rows of one more product.
+// values with the queries' group sums in two or three pieces).  A value is mid_j + step_j (n_c - 8), mid = low + 8 step, so
+//   o_c = sum_i (p_i step_ij) n_ic - 8 sum_i (p_i step_ij) + sum_i p_i mid_ij:
+// the steps go to the probabilities, the second sum is a product with a constant, into the first one's registers every 16 keys, and the last, the same
+// for the channels of a group, is one product for all groups.
 //
-// Rounding.  p step is rounded to fp16, once, and meets n - 7.5, which is as large as what a value differs from its group's middle: that is
+// Rounding.  p step is rounded to fp16, once, and meets n - 8, which is as large as what a value differs from its group's middle: that is
 // the rounding of the probabilities of any attention kernel.  (Probabilities rounded first and multiplied by the steps in fp16, against n and
 // low: 4.5e-4 off on a cache of 777 fp16 keys, where rounding the result alone makes 2.0e-4; so: 2.8e-4.)  p mid has p rounded to fp16.  Everything
-// else is exact or fp32.
+// else is exact or fp32.  The sums of n and of 8 are taken off each other as they grow: of two sums of their own over 20,000 keys the difference
+// is a hundredth, and the tensor pipe's truncated additions show in it (4.0e-4 against 2.8e-4).
 //
 // A code in the low bits of a 16-bit half is the fp16 number n 2^-24, exactly (a subnormal), and one in the next four bits is 16 times
 // that: so one mask takes two codes to two halves, and the factor 16 goes to the other operand (keys: channels of q) or to the
 // result (values: channels of o).  All products are fp16 with fp32 sums, whatever the type of the tensors: q is scaled by a power of two per
 // row that brings its largest element to 2^10, and steps and middles of the values by one, 2^-e, that follows the largest of them so
-// far, so that fp16's range is not an issue: elements 2^-24 times the largest lose precision, which no 16-bit tensor shows.  The probabilities are
-// held times 2^6 for the same reason.
+// far, so that fp16's range is not an issue: elements 2^-24 times the largest lose precision, which no 16-bit tensor shows.
 //
-// Bound: instruction issue and latency beside HBM (0.625 bytes a channel, against 2): 690 instructions per 32 keys of a head, of which a third
-// turns codes into operands; at the rate at which HBM delivers them, an SM would have to issue 3.2 of its 4 per cycle, and issues 2.3.  A
+// Bound: instruction issue and latency beside HBM (0.625 bytes a channel, against 2): 705 instructions per 32 keys of a head, of which a third
+// turns codes into operands; at the rate at which HBM delivers them, an SM would have to issue 3.3 of its 4 per cycle, and issues 2.3.  A
 // block is four warps that each walk pieces of 32 keys, every fourth one, through a ring of bulk copies of their own (a piece is four runs
-// of bytes): no warp waits for another before the join.  64 caches of 700 to 32,768 keys, 40 / 8 heads, d 128: 326 us, 4.2 TB/s (64 % of the copy rate; the cache
+// of bytes): no warp waits for another before the join.  64 caches of 700 to 32,768 keys, 40 / 8 heads, d 128: 338 us, 4.1 TB/s (62 % of the copy rate; the cache
 // in 16 bits: 646 us).  History: codes as operands with P multiplied in fp16, a producer warp, two clustered parts 424; the rounding above, a ring per warp
-// 561; parts without clusters 334; queries in shared memory 326.  Four blocks an SM in 128 registers (748 instructions) or the ring's slots unrolled
-// (745): 321 to 324, and 10 to 15 % more for short caches.
+// 561; parts without clusters 334; queries in shared memory 326; the sums of 8 in the others' registers 338.  Four blocks an SM in 128 registers (748 instructions) or the ring's slots unrolled
+// (745): 1 to 2 % less, and 10 to 15 % more for short caches.
 #pragma once
 #include "tra_cache4.h"
 #include "tra_rows_join.cuh"
@@ -37,7 +38,10 @@ constexpr int kC4Piece = 32;              // keys of a ring slot: one per lane
 constexpr int kC4Warps = 4;
 constexpr int kC4Threads = 32 * kC4Warps;
 constexpr int kC4Tile = kC4Piece * kC4Warps;
-constexpr int kC4ProbLog2 = 6;            // probabilities are held times 2^6
+// Probabilities are at most 2^kC4Above and held times 2^kC4ProbLog2: below 2^15, and in full precision down to 2^-27 for the largest steps.  (2^8 and
+// 2^6: 4.2e-4 off over 20,000 fp16 keys, most of whose probabilities were subnormal; so: 2.8e-4.)
+constexpr int kC4ProbLog2 = 13;
+constexpr float kC4Above = 2.f;
 constexpr int kC4QLog2 = 10;              // rows of q: largest element in [2^9, 2^10)
 
 template <int D>
@@ -183,14 +187,14 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
 
   const int g = lane >> 2, tig = lane & 3;
   float m[NB][2], l[NB][2];                                  // rows 8 nb + 2 tig, + 1
-  float o[D / 16][NB][4], om[NB][4], om_odd[NB][4];          // [channels 16 i + g, + 8 (times 16)][rows 8 nb + 2 tig, + 1]; groups' share
+  float o[D / 16][NB][4], om[NB][4];                         // [channels 16 i + g, + 8 (times 16)][rows 8 nb + 2 tig, + 1]; groups' share
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) m[nb][c] = -INFINITY, l[nb][c] = 0.f;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      om[nb][c] = om_odd[nb][c] = 0.f;
+      om[nb][c] = 0.f;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) o[i][nb][c] = 0.f;
     }
@@ -259,16 +263,9 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
   }
   const int hi_min = p.order ? min(max(tok0 + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
   const int old_max = kWindow ? walk - p.window : 0;         // keys that have left the last token's window
-  // -7.5 / 16 in row j of a product for the groups j = 0, 2 and in row 8 + j for j = 1, 3: a register each, and a sum for either half
-  uint32_t middle[G];
-#pragma unroll
-  for (int j = 0; j < G; ++j) {
-    middle[j] = g == j ? 0xb780b780u : 0u;
-    asm volatile("" : "+r"(middle[j]));                      // kept, not made again for every product
-  }
+  const uint32_t eight[4] = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};        // -8 2^-24, and 16 times that
   auto scale_sums = [&](float f0, float f1, int nb) {
     om[nb][0] *= f0, om[nb][1] *= f1;
-    om_odd[nb][2] *= f0, om_odd[nb][3] *= f1;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) o[i][nb][0] *= f0, o[i][nb][1] *= f1, o[i][nb][2] *= f0, o[i][nb][3] *= f1;
   };
@@ -310,7 +307,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
         for (int j = 0; j < G; ++j) {
           st[j] *= 16.f;
           top = fmax3(top, fabsf(mid[j]), fabsf(st[j]));
-          mid[j] = fmaf(st[j], 0.46875f, mid[j]);            // low + 7.5 step
+          mid[j] = fmaf(st[j], 0.5f, mid[j]);                // low + 8 step
           st[j] = fmaxf(st[j], 0.f);                         // NaN (a group that is not finite) stays in the middle alone
         }
         const int e = min((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23) - 126, 126);       // all below 2^e
@@ -425,8 +422,8 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
           mx[c] = fmaxf(mx[c], __shfl_xor_sync(0xffffffffu, mx[c], 8));
           mx[c] = fmaxf(mx[c], __shfl_xor_sync(0xffffffffu, mx[c], 16)) * row_mul[nb][c];
         }
-        // exact whatever the reference is, as long as all terms share it: raised only when it is 8 (2^8) behind
-        if (mx[0] > m[nb][0] + kRescaleThreshold || mx[1] > m[nb][1] + kRescaleThreshold) {
+        // exact whatever the reference is, as long as all terms share it: raised only when it is kC4Above behind
+        if (mx[0] > m[nb][0] + kC4Above || mx[1] > m[nb][1] + kC4Above) {
           float alpha[2];
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
@@ -500,8 +497,8 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
             const uint32_t b1 = transpose8x8(pack_pair<__half>(q[2] * st[1][j], q[3] * st[1][j]));
             mma16816<__half>(o[2 * j][nb], a0, b0, b1);
             mma16816<__half>(o[2 * j + 1][nb], a1, b0, b1);
-            mma1688<__half>(j & 1 ? om_odd[nb] : om[nb], middle[j & ~1], middle[j | 1], b0);
-            mma1688<__half>(j & 1 ? om_odd[nb] : om[nb], middle[j & ~1], middle[j | 1], b1);
+            mma16816<__half>(o[2 * j][nb], eight, b0, b1);
+            mma16816<__half>(o[2 * j + 1][nb], eight, b0, b1);
           }
         }
       }
@@ -537,9 +534,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
         float* dst = part + r * D;
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-          // row j: its middles and, of an even group, what the codes are above them; of an odd one the latter in row 8 + j
-          const float mine = om[nb][c] + (g & 1 ? om_odd[nb][c + 2] : 0.f);
-          const float low = __shfl_sync(0xffffffffu, mine, j * 4 + tig) * f;
+          const float low = __shfl_sync(0xffffffffu, om[nb][c], j * 4 + tig) * f;        // row j
 #pragma unroll
           for (int i = 2 * j; i < 2 * j + 2; ++i) {
             dst[i * 16 + g] = fmaf(o[i][nb][c] * 0x1p20f, f, low);        // codes 2^24, steps 2^-4

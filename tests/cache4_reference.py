@@ -8,7 +8,7 @@ h = 2^-11 of fp16, in which the products over codes run:
   - the exponent: the scores are sums over the codes and over the lowest values, fp32 behind exact products, d + 8 additions of one unit
     2^-23 of scale |q| |(|low| + 15 step)| each (norms over the channels), 8 more where the two sums and the row's factor meet; ex2, 2^-21;
   - fp16 numbers below 2^-14: steps and lowest values are off by 2^-24 of the largest of them, top = max (|low|, 16 step) times 2; probabilities, held
-    times 2^6 and at most 2^8 above the reference, by 2^-25 in sums that are at least 2^-2: 2^-22 top per key;
+    times 2^13 and at most 2^2 above the reference, by 2^-25 in sums that are at least 2^11: less than 2^-22 top per key;
   - sums over n keys: n + 16 units 2^-23 of sum p (|low| + 15 step).
 Calls of more than 64 rows per key/value head (`pieces`) round probabilities to fp16, h sum p |v - o|, and 2^-25 per key of the largest value
 below 2^-14; keys and values are in fp16 two numbers each, off by h^2 of an element, in bf16 one number of fp16, off by h of an element and by
