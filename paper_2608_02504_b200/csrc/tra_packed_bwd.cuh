@@ -1265,13 +1265,22 @@ __global__ void __launch_bounds__(256) tra_packed_sinks_kernel(const __grid_cons
     float sum[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) sum[i] = 0.f;
-    for (int c = 0; c < count; ++c) {
-      const float* part = p.sink_part + (((long long)(slot + c) * p.kv_heads + kvh) * p.sinks + key) * (2 * D) + lane * kPer;
+    const long long stride = (long long)p.kv_heads * p.sinks * (2 * D);
+    const float* part = p.sink_part + slot * stride + ((long long)kvh * p.sinks + key) * (2 * D) + lane * kPer;
+    constexpr int kAhead = 8;                  // units whose loads are in flight (one after the other 20 of them took 10 us)
+    for (int c = 0; c < count; c += kAhead, part += kAhead * stride) {
+      float4 x[kAhead][kPer / 4];
 #pragma unroll
-      for (int i = 0; i < kPer; i += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(part + i);
-        sum[i] += x.x, sum[i + 1] += x.y, sum[i + 2] += x.z, sum[i + 3] += x.w;
-      }
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int i = 0; i < kPer / 4; ++i)
+          x[u][i] = c + u < count ? *reinterpret_cast<const float4*>(part + u * stride + 4 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int i = 0; i < kPer / 4; ++i) {
+          sum[4 * i] += x[u][i].x, sum[4 * i + 1] += x[u][i].y, sum[4 * i + 2] += x[u][i].z, sum[4 * i + 3] += x[u][i].w;
+        }
     }
     const long long row = k.begin + key;
     T* out = of_v ? (T*)p.dv + row * p.dv_stride[0] + kvh * p.dv_stride[1] : (T*)p.dk + row * p.dk_stride[0] + kvh * p.dk_stride[1];
