@@ -367,3 +367,40 @@ def test_refusals(api):
             call()
     torch.cuda.synchronize()
     attn.check_status()
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("nq", [1, 12, 100])
+def test_strided_queries_and_outputs(api, dtype, nq):
+    """Queries as a slice of a fused projection or stored heads first, outputs inside a larger tensor: the bits of the contiguous call."""
+    d, hq, hk, m = 128, 6, 2, 700
+    attn = api.PackedAttn(hq, hk, d, dtype=dtype, window=300, sinks=5)
+    cache = api.Cache4(attn, m)
+    cache.write(randn((m, hk, d), dtype, 1), randn((m, hk, d), dtype, 2), torch.arange(m, dtype=torch.int32, device="cuda"))
+    fused = randn((nq, hq + 2 * hk, d), dtype, 3)
+    q, cu = fused[:, :hq], i32([0, nq])
+    kw = dict(k_range=(i32([0]), i32([m])), max_q=nq, max_k=m, want_lse=True)
+    want = attn.forward_cache4(q.contiguous(), cache, cu, **kw)
+    big = torch.full((nq, 2 * hq + 1, d), 9.0, dtype=dtype, device="cuda")
+    got = attn.forward_cache4(q, cache, cu, o=big[:, ::2][:, :hq], **kw)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and (big[:, 1::2] == 9).all()
+    got = attn.forward_cache4(q.transpose(0, 1).contiguous().transpose(0, 1), cache, cu, **kw)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("nq", [1, 90])
+def test_scales_and_shared_keys(api, nq):
+    """Scales far from the usual one; two sequences that share their first keys, whose ranges overlap."""
+    d, hq, hk, m = 64, 4, 2, 500
+    for dtype, scale in ((BF, 3.0), (HALF, 1e-6), (HALF, 0.5)):
+        attn = api.PackedAttn(hq, hk, d, dtype=dtype)
+        cache = api.Cache4(attn, m)
+        k, v = randn((m, hk, d), dtype, 1), randn((m, hk, d), dtype, 2)
+        cache.write(k, v, torch.arange(m, dtype=torch.int32, device="cuda"))
+        q = randn((2 * nq, hq, d), dtype, 3)
+        kb, ke = [0, 0], [m, m - 77]
+        o, lse = attn.forward_cache4(q, cache, i32([0, nq, 2 * nq]), k_range=(i32(kb), i32(ke)), max_q=nq, max_k=m, sm_scale=scale, want_lse=True)
+        want = attention(q, k, v, [0, nq, 2 * nq], kb, ke, 0, 0, scale, nq > 32)
+        check(o, want["o"], want["o_tol"], "o")
+        check(lse, want["lse"], want["lse_tol"], "lse")
+        attn.check_status()
