@@ -815,11 +815,16 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
 // (five of them: 5 us of 12.6).  So a block takes dq_tiles consecutive tiles of a sequence: the next one's Q and dO are loaded, and its
 // first scores formed, under the last steps and the stores of the one before.  Steps are counted through (g), so that every barrier keeps one phase per step
 // or per tile.  Prompts of up to 8,192 tokens, 40 / 8 heads, d 128, window 512: dQ alone 354 us with a tile per block, 319, 305 and 318 with two, four and
-// eight; all gradients 651 -> 605 us (490 TFLOP/s of what is seen; of the rows and keys that a 128-key tile and its queries' windows multiply, 74 % see each
+// eight; all gradients 651 -> 605 us, 625 with second pieces of dS (475 TFLOP/s of what is seen; of the rows and keys that a 128-key tile and its queries' windows multiply, 74 % see each
 // other, and of those of a dQ tile 80 %).
 template <typename T, int D, int kHalves>
 __device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
   using C = BwdCfg<D, kHalves>;
+  // Rounding dS for its product adds as much to dq's error as rounding dq, and the rounding of P in the O that delta is made of a third of that: 1.52 times
+  // the rounding of dq alone, over keys that are few enough for neither to average out.  Every first 32 of 64 keys have their dS in two pieces, which
+  // takes half of its part away (1.42 times) for 2 to 5 % of a training step (d 128, d 64); all of them would cost 6 to 8.
+  constexpr int kRest = C::kSum1 + 32 * kHalves;            // tensor memory: behind dS
+  static_assert(kRest + 16 * kHalves <= C::kColumns, "tensor memory of the second pieces");
   uint8_t* sQ = smem;
   uint8_t* sDO = smem + C::kTileBytes;
   uint8_t* sA = smem + 2 * C::kTileBytes;                   // K tiles
@@ -989,6 +994,9 @@ __device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8
 #pragma unroll
           for (int kk = 0; kk < 4 * kHalves; ++kk)
             tc_mma_ts(tmem + C::kSum0, tmem + C::kSum1 + kk * 8, k_mn + kk * (2048 >> 4), kHi, kIdescD, kk > 0 ? 1u : (i > 0 ? 1u : 0u));
+#pragma unroll
+          for (int kk = 0; kk < 2 * kHalves; ++kk)                          // the second pieces, of every first 32 of 64 keys
+            tc_mma_ts(tmem + C::kSum0, tmem + kRest + kk * 8, k_mn + ((kk >> 1) * 4 + (kk & 1)) * (2048 >> 4), kHi, kIdescD, 1u);
           tc_commit(smem_u32(&ctl->a_free[kd.slot]));
           kd.next();
         }
@@ -1081,6 +1089,7 @@ __device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8
           const uint64_t dp = pack2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
           unpack2(fmul2(pack2(pr[2 * c], pr[2 * c + 1]), kScaled<T> ? ffma2(dp, tau2, neg_delta2) : fadd2(dp, neg_delta2)), t0, t1);
           pk[c] = pack_pair<T>(t0, t1);
+          if (c < 16) s[c] = rest_pair<T>(t0, t1, pk[c]);
         }
         // the product that read the last dS has retired (it also freed that stage)
         if (g > 0) {
@@ -1092,6 +1101,7 @@ __device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8
         }
         tc_fence_after();
         tmem_st32(tmem + lane_base + C::kSum1 + h * 32, pk);
+        tmem_st16(tmem + lane_base + kRest + h * 16, s);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
