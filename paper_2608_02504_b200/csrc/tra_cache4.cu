@@ -545,13 +545,14 @@ Choice4 choose4(const tra_packed_t* h, int n_seq, int max_q, int max_k) {
       longest = more < max_k ? (int)more : max_k;
     }
     // Blocks that fit the GPU at once.  Few units: as many parts as fill it once, each of at least 256 keys, in a cluster where eight
-    // are enough or the cache is short (see choose in tra_packed.cu).  Many units: parts of about 3,072 keys, so that blocks of different
+    // are enough or the cache is short (see choose in tra_packed.cu).  Many units: parts of about 3,328 keys, so that blocks of different
     // lengths spread evenly, and no clusters, whose blocks start and end together (64 caches of up to 32K keys, eight heads: 510 us
-    // whole, 555 in two clustered parts, 405 in two, 335 in eight to eleven).
+    // whole, 555 in two clustered parts, 405 in two, 332 in parts of 3,328, 348 in parts of 2,048; 32 windows of 4,096 keys: 61 whole, 64
+    // to 74 in two to six).
     const long long slots = (long long)(rows <= 8 ? 3 : 2) * h->sm_count;
     const long long units = (long long)n_seq * h->cfg.kv_heads * c.row_tiles;
     const bool many = 2 * units > slots;
-    long long parts = many ? (longest + 1535) / 3072 : slots / units;
+    long long parts = many ? (longest + 1663) / 3328 : slots / units;
     const long long most = ((long long)longest + 255) / 256;
     if (parts > most) parts = most;
     if (!many && parts > kClusterMax && longest <= 1024 * kClusterMax) parts = kClusterMax;

@@ -24,7 +24,7 @@
 // Bound: instruction issue and latency beside HBM (0.625 bytes a channel, against 2): 705 instructions per 32 keys of a head, of which a third
 // turns codes into operands; at the rate at which HBM delivers them, an SM would have to issue 3.3 of its 4 per cycle, and issues 2.3.  A
 // block is four warps that each walk pieces of 32 keys, every fourth one, through a ring of bulk copies of their own (a piece is four runs
-// of bytes): no warp waits for another before the join.  64 caches of 700 to 32,768 keys, 40 / 8 heads, d 128: 338 us, 4.1 TB/s (62 % of the copy rate; the cache
+// of bytes): no warp waits for another before the join.  64 caches of 700 to 32,768 keys, 40 / 8 heads, d 128: 333 us, 4.1 TB/s (63 % of the copy rate; the cache
 // in 16 bits: 646 us).  History: codes as operands with P multiplied in fp16, a producer warp, two clustered parts 424; the rounding above, a ring per warp
 // 561; parts without clusters 334; queries in shared memory 326; the sums of 8 in the others' registers 338.  Four blocks an SM in 128 registers (748 instructions) or the ring's slots unrolled
 // (745): 1 to 2 % less, and 10 to 15 % more for short caches.
