@@ -256,7 +256,8 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      row_mul[nb][c] = p.sm_scale * kLog2e * 0x1p24f * pow2i(__shfl_sync(0xffffffffu, e, (2 * tig + c) * 4) - kC4QLog2);
+      // (never 0, which would make NaN of masked keys: products are below 2^121)
+      row_mul[nb][c] = fmaxf(p.sm_scale * kLog2e * 0x1p24f * pow2i(__shfl_sync(0xffffffffu, e, (2 * tig + c) * 4) - kC4QLog2), 0x1p-149f);
       const int tok = min((row0 + nb * 8 + 2 * tig + c) / p.group, tok1);
       hi[nb][c] = p.order ? min(max(tok + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
     }

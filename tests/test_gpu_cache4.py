@@ -404,3 +404,21 @@ def test_scales_and_shared_keys(api, nq):
         check(o, want["o"], want["o_tol"], "o")
         check(lse, want["lse"], want["lse_tol"], "lse")
         attn.check_status()
+
+
+@pytest.mark.parametrize("q_size,k_size,scale", [(0.0, 0.0, None), (0.0, 1e-8, None), (1e-30, 1e-12, None), (0.0, 1.0, 1e-30), (1e-25, 0.0, 1e-25)])
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("nq,window", [(1, 0), (9, 0), (9, 40), (100, 0), (100, 40)])
+def test_scores_of_zero_and_next_to_it(api, dtype, nq, window, q_size, k_size, scale):
+    """Queries or keys of zeros (a padded row, a cache that is still empty) leave every row the mean of the values it sees."""
+    n, d = 300, 64
+    q = randn((nq, 2, d), dtype, 1) * q_size
+    k, v = randn((n, 1, d), dtype, 2) * k_size, randn((n, 1, d), dtype, 3)
+    attn = api.PackedAttn(2, 1, d, dtype=dtype, window=window)
+    cache = api.Cache4(attn, n)
+    cache.write(k, v, torch.arange(n, dtype=torch.int32, device="cuda"))
+    o, lse = attn.forward_cache4(q, cache, i32([0, nq]), k_range=(i32([0]), i32([n])), max_q=nq, max_k=n, want_lse=True, sm_scale=scale)
+    attn.check_status()
+    want = attention(q, k, v, [0, nq], [0], [n], window, 0, d ** -0.5 if scale is None else scale, 2 * nq > 64, True)
+    check(lse, want["lse"], want["lse_tol"], "lse")
+    check(o, want["o"], want["o_tol"], "o")
