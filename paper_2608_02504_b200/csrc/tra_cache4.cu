@@ -578,7 +578,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 struct Layout4 {
   size_t v, ranges, top, q_mul, q, attn, bytes;
 };
-Layout4 layout4(const tra_packed_t* h, const Choice4& c, int total_q, int max_q) {
+Layout4 layout4(const tra_packed_t* h, const Choice4& c, int n_seq, int total_q, int max_q) {
   const bool bf16 = h->cfg.dtype == TRA_BF16;
   const size_t d = h->cfg.head_dim, kv = h->cfg.kv_heads, heads = h->cfg.heads;
   Layout4 l;
@@ -588,14 +588,18 @@ Layout4 layout4(const tra_packed_t* h, const Choice4& c, int total_q, int max_q)
   l.q_mul = l.top + (bf16 ? round256(sizeof(uint32_t) * 2 * c.seqs * kv) : 0);
   l.q = l.q_mul + (bf16 ? round256(sizeof(float) * total_q * heads) : 0);
   l.attn = l.q + (bf16 ? round256((size_t)total_q * heads * d * 2) : 0);
-  l.bytes = l.attn + tra_packed_attn_workspace_bytes(h, c.seqs, total_q, max_q, c.stride);
+  // (the last pass may hold fewer sequences, which take more parts)
+  const int last = n_seq % c.seqs;
+  const size_t pass = tra_packed_attn_workspace_bytes(h, c.seqs, total_q, max_q, c.stride);
+  const size_t end = last ? tra_packed_attn_workspace_bytes(h, last, total_q, max_q, c.stride) : 0;
+  l.bytes = l.attn + (pass > end ? pass : end);
   return l;
 }
 
 size_t workspace4(const tra_packed_t* h, const Choice4& c, int n_seq, int total_q, int max_q) {
   if (max_q == 0) return 0;
   if (c.direct) return c.splits > 1 && !c.clustered ? sizeof(float) * (size_t)c.splits * total_q * h->cfg.heads * (h->cfg.head_dim + 2) : 0;
-  return layout4(h, c, total_q, max_q).bytes;
+  return layout4(h, c, n_seq, total_q, max_q).bytes;
 }
 
 template <typename T, int D>
@@ -711,7 +715,7 @@ extern "C" int tra_packed_attn_cache4(const tra_packed_t* h, const tra_packed_ar
   // many rows: passes over sequences, keys read back into the workspace
   const bool bf16 = h->cfg.dtype == TRA_BF16;
   const int kv = h->cfg.kv_heads, d = h->cfg.head_dim;
-  const Layout4 l = layout4(h, c, a.total_q, a.max_q);
+  const Layout4 l = layout4(h, c, a.n_seq, a.total_q, a.max_q);
   uint8_t* ws = (uint8_t*)workspace;
   Cache4Expand e;
   memset(&e, 0, sizeof(e));

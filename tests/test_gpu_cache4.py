@@ -422,3 +422,24 @@ def test_scores_of_zero_and_next_to_it(api, dtype, nq, window, q_size, k_size, s
     want = attention(q, k, v, [0, nq], [0], [n], window, 0, d ** -0.5 if scale is None else scale, 2 * nq > 64, True)
     check(lse, want["lse"], want["lse_tol"], "lse")
     check(o, want["o"], want["o_tol"], "o")
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+def test_a_last_pass_of_fewer_sequences(api, dtype):
+    """What is read back at a time holds some of the sequences; the ones that are left are fewer, and their launch takes more parts."""
+    m, nq, d = 200000, 70, 64
+    n_seq = 11 if dtype is BF else 6
+    k, v = randn((m, 1, d), dtype, 1), randn((m, 1, d), dtype, 2)
+    q = randn((n_seq * nq, 1, d), dtype, 3)
+    attn = api.PackedAttn(1, 1, d, dtype=dtype)
+    cache = api.Cache4(attn, m)
+    cache.write(k, v, torch.arange(m, dtype=torch.int32, device="cuda"))
+    begin, end = [7 * s for s in range(n_seq)], [m - 31 * s for s in range(n_seq)]
+    cu = [nq * s for s in range(n_seq + 1)]
+    o, lse = attn.forward_cache4(q, cache, i32(cu), k_range=(i32(begin), i32(end)), max_q=nq, max_k=m, want_lse=True)
+    attn.check_status()
+    for s in (0, n_seq - 2, n_seq - 1):
+        rows = slice(cu[s], cu[s + 1])
+        want = attention(q[rows], k, v, [0, nq], [begin[s]], [end[s]], 0, 0, d ** -0.5, True, True)
+        check(lse[rows], want["lse"], want["lse_tol"], f"lse of {s}")
+        check(o[rows], want["o"], want["o_tol"], f"o of {s}")
