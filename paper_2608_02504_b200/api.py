@@ -672,6 +672,8 @@ class PackedAttn:
     def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, causal=True, window=0, sinks=0):
         if dtype not in (torch.bfloat16, torch.float16):
             raise ValueError("dtype: expected bf16 or fp16")
+        if max(abs(window), abs(sinks)) >= 2 ** 31:               # (a C int would wrap)
+            raise ValueError("window, sinks: expected numbers below 2^31")
         cfg = tra_packed_config_t(heads, kv_heads, head_dim, _DTYPES[dtype], int(causal), window, sinks)
         self._h = ctypes.c_void_p()
         _check(_lib.tra_packed_create(ctypes.byref(self._h), ctypes.byref(cfg)), "tra_packed_create")

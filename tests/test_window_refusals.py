@@ -27,3 +27,9 @@ def test_workspace_follows_the_window():
     size = lambda window: api._lib.tra_packed_attn_workspace_bytes(
         ctypes.byref(Handle(api.tra_packed_config_t(40, 8, 128, 0, 1, window, 0), -7, 148, None)), 1, 1, 1, 100000)
     assert size(0) > 0 and size(100000) == size(0) and size(500) == 0
+
+
+@pytest.mark.parametrize("sizes", [dict(window=2 ** 32 + 5), dict(window=5, sinks=2 ** 32), dict(window=-2 ** 32)])
+def test_numbers_that_a_c_int_would_wrap(sizes):
+    with pytest.raises(ValueError):
+        api.PackedAttn(4, 2, 64, **sizes)
