@@ -470,15 +470,20 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
     p.dk_stride[i] = g->dk_stride[i];
     p.dv_stride[i] = g->dv_stride[i];
   }
+  // Sequences that the window hides nothing of take the window's kernels too, whose dq has second pieces of dS (dq_tiles_block): 1.2 times the error of
+  // rounding dq alone, against 1.51 to 1.53 at d 64, where it costs nothing over long sequences (four of 8,190 tokens: 1.89 ms, causal order 1.90), and
+  // up to 1.58 over a few keys.  Not long ones at d 128 (four of 4,096 tokens, 40 / 8 heads: 2.25 ms against 1.94 for 1.49 times; 64 of 300: 0.52, 0.60).
+  if (h->cfg.window > 0 && p.order == kOrderCausal && (h->cfg.head_dim == 64 || p.max_k <= 1024))
+    p.order = kOrderWindow, p.window = 1 << 30, p.sinks = p.sink_rows = 0;
   p.stream_rows = backward_stream_rows(h);
   p.stream_tokens = p.stream_rows / p.group;
   // dQ blocks of about 24 steps, as long as there are three for every SM (times two where two share one)
-  const long long walked = ((long long)p.sink_rows + p.window + p.tile_tokens) / p.stream_rows + 1;
+  const long long most = (long long)p.sink_rows + p.window + p.tile_tokens, walked = (most < a->max_k ? most : a->max_k) / p.stream_rows + 1;
   const long long tiles = ((long long)a->total_q / p.tile_tokens + 1) * p.kv_heads, three = 3ll * h->sm_count * (p.stream_rows == 64 ? 2 : 1);
   p.dq_tiles = (int)(walked >= 24 ? 1 : 24 / walked);
   while (p.dq_tiles > 1 && tiles / p.dq_tiles < three) --p.dq_tiles;
   const SinkPlan sinks = sink_plan(h, a->total_q);
-  if (p.order == kOrderWindow && sinks.slots > 0) {
+  if (p.order == kOrderWindow && p.sinks > 0 && sinks.slots > 0) {
     p.sink_steps = sinks.steps, p.sink_slots = (int)sinks.slots;
     p.sink_part = (float*)((uint8_t*)workspace + round16(delta_bytes(h, a->total_q)));
   }

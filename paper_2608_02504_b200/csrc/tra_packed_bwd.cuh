@@ -835,7 +835,8 @@ __device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8
 
   // set-up in parallel, one barrier (see the forward kernel)
   if (warp == 0) {
-    const tra_unit u = tra_find_unit(p, false, p.max_q <= unit_tokens, unit_tokens, unit);
+    tra_unit u = tra_find_unit(p, false, p.max_q <= unit_tokens, unit_tokens, unit);
+    u.index = u.count - 1 - u.index;                         // last queries first: the first ones have less to do
     if (lane == 0) ctl->unit = u;
   } else if (warp == C::kSoftWarps + 1) {
     tmem_alloc<C::kColumns>(&ctl->tmem_base);
