@@ -22,7 +22,7 @@ SOURCES = ["tra_plan.cu", "tra_radius.cu", "tra_mask.cu", "tra_attn.cu", "tra_at
            "tra_attn_d64_b64.cu", "tra_attn_d64_b128.cu", "tra_attn_d128_b64.cu", "tra_host.cu", "tra_rotary.cu",
            "tra_packed.cu", "tra_packed_rows.cu", "tra_packed_fwd_d128.cu", "tra_packed_fwd_d64.cu",
            "tra_packed_bwd_d128.cu", "tra_packed_bwd_d64.cu", "tra_packed_fwd_window_d128.cu", "tra_packed_fwd_window_d64.cu",
-           "tra_packed_bwd_window_d128.cu", "tra_packed_bwd_window_d64.cu", "tra_cache4.cu", "tra_cache4_rows.cu",
+           "tra_packed_bwd_window_d128.cu", "tra_packed_bwd_window_d64.cu", "tra_packed_bwd_few_d128.cu", "tra_packed_bwd_few_d64.cu", "tra_cache4.cu", "tra_cache4_rows.cu",
            "tra_packed_fwd_pieces_d128.cu", "tra_packed_fwd_pieces_d64.cu", "tra_packed_fwd_fp16_d128.cu", "tra_packed_fwd_fp16_d64.cu"] + \
           [f"tra_attn_d{d}_any{bn}.cu" for d in (128, 64) for bn in (48, 64, 80, 96, 112, 128)]
 

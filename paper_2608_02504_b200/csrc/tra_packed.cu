@@ -429,6 +429,12 @@ SinkPlan sink_plan(const tra_packed* h, int total_q) {
   }
   return s;
 }
+// Whether no key tile walks streamed tiles of more than 384 rows (one of the first tokens may): all queries', or those that a window's length and
+// the tile's cover.
+bool few_steps(const tra_packed_launch& p) {
+  const long long all = ((long long)p.max_q + p.stream_tokens - 1) / p.stream_tokens, seen = ((long long)p.window + kTileM - 2) / p.stream_tokens + 2;
+  return (all < seen ? all : seen) * p.stream_rows <= 3 * kTileM;
+}
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 // delta, and (fp16) the largest norms behind it
 size_t delta_bytes(const tra_packed* h, int total_q) {
@@ -501,6 +507,9 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
     if ((rc = make_packed_map(&p.map_q_stream, h, qq, qs, q_heads, nq, q_box, p.stream_tokens)) != TRA_OK) return rc;
     if ((rc = make_packed_map(&p.map_do_stream, h, oo, os, q_heads, nq, q_box, p.stream_tokens)) != TRA_OK) return rc;
   }
-  if (p.order == kOrderWindow) return h->cfg.head_dim == 128 ? tra_packed_bwd_window_d128(ctx, p) : tra_packed_bwd_window_d64(ctx, p);
+  if (p.order == kOrderWindow) {
+    if (few_steps(p)) return h->cfg.head_dim == 128 ? tra_packed_bwd_few_d128(ctx, p) : tra_packed_bwd_few_d64(ctx, p);
+    return h->cfg.head_dim == 128 ? tra_packed_bwd_window_d128(ctx, p) : tra_packed_bwd_window_d64(ctx, p);
+  }
   return h->cfg.head_dim == 128 ? tra_packed_bwd_d128(ctx, p) : tra_packed_bwd_d64(ctx, p);
 }

@@ -68,6 +68,8 @@ int tra_packed_fwd_fp16_d128(const tra_packed_ctx& c, const tra_packed_launch& a
 int tra_packed_fwd_fp16_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_window_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_bwd_window_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_bwd_few_d128(const tra_packed_ctx& c, const tra_packed_launch& a);
+int tra_packed_bwd_few_d64(const tra_packed_ctx& c, const tra_packed_launch& a);
 int tra_packed_rows(const tra_packed_ctx& c, const tra_packed_launch& a, int chunk, bool clustered);
 
 #ifdef __CUDACC__

@@ -2,5 +2,5 @@
 #include "tra_packed_bwd.cuh"
 
 int tra_packed_bwd_window_d64(const tra_packed_ctx& c, const tra_packed_launch& a) {
-  return a.stream_rows == 64 ? launch_bwd_window<64, 1>(c, a) : launch_bwd_window<64, 2>(c, a);
+  return a.stream_rows == 64 ? launch_bwd_window<64, 1, false>(c, a) : launch_bwd_window<64, 2, false>(c, a);
 }

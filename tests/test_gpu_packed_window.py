@@ -275,3 +275,24 @@ def test_first_keys_of_long_sequences(api, dtype, d, hq, hk, window, sinks):
     """Sequences whose queries are cut into units for the first keys' gradients, among others that are not; more keys than queries."""
     backward(api, dtype, d, hq, hk, window, sinks, [3, 2500, 0, 130, 1, 1200, 511])
     backward(api, dtype, d, hq, hk, window, sinks, [900, 0, 1500, 20], [1900, 10, 1400, 20])
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("d,hq,hk,window,sinks,lens", [(64, 2, 2, 16, 2, [64, 37]), (128, 4, 4, 200, 0, [100]), (128, 3, 1, 90, 3, [37, 20, 9]), (64, 5, 1, 10, 0, [25, 50]),
+                                                       (64, 2, 1, 4000, 0, [150, 33])])
+def test_gradients_of_few_rows_are_near_their_rounding(api, dtype, d, hq, hk, window, sinks, lens):
+    """Of squared errors, with that of rounding a gradient as 1: rounding dS once would add 1 (it is as large relative to its terms), and the P rounded for
+    the O that delta is made of a third.  In two pieces dS adds 2^-16 of that for dk, and a half at most for dq, whose every second 32 keys have one piece: sqrt(1.34) =
+    1.16 and sqrt(1.84) = 1.36, and 5 % for sums of few terms."""
+    n = sum(lens)
+    q, do = randn((n, hq, d), dtype, 1), randn((n, hq, d), dtype, 4)
+    k, v = randn((n, hk, d), dtype, 2), randn((n, hk, d), dtype, 3)
+    attn = api.PackedAttn(hq, hk, d, dtype=dtype, window=window, sinks=sinks)
+    cu = packed(lens)
+    kw = dict(max_q=max(lens), max_k=max(lens))
+    o, lse = attn.forward(q, k, v, i32(cu), want_lse=True, **kw)
+    dq, dk, _ = attn.backward(do, q, k, v, o, lse, i32(cu), **kw)
+    want = reference(q, k, v, cu, cu[:-1], cu[1:], window, sinks, d ** -0.5, do=do)
+    for got, name, most in ((dq, "dq", 1.36), (dk, "dk", 1.16)):
+        x = want[name]
+        assert (got.double() - x).norm() <= 1.05 * most * (x.to(dtype).double() - x).norm(), name
