@@ -833,9 +833,9 @@ __device__ __forceinline__ void dq_block(const tra_packed_launch& p, uint8_t* sm
 template <typename T, int D, int kHalves>
 __device__ __forceinline__ void dq_tiles_block(const tra_packed_launch& p, uint8_t* smem, const int unit, const int kvh) {
   using C = BwdCfg<D, kHalves>;
-  // Rounding dS for its product adds as much to dq's error as rounding dq, and the rounding of P in the O that delta is made of a third of that: 1.52 times
-  // the rounding of dq alone, over keys that are few enough for neither to average out.  Every first 32 of 64 keys have their dS in two pieces, which
-  // takes half of its part away (1.42 times) for 2 to 5 % of a training step (d 128, d 64); all of them would cost 6 to 8.
+  // Rounding dS for its product adds as much to dq's error as rounding dq, and the rounding of P in the O that delta is made of a third of that: 1.5 times
+  // the rounding of dq alone, over keys that are few enough for neither to average out.  Every first 32 of 64 keys have their dS in two pieces: 1.06 to
+  // 1.31 times, for 2 to 5 % of a training step (d 128, d 64); all of them would cost 6 to 8.
   constexpr int kRest = C::kSum1 + 32 * kHalves;            // tensor memory: behind dS
   static_assert(kRest + 16 * kHalves <= C::kColumns, "tensor memory of the second pieces");
   uint8_t* sQ = smem;
