@@ -18,8 +18,10 @@
 // A code in the low bits of a 16-bit half is the fp16 number n 2^-24, exactly (a subnormal), and one in the next four bits is 16 times
 // that: so one mask takes two codes to two halves, and the factor 16 goes to the other operand (keys: channels of q) or to the
 // result (values: channels of o).  All products are fp16 with fp32 sums, whatever the type of the tensors: q is scaled by a power of two per
-// row that brings its largest element to 2^10, and steps and middles of the values by one, 2^-e, that follows the largest of them so
-// far, so that fp16's range is not an issue: elements 2^-24 times the largest lose precision, which no 16-bit tensor shows.
+// row that brings its largest element to 2^10, and steps and middles of the values by one that follows the largest of them so far (of a
+// warp's keys, all groups): 16 steps are held below 1, for their products with probabilities of up to 2^15, and middles below 1.5 2^14.  So middles
+// keep 11 bits down to 2^-28 of the largest, which covers the normal numbers of fp16 tensors; bf16 values further apart than that lose bits.  (Middles held
+// below 1.5: a group 2^-16 of another 6.3e-3 off instead of 4.5e-4 in fp16, and values of 0.01 0.2 off beside a weightless one of 6e4.)
 //
 // Bound: instruction issue and latency beside HBM (0.625 bytes a channel, against 2): 705 instructions per 32 keys of a head, of which a third
 // turns codes into operands; at the rate at which HBM delivers them, an SM would have to issue 3.3 of its 4 per cycle, and issues 2.3.  A
@@ -42,6 +44,7 @@ constexpr int kC4Tile = kC4Piece * kC4Warps;
 // 2^6: 4.2e-4 off over 20,000 fp16 keys, most of whose probabilities were subnormal; so: 2.8e-4.)
 constexpr int kC4ProbLog2 = 13;
 constexpr float kC4Above = 2.f;
+constexpr int kC4MidLog2 = 14;            // middles of the values: see above
 constexpr int kC4QLog2 = 10;              // rows of q: largest element in [2^9, 2^10)
 
 template <int D>
@@ -199,7 +202,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
       for (int i = 0; i < D / 16; ++i) o[i][nb][c] = 0.f;
     }
   }
-  int e_run = -120;                                          // values are held times 2^-e_run
+  int e_run = -112;                                          // steps are held times 2^-e_run, middles times 2^(14 - e_run)
 
   // ---- queries as the second operand: column g of a product is row 8 nb + g
   constexpr int kPieces = std::is_same<T, __nv_bfloat16>::value ? 3 : 2;        // of the group sums, in T
@@ -318,13 +321,13 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) scale_sums(f, f, nb);
         }
-        const float mul = pow2i(-e_run);
+        const float mul = pow2i(-e_run), mul_mid = pow2i(kC4MidLog2 - e_run);
         const int r = lane & 7, logical = c4_row(r), half = (lane >> 3) & 1, sub = lane >> 4;
         __half* mid_at = v_mid + (sub * 4 + (logical >> 1)) * 4 + half * 2 + (logical & 1);
 #pragma unroll
         for (int j = 0; j < G; ++j) {
           st[j] *= mul;
-          mid_at[j * kC4Piece] = __float2half_rn(mid[j] * mul);
+          mid_at[j * kC4Piece] = __float2half_rn(mid[j] * mul_mid);
         }
         // in the order of the products' rows
         const int at = ((lane & ~7) + logical) * G;
@@ -526,7 +529,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
     if (!clustered) return;
   }
   rows_join<T, D, kC4Warps, kC4Threads, 8 * NB>(p, {qr, kvh, row0, n_rows, parts, clustered != 0}, (float*)smem, [&](float* part, float* stat) {
-    const float f = pow2i(e_run);
+    const float f = pow2i(e_run), f_mid = pow2i(e_run - kC4MidLog2);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -535,7 +538,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
         float* dst = part + r * D;
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-          const float low = __shfl_sync(0xffffffffu, om[nb][c], j * 4 + tig) * f;        // row j
+          const float low = __shfl_sync(0xffffffffu, om[nb][c], j * 4 + tig) * f_mid;    // row j
 #pragma unroll
           for (int i = 2 * j; i < 2 * j + 2; ++i) {
             dst[i * 16 + g] = fmaf(o[i][nb][c] * 0x1p20f, f, low);        // codes 2^24, steps 2^-4
