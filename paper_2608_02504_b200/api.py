@@ -829,7 +829,8 @@ class PackedAttn:
         if k_range is None:
             raise ValueError("k_range: expected (begin, end)")
         a = self._args(q, None, None, o, lse, None, cu_q, None, k_range, max_q, max_k, sm_scale, cached=cache.tokens)
-        n = _lib.tra_packed_attn_cache4_workspace_bytes(self._h, cu_q.shape[0] - 1, q.shape[0], max_q, max_k)
+        # (a larger max_k is refused by the call; its workspace might not fit the GPU)
+        n = _lib.tra_packed_attn_cache4_workspace_bytes(self._h, cu_q.shape[0] - 1, q.shape[0], max_q, max_k) if max_k <= cache.tokens else 0
         ws = q.new_empty((n,), dtype=torch.uint8) if n else None
         _check(_lib.tra_packed_attn_cache4(self._h, a, cache._desc(), ws.data_ptr() if n else None, n, _raw_stream(self._index)),
                "tra_packed_attn_cache4")

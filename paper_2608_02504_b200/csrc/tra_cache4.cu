@@ -677,6 +677,7 @@ extern "C" int tra_cache4_read(const tra_packed_t* h, const tra_cache4_t* c, voi
 
 extern "C" size_t tra_packed_attn_cache4_workspace_bytes(const tra_packed_t* h, int n_seq, int total_q, int max_q, int max_k) {
   if (!h || n_seq < 1 || total_q < 0 || max_q < 0 || max_k < 0 || max_q > total_q) return 0;
+  if (total_q > (1 << 30) || max_k > (1 << 30)) return 0;    // sizes that the call refuses
   return workspace4(h, choose4(h, n_seq, max_q, max_k), n_seq, total_q, max_q);
 }
 
