@@ -392,6 +392,7 @@ struct Cache4Expand {
   __half* q;                   //       [total_q][heads][d]
   float* q_mul;                //       [total_q][heads]
   int step_blocks;             //       blocks of a (sequence, head, side) that look at its steps
+  bool wide;                   // k and v start on 32 bytes (a workspace need not); their rows then do
 };
 
 // A sequence's keys as the launches of a pass see them.
@@ -507,8 +508,8 @@ __global__ void __launch_bounds__(256) tra_cache4_expand_kernel(const __grid_con
   });
   if (v0 >= range.len) return;
   T* dst = (T*)(of_v ? e.v : e.k) + (((long long)seq * e.stride + v0) * (kFp16 ? 2 : 1) * p.kv_heads + head) * D + j * kCacheGroup;
-  store64(dst, true, v);
-  if constexpr (kFp16) store64(dst + (long long)p.kv_heads * D, true, rest);
+  store64(dst, e.wide, v);
+  if constexpr (kFp16) store64(dst + (long long)p.kv_heads * D, e.wide, rest);
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -724,6 +725,7 @@ extern "C" int tra_packed_attn_cache4(const tra_packed_t* h, const tra_packed_ar
   if (e.a.order != kOrderWindow) e.a.sink_rows = 0;
   e.k_codes = (const uint8_t*)cache->k, e.v_codes = (const uint8_t*)cache->v, e.k_step = cache->k_step, e.v_step = cache->v_step;
   e.k = ws, e.v = ws + l.v;
+  e.wide = !((uintptr_t)ws & 31);
   e.begin = (int32_t*)(ws + l.ranges), e.end = e.begin + c.seqs;
   e.top = (uint32_t*)(ws + l.top), e.q_mul = (float*)(ws + l.q_mul), e.q = (__half*)(ws + l.q);
   e.stride = c.stride;
