@@ -456,8 +456,8 @@ typedef struct {
 int tra_cache4_write(const tra_packed_t* packed, const tra_cache4_t* cache, const void* k, const void* v, const int64_t* k_stride,
                      const int64_t* v_stride, const int32_t* slots, int n, void* stream);
 
-/* The way back: rows slots[i] of the cache, rounded once to the type, to token i of k and v.  Tokens of slots that are left out stay as
- * they are.  A slot may be named several times. */
+/* The way back: rows slots[i] of the cache, rounded once to the type (to its largest number where low + 15 step passes that), to token i of k
+ * and v.  Tokens of slots that are left out stay as they are.  A slot may be named several times. */
 int tra_cache4_read(const tra_packed_t* packed, const tra_cache4_t* cache, void* k, void* v, const int64_t* k_stride, const int64_t* v_stride,
                     const int32_t* slots, int n, void* stream);
 

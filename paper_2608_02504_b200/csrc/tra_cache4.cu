@@ -313,12 +313,13 @@ __global__ void __launch_bounds__(256) tra_cache4_write_kernel(const __grid_cons
 
 // ------------------------------------------------------------------------------------ read
 // A group's values, rounded once: code * step + low is one fused multiply-add of the type.  Pairs of codes become pairs of numbers by an OR
-// with a power of two that is taken off again (fp16: 1024 + n, bf16: 128 + n, both exact).
+// with a power of two that is taken off again (fp16: 1024 + n, bf16: 128 + n, both exact).  Of a range next to the type's own, low + 15 step passes the
+// largest number by what the step was rounded up (-65504 and 65504 in fp16: 65536): it becomes that number.  A group that is not finite stays NaN.
 template <typename T>
 __device__ __forceinline__ uint32_t value_pair(uint32_t codes, uint32_t step2, uint32_t low2) {
   constexpr bool kHalf = std::is_same<T, __half>::value;
   const auto n = __hsub2(as_pair<T>(codes | (kHalf ? 0x64006400u : 0x43004300u)), as_pair<T>(kHalf ? 0x64006400u : 0x43004300u));
-  return as_bits<T>(__hfma2(n, as_pair<T>(step2), as_pair<T>(low2)));
+  return as_bits<T>(__hmin2_nan(__hfma2(n, as_pair<T>(step2), as_pair<T>(low2)), as_pair<T>(kHalf ? 0x7bff7bffu : 0x7f7f7f7fu)));
 }
 
 // A lane's share of a row: codes 16 j .. of the row, and group j's step and lowest value.
