@@ -18,10 +18,11 @@
 // A code in the low bits of a 16-bit half is the fp16 number n 2^-24, exactly (a subnormal), and one in the next four bits is 16 times
 // that: so one mask takes two codes to two halves, and the factor 16 goes to the other operand (keys: channels of q) or to the
 // result (values: channels of o).  All products are fp16 with fp32 sums, whatever the type of the tensors: q is scaled by a power of two per
-// row that brings its largest element to 2^10, and steps and middles of the values by one that follows the largest of them so far (of a
-// warp's keys, all groups): 16 steps are held below 1, for their products with probabilities of up to 2^15, and middles below 1.5 2^14.  So middles
-// keep 11 bits down to 2^-28 of the largest, which covers the normal numbers of fp16 tensors; bf16 values further apart than that lose bits.  (Middles held
-// below 1.5: a group 2^-16 of another 6.3e-3 off instead of 4.5e-4 in fp16, and values of 0.01 0.2 off beside a weightless one of 6e4.)
+// row that brings its largest element to 2^10, and steps and middles of the values by one that follows the largest value so far (of a
+// warp's keys, all groups), 2^e above it: the range 15 step is below 2 2^e, so that 8 steps are held below 16 / 15, for their products with
+// probabilities of up to 2^15, and middles below 2^15.  So middles keep 11 bits down to 2^-29 of the largest value, which covers the normal numbers of fp16
+// tensors; bf16 values further apart than that lose bits.  (Middles held below 1.5: values of 0.01 were 0.08 to 0.25 of their norm off beside one of 6e4 that the
+// order hides; so: 2.8e-4, where the result's rounding alone makes 2.0e-4.)
 //
 // Bound: instruction issue and latency beside HBM (0.625 bytes a channel, against 2): 705 instructions per 32 keys of a head, of which a third
 // turns codes into operands; at the rate at which HBM delivers them, an SM would have to issue 3.3 of its 4 per cycle, and issues 2.3.  A
@@ -44,7 +45,7 @@ constexpr int kC4Tile = kC4Piece * kC4Warps;
 // 2^6: 4.2e-4 off over 20,000 fp16 keys, most of whose probabilities were subnormal; so: 2.8e-4.)
 constexpr int kC4ProbLog2 = 13;
 constexpr float kC4Above = 2.f;
-constexpr int kC4MidLog2 = 14;            // middles of the values: see above
+constexpr int kC4MidLog2 = 15, kC4StepLog2 = 3;        // middles and steps of the values: see above
 constexpr int kC4QLog2 = 10;              // rows of q: largest element in [2^9, 2^10)
 
 template <int D>
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
       for (int i = 0; i < D / 16; ++i) o[i][nb][c] = 0.f;
     }
   }
-  int e_run = -112;                                          // steps are held times 2^-e_run, middles times 2^(14 - e_run)
+  int e_run = -111;                                          // middles are held times 2^(15 - e_run), steps times 2^(3 - e_run)
 
   // ---- queries as the second operand: column g of a product is row 8 nb + g
   constexpr int kPieces = std::is_same<T, __nv_bfloat16>::value ? 3 : 2;        // of the group sums, in T
@@ -309,19 +310,18 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
         }
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-          st[j] *= 16.f;
-          top = fmax3(top, fabsf(mid[j]), fabsf(st[j]));
-          mid[j] = fmaf(st[j], 0.5f, mid[j]);                // low + 8 step
+          top = fmax3(top, fabsf(mid[j]), fabsf(fmaf(st[j], 15.f, mid[j])));        // lowest and largest value (infinite: 2^128)
+          mid[j] = fmaf(st[j], 8.f, mid[j]);                 // low + 8 step
           st[j] = fmaxf(st[j], 0.f);                         // NaN (a group that is not finite) stays in the middle alone
         }
-        const int e = min((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23) - 126, 126);       // all below 2^e
+        const int e = min((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23) - 126, 128);       // all below 2^e
         if (e > e_run) {
           const float f = ex2((float)(e_run - e));
           e_run = e;
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) scale_sums(f, f, nb);
         }
-        const float mul = pow2i(-e_run), mul_mid = pow2i(kC4MidLog2 - e_run);
+        const float mul = pow2i(kC4StepLog2 - e_run), mul_mid = pow2i(kC4MidLog2 - e_run);
         const int r = lane & 7, logical = c4_row(r), half = (lane >> 3) & 1, sub = lane >> 4;
         __half* mid_at = v_mid + (sub * 4 + (logical >> 1)) * 4 + half * 2 + (logical & 1);
 #pragma unroll
@@ -529,7 +529,12 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
     if (!clustered) return;
   }
   rows_join<T, D, kC4Warps, kC4Threads, 8 * NB>(p, {qr, kvh, row0, n_rows, parts, clustered != 0}, (float*)smem, [&](float* part, float* stat) {
-    const float f = pow2i(e_run), f_mid = pow2i(e_run - kC4MidLog2);
+    // To the values' own scale.  Sums of numbers next to the type's largest would pass fp32 before they are divided: there the whole part is held times
+    // 2^-20, its reference as much above.
+    const int room = e_run > 96 ? 20 : 0;
+    const float f = pow2i(e_run - kC4MidLog2 - room), f_l = pow2i(-kC4ProbLog2 - room);
+    constexpr float kProb = 1.f / (1 << kC4ProbLog2);
+    constexpr float kSteps = kProb * 0x1p24f * (1 << (kC4MidLog2 - kC4StepLog2));       // (codes are held times 2^-24)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -538,18 +543,18 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
         float* dst = part + r * D;
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-          const float low = __shfl_sync(0xffffffffu, om[nb][c], j * 4 + tig) * f_mid;    // row j
+          const float low = __shfl_sync(0xffffffffu, om[nb][c], j * 4 + tig) * kProb * f;        // row j
 #pragma unroll
           for (int i = 2 * j; i < 2 * j + 2; ++i) {
-            dst[i * 16 + g] = fmaf(o[i][nb][c] * 0x1p20f, f, low);        // codes 2^24, steps 2^-4
-            dst[i * 16 + g + 8] = fmaf(o[i][nb][c + 2] * 0x1p16f, f, low);
+            dst[i * 16 + g] = fmaf(o[i][nb][c] * kSteps, f, low);
+            dst[i * 16 + g + 8] = fmaf(o[i][nb][c + 2] * (kSteps * 0.0625f), f, low);
           }
         }
         if (g == 0) {
           float* st = stat + r * 4;
-          st[0] = m[nb][c] - kC4ProbLog2;
-          st[1] = gave_up ? 0.f : l[nb][c];
-          st[2] = l[nb][c];
+          st[0] = m[nb][c] + (float)room;
+          st[1] = gave_up ? 0.f : l[nb][c] * f_l;
+          st[2] = l[nb][c] * f_l;
         }
       }
   });

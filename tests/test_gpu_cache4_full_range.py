@@ -1,0 +1,38 @@
+"""Groups that span the whole range of the type: attention over them stays finite."""
+import pytest
+import torch
+
+from tests.cache4_reference import values
+from tests.packed_reference import i32
+
+pytestmark = pytest.mark.gpu
+BF, HALF = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2608_02504_b200 import api as a
+    return a
+
+
+@pytest.mark.parametrize("m", [1, 3, 40])
+@pytest.mark.parametrize("nq", [1, 2, 70])
+@pytest.mark.parametrize("dtype", [BF, HALF])
+def test_values_of_the_whole_range(api, dtype, nq, m):
+    """One key takes all: o is its values, rounded, within 2^-11 of the largest for the roundings of the middle and of the step, or of the multiple."""
+    d = 64
+    most = torch.finfo(dtype).max
+    x = torch.rand(m, 1, d, device="cuda", generator=torch.Generator("cuda").manual_seed(1)) * 2 - 1
+    v = (x.double() * 0.96 * most).to(dtype)
+    v[:, 0, 3], v[:, 0, 40] = 0.96 * most, -0.96 * most
+    q, k = torch.full((nq, 1, d), 8.0, dtype=dtype, device="cuda"), torch.full((m, 1, d), -8.0, dtype=dtype, device="cuda")
+    k[0] = 8.0
+    attn = api.PackedAttn(64 if nq > 2 else 1, 1, d, dtype=dtype, causal=False)
+    q = q.expand(nq, attn.heads, d).contiguous()
+    cache = api.Cache4(attn, m)
+    cache.write(k, v, torch.arange(m, dtype=torch.int32, device="cuda"))
+    o, _ = attn.forward_cache4(q, cache, i32([0, nq]), k_range=(i32([0]), i32([m])), max_q=nq, max_k=m)
+    attn.check_status()
+    want = values(v[0, 0])
+    assert o.isfinite().all()
+    assert ((o.double() - want).abs() <= torch.finfo(dtype).eps / 2 * want.abs() * (1 + 2.0 ** -8) + 2 * 2.0 ** -11 * most).all()
