@@ -77,7 +77,7 @@ namespace {
 
 // The power of two that brings numbers of up to `top` below 2^15, where fp16 holds the most of them.
 __device__ __forceinline__ float tra_fp16_mul(float top) {
-  const int e = min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 127);        // top < 2^e
+  const int e = min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 128);        // top < 2^e
   return __uint_as_float((uint32_t)(127 + 15 - e) << 23);
 }
 __device__ __forceinline__ float tra_inverse_pow2(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }

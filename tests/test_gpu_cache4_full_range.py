@@ -4,6 +4,7 @@ import torch
 
 from tests.cache4_reference import values
 from tests.packed_reference import i32
+from tests.test_gpu_cache4_values import attend
 
 pytestmark = pytest.mark.gpu
 BF, HALF = torch.bfloat16, torch.float16
@@ -36,3 +37,16 @@ def test_values_of_the_whole_range(api, dtype, nq, m):
     want = values(v[0, 0])
     assert o.isfinite().all()
     assert ((o.double() - want).abs() <= torch.finfo(dtype).eps / 2 * want.abs() * (1 + 2.0 ** -8) + 2 * 2.0 ** -11 * most).all()
+
+
+def test_many_rows_of_values_past_the_largest_number(api):
+    """low + 15 step of a group next to the type's range, 1.4 % above the largest number: its multiple has to be one of fp16 as well."""
+    nq, d = 70, 64
+    most = torch.finfo(BF).max
+    v = torch.zeros(2, 1, d, dtype=BF, device="cuda")
+    v[0, 0, ::2], v[0, 0, 1::2] = most, -most * (1 - 26 * 2.0 ** -8)
+    q, k = torch.zeros(nq, 1, d, dtype=BF, device="cuda"), torch.zeros(2, 1, d, dtype=BF, device="cuda")
+    o = attend(api, q, k, v, causal=False)
+    want = values(v).mean(0)
+    assert values(v).max() > 1.01 * most
+    assert ((o.double() - want).abs() <= (2.0 ** -9 + 2.0 ** -11) * want.abs() * (1 + 2.0 ** -8)).all()

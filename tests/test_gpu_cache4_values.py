@@ -16,9 +16,9 @@ def api():
     return a
 
 
-def attend(api, q, k, v):
+def attend(api, q, k, v, causal=True):
     (n, hq, d), (m, hk) = q.shape, k.shape[:2]
-    attn = api.PackedAttn(hq, hk, d, dtype=q.dtype)
+    attn = api.PackedAttn(hq, hk, d, dtype=q.dtype, causal=causal)
     cache = api.Cache4(attn, m)
     cache.write(k, v, torch.arange(m, dtype=torch.int32, device="cuda"))
     o, _ = attn.forward_cache4(q, cache, i32([0, n]), k_range=(i32([0]), i32([m])), max_q=n, max_k=m)
