@@ -18,7 +18,8 @@
 // A code in the low bits of a 16-bit half is the fp16 number n 2^-24, exactly (a subnormal), and one in the next four bits is 16 times
 // that: so one mask takes two codes to two halves, and the factor 16 goes to the other operand (keys: channels of q) or to the
 // result (values: channels of o).  All products are fp16 with fp32 sums, whatever the type of the tensors: q is scaled by a power of two per
-// row that brings its largest element to 2^10, and steps and middles of the values by one that follows the largest value so far (of a
+// row that brings its largest element to 2^15 (bf16 elements keep their 8 bits down to 2^-29 of it, fp16 ones their 11 down to 2^-25; from 2^10 a group of
+// fp16 queries 2^-20 of another, on keys as much larger, took o 1.1e-3 off, from 2^15 2.5e-4, as if all were alike), and steps and middles of the values by one that follows the largest value so far (of a
 // warp's keys, all groups), 2^e above it: the range 15 step is below 2 2^e, so that 8 steps are held below 16 / 15, for their products with
 // probabilities of up to 2^15, and middles below 2^15.  So middles keep 11 bits down to 2^-29 of the largest value, which covers the normal numbers of fp16
 // tensors; bf16 values further apart than that lose bits.  (Middles held below 1.5: values of 0.01 were 0.08 to 0.25 of their norm off beside one of 6e4 that the
@@ -46,7 +47,7 @@ constexpr int kC4Tile = kC4Piece * kC4Warps;
 constexpr int kC4ProbLog2 = 13;
 constexpr float kC4Above = 2.f;
 constexpr int kC4MidLog2 = 15, kC4StepLog2 = 3;        // middles and steps of the values: see above
-constexpr int kC4QLog2 = 10;              // rows of q: largest element in [2^9, 2^10)
+constexpr int kC4QLog2 = 15;              // rows of q: largest element in [2^14, 2^15)
 
 template <int D>
 struct C4Cfg {
@@ -206,7 +207,11 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
   int e_run = -111;                                          // middles are held times 2^(15 - e_run), steps times 2^(3 - e_run)
 
   // ---- queries as the second operand: column g of a product is row 8 nb + g
-  constexpr int kPieces = std::is_same<T, __nv_bfloat16>::value ? 3 : 2;        // of the group sums, in T
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  constexpr int kPieces = kBf16 ? 3 : 2;                     // of the group sums, in T
+  // Their products with the lowest values join those with the codes, which are held times 2^-24.  Sums of up to 2^20 are
+  // brought into fp16's range.
+  constexpr float kSumMul = 0x1p-5f, kLowMul = 0x1p-24f / kSumMul;
   // (in shared memory: registers are what limits the blocks of an SM)
   uint32_t qs[NB][2];
   float row_mul[NB][2];                                      // to scores in base 2, codes' factor 2^24 included
@@ -247,7 +252,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
       // piece x of group j is row x G + j of the operand: rows 2 tig, 2 tig + 1 in one register, 8 more in the other
-      float left = sum;
+      float left = sum * kSumMul;
 #pragma unroll
       for (int x = 0; x < kPieces; ++x) {
         const int at = x * G + j;
@@ -372,7 +377,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
             mma1688<T>(c, low0, low1, qs[nb][0]);
             if (kPieces * G > 8) mma1688<T>(c, low0, low1, qs[nb][1]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[sub][nb][i] = c[i] * 0x1p-24f;
+            for (int i = 0; i < 4; ++i) s[sub][nb][i] = c[i] * kLowMul;
           }
         }
 #pragma unroll
