@@ -209,9 +209,9 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
   // ---- queries as the second operand: column g of a product is row 8 nb + g
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   constexpr int kPieces = kBf16 ? 3 : 2;                     // of the group sums, in T
-  // Their products with the lowest values join those with the codes, which are held times 2^-24.  Sums of up to 2^20 are
-  // brought into fp16's range.
-  constexpr float kSumMul = 0x1p-5f, kLowMul = 0x1p-24f / kSumMul;
+  // Their products with the lowest values join those with the codes, which are held times 2^-24.  fp16: sums of up to 2^20 are brought into its range.  bf16:
+  // times 2^-23 no lowest value takes a product past fp32 (times 2^-24 the loop has one factor less and the compiler lays it out worse: 335 us for 333).
+  constexpr float kSumMul = kBf16 ? 0x1p-23f : 0x1p-5f, kLowMul = 0x1p-24f / kSumMul;
   // (in shared memory: registers are what limits the blocks of an SM)
   uint32_t qs[NB][2];
   float row_mul[NB][2];                                      // to scores in base 2, codes' factor 2^24 included
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int e = min(max((int)(__float_as_uint(top) >> 23) - 126, -90), 128);        // |q| < 2^e
+    const int e = min(max((int)(__float_as_uint(top) >> 23) - 126, -110), 128);       // |q| < 2^e
     const float mul = pow2i(kC4QLog2 - e);
     qs[nb][0] = qs[nb][1] = 0u;
 #pragma unroll
@@ -265,8 +265,9 @@ __global__ void __launch_bounds__(kC4Threads, NB == 1 ? 3 : 2)
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      // (never 0, which would make NaN of masked keys: products are below 2^121)
-      row_mul[nb][c] = fmaxf(p.sm_scale * kLog2e * 0x1p24f * pow2i(__shfl_sync(0xffffffffu, e, (2 * tig + c) * 4) - kC4QLog2), 0x1p-149f);
+      // (never 0, which would make NaN of masked keys: products are below 2^128; nor infinite, which would of scores of 0)
+      const float mul_c = p.sm_scale * kLog2e * 0x1p24f * pow2i(__shfl_sync(0xffffffffu, e, (2 * tig + c) * 4) - kC4QLog2);
+      row_mul[nb][c] = fminf(fmaxf(mul_c, 0x1p-149f), 0x1.fffffep127f);
       const int tok = min((row0 + nb * 8 + 2 * tig + c) / p.group, tok1);
       hi[nb][c] = p.order ? min(max(tok + 1 + ahead - axis.gap, 0), axis.len) : kr.len;
     }

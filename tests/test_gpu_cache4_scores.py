@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from tests.cache4_norms import attention, check_norm
+from tests.cache4_reference import values
 from tests.packed_reference import randn
 from tests.test_gpu_cache4_values import attend
 
@@ -29,3 +30,24 @@ def test_small_queries_meet_large_keys(api, dtype, log2, d, nq):
     q[..., 32:64] *= 2.0 ** -log2
     k[..., 32:64] *= 2.0 ** log2
     check_norm(attend(api, q, k, v), attention(q, k, v, many=nq * hq // hk > 64), "o")
+
+
+@pytest.mark.parametrize("nq", [1, 3, 70])
+@pytest.mark.parametrize("q_size,k_size", [(1e-35, 1e35), (1e35, 1e-35), (1e-20, 1e20), (1e20, 1e-20)])
+def test_queries_and_keys_at_the_ends_of_the_range(api, q_size, k_size, nq):
+    m, hq, hk, d = 300, 4, 2, 64
+    q, k, v = randn((nq, hq, d), BF, 1, 1.5 * q_size), randn((m, hk, d), BF, 2, k_size), randn((m, hk, d), BF, 3)
+    check_norm(attend(api, q, k, v), attention(q, k, v, many=nq * hq // hk > 64), "o")
+
+
+@pytest.mark.parametrize("nq", [1, 3])
+def test_the_largest_queries(api, nq):
+    """Scores of 0 beside ones of 2^130: the largest takes all."""
+    m, d = 40, 64
+    q = torch.full((nq, 2, d), 2.0 ** 126, dtype=BF, device="cuda")
+    k, v = torch.zeros(m, 1, d, dtype=BF, device="cuda"), randn((m, 1, d), BF, 3)
+    k[5], k[6] = 1.0, -1.0
+    o = attend(api, q, k, v).double()
+    want = values(v[5, 0])
+    # P is 1: the result's rounding, and that of the middle and of the step in fp16
+    assert ((o - want).abs() <= 2.0 ** -8 * want.abs() + 2 * 2.0 ** -11 * v.abs().max() * 2).all()
