@@ -8,6 +8,9 @@
  * (a cudaStream_t passed as void*, NULL = default stream) and return a status
  * code; none of them synchronises the device or throws.
  *
+ * The structures carry neither size nor version, and new fields come at their ends: a caller is compiled against the header of the library that it
+ * loads, and clears a structure before it fills the fields it knows.
+ *
  * Token order.  N = T*H*W video tokens.  Every token-indexed array handed to the
  * four hot calls is in TILE-MAJOR order (Section 3.3, "Flash Radius Mask Kernel":
  * each H x W frame is cut into tile_h x tile_w tiles, edge tiles clipped; tokens
@@ -424,6 +427,9 @@ int tra_packed_attn(const tra_packed_t* packed, const tra_packed_args_t* args, v
  * inside one thread block: the same bits every time.  d_o outside the sequences may be anything.
  * fp16: the probabilities and their gradients are rounded for their products as multiples by powers of two that follow the
  * largest rows of d_o and v of a key/value head, so that the relative precision does not depend on the size of d_o.
+ * The launch follows from max_q, max_k and total_q, not from the lengths, and with a window so does how dS is rounded for its products: dq is 1.1 to 1.3 times as
+ * far off as its own rounding, but 1.5 times at head_dim 128 where max_k is above 1,024 and the window hides nothing of that many keys; dk
+ * is 1.05 times where the window or max_q spans at most three tiles of 128 rows, else 1.4 to 1.6 over a few dozen keys.  Loose bounds cost that much, and time.
  *   workspace: device memory of tra_packed_attn_backward_workspace_bytes, as for the forward call. */
 typedef struct {
   const void* d_o;        /* the gradient of o */
@@ -441,7 +447,7 @@ int tra_packed_attn_backward(const tra_packed_t* packed, const tra_packed_args_t
 /* Heads, head_dim and type are those of a tra_packed_t.  A row (one token of one key/value head) is held in groups of 32 channels:
  *   low = the group's smallest element, step = the smallest number of the type with 15 step >= largest - low,
  *   code = floor((x - low) / step + 1/2) in 0 .. 15; it stands for low + code step, so that it is off by step / 2 at most.
- * A group that holds a NaN or an infinity reads back as NaN.  Where the codes lie inside a row is the library's affair: rows are
+ * Differences and quotients are fp32's, and a quotient less than 2^-22 of itself below a half may go up: step / 2 (1 + 2^-16) at most.  A group that holds a NaN or an infinity reads back as NaN.  Where the codes lie inside a row is the library's affair: rows are
  * written and read by these calls.  A row takes d / 2 + d / 8 bytes, for keys and for values each. */
 typedef struct {
   void *k, *v;             /* [kv_heads, tokens, d / 2] bytes, 16-byte aligned                                          */
@@ -464,8 +470,9 @@ int tra_cache4_read(const tra_packed_t* packed, const tra_cache4_t* cache, void*
 /* Attention over the cache: tra_packed_attn with the values that the codes stand for as keys and values (not rounded to the type; where a
  * sequence has more than 64 rows per key/value head, they are read back, rounded, into the workspace first, half a gigabyte or one sequence
  * at a time).  k_begin, k_end: rows of the cache.  args->k, v and their strides are not used, total_k is the cache's tokens; o_rest must be
- * NULL (there are no gradients with respect to a cache).  What lies in rows outside the sequences' ranges may be anything.  Workspace,
- * status and errors as for tra_packed_attn. */
+ * NULL (there are no gradients with respect to a cache).  What lies in rows outside the sequences' ranges may be anything.  Products are fp16's,
+ * of multiples that follow a head's largest value and a row's largest query element: bf16 values 2^-26 and query elements 2^-24 of the largest, hidden keys
+ * included, begin to lose bits.  Workspace, status and errors as for tra_packed_attn; the workspace query is 0 for sizes that the call refuses. */
 size_t tra_packed_attn_cache4_workspace_bytes(const tra_packed_t* packed, int n_seq, int total_q, int max_q, int max_k);
 int tra_packed_attn_cache4(const tra_packed_t* packed, const tra_packed_args_t* args, const tra_cache4_t* cache, void* workspace,
                            size_t workspace_bytes, void* stream);

@@ -189,7 +189,7 @@ __device__ __forceinline__ void row_to_value_pairs(uint32_t* w, uint32_t* p, int
 
 // ------------------------------------------------------------------------------------ write
 // Of a group of 32 channels x: low = min x, step = the smallest number of the type with 15 step >= max x - low, code = floor((x - low) / step + 1/2)
-// (so that |x - (low + code step)| <= step / 2).  A group that holds a NaN or an infinity gets a step and a lowest value of NaN.
+// (so that |x - (low + code step)| <= step / 2, times 1 + 2^-16 for what follows).  A group that holds a NaN or an infinity gets a step and a lowest value of NaN.
 //
 // The quotient is a product with the reciprocal, taken 2^-22 too large so that halves go up, added to 1.5 2^23, where the last bit is 1 and the
 // rounding to a whole number is the addition's.  (A quotient less than 2^-22 of itself below a half goes up as well.  Differences and

@@ -18,7 +18,7 @@
 // A code in the low bits of a 16-bit half is the fp16 number n 2^-24, exactly (a subnormal), and one in the next four bits is 16 times
 // that: so one mask takes two codes to two halves, and the factor 16 goes to the other operand (keys: channels of q) or to the
 // result (values: channels of o).  All products are fp16 with fp32 sums, whatever the type of the tensors: q is scaled by a power of two per
-// row that brings its largest element to 2^15 (bf16 elements keep their 8 bits down to 2^-29 of it, fp16 ones their 11 down to 2^-25; from 2^10 a group of
+// row that brings its largest element to 2^15 (bf16 elements keep their 8 bits down to 2^-28 of it, fp16 ones their 11 down to 2^-25; from 2^10 a group of
 // fp16 queries 2^-20 of another, on keys as much larger, took o 1.1e-3 off, from 2^15 2.5e-4, as if all were alike), and steps and middles of the values by one that follows the largest value so far (of a
 // warp's keys, all groups), 2^e above it: the range 15 step is below 2 2^e, so that 8 steps are held below 16 / 15, for their products with
 // probabilities of up to 2^15, and middles below 2^15.  So middles keep 11 bits down to 2^-29 of the largest value, which covers the normal numbers of fp16
