@@ -198,7 +198,7 @@ __device__ __forceinline__ void row_to_value_pairs(uint32_t* w, uint32_t* p, int
 //
 // Bound: HBM beside instruction issue (0.63 of a slot per cycle).  A thread takes one group, G = d / 32 neighbouring lanes a row.  16,381 tokens of
 // eight heads, d 128, keys and values: 17 us, 5.1 TB/s (25 with 16-byte accesses 64 bytes apart, a quotient checked by its remainder, and codes packed
-// one by one); read back 15 us (25).
+// one by one); read back 16 us (25).
 template <typename T>
 struct Group {
   uint32_t x[16];              // pairs of channels
@@ -515,7 +515,11 @@ __global__ void __launch_bounds__(256) tra_cache4_expand_kernel(const __grid_con
 
 // ------------------------------------------------------------------------------------ host side
 constexpr int kMaxSplits = 256, kClusterMax = 8;
-constexpr int kRowsDirect = 64;                  // rows per key/value head up to which the codes are read by the products' kernel
+// Rows per key/value head up to which the codes are read by the products' kernel; more are read back first.  40 / 8 heads, d 128, 60 and 80 rows, us, directly and
+// read back: bf16, one sequence of 30,000 keys 71 and 146, 79 and 79; 16 of 16,000 528 and 645, 492 and 493; 64 of 1,000 165 and 209, 148 and 149; 8 of 4,000 75
+// and 123, 82 and 82.  fp16: 70 and 137, 121 and 121; 516 and 632, 892 and 892; 162 and 207, 225 and 225: level at about 110 rows
+// there (more rows only repeat the reading of the codes, 16 rows at a time).
+constexpr int kRowsDirect = 64;
 constexpr size_t kExpandBytes = 512u << 20;      // keys and values read back at a time (one sequence at least)
 
 bool bad_cache(const tra_packed_t* h, const tra_cache4_t* c) {
@@ -550,7 +554,9 @@ Choice4 choose4(const tra_packed_t* h, int n_seq, int max_q, int max_k) {
     // are enough or the cache is short (see choose in tra_packed.cu).  Many units: parts of about 3,328 keys, so that blocks of different
     // lengths spread evenly, and no clusters, whose blocks start and end together (64 caches of up to 32K keys, eight heads: 510 us
     // whole, 555 in two clustered parts, 405 in two, 332 in parts of 3,328, 348 in parts of 2,048; 32 windows of 4,096 keys: 61 whole, 64
-    // to 74 in two to six).
+    // to 74 in two to six).  Parts of 2,048, 3,328, 5,120, 8,192 keys and whole, us: 64 caches of 32,768 632, 609, 607, 608, 738; 40 of up to 65,536
+    // 428, 409, 408, 420, 759; 32 of 16,384 169, 166, 179, 197, 189; 128 of up to 8,192 188, 189, 190, 202, 202; 256 of 4,096 325, 300, 309, 309, 309; 200 of up to
+    // 3,000 all 121; d 64, fp16, 12 heads, 64 of up to 32,768 335, 323, 326, 334, 429.
     const long long slots = (long long)(rows <= 8 ? 3 : 2) * h->sm_count;
     const long long units = (long long)n_seq * h->cfg.kv_heads * c.row_tiles;
     const bool many = 2 * units > slots;

@@ -21,11 +21,11 @@
 // row that brings its largest element to 2^15 (bf16 elements keep their 8 bits down to 2^-28 of it, fp16 ones their 11 down to 2^-25; from 2^10 a group of
 // fp16 queries 2^-20 of another, on keys as much larger, took o 1.1e-3 off, from 2^15 2.5e-4, as if all were alike), and steps and middles of the values by one that follows the largest value so far (of a
 // warp's keys, all groups), 2^e above it: the range 15 step is below 2 2^e, so that 8 steps are held below 16 / 15, for their products with
-// probabilities of up to 2^15, and middles below 2^15.  So middles keep 11 bits down to 2^-29 of the largest value, which covers the normal numbers of fp16
-// tensors; bf16 values further apart than that lose bits.  (Middles held below 1.5: values of 0.01 were 0.08 to 0.25 of their norm off beside one of 6e4 that the
+// probabilities of up to 2^15, and middles below 2^15.  So middles keep 11 bits down to 2^-29 of 2^e, which covers fp16's normal numbers beside values of up
+// to 2^15; bf16 values further apart than that lose bits.  (Middles held below 1.5: values of 0.01 were 0.08 to 0.25 of their norm off beside one of 6e4 that the
 // order hides; so: 2.8e-4, where the result's rounding alone makes 2.0e-4.)
 //
-// Bound: instruction issue and latency beside HBM (0.625 bytes a channel, against 2): 705 instructions per 32 keys of a head, of which a third
+// Bound: instruction issue and latency beside HBM (0.625 bytes a channel, against 2): 702 instructions per 32 keys of a head, of which a third
 // turns codes into operands; at the rate at which HBM delivers them, an SM would have to issue 3.3 of its 4 per cycle, and issues 2.3.  A
 // block is four warps that each walk pieces of 32 keys, every fourth one, through a ring of bulk copies of their own (a piece is four runs
 // of bytes): no warp waits for another before the join.  64 caches of 700 to 32,768 keys, 40 / 8 heads, d 128: 333 us, 4.1 TB/s (63 % of the copy rate; the cache

@@ -478,7 +478,9 @@ extern "C" int tra_packed_attn_backward(const tra_packed_t* h, const tra_packed_
   }
   // Sequences that the window hides nothing of take the window's kernels too, whose dq has second pieces of dS (dq_tiles_block): 1.2 times the error of
   // rounding dq alone, against 1.51 to 1.53 at d 64, where it costs nothing over long sequences (four of 8,190 tokens: 1.89 ms, causal order 1.90), and
-  // up to 1.58 over a few keys.  Not long ones at d 128 (four of 4,096 tokens, 40 / 8 heads: 2.25 ms against 1.94 for 1.49 times; 64 of 300: 0.52, 0.60).
+  // up to 1.58 over a few keys.  Not long ones at d 128 (40 / 8 heads, the window's kernels and the others: four of
+  // 4,096 tokens 2.40 ms and 2.20, eight of 2,048 1.43 and 1.27, ten of 1,536 1.10 and 1.02, 16 of 1,024 0.87 and 0.84, 32 of 512 0.58 and 0.62, 54 of 300 0.45 and 0.51;
+  // 16 heads: 1,035 us and 939, 641 and 565, 505 and 441, 412 and 374, 300 and 297, 361 and 355).  (Precision sets the border: rows of few keys need it.)
   if (h->cfg.window > 0 && p.order == kOrderCausal && (h->cfg.head_dim == 64 || p.max_k <= 1024))
     p.order = kOrderWindow, p.window = 1 << 30, p.sinks = p.sink_rows = 0;
   p.stream_rows = backward_stream_rows(h);
