@@ -535,8 +535,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1) tra_packed_fwd_kernel(const __
           __syncwarp();
         }
       } else {
-        // (never 0, which would make NaN of masked columns: products of multiples are below 2^37, so that 2^-126 of them is nothing)
-        const float scale_log2 = kPieces == 0 ? fmaxf(p.sm_scale * kLog2e * row_mul, 0x1p-126f) : p.sm_scale * kLog2e;
+        // (never 0, which would make NaN of masked columns: products of multiples are below 2^37, so that 2^-126 of them is nothing; nor infinite, which
+        // would of scores of 0: other products of multiples are above 2^-49, and infinite all the same)
+        const float scale_log2 = kPieces == 0 ? fminf(fmaxf(p.sm_scale * kLog2e * row_mul, 0x1p-126f), 0x1.fffffep127f) : p.sm_scale * kLog2e;
         for (int e = 0; e < n; ++e, col_limit -= kKeyTile) {
           if (!mbar_wait_warp(smem_u32(&ctl->s_full[k]), entries & 1u, abort_flag, p.status)) {
             alive = false;

@@ -12,7 +12,7 @@ the smallest fp16 number is 2^-38 of it; rounded to 0, a number is off by itself
     are below 2 top; P times the step, max (h P step, 2^-40 top) |code - 8| (steps held times 8 in the same scale);
   - per key: the exponent, P |v - o| times d + 16 additions of one unit 2^-23 of scale sum |q| (|low| + 15 step), and 2^-21 of ex2.
 Many rows: P in numerator and denominator, max (h P, 2^-25) |v - o| (of at most 2^8); the values' fp16 multiples in bf16, max (h |v|, 2^-38 top) P; the
-exponent, in bf16 with the keys' multiples, scale |q k| h over the channels, and 2^-38 of the largest.  fp16 values in two pieces are off by h^2.
+exponent, in bf16 with the keys' multiples, which are off by max (h |k|, 2^-38 of the largest) and by |k| at most.  fp16 values in two pieces are off by h^2.
 The sums themselves (`sums`): `terms` additions, one unit 2^-23 each of what is summed, which need not average out."""
 import math
 
@@ -45,7 +45,8 @@ def attention(q, k, v, window=0, sinks=0, scale=None, many=False, terms=None):
         o = p @ V
         e = scale * (Q.abs() @ Ks.T) * (d + 16) * UNIT + 2.0 ** -21
         if many and q.dtype == torch.bfloat16:
-            e = (e ** 2 + (scale * H) ** 2 * (Q ** 2 @ (K ** 2).T) + (scale * 2.0 ** -38 * k_top) ** 2 * (Q ** 2).sum(-1, keepdim=True)).sqrt()
+            off = torch.minimum(torch.clamp_min(H * K.abs(), 2.0 ** -38 * k_top), K.abs())
+            e = (e ** 2 + scale ** 2 * (Q ** 2 @ (off ** 2).T)).sqrt()
         flat = lambda x: x.expand(m, d // GROUP, GROUP).flatten(-2)
         around = lambda w: w @ V ** 2 - 2 * o * (w @ V) + o ** 2 * w.sum(-1, keepdim=True)       # sum of w (v - o)^2
         square = torch.clamp_min(u * o.abs(), least) ** 2 + around((p * e) ** 2)

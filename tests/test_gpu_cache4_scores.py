@@ -51,3 +51,13 @@ def test_the_largest_queries(api, nq):
     want = values(v[5, 0])
     # P is 1: the result's rounding, and that of the middle and of the step in fp16
     assert ((o - want).abs() <= 2.0 ** -8 * want.abs() + 2 * 2.0 ** -11 * v.abs().max() * 2).all()
+
+
+@pytest.mark.parametrize("nq", [1, 3, 70])
+@pytest.mark.parametrize("size", [1e20, 1e36])
+def test_large_keys_that_large_queries_do_not_meet(api, nq, size):
+    """Queries in one group of channels, keys in the other: every score is 0, and o the mean of the values seen."""
+    m, d = 200, 64
+    q, k, v = randn((nq, 2, d), BF, 1, size), randn((m, 1, d), BF, 2, size), randn((m, 1, d), BF, 3)
+    q[..., 32:], k[..., :32] = 0.0, 0.0
+    check_norm(attend(api, q, k, v), attention(q, k, v, many=nq * 2 > 64), "o")
