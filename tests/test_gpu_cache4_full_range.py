@@ -2,8 +2,9 @@
 import pytest
 import torch
 
-from tests.cache4_reference import values
-from tests.packed_reference import i32
+from tests.cache4_norms import attention, check_norm
+from tests.cache4_reference import attention as elements, values
+from tests.packed_reference import check, i32, randn
 from tests.test_gpu_cache4_values import attend
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +51,21 @@ def test_many_rows_of_values_past_the_largest_number(api):
     want = values(v).mean(0)
     assert values(v).max() > 1.01 * most
     assert ((o.double() - want).abs() <= (2.0 ** -9 + 2.0 ** -11) * want.abs() * (1 + 2.0 ** -8)).all()
+
+
+@pytest.mark.parametrize("nq,window,sinks", [(1, 0, 0), (3, 0, 0), (3, 100, 5), (70, 0, 0)])
+@pytest.mark.parametrize("m", [300, 20000])
+@pytest.mark.parametrize("size", [2e37, 1e30, 1e-30])
+def test_sums_of_large_and_small_values(api, size, m, nq, window, sinks):
+    """Sums over many keys, in clusters and in parts, of values whose sum is past fp32's largest number, or next to its smallest."""
+    d, hq, hk = 64, 4, 2
+    q, k, v = randn((nq, hq, d), BF, 1), randn((m, hk, d), BF, 2), randn((m, hk, d), BF, 3, size)
+    attn = api.PackedAttn(hq, hk, d, window=window, sinks=sinks)
+    cache = api.Cache4(attn, m)
+    cache.write(k, v, torch.arange(m, dtype=torch.int32, device="cuda"))
+    o, lse = attn.forward_cache4(q, cache, i32([0, nq]), k_range=(i32([0]), i32([m])), max_q=nq, max_k=m, want_lse=True)
+    attn.check_status()
+    many = nq * hq // hk > 64
+    check_norm(o, attention(q, k, v, window, sinks, many=many, terms=128), "o")
+    want = elements(q, k, v, [0, nq], [0], [m], window, sinks, d ** -0.5, many)
+    check(lse, want["lse"], want["lse_tol"], "lse")
